@@ -7,8 +7,9 @@
   spmm8    Y = act(W X + bias) of such a layer, X quantised on the way with a scale for each 128 of a column (HybridLayer.spmm8)
 
 Both 8-bit formats hold x as code * 2^E, with the smallest E that lets the largest value of the block be held.  Weights and activations are rounded
-to the nearest e4m3 (even at ties).  Optimizer states (m: sign and e4m3; sqrt(v): e4m4 without sign) and bf16 weights are rounded up where 16 bits
-of a hash of (seed, step, tensor, element) say so, and sqrt(v) > 0 is never held as 0.
+to the nearest e4m3 (even at ties).  Optimizer states (m: sign and e4m3; sqrt(v): e4m4 without sign) and bf16 weights are rounded at random: up where
+the part below the code, plus an odd multiple of 2^-11 (m) or 2^-12 from a hash of (seed, step, tensor, element), reaches one.  sqrt(v) > 0 is never
+held as 0.
 """
 import math
 
@@ -185,8 +186,8 @@ def _prepare_adamw(case, seed, rng, randn):
     if case["bits"] == 32:
         state["m"], state["v"] = m, root * root
     else:
-        half = torch.full((total,), 0x8000, dtype=torch.int32, device="cuda")
-        state["m"], state["m_exp"] = _round_state(m, half, False)
+        half = torch.full((total,), 1 << 18, dtype=torch.int32, device="cuda")
+        state["m"], state["m_exp"] = _round_state(m, half * 2, False)
         state["v"], state["v_exp"] = _round_state(root, half, True)
     if own:
         from paper_2311_14272_b200 import binding as B
@@ -251,14 +252,15 @@ def _hash(seed, step, tensor, index):
 
 
 def _round_state(x, random, root):
-    """Codes (uint8) and biased exponents (uint8, one for each 128) of a flat state; random: 16 bits an element.  root: e4m4 without a sign, not 0."""
+    """Codes (uint8) and biased exponents (uint8, one for each 128) of a flat state; random: an integer an element, in units of the last bit of the 20
+    (root: 19) below the code.  root: e4m4 without a sign, not 0."""
     blocks, random = x.view(-1, 128), random.view(-1, 128)
     e = _scale_exponent(blocks.abs().amax(1, keepdim=True), 496.0 if root else 448.0)
     bits = (blocks.abs() * _power(-e) * 2.0**-120).view(torch.int32)       # exponent field as the code has it, 19 or 20 bits of fraction below
     if root:
-        codes = torch.where(blocks > 0, ((bits + (random << 3)) >> 19).clamp(min=1), 0)
+        codes = torch.where(blocks > 0, ((bits + random) >> 19).clamp(min=1), 0)
     else:
-        codes = ((bits + (random << 4)) >> 20) | torch.where(blocks < 0, 128, 0)
+        codes = ((bits + random) >> 20) | torch.where(blocks < 0, 128, 0)
     return codes.to(torch.uint8).view(-1), (e + 127).to(torch.uint8).view(-1)
 
 
@@ -286,15 +288,15 @@ def _plain_adamw(s):
         s["copy"].copy_(w)
         out = [s["w"], s["copy"]]
     else:
-        up = (_mix(h ^ 0x9E3779B9) & 0xFFFF).int()
+        up = (((h >> 21) << 5) + 16).int()
         s["w"].copy_(((w.view(torch.int32) + up) & -65536).view(torch.float32))
         out = [s["w"]]
     if not narrow:
         s["m"].copy_(m)
         s["v"].copy_(v)
         return out + [s["m"], s["v"]]
-    s["m"], s["m_exp"] = _round_state(m, (h & 0xFFFF).int(), False)
-    s["v"], s["v_exp"] = _round_state(v.sqrt(), (h >> 16).int(), True)
+    s["m"], s["m_exp"] = _round_state(m, (((h & 0x3FF) << 10) + 512).int(), False)
+    s["v"], s["v_exp"] = _round_state(v.sqrt(), (((h >> 10 & 0x7FF) << 8) + 128).int(), True)
     return out + [_state_values(s["m"], s["m_exp"], False).bfloat16(), _state_values(s["v"], s["v_exp"], True).bfloat16()]
 
 
@@ -394,10 +396,10 @@ def _exact_adamw(s):
     else:
         _, exponent = torch.frexp(w)
         spacing = torch.exp2((exponent - 1).double() - 7)
-        out = [torch.sign(w) * torch.floor(w.abs() / spacing + (spread(h ^ 0x9E3779B9) % 65536).double() / 65536) * spacing]
+        out = [torch.sign(w) * torch.floor(w.abs() / spacing + (2 * (h // 2**21) + 1).double() / 4096) * spacing]
     if not narrow:
         return out + [m, v]
-    return out + [_exact_blocks(m, (h % 65536).double() / 65536, False), _exact_blocks(torch.sqrt(v), (h // 65536).double() / 65536, True)]
+    return out + [_exact_blocks(m, (2 * (h % 1024) + 1).double() / 2048, False), _exact_blocks(torch.sqrt(v), (2 * (h // 1024 % 2048) + 1).double() / 4096, True)]
 
 
 def exact(case, seed):
