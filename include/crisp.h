@@ -321,6 +321,63 @@ CRISP_API crisp_status_t crisp_prune_encode_sizes(int32_t n_layers, const crisp_
 CRISP_API crisp_status_t crisp_prune_encode(int32_t n_layers, const crisp_prune_layer_t *layers, void *stream,
                                             crisp_mask_t *masks, crisp_handle_t *handles);
 
+/*
+ * Fine-tuning (Algorithm 1, "fine-tune the pruned model"; the paper trains with SGD and gives no formula of its own):
+ * one AdamW step over all tensors of a network,
+ *
+ *   g = grad * grad_scale        m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
+ *   w = w (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
+ *
+ * in fp32, element by element.  Where a tensor's mask has no bit, w, m and v become 0, whatever the gradient is there (a mask of
+ * NULL updates every weight: the dense update of the straight-through estimator).  Weights are fp32, or bf16 rounded at random (below); an
+ * fp32 weight may have a bf16 copy (nearest even), the input of crisp_encode.
+ *
+ * state_bits 32: d_m, d_v are fp32 [rows * k].  state_bits 8: one byte an element, and one byte of scale for each 128 consecutive
+ * elements of the tensor (rows * k of them in order, the last block may be shorter).  Element e is held as
+ *   m        d_m[e] = sign, 4 bits of exponent, 3 of fraction (e4m3, bias 7)      times 2^(d_m_exp[e / 128] - 127)
+ *   sqrt(v)  d_v[e] = 4 bits of exponent, 4 of fraction (bias 7, no sign)         times 2^(d_v_exp[e / 128] - 127)
+ * with the smallest scale, 2^-126 at least, under which the block's largest value is at most 448 (m) or 496 (sqrt(v)).  All zero bytes are a
+ * state of zeros.  Values are rounded up where the fraction that the code cannot hold plus a pseudo-random number from (0, 1) reaches
+ * one, and down elsewhere: rounded to nearest, an average that moves by less than half a step (1/16 and 1/32 of the value, while beta2 =
+ * 0.999 moves v by a thousandth) would stand still.  The number comes from a hash of seed, step, the tensor's place in the
+ * call and e, so a step's result does not depend on the launch.  A sqrt(v) above 0 is never held as 0 (m / eps would follow).
+ * An element that is not finite is held as 0 and leaves its block's scale alone; its weight is not finite from then on.
+ *
+ * `tensors` is read before the call returns.  Two entries must not share weights or state.  d_grad = NULL leaves a tensor as
+ * it is.  n = 0 and tensors without elements are fine.  The scalars are those of the call; a step that is captured into a graph takes what
+ * changes from one replay to the next from device memory (d_lr, d_step, read when the kernel runs).  Weights and gradients may
+ * lie at any address of their type; rows that are not packed or aligned to 16 bytes are slower.  Errors: INVALID_ARG for null or misaligned pointers, a scalar out
+ * of its range, a tensor twice, a mask of another shape (BAD_SHAPE).
+ */
+typedef struct {
+    int64_t rows, k;                  /* rows * k elements; k consecutive ones in a row of w, copy and grad   */
+    void *d_w; int64_t ld_w;
+    int32_t w_dtype, grad_dtype;      /* 0 bf16, 1 fp32                                                       */
+    uint16_t *d_copy_bf16; int64_t ld_copy;      /* NULL: none.  Only with fp32 weights                       */
+    const void *d_grad; int64_t ld_grad;
+    void *d_m, *d_v;                  /* state, packed, 16-byte aligned                                       */
+    uint8_t *d_m_exp, *d_v_exp;       /* state_bits 8: [ceil(rows * k / 128)]                                 */
+    crisp_mask_t mask;                /* of a layer of this shape, or NULL                                    */
+} crisp_adamw_tensor_t;
+
+typedef struct {
+    double lr, beta1, beta2, eps, weight_decay;      /* beta1, beta2 in [0, 1), the others finite, eps >= 0   */
+    int64_t step;                     /* of this call, from 1                                                 */
+    uint64_t seed;
+    int32_t state_bits;               /* 32 or 8                                                              */
+    int32_t reserved;                 /* 0                                                                    */
+    const float *d_lr;                /* device, or NULL: lr above                                            */
+    const int64_t *d_step;            /* device, or NULL: step above                                          */
+    const float *d_grad_scale;        /* device, or NULL: 1 (gradient clipping, loss scaling)                 */
+} crisp_adamw_t;
+
+CRISP_API crisp_status_t crisp_adamw(int32_t n, const crisp_adamw_tensor_t *tensors, const crisp_adamw_t *params, void *stream);
+
+/* What 8-bit states stand for: d_m_bf16[e] = m and d_root_bf16[e] = sqrt(v) of `count` elements of one tensor, or of several whose states lie one
+ * behind the other in whole blocks of 128 (both are exact in bf16).  d_m, d_v 16-byte aligned. */
+CRISP_API crisp_status_t crisp_adamw_moments(const uint8_t *d_m, const uint8_t *d_m_exp, const uint8_t *d_v, const uint8_t *d_v_exp,
+                                             int64_t count, uint16_t *d_m_bf16, uint16_t *d_root_bf16, void *stream);
+
 /* Copy the mask to host: h_blk_col [nrt*kkeep] int32, h_nm_bits [nrt*block_rows *
  * nblk*block_k/32] uint32.  Either may be NULL.  Synchronises `stream`. */
 CRISP_API crisp_status_t crisp_mask_export(crisp_mask_t mask, int32_t *h_blk_col, uint32_t *h_nm_bits,

@@ -39,6 +39,18 @@ class PruneLayer(C.Structure):
                 ("d_canonical_buf", C.c_void_p), ("d_exec_buf", C.c_void_p)]
 
 
+class AdamwTensor(C.Structure):
+    _fields_ = [("rows", C.c_int64), ("k", C.c_int64), ("d_w", C.c_void_p), ("ld_w", C.c_int64), ("w_dtype", C.c_int32), ("grad_dtype", C.c_int32),
+                ("d_copy_bf16", C.c_void_p), ("ld_copy", C.c_int64), ("d_grad", C.c_void_p), ("ld_grad", C.c_int64), ("d_m", C.c_void_p),
+                ("d_v", C.c_void_p), ("d_m_exp", C.c_void_p), ("d_v_exp", C.c_void_p), ("mask", C.c_void_p)]
+
+
+class AdamwParams(C.Structure):
+    _fields_ = [("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double), ("eps", C.c_double), ("weight_decay", C.c_double),
+                ("step", C.c_int64), ("seed", C.c_uint64), ("state_bits", C.c_int32), ("reserved", C.c_int32), ("d_lr", C.c_void_p),
+                ("d_step", C.c_void_p), ("d_grad_scale", C.c_void_p)]
+
+
 class ConvDesc(C.Structure):
     _fields_ = [("batch", C.c_int32), ("height", C.c_int32), ("width", C.c_int32), ("channels", C.c_int32),
                 ("kernel_h", C.c_int32), ("kernel_w", C.c_int32), ("pad", C.c_int32), ("y_layout", C.c_int32)]
@@ -176,6 +188,8 @@ def load(path: Optional[str] = None):
         "crisp_prune_encode": [i32, P(PruneLayer), vp, P(vp), P(vp)],
         "crisp_destroy_layers": [i32, P(vp), P(vp)],
         "crisp_global_rank": [i32, P(RankLayer), C.c_double, vp, vp, vp],
+        "crisp_adamw": [i32, P(AdamwTensor), P(AdamwParams), vp],
+        "crisp_adamw_moments": [vp, vp, vp, vp, i64, vp, vp, vp],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -355,6 +369,16 @@ def crisp_prune_encode(layers, stream=None):
     m, h = (C.c_void_p * len(layers))(), (C.c_void_p * len(layers))()
     _check(load().crisp_prune_encode(len(layers), layers, _stream(stream), m, h), "crisp_prune_encode")
     return list(m), list(h)
+
+
+def crisp_adamw(tensors, params: AdamwParams, stream=None):
+    """tensors: ctypes array of AdamwTensor."""
+    _check(load().crisp_adamw(len(tensors), tensors, C.byref(params), _stream(stream)), "crisp_adamw")
+
+
+def crisp_adamw_moments(d_m, d_m_exp, d_v, d_v_exp, count: int, d_m_bf16, d_root_bf16, stream=None):
+    _check(load().crisp_adamw_moments(_ptr(d_m), _ptr(d_m_exp), _ptr(d_v), _ptr(d_v_exp), count, _ptr(d_m_bf16), _ptr(d_root_bf16),
+                                      _stream(stream)), "crisp_adamw_moments")
 
 
 def crisp_build_mask(d_saliency, ld_s: int, desc: LayerDesc, d_mask_buf, d_workspace, stream=None) -> int:
@@ -835,6 +859,123 @@ class PruningNetwork:
         crisp_destroy_layers(old_masks, old_handles)
         return kk
 
+    def optimizer(self, weights, **options):
+        """AdamW for this network's weights, which are held where the layers' masks have no bit to zero: weights[l] is what `step` prunes
+        or, fp32, what it was rounded from (then with copies=: the bf16 tensors that `step` takes).  Options as for AdamW.  The masks are those that the
+        layers have when the optimizer's step is called; a layer without one is updated everywhere."""
+        return AdamW(weights, masks=self.layers, **options)
+
     def close(self):
         for L in self.layers:
             L.close()
+
+
+def _rows_of(t):
+    """(rows, k, pitch) of a tensor whose elements lie in rows of consecutive ones, or None."""
+    shape, strides = t.shape, t.stride()
+    if len(shape) == 0 or 0 in shape:
+        return (1, t.numel(), t.numel())
+    if t.is_contiguous():
+        k = t.numel() // shape[0]
+        return (shape[0], k, k) if len(shape) > 1 else (1, shape[0], shape[0])
+    if len(shape) == 2 and (strides[1] == 1 or shape[1] == 1) and strides[0] >= shape[1]:
+        return (shape[0], shape[1], strides[0])
+    return None
+
+
+class AdamW:
+    """AdamW over many tensors in one call (crisp_adamw): the fine-tuning that follows a pruning step.
+
+    weights   CUDA tensors, fp32 or bf16, contiguous or matrices of consecutive rows; updated in place (bf16 ones are rounded at random)
+    copies    bf16 tensors of the same shapes, or None for none: what fp32 weights are rounded to after every step
+    masks     for each tensor None, or a HybridLayer of its shape (or a crisp_mask_t): weights without a bit in its mask become and stay 0
+    state_bits 32, or 8 with a scale for each 128 elements.  The states of all tensors lie in the flat buffers m and v, each beginning at a multiple
+              of 128 elements (`starts`): fp32 m and v, or uint8 codes of m and sqrt(v) with biased exponents in m_exp and v_exp (crisp.h).  They,
+              `step_count` and `seed` are all there is to save.
+    capturable  the step number is kept in device memory (`d_step`, counted up by every step), and so may lr be (`d_lr`): a captured step
+              goes on counting when it is replayed.
+    """
+
+    def __init__(self, weights, copies=None, masks=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, seed=0, step=0,
+                 capturable=False):
+        import torch
+        self.torch = torch
+        self.weights = list(weights)
+        n = len(self.weights)
+        self.copies = [None] * n if copies is None else list(copies)
+        self.masks = [None] * n if masks is None else list(masks)
+        assert len(self.copies) == n and len(self.masks) == n, "a copy and a mask, or None, for each tensor"
+        assert state_bits in (8, 32), "states are held in 8 bits or in 32"
+        self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
+        self.state_bits, self.seed, self.step_count = state_bits, seed, step
+        self.device = self.weights[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        self._table = (AdamwTensor * n)()
+        self.starts, at = [], 0
+        for w in self.weights:
+            self.starts.append(at)
+            at += (w.numel() + 127) // 128 * 128
+        self.elements = at
+        wide = state_bits == 32
+        state = lambda count, dtype: torch.zeros(count, dtype=dtype, device=self.device)  # noqa: E731
+        self.m, self.v = [state(at, torch.float32 if wide else torch.uint8) for _ in range(2)]
+        self.m_exp, self.v_exp = [None if wide else state(at // 128, torch.uint8) for _ in range(2)]
+        self._shapes, spans = [], []
+        for i, (T, w, c) in enumerate(zip(self._table, self.weights, self.copies)):
+            rows = _rows_of(w)
+            assert w.is_cuda and w.device == self.device and w.dtype in (torch.float32, torch.bfloat16) and rows, \
+                "weights are fp32 or bf16 CUDA tensors of one device, in rows of consecutive elements"
+            T.rows, T.k, T.ld_w = rows
+            T.d_w, T.w_dtype = w.data_ptr(), int(w.dtype == torch.float32)
+            if c is not None:
+                there = _rows_of(c)
+                assert c.is_cuda and c.device == self.device and c.dtype == torch.bfloat16 and T.w_dtype and c.shape == w.shape and there, \
+                    "a copy is a bf16 CUDA tensor of the shape of its fp32 weights"
+                T.d_copy_bf16, T.ld_copy = c.data_ptr(), there[2] if there[0] == T.rows else T.k
+            T.d_m, T.d_v = (b.data_ptr() + self.starts[i] * b.element_size() for b in (self.m, self.v))
+            if not wide:
+                T.d_m_exp, T.d_v_exp = (b.data_ptr() + self.starts[i] // 128 for b in (self.m_exp, self.v_exp))
+            self._shapes.append(w.shape)
+            for t in (w, c):
+                if t is not None and t.numel():
+                    spans.append((t.data_ptr(), t.data_ptr() + (sum((s - 1) * d for s, d in zip(t.shape, t.stride())) + 1) * t.element_size()))
+        spans.sort()
+        assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])), "weights or copies lie on one another"
+        self.capturable = capturable
+        self.d_step = torch.full((1,), step, dtype=torch.int64, device=self.device) if capturable else None
+        self.d_lr = torch.full((1,), lr, dtype=torch.float32, device=self.device) if capturable else None
+
+    def step(self, grads, grad_scale=None, stream=None):
+        """One step with grads[i] (bf16 or fp32, of the shape of weights[i], in rows of consecutive elements; None: the tensor is left as it is);
+        grad_scale: an fp32 CUDA tensor of one element that the gradients are multiplied by (a clipping factor, say)."""
+        torch = self.torch
+        assert len(grads) == len(self._table), "a gradient, or None, for each tensor"
+        for T, g, shape, mask in zip(self._table, grads, self._shapes, self.masks):
+            if g is None:
+                T.d_grad = None
+                continue
+            assert g.is_cuda and g.device == self.device and g.dtype in (torch.float32, torch.bfloat16) and g.shape == shape, \
+                "a gradient is a bf16 or fp32 CUDA tensor of its weights' shape"
+            rows = _rows_of(g)
+            assert rows, "a gradient lies in rows of consecutive elements"
+            T.d_grad, T.grad_dtype, T.ld_grad = g.data_ptr(), int(g.dtype == torch.float32), rows[2]
+            T.mask = getattr(mask, "mask", mask) or None
+        p = AdamwParams(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, self.step_count + 1, self.seed, self.state_bits, 0)
+        if grad_scale is not None:
+            assert grad_scale.is_cuda and grad_scale.device == self.device and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1
+            p.d_grad_scale = grad_scale.data_ptr()
+        with torch.cuda.device(self.device):
+            if self.capturable:
+                p.d_step, p.d_lr = self.d_step.data_ptr(), self.d_lr.data_ptr()
+                with torch.cuda.stream(stream):
+                    self.d_step += 1
+            crisp_adamw(self._table, p, stream)
+        self.step_count += 1
+        return self
+
+    def moments(self, stream=None):
+        """(m, sqrt(v)) of 8-bit states as flat bf16 tensors, in which they are exact."""
+        assert self.state_bits == 8, "32-bit states are their values"
+        out = [self.torch.empty(self.elements, dtype=self.torch.bfloat16, device=self.device) for _ in range(2)]
+        with self.torch.cuda.device(self.device):
+            crisp_adamw_moments(self.m, self.m_exp, self.v, self.v_exp, self.elements, *out, stream)
+        return out
