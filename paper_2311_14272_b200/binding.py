@@ -254,6 +254,11 @@ def _bind_current_stream():
 _current_stream = _bind_current_stream
 
 
+def _current_device() -> int:
+    import torch
+    return torch.cuda.current_device()
+
+
 def _stream(stream) -> int:
     if stream is None:
         return _current_stream()
@@ -910,6 +915,7 @@ class AdamW:
         self.state_bits, self.seed, self.step_count = state_bits, seed, step
         self.device = self.weights[0].device if n else torch.device("cuda", torch.cuda.current_device())
         self._table = (AdamwTensor * n)()
+        self._address = C.addressof(self._table)
         self.starts, at = [], 0
         for w in self.weights:
             self.starts.append(at)
@@ -919,58 +925,85 @@ class AdamW:
         state = lambda count, dtype: torch.zeros(count, dtype=dtype, device=self.device)  # noqa: E731
         self.m, self.v = [state(at, torch.float32 if wide else torch.uint8) for _ in range(2)]
         self.m_exp, self.v_exp = [None if wide else state(at // 128, torch.uint8) for _ in range(2)]
-        self._shapes, spans = [], []
+        spans = []
         for i, (T, w, c) in enumerate(zip(self._table, self.weights, self.copies)):
             rows = _rows_of(w)
-            assert w.is_cuda and w.device == self.device and w.dtype in (torch.float32, torch.bfloat16) and rows, \
-                "weights are fp32 or bf16 CUDA tensors of one device, in rows of consecutive elements"
-            T.rows, T.k, T.ld_w = rows
-            T.d_w, T.w_dtype = w.data_ptr(), int(w.dtype == torch.float32)
-            if c is not None:
-                there = _rows_of(c)
-                assert c.is_cuda and c.device == self.device and c.dtype == torch.bfloat16 and T.w_dtype and c.shape == w.shape and there, \
-                    "a copy is a bf16 CUDA tensor of the shape of its fp32 weights"
-                T.d_copy_bf16, T.ld_copy = c.data_ptr(), there[2] if there[0] == T.rows else T.k
+            assert rows and w.dtype in (torch.float32, torch.bfloat16), "weights are fp32 or bf16 CUDA tensors, in rows of consecutive elements"
+            (T.rows, T.k, _), T.w_dtype = rows, int(w.dtype == torch.float32)
+            self._place(T, w, c)
             T.d_m, T.d_v = (b.data_ptr() + self.starts[i] * b.element_size() for b in (self.m, self.v))
             if not wide:
                 T.d_m_exp, T.d_v_exp = (b.data_ptr() + self.starts[i] // 128 for b in (self.m_exp, self.v_exp))
-            self._shapes.append(w.shape)
             for t in (w, c):
                 if t is not None and t.numel():
                     spans.append((t.data_ptr(), t.data_ptr() + (sum((s - 1) * d for s, d in zip(t.shape, t.stride())) + 1) * t.element_size()))
         spans.sort()
         assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])), "weights or copies lie on one another"
+        load()
+        if _network is None:
+            _bind_network()
+        self._params = AdamwParams(state_bits=state_bits)
         self.capturable = capturable
         self.d_step = torch.full((1,), step, dtype=torch.int64, device=self.device) if capturable else None
         self.d_lr = torch.full((1,), lr, dtype=torch.float32, device=self.device) if capturable else None
+        if capturable:
+            self._params.d_step, self._params.d_lr = self.d_step.data_ptr(), self.d_lr.data_ptr()
+
+    def _place(self, T, w, c):
+        """Where a tensor's weights and their copy lie."""
+        torch, rows = self.torch, _rows_of(w)
+        assert w.is_cuda and w.device == self.device and rows and rows[:2] == (T.rows, T.k) and w.dtype == (torch.float32 if T.w_dtype else torch.bfloat16), \
+            "weights are CUDA tensors of one device and keep their shape and type"
+        T.d_w, T.ld_w = w.data_ptr(), rows[2]
+        if c is not None:
+            rows = _rows_of(c)
+            assert c.is_cuda and c.device == self.device and c.dtype == torch.bfloat16 and T.w_dtype and c.shape == w.shape and rows, \
+                "a copy is a bf16 CUDA tensor of the shape of its fp32 weights"
+            T.d_copy_bf16, T.ld_copy = c.data_ptr(), rows[2]
 
     def step(self, grads, grad_scale=None, stream=None):
         """One step with grads[i] (bf16 or fp32, of the shape of weights[i], in rows of consecutive elements; None: the tensor is left as it is);
         grad_scale: an fp32 CUDA tensor of one element that the gradients are multiplied by (a clipping factor, say)."""
-        torch = self.torch
         assert len(grads) == len(self._table), "a gradient, or None, for each tensor"
-        for T, g, shape, mask in zip(self._table, grads, self._shapes, self.masks):
+        if not (_network and type(grads) is list and _network.gradients(self._address, self.weights, self.copies, grads, self.masks)):
+            self._gradients(grads)
+        p = self._params
+        p.lr, (p.beta1, p.beta2), p.eps, p.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
+        p.step, p.seed = self.step_count + 1, self.seed
+        if grad_scale is not None:
+            assert grad_scale.is_cuda and grad_scale.device == self.device and grad_scale.dtype is self.torch.float32 and grad_scale.numel() == 1, \
+                "grad_scale is an fp32 CUDA tensor of one element"
+        p.d_grad_scale = grad_scale.data_ptr() if grad_scale is not None else None
+        if self.device.index == _current_device():
+            self._launch(p, stream)
+        else:
+            with self.torch.cuda.device(self.device):
+                self._launch(p, stream)
+        self.step_count += 1
+        return self
+
+    def _launch(self, p, stream):
+        if self.capturable:
+            with self.torch.cuda.stream(stream):
+                self.d_step += 1
+        code = _lib.crisp_adamw(len(self._table), self._table, p, _stream(stream))
+        if code:
+            raise CrispError(code, "crisp_adamw")
+
+    def _gradients(self, grads):
+        """Fills in what a step's gradients and masks bring, or says what is wrong with them."""
+        torch = self.torch
+        for T, g, w, c, mask in zip(self._table, grads, self.weights, self.copies, self.masks):
             if g is None:
                 T.d_grad = None
                 continue
-            assert g.is_cuda and g.device == self.device and g.dtype in (torch.float32, torch.bfloat16) and g.shape == shape, \
+            self._place(T, w, c)
+            assert g.is_cuda and g.device == self.device and g.dtype in (torch.float32, torch.bfloat16) and g.shape == w.shape, \
                 "a gradient is a bf16 or fp32 CUDA tensor of its weights' shape"
             rows = _rows_of(g)
             assert rows, "a gradient lies in rows of consecutive elements"
             T.d_grad, T.grad_dtype, T.ld_grad = g.data_ptr(), int(g.dtype == torch.float32), rows[2]
             T.mask = getattr(mask, "mask", mask) or None
-        p = AdamwParams(self.lr, self.betas[0], self.betas[1], self.eps, self.weight_decay, self.step_count + 1, self.seed, self.state_bits, 0)
-        if grad_scale is not None:
-            assert grad_scale.is_cuda and grad_scale.device == self.device and grad_scale.dtype == torch.float32 and grad_scale.numel() == 1
-            p.d_grad_scale = grad_scale.data_ptr()
-        with torch.cuda.device(self.device):
-            if self.capturable:
-                p.d_step, p.d_lr = self.d_step.data_ptr(), self.d_lr.data_ptr()
-                with torch.cuda.stream(stream):
-                    self.d_step += 1
-            crisp_adamw(self._table, p, stream)
-        self.step_count += 1
-        return self
 
     def moments(self, stream=None):
         """(m, sqrt(v)) of 8-bit states as flat bf16 tensors, in which they are exact."""

@@ -81,39 +81,45 @@ __device__ __forceinline__ float from_bf16(uint16_t b) { return __uint_as_float(
 __device__ __forceinline__ uint16_t nearest(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
 
 // The 8-bit forms.  A code is the top of an fp32 number whose exponent field has been brought down by 120 (127 - 7), so that small codes are
-// subnormal as fp32's are: reading is a shift and a product by 2^120, rounding an addition to the bits below the code.
+// subnormal as fp32's are: reading sqrt(v) is a shift and a product by 2^120, rounding an addition to the bits below the code.
 __device__ __forceinline__ float power_of(uint32_t biased) { return __uint_as_float(biased << 23); }       // 2^(biased - 127), 0 for 0
-__device__ __forceinline__ float value_m(uint32_t code, float scale) {
-    return __uint_as_float(((code & 0x7Fu) << 20) | ((code & 0x80u) << 24)) * 0x1p120f * scale;
+// One power of two for both factors, 2^120 and the scale; the product of the two exponents' rest, beyond fp32's range, is `beyond` (1 for scales up to 2^7).
+__device__ __forceinline__ float power_120(uint32_t biased, float *beyond) {
+    const uint32_t near = min(biased, 134u);
+    *beyond = power_of(127u + biased - near);
+    return power_of(near + 120u);
 }
-__device__ __forceinline__ float value_root(uint32_t code, float scale) { return __uint_as_float(code << 19) * 0x1p120f * scale; }
-// Biased exponent of the scale under which `largest` (bits of a value >= 0) is at most 448 (`fraction` 0x600000) or 496 (0x780000).
-__device__ __forceinline__ uint32_t scale_of(uint32_t largest, uint32_t fraction) {
-    const int e = (int)(largest >> 23) - 8 + ((largest & 0x7FFFFFu) > fraction ? 1 : 0);
-    return (uint32_t)max(e, 1);
+__device__ __forceinline__ float root_bits(uint32_t codes, int byte) {                                       // code << 19 as fp32
+    return __uint_as_float(__byte_perm(codes, 0, 0x0444 | (uint32_t)byte << 12) >> 5);
 }
-__device__ __forceinline__ uint32_t max_of_block(uint32_t v) {                                              // over the 16 lanes of a block
+__device__ __forceinline__ float2 values_m(uint32_t codes, int pair) {                                       // two e4m3 codes
+    const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes >> (16 * pair)), __NV_E4M3);
+    return __half22float2(__half2(h));
+}
+// Biased exponent of the scale under which `largest` (bits of a value >= 0) is at most 448 (`fraction` 0x600000) or 496 (0x780000): its own exponent less 8,
+// one more where the fraction is above that one's.
+__device__ __forceinline__ uint32_t scale_of(float largest, uint32_t fraction) {
+    return (uint32_t)max((int)((__float_as_uint(largest) + (0x7FFFFFu - fraction)) >> 23) - 8, 1);
+}
+// The larger of each half over the 16 lanes of a block.
+__device__ __forceinline__ uint32_t max_of_block(uint32_t v) {
 #pragma unroll
-    for (int d = 8; d; d >>= 1) v = max(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
+    for (int d = 8; d; d >>= 1) v = __vmaxu2(v, __shfl_xor_sync(0xFFFFFFFFu, v, d));
     return v;
 }
-
-// Largest |x| of the block's 128 values as bits.  What is not finite counts as 0, and becomes 0 (rare: looked for in the block's maximum).
-__device__ __forceinline__ uint32_t largest_of_block(float (&x)[kPer]) {
-    uint32_t a = 0;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) a = max(a, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-    uint32_t all = max_of_block(a);
-    if (__any_sync(0xFFFFFFFFu, all >= 0x7F800000u)) {
-        a = 0;
-#pragma unroll
-        for (int i = 0; i < kPer; ++i) {
-            if ((__float_as_uint(x[i]) & 0x7FFFFFFFu) >= 0x7F800000u) x[i] = 0.f;
-            a = max(a, __float_as_uint(x[i]) & 0x7FFFFFFFu);
-        }
-        all = max_of_block(a);
-    }
-    return all;
+__device__ __forceinline__ float sqrt_near(float x) {          // two units of the last place, subnormal numbers too
+    float r;
+    asm("sqrt.approx.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+__device__ __forceinline__ float reciprocal_near(float x) {
+    float r;
+    asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
+    return r;
+}
+// Bit i of the byte in every bit of byte i of (lo, hi).
+__device__ __forceinline__ uint2 bytes_of_bits(uint32_t keep) {
+    return make_uint2(((keep & 15u) * 0x00204081u & 0x01010101u) * 255u, ((keep >> 4) * 0x00204081u & 0x01010101u) * 255u);
 }
 
 template <bool kNarrow, bool kW32, int CAP>
@@ -148,7 +154,7 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
     float w[kPer] = {}, g[kPer] = {}, m[kPer] = {}, v[kPer] = {};
     uint32_t keep = 0xFFu;
     uint2 mc = make_uint2(0, 0), vc = make_uint2(0, 0);
-    float m_scale = 0.f, v_scale = 0.f;
+    uint32_t m_exp = 0, v_exp = 0;
     if (vec) {
         if constexpr (kW32) load8(reinterpret_cast<const float *>(T.w) + at(T.ldw, 0), w);
         else unpack8(*reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(T.w) + at(T.ldw, 0)), w);
@@ -185,7 +191,7 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
                     (i < 4 ? vc.x : vc.y) |= (uint32_t)pv[i] << (8 * (i & 3));
                 }
         }
-        if (count) { m_scale = power_of(T.m_exp[e0 >> 7]); v_scale = power_of(T.v_exp[e0 >> 7]); }
+        if (count) { m_exp = T.m_exp[e0 >> 7]; v_exp = T.v_exp[e0 >> 7]; }
     }
     if (T.mask && count) {
         if (T.bytes) {
@@ -221,22 +227,39 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
     if (kNarrow || !kW32)
         if (e0 >> 32) spread = mix((uint32_t)(e0 >> 32) ^ key);
 
+    // Where the mask has no bit: zeros go in and zeros come out (eps is above 0).
+    if (T.mask) {
+        if constexpr (kNarrow) {
+            const uint2 b8 = bytes_of_bits(keep);
+            mc.x &= b8.x; mc.y &= b8.y; vc.x &= b8.x; vc.y &= b8.y;
+        }
+#pragma unroll
+        for (int i = 0; i < kPer; ++i)
+            if (!(keep >> i & 1u)) { w[i] = 0.f; g[i] = 0.f; m[i] = 0.f; v[i] = 0.f; }
+    }
+    float v_beyond;
+    const float m_scale = power_of(m_exp), v_scale = power_120(v_exp, &v_beyond);
+    const bool wide_scale = kNarrow && v_beyond != 1.f;
+
     uint32_t h[kPer];
-    float root[kPer];
+    float root[kPer], bad = 0.f;
 #pragma unroll
     for (int i = 0; i < kPer; ++i) {
         if constexpr (kNarrow) {
-            const uint32_t word_m = i < 4 ? mc.x : mc.y, word_v = i < 4 ? vc.x : vc.y;
-            m[i] = value_m(word_m >> (8 * (i & 3)) & 0xFFu, m_scale);
-            const float u = value_root(word_v >> (8 * (i & 3)) & 0xFFu, v_scale);
+            if ((i & 1) == 0) {
+                const float2 two = values_m(i < 4 ? mc.x : mc.y, i >> 1 & 1);
+                m[i] = two.x * m_scale; m[i + 1] = two.y * m_scale;
+            }
+            float u = root_bits(i < 4 ? vc.x : vc.y, i & 3) * v_scale;
+            if (wide_scale) u *= v_beyond;
             v[i] = u * u;
         }
         const float gi = g[i] * grad_scale;
         m[i] = s.beta1 * m[i] + s.one_beta1 * gi;
         v[i] = s.beta2 * v[i] + s.one_beta2 * gi * gi;
-        root[i] = __fsqrt_rn(v[i]);
-        w[i] = w[i] * decay - step_size * __fdividef(m[i], root[i] * root_scale + s.eps);
-        if (!(keep >> i & 1u)) { w[i] = 0.f; m[i] = 0.f; v[i] = 0.f; root[i] = 0.f; }
+        root[i] = sqrt_near(v[i]);
+        w[i] = w[i] * decay - step_size * (m[i] * reciprocal_near(root[i] * root_scale + s.eps));
+        bad = fmaf(w[i], 0.f, bad);
         if constexpr (kNarrow || !kW32) h[i] = mix((uint32_t)(e0 + i) ^ spread);
     }
 
@@ -257,11 +280,12 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
     } else {
         uint32_t r[kPer];
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) {                      // bf16 weights: 11 bits of the hash decide about the 16 that do not fit
-            const uint32_t bits = __float_as_uint(w[i]);
-            r[i] = (bits + ((h[i] >> 21 << 5) | 16u)) >> 16;
-            if ((bits & 0x7F800000u) == 0x7F800000u) r[i] = nearest(w[i]);
-        }
+        for (int i = 0; i < kPer; ++i)                        // bf16 weights: 11 bits of the hash decide about the 16 that do not fit
+            r[i] = (__float_as_uint(w[i]) + (h[i] >> 21 << 5 | 16u)) >> 16;
+        if (bad != 0.f)                                       // (NaN: a weight is not finite, and adding to its bits may have made a number of it)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (!(fabsf(w[i]) <= 3.402823466e38f)) r[i] = nearest(w[i]);
         if (vec) {
             *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(T.w) + at(T.ldw, 0)) =
                 make_uint4(r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16);
@@ -282,14 +306,37 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
         }
     } else {
         // (elements beyond the tensor's last one are zero: g, m and v were not read there)
-        const uint32_t em = scale_of(largest_of_block(m), 0x600000u), ev = scale_of(largest_of_block(root), 0x780000u);
-        const float down_m = power_of(254u - em), down_v = power_of(254u - ev);
+        float am = 0.f, av = 0.f;
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) { am = fmaxf(am, fabsf(m[i])); av = fmaxf(av, root[i]); }
+        if (bad != 0.f || !(am <= 3.402823466e38f) || !(av <= 3.402823466e38f)) {       // what is not finite is held as 0 (NaN in m or root is one in w)
+            am = av = 0.f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (!(fabsf(m[i]) <= 3.402823466e38f)) m[i] = 0.f;
+                if (!(root[i] <= 3.402823466e38f)) root[i] = 0.f;
+                am = fmaxf(am, fabsf(m[i])); av = fmaxf(av, root[i]);
+            }
+        }
+        // (the exponent of a block's scale is the largest of its threads': their two travel in one word)
+        const uint32_t both = max_of_block(scale_of(am, 0x600000u) | scale_of(av, 0x780000u) << 16);
+        const uint32_t em = both & 0xFFFFu, ev = both >> 16;
+        // 2^-E 2^-120 in one factor; where that is below fp32's range, the values come down by 2^-120 first
+        float down_m = power_of(134u - min(em, 133u)), down_v = power_of(134u - min(ev, 133u));
+        if (em > 133u || ev > 133u) {
+            const float first_m = em > 133u ? 0x1p-120f : 1.f, first_v = ev > 133u ? 0x1p-120f : 1.f;
+            if (em > 133u) down_m = power_of(254u - em);
+            if (ev > 133u) down_v = power_of(254u - ev);
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) { m[i] *= first_m; root[i] *= first_v; }
+        }
         uint32_t cm[kPer], cv[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const uint32_t bm = __float_as_uint(fabsf(m[i]) * down_m * 0x1p-120f), bv = __float_as_uint(root[i] * down_v * 0x1p-120f);
-            cm[i] = (bm + (h[i] << 10 & 0xFFC00u | 512u)) >> 20 | (__float_as_uint(m[i]) >> 24 & 0x80u);
-            cv[i] = root[i] > 0.f ? max((bv + (h[i] >> 2 & 0x7FF00u | 128u)) >> 19, 1u) : 0u;
+            const uint32_t tm = (__float_as_uint(m[i] * down_m) + (h[i] << 10 & 0xFFC00u | 512u)) >> 20;       // sign, 4 zeros, code
+            cm[i] = (tm >> 4 & 0x80u) | (tm & 0x7Fu);
+            const uint32_t tv = (__float_as_uint(root[i] * down_v) + (h[i] >> 2 & 0x7FF00u | 128u)) >> 19;
+            cv[i] = max(tv, (uint32_t)(root[i] > 0.f));
         }
         mc = make_uint2(cm[0] | cm[1] << 8 | cm[2] << 16 | cm[3] << 24, cm[4] | cm[5] << 8 | cm[6] << 16 | cm[7] << 24);
         vc = make_uint2(cv[0] | cv[1] << 8 | cv[2] << 16 | cv[3] << 24, cv[4] | cv[5] << 8 | cv[6] << 16 | cv[7] << 24);
@@ -310,24 +357,37 @@ moments_kernel(const uint8_t *m, const uint8_t *m_exp, const uint8_t *v, const u
     wait_for_prerequisites();
     const int64_t e0 = ((int64_t)blockIdx.x * kAdamThreads + threadIdx.x) * kPer;
     if (e0 >= count) return;
-    const float sm = power_of(m_exp[e0 >> 7]), sv = power_of(v_exp[e0 >> 7]);
-    if (vec && e0 + kPer <= count) {
-        const uint2 mc = *reinterpret_cast<const uint2 *>(m + e0), vc = *reinterpret_cast<const uint2 *>(v + e0);
-        uint32_t a[4], r[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t cm = (i < 2 ? mc.x : mc.y) >> (16 * (i & 1)), cv = (i < 2 ? vc.x : vc.y) >> (16 * (i & 1));
-            a[i] = nearest2(value_m(cm & 0xFFu, sm), value_m(cm >> 8 & 0xFFu, sm));
-            r[i] = nearest2(value_root(cv & 0xFFu, sv), value_root(cv >> 8 & 0xFFu, sv));
+    float beyond;
+    const float sm = power_of(m_exp[e0 >> 7]), sv = power_120(v_exp[e0 >> 7], &beyond);
+    const int here = (int)min((int64_t)kPer, count - e0);
+    uint2 mc = make_uint2(0, 0), vc = make_uint2(0, 0);
+    if (here == kPer) {
+        mc = *reinterpret_cast<const uint2 *>(m + e0); vc = *reinterpret_cast<const uint2 *>(v + e0);
+    } else {
+        for (int i = 0; i < here; ++i) {
+            (i < 4 ? mc.x : mc.y) |= (uint32_t)m[e0 + i] << (8 * (i & 3));
+            (i < 4 ? vc.x : vc.y) |= (uint32_t)v[e0 + i] << (8 * (i & 3));
         }
+    }
+    uint32_t a[4], r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const float2 two = values_m(i < 2 ? mc.x : mc.y, i & 1);
+        const uint32_t c = i < 2 ? vc.x : vc.y;
+        a[i] = nearest2(two.x * sm, two.y * sm);
+        r[i] = nearest2(root_bits(c, 2 * (i & 1)) * sv * beyond, root_bits(c, 2 * (i & 1) + 1) * sv * beyond);
+    }
+    if (vec && here == kPer) {
         *reinterpret_cast<uint4 *>(m_out + e0) = make_uint4(a[0], a[1], a[2], a[3]);
         *reinterpret_cast<uint4 *>(root_out + e0) = make_uint4(r[0], r[1], r[2], r[3]);
         return;
     }
-    for (int64_t e = e0; e < min(e0 + kPer, count); ++e) {
-        m_out[e] = nearest(value_m(m[e], sm));
-        root_out[e] = nearest(value_root(v[e], sv));
-    }
+#pragma unroll
+    for (int i = 0; i < kPer; ++i)
+        if (i < here) {
+            m_out[e0 + i] = (uint16_t)(a[i >> 1] >> (16 * (i & 1)));
+            root_out[e0 + i] = (uint16_t)(r[i >> 1] >> (16 * (i & 1)));
+        }
 }
 
 template <int CAP>
@@ -412,7 +472,7 @@ crisp_status_t crisp_adamw(int32_t n, const crisp_adamw_tensor_t *tensors, const
     s.lr = (float)p->lr;
     s.beta1 = (float)p->beta1; s.one_beta1 = (float)(1.0 - p->beta1);
     s.beta2 = (float)p->beta2; s.one_beta2 = (float)(1.0 - p->beta2);
-    s.eps = (float)p->eps;
+    s.eps = std::max((float)p->eps, 1.17549435e-38f);          // 0 / 0 is 0; no root above 0 is that small
     s.weight_decay = (float)p->weight_decay;
     s.decay = (float)(1.0 - p->lr * p->weight_decay);
     // (the factor of a device lr: taken with lr = 1, so that nothing is divided by an lr of 0)

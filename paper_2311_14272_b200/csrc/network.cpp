@@ -187,6 +187,68 @@ PyObject *decode(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// Rows, columns and pitch of a tensor whose elements lie in rows of consecutive ones (as the binding's _rows_of has them); false: it does not.
+bool rows_of(const at::Tensor &t, int64_t (&v)[3]) {
+    const int64_t n = t.numel();
+    if (t.dim() == 0 || n == 0) {
+        v[0] = 1; v[1] = v[2] = n;
+    } else if (t.is_contiguous()) {
+        v[0] = t.dim() > 1 ? t.size(0) : 1;
+        v[1] = v[2] = n / v[0];
+    } else if (t.dim() == 2 && (t.stride(1) == 1 || t.size(1) == 1) && t.stride(0) >= t.size(1)) {
+        v[0] = t.size(0); v[1] = t.size(1); v[2] = t.stride(0);
+    } else {
+        return false;
+    }
+    return true;
+}
+
+// gradients(array of crisp_adamw_tensor_t, weights, copies, gradients, masks): where the tensors of a step lie, and its masks, or None: not filled in.  The four
+// are lists of one length; an entry of `copies` and `gradients` may be None, one of `masks` a layer or None.  (The shapes and types of weights and copies
+// are those that the array was made for, or it is not filled in.)
+PyObject *gradients(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arguments("gradients", n, 5)) return nullptr;
+    crisp_adamw_tensor_t *arr = address<crisp_adamw_tensor_t>(args[0]);
+    if (!arr) return PyErr_Occurred() ? nullptr : Py_NewRef(Py_None);
+    for (int i = 1; i < 5; ++i)
+        if (!PyList_CheckExact(args[i]) || PyList_GET_SIZE(args[i]) != PyList_GET_SIZE(args[1])) Py_RETURN_NONE;
+    for (Py_ssize_t l = 0; l < PyList_GET_SIZE(args[1]); ++l) {
+        crisp_adamw_tensor_t &T = arr[l];
+        PyObject *wo = PyList_GET_ITEM(args[1], l), *co = PyList_GET_ITEM(args[2], l), *go = PyList_GET_ITEM(args[3], l), *mo = PyList_GET_ITEM(args[4], l);
+        T.d_grad = nullptr;
+        if (go == Py_None) continue;
+        if (!THPVariable_CheckExact(go) || !THPVariable_Check(wo) || (co != Py_None && !THPVariable_Check(co))) Py_RETURN_NONE;
+        const at::Tensor &g = THPVariable_Unpack(go), &w = THPVariable_Unpack(wo);
+        int64_t rows[3];
+        if (!w.is_cuda() || w.layout() != at::kStrided || w.scalar_type() != (T.w_dtype ? at::kFloat : at::kBFloat16) || !rows_of(w, rows) || rows[0] != T.rows ||
+            rows[1] != T.k)
+            Py_RETURN_NONE;
+        T.d_w = w.data_ptr(); T.ld_w = rows[2];
+        if (co != Py_None) {
+            const at::Tensor &c = THPVariable_Unpack(co);
+            if (!c.is_cuda() || c.layout() != at::kStrided || c.device() != w.device() || c.scalar_type() != at::kBFloat16 || !c.sizes().equals(w.sizes()) ||
+                !rows_of(c, rows))
+                Py_RETURN_NONE;
+            T.d_copy_bf16 = static_cast<uint16_t *>(c.data_ptr()); T.ld_copy = rows[2];
+        }
+        if (!g.is_cuda() || g.layout() != at::kStrided || g.device() != w.device() || (g.scalar_type() != at::kBFloat16 && g.scalar_type() != at::kFloat) ||
+            !g.sizes().equals(w.sizes()) || !rows_of(g, rows))
+            Py_RETURN_NONE;
+        void *mask = nullptr;
+        if (mo != Py_None) {
+            Ref m(PyObject_GetAttr(mo, names.mask));
+            if (!m.p) { PyErr_Clear(); Py_RETURN_NONE; }
+            mask = PyLong_AsVoidPtr(m.p);
+            if (PyErr_Occurred()) { PyErr_Clear(); Py_RETURN_NONE; }
+        }
+        T.d_grad = g.data_ptr(); T.ld_grad = rows[2]; T.grad_dtype = g.scalar_type() == at::kFloat;
+        T.mask = static_cast<crisp_mask_t>(mask);
+    }
+    Py_RETURN_TRUE;
+    END_HANDLE_TH_ERRORS
+}
+
 // bind(address of crisp_decode)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
     if (!arguments("bind", n, 1)) return nullptr;
@@ -196,7 +258,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 #define CRISP_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {CRISP_METHOD(bind), CRISP_METHOD(table), CRISP_METHOD(encodings), CRISP_METHOD(encoded), CRISP_METHOD(decode), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {CRISP_METHOD(bind), CRISP_METHOD(table), CRISP_METHOD(encodings), CRISP_METHOD(encoded), CRISP_METHOD(decode), CRISP_METHOD(gradients), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_network", nullptr, 0, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
