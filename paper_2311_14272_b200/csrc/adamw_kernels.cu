@@ -40,24 +40,31 @@ struct AdamTensor {
     uint8_t flat;            // w, g and copy are packed: element e lies at e
     uint8_t vec;             // eight elements from a multiple of eight on lie in a row and at multiples of 16 bytes
     uint8_t bytes;           // k is a multiple of 8: eight elements' mask bits are one byte
+    uint8_t plain;           // flat, vec and, under a mask, bytes
 };
+
+// Powers of two as parameters of the kernel.  The 8-bit kernel is bound by the integer pipe, and a product with a number that the compiler does not
+// know goes to the multiply-add pipe instead of becoming a shift.
+struct Powers { uint32_t p1 = 1u << 1, p4 = 1u << 4, p5 = 1u << 5, p7 = 1u << 7, p9 = 1u << 9, p19 = 1u << 19; };
 
 struct AdamScalars {
     float lr, beta1, one_beta1, beta2, one_beta2, eps, decay, weight_decay;
     float step_size, root_scale;                              // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
     float log_beta1, log_beta2;
     uint32_t seed_key;
+    Powers by;
     const float *d_lr, *d_grad_scale;
     const int64_t *d_step;
 };
 
 // A bijection of 32-bit words in which every bit of the input moves every bit of the output (xorshift-multiply with the constants that Wellons'
 // search published as lowbias32).
-__host__ __device__ __forceinline__ uint32_t mix(uint32_t h) {
-    h ^= h >> 16; h *= 0x7FEB352Du;
+__host__ __device__ __forceinline__ uint32_t mix_rest(uint32_t h) {
+    h *= 0x7FEB352Du;
     h ^= h >> 15; h *= 0x846CA68Bu;
     return h ^ (h >> 16);
 }
+__host__ __device__ __forceinline__ uint32_t mix(uint32_t h) { return mix_rest(h ^ (h >> 16)); }
 
 // Eight elements at a multiple of 16 bytes.
 __device__ __forceinline__ void load8(const float *p, float (&x)[kPer]) {
@@ -89,8 +96,12 @@ __device__ __forceinline__ float power_120(uint32_t biased, float *beyond) {
     *beyond = power_of(127u + biased - near);
     return power_of(near + 120u);
 }
-__device__ __forceinline__ float root_bits(uint32_t codes, int byte) {                                       // code << 19 as fp32
-    return __uint_as_float(__byte_perm(codes, 0, 0x0444 | (uint32_t)byte << 12) >> 5);
+__device__ __forceinline__ float root_bits(uint32_t codes, int byte, uint32_t p19) {                         // code << 19 as fp32
+    return __uint_as_float(__byte_perm(codes, 0, 0x4440 | (uint32_t)byte) * p19);
+}
+// The top bytes of four words.
+__device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
 }
 __device__ __forceinline__ float2 values_m(uint32_t codes, int pair) {                                       // two e4m3 codes
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes >> (16 * pair)), __NV_E4M3);
@@ -122,20 +133,17 @@ __device__ __forceinline__ uint2 bytes_of_bits(uint32_t keep) {
     return make_uint2(((keep & 15u) * 0x00204081u & 0x01010101u) * 255u, ((keep >> 4) * 0x00204081u & 0x01010101u) * 255u);
 }
 
-template <bool kNarrow, bool kW32, int CAP>
-__global__ void __launch_bounds__(kAdamThreads)
-adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_constant__ AdamScalars s) {
-    wait_for_prerequisites();
-    const int l = b.find(blockIdx.x);
-    const AdamTensor &T = b.layer[l];
-    const int64_t e0 = (int64_t)(blockIdx.x - b.first[l]) * kPiece + threadIdx.x * kPer;
-    const int count = (int)max((int64_t)0, min((int64_t)kPer, T.total - e0));
-    const bool whole = count == kPer, vec = T.vec && whole;
+// Eight elements of a thread, from e0 on.  kPlain: all of the CTA's elements are the tensor's, lie packed at multiples of 16 bytes, and their mask bits in whole
+// bytes; what every other piece has to ask for each element is left out (8-bit states, 4 x 4096 x 4096: MEASURE us against MEASURE).
+template <bool kNarrow, bool kW32, bool kPlain>
+__device__ __forceinline__ void eight(const AdamTensor &T, const AdamScalars &s, const int64_t e0) {
+    const int count = kPlain ? kPer : (int)max((int64_t)0, min((int64_t)kPer, T.total - e0));
+    const bool whole = kPlain || count == kPer, vec = kPlain || (T.vec && whole), flat = kPlain || T.flat, bytes = kPlain || T.bytes;
 
     // where the elements lie: row and column of the first one, needed for rows that are not packed and for masks
     int64_t row = 0;
     uint32_t col = 0;
-    if (T.mask || !T.flat) {
+    if (T.mask || !flat) {
         if (T.total <= 0xFFFFFFFFll) {
             const uint32_t r = (uint32_t)e0 / T.k;
             row = r; col = (uint32_t)e0 - r * T.k;
@@ -144,7 +152,7 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
         }
     }
     const auto at = [&](int64_t ld, int i) -> int64_t {       // the address of element i, for rows of pitch ld
-        if (T.flat) return e0 + i;
+        if (flat) return e0 + i;
         int64_t r = row;
         uint32_t c = col + i;
         while (c >= T.k) { c -= T.k; ++r; }
@@ -194,7 +202,7 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
         if (count) { m_exp = T.m_exp[e0 >> 7]; v_exp = T.v_exp[e0 >> 7]; }
     }
     if (T.mask && count) {
-        if (T.bytes) {
+        if (bytes) {
             keep = reinterpret_cast<const uint8_t *>(T.mask + row * T.wpr)[col >> 3];
         } else {
             int64_t r = row;
@@ -241,6 +249,8 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
     const float m_scale = power_of(m_exp), v_scale = power_120(v_exp, &v_beyond);
     const bool wide_scale = kNarrow && v_beyond != 1.f;
 
+    // (e0 is a multiple of 8: the hash of e0 + i differs from that of e0 in three low bits until its first product)
+    const uint32_t first = ((uint32_t)e0 ^ spread) ^ (((uint32_t)e0 ^ spread) >> 16);
     uint32_t h[kPer];
     float root[kPer], bad = 0.f;
 #pragma unroll
@@ -250,7 +260,7 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
                 const float2 two = values_m(i < 4 ? mc.x : mc.y, i >> 1 & 1);
                 m[i] = two.x * m_scale; m[i + 1] = two.y * m_scale;
             }
-            float u = root_bits(i < 4 ? vc.x : vc.y, i & 3) * v_scale;
+            float u = root_bits(i < 4 ? vc.x : vc.y, i & 3, s.by.p19) * v_scale;
             if (wide_scale) u *= v_beyond;
             v[i] = u * u;
         }
@@ -260,7 +270,7 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
         root[i] = sqrt_near(v[i]);
         w[i] = w[i] * decay - step_size * (m[i] * reciprocal_near(root[i] * root_scale + s.eps));
         bad = fmaf(w[i], 0.f, bad);
-        if constexpr (kNarrow || !kW32) h[i] = mix((uint32_t)(e0 + i) ^ spread);
+        if constexpr (kNarrow || !kW32) h[i] = mix_rest(first ^ (uint32_t)i);
     }
 
     if constexpr (kW32) {
@@ -281,18 +291,18 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
         uint32_t r[kPer];
 #pragma unroll
         for (int i = 0; i < kPer; ++i)                        // bf16 weights: 11 bits of the hash decide about the 16 that do not fit
-            r[i] = (__float_as_uint(w[i]) + (h[i] >> 21 << 5 | 16u)) >> 16;
+            r[i] = (h[i] >> 20 | 1u) * s.by.p4 + __float_as_uint(w[i]);
         if (bad != 0.f)                                       // (NaN: a weight is not finite, and adding to its bits may have made a number of it)
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
-                if (!(fabsf(w[i]) <= 3.402823466e38f)) r[i] = nearest(w[i]);
+                if (!(fabsf(w[i]) <= 3.402823466e38f)) r[i] = (uint32_t)nearest(w[i]) << 16;
         if (vec) {
             *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(T.w) + at(T.ldw, 0)) =
-                make_uint4(r[0] | r[1] << 16, r[2] | r[3] << 16, r[4] | r[5] << 16, r[6] | r[7] << 16);
+                make_uint4(__byte_perm(r[0], r[1], 0x7632), __byte_perm(r[2], r[3], 0x7632), __byte_perm(r[4], r[5], 0x7632), __byte_perm(r[6], r[7], 0x7632));
         } else {
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
-                if (i < count) reinterpret_cast<uint16_t *>(T.w)[at(T.ldw, i)] = (uint16_t)r[i];
+                if (i < count) reinterpret_cast<uint16_t *>(T.w)[at(T.ldw, i)] = (uint16_t)(r[i] >> 16);
         }
     }
     if constexpr (!kNarrow) {
@@ -330,26 +340,44 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
 #pragma unroll
             for (int i = 0; i < kPer; ++i) { m[i] *= first_m; root[i] *= first_v; }
         }
-        uint32_t cm[kPer], cv[kPer];
+        uint32_t cm[kPer], cv[kPer];                          // codes as top bytes
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
-            const uint32_t tm = (__float_as_uint(m[i] * down_m) + (h[i] << 10 & 0xFFC00u | 512u)) >> 20;       // sign, 4 zeros, code
-            cm[i] = (tm >> 4 & 0x80u) | (tm & 0x7Fu);
-            const uint32_t tv = (__float_as_uint(root[i] * down_v) + (h[i] >> 2 & 0x7FF00u | 128u)) >> 19;
-            cv[i] = max(tv, (uint32_t)(root[i] > 0.f));
+            // 20 (19) bits below the code, of which the hash gives the upper ten (eleven) and the one below them is set
+            cm[i] = (((h[i] * s.by.p1 + 1u) & 0x7FFu) * s.by.p9 + __float_as_uint(m[i] * down_m)) * s.by.p4;
+            const uint32_t t = ((h[i] >> 9 & 0xFFEu) | 1u) * s.by.p7 + __float_as_uint(root[i] * down_v);
+            cv[i] = max(t, __float_as_uint(__saturatef(root[i] * 0x1p80f) * 0x1p-130f)) * s.by.p5;             // at least 1 where root is above 0
         }
-        mc = make_uint2(cm[0] | cm[1] << 8 | cm[2] << 16 | cm[3] << 24, cm[4] | cm[5] << 8 | cm[6] << 16 | cm[7] << 24);
-        vc = make_uint2(cv[0] | cv[1] << 8 | cv[2] << 16 | cv[3] << 24, cv[4] | cv[5] << 8 | cv[6] << 16 | cv[7] << 24);
+        mc.x = top_bytes(cm[0], cm[1], cm[2], cm[3]);
+        mc.y = top_bytes(cm[4], cm[5], cm[6], cm[7]);
+        const auto sign = [&](int i) { return top_bytes(__float_as_uint(m[i]), __float_as_uint(m[i + 1]), __float_as_uint(m[i + 2]), __float_as_uint(m[i + 3])) & 0x80808080u; };
+        mc.x |= sign(0);
+        mc.y |= sign(4);
+        vc = make_uint2(top_bytes(cv[0], cv[1], cv[2], cv[3]), top_bytes(cv[4], cv[5], cv[6], cv[7]));
         uint8_t *pm = reinterpret_cast<uint8_t *>(T.m) + e0, *pv = reinterpret_cast<uint8_t *>(T.v) + e0;
         if (whole) {
             *reinterpret_cast<uint2 *>(pm) = mc; *reinterpret_cast<uint2 *>(pv) = vc;
         } else {
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
-                if (i < count) { pm[i] = (uint8_t)cm[i]; pv[i] = (uint8_t)cv[i]; }
+                if (i < count) {
+                    pm[i] = (uint8_t)((i < 4 ? mc.x : mc.y) >> (8 * (i & 3)));
+                    pv[i] = (uint8_t)((i < 4 ? vc.x : vc.y) >> (8 * (i & 3)));
+                }
         }
         if ((threadIdx.x & 15) == 0 && count) { T.m_exp[e0 >> 7] = (uint8_t)em; T.v_exp[e0 >> 7] = (uint8_t)ev; }
     }
+}
+
+template <bool kNarrow, bool kW32, int CAP>
+__global__ void __launch_bounds__(kAdamThreads, kNarrow ? 5 : 4)
+adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_constant__ AdamScalars s) {
+    wait_for_prerequisites();
+    const int l = b.find(blockIdx.x);
+    const AdamTensor &T = b.layer[l];
+    const int64_t first = (int64_t)(blockIdx.x - b.first[l]) * kPiece;
+    if (T.plain && first + kPiece <= T.total) eight<kNarrow, kW32, true>(T, s, first + threadIdx.x * kPer);
+    else eight<kNarrow, kW32, false>(T, s, first + threadIdx.x * kPer);
 }
 
 __global__ void __launch_bounds__(kAdamThreads)
@@ -375,7 +403,7 @@ moments_kernel(const uint8_t *m, const uint8_t *m_exp, const uint8_t *v, const u
         const float2 two = values_m(i < 2 ? mc.x : mc.y, i & 1);
         const uint32_t c = i < 2 ? vc.x : vc.y;
         a[i] = nearest2(two.x * sm, two.y * sm);
-        r[i] = nearest2(root_bits(c, 2 * (i & 1)) * sv * beyond, root_bits(c, 2 * (i & 1) + 1) * sv * beyond);
+        r[i] = nearest2(root_bits(c, 2 * (i & 1), 1u << 19) * sv * beyond, root_bits(c, 2 * (i & 1) + 1, 1u << 19) * sv * beyond);
     }
     if (vec && here == kPer) {
         *reinterpret_cast<uint4 *>(m_out + e0) = make_uint4(a[0], a[1], a[2], a[3]);
@@ -448,6 +476,7 @@ crisp_status_t entry(const crisp_adamw_tensor_t &t, int32_t ordinal, const crisp
         if (t.mask->g.rows != t.rows || t.mask->g.k != t.k) return CRISP_BAD_SHAPE;
         T->mask = t.mask->d_nm_bits; T->wpr = (uint32_t)t.mask->g.wpr;
     }
+    T->plain = T->flat && T->vec && (T->bytes || !T->mask);
     T->ordinal = (uint32_t)ordinal;
     return CRISP_OK;
 }
