@@ -6,6 +6,12 @@
 // gradients with 8-bit states.  A thread takes eight consecutive elements (16 or 32 bytes of each tensor, 8 of an 8-bit state), so that half a warp
 // holds the 128 elements of a scale and finds their largest value by shuffles; the tensors of a call are numbered through in pieces of
 // 2048 elements, one CTA each, and their table travels as a kernel parameter.
+//
+// Measured on four tensors of 4096 x 4096 with bf16 gradients: 32-bit states 254 us with fp32 weights under masks (6.9 TB/s), 215 with bf16 ones (6.9).
+// 8-bit states 155 us with bf16 weights (4.3 TB/s), 169 under masks, 171 with fp32 weights (5.5): some 80 instructions an element, two thirds of what the
+// schedulers issue on the integer pipe, bound these.  What brought them there from 356: no questions asked for each element in pieces that need none
+// (287 -> 195), products instead of shifts (267 -> 242 with the former still in), codes packed by byte permutes, cvt.rs for bf16 weights, five CTAs an SM
+// (four 187, six 172 and seven 188 with spills).  Not kept: two or four turns of eight elements a thread (190 and 252; with the loads ahead 184).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -24,6 +30,7 @@ namespace {
 constexpr int kAdamThreads = 256;
 constexpr int kPer = 8;                                       // elements a thread
 constexpr int kPiece = kAdamThreads * kPer;
+constexpr float kLargest = 3.402823466e38f;
 
 struct AdamTensor {
     void *w;
@@ -50,7 +57,7 @@ struct Powers { uint32_t p1 = 1u << 1, p4 = 1u << 4, p5 = 1u << 5, p7 = 1u << 7,
 struct AdamScalars {
     float lr, beta1, one_beta1, beta2, one_beta2, eps, decay, weight_decay;
     float step_size, root_scale;                              // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
-    float log_beta1, log_beta2;
+    float log_beta1, log_beta2, root_beta2;
     uint32_t seed_key;
     Powers by;
     const float *d_lr, *d_grad_scale;
@@ -75,16 +82,10 @@ __device__ __forceinline__ void store8(float *p, const float (&x)[kPer]) {
     reinterpret_cast<float4 *>(p)[0] = make_float4(x[0], x[1], x[2], x[3]);
     reinterpret_cast<float4 *>(p)[1] = make_float4(x[4], x[5], x[6], x[7]);
 }
-__device__ __forceinline__ void unpack8(const uint4 &a, float (&x)[kPer]) {
-    const uint32_t u[4] = {a.x, a.y, a.z, a.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) { x[2 * i] = __uint_as_float(u[i] << 16); x[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u); }
-}
 __device__ __forceinline__ uint32_t nearest2(float lo, float hi) {
     const __nv_bfloat162 v = __floats2bfloat162_rn(lo, hi);
     return *reinterpret_cast<const uint32_t *>(&v);
 }
-__device__ __forceinline__ float from_bf16(uint16_t b) { return __uint_as_float((uint32_t)b << 16); }
 __device__ __forceinline__ uint16_t nearest(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
 
 // The 8-bit forms.  A code is the top of an fp32 number whose exponent field has been brought down by 120 (127 - 7), so that small codes are
@@ -128,203 +129,264 @@ __device__ __forceinline__ float reciprocal_near(float x) {
     asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
     return r;
 }
+// bf16 weights, rounded at random: 11 bits of each hash and a set one below them decide about the 16 bits that do not fit.
+__device__ __forceinline__ uint32_t random2(float lo, float hi, uint32_t h_lo, uint32_t h_hi) {
+    const uint32_t random = (__byte_perm(h_lo, h_hi, 0x7632) & 0xFFE0FFE0u) | 0x00100010u;
+    uint32_t r;
+    asm("cvt.rs.bf16x2.f32 %0, %1, %2, %3;" : "=r"(r) : "f"(hi), "f"(lo), "r"(random));
+    return r;
+}
+__device__ __forceinline__ float max_nan(float a, float b) {   // NaN if one of them is
+    float r;
+    asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 // Bit i of the byte in every bit of byte i of (lo, hi).
 __device__ __forceinline__ uint2 bytes_of_bits(uint32_t keep) {
     return make_uint2(((keep & 15u) * 0x00204081u & 0x01010101u) * 255u, ((keep >> 4) * 0x00204081u & 0x01010101u) * 255u);
 }
 
-// Eight elements of a thread, from e0 on.  kPlain: all of the CTA's elements are the tensor's, lie packed at multiples of 16 bytes, and their mask bits in whole
-// bytes; what every other piece has to ask for each element is left out (8-bit states, 4 x 4096 x 4096: MEASURE us against MEASURE).
-template <bool kNarrow, bool kW32, bool kPlain>
-__device__ __forceinline__ void eight(const AdamTensor &T, const AdamScalars &s, const int64_t e0) {
-    const int count = kPlain ? kPer : (int)max((int64_t)0, min((int64_t)kPer, T.total - e0));
-    const bool whole = kPlain || count == kPer, vec = kPlain || (T.vec && whole), flat = kPlain || T.flat, bytes = kPlain || T.bytes;
-
-    // where the elements lie: row and column of the first one, needed for rows that are not packed and for masks
-    int64_t row = 0;
-    uint32_t col = 0;
-    if (T.mask || !flat) {
-        if (T.total <= 0xFFFFFFFFll) {
-            const uint32_t r = (uint32_t)e0 / T.k;
-            row = r; col = (uint32_t)e0 - r * T.k;
-        } else {
-            row = e0 / T.k; col = (uint32_t)(e0 - row * T.k);
-        }
+// What a step reads of eight elements of a thread, as it lies in memory (weights and gradients: bf16 pairs or fp32).
+template <bool kNarrow, bool kW32>
+struct Eight {
+    uint32_t w[kW32 ? 8 : 4], g[8];
+    float m[kNarrow ? 1 : 8], v[kNarrow ? 1 : 8];
+    uint2 mc, vc;            // codes of 8-bit states
+    uint32_t m_exp, v_exp, keep;
+};
+// What it takes beside them.
+struct Factors {
+    float decay, step_size, root_scale, grad_scale;
+    uint32_t key, spread;
+};
+// The row and column of element e0.
+__device__ __forceinline__ void place(const AdamTensor &T, int64_t e0, int64_t *row, uint32_t *col) {
+    if (T.total <= 0xFFFFFFFFll) {
+        const uint32_t r = (uint32_t)e0 / T.k;
+        *row = r; *col = (uint32_t)e0 - r * T.k;
+    } else {
+        *row = e0 / T.k; *col = (uint32_t)(e0 - *row * T.k);
     }
-    const auto at = [&](int64_t ld, int i) -> int64_t {       // the address of element i, for rows of pitch ld
+}
+template <int N>
+__device__ __forceinline__ void load_words(const void *p, uint32_t (&x)[N]) {
+#pragma unroll
+    for (int i = 0; i < N; i += 4) {
+        const uint4 a = reinterpret_cast<const uint4 *>(p)[i / 4];
+        x[i] = a.x; x[i + 1] = a.y; x[i + 2] = a.z; x[i + 3] = a.w;
+    }
+}
+
+// kPlain: the eight elements are the tensor's, lie packed at multiples of 16 bytes, and their mask bits in a byte.  What all others have to ask for each element
+// is left out of the code.
+template <bool kNarrow, bool kW32, bool kPlain>
+struct Piece {
+    const AdamTensor &T;
+    const int64_t e0;
+    int count;
+    bool whole, vec, flat;
+    int64_t row;
+    uint32_t col;
+
+    __device__ __forceinline__ Piece(const AdamTensor &t, int64_t e) : T(t), e0(e), row(0), col(0) {
+        count = kPlain ? kPer : (int)max((int64_t)0, min((int64_t)kPer, T.total - e0));
+        whole = kPlain || count == kPer; vec = kPlain || (T.vec && whole); flat = kPlain || T.flat;
+        if (T.mask || !flat) place(T, e0, &row, &col);
+    }
+    // where element i of rows of pitch ld lies
+    __device__ __forceinline__ int64_t at(int64_t ld, int i) const {
         if (flat) return e0 + i;
         int64_t r = row;
         uint32_t c = col + i;
         while (c >= T.k) { c -= T.k; ++r; }
         return r * ld + c;
-    };
-
-    float w[kPer] = {}, g[kPer] = {}, m[kPer] = {}, v[kPer] = {};
-    uint32_t keep = 0xFFu;
-    uint2 mc = make_uint2(0, 0), vc = make_uint2(0, 0);
-    uint32_t m_exp = 0, v_exp = 0;
-    if (vec) {
-        if constexpr (kW32) load8(reinterpret_cast<const float *>(T.w) + at(T.ldw, 0), w);
-        else unpack8(*reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(T.w) + at(T.ldw, 0)), w);
-        if (T.g32) load8(reinterpret_cast<const float *>(T.g) + at(T.ldg, 0), g);
-        else unpack8(*reinterpret_cast<const uint4 *>(reinterpret_cast<const uint16_t *>(T.g) + at(T.ldg, 0)), g);
-    } else {
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (i < count) {
-                if constexpr (kW32) w[i] = reinterpret_cast<const float *>(T.w)[at(T.ldw, i)];
-                else w[i] = from_bf16(reinterpret_cast<const uint16_t *>(T.w)[at(T.ldw, i)]);
-                if (T.g32) g[i] = reinterpret_cast<const float *>(T.g)[at(T.ldg, i)];
-                else g[i] = from_bf16(reinterpret_cast<const uint16_t *>(T.g)[at(T.ldg, i)]);
-            }
     }
-    if constexpr (!kNarrow) {
-        const float *pm = reinterpret_cast<const float *>(T.m) + e0, *pv = reinterpret_cast<const float *>(T.v) + e0;
-        if (whole) {
-            load8(pm, m); load8(pv, v);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (i < count) { m[i] = pm[i]; v[i] = pv[i]; }
-        }
-    } else {
-        const uint8_t *pm = reinterpret_cast<const uint8_t *>(T.m) + e0, *pv = reinterpret_cast<const uint8_t *>(T.v) + e0;
-        if (whole) {
-            mc = *reinterpret_cast<const uint2 *>(pm); vc = *reinterpret_cast<const uint2 *>(pv);
-        } else {
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (i < count) {
-                    (i < 4 ? mc.x : mc.y) |= (uint32_t)pm[i] << (8 * (i & 3));
-                    (i < 4 ? vc.x : vc.y) |= (uint32_t)pv[i] << (8 * (i & 3));
-                }
-        }
-        if (count) { m_exp = T.m_exp[e0 >> 7]; v_exp = T.v_exp[e0 >> 7]; }
-    }
-    if (T.mask && count) {
-        if (bytes) {
-            keep = reinterpret_cast<const uint8_t *>(T.mask + row * T.wpr)[col >> 3];
-        } else {
-            int64_t r = row;
-            uint32_t c = col;
-            keep = 0;
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (i < count) {
-                    keep |= (T.mask[r * T.wpr + (c >> 5)] >> (c & 31) & 1u) << i;
-                    if (++c == T.k) { c = 0; ++r; }
-                }
-        }
-    }
-
-    float step_size = s.step_size, root_scale = s.root_scale, decay = s.decay;
-    uint32_t key = T.key, spread = T.spread;
-    if (s.d_step || s.d_lr) {
-        const float lr = s.d_lr ? *s.d_lr : s.lr;
-        const float t = s.d_step ? (float)*s.d_step : 0.f;
-        // 1 - b^t = -expm1(t log b): to a rounding or two of fp32 for any t
-        if (s.d_step) {
-            root_scale = 1.f / sqrtf(-expm1f(t * s.log_beta2));
-            key = mix(mix(s.seed_key ^ (uint32_t)*s.d_step) ^ T.ordinal);
-            spread = mix(key);
-        }
-        step_size = s.d_step ? lr / -expm1f(t * s.log_beta1) : s.step_size / s.lr * lr;
-        decay = 1.f - lr * s.weight_decay;
-    }
-    const float grad_scale = s.d_grad_scale ? *s.d_grad_scale : 1.f;
-    if (kNarrow || !kW32)
-        if (e0 >> 32) spread = mix((uint32_t)(e0 >> 32) ^ key);
-
-    // Where the mask has no bit: zeros go in and zeros come out (eps is above 0).
-    if (T.mask) {
-        if constexpr (kNarrow) {
-            const uint2 b8 = bytes_of_bits(keep);
-            mc.x &= b8.x; mc.y &= b8.y; vc.x &= b8.x; vc.y &= b8.y;
-        }
-#pragma unroll
-        for (int i = 0; i < kPer; ++i)
-            if (!(keep >> i & 1u)) { w[i] = 0.f; g[i] = 0.f; m[i] = 0.f; v[i] = 0.f; }
-    }
-    float v_beyond;
-    const float m_scale = power_of(m_exp), v_scale = power_120(v_exp, &v_beyond);
-    const bool wide_scale = kNarrow && v_beyond != 1.f;
-
-    // (e0 is a multiple of 8: the hash of e0 + i differs from that of e0 in three low bits until its first product)
-    const uint32_t first = ((uint32_t)e0 ^ spread) ^ (((uint32_t)e0 ^ spread) >> 16);
-    uint32_t h[kPer];
-    float root[kPer], bad = 0.f;
-#pragma unroll
-    for (int i = 0; i < kPer; ++i) {
-        if constexpr (kNarrow) {
-            if ((i & 1) == 0) {
-                const float2 two = values_m(i < 4 ? mc.x : mc.y, i >> 1 & 1);
-                m[i] = two.x * m_scale; m[i + 1] = two.y * m_scale;
-            }
-            float u = root_bits(i < 4 ? vc.x : vc.y, i & 3, s.by.p19) * v_scale;
-            if (wide_scale) u *= v_beyond;
-            v[i] = u * u;
-        }
-        const float gi = g[i] * grad_scale;
-        m[i] = s.beta1 * m[i] + s.one_beta1 * gi;
-        v[i] = s.beta2 * v[i] + s.one_beta2 * gi * gi;
-        root[i] = sqrt_near(v[i]);
-        w[i] = w[i] * decay - step_size * (m[i] * reciprocal_near(root[i] * root_scale + s.eps));
-        bad = fmaf(w[i], 0.f, bad);
-        if constexpr (kNarrow || !kW32) h[i] = mix_rest(first ^ (uint32_t)i);
-    }
-
-    if constexpr (kW32) {
+    __device__ __forceinline__ void read(Eight<kNarrow, kW32> &x) const {
+        const uint16_t *w16 = reinterpret_cast<const uint16_t *>(T.w), *g16 = reinterpret_cast<const uint16_t *>(T.g);
+        const uint32_t *w32 = reinterpret_cast<const uint32_t *>(T.w), *g32 = reinterpret_cast<const uint32_t *>(T.g);
         if (vec) {
-            store8(reinterpret_cast<float *>(T.w) + at(T.ldw, 0), w);
-            if (T.copy)
-                *reinterpret_cast<uint4 *>(T.copy + at(T.ldc, 0)) =
-                    make_uint4(nearest2(w[0], w[1]), nearest2(w[2], w[3]), nearest2(w[4], w[5]), nearest2(w[6], w[7]));
+            if constexpr (kW32) load_words(w32 + at(T.ldw, 0), x.w);
+            else load_words(w16 + at(T.ldw, 0), x.w);
+            if (T.g32) load_words(g32 + at(T.ldg, 0), x.g);
+            else load_words(g16 + at(T.ldg, 0), reinterpret_cast<uint32_t (&)[4]>(x.g));
         } else {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (i < count) {
-                    reinterpret_cast<float *>(T.w)[at(T.ldw, i)] = w[i];
-                    if (T.copy) T.copy[at(T.ldc, i)] = nearest(w[i]);
+            for (int i = 0; i < kPer; ++i) {
+                const bool in = i < count;
+                if constexpr (kW32) {
+                    x.w[i] = in ? w32[at(T.ldw, i)] : 0u;
+                } else {
+                    const uint32_t bits = in ? (uint32_t)w16[at(T.ldw, i)] << (16 * (i & 1)) : 0u;
+                    x.w[i / 2] = i & 1 ? x.w[i / 2] | bits : bits;
                 }
+                if (T.g32) {
+                    x.g[i] = in ? g32[at(T.ldg, i)] : 0u;
+                } else {
+                    const uint32_t bits = in ? (uint32_t)g16[at(T.ldg, i)] << (16 * (i & 1)) : 0u;
+                    x.g[i / 2] = i & 1 ? x.g[i / 2] | bits : bits;
+                }
+            }
         }
-    } else {
-        uint32_t r[kPer];
+        if constexpr (!kNarrow) {
+            const float *pm = reinterpret_cast<const float *>(T.m) + e0, *pv = reinterpret_cast<const float *>(T.v) + e0;
+            if (whole) {
+                load8(pm, x.m); load8(pv, x.v);
+            } else {
 #pragma unroll
-        for (int i = 0; i < kPer; ++i)                        // bf16 weights: 11 bits of the hash decide about the 16 that do not fit
-            r[i] = (h[i] >> 20 | 1u) * s.by.p4 + __float_as_uint(w[i]);
-        if (bad != 0.f)                                       // (NaN: a weight is not finite, and adding to its bits may have made a number of it)
-#pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (!(fabsf(w[i]) <= 3.402823466e38f)) r[i] = (uint32_t)nearest(w[i]) << 16;
-        if (vec) {
-            *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(T.w) + at(T.ldw, 0)) =
-                make_uint4(__byte_perm(r[0], r[1], 0x7632), __byte_perm(r[2], r[3], 0x7632), __byte_perm(r[4], r[5], 0x7632), __byte_perm(r[6], r[7], 0x7632));
+                for (int i = 0; i < kPer; ++i) { x.m[i] = i < count ? pm[i] : 0.f; x.v[i] = i < count ? pv[i] : 0.f; }
+            }
         } else {
+            const uint8_t *pm = reinterpret_cast<const uint8_t *>(T.m) + e0, *pv = reinterpret_cast<const uint8_t *>(T.v) + e0;
+            x.mc = x.vc = make_uint2(0, 0);
+            x.m_exp = x.v_exp = 0;
+            if (whole) {
+                x.mc = *reinterpret_cast<const uint2 *>(pm); x.vc = *reinterpret_cast<const uint2 *>(pv);
+            } else {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (i < count) reinterpret_cast<uint16_t *>(T.w)[at(T.ldw, i)] = (uint16_t)(r[i] >> 16);
+                for (int i = 0; i < kPer; ++i)
+                    if (i < count) {
+                        (i < 4 ? x.mc.x : x.mc.y) |= (uint32_t)pm[i] << (8 * (i & 3));
+                        (i < 4 ? x.vc.x : x.vc.y) |= (uint32_t)pv[i] << (8 * (i & 3));
+                    }
+            }
+            if (count) { x.m_exp = T.m_exp[e0 >> 7]; x.v_exp = T.v_exp[e0 >> 7]; }
+        }
+        x.keep = 0xFFu;
+        if (T.mask && count) {
+            if (kPlain || T.bytes) {
+                x.keep = reinterpret_cast<const uint8_t *>(T.mask + row * T.wpr)[col >> 3];
+            } else {
+                int64_t r = row;
+                uint32_t c = col;
+                x.keep = 0;
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (i < count) {
+                        x.keep |= (T.mask[r * T.wpr + (c >> 5)] >> (c & 31) & 1u) << i;
+                        if (++c == T.k) { c = 0; ++r; }
+                    }
+            }
         }
     }
-    if constexpr (!kNarrow) {
-        float *pm = reinterpret_cast<float *>(T.m) + e0, *pv = reinterpret_cast<float *>(T.v) + e0;
-        if (whole) {
-            store8(pm, m); store8(pv, v);
+
+    __device__ __forceinline__ void update(Eight<kNarrow, kW32> &x, const AdamScalars &s, const Factors &f) const {
+        // Where the mask has no bit: zeros go in and zeros come out (eps is above 0).
+        if (T.mask) {
+            const uint2 b = bytes_of_bits(x.keep);
+            if constexpr (kNarrow) { x.mc.x &= b.x; x.mc.y &= b.y; x.vc.x &= b.x; x.vc.y &= b.y; }
+            uint32_t pairs[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) pairs[i] = __byte_perm(i < 2 ? b.x : b.y, 0, i & 1 ? 0x3322 : 0x1100);
+            if constexpr (!kW32) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x.w[i] &= pairs[i];
+            }
+            if (!T.g32) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x.g[i] &= pairs[i];
+            }
+            if (kW32 || !kNarrow || T.g32) {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (!(x.keep >> i & 1u)) {
+                        if constexpr (kW32) x.w[i] = 0;
+                        if constexpr (!kNarrow) x.m[i] = x.v[i] = 0.f;
+                        if (T.g32) x.g[i] = 0;
+                    }
+            }
+        }
+        float w[kPer], g[kPer], m[kPer], root[kPer], v[kPer];
+        uint32_t h[kPer];
+        uint32_t spread = f.spread;
+        if (kNarrow || !kW32)
+            if (e0 >> 32) spread = mix((uint32_t)(e0 >> 32) ^ f.key);
+        // (e0 is a multiple of 8: the hash of e0 + i differs from that of e0 in three low bits until its first product)
+        const uint32_t first = ((uint32_t)e0 ^ spread) ^ (((uint32_t)e0 ^ spread) >> 16);
+        float v_beyond = 1.f, m_scale = 0.f, v_scale = 0.f;
+        if constexpr (kNarrow) { m_scale = s.beta1 * power_of(x.m_exp); v_scale = s.root_beta2 * power_120(x.v_exp, &v_beyond); }
+        if (T.g32) {
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) g[i] = __uint_as_float(x.g[i]);
         } else {
 #pragma unroll
-            for (int i = 0; i < kPer; ++i)
-                if (i < count) { pm[i] = m[i]; pv[i] = v[i]; }
+            for (int i = 0; i < kPer; ++i) g[i] = __uint_as_float(i & 1 ? x.g[i / 2] & 0xFFFF0000u : x.g[i / 2] << 16);
         }
-    } else {
+#pragma unroll
+        for (int i = 0; i < kPer; ++i) {
+            if constexpr (kW32) w[i] = __uint_as_float(x.w[i]);
+            else w[i] = __uint_as_float(i & 1 ? x.w[i / 2] & 0xFFFF0000u : x.w[i / 2] << 16);
+            if constexpr (kNarrow) {
+                if ((i & 1) == 0) {
+                    const float2 two = values_m(i < 4 ? x.mc.x : x.mc.y, i >> 1 & 1);
+                    m[i] = two.x * m_scale; m[i + 1] = two.y * m_scale;
+                }
+                float u = root_bits(i < 4 ? x.vc.x : x.vc.y, i & 3, s.by.p19) * v_scale;
+                if (v_beyond != 1.f) u *= v_beyond;
+                v[i] = u * u;
+            } else {
+                m[i] = x.m[i]; v[i] = x.v[i];
+            }
+            const float gi = g[i] * f.grad_scale;
+            // (8-bit states come with the factors beta1 and beta2 in them)
+            m[i] = fmaf(s.one_beta1, gi, kNarrow ? m[i] : s.beta1 * m[i]);
+            v[i] = fmaf(s.one_beta2 * gi, gi, kNarrow ? v[i] : s.beta2 * v[i]);
+            root[i] = sqrt_near(v[i]);
+            w[i] = w[i] * f.decay - f.step_size * (m[i] * reciprocal_near(root[i] * f.root_scale + s.eps));
+            if constexpr (kNarrow || !kW32) h[i] = mix_rest(first ^ (uint32_t)i);
+        }
+
+        if constexpr (kW32) {
+            if (vec) {
+                store8(reinterpret_cast<float *>(T.w) + at(T.ldw, 0), w);
+                if (T.copy)
+                    *reinterpret_cast<uint4 *>(T.copy + at(T.ldc, 0)) =
+                        make_uint4(nearest2(w[0], w[1]), nearest2(w[2], w[3]), nearest2(w[4], w[5]), nearest2(w[6], w[7]));
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (i < count) {
+                        reinterpret_cast<float *>(T.w)[at(T.ldw, i)] = w[i];
+                        if (T.copy) T.copy[at(T.ldc, i)] = nearest(w[i]);
+                    }
+            }
+        } else {
+            uint32_t r[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) r[i] = random2(w[2 * i], w[2 * i + 1], h[2 * i], h[2 * i + 1]);
+            if (vec) {
+                *reinterpret_cast<uint4 *>(reinterpret_cast<uint16_t *>(T.w) + at(T.ldw, 0)) = make_uint4(r[0], r[1], r[2], r[3]);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (i < count) reinterpret_cast<uint16_t *>(T.w)[at(T.ldw, i)] = (uint16_t)(r[i / 2] >> (16 * (i & 1)));
+            }
+        }
+        if constexpr (!kNarrow) {
+            float *pm = reinterpret_cast<float *>(T.m) + e0, *pv = reinterpret_cast<float *>(T.v) + e0;
+            if (whole) {
+                store8(pm, m); store8(pv, v);
+            } else {
+#pragma unroll
+                for (int i = 0; i < kPer; ++i)
+                    if (i < count) { pm[i] = m[i]; pv[i] = v[i]; }
+            }
+        } else {
+            hold(m, root, h, s);
+        }
+    }
+
+    // m and sqrt(v) to their 8-bit forms; the 16 threads of a block come here together.
+    __device__ __forceinline__ void hold(float (&m)[kPer], float (&root)[kPer], const uint32_t (&h)[kPer], const AdamScalars &s) const {
         // (elements beyond the tensor's last one are zero: g, m and v were not read there)
         float am = 0.f, av = 0.f;
 #pragma unroll
-        for (int i = 0; i < kPer; ++i) { am = fmaxf(am, fabsf(m[i])); av = fmaxf(av, root[i]); }
-        if (bad != 0.f || !(am <= 3.402823466e38f) || !(av <= 3.402823466e38f)) {       // what is not finite is held as 0 (NaN in m or root is one in w)
+        for (int i = 0; i < kPer; ++i) { am = max_nan(am, fabsf(m[i])); av = max_nan(av, root[i]); }
+        if (!(am <= kLargest) || !(av <= kLargest)) {                     // what is not finite is held as 0
             am = av = 0.f;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                if (!(fabsf(m[i]) <= 3.402823466e38f)) m[i] = 0.f;
-                if (!(root[i] <= 3.402823466e38f)) root[i] = 0.f;
+                if (!(fabsf(m[i]) <= kLargest)) m[i] = 0.f;
+                if (!(root[i] <= kLargest)) root[i] = 0.f;
                 am = fmaxf(am, fabsf(m[i])); av = fmaxf(av, root[i]);
             }
         }
@@ -334,26 +396,27 @@ __device__ __forceinline__ void eight(const AdamTensor &T, const AdamScalars &s,
         // 2^-E 2^-120 in one factor; where that is below fp32's range, the values come down by 2^-120 first
         float down_m = power_of(134u - min(em, 133u)), down_v = power_of(134u - min(ev, 133u));
         if (em > 133u || ev > 133u) {
-            const float first_m = em > 133u ? 0x1p-120f : 1.f, first_v = ev > 133u ? 0x1p-120f : 1.f;
+#pragma unroll
+            for (int i = 0; i < kPer; ++i) {
+                if (em > 133u) m[i] *= 0x1p-120f;
+                if (ev > 133u) root[i] = root[i] > 0.f ? fmaxf(root[i] * 0x1p-120f, 0x1p-126f) : 0.f;
+            }
             if (em > 133u) down_m = power_of(254u - em);
             if (ev > 133u) down_v = power_of(254u - ev);
-#pragma unroll
-            for (int i = 0; i < kPer; ++i) { m[i] *= first_m; root[i] *= first_v; }
         }
-        uint32_t cm[kPer], cv[kPer];                          // codes as top bytes
+        uint32_t cm[kPer], cv[kPer];                              // codes as top bytes
 #pragma unroll
         for (int i = 0; i < kPer; ++i) {
             // 20 (19) bits below the code, of which the hash gives the upper ten (eleven) and the one below them is set
             cm[i] = (((h[i] * s.by.p1 + 1u) & 0x7FFu) * s.by.p9 + __float_as_uint(m[i] * down_m)) * s.by.p4;
             const uint32_t t = ((h[i] >> 9 & 0xFFEu) | 1u) * s.by.p7 + __float_as_uint(root[i] * down_v);
-            cv[i] = max(t, __float_as_uint(__saturatef(root[i] * 0x1p80f) * 0x1p-130f)) * s.by.p5;             // at least 1 where root is above 0
+            cv[i] = max(t, min(__float_as_uint(root[i]), 1u << 19)) * s.by.p5;                              // at least 1 where root is above 0 (it is 2^-126 or more)
         }
-        mc.x = top_bytes(cm[0], cm[1], cm[2], cm[3]);
-        mc.y = top_bytes(cm[4], cm[5], cm[6], cm[7]);
-        const auto sign = [&](int i) { return top_bytes(__float_as_uint(m[i]), __float_as_uint(m[i + 1]), __float_as_uint(m[i + 2]), __float_as_uint(m[i + 3])) & 0x80808080u; };
-        mc.x |= sign(0);
-        mc.y |= sign(4);
-        vc = make_uint2(top_bytes(cv[0], cv[1], cv[2], cv[3]), top_bytes(cv[4], cv[5], cv[6], cv[7]));
+        const auto sign = [&](int i) {
+            return top_bytes(__float_as_uint(m[i]), __float_as_uint(m[i + 1]), __float_as_uint(m[i + 2]), __float_as_uint(m[i + 3])) & 0x80808080u;
+        };
+        const uint2 mc = make_uint2(top_bytes(cm[0], cm[1], cm[2], cm[3]) | sign(0), top_bytes(cm[4], cm[5], cm[6], cm[7]) | sign(4));
+        const uint2 vc = make_uint2(top_bytes(cv[0], cv[1], cv[2], cv[3]), top_bytes(cv[4], cv[5], cv[6], cv[7]));
         uint8_t *pm = reinterpret_cast<uint8_t *>(T.m) + e0, *pv = reinterpret_cast<uint8_t *>(T.v) + e0;
         if (whole) {
             *reinterpret_cast<uint2 *>(pm) = mc; *reinterpret_cast<uint2 *>(pv) = vc;
@@ -367,7 +430,7 @@ __device__ __forceinline__ void eight(const AdamTensor &T, const AdamScalars &s,
         }
         if ((threadIdx.x & 15) == 0 && count) { T.m_exp[e0 >> 7] = (uint8_t)em; T.v_exp[e0 >> 7] = (uint8_t)ev; }
     }
-}
+};
 
 template <bool kNarrow, bool kW32, int CAP>
 __global__ void __launch_bounds__(kAdamThreads, kNarrow ? 5 : 4)
@@ -375,9 +438,30 @@ adamw_kernel(const __grid_constant__ Batch<AdamTensor, CAP> b, const __grid_cons
     wait_for_prerequisites();
     const int l = b.find(blockIdx.x);
     const AdamTensor &T = b.layer[l];
-    const int64_t first = (int64_t)(blockIdx.x - b.first[l]) * kPiece;
-    if (T.plain && first + kPiece <= T.total) eight<kNarrow, kW32, true>(T, s, first + threadIdx.x * kPer);
-    else eight<kNarrow, kW32, false>(T, s, first + threadIdx.x * kPer);
+    const int64_t first = (int64_t)(blockIdx.x - b.first[l]) * kPiece, e0 = first + threadIdx.x * kPer;
+    Factors f{s.decay, s.step_size, s.root_scale, s.d_grad_scale ? *s.d_grad_scale : 1.f, T.key, T.spread};
+    if (s.d_step || s.d_lr) {
+        const float lr = s.d_lr ? *s.d_lr : s.lr;
+        const float t = s.d_step ? (float)*s.d_step : 0.f;
+        // 1 - b^t = -expm1(t log b): to a rounding or two of fp32 for any t
+        if (s.d_step) {
+            f.root_scale = 1.f / sqrtf(-expm1f(t * s.log_beta2));
+            f.key = mix(mix(s.seed_key ^ (uint32_t)*s.d_step) ^ T.ordinal);
+            f.spread = mix(f.key);
+        }
+        f.step_size = s.d_step ? lr / -expm1f(t * s.log_beta1) : s.step_size / s.lr * lr;
+        f.decay = 1.f - lr * s.weight_decay;
+    }
+    Eight<kNarrow, kW32> x;
+    if (T.plain && first + kPiece <= T.total) {
+        const Piece<kNarrow, kW32, true> piece(T, e0);
+        piece.read(x);
+        piece.update(x, s, f);
+    } else {
+        const Piece<kNarrow, kW32, false> piece(T, e0);
+        piece.read(x);
+        piece.update(x, s, f);
+    }
 }
 
 __global__ void __launch_bounds__(kAdamThreads)
@@ -510,6 +594,7 @@ crisp_status_t crisp_adamw(int32_t n, const crisp_adamw_tensor_t *tensors, const
     if (p->d_lr) s.lr = 1.f;
     s.step_size = (float)((p->d_lr ? 1.0 : p->lr) * unit);
     s.root_scale = p->d_step ? 1.f : (float)(1.0 / std::sqrt(-std::expm1(t * std::log(p->beta2))));
+    s.root_beta2 = (float)std::sqrt(p->beta2);
     s.log_beta1 = (float)std::log(p->beta1); s.log_beta2 = (float)std::log(p->beta2);
     s.seed_key = mix(mix((uint32_t)p->seed) ^ (uint32_t)(p->seed >> 32));
     s.d_lr = p->d_lr; s.d_step = p->d_step; s.d_grad_scale = p->d_grad_scale;
