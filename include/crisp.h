@@ -484,6 +484,56 @@ CRISP_API crisp_status_t crisp_spmm_conv(crisp_handle_t handle, const uint16_t *
  */
 CRISP_API crisp_status_t crisp_set_epilogue(crisp_handle_t handle, const float *d_bias_f32, int32_t relu);
 
+/*
+ * The same product in 8 bits, for layers pruned in blocks of 128 x 128 (block_rows = block_k = 128, any n:m; UNSUPPORTED otherwise): weights and
+ * activations are e4m3 floats with a power-of-two scale for each block of 128, kept as its exponent (E8M0), and the tensor cores apply the scales:
+ *
+ *   Y[r, c] = act( sum over kept blocks b of r's row tile of  2^(Ew[r/128, b] + Ex[b, c]) * sum_(k in b) qw[r, k] qx[k, c]  + bias[r] )
+ *
+ *   weights      Ew of a kept block: the smallest exponent with max |w| <= 448 * 2^Ew over what its mask keeps; qw = w * 2^-Ew, to the nearest e4m3 (even at ties)
+ *   activations  Ex of a column and 128 consecutive k (from a multiple of 128 on): the same over those, whatever the layer's mask
+ *
+ * Exponents are at least -126.  (A power of two costs no precision against a scale of 24 bits but for the smallest 2^-9 of a block's range: e4m3 is a float.)
+ * What is not finite becomes NaN (e4m3 has no infinity) and leaves its block's scale alone; a NaN of X reaches the rows of every row tile that keeps its block,
+ * also where the mask has a zero weight for it.  Accumulation is the tensor cores' fp32; bf16 Y is rounded to nearest even from it.
+ *
+ * crisp_encode8 fills d_buf (crisp_encode8_sizes bytes, 256-byte aligned) from the dense weights and the mask, as crisp_encode does; the handle refers to d_buf
+ * only.  crisp_decode8 writes the dense bf16 matrix that it stands for (zeros elsewhere).
+ */
+typedef struct crisp_handle8_s *crisp_handle8_t;
+CRISP_API crisp_status_t crisp_encode8_sizes(crisp_mask_t mask, size_t *bytes);
+CRISP_API crisp_status_t crisp_encode8(const uint16_t *d_w_bf16, int64_t ld_w, crisp_mask_t mask, void *d_buf, void *stream, crisp_handle8_t *out);
+CRISP_API crisp_status_t crisp_decode8(crisp_handle8_t h, uint16_t *d_w_dense_bf16, int64_t ld, void *stream);
+
+/*
+ * Activations in 8 bits.  x_layout 0: X is [k, ncols] with ncols contiguous, as crisp_spmm takes it (ldx >= ncols); 1: X is [ncols, k], one token a row
+ * (ldx >= k).  Any even address and pitch; 16-byte ones are faster.  d_act: crisp_quantize8_sizes bytes, 256-byte aligned, in a form of the library's own.  It holds k * ncols
+ * codes, and may be multiplied by several layers of the same k.
+ */
+CRISP_API crisp_status_t crisp_quantize8_sizes(int64_t k, int64_t ncols, size_t *bytes);
+CRISP_API crisp_status_t crisp_quantize8(const uint16_t *d_x_bf16, int64_t ldx, int32_t x_layout, int64_t k, int64_t ncols, void *d_act, void *stream);
+
+/*
+ * The product.  crisp_spmm8 quantises X into d_act (as crisp_quantize8 does, in front of the product, which begins to fetch weights meanwhile) and multiplies;
+ * crisp_spmm8_quantized multiplies what crisp_quantize8 left there, with the layer's k and the same ncols.
+ *   d_y   y_layout 0: [rows, ncols], ldy >= ncols; 1: [ncols, rows], ldy >= rows.  bf16 (y_dtype 0) or fp32 (1).  Y must not lie on X or d_act.
+ * Every number of columns from one on; a layer without kept blocks gives act(bias).  Results do not depend on what else runs.  Handles may be used by
+ * several host threads, each with its own d_act; a handle's settings are changed, its buffer is encoded anew, and it is destroyed, only while none is in such a call.
+ */
+CRISP_API crisp_status_t crisp_spmm8(crisp_handle8_t h, const uint16_t *d_x_bf16, int64_t ldx, int32_t x_layout, int64_t ncols, void *d_act, void *d_y,
+                                     int64_t ldy, int32_t y_layout, int32_t y_dtype, void *stream);
+CRISP_API crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_act, int64_t ncols, void *d_y, int64_t ldy, int32_t y_layout,
+                                               int32_t y_dtype, void *stream);
+
+/* crisp_set_epilogue, crisp_last_launch (stack: CTAs that share one tile's blocks), crisp_device_status and crisp_reset_status of an 8-bit handle, and the last two
+ * arguments of crisp_set_tuning. */
+CRISP_API crisp_status_t crisp_set_epilogue8(crisp_handle8_t h, const float *d_bias_f32, int32_t relu);
+CRISP_API crisp_status_t crisp_last_launch8(crisp_handle8_t h, crisp_launch_info_t *out);
+CRISP_API crisp_status_t crisp_device_status8(crisp_handle8_t h, void *stream, int32_t *status_out);
+CRISP_API crisp_status_t crisp_reset_status8(crisp_handle8_t h, void *stream);
+CRISP_API crisp_status_t crisp_set_tuning8(crisp_handle8_t h, uint64_t wait_limit_cycles, int32_t skip_fill);
+CRISP_API void crisp_destroy8(crisp_handle8_t h);
+
 /* Restrict crisp_spmm of this handle to one kernel family (CRISP_PATH_*), or -1 for the
  * default choice.  UNSUPPORTED if the handle's execution image cannot serve that path. */
 CRISP_API crisp_status_t crisp_set_path(crisp_handle_t h, int32_t path);

@@ -188,6 +188,18 @@ def load(path: Optional[str] = None):
         "crisp_prune_encode": [i32, P(PruneLayer), vp, P(vp), P(vp)],
         "crisp_destroy_layers": [i32, P(vp), P(vp)],
         "crisp_global_rank": [i32, P(RankLayer), C.c_double, vp, vp, vp],
+        "crisp_encode8_sizes": [vp, P(sz)],
+        "crisp_encode8": [vp, i64, vp, vp, vp, P(vp)],
+        "crisp_decode8": [vp, vp, i64, vp],
+        "crisp_quantize8_sizes": [i64, i64, P(sz)],
+        "crisp_quantize8": [vp, i64, i32, i64, i64, vp, vp],
+        "crisp_spmm8": [vp, vp, i64, i32, i64, vp, vp, i64, i32, i32, vp],
+        "crisp_spmm8_quantized": [vp, vp, i64, vp, i64, i32, i32, vp],
+        "crisp_set_epilogue8": [vp, vp, i32],
+        "crisp_last_launch8": [vp, P(LaunchInfo)],
+        "crisp_device_status8": [vp, vp, P(i32)],
+        "crisp_reset_status8": [vp, vp],
+        "crisp_set_tuning8": [vp, C.c_uint64, i32],
         "crisp_adamw": [i32, P(AdamwTensor), P(AdamwParams), vp],
         "crisp_adamw_moments": [vp, vp, vp, vp, i64, vp, vp, vp],
     }
@@ -199,6 +211,8 @@ def load(path: Optional[str] = None):
     lib.crisp_mask_destroy.restype = None
     lib.crisp_destroy.argtypes = [vp]
     lib.crisp_destroy.restype = None
+    lib.crisp_destroy8.argtypes = [vp]
+    lib.crisp_destroy8.restype = None
     lib.crisp_status_string.argtypes = [C.c_int]
     lib.crisp_status_string.restype = C.c_char_p
     try:
@@ -515,6 +529,85 @@ def crisp_destroy(handle: int):
         load().crisp_destroy(handle)
 
 
+# ------------------------------------------------------------------ the 8-bit product
+
+def crisp_encode8_sizes(mask: int) -> int:
+    out = C.c_size_t()
+    _check(load().crisp_encode8_sizes(mask, C.byref(out)), "crisp_encode8_sizes")
+    return out.value
+
+
+def crisp_encode8(d_w, ld_w: int, mask: int, d_buf, stream=None) -> int:
+    out = C.c_void_p()
+    _check(load().crisp_encode8(_ptr(d_w), ld_w, mask, _ptr(d_buf), _stream(stream), C.byref(out)), "crisp_encode8")
+    return out.value
+
+
+def crisp_decode8(handle8: int, d_w_dense, ld: int, stream=None):
+    _check(load().crisp_decode8(handle8, _ptr(d_w_dense), ld, _stream(stream)), "crisp_decode8")
+
+
+def crisp_quantize8_sizes(k: int, ncols: int) -> int:
+    out = C.c_size_t()
+    _check(load().crisp_quantize8_sizes(k, ncols, C.byref(out)), "crisp_quantize8_sizes")
+    return out.value
+
+
+def crisp_quantize8(d_x, ldx: int, x_layout: int, k: int, ncols: int, d_act, stream=None):
+    _check(load().crisp_quantize8(_ptr(d_x), ldx, x_layout, k, ncols, _ptr(d_act), _stream(stream)), "crisp_quantize8")
+
+
+def crisp_spmm8(handle8: int, d_x, ldx: int, x_layout: int, ncols: int, d_act, d_y, ldy: int, y_layout: int, y_dtype: int = 0, stream=None):
+    _check(load().crisp_spmm8(handle8, _ptr(d_x), ldx, x_layout, ncols, _ptr(d_act), _ptr(d_y), ldy, y_layout, y_dtype, _stream(stream)),
+           "crisp_spmm8")
+
+
+def crisp_spmm8_quantized(handle8: int, d_act, ncols: int, d_y, ldy: int, y_layout: int, y_dtype: int = 0, stream=None):
+    _check(load().crisp_spmm8_quantized(handle8, _ptr(d_act), ncols, _ptr(d_y), ldy, y_layout, y_dtype, _stream(stream)), "crisp_spmm8_quantized")
+
+
+def crisp_set_epilogue8(handle8: int, d_bias_f32, relu: int):
+    _check(load().crisp_set_epilogue8(handle8, _ptr(d_bias_f32), int(relu)), "crisp_set_epilogue8")
+
+
+def crisp_last_launch8(handle8: int) -> dict:
+    """Tile, grid and stages of the last 8-bit product through the handle; `stack`: CTAs that shared one tile's blocks."""
+    info = LaunchInfo()
+    _check(load().crisp_last_launch8(handle8, C.byref(info)), "crisp_last_launch8")
+    return info.as_dict()
+
+
+def crisp_device_status8(handle8: int, stream=None) -> int:
+    s = C.c_int32()
+    _check(load().crisp_device_status8(handle8, _stream(stream), C.byref(s)), "crisp_device_status8")
+    return s.value
+
+
+def crisp_reset_status8(handle8: int, stream=None):
+    _check(load().crisp_reset_status8(handle8, _stream(stream)), "crisp_reset_status8")
+
+
+def crisp_set_tuning8(handle8: int, wait_limit_cycles: int = 0, skip_fill: int = -1):
+    _check(load().crisp_set_tuning8(handle8, wait_limit_cycles, skip_fill), "crisp_set_tuning8")
+
+
+def crisp_destroy8(handle8: int):
+    if handle8:
+        load().crisp_destroy8(handle8)
+
+
+def _pitch(t) -> int:
+    """Elements from one row of a matrix to the next (torch gives a single row any stride)."""
+    return t.stride()[0] if t.shape[0] > 1 else t.shape[1]
+
+
+class Activations8:
+    """Activations in 8 bits (HybridLayer.quantize8): a buffer of the library's form that layers of the same k multiply."""
+
+    def __init__(self, k, ncols, buffer):
+        self.k, self.ncols, self.buffer = k, ncols, buffer
+
+
 # -------------------------------------------------- buffer-owning convenience wrapper
 
 class HybridLayer:
@@ -537,6 +630,9 @@ class HybridLayer:
         self.device = self.mask_buf.device                   # with its index: results lie beside the buffers, whatever device is current by then
         self.mask = 0
         self.handle = 0
+        self.handle8 = 0
+        self.buf8 = None
+        self._bias8 = None
         self.canonical_buf = None
         self.exec_buf = None
         self._gpu = self.device.index if (_network or _bind_network()) else None       # (decode makes its tensors through it)
@@ -675,6 +771,84 @@ class HybridLayer:
     def set_path(self, path: int):
         crisp_set_path(self.handle, path)
 
+    # The layer in 8 bits, beside or instead of its bf16 encoding (masks of 128 x 128 blocks).
+    def encode8(self, w, stream=None):
+        """Compress the weights under the mask to e4m3 with a scale for each kept block (crisp_encode8)."""
+        assert w.is_cuda and w.dtype == self.torch.bfloat16 and (w.stride()[1] == 1 or w.shape[1] == 1) and w.shape == (self.desc.rows, self.desc.k), \
+            "weights are a bf16 CUDA matrix of the layer's shape with consecutive columns"
+        size = crisp_encode8_sizes(self.mask)
+        if self.buf8 is None or self.buf8.numel() < size:
+            self.buf8 = self.torch.empty(size, dtype=self.torch.uint8, device=self.device)
+        old, self.handle8 = self.handle8, 0
+        crisp_destroy8(old)
+        self._bias8 = None
+        self.handle8 = crisp_encode8(w, _pitch(w), self.mask, self.buf8, stream)
+        return self
+
+    def decode8(self, stream=None):
+        """The dense bf16 weights that the 8-bit encoding stands for."""
+        w = self.torch.empty_strided((self.desc.rows, self.desc.k), (self.desc.k, 1), dtype=self.torch.bfloat16, device=self.device)
+        crisp_decode8(self.handle8, w, self.desc.k, stream)
+        return w
+
+    def quantize8(self, x, tokens=False, stream=None):
+        """X in 8 bits, for this layer and others of its k: x is [k, ncols], or with tokens=True [ncols, k]."""
+        ncols = self._columns8(x, tokens)
+        k = self.desc.k
+        act = self.torch.empty(crisp_quantize8_sizes(k, ncols), dtype=self.torch.uint8, device=self.device)
+        crisp_quantize8(x, _pitch(x), int(tokens), k, ncols, act, stream)
+        return Activations8(k, ncols, act)
+
+    def _columns8(self, x, tokens):
+        shape = x.shape
+        assert x.is_cuda and x.dtype == self.torch.bfloat16 and len(shape) == 2 and (x.stride()[1] == 1 or shape[1] == 1) and shape[1 if tokens else 0] == self.desc.k, \
+            "X is a bf16 CUDA matrix, [k, ncols] or with tokens=True [ncols, k], with consecutive elements in a row"
+        return shape[0 if tokens else 1]
+
+    def spmm8(self, x, y=None, y_dtype=0, tokens=False, stream=None):
+        """act(W X + bias) in 8 bits.  x: [k, ncols] -> Y [rows, ncols]; with tokens=True [ncols, k] -> Y [ncols, rows]; or what quantize8 returned, with tokens for
+        the layout of Y."""
+        torch, rows = self.torch, self.desc.rows
+        held = isinstance(x, Activations8)
+        ncols = x.ncols if held else self._columns8(x, tokens)
+        assert not held or x.k == self.desc.k, "activations of another k"
+        shape = (ncols, rows) if tokens else (rows, ncols)
+        dtype = torch.float32 if y_dtype else torch.bfloat16
+        if y is None:
+            y = torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=self.device)
+        else:
+            assert y.is_cuda and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1), "Y has the product's shape and type, and consecutive elements in a row"
+        if held:
+            code = _lib.crisp_spmm8_quantized(self.handle8, x.buffer.data_ptr(), ncols, y.data_ptr(), _pitch(y), int(tokens), y_dtype, _stream(stream))
+        else:
+            act = torch.empty_strided((crisp_quantize8_sizes(self.desc.k, ncols),), (1,), dtype=torch.uint8, device=self.device)
+            code = _lib.crisp_spmm8(self.handle8, x.data_ptr(), _pitch(x), int(tokens), ncols, act.data_ptr(), y.data_ptr(), _pitch(y), int(tokens),
+                                    y_dtype, _stream(stream))
+        if code:
+            raise CrispError(code, "crisp_spmm8")
+        return y
+
+    def set_epilogue8(self, bias=None, relu=False):
+        """Y = act(W X + bias) for later 8-bit products; `bias` is an fp32 CUDA tensor [rows] that this object keeps."""
+        if bias is not None:
+            assert bias.is_cuda and bias.dtype == self.torch.float32 and bias.numel() == self.desc.rows and bias.is_contiguous()
+        self._bias8 = bias
+        crisp_set_epilogue8(self.handle8, bias, 1 if relu else 0)
+        return self
+
+    def device_status8(self, stream=None) -> int:
+        return crisp_device_status8(self.handle8, stream)
+
+    def last_launch8(self) -> dict:
+        return crisp_last_launch8(self.handle8)
+
+    def set_tuning8(self, wait_limit_cycles=0, skip_fill=-1):
+        crisp_set_tuning8(self.handle8, wait_limit_cycles, skip_fill)
+        return self
+
+    def reset_status8(self, stream=None):
+        crisp_reset_status8(self.handle8, stream)
+
     def device_status(self, stream=None) -> int:
         return crisp_device_status(self.handle, stream)
 
@@ -700,8 +874,9 @@ class HybridLayer:
 
     def close(self):
         crisp_destroy(self.handle)
+        crisp_destroy8(self.handle8)
         crisp_mask_destroy(self.mask)
-        self.handle = 0
+        self.handle = self.handle8 = 0
         self.mask = 0
 
     def __del__(self):

@@ -1,0 +1,300 @@
+// Weights and activations to 8-bit floats with a power-of-two scale for each block of 128, and weights back.
+//
+//   E = the smallest exponent with max |x| <= 448 * 2^E,   q = x * 2^-E to the nearest e4m3 (even at ties)
+//
+// The scale is a power of two, so x * 2^-E is exact and the code is rounded once.  All of it moves bytes and little else: each value is read once, held in registers
+// while its block's largest one is found, and written once, in the layout of block8.h.
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+#include <cuda_fp8.h>
+
+#include "block8.h"
+
+namespace crisp {
+
+namespace {
+
+__device__ __forceinline__ float2 floats(uint32_t pair) { return make_float2(__uint_as_float(pair << 16), __uint_as_float(pair & 0xFFFF0000u)); }
+// The larger magnitudes of two pairs of bf16, as their bits.
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t pair) { return __vmaxu2(a, pair & 0x7FFF7FFFu); }
+__device__ __forceinline__ uint32_t larger_of(uint32_t a) { return max(a & 0xFFFFu, a >> 16); }
+// What is not finite becomes NaN and leaves the block's largest value alone: the pair with zeros in its place.
+__device__ __forceinline__ uint32_t finite(uint32_t pair) {
+    if ((pair & 0x7F80u) == 0x7F80u) pair &= 0xFFFF0000u;
+    if ((pair & 0x7F800000u) == 0x7F800000u) pair &= 0xFFFFu;
+    return pair;
+}
+__device__ __forceinline__ uint32_t nan_for_infinity(uint32_t pair) {
+    if ((pair & 0x7F80u) == 0x7F80u) pair |= 0x7FFFu;
+    if ((pair & 0x7F800000u) == 0x7F800000u) pair |= 0x7FFF0000u;
+    return pair;
+}
+// Biased exponent (E + 127) for a largest magnitude given as bf16 bits: its own exponent less 8, one more where its fraction is above 448's.
+__device__ __forceinline__ uint32_t exponent_of(uint32_t bits) { return (uint32_t)max((int)((bits + (0x7Fu - 0x60u)) >> 7) - 8, 1); }
+__device__ __forceinline__ uint32_t codes2(uint32_t pair, float down) {
+    const float2 v = floats(pair);
+    return __nv_cvt_float2_to_fp8x2(make_float2(v.x * down, v.y * down), __NV_SATFINITE, __NV_E4M3);
+}
+__device__ __forceinline__ float power_of(uint32_t biased) { return __uint_as_float(biased << 23); }
+
+// -------------------------------------------------------------------------------------------------------------- weights
+
+// One CTA a kept block: thread t takes eight columns (t % 16) of rows t / 16, + 16, ...
+__global__ void __launch_bounds__(256)
+encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_blk_col, const uint32_t *nm_bits, int32_t *blk_col, uint8_t *exps, uint8_t *image,
+               uint32_t *header, int vec_ok) {
+    __shared__ uint32_t largest[8];
+    chain_kernels();
+    const int slot = blockIdx.x, rt = slot / g.kkeep, kb = mask_blk_col[slot];
+    const int chunk = threadIdx.x & 15, row0 = threadIdx.x >> 4;
+    const int64_t col = (int64_t)kb * 128 + chunk * 8;
+    const bool vec = vec_ok && col + 8 <= g.k;
+    uint32_t x[8][4], top = 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int64_t row = (int64_t)rt * 128 + row0 + 16 * i;
+        uint32_t keep = 0;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) x[i][j] = 0;
+        if (row < g.rows) {
+            keep = reinterpret_cast<const uint8_t *>(nm_bits + row * g.wpr)[kb * 16 + chunk];
+            const uint16_t *p = w + row * ld + col;
+            if (vec) {
+                const uint4 v = *reinterpret_cast<const uint4 *>(p);
+                x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (col + j < g.k) x[i][j / 2] |= (uint32_t)p[j] << (16 * (j & 1));
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const uint32_t two = keep >> (2 * j) & 3u;
+            x[i][j] &= (two & 1u ? 0xFFFFu : 0u) | (two & 2u ? 0xFFFF0000u : 0u);
+            top = larger(top, x[i][j]);
+        }
+    }
+    if (__syncthreads_or(larger_of(top) >= 0x7F80u)) {
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                top = larger(top, finite(x[i][j]));
+                x[i][j] = nan_for_infinity(x[i][j]);
+            }
+    }
+    top = __reduce_max_sync(0xFFFFFFFFu, larger_of(top));
+    if ((threadIdx.x & 31) == 0) largest[threadIdx.x >> 5] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = max(top, largest[i]);
+    const uint32_t e = exponent_of(top);
+    const float down = power_of(254u - e);
+    uint8_t *entry = image + (int64_t)slot * kEntry8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int row = row0 + 16 * i;
+        uint8_t *at = entry + (row >> 3) * 1024 + (row & 7) * 128 + (((chunk >> 1) ^ (row & 7)) << 4) + (chunk & 1) * 8;
+        *reinterpret_cast<uint2 *>(at) = make_uint2(codes2(x[i][0], down) | codes2(x[i][1], down) << 16, codes2(x[i][2], down) | codes2(x[i][3], down) << 16);
+    }
+    if (threadIdx.x < 128) reinterpret_cast<uint32_t *>(entry + kTile8)[threadIdx.x] = e * 0x01010101u;
+    if (threadIdx.x == 0) { blk_col[slot] = kb; exps[slot] = (uint8_t)e; }
+    if (slot == 0 && threadIdx.x < 64) header[threadIdx.x] = 0;
+}
+
+// One CTA a block of the dense matrix, kept or not.
+__global__ void __launch_bounds__(256)
+decode8_kernel(Geometry g, const int32_t *blk_col, const uint8_t *exps, const uint8_t *image, uint16_t *w, int64_t ld, int vec_ok) {
+    __shared__ int found;
+    chain_kernels();
+    const int rt = blockIdx.x / g.nblk, kb = blockIdx.x - rt * g.nblk;
+    if (threadIdx.x == 0) found = -1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < g.kkeep; i += 256)
+        if (blk_col[rt * g.kkeep + i] == kb) found = rt * g.kkeep + i;
+    __syncthreads();
+    const int slot = found;
+    const int chunk = threadIdx.x & 15, row0 = threadIdx.x >> 4;
+    const int64_t col = (int64_t)kb * 128 + chunk * 8;
+    const float up = slot < 0 ? 0.f : power_of(exps[slot]);
+    const uint8_t *entry = image + (int64_t)slot * kEntry8;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int r = row0 + 16 * i;
+        const int64_t row = (int64_t)rt * 128 + r;
+        if (row >= g.rows || col >= g.k) continue;
+        uint32_t out[4] = {};
+        if (slot >= 0) {
+            const uint2 c = *reinterpret_cast<const uint2 *>(entry + (r >> 3) * 1024 + (r & 7) * 128 + (((chunk >> 1) ^ (r & 7)) << 4) + (chunk & 1) * 8);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((j < 2 ? c.x : c.y) >> (16 * (j & 1))), __NV_E4M3);
+                const float2 v = __half22float2(__half2(h));
+                const __nv_bfloat162 b = __floats2bfloat162_rn(v.x * up, v.y * up);
+                out[j] = *reinterpret_cast<const uint32_t *>(&b);
+            }
+        }
+        uint16_t *p = w + row * ld + col;
+        if (vec_ok && col + 8 <= g.k) {
+            *reinterpret_cast<uint4 *>(p) = make_uint4(out[0], out[1], out[2], out[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (col + j < g.k) p[j] = (uint16_t)(out[j / 2] >> (16 * (j & 1)));
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------------------- activations
+
+__device__ __forceinline__ void put_scale(uint8_t *scales, int64_t chunks, int64_t kb, int64_t col, uint32_t e) {
+    *reinterpret_cast<uint32_t *>(scales + (kb * chunks + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4) = e * 0x01010101u;
+}
+
+// X [ncols, k]: a CTA takes eight columns (tokens) and four k-blocks; 16 threads a block of one column, eight values each.
+__global__ void __launch_bounds__(256)
+quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
+                       int vec_ok) {
+    wait_for_prerequisites();
+    launch_dependents();                     // (a product behind this one fetches weights meanwhile: all before this kernel has finished)
+    const int64_t quads = (nblk + 3) / 4;
+    const int64_t group = blockIdx.x / quads, quad = blockIdx.x - group * quads;
+    const int lane = threadIdx.x & 15, r = threadIdx.x >> 4 & 7, side = threadIdx.x >> 7;
+    const int64_t col = group * 8 + r;
+    uint32_t v[2][4], top[2] = {0, 0};
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int64_t at = (quad * 4 + side * 2 + i) * 128 + lane * 8;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[i][j] = 0;
+        if (col < ncols && at < k) {
+            const uint16_t *p = x + col * ldx + at;
+            if (vec_ok && at + 8 <= k) {
+                const uint4 u = *reinterpret_cast<const uint4 *>(p);
+                v[i][0] = u.x; v[i][1] = u.y; v[i][2] = u.z; v[i][3] = u.w;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (at + j < k) v[i][j / 2] |= (uint32_t)p[j] << (16 * (j & 1));
+            }
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const int64_t kb = quad * 4 + side * 2 + i;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top[i] = larger(top[i], v[i][j]);
+        if (__any_sync(0xFFFFFFFFu, larger_of(top[i]) >= 0x7F80u)) {
+            top[i] = 0;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                top[i] = larger(top[i], finite(v[i][j]));
+                v[i][j] = nan_for_infinity(v[i][j]);
+            }
+        }
+        uint32_t t = larger_of(top[i]);
+#pragma unroll
+        for (int d = 8; d; d >>= 1) t = max(t, __shfl_xor_sync(0xFFFFFFFFu, t, d));
+        const uint32_t e = exponent_of(t);
+        const float down = power_of(254u - e);
+        if (kb >= nblk) continue;            // (the whole warp: its two columns share the k-block)
+        uint8_t *at = codes + (kb * groups + group) * 1024 + r * 128 + (((lane >> 1) ^ r) << 4) + (lane & 1) * 8;
+        *reinterpret_cast<uint2 *>(at) = make_uint2(codes2(v[i][0], down) | codes2(v[i][1], down) << 16, codes2(v[i][2], down) | codes2(v[i][3], down) << 16);
+        if (lane == 0 && col < ncols) put_scale(scales, chunks, kb, col, e);
+    }
+}
+
+// X [k, ncols]: a CTA takes 64 columns of one k-block.  A warp reads 16 rows of it, a lane two neighbouring columns; the 16 values of a column in a warp are one
+// 16-byte chunk of its codes.
+__global__ void __launch_bounds__(256)
+quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
+                        int pair_ok) {
+    __shared__ uint32_t largest[8][32];
+    __shared__ __align__(16) uint8_t tile[8192];
+    wait_for_prerequisites();
+    launch_dependents();
+    const int64_t kb = blockIdx.x % nblk, c0 = (int64_t)(blockIdx.x / nblk) * 64;
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t col = c0 + 2 * lane, row0 = kb * 128 + warp * 16;
+    uint32_t v[16], top = 0;
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        v[i] = 0;
+        if (row0 + i < k) {
+            const uint16_t *p = x + (row0 + i) * ldx + col;
+            if (pair_ok && col + 1 < ncols) {
+                v[i] = *reinterpret_cast<const uint32_t *>(p);
+            } else {
+                if (col < ncols) v[i] = p[0];
+                if (col + 1 < ncols) v[i] |= (uint32_t)p[1] << 16;
+            }
+        }
+        top = larger(top, v[i]);
+    }
+    if (larger_of(top) >= 0x7F80u) {
+        top = 0;
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            top = larger(top, finite(v[i]));
+            v[i] = nan_for_infinity(v[i]);
+        }
+    }
+    largest[warp][lane] = top;
+    __syncthreads();
+#pragma unroll
+    for (int i = 0; i < 8; ++i) top = __vmaxu2(top, largest[i][lane]);
+    const uint32_t e[2] = {exponent_of(top & 0xFFFFu), exponent_of(top >> 16)};
+    const float down[2] = {power_of(254u - e[0]), power_of(254u - e[1])};
+    uint32_t q[2][4] = {};
+#pragma unroll
+    for (int i = 0; i < 16; i += 2) {
+        const float2 a = floats(v[i]), b = floats(v[i + 1]);
+        q[0][i / 4] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a.x * down[0], b.x * down[0]), __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
+        q[1][i / 4] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a.y * down[1], b.y * down[1]), __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
+    }
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+        const int c = 2 * lane + s;
+        *reinterpret_cast<uint4 *>(tile + (c >> 3) * 1024 + (c & 7) * 128 + ((warp ^ (c & 7)) << 4)) = make_uint4(q[s][0], q[s][1], q[s][2], q[s][3]);
+        if (warp == 0 && col + s < ncols) put_scale(scales, chunks, kb, col + s, e[s]);
+    }
+    __syncthreads();
+    // the atoms lie one behind the other
+    const int64_t first = c0 >> 3;
+    const int atoms = (int)min((int64_t)8, groups - first);
+    uint4 *out = reinterpret_cast<uint4 *>(codes + (kb * groups + first) * 1024);
+    for (int i = threadIdx.x; i < atoms * 64; i += 256) out[i] = reinterpret_cast<const uint4 *>(tile)[i];
+}
+
+bool aligned16(const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; }
+
+}  // namespace
+
+cudaError_t launch_encode8(const Geometry &g, const uint16_t *w, int64_t ld, const int32_t *mask_blk_col, const uint32_t *nm_bits, uint8_t *buf,
+                           cudaStream_t st) {
+    const Image8 I = image8(g);
+    if ((int64_t)g.nrt * g.kkeep == 0) return cudaMemsetAsync(buf, 0, kAlign, st);
+    return launch_chained(encode8_kernel, (unsigned)(g.nrt * g.kkeep), 256, 0, st, g, w, ld, mask_blk_col, nm_bits, reinterpret_cast<int32_t *>(buf + I.col_off),
+                          buf + I.exp_off, buf + I.image_off, reinterpret_cast<uint32_t *>(buf), (int)aligned16(w, ld));
+}
+
+cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, int64_t ld, cudaStream_t st) {
+    const Image8 I = image8(g);
+    return launch_chained(decode8_kernel, (unsigned)(g.nrt * g.nblk), 256, 0, st, g, reinterpret_cast<const int32_t *>(buf + I.col_off), buf + I.exp_off,
+                          buf + I.image_off, w, ld, (int)aligned16(w, ld));
+}
+
+cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t k, int64_t ncols, uint8_t *act, cudaStream_t st) {
+    const Act8 a = act8(k, ncols);
+    const int64_t ctas = layout ? a.groups * ((a.nblk + 3) / 4) : a.nblk * ((ncols + 63) / 64);
+    if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
+    if (layout)
+        return launch_chained(quantize_tokens_kernel, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks, act, act + a.scale_off,
+                              (int)aligned16(x, ldx));
+    return launch_chained(quantize_columns_kernel, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks, act, act + a.scale_off,
+                          (int)(reinterpret_cast<uintptr_t>(x) % 4 == 0 && ldx % 2 == 0));
+}
+
+}  // namespace crisp

@@ -1,0 +1,616 @@
+// The 8-bit product on the tensor cores: Y = act(W X + bias) with e4m3 operands and a power-of-two scale for each block of 128 (block8.h has the layout).
+//
+//   Y[r, c] = sum over the kept blocks b of r's row tile of 2^(Ew + Ex[b, c]) sum_k qw[r, k] qx[k, c]
+//
+// tcgen05.mma.kind::mxf8f6f4.block_scale takes a scale for every row of A and column of B and each 32 of K; here the four K steps of a block share theirs, so that the
+// accumulator in tensor memory holds the scaled sum and nothing is rescaled outside.  A CTA multiplies a tile of 128 rows (one row tile of the layer, whose kept
+// blocks it walks) and up to 256 columns.  Per kept block a pipeline stage holds 16.5 KB of weights with their scales (one tiled copy of the weight buffer), the codes
+// of the columns (a contiguous piece of the activation buffer, one copy) and their scales.  Roles as in the bf16 kernel: a thread that fetches weights, one that
+// fetches activations, one that issues scale copies and MMAs, and warps that drain accumulators.
+#include <cuda.h>
+#include <cuda_bf16.h>
+
+#include <atomic>
+#include <cstring>
+#include <cstdlib>
+#include <memory>
+#include <new>
+
+#include "block8.h"
+#include "tc_common.cuh"
+
+namespace crisp {
+
+using namespace tc;
+
+struct Plan8 {                               // launch plan for one activation buffer and number of columns
+    const void *act;
+    int64_t ncols;
+    int tile;                                // columns a tile
+    CUtensorMap map_x, map_s;
+};
+
+}  // namespace crisp
+
+struct crisp_handle8_s {
+    crisp::Geometry g;
+    uint8_t *buf;
+    crisp::Epilogue epilogue;
+    unsigned long long wait_limit_cycles;
+    int skip_fill;
+    CUtensorMap map_a;
+    bool maps;                               // map_a is there (a layer without kept blocks has none)
+    std::mutex plan_lock;                    // of what follows
+    crisp::Plan8 plan;
+    crisp_launch_info_t last;
+};
+
+namespace crisp {
+
+namespace {
+
+struct Params8 {
+    const int32_t *blk_col;
+    int32_t *status;
+    void *y;
+    const float *bias;
+    int64_t ldy, ncols;
+    int64_t groups, chunks;                  // of the activation buffer
+    int rows, nrt, kkeep, num_tiles;
+    int y_layout, f32, relu, vec_ok, stages, early;
+    unsigned long long wait_limit;
+    int skip_fill;
+};
+
+template <int N>
+struct Tile8 {
+    // Chunks of 128 columns' scales that a tile can touch: tiles begin at multiples of N, so that 64-column ones and those of 192 may begin in the middle of
+    // one.  (The MMA takes the scales of B from an even column of tensor memory: a tile that began at an odd multiple of 32 raised a misaligned address.)
+    static_assert(N % 64 == 0 || N <= 32, "wider tiles begin at multiples of 64");
+    static constexpr int kChunks = N <= 128 ? 1 : 2;
+    static constexpr int kAcc = N <= 192 ? 2 : 1;
+    static constexpr int kScaleCols = 4 + 4 * kChunks;                // tensor memory columns of one set of scales
+    static constexpr uint32_t kX = 17 * 1024;                         // codes of the columns in a stage, behind the weights
+    static constexpr uint32_t kS = kX + N * 128;                      // their scales
+    static constexpr uint32_t kStage = (kS + kChunks * kScales8 + 1023) / 1024 * 1024;
+    static constexpr uint32_t kBytes = kEntry8 + N * 128 + kChunks * kScales8;
+    static constexpr int kEpi = N >= 128 ? 8 : 4;                     // draining warps
+    static constexpr int kUsed = kAcc * N + 2 * kScaleCols;
+    static constexpr int kTmemCols = kUsed <= 64 ? 64 : kUsed <= 128 ? 128 : kUsed <= 256 ? 256 : 512;
+    static constexpr uint32_t kStaging = 4096;                        // bytes a draining warp: 32 x 32 results of up to four bytes
+    static_assert(kUsed <= 512, "tensor memory is 512 columns");
+};
+
+__device__ __forceinline__ void copy_scales(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma_scaled(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc) : "memory");
+}
+// Instruction descriptor: e4m3 x e4m3, both K-major, E8M0 scales, M = 128.
+__host__ __device__ constexpr uint32_t make_idesc8(int n) { return (1u << 23) | ((uint32_t)(n >> 3) << 17) | (8u << 24); }
+
+__device__ __forceinline__ float activation(float v, int relu) { return relu && v < 0.f ? 0.f : v; }         // (a NaN stays)
+
+// One draining warp's 32 rows x 32 columns (lane = row, x[i] = column i), through its staging tile, so that the lanes write whole sectors.
+template <bool kF32>
+__device__ __forceinline__ void store_chunk8(const Params8 &p, uint8_t *stage, int lane, const float (&x)[32], int row0, int64_t col0) {
+    constexpr int kSize = kF32 ? 4 : 2, kLine = 32 * kSize;          // bytes of a staged line: a row of Y's 32 elements
+    constexpr int kVecs = kLine / 16;                                // 16-byte pieces of a line
+    const int64_t cols = min((int64_t)32, p.ncols - col0);
+    const int rows = min(32, p.rows - row0);
+    __syncwarp();
+    if (p.y_layout == 0) {
+        // a lane has a line; its pieces are swizzled so that eight lanes' writes touch different banks
+#pragma unroll
+        for (int j = 0; j < kVecs; ++j) {
+            uint4 v;
+            if constexpr (kF32) v = make_uint4(__float_as_uint(x[4 * j]), __float_as_uint(x[4 * j + 1]), __float_as_uint(x[4 * j + 2]), __float_as_uint(x[4 * j + 3]));
+            else v = make_uint4(pack_bf16(x[8 * j], x[8 * j + 1]), pack_bf16(x[8 * j + 2], x[8 * j + 3]), pack_bf16(x[8 * j + 4], x[8 * j + 5]), pack_bf16(x[8 * j + 6], x[8 * j + 7]));
+            *reinterpret_cast<uint4 *>(stage + lane * kLine + ((j ^ (kF32 ? lane & 7 : lane >> 1 & 3)) << 4)) = v;
+        }
+    } else {
+        // a line is a column; the lanes write an element of it each
+#pragma unroll
+        for (int i = 0; i < 32; ++i) {
+            if constexpr (kF32) *reinterpret_cast<float *>(stage + i * kLine + (((lane >> 2) ^ (i & 7)) << 4) + (lane & 3) * 4) = x[i];
+            else *reinterpret_cast<__nv_bfloat16 *>(stage + i * kLine + (((lane >> 3) ^ (i >> 1 & 3)) << 4) + (lane & 7) * 2) = __float2bfloat16_rn(x[i]);
+        }
+    }
+    __syncwarp();
+    const int lines = p.y_layout == 0 ? rows : (int)cols, width = p.y_layout == 0 ? (int)cols : rows;
+    uint8_t *y = reinterpret_cast<uint8_t *>(p.y) + (p.y_layout == 0 ? (int64_t)row0 * p.ldy + col0 : col0 * p.ldy + row0) * kSize;
+    const int64_t pitch = p.ldy * kSize;
+    if (p.vec_ok && width == 32) {
+#pragma unroll
+        for (int j = 0; j < kVecs; ++j) {
+            const int i = j * 32 + lane, line = i / kVecs, piece = i % kVecs;
+            if (line < lines)
+                *reinterpret_cast<uint4 *>(y + line * pitch + piece * 16) =
+                    *reinterpret_cast<const uint4 *>(stage + line * kLine + ((piece ^ (kF32 ? line & 7 : line >> 1 & 3)) << 4));
+        }
+    } else {
+        // (a line a pass, the lanes side by side)
+        for (int line = 0; line < lines; ++line) {
+            const uint8_t *from = stage + line * kLine + (((lane * kSize >> 4) ^ (kF32 ? line & 7 : line >> 1 & 3)) << 4) + (lane * kSize & 15);
+            if (lane < width) {
+                if constexpr (kF32) *reinterpret_cast<float *>(y + line * pitch + lane * 4) = *reinterpret_cast<const float *>(from);
+                else *reinterpret_cast<uint16_t *>(y + line * pitch + lane * 2) = *reinterpret_cast<const uint16_t *>(from);
+            }
+        }
+    }
+}
+
+// kSplit: the CTAs of a cluster share one tile, each walks a part of its blocks, and they add up their accumulators through distributed shared memory, in the
+// order of their ranks.
+template <int N, bool kSplit>
+__global__ void __launch_bounds__(96 + 32 * Tile8<N>::kEpi, 1)
+spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_s,
+             const __grid_constant__ Params8 p, int split) {
+    using T = Tile8<N>;
+    constexpr int kEpi = T::kEpi;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    const uint32_t ring = smem_u32(smem_raw);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t staging = ring + p.stages * T::kStage, ctrl = staging + kEpi * T::kStaging;
+    uint8_t *ctrl_gen = smem_raw + (ctrl - ring);
+    // barriers: full[s] and empty[s] (s < 12), accumulators full and empty
+    const uint32_t bar_full = ctrl, bar_empty = ctrl + 96, bar_tfull = ctrl + 192, bar_tempty = ctrl + 208;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 224);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(ctrl_gen + 228);
+    const bool aligned = (ring & 1023u) == 0;            // (swizzled operands need it; checked, not assumed)
+    if (warp == 1) {
+        tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), T::kTmemCols);
+        tmem_relinquish();
+    }
+    if (threadIdx.x == 0) {
+        if (p.kkeep > 0) { prefetch_tensormap(&map_a); prefetch_tensormap(&map_x); prefetch_tensormap(&map_s); }     // (else there are none)
+        for (int s = 0; s < p.stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        for (int a = 0; a < T::kAcc; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, kEpi); }
+        *abort_flag = aligned ? 0 : 1;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    // (p.early: the kernel in front is the one that quantised X, which began when all before it had finished: the weights and their lists are there)
+    if (!p.early) wait_for_prerequisites();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    if (p.early && warp != 0) wait_for_prerequisites();
+    const int rank = kSplit ? (int)cluster_rank() : 0;
+    const int tile0 = kSplit ? (int)blockIdx.x / split : (int)blockIdx.x, tile_step = kSplit ? p.num_tiles : (int)gridDim.x;
+    // this CTA's part of a tile's blocks
+    const int first = kSplit ? (int)((int64_t)p.kkeep * rank / split) : 0;
+    const int len = (kSplit ? (int)((int64_t)p.kkeep * (rank + 1) / split) : p.kkeep) - first;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            // ---------------------------------------------- weights, and the byte count of a stage
+            uint32_t dst = ring, full = bar_full, empty = bar_empty, ph = 0;
+            int s = 0, fill = 0;
+            bool ok = true;
+            for (int t = tile0; t < p.num_tiles && ok && !*abort_flag; t += tile_step) {
+                int row = ((t % p.nrt) * p.kkeep + first) * (int)(kEntry8 / 256);
+                for (int e = 0; e < len; ++e) {
+                    if (!mbar_wait_early(empty, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
+                    mbar_expect_tx(full, T::kBytes);
+                    if (fill++ != p.skip_fill) tma_load_2d(dst, &map_a, 0, row, full);
+                    row += kEntry8 / 256;
+                    dst += T::kStage; full += 8; empty += 8;
+                    if (++s == p.stages) { s = 0; dst = ring; full = bar_full; empty = bar_empty; ph ^= 1u; }
+                }
+            }
+        }
+        wait_for_prerequisites();                        // (it may have had nothing to wait for; the other warps have waited)
+    } else if (warp == 2 + kEpi) {
+        if (lane == 0) {
+            // ---------------------------------------------- activations and their scales
+            constexpr int kAhead = 8;
+            uint32_t dst = ring, full = bar_full, empty = bar_empty, ph = 0;
+            int s = 0, fill = 0;
+            bool ok = true;
+            for (int t = tile0; t < p.num_tiles && ok && !*abort_flag; t += tile_step) {
+                const int rt = t % p.nrt;
+                const int64_t c0 = (int64_t)(t / p.nrt) * N;
+                const int32_t *cols = p.blk_col + (int64_t)rt * p.kkeep + first;
+                int next[kAhead];
+#pragma unroll
+                for (int u = 0; u < kAhead; ++u) next[u] = u < len ? __ldcg(cols + u) : 0;
+                for (int e0 = 0; e0 < len && ok; e0 += kAhead) {
+#pragma unroll
+                    for (int u = 0; u < kAhead; ++u) {
+                        const int e = e0 + u;
+                        if (e >= len) break;
+                        const int64_t kb = next[u];
+                        if (e + kAhead < len) next[u] = __ldcg(cols + e + kAhead);
+                        if (!mbar_wait(empty, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
+                        if (fill++ != p.skip_fill) {
+                            tma_load_2d(dst + T::kX, &map_x, 0, (int)((kb * p.groups + (c0 >> 3)) * 4), full);
+                            tma_load_2d(dst + T::kS, &map_s, 0, (int)((kb * p.chunks + (c0 >> 7)) * 2), full);
+                        }
+                        dst += T::kStage; full += 8; empty += 8;
+                        if (++s == p.stages) { s = 0; dst = ring; full = bar_full; empty = bar_empty; ph ^= 1u; }
+                    }
+                }
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0) {
+            // ---------------------------------------------- scales to tensor memory, MMAs
+            constexpr uint32_t idesc = make_idesc8(N);
+            const uint64_t a0 = make_smem_desc(ring, 16, 1024, kLayoutSw128), b0 = make_smem_desc(ring + T::kX, 16, 1024, kLayoutSw128);
+            const uint64_t sa0 = make_smem_desc(ring + kTile8, 128, 128, kLayoutNone), sb0 = make_smem_desc(ring + T::kS, 128, 128, kLayoutNone);
+            const uint32_t scales = tmem + T::kAcc * N;
+            uint32_t off = 0, full = bar_full, empty = bar_empty, ph = 0, acc = 0, acc_ph = 0, set = 0;
+            int s = 0;
+            for (int t = tile0; t < p.num_tiles && !*abort_flag; t += tile_step) {
+                const int64_t c0 = (int64_t)(t / p.nrt) * N;
+                const uint32_t shift = (uint32_t)(c0 & 127) >> 5;                // of the tile's first column in its chunk of scales
+                if (!mbar_wait(bar_tempty + 8 * acc, acc_ph ^ 1u, abort_flag, p.wait_limit)) break;
+                tc_fence_after();
+                const uint32_t d = tmem + acc * N;
+                bool ok = true;
+                for (int e = 0; e < len; ++e) {
+                    if (!mbar_wait(full, ph, abort_flag, p.wait_limit)) { ok = false; break; }
+                    tc_fence_after();
+                    const uint32_t sa = scales + set * T::kScaleCols, sb = sa + 4;
+                    copy_scales(sa, sa0 + off);
+#pragma unroll
+                    for (int c = 0; c < T::kChunks; ++c) copy_scales(sb + 4 * c, sb0 + off + c * (kScales8 >> 4));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) mma_scaled(d, a0 + off + 2 * j, b0 + off + 2 * j, idesc, sa, sb + shift, (uint32_t)(e | j));
+                    set ^= 1u;
+                    mma_commit(empty);
+                    off += T::kStage >> 4; full += 8; empty += 8;
+                    if (++s == p.stages) { s = 0; off = 0; full = bar_full; empty = bar_empty; ph ^= 1u; }
+                }
+                if (!ok) break;
+                mma_commit(bar_tfull + 8 * acc);
+                if (++acc == T::kAcc) { acc = 0; acc_ph ^= 1u; }
+            }
+        }
+    } else {
+        // -------------------------------------------------- drain: tensor memory -> registers -> Y (or this CTA's part of a sum)
+        const int ew = warp - 2, q = warp & 3, part = ew >> 2;       // a warp may read the lanes of its quarter only
+        uint8_t *stage = smem_raw + (staging - ring) + ew * T::kStaging;
+        uint32_t acc = 0, acc_ph = 0;
+        for (int t = tile0; t < p.num_tiles; t += tile_step) {
+            const int row0 = (t % p.nrt) * 128 + 32 * q;
+            const int64_t c0 = (int64_t)(t / p.nrt) * N;
+            int go = 0;
+            if (lane == 0) go = !*abort_flag && mbar_wait(bar_tfull + 8 * acc, acc_ph, abort_flag, p.wait_limit);
+            go = __shfl_sync(0xFFFFFFFFu, go, 0);
+            if (!go) break;
+            tc_fence_after();
+            const uint32_t from = tmem + acc * N + ((uint32_t)(32 * q) << 16);
+            // the warp's whole share goes to registers first: the accumulator is free for the next tile while these are stored
+            constexpr int kMine = N >= 32 ? N / 32 / (kEpi / 4) : 1;         // chunks of 32 columns, next to one another
+            uint32_t r[kMine][32];
+            if (len) {
+#pragma unroll
+                for (int i = 0; i < kMine; ++i) {
+                    if constexpr (N == 16) tmem_ld16(from, r[i]);
+                    else tmem_ld32(from + 32 * (kMine * part + i), r[i]);
+                }
+                tmem_ld_wait();
+            } else {
+#pragma unroll
+                for (int i = 0; i < kMine; ++i)
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) r[i][j] = 0;
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar_tempty + 8 * acc);
+            if (++acc == T::kAcc) { acc = 0; acc_ph ^= 1u; }
+            const float bias = !kSplit && p.bias != nullptr && row0 + lane < p.rows ? p.bias[row0 + lane] : 0.f;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const int c = 32 * (kMine * part + i);
+                if constexpr (kSplit) {
+                    // (every stage has been multiplied: the ring is free)
+                    float *sum = reinterpret_cast<float *>(smem_raw);
+#pragma unroll
+                    for (int j = 0; j < 32; ++j)
+                        if (N >= 32 || j < N) sum[(c + j) * 128 + 32 * q + lane] = __uint_as_float(r[i][j]);
+                } else if (c0 + c < p.ncols && row0 < p.rows) {
+                    float x[32];
+#pragma unroll
+                    for (int j = 0; j < 32; ++j) x[j] = activation(__uint_as_float(r[i][j]) + bias, p.relu);
+                    if (p.f32) store_chunk8<true>(p, stage, lane, x, row0, c0 + c);
+                    else store_chunk8<false>(p, stage, lane, x, row0, c0 + c);
+                }
+            }
+        }
+    }
+    __syncwarp();
+    if constexpr (kSplit) {
+        // (all threads of all CTAs come here, also where a wait has run out)
+        cluster_arrive();
+        cluster_wait();
+        const int row0 = (tile0 % p.nrt) * 128;
+        const int64_t c0 = (int64_t)(tile0 / p.nrt) * N;
+        const int cols = (int)min((int64_t)N, p.ncols - c0);
+        if (warp >= 2 && warp < 2 + kEpi) {
+            const int lane128 = ((warp & 3) << 5) | lane, part = (warp - 2) >> 2;
+            const int row = row0 + lane128;
+            const float bias = p.bias != nullptr && row < p.rows ? p.bias[row] : 0.f;
+            for (int c = rank * (kEpi / 4) + part; c < cols; c += split * (kEpi / 4)) {
+                float v = 0.f;
+                for (int s = 0; s < split; ++s) v += __uint_as_float(lds32_peer(peer_address(ring + (c * 128 + lane128) * 4, s)));
+                v = activation(v + bias, p.relu);
+                if (row < p.rows && !*abort_flag) {
+                    const int64_t at = p.y_layout == 0 ? row * p.ldy + c0 + c : (c0 + c) * p.ldy + row;
+                    if (p.f32) reinterpret_cast<float *>(p.y)[at] = v;
+                    else reinterpret_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);
+                }
+            }
+        }
+        cluster_arrive();
+        cluster_wait();
+    }
+    if (warp == 2 + kEpi) launch_dependents();
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0) atomicCAS(p.status, 0, (int)(aligned ? CRISP_TIMEOUT : CRISP_CUDA_ERROR));
+        // copies that may still be in flight land before shared memory is released
+        const unsigned long long t0 = clock64();
+        while ((unsigned long long)(clock64() - t0) < 2000000ull) __nanosleep(1000);
+        __syncthreads();
+    }
+    if (warp == 1) {
+        tc_fence_after();
+        tmem_dealloc(tmem, T::kTmemCols);
+    }
+}
+
+typedef void (*Kernel8)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const Params8, int);
+
+constexpr int kMaxDevices = 64;
+
+struct Variant8 {
+    Kernel8 kern;
+    int threads, stages;
+    uint32_t smem;
+    std::atomic<bool> *configured;
+};
+
+template <int N, bool kSplit>
+Variant8 make_variant8() {
+    static std::atomic<bool> configured[kMaxDevices];
+    using T = Tile8<N>;
+    const uint32_t fixed = T::kEpi * T::kStaging + 256;
+    const int most = (int)((kSmemBudget - fixed) / T::kStage), stages = most < 12 ? most : 12;
+    return Variant8{spmm8_kernel<N, kSplit>, 96 + 32 * T::kEpi, stages, stages * T::kStage + fixed, configured};
+}
+
+template <bool kSplit>
+Variant8 variant8(int tile) {
+    switch (tile) {
+        case 16: return make_variant8<16, kSplit>();
+        case 32: return make_variant8<32, kSplit>();
+        case 64: return make_variant8<64, kSplit>();
+        case 128: return make_variant8<128, kSplit>();
+        case 192: return make_variant8<192, kSplit>();
+        default: return make_variant8<256, kSplit>();
+    }
+}
+
+// Columns a tile and CTAs that share one.
+void choose8(const Geometry &g, int64_t ncols, int sms, int *tile, int *split) {
+    int n = ncols <= 16 ? 16 : ncols <= 32 ? 32 : ncols <= 64 ? 64 : ncols <= 128 ? 128 : 192;
+    const auto tiles = [&](int w) { return (int64_t)g.nrt * ((ncols + w - 1) / w); };
+    while (n > 64 && tiles(n) < sms) n = n == 192 ? 128 : 64;
+    static const int forced = std::getenv("T8") ? std::atoi(std::getenv("T8")) : 0;
+    if (forced && n == 192) n = forced;
+    *tile = n;
+    int s = 1;
+    const int64_t have = tiles(n);
+    while (s < 8 && have * (s * 2) <= sms && s * 4 <= g.kkeep) s *= 2;
+    *split = s;
+}
+
+bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+
+// A buffer as rows of 256 bytes, loaded `rows` at a time, as it lies.
+bool make_map_bytes(CUtensorMap *map, const void *base, uint64_t bytes, uint32_t rows) { return make_map_image(map, base, bytes, rows * 256); }
+
+crisp_status_t check_product(crisp_handle8_s *h, const void *d_act, int64_t ncols, const void *d_y, int64_t ldy, int32_t y_layout, int32_t y_dtype) {
+    if (!h || !d_act || !d_y || (y_layout != 0 && y_layout != 1) || (y_dtype != 0 && y_dtype != 1)) return CRISP_INVALID_ARG;
+    if (ncols <= 0 || ldy < (y_layout ? h->g.rows : ncols)) return CRISP_BAD_SHAPE;
+    if (!aligned_to(d_act, kAlign) || !aligned_to(d_y, y_dtype ? 4 : 2)) return CRISP_INVALID_ARG;
+    // (a buffer's rows of 256 bytes are numbered in 31 bits, and so are tiles)
+    const Act8 a = act8(h->g.k, ncols);
+    if (a.total / 256 >= (1ull << 31) - 4096 || (int64_t)h->g.nrt * ((ncols + 15) / 16) > 0x7FFFFFFFll) return CRISP_UNSUPPORTED;
+    return CRISP_OK;
+}
+
+cudaError_t launch_spmm8(crisp_handle8_s *h, const void *d_act, int64_t ncols, void *d_y, int64_t ldy, int y_layout, int y_dtype, bool early, cudaStream_t st) {
+    int device = 0;
+    cudaError_t e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    if (device < 0 || device >= kMaxDevices) return cudaErrorInvalidDevice;
+    const Geometry &g = h->g;
+    int tile, split;
+    choose8(g, ncols, sm_count_of(device), &tile, &split);
+    const Act8 a = act8(g.k, ncols);
+    const Variant8 v = split > 1 ? variant8<true>(tile) : variant8<false>(tile);
+    if (!v.configured[device].load(std::memory_order_relaxed)) {
+        e = cudaFuncSetAttribute(reinterpret_cast<const void *>(v.kern), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget + 1024);
+        if (e != cudaSuccess) return e;
+        v.configured[device].store(true, std::memory_order_relaxed);
+    }
+    Plan8 plan;
+    {
+        std::lock_guard<std::mutex> hold(h->plan_lock);
+        plan = h->plan;
+    }
+    if (g.kkeep > 0 && (plan.act != d_act || plan.ncols != ncols || plan.tile != tile)) {
+        e = ensure_context(device);
+        if (e != cudaSuccess) return e;
+        plan.act = d_act; plan.ncols = ncols; plan.tile = tile;
+        const int chunks = tile <= 128 ? 1 : 2;
+        if (!make_map_bytes(&plan.map_x, d_act, a.scale_off, tile / 2) ||
+            !make_map_bytes(&plan.map_s, reinterpret_cast<const uint8_t *>(d_act) + a.scale_off, a.total - a.scale_off, 2 * chunks))
+            return cudaErrorInvalidValue;
+        std::lock_guard<std::mutex> hold(h->plan_lock);
+        h->plan = plan;
+    }
+    Params8 p{};
+    const Image8 I = image8(g);
+    p.blk_col = reinterpret_cast<const int32_t *>(h->buf + I.col_off);
+    p.status = reinterpret_cast<int32_t *>(h->buf);
+    p.y = d_y; p.bias = h->epilogue.bias; p.ldy = ldy; p.ncols = ncols; p.groups = a.groups; p.chunks = a.chunks;
+    p.rows = g.rows; p.nrt = g.nrt; p.kkeep = g.kkeep;
+    p.num_tiles = (int)((int64_t)g.nrt * ((ncols + tile - 1) / tile));
+    p.y_layout = y_layout; p.f32 = y_dtype; p.relu = h->epilogue.relu;
+    const int size = y_dtype ? 4 : 2;
+    p.vec_ok = aligned_to(d_y, 16) && ldy * size % 16 == 0;
+    p.stages = v.stages; p.early = early;
+    p.wait_limit = h->wait_limit_cycles ? h->wait_limit_cycles : kWaitLimitCycles;
+    p.skip_fill = h->skip_fill;
+    const int sms = sm_count_of(device);
+    const unsigned grid = (unsigned)(split > 1 ? p.num_tiles * split : (p.num_tiles < sms ? p.num_tiles : sms));
+    e = launch_clusters(v.kern, grid, (unsigned)v.threads, v.smem, st, (unsigned)split, h->map_a, plan.map_x, plan.map_s, p, split);
+    if (e == cudaSuccess) {
+        std::lock_guard<std::mutex> hold(h->plan_lock);
+        h->last = crisp_launch_info_t{CRISP_PATH_DENSE, tile, tile <= 192 ? 2 : 1, split, tile >= 128 ? 8 : 4, v.stages, (int32_t)grid, 0, 1};
+    }
+    return e;
+}
+
+}  // namespace
+
+}  // namespace crisp
+
+extern "C" {
+
+using namespace crisp;
+
+crisp_status_t crisp_encode8_sizes(crisp_mask_t mask, size_t *bytes) {
+    if (!mask || !bytes) return CRISP_INVALID_ARG;
+    if (mask->g.bm != 128 || mask->g.bk != 128) return CRISP_UNSUPPORTED;
+    const Image8 I = image8(mask->g);
+    if (I.total / 256 >= (1ull << 31)) return CRISP_UNSUPPORTED;
+    *bytes = I.total;
+    return CRISP_OK;
+}
+
+crisp_status_t crisp_encode8(const uint16_t *d_w_bf16, int64_t ld_w, crisp_mask_t mask, void *d_buf, void *stream, crisp_handle8_t *out) {
+    if (!out) return CRISP_INVALID_ARG;
+    *out = nullptr;
+    size_t bytes = 0;
+    const crisp_status_t bad = crisp_encode8_sizes(mask, &bytes);
+    if (bad != CRISP_OK) return bad;
+    if (!d_w_bf16 || !d_buf || !aligned_to(d_w_bf16, 2) || !aligned_to(d_buf, kAlign)) return CRISP_INVALID_ARG;
+    const Geometry &g = mask->g;
+    if (ld_w < g.k) return CRISP_BAD_SHAPE;
+    std::unique_ptr<crisp_handle8_s> h(new (std::nothrow) crisp_handle8_s);
+    if (!h) return CRISP_CUDA_ERROR;
+    h->g = g;
+    h->buf = reinterpret_cast<uint8_t *>(d_buf);
+    h->epilogue = Epilogue{nullptr, 0};
+    h->wait_limit_cycles = 0;
+    h->skip_fill = -1;
+    std::memset(&h->plan, 0, sizeof h->plan);
+    std::memset(&h->map_a, 0, sizeof h->map_a);
+    h->last = crisp_launch_info_t{-1, 0, 0, 1, 0, 0, 0, 0, 1};
+    h->maps = (int64_t)g.nrt * g.kkeep > 0;
+    if (h->maps) {
+        int device = 0;
+        if (cudaGetDevice(&device) != cudaSuccess || ensure_context(device) != cudaSuccess) return CRISP_CUDA_ERROR;
+        const Image8 I = image8(g);
+        if (!make_map_image(&h->map_a, h->buf + I.image_off, I.total - I.image_off, kEntry8)) return CRISP_CUDA_ERROR;
+    }
+    if (launch_encode8(g, d_w_bf16, ld_w, mask->d_blk_col, mask->d_nm_bits, h->buf, (cudaStream_t)stream) != cudaSuccess) return CRISP_CUDA_ERROR;
+    *out = h.release();
+    return CRISP_OK;
+}
+
+crisp_status_t crisp_decode8(crisp_handle8_t h, uint16_t *d_w_dense_bf16, int64_t ld, void *stream) {
+    if (!h || !d_w_dense_bf16 || !aligned_to(d_w_dense_bf16, 2)) return CRISP_INVALID_ARG;
+    if (ld < h->g.k) return CRISP_BAD_SHAPE;
+    return launch_decode8(h->g, h->buf, d_w_dense_bf16, ld, (cudaStream_t)stream) == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
+}
+
+crisp_status_t crisp_quantize8_sizes(int64_t k, int64_t ncols, size_t *bytes) {
+    if (!bytes) return CRISP_INVALID_ARG;
+    if (k <= 0 || ncols <= 0) return CRISP_BAD_SHAPE;
+    if (k > (int64_t)kMaxBlocksPerRowTile * 128 || ncols > ((int64_t)1 << 40)) return CRISP_UNSUPPORTED;
+    const Act8 a = act8(k, ncols);
+    if (a.total / 256 >= (1ull << 31) - 4096) return CRISP_UNSUPPORTED;
+    *bytes = a.total;
+    return CRISP_OK;
+}
+
+static crisp_status_t check_quantize(const uint16_t *d_x, int64_t ldx, int32_t x_layout, int64_t k, int64_t ncols, const void *d_act) {
+    size_t bytes = 0;
+    const crisp_status_t bad = crisp_quantize8_sizes(k, ncols, &bytes);
+    if (bad != CRISP_OK) return bad;
+    if (!d_x || !d_act || (x_layout != 0 && x_layout != 1) || !aligned_to(d_x, 2) || !aligned_to(d_act, kAlign)) return CRISP_INVALID_ARG;
+    return ldx < (x_layout ? k : ncols) ? CRISP_BAD_SHAPE : CRISP_OK;
+}
+
+crisp_status_t crisp_quantize8(const uint16_t *d_x_bf16, int64_t ldx, int32_t x_layout, int64_t k, int64_t ncols, void *d_act, void *stream) {
+    const crisp_status_t bad = check_quantize(d_x_bf16, ldx, x_layout, k, ncols, d_act);
+    if (bad != CRISP_OK) return bad;
+    const cudaError_t e = launch_quantize8(d_x_bf16, ldx, x_layout, k, ncols, reinterpret_cast<uint8_t *>(d_act), (cudaStream_t)stream);
+    return e == cudaSuccess ? CRISP_OK : e == cudaErrorInvalidValue ? CRISP_UNSUPPORTED : CRISP_CUDA_ERROR;
+}
+
+crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_act, int64_t ncols, void *d_y, int64_t ldy, int32_t y_layout, int32_t y_dtype,
+                                     void *stream) {
+    const crisp_status_t bad = check_product(h, d_act, ncols, d_y, ldy, y_layout, y_dtype);
+    if (bad != CRISP_OK) return bad;
+    return launch_spmm8(h, d_act, ncols, d_y, ldy, y_layout, y_dtype, false, (cudaStream_t)stream) == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
+}
+
+crisp_status_t crisp_spmm8(crisp_handle8_t h, const uint16_t *d_x_bf16, int64_t ldx, int32_t x_layout, int64_t ncols, void *d_act, void *d_y, int64_t ldy,
+                           int32_t y_layout, int32_t y_dtype, void *stream) {
+    crisp_status_t bad = check_product(h, d_act, ncols, d_y, ldy, y_layout, y_dtype);
+    if (bad == CRISP_OK) bad = check_quantize(d_x_bf16, ldx, x_layout, h->g.k, ncols, d_act);
+    if (bad != CRISP_OK) return bad;
+    bad = crisp_quantize8(d_x_bf16, ldx, x_layout, h->g.k, ncols, d_act, stream);
+    if (bad != CRISP_OK) return bad;
+    return launch_spmm8(h, d_act, ncols, d_y, ldy, y_layout, y_dtype, true, (cudaStream_t)stream) == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
+}
+
+crisp_status_t crisp_set_epilogue8(crisp_handle8_t h, const float *d_bias_f32, int32_t relu) {
+    if (!h || (relu != 0 && relu != 1) || !aligned_to(d_bias_f32, 4)) return CRISP_INVALID_ARG;
+    h->epilogue = Epilogue{d_bias_f32, relu};
+    return CRISP_OK;
+}
+
+crisp_status_t crisp_last_launch8(crisp_handle8_t h, crisp_launch_info_t *out) {
+    if (!h || !out) return CRISP_INVALID_ARG;
+    std::lock_guard<std::mutex> hold(h->plan_lock);
+    *out = h->last;
+    return CRISP_OK;
+}
+
+crisp_status_t crisp_device_status8(crisp_handle8_t h, void *stream, int32_t *status_out) {
+    if (!h || !status_out) return CRISP_INVALID_ARG;
+    cudaStream_t st = (cudaStream_t)stream;
+    if (cudaMemcpyAsync(status_out, h->buf, 4, cudaMemcpyDeviceToHost, st) != cudaSuccess) return CRISP_CUDA_ERROR;
+    return cudaStreamSynchronize(st) == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
+}
+
+crisp_status_t crisp_reset_status8(crisp_handle8_t h, void *stream) {
+    if (!h) return CRISP_INVALID_ARG;
+    return cudaMemsetAsync(h->buf, 0, sizeof(int32_t), (cudaStream_t)stream) == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
+}
+
+crisp_status_t crisp_set_tuning8(crisp_handle8_t h, uint64_t wait_limit_cycles, int32_t skip_fill) {
+    if (!h || skip_fill < -1) return CRISP_INVALID_ARG;
+    h->wait_limit_cycles = wait_limit_cycles;
+    h->skip_fill = skip_fill;
+    return CRISP_OK;
+}
+
+void crisp_destroy8(crisp_handle8_t h) { delete h; }
+
+}  // extern "C"

@@ -1,0 +1,313 @@
+"""Products in 8 bits on the GPU against the same in 64 bits: weights and activations as their 8-bit forms hold them (to the bit), then a plain product.
+
+Tolerances of the product.  A product of two codes has 8 bits and is exact in fp32, as is its scaling by a power of two.  The tensor cores add K of them into an fp32
+accumulator; each addition may lose a unit of the last place of the larger operand (they need not round to nearest), 2^-23 of a partial sum that is at most
+S = sum |w||x|: K 2^-23 S in the worst case, of which the first runs say how much is there; the tests allow sqrt(K) * 4 * 2^-23 S + K-independent 2^-22 S, the size of
+independent errors, for every element.  bf16 results add half a step, 2^-8... of the value: 2^-9 |y| relative to round to nearest (8 bits of significand: half a step is 2^-9
+of the power of two above, at most 2^-8 of the value)."""
+import numpy as np
+import pytest
+
+import block8_reference as ref
+from helpers import bf16_dev, to_dev
+from paper_2311_14272_b200 import workloads as wl
+
+pytestmark = pytest.mark.gpu
+
+
+def bits_of(x):
+    return wl.f32_to_bf16_bits(np.asarray(x, np.float32))
+
+
+def numbers(t):
+    return t.detach().double().cpu().numpy()
+
+
+def layer(B, torch, rows, k, n, m, keep, seed, w=None, pitch=0, odd=0):
+    rng = np.random.default_rng(seed)
+    if w is None:
+        w = rng.standard_normal((rows, k)) * np.exp(rng.standard_normal((rows, 1))) * 0.05
+    bits = bits_of(w)
+    L = B.HybridLayer(rows, k, n, m, 128, 128, keep)
+    L.build_mask(to_dev(rng.random((rows, k)).astype(np.float32), torch))
+    words = L.export_mask()[1]
+    mask = np.unpackbits(words.view(np.uint8), axis=1, bitorder="little")[:rows, :k].astype(bool)
+    whole = torch.full((rows * (k + pitch) + odd,), 9.0, dtype=torch.bfloat16, device="cuda")
+    d_w = whole[odd:].view(rows, k + pitch)[:, :k]
+    d_w.copy_(bf16_dev(bits, torch))
+    L.encode8(d_w)
+    return L, ref.weights(wl.bf16_bits_to_f32(bits).astype(np.float64), mask), mask
+
+
+def activations(rng, k, ncols):
+    x = rng.standard_normal((k, ncols)) * np.exp(rng.standard_normal((1, ncols))) * np.where(rng.random((k, 1)) < 0.02, 20, 1)
+    return bits_of(x)
+
+
+def check(y, w, x, k, f32, bias=None, relu=False):
+    want, size = w @ x, np.abs(w) @ np.abs(x)
+    if bias is not None:
+        want, size = want + bias[:, None], size + np.abs(bias)[:, None]
+    if relu:
+        want = np.maximum(want, 0.0)
+    tol = (4 * np.sqrt(k) + 2) * 2.0**-23 * size + (0 if f32 else 2.0**-8 * np.abs(want))
+    off = np.abs(y - want)
+    assert np.all(off <= tol + 1e-37), float((off / (tol + 1e-37)).max())
+
+
+@pytest.mark.parametrize("rows,k,n,m,keep", [(128, 128, 4, 4, 1.0), (256, 512, 2, 4, 0.5), (130, 200, 1, 4, 0.5), (1, 1, 4, 4, 1.0), (300, 1000, 4, 8, 0.3),
+                                              (64, 27, 2, 4, 1.0), (129, 4100, 2, 8, 0.25), (256, 384, 4, 4, 0.0)])
+@pytest.mark.parametrize("pitch,odd", [(0, 0), (8, 0), (3, 1)])
+def test_weights_are_held_to_the_bit(rows, k, n, m, keep, pitch, odd):
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, want, _ = layer(B, torch, rows, k, n, m, keep, 1, pitch=pitch, odd=odd)
+    assert np.array_equal(numbers(L.decode8()), want)
+    out = torch.full((rows, k + 5), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.crisp_decode8(L.handle8, out, k + 5)
+    assert np.array_equal(numbers(out[:, :k]), want) and torch.all(out[:, k:] == 7.0)
+
+
+@pytest.mark.parametrize("ncols", [1, 7, 16, 17, 33, 64, 100, 224, 257])
+@pytest.mark.parametrize("tokens", [False, True])
+@pytest.mark.parametrize("f32", [0, 1])
+def test_products(ncols, tokens, f32):
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    for rows, k, n, m, keep in ((128, 128, 4, 4, 1.0), (300, 1000, 2, 4, 0.5), (512, 2304, 4, 4, 1.0)):
+        L, w, _ = layer(B, torch, rows, k, n, m, keep, 2)
+        x = activations(np.random.default_rng(ncols), k, ncols)
+        held = ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64))
+        d_x = bf16_dev(x, torch)
+        y = L.spmm8(d_x.t().contiguous() if tokens else d_x, y_dtype=f32, tokens=tokens)
+        assert L.device_status8() == 0
+        check(numbers(y.t() if tokens else y), w, held, k, f32)
+
+
+@pytest.mark.parametrize("tokens", [False, True])
+@pytest.mark.parametrize("f32", [0, 1])
+@pytest.mark.parametrize("pad_x,pad_y,odd", [(1, 1, 1), (3, 5, 0), (8, 8, 0), (0, 2, 1)])
+def test_pitches_odd_addresses_and_what_lies_beside(pad_x, pad_y, odd, f32, tokens):
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    rows, k, ncols = 200, 333, 75
+    L, w, _ = layer(B, torch, rows, k, 4, 4, 0.7, 3)
+    bias = np.random.default_rng(4).standard_normal(rows).astype(np.float32)
+    L.set_epilogue8(to_dev(bias, torch), relu=True)
+    x = activations(np.random.default_rng(5), k, ncols)
+    held = ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64))
+    a, b = (ncols, k) if tokens else (k, ncols)
+    d_x = torch.full((odd + a * (b + pad_x),), float("nan"), dtype=torch.bfloat16, device="cuda")[odd:].view(a, b + pad_x)[:, :b]
+    d_x.copy_(bf16_dev(x, torch).t() if tokens else bf16_dev(x, torch))
+    a, b = (ncols, rows) if tokens else (rows, ncols)
+    whole = torch.full((odd + a * (b + pad_y) + 64,), 7.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+    y = whole[odd:odd + a * (b + pad_y)].view(a, b + pad_y)[:, :b]
+    L.spmm8(d_x, y, y_dtype=f32, tokens=tokens)
+    check(numbers(y.t() if tokens else y), w, held, k, f32, bias.astype(np.float64), True)
+    y.fill_(7.0)
+    assert torch.all(whole == 7.0)
+
+
+@pytest.mark.parametrize("rows,k,ncols,keep", [(4096, 4096, 1, 1.0), (1024, 4096, 40, 0.5), (640, 2304, 700, 0.25), (4096, 1024, 2000, 0.5), (128, 8192, 5, 1.0)])
+def test_tiles_of_every_width_and_parts(rows, k, ncols, keep):
+    """Few columns (a cluster shares a tile's blocks), waves of wide tiles, tiles that begin inside a chunk of 128 scales."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, w, _ = layer(B, torch, rows, k, 4, 4, keep, 6)
+    x = activations(np.random.default_rng(7), k, ncols)
+    held = ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64))
+    d_x = bf16_dev(x, torch).t().contiguous()
+    act = L.quantize8(d_x, tokens=True)
+    for f32 in (0, 1):
+        y = L.spmm8(d_x, tokens=True, y_dtype=f32)
+        check(numbers(y.t()), w, held, k, f32)
+        again = L.spmm8(act, tokens=True, y_dtype=f32)
+        assert torch.equal(y, again)
+    assert L.device_status8() == 0
+    info = L.last_launch8()
+    assert info["tile_cols"] <= 16 or ncols > 16
+    assert info["ctas"] <= 148 or info["stack"] == 1
+
+
+def test_no_kept_block_gives_the_bias():
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, w, _ = layer(B, torch, 200, 300, 4, 4, 0.0, 8)
+    bias = torch.linspace(-1, 1, 200, device="cuda")
+    L.set_epilogue8(bias, relu=True)
+    x = torch.full((300, 50), float("nan"), dtype=torch.bfloat16, device="cuda")
+    for ncols in (1, 50):
+        y = L.spmm8(x[:, :ncols], y_dtype=1)
+        assert torch.equal(y, bias.clamp(min=0)[:, None].expand(200, ncols))
+    assert not L.decode8().any()
+
+
+@pytest.mark.parametrize("tokens", [False, True])
+def test_what_is_not_finite_stays_in_its_column_and_its_row_tiles(tokens):
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    rows, k, ncols = 256, 512, 40
+    rng = np.random.default_rng(9)
+    w0 = rng.standard_normal((rows, k))
+    w0[5, 130], w0[200, 400] = np.nan, np.inf
+    L, w, mask = layer(B, torch, rows, k, 4, 4, 0.5, 9, w=w0)
+    xf = wl.bf16_bits_to_f32(activations(rng, k, ncols)).astype(np.float64)
+    xf[3, 4], xf[140, 7], xf[300, 9] = np.nan, np.inf, -np.inf
+    held = ref.activations(xf)
+    assert np.array_equal(numbers(L.decode8()), w, equal_nan=True)
+    d_x = bf16_dev(bits_of(xf), torch)
+    y = L.spmm8(d_x.t().contiguous() if tokens else d_x, tokens=tokens, y_dtype=1)
+    got = numbers(y.t() if tokens else y)
+    # NaN where a NaN code meets any code of its block, also a zero one
+    bad = np.zeros((rows, ncols), bool)
+    kept = np.stack([mask[rt * 128:(rt + 1) * 128].reshape(-1, k // 128, 128).any((0, 2)) for rt in range(2)])
+    for row, col in ((3, 4), (140, 7), (300, 9)):
+        for rt in range(2):
+            if kept[rt, row // 128]:
+                bad[rt * 128:(rt + 1) * 128, col] = True
+    bad[np.isnan(w).any(1)] = True
+    assert np.array_equal(np.isnan(got), bad)
+    clean_w, clean_x = np.nan_to_num(w), np.nan_to_num(held)
+    want, size = clean_w @ clean_x, np.abs(clean_w) @ np.abs(clean_x)
+    tol = (4 * np.sqrt(k) + 2) * 2.0**-23 * size + 1e-37
+    assert np.all((np.abs(got - want) <= tol) | bad)
+
+
+@pytest.mark.parametrize("power_w,power_x", [(0, -100), (-60, -60), (60, 60), (100, 20), (-120, 110)])
+def test_values_of_any_size(power_w, power_x):
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    rng = np.random.default_rng(10)
+    L, w, _ = layer(B, torch, 128, 256, 4, 4, 1.0, 10, w=rng.standard_normal((128, 256)) * 2.0**power_w)
+    x = bits_of(rng.standard_normal((256, 30)) * 2.0**power_x)
+    y = numbers(L.spmm8(bf16_dev(x, torch), y_dtype=1))
+    held = ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64))
+    size = np.abs(w) @ np.abs(held)
+    assert np.all(np.abs(y - w @ held) <= 66 * 2.0**-23 * size + 2.0**-140)
+
+
+def test_identity_gives_the_weights():
+    """One product a result: every code, scale and place shows."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, w, _ = layer(B, torch, 300, 700, 2, 4, 0.6, 11)
+    y = numbers(L.spmm8(torch.eye(700, dtype=torch.bfloat16, device="cuda"), y_dtype=1))
+    assert np.array_equal(y, w)
+
+
+def test_a_stage_that_never_fills_ends_with_a_status():
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    for ncols in (3, 600):
+        L, w, _ = layer(B, torch, 512, 2048, 4, 4, 1.0, 12)
+        x = activations(np.random.default_rng(13), 2048, ncols)
+        d_x = bf16_dev(x, torch)
+        L.set_tuning8(wait_limit_cycles=2_000_000, skip_fill=1)
+        L.spmm8(d_x)
+        assert L.device_status8() == B.TIMEOUT
+        L.set_tuning8()
+        L.reset_status8()
+        y = L.spmm8(d_x)
+        assert L.device_status8() == 0
+        check(numbers(y), w, ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64)), 2048, 0)
+
+
+def test_captured_products_and_a_layer_encoded_anew_in_between():
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, w, _ = layer(B, torch, 384, 1024, 4, 4, 1.0, 14)
+    x = torch.zeros(1024, 24, dtype=torch.bfloat16, device="cuda")
+    d_w = torch.zeros(384, 1024, dtype=torch.bfloat16, device="cuda")
+    y = torch.zeros(384, 24, dtype=torch.float32, device="cuda")
+    L.spmm8(x, y, y_dtype=1)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        again = B.crisp_encode8(d_w, 1024, L.mask, L.buf8)
+        L.spmm8(x, y, y_dtype=1)
+    rng = np.random.default_rng(15)
+    for _ in range(3):
+        wb, xb = bits_of(rng.standard_normal((384, 1024))), activations(rng, 1024, 24)
+        d_w.copy_(bf16_dev(wb, torch))
+        x.copy_(bf16_dev(xb, torch))
+        graph.replay()
+        torch.cuda.synchronize()
+        held = ref.weights(wl.bf16_bits_to_f32(wb).astype(np.float64), np.ones((384, 1024), bool))
+        check(numbers(y), held, ref.activations(wl.bf16_bits_to_f32(xb).astype(np.float64)), 1024, 1)
+    B.crisp_destroy8(again)
+
+
+def test_encode_and_multiply_in_a_row_on_a_side_stream():
+    """The product begins to fetch weights while X is quantised; an encode right in front of it has finished by then."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, _, _ = layer(B, torch, 1024, 2048, 4, 4, 1.0, 16)
+    rng = np.random.default_rng(17)
+    w = [bf16_dev(bits_of(rng.standard_normal((1024, 2048))), torch) for _ in range(2)]
+    x = [bf16_dev(activations(rng, 2048, 9), torch) for _ in range(2)]
+    want = {}
+    for i in range(2):
+        for j in range(2):
+            L.encode8(w[i])
+            torch.cuda.synchronize()
+            want[i, j] = L.spmm8(x[j])
+            torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    got = []
+    with torch.cuda.stream(side):
+        for n in range(60):
+            L.encode8(w[n % 2])
+            got.append((n % 2, n // 2 % 2, L.spmm8(x[n // 2 % 2])))
+    side.synchronize()
+    assert all(torch.equal(y, want[i, j]) for i, j, y in got)
+
+
+def test_host_threads_share_a_layer():
+    import threading
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, _, _ = layer(B, torch, 512, 1024, 4, 4, 0.5, 18)
+    rng = np.random.default_rng(19)
+    xs = [bf16_dev(activations(rng, 1024, n), torch) for n in (1, 33, 300, 64)]
+    want = [L.spmm8(x) for x in xs]
+    torch.cuda.synchronize()
+    wrong = []
+
+    def work(i):
+        stream = torch.cuda.Stream()
+        with torch.cuda.stream(stream):
+            for _ in range(40):
+                if not torch.equal(L.spmm8(xs[i]), want[i]):
+                    wrong.append(i)
+        stream.synchronize()
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(4)]
+    [t.start() for t in threads]
+    [t.join() for t in threads]
+    assert not wrong
+
+
+def test_prune_fine_tune_and_serve_in_8_bits():
+    """Mask, two steps of AdamW with 8-bit states under it, the result in 8 bits, two layers in a row for some tokens."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    rng = np.random.default_rng(20)
+    shapes = [(384, 256), (130, 384)]
+    weights = [bf16_dev(bits_of(rng.standard_normal(s) * 0.05), torch) for s in shapes]
+    net = B.PruningNetwork(shapes, 2, 4, 128, 128)
+    net.step(weights, [[to_dev(rng.standard_normal(s).astype(np.float32), torch)] for s in shapes], 0.6)
+    opt = net.optimizer(weights, state_bits=8, seed=1)
+    for _ in range(2):
+        opt.step([to_dev(rng.standard_normal(s).astype(np.float32), torch) for s in shapes])
+    x = bits_of(rng.standard_normal((256, 20)))
+    y = bf16_dev(x, torch).t().contiguous()
+    for L, w in zip(net.layers, weights):
+        L.encode8(w)
+        rows, k = w.shape
+        mask = np.unpackbits(L.export_mask()[1].view(np.uint8), axis=1, bitorder="little")[:rows, :k].astype(bool)
+        assert not numbers(w)[~mask].any()
+        held = ref.weights(numbers(w), mask)
+        assert np.array_equal(numbers(L.decode8()), held)
+        before = ref.activations(numbers(y).T)
+        y = L.set_epilogue8(None, relu=True).spmm8(y, tokens=True)
+        check(numbers(y.t()), held, before, k, 0, relu=True)
+    net.close()
