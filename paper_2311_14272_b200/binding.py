@@ -97,7 +97,7 @@ def _bind_network():
         try:
             from . import _network as module
             if getattr(module, "built_for", None) == "%s %d.%d" % (release, *sys.version_info[:2]):
-                module.bind(C.cast(lib.crisp_decode, C.c_void_p).value)
+                module.bind(*[C.cast(f, C.c_void_p).value for f in (lib.crisp_decode, lib.crisp_spmm8_sizes, lib.crisp_spmm8)])
                 _network = module
             else:
                 _network = False
@@ -193,6 +193,7 @@ def load(path: Optional[str] = None):
         "crisp_decode8": [vp, vp, i64, vp],
         "crisp_quantize8_sizes": [i64, i64, P(sz)],
         "crisp_quantize8": [vp, i64, i32, i64, i64, vp, vp],
+        "crisp_spmm8_sizes": [vp, i64, P(sz)],
         "crisp_spmm8": [vp, vp, i64, i32, i64, vp, vp, i64, i32, i32, vp],
         "crisp_spmm8_quantized": [vp, vp, i64, vp, i64, i32, i32, vp],
         "crisp_set_epilogue8": [vp, vp, i32],
@@ -268,9 +269,16 @@ def _bind_current_stream():
 _current_stream = _bind_current_stream
 
 
-def _current_device() -> int:
+def _bind_current_device():
+    """The current device, through the C function that torch.cuda.current_device() asks in the end (as _bind_current_stream has it for the stream)."""
+    global _current_device
     import torch
-    return torch.cuda.current_device()
+    torch.cuda.current_device()                  # initialises CUDA
+    _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    return _current_device()
+
+
+_current_device = _bind_current_device
 
 
 def _stream(stream) -> int:
@@ -557,6 +565,12 @@ def crisp_quantize8(d_x, ldx: int, x_layout: int, k: int, ncols: int, d_act, str
     _check(load().crisp_quantize8(_ptr(d_x), ldx, x_layout, k, ncols, _ptr(d_act), _stream(stream)), "crisp_quantize8")
 
 
+def crisp_spmm8_sizes(handle8: int, ncols: int) -> int:
+    out = C.c_size_t()
+    _check(load().crisp_spmm8_sizes(handle8, ncols, C.byref(out)), "crisp_spmm8_sizes")
+    return out.value
+
+
 def crisp_spmm8(handle8: int, d_x, ldx: int, x_layout: int, ncols: int, d_act, d_y, ldy: int, y_layout: int, y_dtype: int = 0, stream=None):
     _check(load().crisp_spmm8(handle8, _ptr(d_x), ldx, x_layout, ncols, _ptr(d_act), _ptr(d_y), ldy, y_layout, y_dtype, _stream(stream)),
            "crisp_spmm8")
@@ -594,6 +608,12 @@ def crisp_set_tuning8(handle8: int, wait_limit_cycles: int = 0, skip_fill: int =
 def crisp_destroy8(handle8: int):
     if handle8:
         load().crisp_destroy8(handle8)
+
+
+def _allocating_for(stream):
+    """A context in which torch allocates memory for the stream of a call (None: the current one; a torch stream or an address)."""
+    import torch
+    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
 
 
 def _pitch(t) -> int:
@@ -795,7 +815,8 @@ class HybridLayer:
         """X in 8 bits, for this layer and others of its k: x is [k, ncols], or with tokens=True [ncols, k]."""
         ncols = self._columns8(x, tokens)
         k = self.desc.k
-        act = self.torch.empty(crisp_quantize8_sizes(k, ncols), dtype=self.torch.uint8, device=self.device)
+        with _allocating_for(stream):
+            act = self.torch.empty(crisp_quantize8_sizes(k, ncols), dtype=self.torch.uint8, device=self.device)
         crisp_quantize8(x, _pitch(x), int(tokens), k, ncols, act, stream)
         return Activations8(k, ncols, act)
 
@@ -808,24 +829,29 @@ class HybridLayer:
     def spmm8(self, x, y=None, y_dtype=0, tokens=False, stream=None):
         """act(W X + bias) in 8 bits.  x: [k, ncols] -> Y [rows, ncols]; with tokens=True [ncols, k] -> Y [ncols, rows]; or what quantize8 returned, with tokens for
         the layout of Y."""
-        torch, rows = self.torch, self.desc.rows
+        torch, rows, k = self.torch, self.desc.rows, self.desc.k
+        if y is None and stream is None and self._gpu is not None and type(x) is torch.Tensor and self._gpu == _current_device():
+            done = _network.product8(self.handle8, x, rows, k, self._gpu, tokens, y_dtype, _current_stream())
+            if done is not None:
+                if done[0]:
+                    raise CrispError(done[0], "crisp_spmm8")
+                return done[1]
         held = isinstance(x, Activations8)
         ncols = x.ncols if held else self._columns8(x, tokens)
-        assert not held or x.k == self.desc.k, "activations of another k"
+        assert not held or x.k == k, "activations of another k"
         shape = (ncols, rows) if tokens else (rows, ncols)
         dtype = torch.float32 if y_dtype else torch.bfloat16
         if y is None:
             y = torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=self.device)
         else:
-            assert y.is_cuda and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1), "Y has the product's shape and type, and consecutive elements in a row"
+            assert y.is_cuda and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1), \
+                "Y has the product's shape and type, and consecutive elements in a row"
         if held:
-            code = _lib.crisp_spmm8_quantized(self.handle8, x.buffer.data_ptr(), ncols, y.data_ptr(), _pitch(y), int(tokens), y_dtype, _stream(stream))
-        else:
-            act = torch.empty_strided((crisp_quantize8_sizes(self.desc.k, ncols),), (1,), dtype=torch.uint8, device=self.device)
-            code = _lib.crisp_spmm8(self.handle8, x.data_ptr(), _pitch(x), int(tokens), ncols, act.data_ptr(), y.data_ptr(), _pitch(y), int(tokens),
-                                    y_dtype, _stream(stream))
-        if code:
-            raise CrispError(code, "crisp_spmm8")
+            crisp_spmm8_quantized(self.handle8, x.buffer, ncols, y, _pitch(y), int(tokens), y_dtype, stream)
+            return y
+        with _allocating_for(stream):                        # the workspace is given back when this returns: to the stream that uses it
+            act = torch.empty_strided((crisp_spmm8_sizes(self.handle8, ncols),), (1,), dtype=torch.uint8, device=self.device)
+        crisp_spmm8(self.handle8, x, _pitch(x), int(tokens), ncols, act, y, _pitch(y), int(tokens), y_dtype, stream)
         return y
 
     def set_epilogue8(self, bias=None, relu=False):

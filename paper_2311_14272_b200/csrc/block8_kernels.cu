@@ -6,36 +6,15 @@
 // while its block's largest one is found, and written once, in the layout of block8.h.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
-#include <cuda_fp8.h>
 
 #include "block8.h"
+#include "block8.cuh"
 
 namespace crisp {
 
-namespace {
+using namespace block8;
 
-__device__ __forceinline__ float2 floats(uint32_t pair) { return make_float2(__uint_as_float(pair << 16), __uint_as_float(pair & 0xFFFF0000u)); }
-// The larger magnitudes of two pairs of bf16, as their bits.
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t pair) { return __vmaxu2(a, pair & 0x7FFF7FFFu); }
-__device__ __forceinline__ uint32_t larger_of(uint32_t a) { return max(a & 0xFFFFu, a >> 16); }
-// What is not finite becomes NaN and leaves the block's largest value alone: the pair with zeros in its place.
-__device__ __forceinline__ uint32_t finite(uint32_t pair) {
-    if ((pair & 0x7F80u) == 0x7F80u) pair &= 0xFFFF0000u;
-    if ((pair & 0x7F800000u) == 0x7F800000u) pair &= 0xFFFFu;
-    return pair;
-}
-__device__ __forceinline__ uint32_t nan_for_infinity(uint32_t pair) {
-    if ((pair & 0x7F80u) == 0x7F80u) pair |= 0x7FFFu;
-    if ((pair & 0x7F800000u) == 0x7F800000u) pair |= 0x7FFF0000u;
-    return pair;
-}
-// Biased exponent (E + 127) for a largest magnitude given as bf16 bits: its own exponent less 8, one more where its fraction is above 448's.
-__device__ __forceinline__ uint32_t exponent_of(uint32_t bits) { return (uint32_t)max((int)((bits + (0x7Fu - 0x60u)) >> 7) - 8, 1); }
-__device__ __forceinline__ uint32_t codes2(uint32_t pair, float down) {
-    const float2 v = floats(pair);
-    return __nv_cvt_float2_to_fp8x2(make_float2(v.x * down, v.y * down), __NV_SATFINITE, __NV_E4M3);
-}
-__device__ __forceinline__ float power_of(uint32_t biased) { return __uint_as_float(biased << 23); }
+namespace {
 
 // -------------------------------------------------------------------------------------------------------------- weights
 
@@ -276,8 +255,12 @@ cudaError_t launch_encode8(const Geometry &g, const uint16_t *w, int64_t ld, con
                            cudaStream_t st) {
     const Image8 I = image8(g);
     if ((int64_t)g.nrt * g.kkeep == 0) return cudaMemsetAsync(buf, 0, kAlign, st);
-    return launch_chained(encode8_kernel, (unsigned)(g.nrt * g.kkeep), 256, 0, st, g, w, ld, mask_blk_col, nm_bits, reinterpret_cast<int32_t *>(buf + I.col_off),
-                          buf + I.exp_off, buf + I.image_off, reinterpret_cast<uint32_t *>(buf), (int)aligned16(w, ld));
+    begin_encode(st);
+    const cudaError_t e = launch_chained(encode8_kernel, (unsigned)(g.nrt * g.kkeep), 256, 0, st, g, w, ld, mask_blk_col, nm_bits,
+                                         reinterpret_cast<int32_t *>(buf + I.col_off), buf + I.exp_off, buf + I.image_off, reinterpret_cast<uint32_t *>(buf),
+                                         (int)aligned16(w, ld));
+    end_encode();
+    return e;
 }
 
 cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, int64_t ld, cudaStream_t st) {

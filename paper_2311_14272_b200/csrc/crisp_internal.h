@@ -265,6 +265,8 @@ int64_t conv_box(int n, int row, const ConvGeom &cv, int *tw, int *th, int *tb);
 cudaError_t launch_spmm_halo(crisp_handle_s *h, const uint16_t *d_x, void *d_y, int64_t ldy, int y_dtype, const ConvGeom &cv, int device,
                              cudaStream_t st, bool *done);
 extern EncodeCount encodes;                                   // (encode_kernels.cu)
+void begin_encode(cudaStream_t st);                           // around the launches of anything that writes a handle's weights
+void end_encode();
 // After the launch of a product: for crisp_last_launch, and for h->settled; moment: encodes.now() before it.
 void note_launch(crisp_handle_s *h, const crisp_launch_info_t &info, int64_t resident_bytes, cudaStream_t st, uint64_t moment);
 // conv == nullptr: d_x is the [k, ncols] matrix.  Otherwise d_x is the activation and ncols = batch*ho*wo.

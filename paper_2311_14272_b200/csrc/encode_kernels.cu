@@ -548,15 +548,20 @@ void count_graph(cudaStream_t st) {
 
 }  // namespace
 
-cudaError_t launch_encode(const EncodeLayer *layers, int n, cudaStream_t st) {
+void begin_encode(cudaStream_t st) {
     count_graph(st);
     encodes.begin();
+}
+void end_encode() { encodes.end(); }
+
+cudaError_t launch_encode(const EncodeLayer *layers, int n, cudaStream_t st) {
+    begin_encode(st);
     cudaError_t e = cudaSuccess;
     if (n == 1) e = encode_batch<1>(layers, 1, st);
     else
         for (int at = 0; at < n && e == cudaSuccess; at += kBatchLayers)
             e = encode_batch<kBatchLayers>(layers + at, n - at < kBatchLayers ? n - at : kBatchLayers, st);
-    encodes.end();
+    end_encode();
     return e;
 }
 

@@ -18,6 +18,8 @@
 namespace {
 
 decltype(&crisp_decode) lib_decode;
+decltype(&crisp_spmm8_sizes) lib_spmm8_sizes;
+decltype(&crisp_spmm8) lib_spmm8;
 
 // The names of attributes, made once.
 struct {
@@ -249,16 +251,53 @@ PyObject *gradients(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// bind(address of crisp_decode)
+// product8(handle, X, rows, k, GPU, tokens, y_dtype, stream) -> (status, Y), or None: not a plain matrix that the call takes.  Workspace and Y are allocated for the
+// current stream, which `stream` has to be.
+PyObject *product8(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arguments("product8", n, 8)) return nullptr;
+    long long v[8] = {};
+    for (int i = 0; i < 8; ++i)
+        if (i != 1) {
+            v[i] = PyLong_AsLongLong(args[i]);
+            if (v[i] == -1 && PyErr_Occurred()) return nullptr;
+        }
+    const at::Tensor *x = plain(args[1]);
+    const bool tokens = v[5] != 0;
+    if (!x || x->scalar_type() != at::kBFloat16 || x->get_device() != v[4] || (x->stride(1) != 1 && x->size(1) != 1) || x->size(tokens ? 1 : 0) != v[3])
+        Py_RETURN_NONE;
+    const int64_t ncols = x->size(tokens ? 0 : 1), ldx = x->size(0) > 1 ? x->stride(0) : x->size(1), ldy = tokens ? v[2] : ncols;
+    const crisp_handle8_t h = reinterpret_cast<crisp_handle8_t>((uintptr_t)v[0]);
+    size_t bytes = 0;
+    crisp_status_t s = lib_spmm8_sizes(h, ncols, &bytes);
+    const at::TensorOptions on = at::TensorOptions().device(at::Device(at::kCUDA, (at::DeviceIndex)v[4]));
+    at::Tensor y, act;
+    if (s == CRISP_OK) {
+        y = at::empty_strided({tokens ? ncols : v[2], ldy}, {ldy, 1}, on.dtype(v[6] ? at::kFloat : at::kBFloat16));
+        if (bytes) act = at::empty_strided({(int64_t)bytes}, {1}, on.dtype(at::kByte));
+        Py_BEGIN_ALLOW_THREADS
+        s = lib_spmm8(h, static_cast<const uint16_t *>(x->data_ptr()), ldx, (int32_t)tokens, ncols, bytes ? act.data_ptr() : nullptr, y.data_ptr(), ldy, (int32_t)tokens,
+                      (int32_t)v[6], reinterpret_cast<void *>((uintptr_t)v[7]));
+        Py_END_ALLOW_THREADS
+    }
+    if (s != CRISP_OK) return Py_BuildValue("lO", (long)s, Py_None);
+    Ref out(THPVariable_Wrap(std::move(y)));
+    return out.p ? Py_BuildValue("lO", (long)s, out.p) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
+// bind(addresses of crisp_decode, crisp_spmm8_sizes and crisp_spmm8)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    if (!arguments("bind", n, 1)) return nullptr;
+    if (!arguments("bind", n, 3)) return nullptr;
     lib_decode = reinterpret_cast<decltype(&crisp_decode)>(PyLong_AsVoidPtr(args[0]));
+    lib_spmm8_sizes = reinterpret_cast<decltype(&crisp_spmm8_sizes)>(PyLong_AsVoidPtr(args[1]));
+    lib_spmm8 = reinterpret_cast<decltype(&crisp_spmm8)>(PyLong_AsVoidPtr(args[2]));
     if (PyErr_Occurred()) return nullptr;
     Py_RETURN_NONE;
 }
 
 #define CRISP_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {CRISP_METHOD(bind), CRISP_METHOD(table), CRISP_METHOD(encodings), CRISP_METHOD(encoded), CRISP_METHOD(decode), CRISP_METHOD(gradients), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {CRISP_METHOD(bind), CRISP_METHOD(table), CRISP_METHOD(encodings), CRISP_METHOD(encoded), CRISP_METHOD(decode), CRISP_METHOD(gradients), CRISP_METHOD(product8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_network", nullptr, 0, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

@@ -16,12 +16,14 @@
 #include <memory>
 #include <new>
 
+#include "block8.cuh"
 #include "block8.h"
 #include "tc_common.cuh"
 
 namespace crisp {
 
 using namespace tc;
+using namespace block8;
 
 struct Plan8 {                               // launch plan for one activation buffer and number of columns
     const void *act;
@@ -41,6 +43,7 @@ struct crisp_handle8_s {
     CUtensorMap map_a;
     bool maps;                               // map_a is there (a layer without kept blocks has none)
     std::mutex plan_lock;                    // of what follows
+    crisp::Settled settled;                  // whether the next product may read the weights early
     crisp::Plan8 plan;
     crisp_launch_info_t last;
 };
@@ -52,15 +55,21 @@ namespace {
 struct Params8 {
     const int32_t *blk_col;
     int32_t *status;
+    const uint16_t *x;                       // columns that are quantised here
+    int64_t ldx;
+    int k, x_layout, x_vec;
     void *y;
     const float *bias;
     int64_t ldy, ncols;
     int64_t groups, chunks;                  // of the activation buffer
     int rows, nrt, kkeep, num_tiles;
+    int all;                                 // every block is kept: block e of the walk is block e
     int y_layout, f32, relu, vec_ok, stages, early;
     unsigned long long wait_limit;
     int skip_fill;
 };
+
+constexpr int kQuantisers = 8;
 
 template <int N>
 struct Tile8 {
@@ -144,10 +153,29 @@ __device__ __forceinline__ void store_chunk8(const Params8 &p, uint8_t *stage, i
     }
 }
 
+// Eight values of a column that the fused product quantises: k from `at` on.
+__device__ __forceinline__ uint4 fetch8(const Params8 &p, int64_t col, int at) {
+    uint32_t v[4] = {};
+    if (p.x_layout == 1) {
+        const uint16_t *x = p.x + col * p.ldx + at;
+        if (p.x_vec && at + 8 <= p.k) return *reinterpret_cast<const uint4 *>(x);
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (at + j < p.k) v[j / 2] |= (uint32_t)x[j] << (16 * (j & 1));
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (at + j < p.k) v[j / 2] |= (uint32_t)p.x[(at + j) * p.ldx + col] << (16 * (j & 1));
+    }
+    return make_uint4(v[0], v[1], v[2], v[3]);
+}
+
 // kSplit: the CTAs of a cluster share one tile, each walks a part of its blocks, and they add up their accumulators through distributed shared memory, in the
 // order of their ranks.
-template <int N, bool kSplit>
-__global__ void __launch_bounds__(96 + 32 * Tile8<N>::kEpi, 1)
+// kFused: X is not in an activation buffer.  Eight warps fetch and quantise it on the way into the pipeline's stages, a whole stage (a k-block of all columns) each,
+// so that the loads of eight stages are under way at once; each row tile's CTAs do that anew, which a few columns are worth (one launch less).
+template <int N, bool kSplit, bool kFused>
+__global__ void __launch_bounds__(32 * (2 + Tile8<N>::kEpi + (kFused ? kQuantisers : 1)), 1)
 spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_s,
              const __grid_constant__ Params8 p, int split) {
     using T = Tile8<N>;
@@ -167,13 +195,14 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         tmem_relinquish();
     }
     if (threadIdx.x == 0) {
-        if (p.kkeep > 0) { prefetch_tensormap(&map_a); prefetch_tensormap(&map_x); prefetch_tensormap(&map_s); }     // (else there are none)
-        for (int s = 0; s < p.stages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        if (p.kkeep > 0) prefetch_tensormap(&map_a);      // (else there are none)
+        if (p.kkeep > 0 && !kFused) { prefetch_tensormap(&map_x); prefetch_tensormap(&map_s); }
+        for (int s = 0; s < p.stages; ++s) { mbar_init(bar_full + 8 * s, kFused ? 2 : 1); mbar_init(bar_empty + 8 * s, 1); }
         for (int a = 0; a < T::kAcc; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, kEpi); }
         *abort_flag = aligned ? 0 : 1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    // (p.early: the kernel in front is the one that quantised X, which began when all before it had finished: the weights and their lists are there)
+    // (p.early: the weights are there.  The kernel in front is the one that quantised X, which began when all before it had finished, or settled.h says so)
     if (!p.early) wait_for_prerequisites();
     tc_fence_before();
     __syncthreads();
@@ -196,7 +225,7 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 int row = ((t % p.nrt) * p.kkeep + first) * (int)(kEntry8 / 256);
                 for (int e = 0; e < len; ++e) {
                     if (!mbar_wait_early(empty, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
-                    mbar_expect_tx(full, T::kBytes);
+                    mbar_expect_tx(full, kFused ? kEntry8 : T::kBytes);
                     if (fill++ != p.skip_fill) tma_load_2d(dst, &map_a, 0, row, full);
                     row += kEntry8 / 256;
                     dst += T::kStage; full += 8; empty += 8;
@@ -205,8 +234,73 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             }
         }
         wait_for_prerequisites();                        // (it may have had nothing to wait for; the other warps have waited)
-    } else if (warp == 2 + kEpi) {
-        if (lane == 0) {
+    } else if (warp >= 2 + kEpi) {
+        if constexpr (kFused) {
+            // ---------------------------------------------- X: half a warp a column, eight values a lane
+            constexpr int kPasses = N / 2, kAtOnce = kPasses < 8 ? kPasses : 8;
+            const int half = lane >> 4, l16 = lane & 15;
+            int s = warp - (2 + kEpi), e = s, t = tile0;         // this warp's next stage and entry
+            uint32_t ph = 0;
+            while (s >= p.stages) { s -= p.stages; ph ^= 1u; }
+            bool ok = true;
+            for (; t < p.num_tiles && ok; t += tile_step) {
+                const int64_t c0 = (int64_t)(t / p.nrt) * N;
+                const int cols = (int)min((int64_t)N, p.ncols - c0);
+                const int32_t *list = p.blk_col + (int64_t)(t % p.nrt) * p.kkeep + first;
+                for (; e < len; e += kQuantisers) {
+                    const int at = (p.all ? first + e : __ldcg(list + e)) * 128 + l16 * 8;
+                    uint8_t *stage = smem_raw + s * T::kStage;
+                    bool waited = false;
+#pragma unroll 1
+                    for (int g = 0; g < kPasses && 2 * g < cols; g += kAtOnce) {
+                        uint4 v[kAtOnce];
+#pragma unroll
+                        for (int i = 0; i < kAtOnce; ++i) {
+                            const int c = 2 * (g + i) + half;
+                            v[i] = c < cols && at < p.k ? fetch8(p, c0 + c, at) : make_uint4(0, 0, 0, 0);
+                        }
+                        if (!waited) {
+                            int go = 0;
+                            if (lane == 0) go = mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag, p.wait_limit);
+                            ok = __shfl_sync(0xFFFFFFFFu, go, 0) != 0;
+                            waited = true;
+                            if (!ok) break;
+                        }
+#pragma unroll
+                        for (int i = 0; i < kAtOnce; ++i) {
+                            if (2 * (g + i) >= cols) break;
+                            const int c = 2 * (g + i) + half;
+                            uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w}, top = 0;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) top = larger(top, x[j]);
+                            if (__any_sync(0xFFFFFFFFu, larger_of(top) >= 0x7F80u)) {
+                                top = 0;
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    top = larger(top, finite(x[j]));
+                                    x[j] = nan_for_infinity(x[j]);
+                                }
+                            }
+                            uint32_t m = larger_of(top);
+#pragma unroll
+                            for (int d = 8; d; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
+                            const uint32_t exponent = exponent_of(m);
+                            const float down = power_of(254u - exponent);
+                            *reinterpret_cast<uint2 *>(stage + T::kX + (c >> 3) * 1024 + (c & 7) * 128 + (((l16 >> 1) ^ (c & 7)) << 4) + (l16 & 1) * 8) =
+                                make_uint2(codes2(x[0], down) | codes2(x[1], down) << 16, codes2(x[2], down) | codes2(x[3], down) << 16);
+                            if (l16 == 0) *reinterpret_cast<uint32_t *>(stage + T::kS + (c & 31) * 16 + (c >> 5) * 4) = exponent * 0x01010101u;
+                        }
+                    }
+                    if (!ok) break;
+                    fence_async_smem();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar_full + 8 * s);
+                    s += kQuantisers;
+                    while (s >= p.stages) { s -= p.stages; ph ^= 1u; }
+                }
+                e -= len;                                        // (stages are numbered through the tiles)
+            }
+        } else if (lane == 0) {
             // ---------------------------------------------- activations and their scales
             constexpr int kAhead = 8;
             uint32_t dst = ring, full = bar_full, empty = bar_empty, ph = 0;
@@ -218,14 +312,14 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 const int32_t *cols = p.blk_col + (int64_t)rt * p.kkeep + first;
                 int next[kAhead];
 #pragma unroll
-                for (int u = 0; u < kAhead; ++u) next[u] = u < len ? __ldcg(cols + u) : 0;
+                for (int u = 0; u < kAhead; ++u) next[u] = u < len ? (p.all ? first + u : __ldcg(cols + u)) : 0;
                 for (int e0 = 0; e0 < len && ok; e0 += kAhead) {
 #pragma unroll
                     for (int u = 0; u < kAhead; ++u) {
                         const int e = e0 + u;
                         if (e >= len) break;
                         const int64_t kb = next[u];
-                        if (e + kAhead < len) next[u] = __ldcg(cols + e + kAhead);
+                        if (e + kAhead < len) next[u] = p.all ? first + e + kAhead : __ldcg(cols + e + kAhead);
                         if (!mbar_wait(empty, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
                         if (fill++ != p.skip_fill) {
                             tma_load_2d(dst + T::kX, &map_x, 0, (int)((kb * p.groups + (c0 >> 3)) * 4), full);
@@ -352,7 +446,7 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         cluster_arrive();
         cluster_wait();
     }
-    if (warp == 2 + kEpi) launch_dependents();
+    if (warp == 1) launch_dependents();
     tc_fence_before();
     __syncthreads();
     if (*abort_flag) {
@@ -379,13 +473,13 @@ struct Variant8 {
     std::atomic<bool> *configured;
 };
 
-template <int N, bool kSplit>
+template <int N, bool kSplit, bool kFused = false>
 Variant8 make_variant8() {
     static std::atomic<bool> configured[kMaxDevices];
     using T = Tile8<N>;
     const uint32_t fixed = T::kEpi * T::kStaging + 256;
     const int most = (int)((kSmemBudget - fixed) / T::kStage), stages = most < 12 ? most : 12;
-    return Variant8{spmm8_kernel<N, kSplit>, 96 + 32 * T::kEpi, stages, stages * T::kStage + fixed, configured};
+    return Variant8{spmm8_kernel<N, kSplit, kFused>, 32 * (2 + T::kEpi + (kFused ? kQuantisers : 1)), stages, stages * T::kStage + fixed, configured};
 }
 
 template <bool kSplit>
@@ -399,6 +493,11 @@ Variant8 variant8(int tile) {
         default: return make_variant8<256, kSplit>();
     }
 }
+
+// The products that quantise X themselves.
+bool fused8(int64_t ncols) { return ncols <= 32; }
+template <bool kSplit>
+Variant8 fused_variant8(int tile) { return tile == 16 ? make_variant8<16, kSplit, true>() : make_variant8<32, kSplit, true>(); }
 
 // Columns a tile and CTAs that share one.
 void choose8(const Geometry &g, int64_t ncols, int sms, int *tile, int *split) {
@@ -419,8 +518,8 @@ bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p
 // A buffer as rows of 256 bytes, loaded `rows` at a time, as it lies.
 bool make_map_bytes(CUtensorMap *map, const void *base, uint64_t bytes, uint32_t rows) { return make_map_image(map, base, bytes, rows * 256); }
 
-crisp_status_t check_product(crisp_handle8_s *h, const void *d_act, int64_t ncols, const void *d_y, int64_t ldy, int32_t y_layout, int32_t y_dtype) {
-    if (!h || !d_act || !d_y || (y_layout != 0 && y_layout != 1) || (y_dtype != 0 && y_dtype != 1)) return CRISP_INVALID_ARG;
+crisp_status_t check_product(crisp_handle8_s *h, const void *d_act, bool fused, int64_t ncols, const void *d_y, int64_t ldy, int32_t y_layout, int32_t y_dtype) {
+    if (!h || (!d_act && !fused) || !d_y || (y_layout != 0 && y_layout != 1) || (y_dtype != 0 && y_dtype != 1)) return CRISP_INVALID_ARG;
     if (ncols <= 0 || ldy < (y_layout ? h->g.rows : ncols)) return CRISP_BAD_SHAPE;
     if (!aligned_to(d_act, kAlign) || !aligned_to(d_y, y_dtype ? 4 : 2)) return CRISP_INVALID_ARG;
     // (a buffer's rows of 256 bytes are numbered in 31 bits, and so are tiles)
@@ -429,7 +528,9 @@ crisp_status_t check_product(crisp_handle8_s *h, const void *d_act, int64_t ncol
     return CRISP_OK;
 }
 
-cudaError_t launch_spmm8(crisp_handle8_s *h, const void *d_act, int64_t ncols, void *d_y, int64_t ldy, int y_layout, int y_dtype, bool early, cudaStream_t st) {
+// x: what the product quantises itself (columns as fused8 has them); else nullptr, and d_act holds the codes, which the kernel in front wrote if `behind`.
+cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int x_layout, const void *d_act, bool behind, int64_t ncols, void *d_y, int64_t ldy,
+                         int y_layout, int y_dtype, uint64_t moment, cudaStream_t st) {
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
@@ -438,18 +539,20 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const void *d_act, int64_t ncols, v
     int tile, split;
     choose8(g, ncols, sm_count_of(device), &tile, &split);
     const Act8 a = act8(g.k, ncols);
-    const Variant8 v = split > 1 ? variant8<true>(tile) : variant8<false>(tile);
+    const Variant8 v = x ? (split > 1 ? fused_variant8<true>(tile) : fused_variant8<false>(tile)) : split > 1 ? variant8<true>(tile) : variant8<false>(tile);
     if (!v.configured[device].load(std::memory_order_relaxed)) {
         e = cudaFuncSetAttribute(reinterpret_cast<const void *>(v.kern), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget + 1024);
         if (e != cudaSuccess) return e;
         v.configured[device].store(true, std::memory_order_relaxed);
     }
     Plan8 plan;
+    Params8 p{};
     {
         std::lock_guard<std::mutex> hold(h->plan_lock);
         plan = h->plan;
+        p.early = behind || h->settled.holds(st, moment);
     }
-    if (g.kkeep > 0 && (plan.act != d_act || plan.ncols != ncols || plan.tile != tile)) {
+    if (g.kkeep > 0 && !x && (plan.act != d_act || plan.ncols != ncols || plan.tile != tile)) {
         e = ensure_context(device);
         if (e != cudaSuccess) return e;
         plan.act = d_act; plan.ncols = ncols; plan.tile = tile;
@@ -460,8 +563,9 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const void *d_act, int64_t ncols, v
         std::lock_guard<std::mutex> hold(h->plan_lock);
         h->plan = plan;
     }
-    Params8 p{};
     const Image8 I = image8(g);
+    p.x = x; p.ldx = ldx; p.x_layout = x_layout; p.k = g.k; p.x_vec = aligned_to(x, 16) && ldx % 8 == 0;
+    p.all = g.kkeep == g.nblk;
     p.blk_col = reinterpret_cast<const int32_t *>(h->buf + I.col_off);
     p.status = reinterpret_cast<int32_t *>(h->buf);
     p.y = d_y; p.bias = h->epilogue.bias; p.ldy = ldy; p.ncols = ncols; p.groups = a.groups; p.chunks = a.chunks;
@@ -470,14 +574,20 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const void *d_act, int64_t ncols, v
     p.y_layout = y_layout; p.f32 = y_dtype; p.relu = h->epilogue.relu;
     const int size = y_dtype ? 4 : 2;
     p.vec_ok = aligned_to(d_y, 16) && ldy * size % 16 == 0;
-    p.stages = v.stages; p.early = early;
+    p.stages = v.stages;
     p.wait_limit = h->wait_limit_cycles ? h->wait_limit_cycles : kWaitLimitCycles;
     p.skip_fill = h->skip_fill;
     const int sms = sm_count_of(device);
     const unsigned grid = (unsigned)(split > 1 ? p.num_tiles * split : (p.num_tiles < sms ? p.num_tiles : sms));
-    e = launch_clusters(v.kern, grid, (unsigned)v.threads, v.smem, st, (unsigned)split, h->map_a, plan.map_x, plan.map_s, p, split);
+    const auto launch = [&] { return launch_clusters(v.kern, grid, (unsigned)v.threads, v.smem, st, (unsigned)split, h->map_a, plan.map_x, plan.map_s, p, split); };
+    e = behind ? launch() : launch_product(encodes, p, moment, launch);
     if (e == cudaSuccess) {
         std::lock_guard<std::mutex> hold(h->plan_lock);
+        if (!h->settled.holds(st, moment)) {
+            // (what is captured has not run; one name of a stream stands for another stream in every thread)
+            cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+            h->settled.note(st, moment, st != cudaStreamPerThread && cudaStreamIsCapturing(st, &capture) == cudaSuccess && capture == cudaStreamCaptureStatusNone);
+        }
         h->last = crisp_launch_info_t{CRISP_PATH_DENSE, tile, tile <= 192 ? 2 : 1, split, tile >= 128 ? 8 : 4, v.stages, (int32_t)grid, 0, 1};
     }
     return e;
@@ -547,11 +657,11 @@ crisp_status_t crisp_quantize8_sizes(int64_t k, int64_t ncols, size_t *bytes) {
     return CRISP_OK;
 }
 
-static crisp_status_t check_quantize(const uint16_t *d_x, int64_t ldx, int32_t x_layout, int64_t k, int64_t ncols, const void *d_act) {
+static crisp_status_t check_quantize(const uint16_t *d_x, int64_t ldx, int32_t x_layout, int64_t k, int64_t ncols, const void *d_act, bool fused = false) {
     size_t bytes = 0;
     const crisp_status_t bad = crisp_quantize8_sizes(k, ncols, &bytes);
     if (bad != CRISP_OK) return bad;
-    if (!d_x || !d_act || (x_layout != 0 && x_layout != 1) || !aligned_to(d_x, 2) || !aligned_to(d_act, kAlign)) return CRISP_INVALID_ARG;
+    if (!d_x || (!d_act && !fused) || (x_layout != 0 && x_layout != 1) || !aligned_to(d_x, 2) || !aligned_to(d_act, kAlign)) return CRISP_INVALID_ARG;
     return ldx < (x_layout ? k : ncols) ? CRISP_BAD_SHAPE : CRISP_OK;
 }
 
@@ -564,19 +674,29 @@ crisp_status_t crisp_quantize8(const uint16_t *d_x_bf16, int64_t ldx, int32_t x_
 
 crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_act, int64_t ncols, void *d_y, int64_t ldy, int32_t y_layout, int32_t y_dtype,
                                      void *stream) {
-    const crisp_status_t bad = check_product(h, d_act, ncols, d_y, ldy, y_layout, y_dtype);
+    const uint64_t moment = encodes.now();
+    const crisp_status_t bad = check_product(h, d_act, false, ncols, d_y, ldy, y_layout, y_dtype);
     if (bad != CRISP_OK) return bad;
-    return launch_spmm8(h, d_act, ncols, d_y, ldy, y_layout, y_dtype, false, (cudaStream_t)stream) == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
+    return launch_spmm8(h, nullptr, 0, 0, d_act, false, ncols, d_y, ldy, y_layout, y_dtype, moment, (cudaStream_t)stream) == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
+}
+
+crisp_status_t crisp_spmm8_sizes(crisp_handle8_t h, int64_t ncols, size_t *act_bytes) {
+    if (!h || !act_bytes) return CRISP_INVALID_ARG;
+    const crisp_status_t bad = crisp_quantize8_sizes(h->g.k, ncols, act_bytes);
+    if (bad == CRISP_OK && fused8(ncols)) *act_bytes = 0;
+    return bad;
 }
 
 crisp_status_t crisp_spmm8(crisp_handle8_t h, const uint16_t *d_x_bf16, int64_t ldx, int32_t x_layout, int64_t ncols, void *d_act, void *d_y, int64_t ldy,
                            int32_t y_layout, int32_t y_dtype, void *stream) {
-    crisp_status_t bad = check_product(h, d_act, ncols, d_y, ldy, y_layout, y_dtype);
-    if (bad == CRISP_OK) bad = check_quantize(d_x_bf16, ldx, x_layout, h->g.k, ncols, d_act);
+    const uint64_t moment = encodes.now();
+    const bool fused = fused8(ncols);
+    crisp_status_t bad = check_product(h, d_act, fused, ncols, d_y, ldy, y_layout, y_dtype);
+    if (bad == CRISP_OK) bad = check_quantize(d_x_bf16, ldx, x_layout, h->g.k, ncols, d_act, fused);
+    if (bad == CRISP_OK && !fused) bad = crisp_quantize8(d_x_bf16, ldx, x_layout, h->g.k, ncols, d_act, stream);
     if (bad != CRISP_OK) return bad;
-    bad = crisp_quantize8(d_x_bf16, ldx, x_layout, h->g.k, ncols, d_act, stream);
-    if (bad != CRISP_OK) return bad;
-    return launch_spmm8(h, d_act, ncols, d_y, ldy, y_layout, y_dtype, true, (cudaStream_t)stream) == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
+    const cudaError_t e = launch_spmm8(h, fused ? d_x_bf16 : nullptr, ldx, x_layout, d_act, !fused, ncols, d_y, ldy, y_layout, y_dtype, moment, (cudaStream_t)stream);
+    return e == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
 }
 
 crisp_status_t crisp_set_epilogue8(crisp_handle8_t h, const float *d_bias_f32, int32_t relu) {
