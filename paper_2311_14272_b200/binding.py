@@ -200,7 +200,7 @@ def load(path: Optional[str] = None):
         "crisp_last_launch8": [vp, P(LaunchInfo)],
         "crisp_device_status8": [vp, vp, P(i32)],
         "crisp_reset_status8": [vp, vp],
-        "crisp_set_tuning8": [vp, C.c_uint64, i32],
+        "crisp_set_tuning8": [vp, i32, i32, C.c_uint64, i32],
         "crisp_adamw": [i32, P(AdamwTensor), P(AdamwParams), vp],
         "crisp_adamw_moments": [vp, vp, vp, vp, i64, vp, vp, vp],
     }
@@ -601,8 +601,8 @@ def crisp_reset_status8(handle8: int, stream=None):
     _check(load().crisp_reset_status8(handle8, _stream(stream)), "crisp_reset_status8")
 
 
-def crisp_set_tuning8(handle8: int, wait_limit_cycles: int = 0, skip_fill: int = -1):
-    _check(load().crisp_set_tuning8(handle8, wait_limit_cycles, skip_fill), "crisp_set_tuning8")
+def crisp_set_tuning8(handle8: int, tile_cols: int = 0, split: int = 0, wait_limit_cycles: int = 0, skip_fill: int = -1):
+    _check(load().crisp_set_tuning8(handle8, tile_cols, split, wait_limit_cycles, skip_fill), "crisp_set_tuning8")
 
 
 def crisp_destroy8(handle8: int):
@@ -868,8 +868,8 @@ class HybridLayer:
     def last_launch8(self) -> dict:
         return crisp_last_launch8(self.handle8)
 
-    def set_tuning8(self, wait_limit_cycles=0, skip_fill=-1):
-        crisp_set_tuning8(self.handle8, wait_limit_cycles, skip_fill)
+    def set_tuning8(self, tile_cols=0, split=0, wait_limit_cycles=0, skip_fill=-1):
+        crisp_set_tuning8(self.handle8, tile_cols, split, wait_limit_cycles, skip_fill)
         return self
 
     def reset_status8(self, stream=None):

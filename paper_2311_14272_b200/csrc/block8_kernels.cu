@@ -18,20 +18,20 @@ namespace {
 
 // -------------------------------------------------------------------------------------------------------------- weights
 
-// One CTA a kept block: thread t takes eight columns (t % 16) of rows t / 16, + 16, ...
-__global__ void __launch_bounds__(256)
+// One CTA a kept block: thread t takes eight columns (t % 16) of rows t / 16, + 32, ...
+__global__ void __launch_bounds__(512)
 encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_blk_col, const uint32_t *nm_bits, int32_t *blk_col, uint8_t *exps, uint8_t *image,
                uint32_t *header, int vec_ok) {
-    __shared__ uint32_t largest[8];
+    __shared__ uint32_t largest[16];
     chain_kernels();
     const int slot = blockIdx.x, rt = slot / g.kkeep, kb = mask_blk_col[slot];
     const int chunk = threadIdx.x & 15, row0 = threadIdx.x >> 4;
     const int64_t col = (int64_t)kb * 128 + chunk * 8;
     const bool vec = vec_ok && col + 8 <= g.k;
-    uint32_t x[8][4], top = 0;
+    uint32_t x[4][4], top = 0;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int64_t row = (int64_t)rt * 128 + row0 + 16 * i;
+    for (int i = 0; i < 4; ++i) {
+        const int64_t row = (int64_t)rt * 128 + row0 + 32 * i;
         uint32_t keep = 0;
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[i][j] = 0;
@@ -57,7 +57,7 @@ encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_bl
     if (__syncthreads_or(larger_of(top) >= 0x7F80u)) {
         top = 0;
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 top = larger(top, finite(x[i][j]));
@@ -68,13 +68,13 @@ encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_bl
     if ((threadIdx.x & 31) == 0) largest[threadIdx.x >> 5] = top;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = max(top, largest[i]);
+    for (int i = 0; i < 16; ++i) top = max(top, largest[i]);
     const uint32_t e = exponent_of(top);
     const float down = power_of(254u - e);
     uint8_t *entry = image + (int64_t)slot * kEntry8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int row = row0 + 16 * i;
+    for (int i = 0; i < 4; ++i) {
+        const int row = row0 + 32 * i;
         uint8_t *at = entry + (row >> 3) * 1024 + (row & 7) * 128 + (((chunk >> 1) ^ (row & 7)) << 4) + (chunk & 1) * 8;
         *reinterpret_cast<uint2 *>(at) = make_uint2(codes2(x[i][0], down) | codes2(x[i][1], down) << 16, codes2(x[i][2], down) | codes2(x[i][3], down) << 16);
     }
@@ -185,64 +185,75 @@ quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols,
     }
 }
 
-// X [k, ncols]: a CTA takes 64 columns of one k-block.  A warp reads 16 rows of it, a lane two neighbouring columns; the 16 values of a column in a warp are one
-// 16-byte chunk of its codes.
+// X [k, ncols]: a CTA takes 128 columns of one k-block.  A warp reads 16 rows of it, a lane two pairs of neighbouring columns (64 apart: the chunks that eight
+// lanes write side by side then lie in four banks' worth of shared memory and not in two); the 16 values of a column in a warp are one 16-byte chunk of its codes.
+// Neighbouring CTAs read neighbouring columns: by k-blocks instead, 4096 x 8192 took 52 us, as 64 columns a CTA.
 __global__ void __launch_bounds__(256)
 quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
                         int pair_ok) {
-    __shared__ uint32_t largest[8][32];
-    __shared__ __align__(16) uint8_t tile[8192];
+    __shared__ uint32_t largest[2][8][32];
+    __shared__ __align__(16) uint8_t tile[16384];
     wait_for_prerequisites();
     launch_dependents();
-    const int64_t kb = blockIdx.x % nblk, c0 = (int64_t)(blockIdx.x / nblk) * 64;
+    const int64_t kb = blockIdx.x / chunks, c0 = (blockIdx.x - kb * chunks) * 128;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    const int64_t col = c0 + 2 * lane, row0 = kb * 128 + warp * 16;
-    uint32_t v[16], top = 0;
+    const int64_t row0 = kb * 128 + warp * 16;
+    uint32_t v[2][16], top[2] = {0, 0};
 #pragma unroll
-    for (int i = 0; i < 16; ++i) {
-        v[i] = 0;
-        if (row0 + i < k) {
-            const uint16_t *p = x + (row0 + i) * ldx + col;
-            if (pair_ok && col + 1 < ncols) {
-                v[i] = *reinterpret_cast<const uint32_t *>(p);
-            } else {
-                if (col < ncols) v[i] = p[0];
-                if (col + 1 < ncols) v[i] |= (uint32_t)p[1] << 16;
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int64_t col = c0 + 64 * h + 2 * lane;
+            v[h][i] = 0;
+            if (row0 + i < k) {
+                const uint16_t *p = x + (row0 + i) * ldx + col;
+                if (pair_ok && col + 1 < ncols) {
+                    v[h][i] = *reinterpret_cast<const uint32_t *>(p);
+                } else {
+                    if (col < ncols) v[h][i] = p[0];
+                    if (col + 1 < ncols) v[h][i] |= (uint32_t)p[1] << 16;
+                }
             }
         }
-        top = larger(top, v[i]);
-    }
-    if (larger_of(top) >= 0x7F80u) {
-        top = 0;
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            top = larger(top, finite(v[i]));
-            v[i] = nan_for_infinity(v[i]);
+    for (int h = 0; h < 2; ++h) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) top[h] = larger(top[h], v[h][i]);
+        if (larger_of(top[h]) >= 0x7F80u) {
+            top[h] = 0;
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                top[h] = larger(top[h], finite(v[h][i]));
+                v[h][i] = nan_for_infinity(v[h][i]);
+            }
         }
+        largest[h][warp][lane] = top[h];
     }
-    largest[warp][lane] = top;
     __syncthreads();
 #pragma unroll
-    for (int i = 0; i < 8; ++i) top = __vmaxu2(top, largest[i][lane]);
-    const uint32_t e[2] = {exponent_of(top & 0xFFFFu), exponent_of(top >> 16)};
-    const float down[2] = {power_of(254u - e[0]), power_of(254u - e[1])};
-    uint32_t q[2][4] = {};
+    for (int h = 0; h < 2; ++h) {
 #pragma unroll
-    for (int i = 0; i < 16; i += 2) {
-        const float2 a = floats(v[i]), b = floats(v[i + 1]);
-        q[0][i / 4] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a.x * down[0], b.x * down[0]), __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
-        q[1][i / 4] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a.y * down[1], b.y * down[1]), __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
-    }
+        for (int i = 0; i < 8; ++i) top[h] = __vmaxu2(top[h], largest[h][i][lane]);
+        const uint32_t e[2] = {exponent_of(top[h] & 0xFFFFu), exponent_of(top[h] >> 16)};
+        const float down[2] = {power_of(254u - e[0]), power_of(254u - e[1])};
+        uint32_t q[2][4] = {};
 #pragma unroll
-    for (int s = 0; s < 2; ++s) {
-        const int c = 2 * lane + s;
-        *reinterpret_cast<uint4 *>(tile + (c >> 3) * 1024 + (c & 7) * 128 + ((warp ^ (c & 7)) << 4)) = make_uint4(q[s][0], q[s][1], q[s][2], q[s][3]);
-        if (warp == 0 && col + s < ncols) put_scale(scales, chunks, kb, col + s, e[s]);
+        for (int i = 0; i < 16; i += 2) {
+            const float2 a = floats(v[h][i]), b = floats(v[h][i + 1]);
+            q[0][i / 4] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a.x * down[0], b.x * down[0]), __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
+            q[1][i / 4] |= (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(a.y * down[1], b.y * down[1]), __NV_SATFINITE, __NV_E4M3) << (8 * (i & 3));
+        }
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+            const int c = 64 * h + 2 * lane + s;
+            *reinterpret_cast<uint4 *>(tile + (c >> 3) * 1024 + (c & 7) * 128 + ((warp ^ (c & 7)) << 4)) = make_uint4(q[s][0], q[s][1], q[s][2], q[s][3]);
+            if (warp == 0 && c0 + c < ncols) put_scale(scales, chunks, kb, c0 + c, e[s]);
+        }
     }
     __syncthreads();
     // the atoms lie one behind the other
     const int64_t first = c0 >> 3;
-    const int atoms = (int)min((int64_t)8, groups - first);
+    const int atoms = (int)min((int64_t)16, groups - first);
     uint4 *out = reinterpret_cast<uint4 *>(codes + (kb * groups + first) * 1024);
     for (int i = threadIdx.x; i < atoms * 64; i += 256) out[i] = reinterpret_cast<const uint4 *>(tile)[i];
 }
@@ -256,7 +267,7 @@ cudaError_t launch_encode8(const Geometry &g, const uint16_t *w, int64_t ld, con
     const Image8 I = image8(g);
     if ((int64_t)g.nrt * g.kkeep == 0) return cudaMemsetAsync(buf, 0, kAlign, st);
     begin_encode(st);
-    const cudaError_t e = launch_chained(encode8_kernel, (unsigned)(g.nrt * g.kkeep), 256, 0, st, g, w, ld, mask_blk_col, nm_bits,
+    const cudaError_t e = launch_chained(encode8_kernel, (unsigned)(g.nrt * g.kkeep), 512, 0, st, g, w, ld, mask_blk_col, nm_bits,
                                          reinterpret_cast<int32_t *>(buf + I.col_off), buf + I.exp_off, buf + I.image_off, reinterpret_cast<uint32_t *>(buf),
                                          (int)aligned16(w, ld));
     end_encode();
@@ -271,7 +282,7 @@ cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, i
 
 cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t k, int64_t ncols, uint8_t *act, cudaStream_t st) {
     const Act8 a = act8(k, ncols);
-    const int64_t ctas = layout ? a.groups * ((a.nblk + 3) / 4) : a.nblk * ((ncols + 63) / 64);
+    const int64_t ctas = layout ? a.groups * ((a.nblk + 3) / 4) : a.nblk * a.chunks;
     if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
     if (layout)
         return launch_chained(quantize_tokens_kernel, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks, act, act + a.scale_off,

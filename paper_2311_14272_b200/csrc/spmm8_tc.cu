@@ -10,9 +10,9 @@
 #include <cuda.h>
 #include <cuda_bf16.h>
 
+#include <algorithm>
 #include <atomic>
 #include <cstring>
-#include <cstdlib>
 #include <memory>
 #include <new>
 
@@ -38,6 +38,7 @@ struct crisp_handle8_s {
     crisp::Geometry g;
     uint8_t *buf;
     crisp::Epilogue epilogue;
+    int tile_cols, split;                    // tuning: columns a tile and CTAs that share one (0 = chosen by the library)
     unsigned long long wait_limit_cycles;
     int skip_fill;
     CUtensorMap map_a;
@@ -175,7 +176,7 @@ __device__ __forceinline__ uint4 fetch8(const Params8 &p, int64_t col, int at) {
 // kFused: X is not in an activation buffer.  Eight warps fetch and quantise it on the way into the pipeline's stages, a whole stage (a k-block of all columns) each,
 // so that the loads of eight stages are under way at once; each row tile's CTAs do that anew, which a few columns are worth (one launch less).
 template <int N, bool kSplit, bool kFused>
-__global__ void __launch_bounds__(32 * (2 + Tile8<N>::kEpi + (kFused ? kQuantisers : 1)), 1)
+__global__ void __launch_bounds__(32 * (2 + Tile8<N>::kEpi + (kFused ? kQuantisers : 2)), 1)
 spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_s,
              const __grid_constant__ Params8 p, int split) {
     using T = Tile8<N>;
@@ -301,7 +302,8 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 e -= len;                                        // (stages are numbered through the tiles)
             }
         } else if (lane == 0) {
-            // ---------------------------------------------- activations and their scales
+            // ---------------------------------------------- activations, and in a warp of its own their scales (a copy takes its thread some 150 cycles to issue)
+            const bool codes = warp == 2 + kEpi;
             constexpr int kAhead = 8;
             uint32_t dst = ring, full = bar_full, empty = bar_empty, ph = 0;
             int s = 0, fill = 0;
@@ -322,8 +324,8 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         if (e + kAhead < len) next[u] = p.all ? first + e + kAhead : __ldcg(cols + e + kAhead);
                         if (!mbar_wait(empty, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
                         if (fill++ != p.skip_fill) {
-                            tma_load_2d(dst + T::kX, &map_x, 0, (int)((kb * p.groups + (c0 >> 3)) * 4), full);
-                            tma_load_2d(dst + T::kS, &map_s, 0, (int)((kb * p.chunks + (c0 >> 7)) * 2), full);
+                            if (codes) tma_load_2d(dst + T::kX, &map_x, 0, (int)((kb * p.groups + (c0 >> 3)) * 4), full);
+                            else tma_load_2d(dst + T::kS, &map_s, 0, (int)((kb * p.chunks + (c0 >> 7)) * 2), full);
                         }
                         dst += T::kStage; full += 8; empty += 8;
                         if (++s == p.stages) { s = 0; dst = ring; full = bar_full; empty = bar_empty; ph ^= 1u; }
@@ -429,17 +431,38 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         const int64_t c0 = (int64_t)(tile0 / p.nrt) * N;
         const int cols = (int)min((int64_t)N, p.ncols - c0);
         if (warp >= 2 && warp < 2 + kEpi) {
-            const int lane128 = ((warp & 3) << 5) | lane, part = (warp - 2) >> 2;
-            const int row = row0 + lane128;
-            const float bias = p.bias != nullptr && row < p.rows ? p.bias[row] : 0.f;
-            for (int c = rank * (kEpi / 4) + part; c < cols; c += split * (kEpi / 4)) {
-                float v = 0.f;
-                for (int s = 0; s < split; ++s) v += __uint_as_float(lds32_peer(peer_address(ring + (c * 128 + lane128) * 4, s)));
-                v = activation(v + bias, p.relu);
-                if (row < p.rows && !*abort_flag) {
-                    const int64_t at = p.y_layout == 0 ? row * p.ldy + c0 + c : (c0 + c) * p.ldy + row;
-                    if (p.f32) reinterpret_cast<float *>(p.y)[at] = v;
-                    else reinterpret_cast<__nv_bfloat16 *>(p.y)[at] = __float2bfloat16_rn(v);
+            // Four rows of a column at a time, the ranks' parts fetched together and added up in their order.
+            const int me = (warp - 2) * 32 + lane, threads = 32 * kEpi;
+            for (int i = rank * threads + me; i < cols * 32; i += split * threads) {
+                const int c = i >> 5, r = (i & 31) * 4;
+                float4 part[8];
+#pragma unroll
+                for (int s = 0; s < 8; ++s)
+                    if (s < split) part[s] = lds128_peer(peer_address(ring + (c * 128 + r) * 4, s));
+                float v[4] = {part[0].x, part[0].y, part[0].z, part[0].w};
+#pragma unroll
+                for (int s = 1; s < 8; ++s)
+                    if (s < split) { v[0] += part[s].x; v[1] += part[s].y; v[2] += part[s].z; v[3] += part[s].w; }
+                if (*abort_flag) break;
+                uint32_t bits[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int row = row0 + r + j;
+                    v[j] = activation(v[j] + (p.bias != nullptr && row < p.rows ? p.bias[row] : 0.f), p.relu);
+                    bits[j] = __float_as_uint(v[j]);
+                }
+                const int64_t at = p.y_layout == 0 ? (row0 + r) * p.ldy + c0 + c : (c0 + c) * p.ldy + row0 + r;
+                if (p.y_layout == 1 && p.vec_ok && row0 + r + 4 <= p.rows) {
+                    if (p.f32) *reinterpret_cast<uint4 *>(reinterpret_cast<float *>(p.y) + at) = make_uint4(bits[0], bits[1], bits[2], bits[3]);
+                    else *reinterpret_cast<uint2 *>(reinterpret_cast<uint16_t *>(p.y) + at) = make_uint2(pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3]));
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        if (row0 + r + j >= p.rows) break;
+                        const int64_t to = at + j * (p.y_layout == 0 ? p.ldy : 1);
+                        if (p.f32) reinterpret_cast<float *>(p.y)[to] = v[j];
+                        else reinterpret_cast<__nv_bfloat16 *>(p.y)[to] = __float2bfloat16_rn(v[j]);
+                    }
                 }
             }
         }
@@ -477,9 +500,11 @@ template <int N, bool kSplit, bool kFused = false>
 Variant8 make_variant8() {
     static std::atomic<bool> configured[kMaxDevices];
     using T = Tile8<N>;
-    const uint32_t fixed = T::kEpi * T::kStaging + 256;
-    const int most = (int)((kSmemBudget - fixed) / T::kStage), stages = most < 12 ? most : 12;
-    return Variant8{spmm8_kernel<N, kSplit, kFused>, 32 * (2 + T::kEpi + (kFused ? kQuantisers : 1)), stages, stages * T::kStage + fixed, configured};
+    constexpr uint32_t fixed = T::kEpi * T::kStaging + 256;
+    constexpr int most = (int)((kSmemBudget - fixed) / T::kStage), stages = most < 12 ? most : 12;
+    // (a quantising warp goes from one of its stages to the next without looking at those between: it must not come round to one that has not been multiplied)
+    static_assert(!kFused || stages >= kQuantisers, "more quantising warps than stages");
+    return Variant8{spmm8_kernel<N, kSplit, kFused>, 32 * (2 + T::kEpi + (kFused ? kQuantisers : 2)), stages, stages * T::kStage + fixed, configured};
 }
 
 template <bool kSplit>
@@ -499,17 +524,21 @@ bool fused8(int64_t ncols) { return ncols <= 32; }
 template <bool kSplit>
 Variant8 fused_variant8(int tile) { return tile == 16 ? make_variant8<16, kSplit, true>() : make_variant8<32, kSplit, true>(); }
 
+// Tiles that begin within a chunk of scales do so at an even multiple of 32 columns: the narrow ones are for a single tile.
+bool fits8(int tile, int64_t ncols) { return tile >= 64 || ncols <= tile; }
+
 // Columns a tile and CTAs that share one.
-void choose8(const Geometry &g, int64_t ncols, int sms, int *tile, int *split) {
+void choose8(const crisp_handle8_s *h, int64_t ncols, int sms, int *tile, int *split) {
+    const Geometry &g = h->g;
     int n = ncols <= 16 ? 16 : ncols <= 32 ? 32 : ncols <= 64 ? 64 : ncols <= 128 ? 128 : 192;
     const auto tiles = [&](int w) { return (int64_t)g.nrt * ((ncols + w - 1) / w); };
     while (n > 64 && tiles(n) < sms) n = n == 192 ? 128 : 64;
-    static const int forced = std::getenv("T8") ? std::atoi(std::getenv("T8")) : 0;
-    if (forced && n == 192) n = forced;
+    if (h->tile_cols && fits8(h->tile_cols, ncols)) n = h->tile_cols;
     *tile = n;
     int s = 1;
     const int64_t have = tiles(n);
     while (s < 8 && have * (s * 2) <= sms && s * 4 <= g.kkeep) s *= 2;
+    if (h->split) s = std::max(1, std::min(h->split, g.kkeep));
     *split = s;
 }
 
@@ -537,7 +566,8 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int
     if (device < 0 || device >= kMaxDevices) return cudaErrorInvalidDevice;
     const Geometry &g = h->g;
     int tile, split;
-    choose8(g, ncols, sm_count_of(device), &tile, &split);
+    choose8(h, ncols, sm_count_of(device), &tile, &split);
+    if (x && tile > 32) tile = 32;
     const Act8 a = act8(g.k, ncols);
     const Variant8 v = x ? (split > 1 ? fused_variant8<true>(tile) : fused_variant8<false>(tile)) : split > 1 ? variant8<true>(tile) : variant8<false>(tile);
     if (!v.configured[device].load(std::memory_order_relaxed)) {
@@ -624,6 +654,7 @@ crisp_status_t crisp_encode8(const uint16_t *d_w_bf16, int64_t ld_w, crisp_mask_
     h->g = g;
     h->buf = reinterpret_cast<uint8_t *>(d_buf);
     h->epilogue = Epilogue{nullptr, 0};
+    h->tile_cols = h->split = 0;
     h->wait_limit_cycles = 0;
     h->skip_fill = -1;
     std::memset(&h->plan, 0, sizeof h->plan);
@@ -724,8 +755,11 @@ crisp_status_t crisp_reset_status8(crisp_handle8_t h, void *stream) {
     return cudaMemsetAsync(h->buf, 0, sizeof(int32_t), (cudaStream_t)stream) == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
 }
 
-crisp_status_t crisp_set_tuning8(crisp_handle8_t h, uint64_t wait_limit_cycles, int32_t skip_fill) {
-    if (!h || skip_fill < -1) return CRISP_INVALID_ARG;
+crisp_status_t crisp_set_tuning8(crisp_handle8_t h, int32_t tile_cols, int32_t split, uint64_t wait_limit_cycles, int32_t skip_fill) {
+    if (!h || skip_fill < -1 || split < 0 || split > 8) return CRISP_INVALID_ARG;
+    if (tile_cols != 0 && tile_cols != 16 && tile_cols != 32 && tile_cols != 64 && tile_cols != 128 && tile_cols != 192 && tile_cols != 256) return CRISP_INVALID_ARG;
+    h->tile_cols = tile_cols;
+    h->split = split;
     h->wait_limit_cycles = wait_limit_cycles;
     h->skip_fill = skip_fill;
     return CRISP_OK;

@@ -48,7 +48,7 @@ def test_null_handles_and_masks(lib):
     assert lib.crisp_last_launch8(None, C.byref(info)) == B.INVALID_ARG
     assert lib.crisp_device_status8(None, None, None) == B.INVALID_ARG
     assert lib.crisp_reset_status8(None, None) == B.INVALID_ARG
-    assert lib.crisp_set_tuning8(None, 0, -1) == B.INVALID_ARG
+    assert lib.crisp_set_tuning8(None, 0, 0, 0, -1) == B.INVALID_ARG
     lib.crisp_destroy8(None)
 
 

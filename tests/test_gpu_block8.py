@@ -129,6 +129,48 @@ def test_tiles_of_every_width_and_parts(rows, k, ncols, keep):
     assert info["ctas"] <= 148 or info["stack"] == 1
 
 
+@pytest.mark.parametrize("tile", [64, 128, 192, 256])
+@pytest.mark.parametrize("split", [1, 2, 3, 8])
+def test_the_result_does_not_depend_on_the_tiling(tile, split):
+    """Every tile width, alone and with clusters: the sums of the parts differ in their roundings only."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    rows, k, ncols = 300, 1500, 333
+    L, w, _ = layer(B, torch, rows, k, 4, 4, 0.8, 30)
+    x = activations(np.random.default_rng(31), k, ncols)
+    held = ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64))
+    d_x = bf16_dev(x, torch)
+    bias = np.random.default_rng(32).standard_normal(rows).astype(np.float32)
+    L.set_epilogue8(to_dev(bias, torch), relu=True)
+    L.set_tuning8(tile_cols=tile, split=split)
+    for tokens in (False, True):
+        for f32 in (0, 1):
+            y = L.spmm8(d_x.t().contiguous() if tokens else d_x, tokens=tokens, y_dtype=f32)
+            info = L.last_launch8()
+            assert info["tile_cols"] == tile and info["stack"] == split
+            check(numbers(y.t() if tokens else y), w, held, k, f32, bias.astype(np.float64), True)
+    with pytest.raises(B.CrispError):
+        L.set_tuning8(tile_cols=96)
+    with pytest.raises(B.CrispError):
+        L.set_tuning8(split=9)
+
+
+@pytest.mark.parametrize("ncols,tile", [(1, 32), (16, 64), (20, 64), (32, 32)])
+def test_narrow_tiles_that_are_not_the_first_choice(ncols, tile):
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, w, _ = layer(B, torch, 256, 1024, 4, 4, 1.0, 33)
+    x = activations(np.random.default_rng(34), 1024, ncols)
+    held = ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64))
+    for split in (1, 4):
+        L.set_tuning8(tile_cols=tile, split=split)
+        act = L.quantize8(bf16_dev(x, torch))
+        y = L.spmm8(act, y_dtype=1)
+        assert L.last_launch8()["tile_cols"] == tile
+        check(numbers(y), w, held, 1024, 1)
+        check(numbers(L.spmm8(bf16_dev(x, torch), y_dtype=1)), w, held, 1024, 1)
+
+
 def test_no_kept_block_gives_the_bias():
     import torch
     from paper_2311_14272_b200 import binding as B
