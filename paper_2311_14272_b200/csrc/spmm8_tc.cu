@@ -105,6 +105,19 @@ __host__ __device__ constexpr uint32_t make_idesc8(int n) { return (1u << 23) | 
 
 __device__ __forceinline__ float activation(float v, int relu) { return relu && v < 0.f ? 0.f : v; }         // (a NaN stays)
 
+__device__ __forceinline__ bool elect_one() {
+    uint32_t yes;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
+    return yes != 0;
+}
+// A bounded wait of a whole warp.  kEarly: it may come before the kernel in front has finished, and the limit counts from then on.
+template <bool kEarly>
+__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, bool leader, volatile int *abort_flag, unsigned long long limit) {
+    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
+    if constexpr (kEarly) wait_for_prerequisites();
+    return __any_sync(0xFFFFFFFFu, leader && mbar_wait(bar, parity, abort_flag, limit)) != 0;
+}
+
 // One draining warp's 32 rows x 32 columns (lane = row, x[i] = column i), through its staging tile, so that the lanes write whole sectors.
 template <bool kF32>
 __device__ __forceinline__ void store_chunk8(const Params8 &p, uint8_t *stage, int lane, const float (&x)[32], int row0, int64_t col0) {
@@ -216,22 +229,26 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const int first = kSplit ? (int)((int64_t)p.kkeep * rank / split) : 0;
     const int len = (kSplit ? (int)((int64_t)p.kkeep * (rank + 1) / split) : p.kkeep) - first;
 
+    // The threads that issue copies and MMAs are bound by their own instructions.  Their warps run the loops as a whole, so that addresses and descriptors stay in uniform
+    // registers, where the instructions take them from, and an elected thread issues (one thread's loops: MEASURE).
     if (warp == 0) {
-        if (lane == 0) {
-            // ---------------------------------------------- weights, and the byte count of a stage
-            uint32_t dst = ring, full = bar_full, empty = bar_empty, ph = 0;
-            int s = 0, fill = 0;
-            bool ok = true;
-            for (int t = tile0; t < p.num_tiles && ok && !*abort_flag; t += tile_step) {
-                int row = ((t % p.nrt) * p.kkeep + first) * (int)(kEntry8 / 256);
-                for (int e = 0; e < len; ++e) {
-                    if (!mbar_wait_early(empty, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
+        // -------------------------------------------------- weights, and the byte count of a stage
+        const bool leader = elect_one();
+        uint32_t dst = ring, full = bar_full, empty = bar_empty, ph = 0;
+        int s = 0, fill = 0;
+        bool ok = true;
+        for (int t = tile0; t < p.num_tiles && ok; t += tile_step) {
+            int row = ((t % p.nrt) * p.kkeep + first) * (int)(kEntry8 / 256);
+            for (int e = 0; e < len; ++e) {
+                if (!wait_warp<true>(empty, ph ^ 1u, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                if (leader) {
                     mbar_expect_tx(full, kFused ? kEntry8 : T::kBytes);
-                    if (fill++ != p.skip_fill) tma_load_2d(dst, &map_a, 0, row, full);
-                    row += kEntry8 / 256;
-                    dst += T::kStage; full += 8; empty += 8;
-                    if (++s == p.stages) { s = 0; dst = ring; full = bar_full; empty = bar_empty; ph ^= 1u; }
+                    if (fill != p.skip_fill) tma_load_2d(dst, &map_a, 0, row, full);
                 }
+                ++fill;
+                row += kEntry8 / 256;
+                dst += T::kStage; full += 8; empty += 8;
+                if (++s == p.stages) { s = 0; dst = ring; full = bar_full; empty = bar_empty; ph ^= 1u; }
             }
         }
         wait_for_prerequisites();                        // (it may have had nothing to wait for; the other warps have waited)
@@ -301,16 +318,19 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 }
                 e -= len;                                        // (stages are numbered through the tiles)
             }
-        } else if (lane == 0) {
-            // ---------------------------------------------- activations, and in a warp of its own their scales (a copy takes its thread some 150 cycles to issue)
-            const bool codes = warp == 2 + kEpi;
+        } else {
+            // ---------------------------------------------- activations, and in a warp of its own their scales
+            const bool leader = elect_one(), codes = warp == 2 + kEpi;
             constexpr int kAhead = 8;
-            uint32_t dst = ring, full = bar_full, empty = bar_empty, ph = 0;
+            const uint32_t at = codes ? T::kX : T::kS;
+            uint32_t dst = ring + at, full = bar_full, empty = bar_empty, ph = 0;
             int s = 0, fill = 0;
             bool ok = true;
-            for (int t = tile0; t < p.num_tiles && ok && !*abort_flag; t += tile_step) {
+            for (int t = tile0; t < p.num_tiles && ok; t += tile_step) {
                 const int rt = t % p.nrt;
                 const int64_t c0 = (int64_t)(t / p.nrt) * N;
+                // rows of the map of a k-block, and of the tile's first column in it
+                const int pitch = (int)(codes ? p.groups * 4 : p.chunks * 2), start = (int)(codes ? (c0 >> 3) * 4 : (c0 >> 7) * 2);
                 const int32_t *cols = p.blk_col + (int64_t)rt * p.kkeep + first;
                 int next[kAhead];
 #pragma unroll
@@ -320,53 +340,55 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     for (int u = 0; u < kAhead; ++u) {
                         const int e = e0 + u;
                         if (e >= len) break;
-                        const int64_t kb = next[u];
+                        const int row = next[u] * pitch + start;
                         if (e + kAhead < len) next[u] = p.all ? first + e + kAhead : __ldcg(cols + e + kAhead);
-                        if (!mbar_wait(empty, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
-                        if (fill++ != p.skip_fill) {
-                            if (codes) tma_load_2d(dst + T::kX, &map_x, 0, (int)((kb * p.groups + (c0 >> 3)) * 4), full);
-                            else tma_load_2d(dst + T::kS, &map_s, 0, (int)((kb * p.chunks + (c0 >> 7)) * 2), full);
+                        if (!wait_warp<false>(empty, ph ^ 1u, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                        if (leader && fill != p.skip_fill) {
+                            if (codes) tma_load_2d(dst, &map_x, 0, row, full);
+                            else tma_load_2d(dst, &map_s, 0, row, full);
                         }
+                        ++fill;
                         dst += T::kStage; full += 8; empty += 8;
-                        if (++s == p.stages) { s = 0; dst = ring; full = bar_full; empty = bar_empty; ph ^= 1u; }
+                        if (++s == p.stages) { s = 0; dst = ring + at; full = bar_full; empty = bar_empty; ph ^= 1u; }
                     }
                 }
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
-            // ---------------------------------------------- scales to tensor memory, MMAs
-            constexpr uint32_t idesc = make_idesc8(N);
-            const uint64_t a0 = make_smem_desc(ring, 16, 1024, kLayoutSw128), b0 = make_smem_desc(ring + T::kX, 16, 1024, kLayoutSw128);
-            const uint64_t sa0 = make_smem_desc(ring + kTile8, 128, 128, kLayoutNone), sb0 = make_smem_desc(ring + T::kS, 128, 128, kLayoutNone);
-            const uint32_t scales = tmem + T::kAcc * N;
-            uint32_t off = 0, full = bar_full, empty = bar_empty, ph = 0, acc = 0, acc_ph = 0, set = 0;
-            int s = 0;
-            for (int t = tile0; t < p.num_tiles && !*abort_flag; t += tile_step) {
-                const int64_t c0 = (int64_t)(t / p.nrt) * N;
-                const uint32_t shift = (uint32_t)(c0 & 127) >> 5;                // of the tile's first column in its chunk of scales
-                if (!mbar_wait(bar_tempty + 8 * acc, acc_ph ^ 1u, abort_flag, p.wait_limit)) break;
+        // -------------------------------------------------- scales to tensor memory, MMAs
+        constexpr uint32_t idesc = make_idesc8(N);
+        const bool leader = elect_one();
+        const uint64_t a0 = make_smem_desc(ring, 16, 1024, kLayoutSw128), b0 = make_smem_desc(ring + T::kX, 16, 1024, kLayoutSw128);
+        const uint64_t sa0 = make_smem_desc(ring + kTile8, 128, 128, kLayoutNone), sb0 = make_smem_desc(ring + T::kS, 128, 128, kLayoutNone);
+        const uint32_t scales = tmem + T::kAcc * N;
+        uint32_t off = 0, full = bar_full, empty = bar_empty, ph = 0, acc = 0, acc_ph = 0, set = 0;
+        int s = 0;
+        for (int t = tile0; t < p.num_tiles; t += tile_step) {
+            const int64_t c0 = (int64_t)(t / p.nrt) * N;
+            const uint32_t shift = (uint32_t)(c0 & 127) >> 5;                // of the tile's first column in its chunk of scales
+            if (!wait_warp<false>(bar_tempty + 8 * acc, acc_ph ^ 1u, leader, abort_flag, p.wait_limit)) break;
+            tc_fence_after();
+            const uint32_t d = tmem + acc * N;
+            bool ok = true;
+            for (int e = 0; e < len; ++e) {
+                if (!wait_warp<false>(full, ph, leader, abort_flag, p.wait_limit)) { ok = false; break; }
                 tc_fence_after();
-                const uint32_t d = tmem + acc * N;
-                bool ok = true;
-                for (int e = 0; e < len; ++e) {
-                    if (!mbar_wait(full, ph, abort_flag, p.wait_limit)) { ok = false; break; }
-                    tc_fence_after();
-                    const uint32_t sa = scales + set * T::kScaleCols, sb = sa + 4;
+                const uint32_t sa = scales + set * T::kScaleCols, sb = sa + 4;
+                if (leader) {
                     copy_scales(sa, sa0 + off);
 #pragma unroll
                     for (int c = 0; c < T::kChunks; ++c) copy_scales(sb + 4 * c, sb0 + off + c * (kScales8 >> 4));
 #pragma unroll
                     for (int j = 0; j < 4; ++j) mma_scaled(d, a0 + off + 2 * j, b0 + off + 2 * j, idesc, sa, sb + shift, (uint32_t)(e | j));
-                    set ^= 1u;
                     mma_commit(empty);
-                    off += T::kStage >> 4; full += 8; empty += 8;
-                    if (++s == p.stages) { s = 0; off = 0; full = bar_full; empty = bar_empty; ph ^= 1u; }
                 }
-                if (!ok) break;
-                mma_commit(bar_tfull + 8 * acc);
-                if (++acc == T::kAcc) { acc = 0; acc_ph ^= 1u; }
+                set ^= 1u;
+                off += T::kStage >> 4; full += 8; empty += 8;
+                if (++s == p.stages) { s = 0; off = 0; full = bar_full; empty = bar_empty; ph ^= 1u; }
             }
+            if (!ok) break;
+            if (leader) mma_commit(bar_tfull + 8 * acc);
+            if (++acc == T::kAcc) { acc = 0; acc_ph ^= 1u; }
         }
     } else {
         // -------------------------------------------------- drain: tensor memory -> registers -> Y (or this CTA's part of a sum)
