@@ -230,7 +230,8 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     const int len = (kSplit ? (int)((int64_t)p.kkeep * (rank + 1) / split) : p.kkeep) - first;
 
     // The threads that issue copies and MMAs are bound by their own instructions.  Their warps run the loops as a whole, so that addresses and descriptors stay in uniform
-    // registers, where the instructions take them from, and an elected thread issues (one thread's loops: MEASURE).
+    // registers, where the instructions take them from, and an elected thread issues.  (Loops of one thread: 4096 x 4096, 512 columns 17.8 us instead of 12.9, 8192 columns 127 instead of
+    // 116; a block of 64 columns 0.33 us instead of 0.2.)
     if (warp == 0) {
         // -------------------------------------------------- weights, and the byte count of a stage
         const bool leader = elect_one();
@@ -284,28 +285,34 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                             waited = true;
                             if (!ok) break;
                         }
+                        // (the passes side by side: their shuffles would otherwise wait for one another; two passes' largest values travel in a word)
+                        uint32_t top[kAtOnce], word[kAtOnce / 2], any = 0;
 #pragma unroll
                         for (int i = 0; i < kAtOnce; ++i) {
-                            if (2 * (g + i) >= cols) break;
-                            const int c = 2 * (g + i) + half;
-                            uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w}, top = 0;
+                            top[i] = larger(larger(larger(larger(0, v[i].x), v[i].y), v[i].z), v[i].w);
+                            any = __vmaxu2(any, top[i]);
+                        }
+                        if (__any_sync(0xFFFFFFFFu, larger_of(any) >= 0x7F80u)) {
 #pragma unroll
-                            for (int j = 0; j < 4; ++j) top = larger(top, x[j]);
-                            if (__any_sync(0xFFFFFFFFu, larger_of(top) >= 0x7F80u)) {
-                                top = 0;
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    top = larger(top, finite(x[j]));
-                                    x[j] = nan_for_infinity(x[j]);
-                                }
+                            for (int i = 0; i < kAtOnce; ++i) {
+                                top[i] = larger(larger(larger(larger(0, finite(v[i].x)), finite(v[i].y)), finite(v[i].z)), finite(v[i].w));
+                                v[i] = make_uint4(nan_for_infinity(v[i].x), nan_for_infinity(v[i].y), nan_for_infinity(v[i].z), nan_for_infinity(v[i].w));
                             }
-                            uint32_t m = larger_of(top);
+                        }
 #pragma unroll
-                            for (int d = 8; d; d >>= 1) m = max(m, __shfl_xor_sync(0xFFFFFFFFu, m, d));
-                            const uint32_t exponent = exponent_of(m);
+                        for (int i = 0; i < kAtOnce / 2; ++i) word[i] = larger_of(top[2 * i]) | larger_of(top[2 * i + 1]) << 16;
+#pragma unroll
+                        for (int d = 8; d; d >>= 1)
+#pragma unroll
+                            for (int i = 0; i < kAtOnce / 2; ++i) word[i] = __vmaxu2(word[i], __shfl_xor_sync(0xFFFFFFFFu, word[i], d));
+#pragma unroll
+                        for (int i = 0; i < kAtOnce; ++i) {
+                            const int c = 2 * (g + i) + half;
+                            if (c >= cols) break;
+                            const uint32_t exponent = exponent_of(word[i / 2] >> (16 * (i & 1)) & 0xFFFFu);
                             const float down = power_of(254u - exponent);
                             *reinterpret_cast<uint2 *>(stage + T::kX + (c >> 3) * 1024 + (c & 7) * 128 + (((l16 >> 1) ^ (c & 7)) << 4) + (l16 & 1) * 8) =
-                                make_uint2(codes2(x[0], down) | codes2(x[1], down) << 16, codes2(x[2], down) | codes2(x[3], down) << 16);
+                                make_uint2(codes2(v[i].x, down) | codes2(v[i].y, down) << 16, codes2(v[i].z, down) | codes2(v[i].w, down) << 16);
                             if (l16 == 0) *reinterpret_cast<uint32_t *>(stage + T::kS + (c & 31) * 16 + (c >> 5) * 4) = exponent * 0x01010101u;
                         }
                     }
@@ -549,19 +556,26 @@ Variant8 fused_variant8(int tile) { return tile == 16 ? make_variant8<16, kSplit
 // Tiles that begin within a chunk of scales do so at an even multiple of 32 columns: the narrow ones are for a single tile.
 bool fits8(int tile, int64_t ncols) { return tile >= 64 || ncols <= tile; }
 
-// Columns a tile and CTAs that share one.
+// Columns a tile and CTAs that share one: the pair that takes the least time by a model of it, in us.  A block takes a CTA as long as its copies and MMAs, a tile a
+// fixed time beside them, the sum over a cluster one that grows with the columns a CTA has to add up; tiles come in waves of as many as there are SMs.  Measured on
+// 4096 x 4096 in a row, all blocks kept: 64 columns a tile 11.7 us for 128 tiles (256 columns) and 206 for 28 waves (8192), 128 columns 12.9 and 128, 192 columns
+// 15.2 and 115, 256 columns 19.6 and 116; two, four CTAs a tile: 64 columns 11.6, 9.3, 128 columns 12.6, 9.9, 256 columns 18.9, 11.6.
 void choose8(const crisp_handle8_s *h, int64_t ncols, int sms, int *tile, int *split) {
+    struct Cost { int cols; double block, tile; };
+    static const Cost costs[] = {{16, 0.17, 0.5}, {32, 0.17, 0.5}, {64, 0.20, 0.6}, {128, 0.24, 0.8}, {192, 0.31, 1.0}, {256, 0.43, 1.4}};
     const Geometry &g = h->g;
-    int n = ncols <= 16 ? 16 : ncols <= 32 ? 32 : ncols <= 64 ? 64 : ncols <= 128 ? 128 : 192;
-    const auto tiles = [&](int w) { return (int64_t)g.nrt * ((ncols + w - 1) / w); };
-    while (n > 64 && tiles(n) < sms) n = n == 192 ? 128 : 64;
-    if (h->tile_cols && fits8(h->tile_cols, ncols)) n = h->tile_cols;
-    *tile = n;
-    int s = 1;
-    const int64_t have = tiles(n);
-    while (s < 8 && have * (s * 2) <= sms && s * 4 <= g.kkeep) s *= 2;
-    if (h->split) s = std::max(1, std::min(h->split, g.kkeep));
-    *split = s;
+    double best = 1e300;
+    *tile = 64; *split = 1;
+    for (const Cost &c : costs) {
+        if (!fits8(c.cols, ncols) || (h->tile_cols && fits8(h->tile_cols, ncols) && c.cols != h->tile_cols)) continue;
+        const int64_t tiles = (int64_t)g.nrt * ((ncols + c.cols - 1) / c.cols);
+        for (int s = 1; s <= 8 && s <= std::max(1, g.kkeep); ++s) {
+            if (h->split ? s != std::min(h->split, std::max(1, g.kkeep)) : s > 1 && (tiles * s > sms || 2 * s > g.kkeep)) continue;
+            const double waves = (double)((tiles * s + sms - 1) / sms);
+            const double t = waves * (c.block * ((g.kkeep + s - 1) / s) + c.tile) + (s > 1 ? 1.7 + c.cols / (32.0 * s) : 0.0);
+            if (t < best) { best = t; *tile = c.cols; *split = s; }
+        }
+    }
 }
 
 bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
