@@ -1209,7 +1209,15 @@ class AdamW:
     def moments(self, stream=None):
         """(m, sqrt(v)) of 8-bit states as flat bf16 tensors, in which they are exact."""
         assert self.state_bits == 8, "32-bit states are their values"
-        out = [self.torch.empty(self.elements, dtype=self.torch.bfloat16, device=self.device) for _ in range(2)]
-        with self.torch.cuda.device(self.device):
-            crisp_adamw_moments(self.m, self.m_exp, self.v, self.v_exp, self.elements, *out, stream)
-        return out
+        n = self.elements
+        both = self.torch.empty_strided((2, n), (n, 1), dtype=self.torch.bfloat16, device=self.device)
+        at = both.data_ptr()
+        args = (self.m.data_ptr(), self.m_exp.data_ptr(), self.v.data_ptr(), self.v_exp.data_ptr(), n, at, at + 2 * n)
+        if self.device.index == _current_device():
+            code = _lib.crisp_adamw_moments(*args, _stream(stream))
+        else:
+            with self.torch.cuda.device(self.device):
+                code = _lib.crisp_adamw_moments(*args, _stream(stream))
+        if code:
+            raise CrispError(code, "crisp_adamw_moments")
+        return list(both.unbind(0))

@@ -18,16 +18,18 @@ namespace {
 
 // -------------------------------------------------------------------------------------------------------------- weights
 
-// One CTA a kept block: thread t takes eight columns (t % 16) of rows t / 16, + 32, ...
-__global__ void __launch_bounds__(512)
+// One CTA a kept block: thread t takes eight columns (t % 16) of rows t / 16, + 32, ...  `vec`: 8, 2 or 1 columns a load, by what address and pitch allow.
+// Bound by the chain of a CTA (list, mask and weights, largest value, codes): 4096 x 4096 2:4 keep 0.5 8.8 us, all of it 13.4, with four CTAs an SM; two 11.3 and
+// 18.3, three 10.8 and 15.7.
+__global__ void __launch_bounds__(512, 4)
 encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_blk_col, const uint32_t *nm_bits, int32_t *blk_col, uint8_t *exps, uint8_t *image,
-               uint32_t *header, int vec_ok) {
+               uint32_t *header, int wide) {
     __shared__ uint32_t largest[16];
     chain_kernels();
-    const int slot = blockIdx.x, rt = slot / g.kkeep, kb = mask_blk_col[slot];
+    const int slot = blockIdx.x, rt = slot / g.kkeep, kb = g.kkeep == g.nblk ? slot - rt * g.kkeep : mask_blk_col[slot];
     const int chunk = threadIdx.x & 15, row0 = threadIdx.x >> 4;
     const int64_t col = (int64_t)kb * 128 + chunk * 8;
-    const bool vec = vec_ok && col + 8 <= g.k;
+    const int vec = col + 8 <= g.k ? wide : 1;
     uint32_t x[4][4], top = 0;
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
@@ -36,11 +38,14 @@ encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_bl
 #pragma unroll
         for (int j = 0; j < 4; ++j) x[i][j] = 0;
         if (row < g.rows) {
-            keep = reinterpret_cast<const uint8_t *>(nm_bits + row * g.wpr)[kb * 16 + chunk];
+            keep = g.n == g.m ? 0xFFu : reinterpret_cast<const uint8_t *>(nm_bits + row * g.wpr)[kb * 16 + chunk];
             const uint16_t *p = w + row * ld + col;
-            if (vec) {
+            if (vec == 8) {
                 const uint4 v = *reinterpret_cast<const uint4 *>(p);
                 x[i][0] = v.x; x[i][1] = v.y; x[i][2] = v.z; x[i][3] = v.w;
+            } else if (vec == 2) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) x[i][j] = reinterpret_cast<const uint32_t *>(p)[j];
             } else {
 #pragma unroll
                 for (int j = 0; j < 8; ++j)
@@ -84,24 +89,34 @@ encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_bl
 }
 
 // One CTA a block of the dense matrix, kept or not.
-__global__ void __launch_bounds__(256)
-decode8_kernel(Geometry g, const int32_t *blk_col, const uint8_t *exps, const uint8_t *image, uint16_t *w, int64_t ld, int vec_ok) {
-    __shared__ int found;
+__global__ void __launch_bounds__(512)
+decode8_kernel(Geometry g, const int32_t *blk_col, const uint8_t *exps, const uint8_t *image, uint16_t *w, int64_t ld, int wide) {
+    __shared__ int found, scale;
     chain_kernels();
     const int rt = blockIdx.x / g.nblk, kb = blockIdx.x - rt * g.nblk;
-    if (threadIdx.x == 0) found = -1;
-    __syncthreads();
-    for (int i = threadIdx.x; i < g.kkeep; i += 256)
-        if (blk_col[rt * g.kkeep + i] == kb) found = rt * g.kkeep + i;
-    __syncthreads();
-    const int slot = found;
+    int slot = rt * g.kkeep + kb;
+    uint32_t e = 0;
+    if (g.kkeep == g.nblk) {
+        e = exps[slot];
+    } else {
+        // where the block is in its row tile's list, if it is, and its exponent
+        if (threadIdx.x == 0) found = -1;
+        __syncthreads();
+        for (int i = threadIdx.x; i < g.kkeep; i += 512) {
+            const int at = rt * g.kkeep + i, col = blk_col[at], here = exps[at];
+            if (col == kb) { found = at; scale = here; }
+        }
+        __syncthreads();
+        slot = found;
+        e = (uint32_t)scale;
+    }
     const int chunk = threadIdx.x & 15, row0 = threadIdx.x >> 4;
     const int64_t col = (int64_t)kb * 128 + chunk * 8;
-    const float up = slot < 0 ? 0.f : power_of(exps[slot]);
+    const float up = power_of(e);
     const uint8_t *entry = image + (int64_t)slot * kEntry8;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-        const int r = row0 + 16 * i;
+    for (int i = 0; i < 4; ++i) {
+        const int r = row0 + 32 * i;
         const int64_t row = (int64_t)rt * 128 + r;
         if (row >= g.rows || col >= g.k) continue;
         uint32_t out[4] = {};
@@ -116,8 +131,12 @@ decode8_kernel(Geometry g, const int32_t *blk_col, const uint8_t *exps, const ui
             }
         }
         uint16_t *p = w + row * ld + col;
-        if (vec_ok && col + 8 <= g.k) {
+        const int vec = col + 8 <= g.k ? wide : 1;
+        if (vec == 8) {
             *reinterpret_cast<uint4 *>(p) = make_uint4(out[0], out[1], out[2], out[3]);
+        } else if (vec == 2) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) reinterpret_cast<uint32_t *>(p)[j] = out[j];
         } else {
 #pragma unroll
             for (int j = 0; j < 8; ++j)
@@ -132,20 +151,21 @@ __device__ __forceinline__ void put_scale(uint8_t *scales, int64_t chunks, int64
     *reinterpret_cast<uint32_t *>(scales + (kb * chunks + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4) = e * 0x01010101u;
 }
 
-// X [ncols, k]: a CTA takes eight columns (tokens) and four k-blocks; 16 threads a block of one column, eight values each.
+// X [ncols, k]: a CTA takes eight columns (tokens) and 2 U k-blocks; 16 threads a block of one column, eight values each, U blocks a thread.
+template <int U>
 __global__ void __launch_bounds__(256)
 quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
                        int vec_ok) {
     wait_for_prerequisites();
     launch_dependents();                     // (a product behind this one fetches weights meanwhile: all before this kernel has finished)
-    const int64_t quads = (nblk + 3) / 4;
-    const int64_t group = blockIdx.x / quads, quad = blockIdx.x - group * quads;
+    const int64_t spans = (nblk + 2 * U - 1) / (2 * U);
+    const int64_t group = blockIdx.x / spans, kb0 = (blockIdx.x - group * spans) * (2 * U);
     const int lane = threadIdx.x & 15, r = threadIdx.x >> 4 & 7, side = threadIdx.x >> 7;
     const int64_t col = group * 8 + r;
-    uint32_t v[2][4], top[2] = {0, 0};
+    uint32_t v[U][4], top[U] = {};
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int64_t at = (quad * 4 + side * 2 + i) * 128 + lane * 8;
+    for (int i = 0; i < U; ++i) {
+        const int64_t at = (kb0 + side * U + i) * 128 + lane * 8;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i][j] = 0;
         if (col < ncols && at < k) {
@@ -161,8 +181,8 @@ quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols,
         }
     }
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const int64_t kb = quad * 4 + side * 2 + i;
+    for (int i = 0; i < U; ++i) {
+        const int64_t kb = kb0 + side * U + i;
 #pragma unroll
         for (int j = 0; j < 4; ++j) top[i] = larger(top[i], v[i][j]);
         if (__any_sync(0xFFFFFFFFu, larger_of(top[i]) >= 0x7F80u)) {
@@ -185,12 +205,12 @@ quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols,
     }
 }
 
-// X [k, ncols]: a CTA takes 128 columns of one k-block.  A warp reads 16 rows of it, a lane two pairs of neighbouring columns (64 apart: the chunks that eight
-// lanes write side by side then lie in four banks' worth of shared memory and not in two); the 16 values of a column in a warp are one 16-byte chunk of its codes.
-// Neighbouring CTAs read neighbouring columns: by k-blocks instead, 4096 x 8192 took 52 us, as 64 columns a CTA.
+// X [k, ncols]: a CTA takes 128 columns of one k-block.  A warp reads 16 rows of it, a lane four neighbouring columns; the 16 values of a column in a warp are one
+// 16-byte chunk of its codes.  Neighbouring CTAs read neighbouring columns.  4096 x 8192: 18.2 us (5.5 TB/s); two pairs of columns a lane, 64 apart (fewer bank
+// conflicts), 23.4; neighbouring CTAs on neighbouring k-blocks, 64 columns each, 52.
 __global__ void __launch_bounds__(256)
 quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
-                        int pair_ok) {
+                        int pair_ok, int quad_ok) {
     __shared__ uint32_t largest[2][8][32];
     __shared__ __align__(16) uint8_t tile[16384];
     wait_for_prerequisites();
@@ -199,11 +219,18 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row0 = kb * 128 + warp * 16;
     uint32_t v[2][16], top[2] = {0, 0};
+    if (quad_ok && c0 + 128 <= ncols && row0 + 16 <= k) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+            const uint2 two = *reinterpret_cast<const uint2 *>(x + (row0 + i) * ldx + c0 + 4 * lane);
+            v[0][i] = two.x; v[1][i] = two.y;
+        }
+    } else
 #pragma unroll
     for (int i = 0; i < 16; ++i)
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-            const int64_t col = c0 + 64 * h + 2 * lane;
+            const int64_t col = c0 + 4 * lane + 2 * h;
             v[h][i] = 0;
             if (row0 + i < k) {
                 const uint16_t *p = x + (row0 + i) * ldx + col;
@@ -245,7 +272,7 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int c = 64 * h + 2 * lane + s;
+            const int c = 4 * lane + 2 * h + s;
             *reinterpret_cast<uint4 *>(tile + (c >> 3) * 1024 + (c & 7) * 128 + ((warp ^ (c & 7)) << 4)) = make_uint4(q[s][0], q[s][1], q[s][2], q[s][3]);
             if (warp == 0 && c0 + c < ncols) put_scale(scales, chunks, kb, c0 + c, e[s]);
         }
@@ -258,6 +285,11 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
     for (int i = threadIdx.x; i < atoms * 64; i += 256) out[i] = reinterpret_cast<const uint4 *>(tile)[i];
 }
 
+// Columns that a load or store may take.
+int columns_of(const void *p, int64_t ld) {
+    const uintptr_t a = reinterpret_cast<uintptr_t>(p);
+    return a % 16 == 0 && ld % 8 == 0 ? 8 : a % 4 == 0 && ld % 2 == 0 ? 2 : 1;
+}
 bool aligned16(const void *p, int64_t ld) { return reinterpret_cast<uintptr_t>(p) % 16 == 0 && ld % 8 == 0; }
 
 }  // namespace
@@ -269,26 +301,28 @@ cudaError_t launch_encode8(const Geometry &g, const uint16_t *w, int64_t ld, con
     begin_encode(st);
     const cudaError_t e = launch_chained(encode8_kernel, (unsigned)(g.nrt * g.kkeep), 512, 0, st, g, w, ld, mask_blk_col, nm_bits,
                                          reinterpret_cast<int32_t *>(buf + I.col_off), buf + I.exp_off, buf + I.image_off, reinterpret_cast<uint32_t *>(buf),
-                                         (int)aligned16(w, ld));
+                                         columns_of(w, ld));
     end_encode();
     return e;
 }
 
 cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, int64_t ld, cudaStream_t st) {
     const Image8 I = image8(g);
-    return launch_chained(decode8_kernel, (unsigned)(g.nrt * g.nblk), 256, 0, st, g, reinterpret_cast<const int32_t *>(buf + I.col_off), buf + I.exp_off,
-                          buf + I.image_off, w, ld, (int)aligned16(w, ld));
+    return launch_chained(decode8_kernel, (unsigned)(g.nrt * g.nblk), 512, 0, st, g, reinterpret_cast<const int32_t *>(buf + I.col_off), buf + I.exp_off,
+                          buf + I.image_off, w, ld, columns_of(w, ld));
 }
 
 cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t k, int64_t ncols, uint8_t *act, cudaStream_t st) {
     const Act8 a = act8(k, ncols);
-    const int64_t ctas = layout ? a.groups * ((a.nblk + 3) / 4) : a.nblk * a.chunks;
+    // (four blocks a thread where there are CTAs enough)
+    const int u = a.groups * a.nblk >= 8 * 1184 ? 4 : 2;
+    const int64_t ctas = layout ? a.groups * ((a.nblk + 2 * u - 1) / (2 * u)) : a.nblk * a.chunks;
     if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
     if (layout)
-        return launch_chained(quantize_tokens_kernel, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks, act, act + a.scale_off,
-                              (int)aligned16(x, ldx));
+        return launch_chained(u == 4 ? quantize_tokens_kernel<4> : quantize_tokens_kernel<2>, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks, act,
+                              act + a.scale_off, (int)aligned16(x, ldx));
     return launch_chained(quantize_columns_kernel, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks, act, act + a.scale_off,
-                          (int)(reinterpret_cast<uintptr_t>(x) % 4 == 0 && ldx % 2 == 0));
+                          (int)(reinterpret_cast<uintptr_t>(x) % 4 == 0 && ldx % 2 == 0), (int)(reinterpret_cast<uintptr_t>(x) % 8 == 0 && ldx % 4 == 0));
 }
 
 }  // namespace crisp

@@ -572,7 +572,7 @@ void choose8(const crisp_handle8_s *h, int64_t ncols, int sms, int *tile, int *s
         for (int s = 1; s <= 8 && s <= std::max(1, g.kkeep); ++s) {
             if (h->split ? s != std::min(h->split, std::max(1, g.kkeep)) : s > 1 && (tiles * s > sms || 2 * s > g.kkeep)) continue;
             const double waves = (double)((tiles * s + sms - 1) / sms);
-            const double t = waves * (c.block * ((g.kkeep + s - 1) / s) + c.tile) + (s > 1 ? 1.7 + c.cols / (32.0 * s) : 0.0);
+            const double t = waves * (c.block * ((g.kkeep + s - 1) / s) + c.tile) + (s > 1 ? 0.9 + c.cols / (48.0 * s) : 0.0);
             if (t < best) { best = t; *tile = c.cols; *split = s; }
         }
     }
