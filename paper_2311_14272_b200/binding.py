@@ -97,7 +97,8 @@ def _bind_network():
         try:
             from . import _network as module
             if getattr(module, "built_for", None) == "%s %d.%d" % (release, *sys.version_info[:2]):
-                module.bind(*[C.cast(f, C.c_void_p).value for f in (lib.crisp_decode, lib.crisp_spmm8_sizes, lib.crisp_spmm8)])
+                module.bind(*[C.cast(f, C.c_void_p).value for f in (lib.crisp_decode, lib.crisp_spmm8_sizes, lib.crisp_spmm8, lib.crisp_decode8,
+                                                                        lib.crisp_encode8_sizes, lib.crisp_encode8, lib.crisp_destroy8)])
                 _network = module
             else:
                 _network = False
@@ -794,6 +795,14 @@ class HybridLayer:
     # The layer in 8 bits, beside or instead of its bf16 encoding (masks of 128 x 128 blocks).
     def encode8(self, w, stream=None):
         """Compress the weights under the mask to e4m3 with a scale for each kept block (crisp_encode8)."""
+        if self._gpu is not None and self._gpu == _current_device():
+            done = _network.encode8(self.mask, w, self.desc.rows, self.desc.k, self._gpu, self.buf8, self.handle8, _stream(stream))
+            if done is not None and not done[2]:
+                code, self.handle8, _ = done
+                self._bias8 = None
+                if code:
+                    raise CrispError(code, "crisp_encode8")
+                return self
         assert w.is_cuda and w.dtype == self.torch.bfloat16 and (w.stride()[1] == 1 or w.shape[1] == 1) and w.shape == (self.desc.rows, self.desc.k), \
             "weights are a bf16 CUDA matrix of the layer's shape with consecutive columns"
         size = crisp_encode8_sizes(self.mask)
@@ -807,6 +816,11 @@ class HybridLayer:
 
     def decode8(self, stream=None):
         """The dense bf16 weights that the 8-bit encoding stands for."""
+        if self._gpu is not None and self._gpu == _current_device():
+            code, w = _network.decode8(self.handle8, self.desc.rows, self.desc.k, self._gpu, _stream(stream))
+            if code:
+                raise CrispError(code, "crisp_decode8")
+            return w
         w = self.torch.empty_strided((self.desc.rows, self.desc.k), (self.desc.k, 1), dtype=self.torch.bfloat16, device=self.device)
         crisp_decode8(self.handle8, w, self.desc.k, stream)
         return w

@@ -57,7 +57,7 @@ struct Powers { uint32_t p1 = 1u << 1, p4 = 1u << 4, p5 = 1u << 5, p7 = 1u << 7,
 struct AdamScalars {
     float lr, beta1, one_beta1, beta2, one_beta2, eps, decay, weight_decay;
     float step_size, root_scale;                              // lr / (1 - b1^t), 1 / sqrt(1 - b2^t)
-    float log_beta1, log_beta2, root_beta2;
+    float log_beta1, log_beta2;
     uint32_t seed_key;
     Powers by;
     const float *d_lr, *d_grad_scale;
@@ -303,7 +303,7 @@ struct Piece {
         // (e0 is a multiple of 8: the hash of e0 + i differs from that of e0 in three low bits until its first product)
         const uint32_t first = ((uint32_t)e0 ^ spread) ^ (((uint32_t)e0 ^ spread) >> 16);
         float v_beyond = 1.f, m_scale = 0.f, v_scale = 0.f;
-        if constexpr (kNarrow) { m_scale = s.beta1 * power_of(x.m_exp); v_scale = s.root_beta2 * power_120(x.v_exp, &v_beyond); }
+        if constexpr (kNarrow) { m_scale = s.beta1 * power_of(x.m_exp); v_scale = power_120(x.v_exp, &v_beyond); }
         if (T.g32) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) g[i] = __uint_as_float(x.g[i]);
@@ -327,9 +327,9 @@ struct Piece {
                 m[i] = x.m[i]; v[i] = x.v[i];
             }
             const float gi = g[i] * f.grad_scale;
-            // (8-bit states come with the factors beta1 and beta2 in them)
+            // (m in 8 bits comes with the factor beta1 in its scale)
             m[i] = fmaf(s.one_beta1, gi, kNarrow ? m[i] : s.beta1 * m[i]);
-            v[i] = fmaf(s.one_beta2 * gi, gi, kNarrow ? v[i] : s.beta2 * v[i]);
+            v[i] = fmaf(s.one_beta2 * gi, gi, s.beta2 * v[i]);
             root[i] = sqrt_near(v[i]);
             w[i] = w[i] * f.decay - f.step_size * (m[i] * reciprocal_near(root[i] * f.root_scale + s.eps));
             if constexpr (kNarrow || !kW32) h[i] = mix_rest(first ^ (uint32_t)i);
@@ -594,7 +594,6 @@ crisp_status_t crisp_adamw(int32_t n, const crisp_adamw_tensor_t *tensors, const
     if (p->d_lr) s.lr = 1.f;
     s.step_size = (float)((p->d_lr ? 1.0 : p->lr) * unit);
     s.root_scale = p->d_step ? 1.f : (float)(1.0 / std::sqrt(-std::expm1(t * std::log(p->beta2))));
-    s.root_beta2 = (float)std::sqrt(p->beta2);
     s.log_beta1 = (float)std::log(p->beta1); s.log_beta2 = (float)std::log(p->beta2);
     s.seed_key = mix(mix((uint32_t)p->seed) ^ (uint32_t)(p->seed >> 32));
     s.d_lr = p->d_lr; s.d_step = p->d_step; s.d_grad_scale = p->d_grad_scale;

@@ -20,6 +20,10 @@ namespace {
 decltype(&crisp_decode) lib_decode;
 decltype(&crisp_spmm8_sizes) lib_spmm8_sizes;
 decltype(&crisp_spmm8) lib_spmm8;
+decltype(&crisp_decode8) lib_decode8;
+decltype(&crisp_encode8_sizes) lib_encode8_sizes;
+decltype(&crisp_encode8) lib_encode8;
+decltype(&crisp_destroy8) lib_destroy8;
 
 // The names of attributes, made once.
 struct {
@@ -170,10 +174,11 @@ PyObject *encoded(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// decode(handle, rows, k, GPU, stream) -> (status, bf16 tensor [rows, k])
-PyObject *decode(PyObject *, PyObject *const *args, Py_ssize_t n) {
+// decode(handle, rows, k, GPU, stream) and decode8(...) -> (status, bf16 tensor [rows, k])
+template <typename Handle>
+PyObject *dense(crisp_status_t (*call)(Handle, uint16_t *, int64_t, void *), const char *name, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    if (!arguments("decode", n, 5)) return nullptr;
+    if (!arguments(name, n, 5)) return nullptr;
     long long v[5];
     for (int i = 0; i < 5; ++i) {
         v[i] = PyLong_AsLongLong(args[i]);
@@ -182,12 +187,14 @@ PyObject *decode(PyObject *, PyObject *const *args, Py_ssize_t n) {
     at::Tensor w = at::empty_strided({v[1], v[2]}, {v[2], 1}, at::TensorOptions().dtype(at::kBFloat16).device(at::Device(at::kCUDA, (at::DeviceIndex)v[3])));
     crisp_status_t s;
     Py_BEGIN_ALLOW_THREADS
-    s = lib_decode(reinterpret_cast<crisp_handle_t>((uintptr_t)v[0]), static_cast<uint16_t *>(w.data_ptr()), v[2], reinterpret_cast<void *>((uintptr_t)v[4]));
+    s = call(reinterpret_cast<Handle>((uintptr_t)v[0]), static_cast<uint16_t *>(w.data_ptr()), v[2], reinterpret_cast<void *>((uintptr_t)v[4]));
     Py_END_ALLOW_THREADS
     Ref out(THPVariable_Wrap(std::move(w)));
     return out.p ? Py_BuildValue("lO", (long)s, out.p) : nullptr;
     END_HANDLE_TH_ERRORS
 }
+PyObject *decode(PyObject *, PyObject *const *args, Py_ssize_t n) { return dense(lib_decode, "decode", args, n); }
+PyObject *decode8(PyObject *, PyObject *const *args, Py_ssize_t n) { return dense(lib_decode8, "decode8", args, n); }
 
 // Rows, columns and pitch of a tensor whose elements lie in rows of consecutive ones (as the binding's _rows_of has them); false: it does not.
 bool rows_of(const at::Tensor &t, int64_t (&v)[3]) {
@@ -251,6 +258,37 @@ PyObject *gradients(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
+// encode8(mask, W, rows, k, GPU, buffer, handle that is replaced, stream) -> (status, handle, bytes that the buffer would need), or None: not a plain matrix that
+// the call takes.  Where the buffer is too small nothing is done and the handle is 0.
+PyObject *encode8(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arguments("encode8", n, 8)) return nullptr;
+    long long v[8] = {};
+    for (int i = 0; i < 8; ++i)
+        if (i != 1 && i != 5) {
+            v[i] = PyLong_AsLongLong(args[i]);
+            if (v[i] == -1 && PyErr_Occurred()) return nullptr;
+        }
+    const at::Tensor *w = plain(args[1]);
+    if (!w || w->scalar_type() != at::kBFloat16 || w->get_device() != v[4] || (w->stride(1) != 1 && w->size(1) != 1) || w->size(0) != v[2] || w->size(1) != v[3])
+        Py_RETURN_NONE;
+    const crisp_mask_t mask = reinterpret_cast<crisp_mask_t>((uintptr_t)v[0]);
+    size_t bytes = 0;
+    crisp_status_t s = lib_encode8_sizes(mask, &bytes);
+    crisp_handle8_t h = nullptr;
+    const at::Tensor *buffer = args[5] != Py_None && THPVariable_CheckExact(args[5]) ? &THPVariable_Unpack(args[5]) : nullptr;
+    if (s == CRISP_OK && buffer && (size_t)buffer->numel() >= bytes) {
+        const int64_t ld = w->size(0) > 1 ? w->stride(0) : w->size(1);
+        Py_BEGIN_ALLOW_THREADS
+        lib_destroy8(reinterpret_cast<crisp_handle8_t>((uintptr_t)v[6]));
+        s = lib_encode8(static_cast<const uint16_t *>(w->data_ptr()), ld, mask, buffer->data_ptr(), reinterpret_cast<void *>((uintptr_t)v[7]), &h);
+        Py_END_ALLOW_THREADS
+        bytes = 0;
+    }
+    return Py_BuildValue("lKK", (long)s, (unsigned long long)(uintptr_t)h, (unsigned long long)bytes);
+    END_HANDLE_TH_ERRORS
+}
+
 // product8(handle, X, rows, k, GPU, tokens, y_dtype, stream) -> (status, Y), or None: not a plain matrix that the call takes.  Workspace and Y are allocated for the
 // current stream, which `stream` has to be.
 PyObject *product8(PyObject *, PyObject *const *args, Py_ssize_t n) {
@@ -286,9 +324,13 @@ PyObject *product8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses of crisp_decode, crisp_spmm8_sizes and crisp_spmm8)
+// bind(addresses of crisp_decode, crisp_spmm8_sizes, crisp_spmm8, crisp_decode8, crisp_encode8_sizes, crisp_encode8 and crisp_destroy8)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    if (!arguments("bind", n, 3)) return nullptr;
+    if (!arguments("bind", n, 7)) return nullptr;
+    lib_decode8 = reinterpret_cast<decltype(&crisp_decode8)>(PyLong_AsVoidPtr(args[3]));
+    lib_encode8_sizes = reinterpret_cast<decltype(&crisp_encode8_sizes)>(PyLong_AsVoidPtr(args[4]));
+    lib_encode8 = reinterpret_cast<decltype(&crisp_encode8)>(PyLong_AsVoidPtr(args[5]));
+    lib_destroy8 = reinterpret_cast<decltype(&crisp_destroy8)>(PyLong_AsVoidPtr(args[6]));
     lib_decode = reinterpret_cast<decltype(&crisp_decode)>(PyLong_AsVoidPtr(args[0]));
     lib_spmm8_sizes = reinterpret_cast<decltype(&crisp_spmm8_sizes)>(PyLong_AsVoidPtr(args[1]));
     lib_spmm8 = reinterpret_cast<decltype(&crisp_spmm8)>(PyLong_AsVoidPtr(args[2]));
@@ -297,7 +339,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 #define CRISP_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {CRISP_METHOD(bind), CRISP_METHOD(table), CRISP_METHOD(encodings), CRISP_METHOD(encoded), CRISP_METHOD(decode), CRISP_METHOD(gradients), CRISP_METHOD(product8), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {CRISP_METHOD(bind), CRISP_METHOD(table), CRISP_METHOD(encodings), CRISP_METHOD(encoded), CRISP_METHOD(decode), CRISP_METHOD(gradients), CRISP_METHOD(product8), CRISP_METHOD(encode8), CRISP_METHOD(decode8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_network", nullptr, 0, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace
