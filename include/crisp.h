@@ -526,8 +526,9 @@ CRISP_API crisp_status_t crisp_spmm8(crisp_handle8_t h, const uint16_t *d_x_bf16
 CRISP_API crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_act, int64_t ncols, void *d_y, int64_t ldy, int32_t y_layout,
                                                int32_t y_dtype, void *stream);
 
-/* crisp_set_epilogue, crisp_last_launch (stack: CTAs that share one tile's blocks), crisp_device_status, crisp_reset_status and crisp_set_tuning of an 8-bit handle.
- * tile_cols: columns a tile, 64, 128, 192 or 256, or 16 or 32 for products of no more columns (else it is not heeded); split: CTAs that share a tile, 1 to 8; 0 = chosen
+/* crisp_set_epilogue, crisp_last_launch (stack: CTAs that share one tile's blocks, -1 for pairs), crisp_device_status, crisp_reset_status and crisp_set_tuning of an 8-bit handle.
+ * tile_cols: columns a tile, 64, 128, 192 or 256, or 16 or 32 for products of no more columns (else it is not heeded); split: CTAs that share a tile, 1 to 8, or -1:
+ * pairs of CTAs that multiply two row tiles by 128, 192 or 256 columns with one instruction, for layers of two row tiles and more that keep every block; 0 = chosen
  * by the library. */
 CRISP_API crisp_status_t crisp_set_epilogue8(crisp_handle8_t h, const float *d_bias_f32, int32_t relu);
 CRISP_API crisp_status_t crisp_last_launch8(crisp_handle8_t h, crisp_launch_info_t *out);

@@ -259,7 +259,7 @@ PyObject *gradients(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 // encode8(mask, W, rows, k, GPU, buffer, handle that is replaced, stream) -> (status, handle, bytes that the buffer would need), or None: not a plain matrix that
-// the call takes.  Where the buffer is too small nothing is done and the handle is 0.
+// the call takes.  Where the buffer is too small nothing is done, and the handle is the old one.
 PyObject *encode8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
     if (!arguments("encode8", n, 8)) return nullptr;
@@ -275,12 +275,13 @@ PyObject *encode8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     const crisp_mask_t mask = reinterpret_cast<crisp_mask_t>((uintptr_t)v[0]);
     size_t bytes = 0;
     crisp_status_t s = lib_encode8_sizes(mask, &bytes);
-    crisp_handle8_t h = nullptr;
+    crisp_handle8_t h = reinterpret_cast<crisp_handle8_t>((uintptr_t)v[6]);          // (kept where nothing is done)
     const at::Tensor *buffer = args[5] != Py_None && THPVariable_CheckExact(args[5]) ? &THPVariable_Unpack(args[5]) : nullptr;
     if (s == CRISP_OK && buffer && (size_t)buffer->numel() >= bytes) {
         const int64_t ld = w->size(0) > 1 ? w->stride(0) : w->size(1);
         Py_BEGIN_ALLOW_THREADS
-        lib_destroy8(reinterpret_cast<crisp_handle8_t>((uintptr_t)v[6]));
+        lib_destroy8(h);
+        h = nullptr;
         s = lib_encode8(static_cast<const uint16_t *>(w->data_ptr()), ld, mask, buffer->data_ptr(), reinterpret_cast<void *>((uintptr_t)v[7]), &h);
         Py_END_ALLOW_THREADS
         bytes = 0;

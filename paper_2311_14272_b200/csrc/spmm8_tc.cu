@@ -28,7 +28,8 @@ using namespace block8;
 struct Plan8 {                               // launch plan for one activation buffer and number of columns
     const void *act;
     int64_t ncols;
-    int tile;                                // columns a tile
+    int box;                                 // columns a copy brings
+    int chunks;                              // and chunks of 128 scales
     CUtensorMap map_x, map_s;
 };
 
@@ -38,7 +39,7 @@ struct crisp_handle8_s {
     crisp::Geometry g;
     uint8_t *buf;
     crisp::Epilogue epilogue;
-    int tile_cols, split;                    // tuning: columns a tile and CTAs that share one (0 = chosen by the library)
+    int tile_cols, split;                    // tuning: columns a tile and CTAs that share one, -1 for pairs (0 = chosen by the library)
     unsigned long long wait_limit_cycles;
     int skip_fill;
     CUtensorMap map_a;
@@ -514,6 +515,235 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     }
 }
 
+// ------------------------------------------------------------------------------------------------ pairs of SMs
+//
+// Where every block is kept, two row tiles walk the same list, and two CTAs (a cluster) multiply 256 rows by N columns with cta_group::2: each holds its row tile's
+// weights and half of the columns, and the tensor cores of both read both halves.  What bounds the single CTA's MMAs is the operands they read from shared memory, 64
+// bytes a cycle (128 x N x 32: 4 KB + 32 N bytes; 98, 118, 160 and 191 cycles measured for 64, 128, 192 and 256 columns where the products need 32, 64, 96 and 128); a
+// pair reads half of the columns' bytes a CTA, and fetches half of them from L2.
+//
+// The CTA of rank 0 issues for both.  Its peer's stages are announced to it by the peer's warp 1; commits go to both (multicast); accumulators are handed back by the
+// draining warps of both.
+template <int N>
+struct Pair8 {
+    static constexpr int kChunks = N <= 128 ? 1 : 2;
+    static constexpr int kAcc = N <= 192 ? 2 : 1;
+    static constexpr int kScaleCols = 4 + 4 * kChunks;
+    static constexpr uint32_t kX = 17 * 1024;
+    static constexpr uint32_t kS = kX + N / 2 * 128;
+    static constexpr uint32_t kStage = (kS + kChunks * kScales8 + 1023) / 1024 * 1024;
+    static constexpr uint32_t kBytes = kEntry8 + N / 2 * 128 + kChunks * kScales8;
+    static constexpr int kEpi = 8;
+    static constexpr uint32_t kStaging = 4096;
+    static constexpr uint32_t kFixed = kEpi * kStaging + 384;
+    static constexpr int kMost = (int)((kSmemBudget - kFixed) / kStage), kStages = kMost < 12 ? kMost : 12;
+    static_assert(kAcc * N + 2 * kScaleCols <= 512, "tensor memory is 512 columns");
+    static_assert(N % 64 == 0 && N / 2 * 128 % 1024 == 0, "halves are whole atoms, and scales begin at even columns");
+};
+
+__device__ __forceinline__ void copy_scales_pair(uint32_t taddr, uint64_t desc) {
+    asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(desc) : "memory");
+}
+__device__ __forceinline__ void mma_scaled_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %6, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {          // to the barrier at this place in both CTAs
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+
+template <int N>
+__global__ void __launch_bounds__(32 * (4 + Pair8<N>::kEpi), 1)
+spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_s,
+                  const __grid_constant__ Params8 p, int) {
+    using T = Pair8<N>;
+    constexpr int kEpi = T::kEpi, kTmemCols = 512;
+    extern __shared__ __align__(1024) uint8_t smem_raw[];
+    const uint32_t ring = smem_u32(smem_raw);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t staging = ring + T::kStages * T::kStage, ctrl = staging + kEpi * T::kStaging;
+    uint8_t *ctrl_gen = smem_raw + (ctrl - ring);
+    // barriers: full[s], empty[s] and (rank 0) the peer's full[s], s < 12; accumulators full, and (rank 0) empty
+    const uint32_t bar_full = ctrl, bar_empty = ctrl + 96, bar_peer = ctrl + 192, bar_tfull = ctrl + 288, bar_tempty = ctrl + 304;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 320);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(ctrl_gen + 324);
+    const uint32_t rank = cluster_rank();
+    const bool aligned = (ring & 1023u) == 0;
+    if (warp == 1) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(const_cast<uint32_t *>(tmem_slot))), "r"(kTmemCols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    if (threadIdx.x == 0) {
+        prefetch_tensormap(&map_a); prefetch_tensormap(&map_x); prefetch_tensormap(&map_s);
+        for (int s = 0; s < T::kStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); mbar_init(bar_peer + 8 * s, 1); }
+        for (int a = 0; a < T::kAcc; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, 2 * kEpi); }
+        *abort_flag = aligned ? 0 : 1;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (!p.early) wait_for_prerequisites();
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive();                                        // (the peer's barriers are there, and its tensor memory)
+    cluster_wait();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    if (p.early && warp != 0) wait_for_prerequisites();
+    const int pairs = (p.nrt + 1) >> 1, tile0 = (int)(blockIdx.x >> 1), tile_step = (int)(gridDim.x >> 1), len = p.kkeep;
+
+    if (warp == 0) {
+        // -------------------------------------------------- this CTA's weights (an odd number of row tiles: the last one's once more), and its byte count
+        const bool leader = elect_one();
+        uint32_t dst = ring, full = bar_full, empty = bar_empty, ph = 0;
+        int s = 0, fill = 0;
+        bool ok = true;
+        for (int t = tile0; t < p.num_tiles && ok; t += tile_step) {
+            int row = min(2 * (t % pairs) + (int)rank, p.nrt - 1) * len * (int)(kEntry8 / 256);
+            for (int e = 0; e < len; ++e) {
+                if (!wait_warp<true>(empty, ph ^ 1u, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                if (leader) {
+                    mbar_expect_tx(full, T::kBytes);
+                    if (fill != p.skip_fill) tma_load_2d(dst, &map_a, 0, row, full);
+                }
+                ++fill;
+                row += kEntry8 / 256;
+                dst += T::kStage; full += 8; empty += 8;
+                if (++s == T::kStages) { s = 0; dst = ring; full = bar_full; empty = bar_empty; ph ^= 1u; }
+            }
+        }
+        wait_for_prerequisites();
+    } else if (warp >= 2 + kEpi) {
+        // -------------------------------------------------- this CTA's half of the columns, and the scales of all of them
+        const bool leader = elect_one(), codes = warp == 2 + kEpi;
+        const uint32_t at = codes ? T::kX : T::kS;
+        uint32_t dst = ring + at, full = bar_full, empty = bar_empty, ph = 0;
+        int s = 0, fill = 0;
+        bool ok = true;
+        const int pitch = (int)(codes ? p.groups * 4 : p.chunks * 2);
+        for (int t = tile0; t < p.num_tiles && ok; t += tile_step) {
+            const int64_t c0 = (int64_t)(t / pairs) * N;
+            int row = (int)(codes ? ((c0 >> 3) + rank * (N / 16)) * 4 : (c0 >> 7) * 2);
+            for (int e = 0; e < len; ++e) {
+                if (!wait_warp<false>(empty, ph ^ 1u, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                if (leader && fill != p.skip_fill) {
+                    if (codes) tma_load_2d(dst, &map_x, 0, row, full);
+                    else tma_load_2d(dst, &map_s, 0, row, full);
+                }
+                ++fill;
+                row += pitch;
+                dst += T::kStage; full += 8; empty += 8;
+                if (++s == T::kStages) { s = 0; dst = ring + at; full = bar_full; empty = bar_empty; ph ^= 1u; }
+            }
+        }
+    } else if (warp == 1 && rank == 1) {
+        // -------------------------------------------------- tells rank 0 which stages are here
+        const bool leader = elect_one();
+        const uint32_t there = peer_address(bar_peer, 0);
+        uint32_t ph = 0;
+        int s = 0;
+        bool ok = true;
+        for (int t = tile0; t < p.num_tiles && ok; t += tile_step)
+            for (int e = 0; e < len; ++e) {
+                if (!wait_warp<false>(bar_full + 8 * s, ph, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                if (leader) mbar_arrive_at(there + 8 * s);
+                if (++s == T::kStages) { s = 0; ph ^= 1u; }
+            }
+    } else if (warp == 1) {
+        // -------------------------------------------------- scales to tensor memory and MMAs, of both CTAs
+        constexpr uint32_t idesc = (1u << 23) | ((uint32_t)(N >> 3) << 17) | (16u << 24);       // as make_idesc8, M = 256
+        const bool leader = elect_one();
+        const uint64_t a0 = make_smem_desc(ring, 16, 1024, kLayoutSw128), b0 = make_smem_desc(ring + T::kX, 16, 1024, kLayoutSw128);
+        const uint64_t sa0 = make_smem_desc(ring + kTile8, 128, 128, kLayoutNone), sb0 = make_smem_desc(ring + T::kS, 128, 128, kLayoutNone);
+        const uint32_t scales = tmem + T::kAcc * N;
+        uint32_t off = 0, ph = 0, acc = 0, acc_ph = 0, set = 0;
+        int s = 0;
+        for (int t = tile0; t < p.num_tiles; t += tile_step) {
+            const uint32_t shift = (uint32_t)((int64_t)(t / pairs) * N & 127) >> 5;
+            if (!wait_warp<false>(bar_tempty + 8 * acc, acc_ph ^ 1u, leader, abort_flag, p.wait_limit)) break;
+            tc_fence_after();
+            const uint32_t d = tmem + acc * N;
+            bool ok = true;
+            for (int e = 0; e < len; ++e) {
+                if (!wait_warp<false>(bar_full + 8 * s, ph, leader, abort_flag, p.wait_limit) ||
+                    !wait_warp<false>(bar_peer + 8 * s, ph, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                tc_fence_after();
+                const uint32_t sa = scales + set * T::kScaleCols, sb = sa + 4;
+                if (leader) {
+                    copy_scales_pair(sa, sa0 + off);
+#pragma unroll
+                    for (int c = 0; c < T::kChunks; ++c) copy_scales_pair(sb + 4 * c, sb0 + off + c * (kScales8 >> 4));
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) mma_scaled_pair(d, a0 + off + 2 * j, b0 + off + 2 * j, idesc, sa, sb + shift, (uint32_t)(e | j));
+                    mma_commit_pair(bar_empty + 8 * s);
+                }
+                set ^= 1u;
+                off += T::kStage >> 4;
+                if (++s == T::kStages) { s = 0; off = 0; ph ^= 1u; }
+            }
+            if (!ok) break;
+            if (leader) mma_commit_pair(bar_tfull + 8 * acc);
+            if (++acc == T::kAcc) { acc = 0; acc_ph ^= 1u; }
+        }
+    } else {
+        // -------------------------------------------------- drain: this CTA's row tile
+        const int ew = warp - 2, q = warp & 3, part = ew >> 2;
+        uint8_t *stage = smem_raw + (staging - ring) + ew * T::kStaging;
+        const uint32_t back = peer_address(bar_tempty, 0);
+        uint32_t acc = 0, acc_ph = 0;
+        for (int t = tile0; t < p.num_tiles; t += tile_step) {
+            const int row0 = (2 * (t % pairs) + (int)rank) * 128 + 32 * q;
+            const int64_t c0 = (int64_t)(t / pairs) * N;
+            int go = 0;
+            if (lane == 0) go = !*abort_flag && mbar_wait(bar_tfull + 8 * acc, acc_ph, abort_flag, p.wait_limit);
+            go = __shfl_sync(0xFFFFFFFFu, go, 0);
+            if (!go) break;
+            tc_fence_after();
+            const uint32_t from = tmem + acc * N + ((uint32_t)(32 * q) << 16);
+            constexpr int kMine = N / 64;
+            uint32_t r[kMine][32];
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) tmem_ld32(from + 32 * (kMine * part + i), r[i]);
+            tmem_ld_wait();
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive_at(back + 8 * acc);
+            if (++acc == T::kAcc) { acc = 0; acc_ph ^= 1u; }
+            const float bias = p.bias != nullptr && row0 + lane < p.rows ? p.bias[row0 + lane] : 0.f;
+#pragma unroll
+            for (int i = 0; i < kMine; ++i) {
+                const int c = 32 * (kMine * part + i);
+                if (c0 + c >= p.ncols || row0 >= p.rows) break;
+                float x[32];
+#pragma unroll
+                for (int j = 0; j < 32; ++j) x[j] = activation(__uint_as_float(r[i][j]) + bias, p.relu);
+                if (p.f32) store_chunk8<true>(p, stage, lane, x, row0, c0 + c);
+                else store_chunk8<false>(p, stage, lane, x, row0, c0 + c);
+            }
+        }
+    }
+    __syncwarp();
+    if (warp == 1) launch_dependents();
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0) atomicCAS(p.status, 0, (int)(aligned ? CRISP_TIMEOUT : CRISP_CUDA_ERROR));
+        const unsigned long long t0 = clock64();             // (copies that may still be in flight land)
+        while ((unsigned long long)(clock64() - t0) < 2000000ull) __nanosleep(1000);
+        __syncthreads();
+    }
+    cluster_arrive();                                        // neither CTA's memory is read by the other any more
+    cluster_wait();
+    if (warp == 1) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(kTmemCols) : "memory");
+    }
+}
+
 typedef void (*Kernel8)(const CUtensorMap, const CUtensorMap, const CUtensorMap, const Params8, int);
 
 constexpr int kMaxDevices = 64;
@@ -548,6 +778,14 @@ Variant8 variant8(int tile) {
     }
 }
 
+template <int N>
+Variant8 make_pair_variant8() {
+    static std::atomic<bool> configured[kMaxDevices];
+    using T = Pair8<N>;
+    return Variant8{spmm8_pair_kernel<N>, 32 * (4 + T::kEpi), T::kStages, T::kStages * T::kStage + T::kFixed, configured};
+}
+Variant8 pair_variant8(int tile) { return tile == 128 ? make_pair_variant8<128>() : tile == 192 ? make_pair_variant8<192>() : make_pair_variant8<256>(); }
+
 // The products that quantise X themselves.
 bool fused8(int64_t ncols) { return ncols <= 32; }
 template <bool kSplit>
@@ -560,21 +798,30 @@ bool fits8(int tile, int64_t ncols) { return tile >= 64 || ncols <= tile; }
 // fixed time beside them, the sum over a cluster one that grows with the columns a CTA has to add up; tiles come in waves of as many as there are SMs.  Measured on
 // 4096 x 4096 in a row, all blocks kept: 64 columns a tile 11.7 us for 128 tiles (256 columns) and 206 for 28 waves (8192), 128 columns 12.9 and 128, 192 columns
 // 15.2 and 115, 256 columns 19.6 and 116; two, four CTAs a tile: 64 columns 11.6, 9.3, 128 columns 12.6, 9.9, 256 columns 18.9, 11.6.
-void choose8(const crisp_handle8_s *h, int64_t ncols, int sms, int *tile, int *split) {
+void choose8(const crisp_handle8_s *h, int64_t ncols, int sms, int *tile, int *split, bool *pair) {
     struct Cost { int cols; double block, tile; };
     static const Cost costs[] = {{16, 0.17, 0.5}, {32, 0.17, 0.5}, {64, 0.20, 0.6}, {128, 0.24, 0.8}, {192, 0.31, 1.0}, {256, 0.43, 1.4}};
     const Geometry &g = h->g;
     double best = 1e300;
-    *tile = 64; *split = 1;
+    *tile = 64; *split = 1; *pair = false;
     for (const Cost &c : costs) {
         if (!fits8(c.cols, ncols) || (h->tile_cols && fits8(h->tile_cols, ncols) && c.cols != h->tile_cols)) continue;
         const int64_t tiles = (int64_t)g.nrt * ((ncols + c.cols - 1) / c.cols);
         for (int s = 1; s <= 8 && s <= std::max(1, g.kkeep); ++s) {
-            if (h->split ? s != std::min(h->split, std::max(1, g.kkeep)) : s > 1 && (tiles * s > sms || 2 * s > g.kkeep)) continue;
+            if (h->split > 0 ? s != std::min(h->split, std::max(1, g.kkeep)) : s > 1 && (tiles * s > sms || 2 * s > g.kkeep)) continue;
             const double waves = (double)((tiles * s + sms - 1) / sms);
             const double t = waves * (c.block * ((g.kkeep + s - 1) / s) + c.tile) + (s > 1 ? 0.9 + c.cols / (48.0 * s) : 0.0);
             if (t < best) { best = t; *tile = c.cols; *split = s; }
         }
+    }
+    if (g.kkeep < g.nblk || g.nrt < 2 || h->split > 0) return;
+    static const Cost pairs[] = {{128, 0.22, 1.0}, {192, 0.26, 1.5}, {256, 0.30, 2.0}};
+    if (h->split == -1) best = 1e300;
+    for (const Cost &c : pairs) {
+        if (h->tile_cols && h->tile_cols != c.cols && h->tile_cols >= 128) continue;
+        const int64_t tiles = (int64_t)((g.nrt + 1) / 2) * ((ncols + c.cols - 1) / c.cols);
+        const double waves = (double)((tiles + sms / 2 - 1) / (sms / 2)), t = waves * (c.block * g.kkeep + c.tile);
+        if (t < best && (h->split == -1 || !h->tile_cols)) { best = t; *tile = c.cols; *split = 1; *pair = true; }
     }
 }
 
@@ -602,10 +849,12 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int
     if (device < 0 || device >= kMaxDevices) return cudaErrorInvalidDevice;
     const Geometry &g = h->g;
     int tile, split;
-    choose8(h, ncols, sm_count_of(device), &tile, &split);
+    bool pair;
+    choose8(h, ncols, sm_count_of(device), &tile, &split, &pair);
     if (x && tile > 32) tile = 32;
+    if (x) pair = false;
     const Act8 a = act8(g.k, ncols);
-    const Variant8 v = x ? (split > 1 ? fused_variant8<true>(tile) : fused_variant8<false>(tile)) : split > 1 ? variant8<true>(tile) : variant8<false>(tile);
+    const Variant8 v = pair ? pair_variant8(tile) : x ? (split > 1 ? fused_variant8<true>(tile) : fused_variant8<false>(tile)) : split > 1 ? variant8<true>(tile) : variant8<false>(tile);
     if (!v.configured[device].load(std::memory_order_relaxed)) {
         e = cudaFuncSetAttribute(reinterpret_cast<const void *>(v.kern), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget + 1024);
         if (e != cudaSuccess) return e;
@@ -613,17 +862,17 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int
     }
     Plan8 plan;
     Params8 p{};
+    const int box = pair ? tile / 2 : tile, chunks = tile <= 128 ? 1 : 2;
     {
         std::lock_guard<std::mutex> hold(h->plan_lock);
         plan = h->plan;
         p.early = behind || h->settled.holds(st, moment);
     }
-    if (g.kkeep > 0 && !x && (plan.act != d_act || plan.ncols != ncols || plan.tile != tile)) {
+    if (g.kkeep > 0 && !x && (plan.act != d_act || plan.ncols != ncols || plan.box != box || plan.chunks != chunks)) {
         e = ensure_context(device);
         if (e != cudaSuccess) return e;
-        plan.act = d_act; plan.ncols = ncols; plan.tile = tile;
-        const int chunks = tile <= 128 ? 1 : 2;
-        if (!make_map_bytes(&plan.map_x, d_act, a.scale_off, tile / 2) ||
+        plan.act = d_act; plan.ncols = ncols; plan.box = box; plan.chunks = chunks;
+        if (!make_map_bytes(&plan.map_x, d_act, a.scale_off, box / 2) ||
             !make_map_bytes(&plan.map_s, reinterpret_cast<const uint8_t *>(d_act) + a.scale_off, a.total - a.scale_off, 2 * chunks))
             return cudaErrorInvalidValue;
         std::lock_guard<std::mutex> hold(h->plan_lock);
@@ -636,7 +885,7 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int
     p.status = reinterpret_cast<int32_t *>(h->buf);
     p.y = d_y; p.bias = h->epilogue.bias; p.ldy = ldy; p.ncols = ncols; p.groups = a.groups; p.chunks = a.chunks;
     p.rows = g.rows; p.nrt = g.nrt; p.kkeep = g.kkeep;
-    p.num_tiles = (int)((int64_t)g.nrt * ((ncols + tile - 1) / tile));
+    p.num_tiles = (int)((int64_t)(pair ? (g.nrt + 1) / 2 : g.nrt) * ((ncols + tile - 1) / tile));
     p.y_layout = y_layout; p.f32 = y_dtype; p.relu = h->epilogue.relu;
     const int size = y_dtype ? 4 : 2;
     p.vec_ok = aligned_to(d_y, 16) && ldy * size % 16 == 0;
@@ -644,8 +893,8 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int
     p.wait_limit = h->wait_limit_cycles ? h->wait_limit_cycles : kWaitLimitCycles;
     p.skip_fill = h->skip_fill;
     const int sms = sm_count_of(device);
-    const unsigned grid = (unsigned)(split > 1 ? p.num_tiles * split : (p.num_tiles < sms ? p.num_tiles : sms));
-    const auto launch = [&] { return launch_clusters(v.kern, grid, (unsigned)v.threads, v.smem, st, (unsigned)split, h->map_a, plan.map_x, plan.map_s, p, split); };
+    const unsigned grid = (unsigned)(pair ? 2 * std::min(p.num_tiles, sms / 2) : split > 1 ? p.num_tiles * split : std::min(p.num_tiles, sms));
+    const auto launch = [&] { return launch_clusters(v.kern, grid, (unsigned)v.threads, v.smem, st, pair ? 2u : (unsigned)split, h->map_a, plan.map_x, plan.map_s, p, split); };
     e = behind ? launch() : launch_product(encodes, p, moment, launch);
     if (e == cudaSuccess) {
         std::lock_guard<std::mutex> hold(h->plan_lock);
@@ -654,7 +903,7 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int
             cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
             h->settled.note(st, moment, st != cudaStreamPerThread && cudaStreamIsCapturing(st, &capture) == cudaSuccess && capture == cudaStreamCaptureStatusNone);
         }
-        h->last = crisp_launch_info_t{CRISP_PATH_DENSE, tile, tile <= 192 ? 2 : 1, split, tile >= 128 ? 8 : 4, v.stages, (int32_t)grid, 0, 1};
+        h->last = crisp_launch_info_t{CRISP_PATH_DENSE, tile, tile <= 192 ? 2 : 1, pair ? -1 : split, tile >= 128 ? 8 : 4, v.stages, (int32_t)grid, 0, 1};
     }
     return e;
 }
@@ -792,7 +1041,7 @@ crisp_status_t crisp_reset_status8(crisp_handle8_t h, void *stream) {
 }
 
 crisp_status_t crisp_set_tuning8(crisp_handle8_t h, int32_t tile_cols, int32_t split, uint64_t wait_limit_cycles, int32_t skip_fill) {
-    if (!h || skip_fill < -1 || split < 0 || split > 8) return CRISP_INVALID_ARG;
+    if (!h || skip_fill < -1 || split < -1 || split > 8) return CRISP_INVALID_ARG;
     if (tile_cols != 0 && tile_cols != 16 && tile_cols != 32 && tile_cols != 64 && tile_cols != 128 && tile_cols != 192 && tile_cols != 256) return CRISP_INVALID_ARG;
     h->tile_cols = tile_cols;
     h->split = split;

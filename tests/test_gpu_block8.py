@@ -155,6 +155,35 @@ def test_the_result_does_not_depend_on_the_tiling(tile, split):
         L.set_tuning8(split=9)
 
 
+@pytest.mark.parametrize("tile", [128, 192, 256])
+@pytest.mark.parametrize("rows,k,ncols", [(256, 128, 256), (257, 1000, 333), (640, 2304, 700), (130, 512, 65), (512, 700, 3000)])
+def test_pairs_of_sms(rows, k, ncols, tile):
+    """Two row tiles (the last of an odd number with itself) multiplied by one instruction; as many tiles as pairs, and more."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, w, _ = layer(B, torch, rows, k, 4, 4, 1.0, 35)
+    x = activations(np.random.default_rng(36), k, ncols)
+    held = ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64))
+    d_x = bf16_dev(x, torch)
+    bias = np.random.default_rng(37).standard_normal(rows).astype(np.float32)
+    L.set_epilogue8(to_dev(bias, torch), relu=True)
+    L.set_tuning8(tile_cols=tile, split=-1)
+    for tokens in (False, True):
+        for f32 in (0, 1):
+            y = L.spmm8(d_x.t().contiguous() if tokens else d_x, tokens=tokens, y_dtype=f32)
+            info = L.last_launch8()
+            assert info["tile_cols"] == tile and info["stack"] == -1 and L.device_status8() == 0
+            check(numbers(y.t() if tokens else y), w, held, k, f32, bias.astype(np.float64), True)
+    L.set_tuning8(tile_cols=tile, split=-1, wait_limit_cycles=2_000_000, skip_fill=0)
+    L.spmm8(d_x)
+    assert L.device_status8() == B.TIMEOUT
+    L.reset_status8()
+    L.set_tuning8(tile_cols=tile, split=-1)
+    again = L.spmm8(d_x)
+    assert L.device_status8() == 0
+    check(numbers(again), w, held, k, 0, bias.astype(np.float64), True)
+
+
 @pytest.mark.parametrize("ncols,tile", [(1, 32), (16, 64), (20, 64), (32, 32)])
 def test_narrow_tiles_that_are_not_the_first_choice(ncols, tile):
     import torch
