@@ -8,8 +8,12 @@ namespace crisp {
 namespace block8 {
 
 __device__ __forceinline__ float2 floats(uint32_t pair) { return make_float2(__uint_as_float(pair << 16), __uint_as_float(pair & 0xFFFF0000u)); }
-// The larger magnitudes of two pairs of bf16, as their bits.
-__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t pair) { return __vmaxu2(a, pair & 0x7FFF7FFFu); }
+// The larger magnitudes of two pairs of bf16, as their bits (NaN if one is).
+__device__ __forceinline__ uint32_t larger(uint32_t a, uint32_t pair) {
+    uint32_t r;
+    asm("{\n\t.reg .b32 m;\n\tabs.bf16x2 m, %2;\n\tmax.NaN.bf16x2 %0, %1, m;\n\t}" : "=r"(r) : "r"(a), "r"(pair));
+    return r;
+}
 __device__ __forceinline__ uint32_t larger_of(uint32_t a) { return max(a & 0xFFFFu, a >> 16); }
 // What is not finite becomes NaN and leaves the block's largest value alone: the pair with zeros in its place.
 __device__ __forceinline__ uint32_t finite(uint32_t pair) {

@@ -151,41 +151,38 @@ __device__ __forceinline__ void put_scale(uint8_t *scales, int64_t chunks, int64
     *reinterpret_cast<uint32_t *>(scales + (kb * chunks + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4) = e * 0x01010101u;
 }
 
-// X [ncols, k]: a CTA takes eight columns (tokens) and 2 U k-blocks; 16 threads a block of one column, eight values each, U blocks a thread.
-template <int U>
-__global__ void __launch_bounds__(256)
-quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
-                       int vec_ok) {
-    wait_for_prerequisites();
-    launch_dependents();                     // (a product behind this one fetches weights meanwhile: all before this kernel has finished)
-    const int64_t spans = (nblk + 2 * U - 1) / (2 * U);
-    const int64_t group = blockIdx.x / spans, kb0 = (blockIdx.x - group * spans) * (2 * U);
+// X [ncols, k]: a CTA takes eight columns (tokens) and 2 U k-blocks; 16 threads a block of one column, eight values each, U blocks a thread.  Bound by instructions
+// (4096 x 8192: 20 a value and 22 us as one loop over the blocks with every question asked in it; now 16.8, 6.0 TB/s): a CTA whose blocks are all there asks nothing,
+// and two blocks' largest values travel through the shuffles in one word.
+template <int U, bool kFull>
+__device__ __forceinline__ void quantize_tokens(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes,
+                                                uint8_t *scales, int vec_ok, int64_t group, int64_t kb0) {
     const int lane = threadIdx.x & 15, r = threadIdx.x >> 4 & 7, side = threadIdx.x >> 7;
-    const int64_t col = group * 8 + r;
-    uint32_t v[U][4], top[U] = {};
+    const int64_t col = group * 8 + r, kb1 = kb0 + side * U;         // (a warp's two columns share their k-blocks)
+    uint32_t v[U][4], top[U], word[U / 2], any = 0;
+    const uint16_t *from = x + col * ldx + kb1 * 128 + lane * 8;
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const int64_t at = (kb0 + side * U + i) * 128 + lane * 8;
+        const int64_t at = (kb1 + i) * 128 + lane * 8;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i][j] = 0;
-        if (col < ncols && at < k) {
-            const uint16_t *p = x + col * ldx + at;
-            if (vec_ok && at + 8 <= k) {
-                const uint4 u = *reinterpret_cast<const uint4 *>(p);
-                v[i][0] = u.x; v[i][1] = u.y; v[i][2] = u.z; v[i][3] = u.w;
-            } else {
+        if (kFull || (vec_ok && col < ncols && at + 8 <= k)) {
+            const uint4 u = *reinterpret_cast<const uint4 *>(from + i * 128);
+            v[i][0] = u.x; v[i][1] = u.y; v[i][2] = u.z; v[i][3] = u.w;
+        } else if (col < ncols) {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (at + j < k) v[i][j / 2] |= (uint32_t)p[j] << (16 * (j & 1));
-            }
+            for (int j = 0; j < 8; ++j)
+                if (at + j < k) v[i][j / 2] |= (uint32_t)from[i * 128 + j] << (16 * (j & 1));
         }
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const int64_t kb = kb0 + side * U + i;
+        top[i] = larger(larger(larger(larger(0, v[i][0]), v[i][1]), v[i][2]), v[i][3]);
+        any = __vmaxu2(any, top[i]);
+    }
+    if (__any_sync(0xFFFFFFFFu, larger_of(any) >= 0x7F80u)) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) top[i] = larger(top[i], v[i][j]);
-        if (__any_sync(0xFFFFFFFFu, larger_of(top[i]) >= 0x7F80u)) {
+        for (int i = 0; i < U; ++i) {
             top[i] = 0;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
@@ -193,16 +190,39 @@ quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols,
                 v[i][j] = nan_for_infinity(v[i][j]);
             }
         }
-        uint32_t t = larger_of(top[i]);
-#pragma unroll
-        for (int d = 8; d; d >>= 1) t = max(t, __shfl_xor_sync(0xFFFFFFFFu, t, d));
-        const uint32_t e = exponent_of(t);
-        const float down = power_of(254u - e);
-        if (kb >= nblk) continue;            // (the whole warp: its two columns share the k-block)
-        uint8_t *at = codes + (kb * groups + group) * 1024 + r * 128 + (((lane >> 1) ^ r) << 4) + (lane & 1) * 8;
-        *reinterpret_cast<uint2 *>(at) = make_uint2(codes2(v[i][0], down) | codes2(v[i][1], down) << 16, codes2(v[i][2], down) | codes2(v[i][3], down) << 16);
-        if (lane == 0 && col < ncols) put_scale(scales, chunks, kb, col, e);
     }
+#pragma unroll
+    for (int i = 0; i < U / 2; ++i) word[i] = larger_of(top[2 * i]) | larger_of(top[2 * i + 1]) << 16;
+#pragma unroll
+    for (int d = 8; d; d >>= 1)
+#pragma unroll
+        for (int i = 0; i < U / 2; ++i) word[i] = __vmaxu2(word[i], __shfl_xor_sync(0xFFFFFFFFu, word[i], d));
+    uint8_t *to = codes + (kb1 * groups + group) * 1024 + r * 128 + (((lane >> 1) ^ r) << 4) + (lane & 1) * 8;
+    uint8_t *scale = scales + (kb1 * chunks + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4;
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        if (!kFull && kb1 + i >= nblk) break;
+        const uint32_t e = exponent_of(word[i / 2] >> (16 * (i & 1)) & 0xFFFFu);
+        const float down = power_of(254u - e);
+        *reinterpret_cast<uint2 *>(to) = make_uint2(codes2(v[i][0], down) | codes2(v[i][1], down) << 16, codes2(v[i][2], down) | codes2(v[i][3], down) << 16);
+        if (lane == 0 && (kFull || col < ncols)) *reinterpret_cast<uint32_t *>(scale) = e * 0x01010101u;
+        to += groups * 1024;
+        scale += chunks * kScales8;
+    }
+}
+
+template <int U>
+__global__ void __launch_bounds__(256)
+quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
+                       int vec_ok) {
+    wait_for_prerequisites();
+    launch_dependents();                     // (a product behind this one fetches weights meanwhile: all before this kernel has finished)
+    const uint32_t spans = (uint32_t)((nblk + 2 * U - 1) / (2 * U)), g = blockIdx.x / spans;
+    const int64_t group = g, kb0 = (int64_t)(blockIdx.x - g * spans) * (2 * U);
+    if (vec_ok && (kb0 + 2 * U) * 128 <= k && group * 8 + 8 <= ncols)
+        quantize_tokens<U, true>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, vec_ok, group, kb0);
+    else
+        quantize_tokens<U, false>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, vec_ok, group, kb0);
 }
 
 // X [k, ncols]: a CTA takes 128 columns of one k-block.  A warp reads 16 rows of it, a lane four neighbouring columns; the 16 values of a column in a warp are one
@@ -219,7 +239,7 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row0 = kb * 128 + warp * 16;
     uint32_t v[2][16], top[2] = {0, 0};
-    if (quad_ok && c0 + 128 <= ncols && row0 + 16 <= k) {
+    if (quad_ok && c0 + 4 * lane + 4 <= ncols && row0 + 16 <= k) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const uint2 two = *reinterpret_cast<const uint2 *>(x + (row0 + i) * ldx + c0 + 4 * lane);
