@@ -98,7 +98,8 @@ def _bind_network():
             from . import _network as module
             if getattr(module, "built_for", None) == "%s %d.%d" % (release, *sys.version_info[:2]):
                 module.bind(*[C.cast(f, C.c_void_p).value for f in (lib.crisp_decode, lib.crisp_spmm8_sizes, lib.crisp_spmm8, lib.crisp_decode8,
-                                                                        lib.crisp_encode8_sizes, lib.crisp_encode8, lib.crisp_destroy8)])
+                                                                        lib.crisp_encode8_sizes, lib.crisp_encode8, lib.crisp_destroy8, lib.crisp_adamw,
+                                                                        lib.crisp_adamw_moments)])
                 _network = module
             else:
                 _network = False
@@ -1180,8 +1181,6 @@ class AdamW:
         """One step with grads[i] (bf16 or fp32, of the shape of weights[i], in rows of consecutive elements; None: the tensor is left as it is);
         grad_scale: an fp32 CUDA tensor of one element that the gradients are multiplied by (a clipping factor, say)."""
         assert len(grads) == len(self._table), "a gradient, or None, for each tensor"
-        if not (_network and type(grads) is list and _network.gradients(self._address, self.weights, self.copies, grads, self.masks)):
-            self._gradients(grads)
         p = self._params
         p.lr, (p.beta1, p.beta2), p.eps, p.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
         p.step, p.seed = self.step_count + 1, self.seed
@@ -1190,20 +1189,31 @@ class AdamW:
                 "grad_scale is an fp32 CUDA tensor of one element"
         p.d_grad_scale = grad_scale.data_ptr() if grad_scale is not None else None
         if self.device.index == _current_device():
-            self._launch(p, stream)
+            self._launch(grads, stream)
         else:
             with self.torch.cuda.device(self.device):
-                self._launch(p, stream)
+                self._launch(grads, stream)
         self.step_count += 1
         return self
 
-    def _launch(self, p, stream):
-        if self.capturable:
+    def _launch(self, grads, stream):
+        if self.capturable:                                  # (the step's own number, made before it and taken back if it is refused)
             with self.torch.cuda.stream(stream):
                 self.d_step += 1
-        code = _lib.crisp_adamw(len(self._table), self._table, p, _stream(stream))
-        if code:
-            raise CrispError(code, "crisp_adamw")
+        try:
+            code = None
+            if _network and type(grads) is list:
+                code = _network.adamw(self._address, self.weights, self.copies, grads, self.masks, C.addressof(self._params), _stream(stream))
+            if code is None:
+                self._gradients(grads)
+                code = _lib.crisp_adamw(len(self._table), self._table, self._params, _stream(stream))
+            if code:
+                raise CrispError(code, "crisp_adamw")
+        except Exception:
+            if self.capturable:
+                with self.torch.cuda.stream(stream):
+                    self.d_step -= 1
+            raise
 
     def _gradients(self, grads):
         """Fills in what a step's gradients and masks bring, or says what is wrong with them."""
@@ -1223,6 +1233,11 @@ class AdamW:
     def moments(self, stream=None):
         """(m, sqrt(v)) of 8-bit states as flat bf16 tensors, in which they are exact."""
         assert self.state_bits == 8, "32-bit states are their values"
+        if _network and self.device.index == _current_device():
+            code, *out = _network.moments(self.m, self.m_exp, self.v, self.v_exp, _stream(stream))
+            if code:
+                raise CrispError(code, "crisp_adamw_moments")
+            return out
         n = self.elements
         both = self.torch.empty_strided((2, n), (n, 1), dtype=self.torch.bfloat16, device=self.device)
         at = both.data_ptr()

@@ -24,6 +24,8 @@ decltype(&crisp_decode8) lib_decode8;
 decltype(&crisp_encode8_sizes) lib_encode8_sizes;
 decltype(&crisp_encode8) lib_encode8;
 decltype(&crisp_destroy8) lib_destroy8;
+decltype(&crisp_adamw) lib_adamw;
+decltype(&crisp_adamw_moments) lib_moments;
 
 // The names of attributes, made once.
 struct {
@@ -212,14 +214,17 @@ bool rows_of(const at::Tensor &t, int64_t (&v)[3]) {
     return true;
 }
 
-// gradients(array of crisp_adamw_tensor_t, weights, copies, gradients, masks): where the tensors of a step lie, and its masks, or None: not filled in.  The four
-// are lists of one length; an entry of `copies` and `gradients` may be None, one of `masks` a layer or None.  (The shapes and types of weights and copies
+// adamw(array of crisp_adamw_tensor_t, weights, copies, gradients, masks, crisp_adamw_t, stream) -> status: where the tensors of a step lie, and its masks, and the step;
+// or None: not a step that this takes, and nothing done.  The four are lists of one length; an entry of `copies` and `gradients` may be None, one of `masks` a layer or None.  (The shapes and types of weights and copies
 // are those that the array was made for, or it is not filled in.)
-PyObject *gradients(PyObject *, PyObject *const *args, Py_ssize_t n) {
+PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    if (!arguments("gradients", n, 5)) return nullptr;
+    if (!arguments("adamw", n, 7)) return nullptr;
     crisp_adamw_tensor_t *arr = address<crisp_adamw_tensor_t>(args[0]);
-    if (!arr) return PyErr_Occurred() ? nullptr : Py_NewRef(Py_None);
+    const crisp_adamw_t *params = address<const crisp_adamw_t>(args[5]);
+    void *stream = PyLong_AsVoidPtr(args[6]);
+    if (PyErr_Occurred()) return nullptr;
+    if (!arr || !params) Py_RETURN_NONE;
     for (int i = 1; i < 5; ++i)
         if (!PyList_CheckExact(args[i]) || PyList_GET_SIZE(args[i]) != PyList_GET_SIZE(args[1])) Py_RETURN_NONE;
     for (Py_ssize_t l = 0; l < PyList_GET_SIZE(args[1]); ++l) {
@@ -254,7 +259,37 @@ PyObject *gradients(PyObject *, PyObject *const *args, Py_ssize_t n) {
         T.d_grad = g.data_ptr(); T.ld_grad = rows[2]; T.grad_dtype = g.scalar_type() == at::kFloat;
         T.mask = static_cast<crisp_mask_t>(mask);
     }
-    Py_RETURN_TRUE;
+    crisp_status_t s;
+    Py_BEGIN_ALLOW_THREADS
+    s = lib_adamw((int32_t)PyList_GET_SIZE(args[1]), arr, params, stream);
+    Py_END_ALLOW_THREADS
+    return PyLong_FromLong(s);
+    END_HANDLE_TH_ERRORS
+}
+
+// moments(m, m's exponents, sqrt(v), its exponents, stream) -> (status, m, sqrt(v)): the buffers of 8-bit states as flat bf16 tensors
+PyObject *moments(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arguments("moments", n, 5)) return nullptr;
+    const uint8_t *p[4];
+    int64_t count = 0;
+    int gpu = 0;
+    for (int i = 0; i < 4; ++i) {
+        if (!THPVariable_CheckExact(args[i])) { PyErr_SetString(PyExc_TypeError, "moments takes plain tensors"); return nullptr; }
+        const at::Tensor &t = THPVariable_Unpack(args[i]);
+        p[i] = static_cast<const uint8_t *>(t.data_ptr());
+        if (i == 0) { count = t.numel(); gpu = t.get_device(); }
+    }
+    void *stream = PyLong_AsVoidPtr(args[4]);
+    if (PyErr_Occurred()) return nullptr;
+    const at::TensorOptions on = at::TensorOptions().dtype(at::kBFloat16).device(at::Device(at::kCUDA, (at::DeviceIndex)gpu));
+    at::Tensor m = at::empty_strided({count}, {1}, on), root = at::empty_strided({count}, {1}, on);
+    crisp_status_t s;
+    Py_BEGIN_ALLOW_THREADS
+    s = lib_moments(p[0], p[1], p[2], p[3], count, static_cast<uint16_t *>(m.data_ptr()), static_cast<uint16_t *>(root.data_ptr()), stream);
+    Py_END_ALLOW_THREADS
+    Ref a(THPVariable_Wrap(std::move(m))), b(THPVariable_Wrap(std::move(root)));
+    return a.p && b.p ? Py_BuildValue("lOO", (long)s, a.p, b.p) : nullptr;
     END_HANDLE_TH_ERRORS
 }
 
@@ -325,9 +360,12 @@ PyObject *product8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses of crisp_decode, crisp_spmm8_sizes, crisp_spmm8, crisp_decode8, crisp_encode8_sizes, crisp_encode8 and crisp_destroy8)
+// bind(addresses of crisp_decode, crisp_spmm8_sizes, crisp_spmm8, crisp_decode8, crisp_encode8_sizes, crisp_encode8, crisp_destroy8, crisp_adamw and
+// crisp_adamw_moments)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    if (!arguments("bind", n, 7)) return nullptr;
+    if (!arguments("bind", n, 9)) return nullptr;
+    lib_adamw = reinterpret_cast<decltype(&crisp_adamw)>(PyLong_AsVoidPtr(args[7]));
+    lib_moments = reinterpret_cast<decltype(&crisp_adamw_moments)>(PyLong_AsVoidPtr(args[8]));
     lib_decode8 = reinterpret_cast<decltype(&crisp_decode8)>(PyLong_AsVoidPtr(args[3]));
     lib_encode8_sizes = reinterpret_cast<decltype(&crisp_encode8_sizes)>(PyLong_AsVoidPtr(args[4]));
     lib_encode8 = reinterpret_cast<decltype(&crisp_encode8)>(PyLong_AsVoidPtr(args[5]));
@@ -340,7 +378,7 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
 }
 
 #define CRISP_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {CRISP_METHOD(bind), CRISP_METHOD(table), CRISP_METHOD(encodings), CRISP_METHOD(encoded), CRISP_METHOD(decode), CRISP_METHOD(gradients), CRISP_METHOD(product8), CRISP_METHOD(encode8), CRISP_METHOD(decode8), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {CRISP_METHOD(bind), CRISP_METHOD(table), CRISP_METHOD(encodings), CRISP_METHOD(encoded), CRISP_METHOD(decode), CRISP_METHOD(adamw), CRISP_METHOD(moments), CRISP_METHOD(product8), CRISP_METHOD(encode8), CRISP_METHOD(decode8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_network", nullptr, 0, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

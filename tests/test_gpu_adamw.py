@@ -292,6 +292,51 @@ def test_a_captured_step_goes_on_counting():
     assert np.array_equal(numbers(made[1][0][0][1]), held)
 
 
+def test_a_step_that_is_refused_changes_nothing():
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    w = torch.ones(8, 16, device="cuda")
+    for capturable in (False, True):
+        opt = B.AdamW([w], capturable=capturable)
+        for bad in ([torch.ones(16, 8, device="cuda").t()], [torch.ones(8, 15, device="cuda")], [torch.ones(8, 16)], [torch.ones(8, 16, device="cuda").double()],
+                    [torch.ones(8, 16, device="cuda").half()], [], [None, None]):
+            with pytest.raises((AssertionError, B.CrispError)):
+                opt.step(bad)
+        opt.betas = (1.0, 0.999)
+        with pytest.raises(B.CrispError):
+            opt.step([torch.ones(8, 16, device="cuda")])
+        assert opt.step_count == 0 and (not capturable or int(opt.d_step) == 0) and torch.all(w == 1) and not opt.m.any()
+    with pytest.raises(AssertionError):
+        B.AdamW([w, w])
+    with pytest.raises(AssertionError):
+        B.AdamW([w, w[1:3]])
+    with pytest.raises(AssertionError):
+        B.AdamW([w.half()])
+    with pytest.raises(AssertionError):
+        B.AdamW([w.bfloat16()], copies=[w.bfloat16()])
+    other = B.HybridLayer(8, 20, 2, 4, 32, 32, 0.5).build_mask(torch.rand(8, 20, device="cuda"))
+    with pytest.raises(B.CrispError) as e:
+        B.AdamW([w], masks=[other]).step([torch.ones(8, 16, device="cuda")])
+    assert e.value.code == B.BAD_SHAPE
+
+
+def test_tuples_of_gradients_and_weights_that_have_moved():
+    """The calls that the C++ path leaves to Python, and a parameter whose storage has been exchanged."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    got = []
+    for kind in (list, tuple):
+        w = torch.nn.Parameter(torch.linspace(-1, 1, 640, device="cuda").view(10, 64))
+        opt = B.AdamW([w])
+        g = torch.linspace(1, 2, 640, device="cuda").view(10, 64)
+        opt.step(kind([g]))
+        w.data = w.data.clone()
+        opt.step(kind([g.bfloat16()]))
+        got.append((w.detach().clone(), opt.m.clone(), opt.v.clone()))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+    assert not torch.equal(got[0][0], torch.linspace(-1, 1, 640, device="cuda").view(10, 64))
+
+
 def test_pitched_gradients_and_streams():
     """A gradient that a side stream makes, in rows 3 elements further apart; the step is issued there too."""
     import torch
