@@ -517,7 +517,8 @@ CRISP_API crisp_status_t crisp_quantize8(const uint16_t *d_x_bf16, int64_t ldx, 
  * The product.  crisp_spmm8 quantises X as crisp_quantize8 does and multiplies; d_act is a workspace of crisp_spmm8_sizes bytes, 256-byte aligned (few columns are
  * quantised within the product and need none: 0 bytes, d_act may be NULL then).  crisp_spmm8_quantized multiplies what crisp_quantize8 left there, with the layer's k and the same ncols.
  *   d_y   y_layout 0: [rows, ncols], ldy >= ncols; 1: [ncols, rows], ldy >= rows.  bf16 (y_dtype 0) or fp32 (1).  Y must not lie on X or d_act.
- * Every number of columns from one on; a layer without kept blocks gives act(bias).  Results do not depend on what else runs.  Handles may be used by
+ * Every number of columns from one on; a layer without kept blocks gives act(bias).  Results do not depend on what else runs, and the two calls' differ by the order of
+ * their fp32 sums at most (few columns, which crisp_spmm8 takes another way).  Handles may be used by
  * several host threads, each with its own d_act; a handle's settings are changed, its buffer is encoded anew, and it is destroyed, only while none is in such a call.
  */
 CRISP_API crisp_status_t crisp_spmm8_sizes(crisp_handle8_t h, int64_t ncols, size_t *act_bytes);
@@ -526,10 +527,11 @@ CRISP_API crisp_status_t crisp_spmm8(crisp_handle8_t h, const uint16_t *d_x_bf16
 CRISP_API crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_act, int64_t ncols, void *d_y, int64_t ldy, int32_t y_layout,
                                                int32_t y_dtype, void *stream);
 
-/* crisp_set_epilogue, crisp_last_launch (stack: CTAs that share one tile's blocks, -1 for pairs), crisp_device_status, crisp_reset_status and crisp_set_tuning of an 8-bit handle.
+/* crisp_set_epilogue, crisp_last_launch (path: CRISP_PATH_DIRECT where one to four columns ran on the CUDA cores; stack: CTAs that
+ * share one tile's blocks, -1 for pairs), crisp_device_status, crisp_reset_status and crisp_set_tuning of an 8-bit handle.
  * tile_cols: columns a tile, 64, 128, 192 or 256, or 16 or 32 for products of no more columns (else it is not heeded); split: CTAs that share a tile, 1 to 8, or -1:
  * pairs of CTAs that multiply two row tiles by 128, 192 or 256 columns with one instruction, for layers of two row tiles and more that keep every block; 0 = chosen
- * by the library. */
+ * by the library (1 to 4 columns: on the tensor cores as soon as one of the two is given). */
 CRISP_API crisp_status_t crisp_set_epilogue8(crisp_handle8_t h, const float *d_bias_f32, int32_t relu);
 CRISP_API crisp_status_t crisp_last_launch8(crisp_handle8_t h, crisp_launch_info_t *out);
 CRISP_API crisp_status_t crisp_device_status8(crisp_handle8_t h, void *stream, int32_t *status_out);

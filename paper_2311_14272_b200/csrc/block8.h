@@ -40,6 +40,19 @@ inline Act8 act8(int64_t k, int64_t ncols) {
     return a;
 }
 
+// Products of a few columns on the CUDA cores (spmm8_few.cu): x is quantised by every CTA.
+struct FewParams {
+    const uint8_t *image;
+    const int32_t *blk_col;
+    const uint16_t *x;
+    void *y;
+    const float *bias;
+    int64_t ldx, ldy;
+    int rows, k, kkeep, all, cols, x_layout, x_vec, y_layout, f32, relu, early;
+};
+bool few8(const Geometry &g, int64_t ncols);
+cudaError_t launch_few8(const FewParams &p, int nrt, int device, cudaStream_t st);
+
 cudaError_t launch_encode8(const Geometry &g, const uint16_t *w, int64_t ld, const int32_t *mask_blk_col, const uint32_t *nm_bits, uint8_t *buf,
                            cudaStream_t st);
 cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, int64_t ld, cudaStream_t st);

@@ -791,6 +791,31 @@ bool fused8(int64_t ncols) { return ncols <= 32; }
 template <bool kSplit>
 Variant8 fused_variant8(int tile) { return tile == 16 ? make_variant8<16, kSplit, true>() : make_variant8<32, kSplit, true>(); }
 
+// How many clusters of s CTAs, one an SM, run at once: fewer than SMs / s, since a cluster lies within one GPC.  (A second wave for two of sixteen clusters of eight
+// made 2048 x 2048 with one column 10.2 us instead of 5.7.)
+int clusters_at_once(int device, int s, int sms) {
+    static std::atomic<int> known[kMaxDevices][9];
+    int n = known[device][s].load(std::memory_order_relaxed);
+    if (n > 0) return n;
+    const Variant8 v = make_variant8<64, true>();
+    cudaLaunchAttribute attr;
+    attr.id = cudaLaunchAttributeClusterDimension;
+    attr.val.clusterDim.x = (unsigned)s; attr.val.clusterDim.y = 1; attr.val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(s * (sms / s)));
+    cfg.blockDim = dim3((unsigned)v.threads);
+    cfg.dynamicSmemBytes = v.smem;
+    cfg.attrs = &attr;
+    cfg.numAttrs = 1;
+    if (cudaFuncSetAttribute(reinterpret_cast<const void *>(v.kern), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget + 1024) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, reinterpret_cast<const void *>(v.kern), &cfg) != cudaSuccess || n <= 0) {
+        (void)cudaGetLastError();
+        n = std::max(1, sms / s - (s > 2 ? 2 : 0));
+    }
+    known[device][s].store(n, std::memory_order_relaxed);
+    return n;
+}
+
 // Tiles that begin within a chunk of scales do so at an even multiple of 32 columns: the narrow ones are for a single tile.
 bool fits8(int tile, int64_t ncols) { return tile >= 64 || ncols <= tile; }
 
@@ -798,7 +823,8 @@ bool fits8(int tile, int64_t ncols) { return tile >= 64 || ncols <= tile; }
 // fixed time beside them, the sum over a cluster one that grows with the columns a CTA has to add up; tiles come in waves of as many as there are SMs.  Measured on
 // 4096 x 4096 in a row, all blocks kept: 64 columns a tile 11.7 us for 128 tiles (256 columns) and 206 for 28 waves (8192), 128 columns 12.9 and 128, 192 columns
 // 15.2 and 115, 256 columns 19.6 and 116; two, four CTAs a tile: 64 columns 11.6, 9.3, 128 columns 12.6, 9.9, 256 columns 18.9, 11.6.
-void choose8(const crisp_handle8_s *h, int64_t ncols, int sms, int *tile, int *split, bool *pair) {
+void choose8(const crisp_handle8_s *h, int64_t ncols, int device, int *tile, int *split, bool *pair) {
+    const int sms = sm_count_of(device);
     struct Cost { int cols; double block, tile; };
     static const Cost costs[] = {{16, 0.17, 0.5}, {32, 0.17, 0.5}, {64, 0.20, 0.6}, {128, 0.24, 0.8}, {192, 0.31, 1.0}, {256, 0.43, 1.4}};
     const Geometry &g = h->g;
@@ -808,7 +834,7 @@ void choose8(const crisp_handle8_s *h, int64_t ncols, int sms, int *tile, int *s
         if (!fits8(c.cols, ncols) || (h->tile_cols && fits8(h->tile_cols, ncols) && c.cols != h->tile_cols)) continue;
         const int64_t tiles = (int64_t)g.nrt * ((ncols + c.cols - 1) / c.cols);
         for (int s = 1; s <= 8 && s <= std::max(1, g.kkeep); ++s) {
-            if (h->split > 0 ? s != std::min(h->split, std::max(1, g.kkeep)) : s > 1 && (tiles * s > sms || 2 * s > g.kkeep)) continue;
+            if (h->split > 0 ? s != std::min(h->split, std::max(1, g.kkeep)) : s > 1 && (tiles > clusters_at_once(device, s, sms) || 2 * s > g.kkeep)) continue;
             const double waves = (double)((tiles * s + sms - 1) / sms);
             const double t = waves * (c.block * ((g.kkeep + s - 1) / s) + c.tile) + (s > 1 ? 0.9 + c.cols / (48.0 * s) : 0.0);
             if (t < best) { best = t; *tile = c.cols; *split = s; }
@@ -848,9 +874,31 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int
     if (e != cudaSuccess) return e;
     if (device < 0 || device >= kMaxDevices) return cudaErrorInvalidDevice;
     const Geometry &g = h->g;
+    const auto settle = [&](const crisp_launch_info_t &info) {                   // (under the lock)
+        h->last = info;
+        if (h->settled.holds(st, moment)) return;
+        // (what is captured has not run; one name of a stream stands for another stream in every thread)
+        cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+        h->settled.note(st, moment, st != cudaStreamPerThread && cudaStreamIsCapturing(st, &capture) == cudaSuccess && capture == cudaStreamCaptureStatusNone);
+    };
+    if (x && few8(g, ncols) && !h->tile_cols && !h->split && h->skip_fill < 0) {
+        const Image8 I = image8(g);
+        FewParams p{h->buf + I.image_off, reinterpret_cast<const int32_t *>(h->buf + I.col_off), x, d_y, h->epilogue.bias, ldx, ldy, g.rows, g.k, g.kkeep,
+                    g.kkeep == g.nblk, (int)ncols, x_layout, aligned_to(x, 16) && ldx % 8 == 0, y_layout, y_dtype, h->epilogue.relu, 0};
+        {
+            std::lock_guard<std::mutex> hold(h->plan_lock);
+            p.early = h->settled.holds(st, moment);
+        }
+        e = launch_product(encodes, p, moment, [&] { return launch_few8(p, g.nrt, device, st); });
+        if (e == cudaSuccess) {
+            std::lock_guard<std::mutex> hold(h->plan_lock);
+            settle(crisp_launch_info_t{CRISP_PATH_DIRECT, 0, 0, 1, 0, 0, g.nrt * 16, 0, 1});
+        }
+        return e;
+    }
     int tile, split;
     bool pair;
-    choose8(h, ncols, sm_count_of(device), &tile, &split, &pair);
+    choose8(h, ncols, device, &tile, &split, &pair);
     if (x && tile > 32) tile = 32;
     if (x) pair = false;
     const Act8 a = act8(g.k, ncols);
@@ -898,12 +946,7 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int
     e = behind ? launch() : launch_product(encodes, p, moment, launch);
     if (e == cudaSuccess) {
         std::lock_guard<std::mutex> hold(h->plan_lock);
-        if (!h->settled.holds(st, moment)) {
-            // (what is captured has not run; one name of a stream stands for another stream in every thread)
-            cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
-            h->settled.note(st, moment, st != cudaStreamPerThread && cudaStreamIsCapturing(st, &capture) == cudaSuccess && capture == cudaStreamCaptureStatusNone);
-        }
-        h->last = crisp_launch_info_t{CRISP_PATH_DENSE, tile, tile <= 192 ? 2 : 1, pair ? -1 : split, tile >= 128 ? 8 : 4, v.stages, (int32_t)grid, 0, 1};
+        settle(crisp_launch_info_t{CRISP_PATH_DENSE, tile, tile <= 192 ? 2 : 1, pair ? -1 : split, tile >= 128 ? 8 : 4, v.stages, (int32_t)grid, 0, 1});
     }
     return e;
 }

@@ -122,7 +122,9 @@ def test_tiles_of_every_width_and_parts(rows, k, ncols, keep):
         y = L.spmm8(d_x, tokens=True, y_dtype=f32)
         check(numbers(y.t()), w, held, k, f32)
         again = L.spmm8(act, tokens=True, y_dtype=f32)
-        assert torch.equal(y, again)
+        if ncols > 4:                                        # (fewer columns: another kernel, another order of the sums)
+            assert torch.equal(y, again)
+        check(numbers(again.t()), w, held, k, f32)
     assert L.device_status8() == 0
     info = L.last_launch8()
     assert info["tile_cols"] <= 16 or ncols > 16
@@ -153,6 +155,30 @@ def test_the_result_does_not_depend_on_the_tiling(tile, split):
         L.set_tuning8(tile_cols=96)
     with pytest.raises(B.CrispError):
         L.set_tuning8(split=9)
+
+
+@pytest.mark.parametrize("ncols", [1, 2, 3, 4])
+@pytest.mark.parametrize("rows,k,keep", [(1, 1, 1.0), (129, 1000, 1.0), (300, 4500, 0.4), (512, 130, 1.0), (256, 12000, 1.0), (256, 5000, 0.7)])
+def test_a_few_columns(rows, k, keep, ncols):
+    """One to four columns on the CUDA cores where their codes fit in shared memory, on the tensor cores else and where a tile is asked for."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, w, _ = layer(B, torch, rows, k, 4, 4, keep, 40)
+    x = activations(np.random.default_rng(41), k, ncols)
+    held = ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64))
+    bias = np.random.default_rng(42).standard_normal(rows).astype(np.float32)
+    L.set_epilogue8(to_dev(bias, torch), relu=True)
+    d_x = bf16_dev(x, torch)
+    odd = torch.full((k * ncols + 1,), 3.0, dtype=torch.bfloat16, device="cuda")[1:].view(ncols, k)
+    odd.copy_(d_x.t())
+    fits = L.kkeep * ncols * 513 <= 100 * 1024
+    for tile in (0, 16):
+        L.set_tuning8(tile_cols=tile)
+        for f32 in (0, 1):
+            for tokens, src in ((False, d_x), (True, d_x.t().contiguous()), (True, odd)):
+                y = L.spmm8(src, tokens=tokens, y_dtype=f32)
+                assert (L.last_launch8()["path"] == B.PATH_DIRECT) == (fits and not tile) and L.device_status8() == 0
+                check(numbers(y.t() if tokens else y), w, held, k, f32, bias.astype(np.float64), True)
 
 
 @pytest.mark.parametrize("tile", [128, 192, 256])
