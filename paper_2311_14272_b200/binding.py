@@ -795,7 +795,7 @@ class HybridLayer:
 
     # The layer in 8 bits, beside or instead of its bf16 encoding (masks of 128 x 128 blocks).
     def encode8(self, w, stream=None):
-        """Compress the weights under the mask to e4m3 with a scale for each kept block (crisp_encode8)."""
+        """Compress the weights under the mask to e4m3 with a scale for each kept block (crisp_encode8).  The epilogue of an encoding before is not carried over."""
         if self._gpu is not None and self._gpu == _current_device():
             done = _network.encode8(self.mask, w, self.desc.rows, self.desc.k, self._gpu, self.buf8, self.handle8, _stream(stream))
             if done is not None and not done[2]:
@@ -806,13 +806,15 @@ class HybridLayer:
                 return self
         assert w.is_cuda and w.dtype == self.torch.bfloat16 and (w.stride()[1] == 1 or w.shape[1] == 1) and w.shape == (self.desc.rows, self.desc.k), \
             "weights are a bf16 CUDA matrix of the layer's shape with consecutive columns"
+        assert w.device == self.device, "weights on another device than the layer"
         size = crisp_encode8_sizes(self.mask)
         if self.buf8 is None or self.buf8.numel() < size:
             self.buf8 = self.torch.empty(size, dtype=self.torch.uint8, device=self.device)
         old, self.handle8 = self.handle8, 0
         crisp_destroy8(old)
         self._bias8 = None
-        self.handle8 = crisp_encode8(w, _pitch(w), self.mask, self.buf8, stream)
+        with self.torch.cuda.device(self.device):
+            self.handle8 = crisp_encode8(w, _pitch(w), self.mask, self.buf8, stream)
         return self
 
     def decode8(self, stream=None):
@@ -823,21 +825,23 @@ class HybridLayer:
                 raise CrispError(code, "crisp_decode8")
             return w
         w = self.torch.empty_strided((self.desc.rows, self.desc.k), (self.desc.k, 1), dtype=self.torch.bfloat16, device=self.device)
-        crisp_decode8(self.handle8, w, self.desc.k, stream)
+        with self.torch.cuda.device(self.device):
+            crisp_decode8(self.handle8, w, self.desc.k, stream)
         return w
 
     def quantize8(self, x, tokens=False, stream=None):
         """X in 8 bits, for this layer and others of its k: x is [k, ncols], or with tokens=True [ncols, k]."""
         ncols = self._columns8(x, tokens)
         k = self.desc.k
-        with _allocating_for(stream):
-            act = self.torch.empty(crisp_quantize8_sizes(k, ncols), dtype=self.torch.uint8, device=self.device)
-        crisp_quantize8(x, _pitch(x), int(tokens), k, ncols, act, stream)
+        with self.torch.cuda.device(self.device):
+            with _allocating_for(stream):
+                act = self.torch.empty(crisp_quantize8_sizes(k, ncols), dtype=self.torch.uint8, device=self.device)
+            crisp_quantize8(x, _pitch(x), int(tokens), k, ncols, act, stream)
         return Activations8(k, ncols, act)
 
     def _columns8(self, x, tokens):
         shape = x.shape
-        assert x.is_cuda and x.dtype == self.torch.bfloat16 and len(shape) == 2 and (x.stride()[1] == 1 or shape[1] == 1) and shape[1 if tokens else 0] == self.desc.k, \
+        assert x.device == self.device and x.dtype == self.torch.bfloat16 and len(shape) == 2 and (x.stride()[1] == 1 or shape[1] == 1) and shape[1 if tokens else 0] == self.desc.k, \
             "X is a bf16 CUDA matrix, [k, ncols] or with tokens=True [ncols, k], with consecutive elements in a row"
         return shape[0 if tokens else 1]
 
@@ -859,14 +863,15 @@ class HybridLayer:
         if y is None:
             y = torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=self.device)
         else:
-            assert y.is_cuda and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1), \
+            assert y.device == self.device and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1), \
                 "Y has the product's shape and type, and consecutive elements in a row"
-        if held:
-            crisp_spmm8_quantized(self.handle8, x.buffer, ncols, y, _pitch(y), int(tokens), y_dtype, stream)
-            return y
-        with _allocating_for(stream):                        # the workspace is given back when this returns: to the stream that uses it
-            act = torch.empty_strided((crisp_spmm8_sizes(self.handle8, ncols),), (1,), dtype=torch.uint8, device=self.device)
-        crisp_spmm8(self.handle8, x, _pitch(x), int(tokens), ncols, act, y, _pitch(y), int(tokens), y_dtype, stream)
+        with torch.cuda.device(self.device):
+            if held:
+                crisp_spmm8_quantized(self.handle8, x.buffer, ncols, y, _pitch(y), int(tokens), y_dtype, stream)
+                return y
+            with _allocating_for(stream):                    # the workspace is given back when this returns: to the stream that uses it
+                act = torch.empty_strided((crisp_spmm8_sizes(self.handle8, ncols),), (1,), dtype=torch.uint8, device=self.device)
+            crisp_spmm8(self.handle8, x, _pitch(x), int(tokens), ncols, act, y, _pitch(y), int(tokens), y_dtype, stream)
         return y
 
     def set_epilogue8(self, bias=None, relu=False):
@@ -1154,7 +1159,7 @@ class AdamW:
                 if t is not None and t.numel():
                     spans.append((t.data_ptr(), t.data_ptr() + (sum((s - 1) * d for s, d in zip(t.shape, t.stride())) + 1) * t.element_size()))
         spans.sort()
-        assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])), "weights or copies lie on one another"
+        assert all(a[1] <= b[0] for a, b in zip(spans, spans[1:])), "the address ranges of two weights or copies overlap"
         load()
         if _network is None:
             _bind_network()
@@ -1206,6 +1211,8 @@ class AdamW:
                 code = _network.adamw(self._address, self.weights, self.copies, grads, self.masks, C.addressof(self._params), _stream(stream))
             if code is None:
                 self._gradients(grads)
+                self.torch.autograd.graph.increment_version([t for ts, g in zip(zip(self.weights, self.copies), grads) for t in ts
+                                                             if t is not None and g is not None and not t.is_inference()])
                 code = _lib.crisp_adamw(len(self._table), self._table, self._params, _stream(stream))
             if code:
                 raise CrispError(code, "crisp_adamw")

@@ -335,6 +335,12 @@ struct Piece {
             if constexpr (kNarrow || !kW32) h[i] = mix_rest(first ^ (uint32_t)i);
         }
 
+        if (T.mask && !(fabsf(f.grad_scale) <= kLargest)) {      // (zero times that is not zero)
+#pragma unroll
+            for (int i = 0; i < kPer; ++i)
+                if (!(x.keep >> i & 1u)) w[i] = m[i] = v[i] = root[i] = 0.f;
+        }
+
         if constexpr (kW32) {
             if (vec) {
                 store8(reinterpret_cast<float *>(T.w) + at(T.ldw, 0), w);
@@ -536,7 +542,7 @@ bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p
 // The entry of one tensor (all arguments but the mask's shape are checked here).
 crisp_status_t entry(const crisp_adamw_tensor_t &t, int32_t ordinal, const crisp_adamw_t &p, AdamTensor *T) {
     if (t.rows < 0 || t.k < 0) return CRISP_BAD_SHAPE;
-    if (t.k > 0x7FFFFFFFll) return CRISP_UNSUPPORTED;
+    if (t.k > 0x7FFFFFFFll && (t.rows > 1 || t.mask)) return CRISP_UNSUPPORTED;        // (columns are counted in 31 bits where they count)
     if (t.k > 0 && t.rows > ((int64_t)1 << 44) / t.k) return CRISP_UNSUPPORTED;
     T->total = t.rows * t.k;
     if (T->total == 0 || !t.d_grad) { T->total = 0; return CRISP_OK; }

@@ -259,6 +259,13 @@ PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n) {
         T.d_grad = g.data_ptr(); T.ld_grad = rows[2]; T.grad_dtype = g.scalar_type() == at::kFloat;
         T.mask = static_cast<crisp_mask_t>(mask);
     }
+    // (autograd is told that they change, as by any operation in place)
+    for (int i = 1; i < 3; ++i)
+        for (Py_ssize_t l = 0; l < PyList_GET_SIZE(args[1]); ++l)
+            if (PyList_GET_ITEM(args[i], l) != Py_None && PyList_GET_ITEM(args[3], l) != Py_None) {
+                const at::Tensor &t = THPVariable_Unpack(PyList_GET_ITEM(args[i], l));
+                if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+            }
     crisp_status_t s;
     Py_BEGIN_ALLOW_THREADS
     s = lib_adamw((int32_t)PyList_GET_SIZE(args[1]), arr, params, stream);

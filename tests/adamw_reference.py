@@ -16,9 +16,11 @@ def mix(h):
     return h ^ (h >> np.uint64(16))
 
 
-def hashes(seed, step, tensor, count):
+def hashes(seed, step, tensor, count, first=0):
+    """Of `count` elements from number `first` on."""
     key = mix(mix(mix(seed & M32) ^ np.uint64(seed >> 32)) ^ np.uint64(step & M32))
-    return mix(np.arange(count, dtype=np.uint64) ^ mix(mix(key ^ np.uint64(tensor))))
+    e = np.arange(first, first + count, dtype=np.uint64)
+    return mix((e & np.uint64(M32)) ^ mix((e >> np.uint64(32)) ^ mix(key ^ np.uint64(tensor))))
 
 
 def decode(codes, biased, root):

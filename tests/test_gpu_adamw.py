@@ -292,6 +292,64 @@ def test_a_captured_step_goes_on_counting():
     assert np.array_equal(numbers(made[1][0][0][1]), held)
 
 
+def test_elements_beyond_32_bits():
+    """The last elements of a tensor of 2^32 + 5000 (bf16 weights, 8-bit states, a mask-less row): their addresses and their random numbers."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    if torch.cuda.mem_get_info()[0] < 60e9:
+        pytest.skip("needs 30 GB")
+    n, tail = 2**32 + 5000, 5000
+    w = torch.full((n,), 0.75, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    rng = np.random.default_rng(50)
+    values = (rng.standard_normal(tail) * 0.01).astype(np.float32)
+    g[-tail:] = to_dev(values, torch).bfloat16()
+    gt = numbers(g[-tail:])
+    opt = B.AdamW([w], state_bits=8, seed=6)
+    opt.step([g])
+    want_w, want_m, want_v = ref.step(np.full(tail, 0.75), gt, np.zeros(tail), np.zeros(tail), 1)
+    h = ref.hashes(6, 1, 0, tail, n - tail)
+    m = ref.decode(opt.m[n - tail:n].cpu().numpy(), opt.m_exp[(n - tail) // 128:].cpu().numpy(), False)
+    root = ref.decode(opt.v[n - tail:n].cpu().numpy(), opt.v_exp[(n - tail) // 128:].cpu().numpy(), True)
+    assert (n - tail) % 128 == 0
+    held, step, _ = ref.hold(want_m, (2 * (h & np.uint64(1023)).astype(np.float64) + 1) / 2048, False)
+    check_held(m, held, step)
+    held, step, _ = ref.hold(np.sqrt(want_v), (2 * (h >> np.uint64(10) & np.uint64(2047)).astype(np.float64) + 1) / 4096, True)
+    check_held(root, held, step)
+    step = ref.spacing(want_w, 7, -126)
+    held = np.floor(want_w / step + (2 * (h >> np.uint64(21)).astype(np.float64) + 1) / 4096) * step
+    off = np.abs(numbers(w[-tail:]) - held)
+    assert np.all(off <= step * 1.0001) and np.count_nonzero(off) <= 50
+    # (before them: no gradients, so weight decay alone moves the weights, by at most one rounding)
+    assert not opt.m[:n - tail].any() and float((w[:1000].float() - 0.75).abs().max()) <= 0.004
+    torch.cuda.empty_cache()
+
+
+def test_autograd_is_told_that_weights_change():
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    for kind in (list, tuple):
+        w = torch.nn.Parameter(torch.ones(4, 8, device="cuda"))
+        loss = (w * w).sum()
+        B.AdamW([w]).step(kind([torch.ones(4, 8, device="cuda")]))
+        with pytest.raises(RuntimeError):
+            loss.backward()
+
+
+def test_a_scale_that_is_not_finite_leaves_pruned_weights_zero():
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    for bits in (8, 32):
+        data = make(torch, [(64, 128)], False, True, 51)
+        layers, bits_of = masks_for(B, torch, [(64, 128)], 2, 4, 32, 0.5, 3)
+        opt = B.AdamW([data[0][0][1]], masks=layers, state_bits=bits)
+        opt.step([data[0][1][1]], grad_scale=torch.tensor([float("inf")], device="cuda"))
+        out = ~bits_of[0]
+        assert not numbers(data[0][0][1])[out].any()
+        m, v = states(opt, 0, out.size)
+        assert not m[out].any() and not v[out].any()
+
+
 def test_a_step_that_is_refused_changes_nothing():
     import torch
     from paper_2311_14272_b200 import binding as B
