@@ -8,10 +8,10 @@
 // 2048 elements, one CTA each, and their table travels as a kernel parameter.
 //
 // Measured on four tensors of 4096 x 4096 with bf16 gradients: 32-bit states 254 us with fp32 weights under masks (6.9 TB/s), 215 with bf16 ones (6.9).
-// 8-bit states 155 us with bf16 weights (4.3 TB/s), 169 under masks, 171 with fp32 weights (5.5): some 80 instructions an element, two thirds of what the
-// schedulers issue on the integer pipe, bound these.  What brought them there from 356: no questions asked for each element in pieces that need none
-// (287 -> 195), products instead of shifts (267 -> 242 with the former still in), codes packed by byte permutes, cvt.rs for bf16 weights, five CTAs an SM
-// (four 187, six 172 and seven 188 with spills).  Not kept: two or four turns of eight elements a thread (190 and 252; with the loads ahead 184).
+// 8-bit states 159 us with bf16 weights (4.2 TB/s), 169 under masks, 171 with fp32 weights (5.5): some 80 instructions an element, six in seven of the schedulers'
+// cycles, bound these.  What brought them there from 356: no questions asked for each element in pieces that need none (287 -> 195), products instead of shifts
+// (287 -> 267 before that), codes packed by byte permutes, cvt.rs for bf16 weights, five CTAs an SM (four 187, six 172 and seven 188 with spills).  Not kept: two or four turns
+// of eight elements a thread (190 and 252; with the loads ahead 184).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 #include <cuda_fp8.h>
@@ -43,6 +43,7 @@ struct AdamTensor {
     uint32_t k, wpr;
     uint32_t key, spread;    // of the hash: the tensor's, and what elements below 2^32 take (filled in for the step of the call)
     uint32_t ordinal;
+    uint32_t by_k, shift;    // e / k = umulhi(e, by_k) >> shift for e below 2^31 (plain tensors under masks)
     uint8_t g32;             // gradients are fp32
     uint8_t flat;            // w, g and copy are packed: element e lies at e
     uint8_t vec;             // eight elements from a multiple of eight on lie in a row and at multiples of 16 bytes
@@ -52,7 +53,7 @@ struct AdamTensor {
 
 // Powers of two as parameters of the kernel.  The 8-bit kernel is bound by the integer pipe, and a product with a number that the compiler does not
 // know goes to the multiply-add pipe instead of becoming a shift.
-struct Powers { uint32_t p1 = 1u << 1, p4 = 1u << 4, p5 = 1u << 5, p7 = 1u << 7, p9 = 1u << 9, p19 = 1u << 19; };
+struct Powers { uint32_t p1 = 1u << 1, p4 = 1u << 4, p5 = 1u << 5, p7 = 1u << 7, p6 = 1u << 6, p9 = 1u << 9; };
 
 struct AdamScalars {
     float lr, beta1, one_beta1, beta2, one_beta2, eps, decay, weight_decay;
@@ -89,20 +90,18 @@ __device__ __forceinline__ uint32_t nearest2(float lo, float hi) {
 __device__ __forceinline__ uint16_t nearest(float x) { return __bfloat16_as_ushort(__float2bfloat16_rn(x)); }
 
 // The 8-bit forms.  A code is the top of an fp32 number whose exponent field has been brought down by 120 (127 - 7), so that small codes are
-// subnormal as fp32's are: reading sqrt(v) is a shift and a product by 2^120, rounding an addition to the bits below the code.
+// subnormal as fp32's are: rounding is an addition to the bits below the code.
 __device__ __forceinline__ float power_of(uint32_t biased) { return __uint_as_float(biased << 23); }       // 2^(biased - 127), 0 for 0
-// One power of two for both factors, 2^120 and the scale; the product of the two exponents' rest, beyond fp32's range, is `beyond` (1 for scales up to 2^7).
-__device__ __forceinline__ float power_120(uint32_t biased, float *beyond) {
-    const uint32_t near = min(biased, 134u);
-    *beyond = power_of(127u + biased - near);
-    return power_of(near + 120u);
-}
-__device__ __forceinline__ float root_bits(uint32_t codes, int byte, uint32_t p19) {                         // code << 19 as fp32
-    return __uint_as_float(__byte_perm(codes, 0, 0x4440 | (uint32_t)byte) * p19);
-}
+// 2^(E + 8) of a biased scale exponent: what a code of sqrt(v) is multiplied by.  (E is 56 at most: sqrt(v) is below 2^64.)
+__device__ __forceinline__ float power_8(uint32_t biased) { return power_of(min(biased + 8u, 254u)); }
 // The top bytes of four words.
 __device__ __forceinline__ uint32_t top_bytes(uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
     return __byte_perm(__byte_perm(a, b, 0x0073), __byte_perm(c, d, 0x0073), 0x5410);
+}
+// Two codes of sqrt(v), 2^8 too small: e4m4 with bias 7 is the top of an fp16 number with bias 15 whose sign and first exponent bit are 0.
+__device__ __forceinline__ float2 values_root(uint32_t codes, int pair, uint32_t p6) {
+    const uint32_t h = __byte_perm(codes, 0, pair ? 0x4342 : 0x4140) * p6;
+    return __half22float2(*reinterpret_cast<const __half2 *>(&h));
 }
 __device__ __forceinline__ float2 values_m(uint32_t codes, int pair) {                                       // two e4m3 codes
     const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes >> (16 * pair)), __NV_E4M3);
@@ -160,8 +159,12 @@ struct Factors {
     uint32_t key, spread;
 };
 // The row and column of element e0.
+template <bool kPlain>
 __device__ __forceinline__ void place(const AdamTensor &T, int64_t e0, int64_t *row, uint32_t *col) {
-    if (T.total <= 0xFFFFFFFFll) {
+    if (kPlain && T.by_k) {                                   // (a product instead of a division of some twenty instructions)
+        const uint32_t r = __umulhi((uint32_t)e0, T.by_k) >> T.shift;
+        *row = r; *col = (uint32_t)e0 - r * T.k;
+    } else if (T.total <= 0xFFFFFFFFll) {
         const uint32_t r = (uint32_t)e0 / T.k;
         *row = r; *col = (uint32_t)e0 - r * T.k;
     } else {
@@ -191,7 +194,7 @@ struct Piece {
     __device__ __forceinline__ Piece(const AdamTensor &t, int64_t e) : T(t), e0(e), row(0), col(0) {
         count = kPlain ? kPer : (int)max((int64_t)0, min((int64_t)kPer, T.total - e0));
         whole = kPlain || count == kPer; vec = kPlain || (T.vec && whole); flat = kPlain || T.flat;
-        if (T.mask || !flat) place(T, e0, &row, &col);
+        if (T.mask || !flat) place<kPlain>(T, e0, &row, &col);
     }
     // where element i of rows of pitch ld lies
     __device__ __forceinline__ int64_t at(int64_t ld, int i) const {
@@ -302,8 +305,8 @@ struct Piece {
             if (e0 >> 32) spread = mix((uint32_t)(e0 >> 32) ^ f.key);
         // (e0 is a multiple of 8: the hash of e0 + i differs from that of e0 in three low bits until its first product)
         const uint32_t first = ((uint32_t)e0 ^ spread) ^ (((uint32_t)e0 ^ spread) >> 16);
-        float v_beyond = 1.f, m_scale = 0.f, v_scale = 0.f;
-        if constexpr (kNarrow) { m_scale = s.beta1 * power_of(x.m_exp); v_scale = power_120(x.v_exp, &v_beyond); }
+        float m_scale = 0.f, v_scale = 0.f;
+        if constexpr (kNarrow) { m_scale = s.beta1 * power_of(x.m_exp); v_scale = power_8(x.v_exp); }
         if (T.g32) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i) g[i] = __uint_as_float(x.g[i]);
@@ -317,12 +320,11 @@ struct Piece {
             else w[i] = __uint_as_float(i & 1 ? x.w[i / 2] & 0xFFFF0000u : x.w[i / 2] << 16);
             if constexpr (kNarrow) {
                 if ((i & 1) == 0) {
-                    const float2 two = values_m(i < 4 ? x.mc.x : x.mc.y, i >> 1 & 1);
+                    const float2 two = values_m(i < 4 ? x.mc.x : x.mc.y, i >> 1 & 1), roots = values_root(i < 4 ? x.vc.x : x.vc.y, i >> 1 & 1, s.by.p6);
                     m[i] = two.x * m_scale; m[i + 1] = two.y * m_scale;
+                    v[i] = roots.x * v_scale; v[i + 1] = roots.y * v_scale;
                 }
-                float u = root_bits(i < 4 ? x.vc.x : x.vc.y, i & 3, s.by.p19) * v_scale;
-                if (v_beyond != 1.f) u *= v_beyond;
-                v[i] = u * u;
+                v[i] *= v[i];
             } else {
                 m[i] = x.m[i]; v[i] = x.v[i];
             }
@@ -475,8 +477,7 @@ moments_kernel(const uint8_t *m, const uint8_t *m_exp, const uint8_t *v, const u
     wait_for_prerequisites();
     const int64_t e0 = ((int64_t)blockIdx.x * kAdamThreads + threadIdx.x) * kPer;
     if (e0 >= count) return;
-    float beyond;
-    const float sm = power_of(m_exp[e0 >> 7]), sv = power_120(v_exp[e0 >> 7], &beyond);
+    const float sm = power_of(m_exp[e0 >> 7]), sv = power_8(v_exp[e0 >> 7]);
     const int here = (int)min((int64_t)kPer, count - e0);
     uint2 mc = make_uint2(0, 0), vc = make_uint2(0, 0);
     if (here == kPer) {
@@ -491,9 +492,9 @@ moments_kernel(const uint8_t *m, const uint8_t *m_exp, const uint8_t *v, const u
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const float2 two = values_m(i < 2 ? mc.x : mc.y, i & 1);
-        const uint32_t c = i < 2 ? vc.x : vc.y;
+        const float2 roots = values_root(i < 2 ? vc.x : vc.y, i & 1, 1u << 6);
         a[i] = nearest2(two.x * sm, two.y * sm);
-        r[i] = nearest2(root_bits(c, 2 * (i & 1), 1u << 19) * sv * beyond, root_bits(c, 2 * (i & 1) + 1, 1u << 19) * sv * beyond);
+        r[i] = nearest2(roots.x * sv, roots.y * sv);
     }
     if (vec && here == kPer) {
         *reinterpret_cast<uint4 *>(m_out + e0) = make_uint4(a[0], a[1], a[2], a[3]);
@@ -568,6 +569,14 @@ crisp_status_t entry(const crisp_adamw_tensor_t &t, int32_t ordinal, const crisp
     }
     T->plain = T->flat && T->vec && (T->bytes || !T->mask);
     T->ordinal = (uint32_t)ordinal;
+    T->by_k = T->shift = 0;
+    if (T->plain && T->mask && T->total < (int64_t)1 << 31) {
+        // l = ceil(log2 k) and by_k = ceil(2^(31 + l) / k) < 2^32: exact for numerators below 2^31
+        uint32_t l = 0;
+        while (((uint64_t)1 << l) < (uint64_t)t.k) ++l;
+        T->by_k = (uint32_t)((((uint64_t)1 << (31 + l)) + (uint64_t)t.k - 1) / (uint64_t)t.k);
+        T->shift = l - 1;                                     // (k is 8 or more)
+    }
     return CRISP_OK;
 }
 
