@@ -225,12 +225,12 @@ quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols,
         quantize_tokens<U, false>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, vec_ok, group, kb0);
 }
 
-// X [k, ncols]: a CTA takes 128 columns of one k-block.  A warp reads 16 rows of it, a lane four neighbouring columns; the 16 values of a column in a warp are one
+// X [k, ncols]: a CTA takes 128 columns of one k-block.  A warp reads 16 rows of it, a lane four columns; the 16 values of a column in a warp are one
 // 16-byte chunk of its codes.  Neighbouring CTAs read neighbouring columns.  4096 x 8192: 18.2 us (5.5 TB/s); two pairs of columns a lane, 64 apart (fewer bank
 // conflicts), 23.4; neighbouring CTAs on neighbouring k-blocks, 64 columns each, 52.
+template <bool kQuads>
 __global__ void __launch_bounds__(256)
-quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
-                        int pair_ok, int quad_ok) {
+quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales) {
     __shared__ uint32_t largest[2][8][32];
     __shared__ __align__(16) uint8_t tile[16384];
     wait_for_prerequisites();
@@ -238,30 +238,26 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
     const int64_t kb = blockIdx.x / chunks, c0 = (blockIdx.x - kb * chunks) * 128;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row0 = kb * 128 + warp * 16;
-    uint32_t v[2][16], top[2] = {0, 0};
-    if (quad_ok && c0 + 4 * lane + 4 <= ncols && row0 + 16 <= k) {
+    uint32_t v[2][16] = {}, top[2] = {0, 0};
+    // a lane's four columns: neighbours where they can be read together, else 32 apart, so that the lanes' are
+    const auto column = [&](int j) { return kQuads ? 4 * lane + j : lane + 32 * j; };
+    if (kQuads && c0 + 4 * lane + 4 <= ncols && row0 + 16 <= k) {
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
             const uint2 two = *reinterpret_cast<const uint2 *>(x + (row0 + i) * ldx + c0 + 4 * lane);
             v[0][i] = two.x; v[1][i] = two.y;
         }
-    } else
+    } else {
 #pragma unroll
-    for (int i = 0; i < 16; ++i)
+        for (int j = 0; j < 4; ++j) {
+            const int64_t col = c0 + column(j);
+            if (col >= ncols) continue;
+            const uint16_t *p = x + row0 * ldx + col;
 #pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int64_t col = c0 + 4 * lane + 2 * h;
-            v[h][i] = 0;
-            if (row0 + i < k) {
-                const uint16_t *p = x + (row0 + i) * ldx + col;
-                if (pair_ok && col + 1 < ncols) {
-                    v[h][i] = *reinterpret_cast<const uint32_t *>(p);
-                } else {
-                    if (col < ncols) v[h][i] = p[0];
-                    if (col + 1 < ncols) v[h][i] |= (uint32_t)p[1] << 16;
-                }
-            }
+            for (int i = 0; i < 16; ++i)
+                if (row0 + i < k) v[j >> 1][i] |= (uint32_t)p[i * ldx] << (16 * (j & 1));
         }
+    }
 #pragma unroll
     for (int h = 0; h < 2; ++h) {
 #pragma unroll
@@ -292,7 +288,7 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int c = 4 * lane + 2 * h + s;
+            const int c = column(2 * h + s);
             *reinterpret_cast<uint4 *>(tile + (c >> 3) * 1024 + (c & 7) * 128 + ((warp ^ (c & 7)) << 4)) = make_uint4(q[s][0], q[s][1], q[s][2], q[s][3]);
             if (warp == 0 && c0 + c < ncols) put_scale(scales, chunks, kb, c0 + c, e[s]);
         }
@@ -341,8 +337,9 @@ cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t
     if (layout)
         return launch_chained(u == 4 ? quantize_tokens_kernel<4> : quantize_tokens_kernel<2>, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks, act,
                               act + a.scale_off, (int)aligned16(x, ldx));
-    return launch_chained(quantize_columns_kernel, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks, act, act + a.scale_off,
-                          (int)(reinterpret_cast<uintptr_t>(x) % 4 == 0 && ldx % 2 == 0), (int)(reinterpret_cast<uintptr_t>(x) % 8 == 0 && ldx % 4 == 0));
+    const bool quads = reinterpret_cast<uintptr_t>(x) % 8 == 0 && ldx % 4 == 0;
+    return launch_chained(quads ? quantize_columns_kernel<true> : quantize_columns_kernel<false>, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks,
+                          act, act + a.scale_off);
 }
 
 }  // namespace crisp
