@@ -517,9 +517,10 @@ CRISP_API crisp_status_t crisp_quantize8(const uint16_t *d_x_bf16, int64_t ldx, 
  * The product.  crisp_spmm8 quantises X as crisp_quantize8 does and multiplies; d_act is a workspace of crisp_spmm8_sizes bytes, 256-byte aligned (0 for few columns, which
  * are quantised within the product: d_act may be NULL then).  crisp_spmm8_quantized multiplies what crisp_quantize8 left there, with the layer's k and the same ncols.
  *   d_y   y_layout 0: [rows, ncols], ldy >= ncols; 1: [ncols, rows], ldy >= rows.  bf16 (y_dtype 0) or fp32 (1).  Y must not lie on X or d_act.
- * Every number of columns from one on; a layer without kept blocks gives act(bias).  Results do not depend on what else runs, and the two calls' differ by the order of
- * their fp32 sums at most (few columns, which crisp_spmm8 takes another way).  Handles may be used by
- * several host threads, each with its own d_act; a handle's settings are changed, its buffer is encoded anew, and it is destroyed, only while none is in such a call.
+ * Every number of columns from one on; a layer without kept blocks gives act(bias).  crisp_spmm8 never reads X under blocks that no row tile kept, apart from few columns.
+ * Results do not depend on what else runs, and the two calls' differ by the order of their fp32 sums at most (few columns, which crisp_spmm8 takes another way).  Handles
+ * may be used by several host threads, each with its own d_act; a handle's settings are changed, its buffer is encoded anew, and it is destroyed, only while none is in
+ * such a call.
  */
 CRISP_API crisp_status_t crisp_spmm8_sizes(crisp_handle8_t h, int64_t ncols, size_t *act_bytes);
 CRISP_API crisp_status_t crisp_spmm8(crisp_handle8_t h, const uint16_t *d_x_bf16, int64_t ldx, int32_t x_layout, int64_t ncols, void *d_act, void *d_y,

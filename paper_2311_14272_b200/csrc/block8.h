@@ -17,14 +17,15 @@ namespace crisp {
 constexpr uint32_t kTile8 = 16384, kScales8 = 512, kEntry8 = kTile8 + kScales8;
 
 struct Image8 {                              // where the parts of a weight buffer lie
-    size_t col_off, exp_off, image_off, total;
+    size_t col_off, exp_off, used_off, image_off, total;
 };
 inline Image8 image8(const Geometry &g) {
     const size_t n = (size_t)g.nrt * g.kkeep;
     Image8 i;
     i.col_off = kAlign;                      // (the status word in front)
     i.exp_off = i.col_off + align_up(n * 4);
-    i.image_off = i.exp_off + align_up(n);
+    i.used_off = i.exp_off + align_up(n);    // a byte a k-block: whether any row tile keeps it
+    i.image_off = i.used_off + align_up((size_t)g.nblk);
     i.total = i.image_off + align_up(n * kEntry8);
     return i;
 }
@@ -56,6 +57,7 @@ cudaError_t launch_few8(const FewParams &p, int nrt, int device, cudaStream_t st
 cudaError_t launch_encode8(const Geometry &g, const uint16_t *w, int64_t ld, const int32_t *mask_blk_col, const uint32_t *nm_bits, uint8_t *buf,
                            cudaStream_t st);
 cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, int64_t ld, cudaStream_t st);
-cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t k, int64_t ncols, uint8_t *act, cudaStream_t st);
+// used: a byte a k-block, 0 for those that are left out, or nullptr for all
+cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t k, int64_t ncols, uint8_t *act, const uint8_t *used, cudaStream_t st);
 
 }  // namespace crisp

@@ -23,7 +23,7 @@ namespace {
 // 18.3, three 10.8 and 15.7.
 __global__ void __launch_bounds__(512, 4)
 encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_blk_col, const uint32_t *nm_bits, int32_t *blk_col, uint8_t *exps, uint8_t *image,
-               uint32_t *header, int wide) {
+               uint32_t *header, uint8_t *used, int wide) {
     __shared__ uint32_t largest[16];
     chain_kernels();
     const int slot = blockIdx.x, rt = slot / g.kkeep, kb = g.kkeep == g.nblk ? slot - rt * g.kkeep : mask_blk_col[slot];
@@ -86,12 +86,21 @@ encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_bl
     if (threadIdx.x < 128) reinterpret_cast<uint32_t *>(entry + kTile8)[threadIdx.x] = e * 0x01010101u;
     if (threadIdx.x == 0) { blk_col[slot] = kb; exps[slot] = (uint8_t)e; }
     if (slot == 0 && threadIdx.x < 64) header[threadIdx.x] = 0;
+    if (g.kkeep == g.nblk) return;
+    // which k-blocks any row tile keeps: a CTA looks one of them up in all lists, with its own values stored (a CTA of its own for it held registers that
+    // the rest spilled: 4096 x 4096 with half of its blocks took 13.0 us, not 8.5)
+    const int n = g.nrt * g.kkeep;
+    for (int b = slot; b < g.nblk; b += n) {
+        int hit = 0;
+        for (int i = threadIdx.x; i < n; i += 512) hit |= mask_blk_col[i] == b;
+        hit = __syncthreads_or(hit);
+        if (threadIdx.x == 0) used[b] = (uint8_t)(hit != 0);
+    }
 }
 
 // One CTA a block of the dense matrix, kept or not.
 __global__ void __launch_bounds__(512)
 decode8_kernel(Geometry g, const int32_t *blk_col, const uint8_t *exps, const uint8_t *image, uint16_t *w, int64_t ld, int wide) {
-    __shared__ int found, scale;
     chain_kernels();
     const int rt = blockIdx.x / g.nblk, kb = blockIdx.x - rt * g.nblk;
     int slot = rt * g.kkeep + kb;
@@ -99,16 +108,18 @@ decode8_kernel(Geometry g, const int32_t *blk_col, const uint8_t *exps, const ui
     if (g.kkeep == g.nblk) {
         e = exps[slot];
     } else {
-        // where the block is in its row tile's list, if it is, and its exponent
-        if (threadIdx.x == 0) found = -1;
-        __syncthreads();
-        for (int i = threadIdx.x; i < g.kkeep; i += 512) {
-            const int at = rt * g.kkeep + i, col = blk_col[at], here = exps[at];
-            if (col == kb) { found = at; scale = here; }
+        // where the block is in its row tile's list, if it is, and its exponent (every warp looks for itself)
+        slot = -1;
+        for (int i0 = 0; i0 < g.kkeep; i0 += 32) {
+            const int i = i0 + (int)(threadIdx.x & 31), at = rt * g.kkeep + i;
+            const int col = i < g.kkeep ? blk_col[at] : -1;
+            const uint32_t here = i < g.kkeep ? exps[at] : 0u, hit = __ballot_sync(0xFFFFFFFFu, col == kb);
+            if (hit) {
+                slot = rt * g.kkeep + i0 + __ffs(hit) - 1;
+                e = __shfl_sync(0xFFFFFFFFu, here, __ffs(hit) - 1);
+                break;
+            }
         }
-        __syncthreads();
-        slot = found;
-        e = (uint32_t)scale;
     }
     const int chunk = threadIdx.x & 15, row0 = threadIdx.x >> 4;
     const int64_t col = (int64_t)kb * 128 + chunk * 8;
@@ -156,16 +167,20 @@ __device__ __forceinline__ void put_scale(uint8_t *scales, int64_t chunks, int64
 // and two blocks' largest values travel through the shuffles in one word.
 template <int U, bool kFull>
 __device__ __forceinline__ void quantize_tokens(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes,
-                                                uint8_t *scales, int vec_ok, int64_t group, int64_t kb0) {
+                                                uint8_t *scales, const uint8_t *used, int vec_ok, int64_t group, int64_t kb0) {
     const int lane = threadIdx.x & 15, r = threadIdx.x >> 4 & 7, side = threadIdx.x >> 7;
     const int64_t col = group * 8 + r, kb1 = kb0 + side * U;         // (a warp's two columns share their k-blocks)
     uint32_t v[U][4], top[U], word[U / 2], any = 0;
     const uint16_t *from = x + col * ldx + kb1 * 128 + lane * 8;
+    bool wanted[U];
+#pragma unroll
+    for (int i = 0; i < U; ++i) wanted[i] = !used || (kb1 + i < nblk && used[kb1 + i]);
 #pragma unroll
     for (int i = 0; i < U; ++i) {
         const int64_t at = (kb1 + i) * 128 + lane * 8;
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i][j] = 0;
+        if (!wanted[i]) continue;
         if (kFull || (vec_ok && col < ncols && at + 8 <= k)) {
             const uint4 u = *reinterpret_cast<const uint4 *>(from + i * 128);
             v[i][0] = u.x; v[i][1] = u.y; v[i][2] = u.z; v[i][3] = u.w;
@@ -204,8 +219,10 @@ __device__ __forceinline__ void quantize_tokens(const uint16_t *x, int64_t ldx, 
         if (!kFull && kb1 + i >= nblk) break;
         const uint32_t e = exponent_of(word[i / 2] >> (16 * (i & 1)) & 0xFFFFu);
         const float down = power_of(254u - e);
-        *reinterpret_cast<uint2 *>(to) = make_uint2(codes2(v[i][0], down) | codes2(v[i][1], down) << 16, codes2(v[i][2], down) | codes2(v[i][3], down) << 16);
-        if (lane == 0 && (kFull || col < ncols)) *reinterpret_cast<uint32_t *>(scale) = e * 0x01010101u;
+        if (wanted[i]) {
+            *reinterpret_cast<uint2 *>(to) = make_uint2(codes2(v[i][0], down) | codes2(v[i][1], down) << 16, codes2(v[i][2], down) | codes2(v[i][3], down) << 16);
+            if (lane == 0 && (kFull || col < ncols)) *reinterpret_cast<uint32_t *>(scale) = e * 0x01010101u;
+        }
         to += groups * 1024;
         scale += chunks * kScales8;
     }
@@ -214,15 +231,15 @@ __device__ __forceinline__ void quantize_tokens(const uint16_t *x, int64_t ldx, 
 template <int U>
 __global__ void __launch_bounds__(256)
 quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
-                       int vec_ok) {
+                       const uint8_t *used, int vec_ok) {
     wait_for_prerequisites();
     launch_dependents();                     // (a product behind this one fetches weights meanwhile: all before this kernel has finished)
     const uint32_t spans = (uint32_t)((nblk + 2 * U - 1) / (2 * U)), g = blockIdx.x / spans;
     const int64_t group = g, kb0 = (int64_t)(blockIdx.x - g * spans) * (2 * U);
     if (vec_ok && (kb0 + 2 * U) * 128 <= k && group * 8 + 8 <= ncols)
-        quantize_tokens<U, true>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, vec_ok, group, kb0);
+        quantize_tokens<U, true>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, used, vec_ok, group, kb0);
     else
-        quantize_tokens<U, false>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, vec_ok, group, kb0);
+        quantize_tokens<U, false>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, used, vec_ok, group, kb0);
 }
 
 // X [k, ncols]: a CTA takes 128 columns of one k-block.  A warp reads 16 rows of it, a lane four columns; the 16 values of a column in a warp are one
@@ -230,12 +247,14 @@ quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols,
 // conflicts), 23.4; neighbouring CTAs on neighbouring k-blocks, 64 columns each, 52.
 template <bool kQuads>
 __global__ void __launch_bounds__(256)
-quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales) {
+quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
+                        const uint8_t *used) {
     __shared__ uint32_t largest[2][8][32];
     __shared__ __align__(16) uint8_t tile[16384];
     wait_for_prerequisites();
     launch_dependents();
     const int64_t kb = blockIdx.x / chunks, c0 = (blockIdx.x - kb * chunks) * 128;
+    if (used && !used[kb]) return;
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row0 = kb * 128 + warp * 16;
     uint32_t v[2][16] = {}, top[2] = {0, 0};
@@ -317,7 +336,7 @@ cudaError_t launch_encode8(const Geometry &g, const uint16_t *w, int64_t ld, con
     begin_encode(st);
     const cudaError_t e = launch_chained(encode8_kernel, (unsigned)(g.nrt * g.kkeep), 512, 0, st, g, w, ld, mask_blk_col, nm_bits,
                                          reinterpret_cast<int32_t *>(buf + I.col_off), buf + I.exp_off, buf + I.image_off, reinterpret_cast<uint32_t *>(buf),
-                                         columns_of(w, ld));
+                                         buf + I.used_off, columns_of(w, ld));
     end_encode();
     return e;
 }
@@ -328,7 +347,7 @@ cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, i
                           buf + I.image_off, w, ld, columns_of(w, ld));
 }
 
-cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t k, int64_t ncols, uint8_t *act, cudaStream_t st) {
+cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t k, int64_t ncols, uint8_t *act, const uint8_t *used, cudaStream_t st) {
     const Act8 a = act8(k, ncols);
     // (four blocks a thread where there are CTAs enough)
     const int u = a.groups * a.nblk >= 8 * 1184 ? 4 : 2;
@@ -336,10 +355,10 @@ cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t
     if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
     if (layout)
         return launch_chained(u == 4 ? quantize_tokens_kernel<4> : quantize_tokens_kernel<2>, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks, act,
-                              act + a.scale_off, (int)aligned16(x, ldx));
+                              act + a.scale_off, used, (int)aligned16(x, ldx));
     const bool quads = reinterpret_cast<uintptr_t>(x) % 8 == 0 && ldx % 4 == 0;
     return launch_chained(quads ? quantize_columns_kernel<true> : quantize_columns_kernel<false>, (unsigned)ctas, 256, 0, st, x, ldx, k, ncols, a.nblk, a.groups, a.chunks,
-                          act, act + a.scale_off);
+                          act, act + a.scale_off, used);
 }
 
 }  // namespace crisp

@@ -1050,11 +1050,14 @@ static crisp_status_t check_quantize(const uint16_t *d_x, int64_t ldx, int32_t x
     return ldx < (x_layout ? k : ncols) ? CRISP_BAD_SHAPE : CRISP_OK;
 }
 
+static crisp_status_t quantize(const uint16_t *d_x, int64_t ldx, int32_t x_layout, int64_t k, int64_t ncols, void *d_act, const uint8_t *used, void *stream) {
+    const cudaError_t e = launch_quantize8(d_x, ldx, x_layout, k, ncols, reinterpret_cast<uint8_t *>(d_act), used, (cudaStream_t)stream);
+    return e == cudaSuccess ? CRISP_OK : e == cudaErrorInvalidValue ? CRISP_UNSUPPORTED : CRISP_CUDA_ERROR;
+}
+
 crisp_status_t crisp_quantize8(const uint16_t *d_x_bf16, int64_t ldx, int32_t x_layout, int64_t k, int64_t ncols, void *d_act, void *stream) {
     const crisp_status_t bad = check_quantize(d_x_bf16, ldx, x_layout, k, ncols, d_act);
-    if (bad != CRISP_OK) return bad;
-    const cudaError_t e = launch_quantize8(d_x_bf16, ldx, x_layout, k, ncols, reinterpret_cast<uint8_t *>(d_act), (cudaStream_t)stream);
-    return e == cudaSuccess ? CRISP_OK : e == cudaErrorInvalidValue ? CRISP_UNSUPPORTED : CRISP_CUDA_ERROR;
+    return bad != CRISP_OK ? bad : quantize(d_x_bf16, ldx, x_layout, k, ncols, d_act, nullptr, stream);
 }
 
 crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_act, int64_t ncols, void *d_y, int64_t ldy, int32_t y_layout, int32_t y_dtype,
@@ -1078,9 +1081,12 @@ crisp_status_t crisp_spmm8(crisp_handle8_t h, const uint16_t *d_x_bf16, int64_t 
     const bool fused = fused8(ncols, x_layout);
     crisp_status_t bad = check_product(h, d_act, fused, ncols, d_y, ldy, y_layout, y_dtype);
     if (bad == CRISP_OK) bad = check_quantize(d_x_bf16, ldx, x_layout, h->g.k, ncols, d_act, fused);
-    if (bad == CRISP_OK && !fused) bad = crisp_quantize8(d_x_bf16, ldx, x_layout, h->g.k, ncols, d_act, stream);
+    // (what no row tile keeps is neither read nor quantised)
+    const bool some = h && h->g.kkeep > 0 && h->g.kkeep < h->g.nblk;
+    if (bad == CRISP_OK && !fused && h->g.kkeep > 0)
+        bad = quantize(d_x_bf16, ldx, x_layout, h->g.k, ncols, d_act, some ? h->buf + image8(h->g).used_off : nullptr, stream);
     if (bad != CRISP_OK) return bad;
-    const cudaError_t e = launch_spmm8(h, fused ? d_x_bf16 : nullptr, ldx, x_layout, d_act, !fused, ncols, d_y, ldy, y_layout, y_dtype, moment, (cudaStream_t)stream);
+    const cudaError_t e = launch_spmm8(h, fused ? d_x_bf16 : nullptr, ldx, x_layout, d_act, !fused && h->g.kkeep > 0, ncols, d_y, ldy, y_layout, y_dtype, moment, (cudaStream_t)stream);
     return e == cudaSuccess ? CRISP_OK : CRISP_CUDA_ERROR;
 }
 

@@ -408,3 +408,72 @@ def test_prune_fine_tune_and_serve_in_8_bits():
         y = L.set_epilogue8(None, relu=True).spmm8(y, tokens=True)
         check(numbers(y.t()), held, before, k, 0, relu=True)
     net.close()
+
+
+def test_the_first_products_of_a_process_may_be_captured():
+    """A process whose first product of each kind is captured: nothing that a call looks up once is refused in a capture."""
+    import os
+    import subprocess
+    import sys
+    code = """
+import torch
+from paper_2311_14272_b200 import binding as B
+torch.manual_seed(0)
+L = B.HybridLayer(300, 700, 4, 4, 128, 128, 1.0).build_mask(torch.rand(300, 700, device="cuda"))
+w = torch.randn(300, 700, device="cuda").bfloat16()
+L.encode8(w)
+xs = [torch.randn(n, 700, device="cuda").bfloat16() for n in (1, 9, 40, 400, 3000)]
+opt = B.AdamW([w], state_bits=8)
+g = torch.randn(300, 700, device="cuda")
+torch.cuda.synchronize()
+graph = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph):
+    ys = [L.spmm8(x, tokens=True) for x in xs]
+    zs = [L.spmm8(x.t().contiguous()) for x in xs]
+graph.replay()
+torch.cuda.synchronize()
+for x, y, z in zip(xs, ys, zs):
+    assert torch.equal(L.spmm8(x, tokens=True), y) and torch.equal(L.spmm8(x.t().contiguous()), z)
+graph2 = torch.cuda.CUDAGraph()
+with torch.cuda.graph(graph2):
+    opt.step([g])
+    m, root = opt.moments()
+graph2.replay()
+torch.cuda.synchronize()
+assert m.abs().sum() > 0 and root.min() >= 0
+print("captured")
+"""
+    env = dict(os.environ, PYTHONPATH=os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
+    out = subprocess.run([sys.executable, "-c", code], capture_output=True, text=True, timeout=300, env=env)
+    assert out.stdout.strip().endswith("captured"), out.stderr[-2000:]
+
+
+@pytest.mark.parametrize("tokens", [False, True])
+@pytest.mark.parametrize("rows,k,n,ncols,keep", [(128, 1024, 4, 40, 0.25), (256, 1000, 2, 700, 0.25), (300, 4100, 4, 129, 0.1), (100, 9000, 4, 33, 0.5)])
+def test_what_no_row_tile_keeps_is_not_read(rows, k, n, ncols, keep, tokens):
+    """NaN in X under blocks that no row tile kept changes nothing, with the masks of two encodings into one buffer."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, w, mask = layer(B, torch, rows, k, n, 4, keep, 31)
+    rng = np.random.default_rng(32)
+    x = activations(rng, k, ncols)
+    for again in range(2):
+        if again:
+            score = rng.random((rows, k)).astype(np.float32)
+            L.build_mask(to_dev(score, torch))
+            words = L.export_mask()[1]
+            mask = np.unpackbits(words.view(np.uint8), axis=1, bitorder="little")[:rows, :k].astype(bool)
+            dense = rng.standard_normal((rows, k))
+            L.encode8(bf16_dev(bits_of(dense), torch))
+            w = ref.weights(wl.bf16_bits_to_f32(bits_of(dense)).astype(np.float64), mask)
+        kept = np.array([mask[:, b * 128:(b + 1) * 128].any() for b in range((k + 127) // 128)])
+        assert kept.any() and not kept.all()
+        spoilt = x.copy()
+        spoilt[~np.repeat(kept, 128)[:k]] = 0x7FC0
+        y = []
+        for bits in (x, spoilt):
+            d_x = bf16_dev(np.ascontiguousarray(bits.T if tokens else bits), torch)
+            out = L.spmm8(d_x, y_dtype=1, tokens=tokens)
+            y.append(numbers(out.t() if tokens else out))
+        assert np.array_equal(y[0], y[1])
+        check(y[1], w, ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64)), k, 1)
