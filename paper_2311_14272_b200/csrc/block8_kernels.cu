@@ -162,12 +162,38 @@ __device__ __forceinline__ void put_scale(uint8_t *scales, int64_t chunks, int64
     *reinterpret_cast<uint32_t *>(scales + (kb * chunks + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4) = e * 0x01010101u;
 }
 
+// 2 kWords elements that start at any even address, out of the two aligned pieces of as many that hold them.
+template <int kWords>
+__device__ __forceinline__ void unaligned(const uint16_t *p, uint32_t (&v)[kWords]) {
+    const uint32_t by = (uint32_t)(reinterpret_cast<uintptr_t>(p) >> 1) & (2 * kWords - 1);
+    uint32_t w[2 * kWords];
+    if constexpr (kWords == 4) {
+        const uint4 *from = reinterpret_cast<const uint4 *>(p - by);
+        const uint4 a = from[0], b = from[1];
+        w[0] = a.x; w[1] = a.y; w[2] = a.z; w[3] = a.w; w[4] = b.x; w[5] = b.y; w[6] = b.z; w[7] = b.w;
+#pragma unroll
+        for (int i = 0; i < 6; ++i) w[i] = by & 4 ? w[i + 2] : w[i];
+    } else {
+        const uint2 *from = reinterpret_cast<const uint2 *>(p - by);
+        const uint2 a = from[0], b = from[1];
+        w[0] = a.x; w[1] = a.y; w[2] = b.x; w[3] = b.y;
+    }
+#pragma unroll
+    for (int i = 0; i <= kWords; ++i)
+        if (i + 1 < 2 * kWords) w[i] = by & 2 ? w[i + 1] : w[i];
+#pragma unroll
+    for (int i = 0; i < kWords; ++i) v[i] = __funnelshift_r(w[i], w[i + 1], 16 * (by & 1));
+}
+
 // X [ncols, k]: a CTA takes eight columns (tokens) and 2 U k-blocks; 16 threads a block of one column, eight values each, U blocks a thread.  Bound by instructions
-// (4096 x 8192: 20 a value and 22 us as one loop over the blocks with every question asked in it; now 16.8, 6.0 TB/s): a CTA whose blocks are all there asks nothing,
-// and two blocks' largest values travel through the shuffles in one word.
-template <int U, bool kFull>
+// (4096 x 8192: 20 a value and 22 us as one loop over the blocks with every question asked in it; now 17.1, 5.9 TB/s): a CTA whose blocks are all there asks nothing,
+// and two blocks' largest values travel through the shuffles in one word.  At other addresses each thread reads the two 16-byte pieces around its values (4097 x 8192:
+// 29.4 us, 35.6 by single elements).
+enum class Read { kAligned, kUnaligned, kParts };             // whole blocks at multiples of 16 bytes, at others, all else
+template <int U, Read kRead>
 __device__ __forceinline__ void quantize_tokens(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes,
                                                 uint8_t *scales, const uint8_t *used, int vec_ok, int64_t group, int64_t kb0) {
+    constexpr bool kFull = kRead != Read::kParts;
     const int lane = threadIdx.x & 15, r = threadIdx.x >> 4 & 7, side = threadIdx.x >> 7;
     const int64_t col = group * 8 + r, kb1 = kb0 + side * U;         // (a warp's two columns share their k-blocks)
     uint32_t v[U][4], top[U], word[U / 2], any = 0;
@@ -181,7 +207,9 @@ __device__ __forceinline__ void quantize_tokens(const uint16_t *x, int64_t ldx, 
 #pragma unroll
         for (int j = 0; j < 4; ++j) v[i][j] = 0;
         if (!wanted[i]) continue;
-        if (kFull || (vec_ok && col < ncols && at + 8 <= k)) {
+        if (kRead == Read::kUnaligned) {
+            unaligned<4>(from + i * 128, v[i]);
+        } else if (kFull || (vec_ok && col < ncols && at + 8 <= k)) {
             const uint4 u = *reinterpret_cast<const uint4 *>(from + i * 128);
             v[i][0] = u.x; v[i][1] = u.y; v[i][2] = u.z; v[i][3] = u.w;
         } else if (col < ncols) {
@@ -236,17 +264,24 @@ quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols,
     launch_dependents();                     // (a product behind this one fetches weights meanwhile: all before this kernel has finished)
     const uint32_t spans = (uint32_t)((nblk + 2 * U - 1) / (2 * U)), g = blockIdx.x / spans;
     const int64_t group = g, kb0 = (int64_t)(blockIdx.x - g * spans) * (2 * U);
-    if (vec_ok && (kb0 + 2 * U) * 128 <= k && group * 8 + 8 <= ncols)
-        quantize_tokens<U, true>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, used, vec_ok, group, kb0);
+    const int64_t end = (kb0 + 2 * U) * 128, first = group * 8;
+    if (end > k || first + 8 > ncols)
+        quantize_tokens<U, Read::kParts>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, used, vec_ok, group, kb0);
+    else if (vec_ok)
+        quantize_tokens<U, Read::kAligned>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, used, vec_ok, group, kb0);
+    else if (first * ldx + kb0 * 128 >= 7 && (first + 7) * ldx + end + 8 <= (ncols - 1) * ldx + k)     // (what lies around the blocks is X, too)
+        quantize_tokens<U, Read::kUnaligned>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, used, vec_ok, group, kb0);
     else
-        quantize_tokens<U, false>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, used, vec_ok, group, kb0);
+        quantize_tokens<U, Read::kParts>(x, ldx, k, ncols, nblk, groups, chunks, codes, scales, used, vec_ok, group, kb0);
 }
 
 // X [k, ncols]: a CTA takes 128 columns of one k-block.  A warp reads 16 rows of it, a lane four columns; the 16 values of a column in a warp are one
-// 16-byte chunk of its codes.  Neighbouring CTAs read neighbouring columns.  4096 x 8192: 18.2 us (5.5 TB/s); two pairs of columns a lane, 64 apart (fewer bank
-// conflicts), 23.4; neighbouring CTAs on neighbouring k-blocks, 64 columns each, 52.
+// 16-byte chunk of its codes.  Neighbouring CTAs read neighbouring columns.  The tile in shared memory is the atoms' with their chunks in another order in each atom,
+// since a warp writes eight atoms' chunks of one place together.  4096 x 8192: 19.7 us (5.1 TB/s); two pairs of columns a lane, 64 apart, 23.4; eight rows a warp, 23.6
+// (more partial maxima); neighbouring CTAs on neighbouring k-blocks, 64 columns each, 52.  Rows that do not start at multiples of 8 bytes take two loads (4096 x 8191:
+// 26.7 us with four CTAs an SM; single elements 41).
 template <bool kQuads>
-__global__ void __launch_bounds__(256)
+__global__ void __launch_bounds__(256, kQuads ? 3 : 4)
 quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint8_t *codes, uint8_t *scales,
                         const uint8_t *used) {
     __shared__ uint32_t largest[2][8][32];
@@ -258,23 +293,36 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t row0 = kb * 128 + warp * 16;
     uint32_t v[2][16] = {}, top[2] = {0, 0};
-    // a lane's four columns: neighbours where they can be read together, else 32 apart, so that the lanes' are
-    const auto column = [&](int j) { return kQuads ? 4 * lane + j : lane + 32 * j; };
-    if (kQuads && c0 + 4 * lane + 4 <= ncols && row0 + 16 <= k) {
+    const int64_t col = c0 + 4 * lane, last = min(row0 + 15, k - 1);
+    const uint16_t *p = x + row0 * ldx + col;
+    if (col + 4 <= ncols && row0 < k && (kQuads || (row0 * ldx + col >= 3 && last * ldx + col + 8 <= (k - 1) * ldx + ncols))) {
+        const auto take = [&](int i, int64_t at) {
+            if constexpr (kQuads) {
+                const uint2 two = *reinterpret_cast<const uint2 *>(p + at);
+                v[0][i] = two.x; v[1][i] = two.y;
+            } else {
+                uint32_t two[2];
+                unaligned<2>(p + at, two);                           // (both pieces lie within X)
+                v[0][i] = two[0]; v[1][i] = two[1];
+            }
+        };
+        if (row0 + 16 <= k) {
 #pragma unroll
-        for (int i = 0; i < 16; ++i) {
-            const uint2 two = *reinterpret_cast<const uint2 *>(x + (row0 + i) * ldx + c0 + 4 * lane);
-            v[0][i] = two.x; v[1][i] = two.y;
+            for (int i = 0; i < 16; ++i) take(i, i * ldx);
+        } else {
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+                take(i, min((int64_t)i, last - row0) * ldx);
+                if (row0 + i >= k) v[0][i] = v[1][i] = 0;
+            }
         }
     } else {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int64_t col = c0 + column(j);
-            if (col >= ncols) continue;
-            const uint16_t *p = x + row0 * ldx + col;
+            if (col + j >= ncols) break;
 #pragma unroll
             for (int i = 0; i < 16; ++i)
-                if (row0 + i < k) v[j >> 1][i] |= (uint32_t)p[i * ldx] << (16 * (j & 1));
+                if (row0 + i < k) v[j >> 1][i] |= (uint32_t)p[i * ldx + j] << (16 * (j & 1));
         }
     }
 #pragma unroll
@@ -307,8 +355,8 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
         }
 #pragma unroll
         for (int s = 0; s < 2; ++s) {
-            const int c = column(2 * h + s);
-            *reinterpret_cast<uint4 *>(tile + (c >> 3) * 1024 + (c & 7) * 128 + ((warp ^ (c & 7)) << 4)) = make_uint4(q[s][0], q[s][1], q[s][2], q[s][3]);
+            const int c = 4 * lane + 2 * h + s;
+            *reinterpret_cast<uint4 *>(tile + (c >> 3) * 1024 + (c & 7) * 128 + ((warp ^ c ^ (c >> 3)) & 7) * 16) = make_uint4(q[s][0], q[s][1], q[s][2], q[s][3]);
             if (warp == 0 && c0 + c < ncols) put_scale(scales, chunks, kb, c0 + c, e[s]);
         }
     }
@@ -317,7 +365,7 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
     const int64_t first = c0 >> 3;
     const int atoms = (int)min((int64_t)16, groups - first);
     uint4 *out = reinterpret_cast<uint4 *>(codes + (kb * groups + first) * 1024);
-    for (int i = threadIdx.x; i < atoms * 64; i += 256) out[i] = reinterpret_cast<const uint4 *>(tile)[i];
+    for (int i = threadIdx.x; i < atoms * 64; i += 256) out[i] = reinterpret_cast<const uint4 *>(tile)[i ^ (i >> 6 & 7)];
 }
 
 // Columns that a load or store may take.

@@ -477,3 +477,26 @@ def test_what_no_row_tile_keeps_is_not_read(rows, k, n, ncols, keep, tokens):
             y.append(numbers(out.t() if tokens else out))
         assert np.array_equal(y[0], y[1])
         check(y[1], w, ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64)), k, 1)
+
+
+@pytest.mark.parametrize("tokens", [False, True])
+@pytest.mark.parametrize("k,ncols", [(1100, 77), (600, 300), (4200, 2500)])
+def test_activations_at_any_even_address(k, ncols, tokens):
+    """Every address and pitch of activations gives the bits of the aligned ones; what lies around them, NaN, is in no result."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, _, _ = layer(B, torch, 128, k, 4, 4, 1.0, 41)
+    x = torch.randn(k, ncols, device="cuda").bfloat16()
+    x[torch.rand(k, ncols, device="cuda") < 0.001] *= 500
+    x = x.t().contiguous() if tokens else x
+    rows, cols = x.shape
+    want = None
+    for pitch in (-cols % 8, -cols % 8 + 1, -cols % 8 + 2, -cols % 8 + 3, 7 + -cols % 8, 4 + -cols % 8):
+        for odd in (0, 1, 2, 3, 4, 5, 7) if want is not None else (0,):
+            whole = torch.full((rows * (cols + pitch) + odd + 16,), float("nan"), dtype=torch.bfloat16, device="cuda")
+            d_x = whole[odd:odd + rows * (cols + pitch)].view(rows, cols + pitch)[:, :cols]
+            d_x.copy_(x)
+            y = L.spmm8(d_x, y_dtype=1, tokens=tokens)
+            if want is None:
+                want = y.clone()
+            assert torch.equal(y, want) and not torch.isnan(y).any(), (pitch, odd)
