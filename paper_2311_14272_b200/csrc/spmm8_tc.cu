@@ -811,11 +811,12 @@ Variant8 make_pair_variant8() {
 }
 Variant8 pair_variant8(int tile) { return tile == 128 ? make_pair_variant8<128>() : tile == 192 ? make_pair_variant8<192>() : make_pair_variant8<256>(); }
 
-// The products that quantise X themselves.
-// (of [k, ncols] a thread fetches its eight values one by one: 1654 x 1348, 31 columns 12.9 us, quantised apart 8.5)
-bool fused8(int64_t ncols, int layout) { return ncols <= (layout ? 32 : 8); }
-template <bool kSplit>
-Variant8 fused_variant8(int tile) { return tile == 16 ? make_variant8<16, kSplit, true>() : make_variant8<32, kSplit, true>(); }
+// The products that quantise X themselves, in every row tile's CTAs: one launch less for the host, which takes some 8 us for two in a row (4.7 for one), but not always
+// less for the device.  In a row from the host and in a graph, us, so and quantised apart: 1024 x 1024, 8 tokens 5.9 and 8.0, in a graph 5.8 and 5.3; 4096 x 4096, half of
+// the blocks, 8 tokens 6.8 and 8.0 (6.8 and 6.1), 12 tokens 7.2 and 8.0 (7.2 and 6.3), 16 tokens 7.6 and 8.1 (7.7 and 6.3), 32 tokens 9.5 and 8.2 (9.5 and 7.1); all blocks, 12
+// tokens 8.6 and 8.9 (8.8 and 8.5), 16 tokens 9.3 and 8.9; 8192 x 8192, half, where a CTA has 16 blocks, 5 tokens 10.5 and 9.5 (10.5 and 8.8).  Of [k, ncols] a thread
+// fetches its values one by one: 4096 x 4096, half, 5 columns 7.6 and 8.7 (7.2 and 8.1), 8 columns 8.4 and 8.4 (8.2 and 7.4).
+bool fused8(const Geometry &g, int64_t ncols, int layout) { return ncols <= (layout ? 12 : 5) && (int64_t)g.nrt * g.kkeep <= 1536; }
 
 // How many clusters of s CTAs, one an SM, run at once: fewer than SMs / s, since a cluster lies within one GPC.  (A second wave for two of sixteen clusters of eight
 // made 2048 x 2048 with one column 10.2 us instead of 5.7.)
@@ -892,7 +893,7 @@ crisp_status_t check_product(crisp_handle8_s *h, const void *d_act, bool fused, 
     return CRISP_OK;
 }
 
-// x: what the product quantises itself (columns as fused8 has them); else nullptr, and d_act holds the codes, which the kernel in front wrote if `behind`.
+// x: what the product quantises itself (fused8); else nullptr, and d_act holds the codes, which the kernel in front wrote if `behind`.
 cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int x_layout, const void *d_act, bool behind, int64_t ncols, void *d_y, int64_t ldy,
                          int y_layout, int y_dtype, uint64_t moment, cudaStream_t st) {
     int device = 0;
@@ -925,10 +926,9 @@ cudaError_t launch_spmm8(crisp_handle8_s *h, const uint16_t *x, int64_t ldx, int
     int tile, split;
     bool pair;
     choose8(h, ncols, device, &tile, &split, &pair);
-    if (x && tile > 32) tile = 32;
-    if (x) pair = false;
+    if (x) { tile = 16; pair = false; }
     const Act8 a = act8(g.k, ncols);
-    const Variant8 v = pair ? pair_variant8(tile) : x ? (split > 1 ? fused_variant8<true>(tile) : fused_variant8<false>(tile)) : split > 1 ? variant8<true>(tile) : variant8<false>(tile);
+    const Variant8 v = pair ? pair_variant8(tile) : x ? (split > 1 ? make_variant8<16, true, true>() : make_variant8<16, false, true>()) : split > 1 ? variant8<true>(tile) : variant8<false>(tile);
     if (!v.configured[device].load(std::memory_order_relaxed)) {
         e = cudaFuncSetAttribute(reinterpret_cast<const void *>(v.kern), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemBudget + 1024);
         if (e != cudaSuccess) return e;
@@ -1071,14 +1071,14 @@ crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_act, int64
 crisp_status_t crisp_spmm8_sizes(crisp_handle8_t h, int64_t ncols, size_t *act_bytes) {
     if (!h || !act_bytes) return CRISP_INVALID_ARG;
     const crisp_status_t bad = crisp_quantize8_sizes(h->g.k, ncols, act_bytes);
-    if (bad == CRISP_OK && fused8(ncols, 0) && fused8(ncols, 1)) *act_bytes = 0;
+    if (bad == CRISP_OK && fused8(h->g, ncols, 0) && fused8(h->g, ncols, 1)) *act_bytes = 0;
     return bad;
 }
 
 crisp_status_t crisp_spmm8(crisp_handle8_t h, const uint16_t *d_x_bf16, int64_t ldx, int32_t x_layout, int64_t ncols, void *d_act, void *d_y, int64_t ldy,
                            int32_t y_layout, int32_t y_dtype, void *stream) {
     const uint64_t moment = encodes.now();
-    const bool fused = fused8(ncols, x_layout);
+    const bool fused = h && fused8(h->g, ncols, x_layout);
     crisp_status_t bad = check_product(h, d_act, fused, ncols, d_y, ldy, y_layout, y_dtype);
     if (bad == CRISP_OK) bad = check_quantize(d_x_bf16, ldx, x_layout, h->g.k, ncols, d_act, fused);
     // (what no row tile keeps is neither read nor quantised)
