@@ -19,8 +19,8 @@ namespace {
 // -------------------------------------------------------------------------------------------------------------- weights
 
 // One CTA a kept block: thread t takes eight columns (t % 16) of rows t / 16, + 32, ...  `vec`: 8, 2 or 1 columns a load, by what address and pitch allow.
-// Bound by the chain of a CTA (list, mask and weights, largest value, codes): 4096 x 4096 2:4 keep 0.5 8.8 us, all of it 13.4, with four CTAs an SM; two 11.3 and
-// 18.3, three 10.8 and 15.7.
+// Bound by the chain of a CTA (list, mask and weights, largest value, codes): 4096 x 4096 2:4 keep 0.5 8.4 us, all of it 13.1, with four CTAs an SM; two 11.3 and
+// 18.3, three 10.8 and 15.7.  A thread's loads all ahead of their use spill at four CTAs (16.0), and take 9.1 and 13.2 at three; two rows a thread 10.0 and 15.9.
 __global__ void __launch_bounds__(512, 4)
 encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_blk_col, const uint32_t *nm_bits, int32_t *blk_col, uint8_t *exps, uint8_t *image,
                uint32_t *header, uint8_t *used, int wide) {
@@ -99,7 +99,8 @@ encode8_kernel(Geometry g, const uint16_t *w, int64_t ld, const int32_t *mask_bl
 }
 
 // One CTA a block of the dense matrix, kept or not.
-__global__ void __launch_bounds__(512)
+constexpr int kDecode = 256;                                   // (4096 x 4096, half kept: 8.3 us; with 128 threads 9.3, 512 8.6, and 10.4 with loads behind stores)
+__global__ void __launch_bounds__(kDecode, 2048 / kDecode)
 decode8_kernel(Geometry g, const int32_t *blk_col, const uint8_t *exps, const uint8_t *image, uint16_t *w, int64_t ld, int wide) {
     chain_kernels();
     const int rt = blockIdx.x / g.nblk, kb = blockIdx.x - rt * g.nblk;
@@ -125,21 +126,27 @@ decode8_kernel(Geometry g, const int32_t *blk_col, const uint8_t *exps, const ui
     const int64_t col = (int64_t)kb * 128 + chunk * 8;
     const float up = power_of(e);
     const uint8_t *entry = image + (int64_t)slot * kEntry8;
+    // (all codes ahead of the first store, which the compiler would not move a load over)
+    constexpr int kRows = 2048 / kDecode;
+    uint2 codes[kRows] = {};
+    if (slot >= 0) {
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int r = row0 + 32 * i;
-        const int64_t row = (int64_t)rt * 128 + r;
-        if (row >= g.rows || col >= g.k) continue;
-        uint32_t out[4] = {};
-        if (slot >= 0) {
-            const uint2 c = *reinterpret_cast<const uint2 *>(entry + (r >> 3) * 1024 + (r & 7) * 128 + (((chunk >> 1) ^ (r & 7)) << 4) + (chunk & 1) * 8);
+        for (int i = 0; i < kRows; ++i) {
+            const int r = row0 + kDecode / 16 * i;
+            codes[i] = *reinterpret_cast<const uint2 *>(entry + (r >> 3) * 1024 + (r & 7) * 128 + (((chunk >> 1) ^ (r & 7)) << 4) + (chunk & 1) * 8);
+        }
+    }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((j < 2 ? c.x : c.y) >> (16 * (j & 1))), __NV_E4M3);
-                const float2 v = __half22float2(__half2(h));
-                const __nv_bfloat162 b = __floats2bfloat162_rn(v.x * up, v.y * up);
-                out[j] = *reinterpret_cast<const uint32_t *>(&b);
-            }
+    for (int i = 0; i < kRows; ++i) {
+        const int64_t row = (int64_t)rt * 128 + row0 + kDecode / 16 * i;
+        if (row >= g.rows || col >= g.k) break;
+        uint32_t out[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const __half2_raw h = __nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((j < 2 ? codes[i].x : codes[i].y) >> (16 * (j & 1))), __NV_E4M3);
+            const float2 v = __half22float2(__half2(h));
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v.x * up, v.y * up);
+            out[j] = *reinterpret_cast<const uint32_t *>(&b);
         }
         uint16_t *p = w + row * ld + col;
         const int vec = col + 8 <= g.k ? wide : 1;
@@ -391,7 +398,7 @@ cudaError_t launch_encode8(const Geometry &g, const uint16_t *w, int64_t ld, con
 
 cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, int64_t ld, cudaStream_t st) {
     const Image8 I = image8(g);
-    return launch_chained(decode8_kernel, (unsigned)(g.nrt * g.nblk), 512, 0, st, g, reinterpret_cast<const int32_t *>(buf + I.col_off), buf + I.exp_off,
+    return launch_chained(decode8_kernel, (unsigned)(g.nrt * g.nblk), kDecode, 0, st, g, reinterpret_cast<const int32_t *>(buf + I.col_off), buf + I.exp_off,
                           buf + I.image_off, w, ld, columns_of(w, ld));
 }
 
