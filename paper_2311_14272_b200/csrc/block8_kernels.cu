@@ -285,7 +285,7 @@ quantize_tokens_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols,
 // X [k, ncols]: a CTA takes 128 columns of one k-block.  A warp reads 16 rows of it, a lane four columns; the 16 values of a column in a warp are one
 // 16-byte chunk of its codes.  Neighbouring CTAs read neighbouring columns.  The tile in shared memory is the atoms' with their chunks in another order in each atom,
 // since a warp writes eight atoms' chunks of one place together.  4096 x 8192: 19.7 us (5.1 TB/s); two pairs of columns a lane, 64 apart, 23.4; eight rows a warp, 23.6
-// (more partial maxima); neighbouring CTAs on neighbouring k-blocks, 64 columns each, 52.  Rows that do not start at multiples of 8 bytes take two loads (4096 x 8191:
+// (more partial maxima); X through shared memory by asynchronous copies, 20.5; neighbouring CTAs on neighbouring k-blocks, 64 columns each, 52.  Rows that do not start at multiples of 8 bytes take two loads (4096 x 8191:
 // 26.7 us with four CTAs an SM; single elements 41).
 template <bool kQuads>
 __global__ void __launch_bounds__(256, kQuads ? 3 : 4)
