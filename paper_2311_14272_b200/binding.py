@@ -6,6 +6,7 @@ PyTorch fallback: if the shared library is missing, loading raises.
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes as C
 import os
 import re
@@ -612,8 +613,13 @@ def crisp_destroy8(handle8: int):
         load().crisp_destroy8(handle8)
 
 
+_AS_IT_IS = contextlib.nullcontext()
+
+
 def _allocating_for(stream):
     """A context in which torch allocates memory for the stream of a call (None: the current one; a torch stream or an address)."""
+    if stream is None:
+        return _AS_IT_IS
     import torch
     return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
 
@@ -793,6 +799,10 @@ class HybridLayer:
     def set_path(self, path: int):
         crisp_set_path(self.handle, path)
 
+    def _on_device(self):
+        """A context in which the layer's device is the current one."""
+        return _AS_IT_IS if self.device.index == _current_device() else self.torch.cuda.device(self.device)
+
     # The layer in 8 bits, beside or instead of its bf16 encoding (masks of 128 x 128 blocks).
     def encode8(self, w, stream=None):
         """Compress the weights under the mask to e4m3 with a scale for each kept block (crisp_encode8).  The epilogue of an encoding before is not carried over."""
@@ -813,7 +823,7 @@ class HybridLayer:
         old, self.handle8 = self.handle8, 0
         crisp_destroy8(old)
         self._bias8 = None
-        with self.torch.cuda.device(self.device):
+        with self._on_device():
             self.handle8 = crisp_encode8(w, _pitch(w), self.mask, self.buf8, stream)
         return self
 
@@ -825,7 +835,7 @@ class HybridLayer:
                 raise CrispError(code, "crisp_decode8")
             return w
         w = self.torch.empty_strided((self.desc.rows, self.desc.k), (self.desc.k, 1), dtype=self.torch.bfloat16, device=self.device)
-        with self.torch.cuda.device(self.device):
+        with self._on_device():
             crisp_decode8(self.handle8, w, self.desc.k, stream)
         return w
 
@@ -833,9 +843,9 @@ class HybridLayer:
         """X in 8 bits, for this layer and others of its k: x is [k, ncols], or with tokens=True [ncols, k]."""
         ncols = self._columns8(x, tokens)
         k = self.desc.k
-        with self.torch.cuda.device(self.device):
+        with self._on_device():
             with _allocating_for(stream):
-                act = self.torch.empty(crisp_quantize8_sizes(k, ncols), dtype=self.torch.uint8, device=self.device)
+                act = self.torch.empty_strided((crisp_quantize8_sizes(k, ncols),), (1,), dtype=self.torch.uint8, device=self.device)
             crisp_quantize8(x, _pitch(x), int(tokens), k, ncols, act, stream)
         return Activations8(k, ncols, act)
 
@@ -865,7 +875,7 @@ class HybridLayer:
         else:
             assert y.device == self.device and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1), \
                 "Y has the product's shape and type, and consecutive elements in a row"
-        with torch.cuda.device(self.device):
+        with self._on_device():
             if held:
                 crisp_spmm8_quantized(self.handle8, x.buffer, ncols, y, _pitch(y), int(tokens), y_dtype, stream)
                 return y
