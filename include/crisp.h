@@ -341,7 +341,8 @@ CRISP_API crisp_status_t crisp_prune_encode(int32_t n_layers, const crisp_prune_
  * one, and down elsewhere: rounded to nearest, an average that moves by less than half a step (1/16 and 1/32 of the value, while beta2 =
  * 0.999 moves v by a thousandth) would stand still.  The number comes from a hash of seed, step, the tensor's place in the
  * call and e, so a step's result does not depend on the launch.  A sqrt(v) above 0 is never held as 0 (m / eps would follow).
- * An element that is not finite is held as 0 and leaves its block's scale alone; its weight is not finite from then on.
+ * An element whose m or v is not finite is held as 0 in both and leaves its block's scale alone.  Its weight is not finite from then on, unless only the
+ * square of a finite gradient left fp32 (above some 5e20): then the weight decays alone in this step, and the averages begin anew.
  *
  * `tensors` is read before the call returns.  Two entries must not share weights or state.  d_grad = NULL leaves a tensor as
  * it is.  n = 0 and tensors without elements are fine.  The scalars are those of the call; a step that is captured into a graph takes what

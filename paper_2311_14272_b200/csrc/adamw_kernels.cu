@@ -389,12 +389,13 @@ struct Piece {
         float am = 0.f, av = 0.f;
 #pragma unroll
         for (int i = 0; i < kPer; ++i) { am = max_nan(am, fabsf(m[i])); av = max_nan(av, root[i]); }
-        if (!(am <= kLargest) || !(av <= kLargest)) {                     // what is not finite is held as 0
+        if (!(am <= kLargest) || !(av <= kLargest)) {
+            // An element of which one is not finite is held as 0 in both: the square of a finite gradient may leave fp32, and its m over an sqrt(v) of 0 would be
+            // the next step's update.
             am = av = 0.f;
 #pragma unroll
             for (int i = 0; i < kPer; ++i) {
-                if (!(fabsf(m[i]) <= kLargest)) m[i] = 0.f;
-                if (!(root[i] <= kLargest)) root[i] = 0.f;
+                if (!(fabsf(m[i]) <= kLargest) || !(root[i] <= kLargest)) m[i] = root[i] = 0.f;
                 am = fmaxf(am, fabsf(m[i])); av = fmaxf(av, root[i]);
             }
         }

@@ -452,3 +452,33 @@ def test_prune_fine_tune_and_serve():
         y, want = net.layers[0].spmm(x).double(), weights[0].double() @ x.double()
         assert float((y - want).norm() / want.norm()) < 5e-3
     net.close()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_a_gradient_whose_square_leaves_fp32_moves_no_weight_later(bits):
+    """|m| / sqrt(v) of gradients that fp32 can square is at most (1 - b1) / sqrt((1 - b2) (1 - b1^2 / b2)) = 7.3, the corrections of early steps only lower it, and
+    a step of lr = 1e-3 then moves a weight by 7.3e-3 and its decay; codes that are off by a step of 1/8 and 1/16 make less than 1e-2 of it.  (1 - b2) g^2 is beyond
+    fp32 from 5.83e20 on: v is infinite there, held as 0 in 8 bits, and so has to be m."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    at, sizes = [0, 3, 130, 140, 255, 299], [6e20, -1e21, 1e30, -3e38, 5.7e20, -5.8e20]
+    rng = np.random.default_rng(60)
+    grads = [(rng.standard_normal(300) * 1e-2 * (s != 1)).astype(np.float32) for s in range(5)]
+    got = []
+    for outliers in (sizes, [0.0] * len(at)):
+        w = torch.ones(300, device="cuda")
+        opt = B.AdamW([w], state_bits=bits, seed=5)
+        grads[0][at] = outliers
+        before = numbers(w)
+        for s, g in enumerate(grads):
+            opt.step([to_dev(g, torch)])
+            now = numbers(w)
+            assert np.all(np.abs(now - before) <= 1e-2), s
+            before = now
+            if s == 0 and bits == 8 and outliers is sizes:
+                m, v = states(opt, 0, 300)
+                assert not m[at[:4]].any() and not v[at[:4]].any() and np.all(v[at[4:]] > 1e38) and np.all(np.abs(m[at[4:]]) > 1e19)
+        got.append(now)
+    # (the first block has no value that large beside those held as 0)
+    others = np.setdiff1d(np.arange(128), at)
+    assert np.array_equal(got[0][others], got[1][others])
