@@ -328,7 +328,7 @@ CRISP_API crisp_status_t crisp_prune_encode(int32_t n_layers, const crisp_prune_
  *   g = grad * grad_scale        m = beta1 m + (1 - beta1) g        v = beta2 v + (1 - beta2) g^2
  *   w = w (1 - lr weight_decay) - lr / (1 - beta1^step) * m / (sqrt(v) / sqrt(1 - beta2^step) + eps)
  *
- * in fp32, element by element (0 / 0 counts as 0).  Where a tensor's mask has no bit, w, m and v become 0, whatever the gradient is there (a mask of
+ * in fp32, element by element (0 / 0 counts as 0).  Where a tensor's mask has no bit, w, m and v become 0, whatever the gradient there and the step's scalars are (a mask of
  * NULL updates every weight: the dense update of the straight-through estimator).  Weights are fp32, or bf16 rounded at random (below); an
  * fp32 weight may have a bf16 copy (nearest even), the input of crisp_encode.
  *

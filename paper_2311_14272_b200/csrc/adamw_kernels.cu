@@ -337,7 +337,8 @@ struct Piece {
             if constexpr (kNarrow || !kW32) h[i] = mix_rest(first ^ (uint32_t)i);
         }
 
-        if (T.mask && !(fabsf(f.grad_scale) <= kLargest)) {      // (zero times that is not zero)
+        // (zero times what is not finite is not zero)
+        if (T.mask && !(fmaf(f.grad_scale, 0.f, fmaf(f.step_size, 0.f, fmaf(f.root_scale, 0.f, f.decay * 0.f))) == 0.f)) {
 #pragma unroll
             for (int i = 0; i < kPer; ++i)
                 if (!(x.keep >> i & 1u)) w[i] = m[i] = v[i] = root[i] = 0.f;

@@ -482,3 +482,21 @@ def test_a_gradient_whose_square_leaves_fp32_moves_no_weight_later(bits):
     # (the first block has no value that large beside those held as 0)
     others = np.setdiff1d(np.arange(128), at)
     assert np.array_equal(got[0][others], got[1][others])
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("which,value", [("d_lr", float("nan")), ("d_lr", float("inf")), ("d_step", 0), ("d_step", -3), ("lr", 1e39), ("weight_decay", -1e300)])
+def test_scalars_that_are_not_finite_leave_pruned_weights_zero(which, value, bits):
+    """(A step number below 1 makes the corrections infinite or NaN; 1e39 is a number of the host's and none of fp32.)"""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    data = make(torch, [(64, 128), (3, 37)], True, True, 52)
+    weights, grads = ([d[j][1] for d in data] for j in range(2))
+    layers, bits_of = masks_for(B, torch, [(64, 128), (3, 37)], 2, 4, 32, 0.5, 3)
+    opt = B.AdamW(weights, masks=layers, state_bits=bits, capturable=which.startswith("d_"))
+    getattr(opt, which).fill_(value) if which.startswith("d_") else setattr(opt, which, value)
+    for _ in range(2):
+        opt.step(grads)
+    for i, b in enumerate(bits_of):
+        m, v = states(opt, i, b.size)
+        assert not numbers(weights[i])[~b].any() and not m[~b].any() and not v[~b].any()
