@@ -4,7 +4,7 @@
 //
 // The weights are read once, and that bounds a product (4096 x 4096: 16.8 MB, 2.6 us at the copy rate).  A CTA takes the eight rows of an atom (block8.h) and its warps
 // the kept blocks in turn: a lane reads 32 bytes of every block, two rows' 16-byte chunks, for four blocks at a time, so that all of the weights are under way at
-// once.  Meanwhile the CTA quantises X into shared memory, block by block (its codes as fp32, and the exponents).  Codes are multiplied in fp32: products of two codes are
+// once.  Meanwhile the CTA quantises X into shared memory, block by block (its codes as fp32, and the scales).  Codes are multiplied in fp32: products of two codes are
 // exact, a block's sum is scaled once, and the sums of lanes and warps are added in a fixed order.
 // Not kept: mma.sync on fp16 codes, 16 rows a CTA.  The quantisation of X in every CTA is what is left then: 4096 x 4096 with half of its blocks, 4 tokens 5.3 instead of 6.5 us, but
 // 2048 x 8192 1 token 9.5 instead of 8.0, 512 x 4608 3.0 instead of 2.5.
@@ -23,7 +23,8 @@ using namespace block8;
 namespace {
 
 constexpr int kFewWarps = 8, kFewBlocks = 4;                  // warps a CTA, blocks of a warp under way
-constexpr int kFewBytes = 100 * 1024;                         // most that X's codes may take in shared memory
+constexpr int kFewBytes = 100 * 1024;                         // most that X's codes may take in shared memory, at 513 bytes a block of a column
+constexpr int kFewEach = 128 * 4 + 8;                         // bytes a block of a column: codes as fp32, and the two factors
 
 // A column's 128 codes of a block in shared memory: 16-byte pieces of the 16 codes of chunk c at piece ^ (c / 2 % 4), so that eight lanes that read one piece of eight
 // chunks touch all banks.
@@ -36,7 +37,9 @@ __global__ void __launch_bounds__(32 * kFewWarps, C == 1 ? 4 : 2)
 few8_kernel(const __grid_constant__ FewParams p) {
     extern __shared__ __align__(16) uint8_t shared[];
     float *codes = reinterpret_cast<float *>(shared);         // [kept block][column][128]
-    uint8_t *exps = shared + (size_t)p.kkeep * C * 512;       // [kept block][column]
+    // [kept block][column]: 2^(Ew + Ex) as two factors, each of half the sum of the exponents.  That sum may be out of fp32's range where the product is not, and so may
+    // the product with one of the two scales.
+    float2 *factors = reinterpret_cast<float2 *>(shared + (size_t)p.kkeep * C * 512);
     __shared__ float sums[kFewWarps][8][C];
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int rt = blockIdx.x >> 4, atom = blockIdx.x & 15;
@@ -45,7 +48,6 @@ few8_kernel(const __grid_constant__ FewParams p) {
     const bool here = rt * 128 + atom * 8 < p.rows;
     // the warp's first blocks: lane reads chunk lane % 8 of rows lane / 8 and lane / 8 + 4
     uint4 w[kFewBlocks][2];
-    uint32_t scale[kFewBlocks];
     const auto fetch = [&](int e0) {
 #pragma unroll
         for (int i = 0; i < kFewBlocks; ++i) {
@@ -54,7 +56,6 @@ few8_kernel(const __grid_constant__ FewParams p) {
                 const uint8_t *at = entries + (int64_t)e * kEntry8;
                 const uint4 *a = reinterpret_cast<const uint4 *>(at + atom * 1024);
                 w[i][0] = __ldcg(a + lane); w[i][1] = __ldcg(a + 32 + lane);
-                scale[i] = __ldcg(at + kTile8);
             }
         }
     };
@@ -68,6 +69,7 @@ few8_kernel(const __grid_constant__ FewParams p) {
         const bool in = u < p.kkeep * C;
         const int e = in ? u / C : 0, c = in ? u - e * C : 0;
         const int at = (p.all ? e : __ldcg(p.blk_col + (int64_t)rt * p.kkeep + e)) * 128 + l16 * 8;
+        const uint32_t ew = __ldcg(entries + (int64_t)e * kEntry8 + kTile8);
         uint32_t v[4] = {};
         if (in && c < p.cols) {
             if (p.x_layout == 1 && p.x_vec && at + 8 <= p.k) {
@@ -100,7 +102,7 @@ few8_kernel(const __grid_constant__ FewParams p) {
             float *block = codes + (e * C + c) * 128;
             *piece_at(block, l16 >> 1, (l16 & 1) * 2) = make_float4(q[0].x, q[0].y, q[1].x, q[1].y);
             *piece_at(block, l16 >> 1, (l16 & 1) * 2 + 1) = make_float4(q[2].x, q[2].y, q[3].x, q[3].y);
-            if (l16 == 0) exps[e * C + c] = (uint8_t)e8;
+            if (l16 == 0) factors[e * C + c] = make_float2(power_of((ew + e8) >> 1), power_of((ew + e8 + 1) >> 1));
         }
     }
     __syncthreads();
@@ -129,8 +131,8 @@ few8_kernel(const __grid_constant__ FewParams p) {
                         s[0] = fmaf(q[2 * j].x, f.x, s[0]); s[1] = fmaf(q[2 * j].y, f.y, s[1]);
                         s[2] = fmaf(q[2 * j + 1].x, f.z, s[2]); s[3] = fmaf(q[2 * j + 1].y, f.w, s[3]);
                     }
-                    // (two factors: the sum of both exponents may be out of fp32's range where the product is not)
-                    acc[r][c] = fmaf(((s[0] + s[1]) + (s[2] + s[3])) * power_of(scale[i] & 0xFFu), power_of(exps[e * C + c]), acc[r][c]);
+                    const float2 f = factors[e * C + c];
+                    acc[r][c] = fmaf(((s[0] + s[1]) + (s[2] + s[3])) * f.x, f.y, acc[r][c]);
                 }
             }
         }
@@ -167,11 +169,11 @@ cudaError_t launch(const FewParams &p, unsigned ctas, int device, cudaStream_t s
     static std::atomic<bool> configured[kMaxDevices];
     if (device < 0 || device >= kMaxDevices) return cudaErrorInvalidDevice;
     if (!configured[device].load(std::memory_order_relaxed)) {
-        const cudaError_t e = cudaFuncSetAttribute(few8_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewBytes);
+        const cudaError_t e = cudaFuncSetAttribute(few8_kernel<C>, cudaFuncAttributeMaxDynamicSharedMemorySize, kFewBytes / 513 * kFewEach);
         if (e != cudaSuccess) return e;
         configured[device].store(true, std::memory_order_relaxed);
     }
-    return launch_chained(few8_kernel<C>, ctas, 32 * kFewWarps, (size_t)p.kkeep * C * 513, st, p);
+    return launch_chained(few8_kernel<C>, ctas, 32 * kFewWarps, (size_t)p.kkeep * C * kFewEach, st, p);
 }
 
 }  // namespace

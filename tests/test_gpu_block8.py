@@ -500,3 +500,24 @@ def test_activations_at_any_even_address(k, ncols, tokens):
             if want is None:
                 want = y.clone()
             assert torch.equal(y, want) and not torch.isnan(y).any(), (pitch, odd)
+
+
+@pytest.mark.parametrize("power_w,power_x", [(0, -100), (-60, -60), (60, 60), (100, 20), (-120, 110), (120, -120), (124, -133), (-133, 120), (-133, 30)])
+@pytest.mark.parametrize("tokens,ncols", [(False, 1), (True, 4), (False, 5), (True, 12), (True, 40), (False, 300)])
+def test_values_of_any_size_in_every_kernel(tokens, ncols, power_w, power_x):
+    """On the CUDA cores, quantised within the product, and quantised apart, with scales whose product lies in fp32's range where one of them does not (tolerance
+    as for the products above; sums below 2^-140 are not looked at)."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    rng = np.random.default_rng(43)
+    k = 256
+    L, w, _ = layer(B, torch, 200, k, 4, 4, 1.0, 43, w=np.clip(rng.standard_normal((200, k)) * 2.0**power_w, -3e38, 3e38))
+    x = bits_of(rng.standard_normal((k, ncols)) * 2.0**power_x)
+    held = ref.activations(wl.bf16_bits_to_f32(x).astype(np.float64))
+    d_x = bf16_dev(np.ascontiguousarray(x.T if tokens else x), torch)
+    size = np.abs(w) @ np.abs(held)
+    tol = (4 * np.sqrt(k) + 2) * 2.0**-23 * size + 2.0**-140
+    for quantised in (False, True):
+        y = numbers(L.spmm8(L.quantize8(d_x, tokens=tokens) if quantised else d_x, y_dtype=1, tokens=tokens))
+        assert (L.last_launch8()["path"] == B.PATH_DIRECT) == (ncols <= 4 and not quantised)
+        assert np.all(np.abs((y.T if tokens else y) - w @ held) <= tol)
