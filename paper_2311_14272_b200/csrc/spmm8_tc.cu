@@ -547,8 +547,10 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 // bytes a cycle (128 x N x 32: 4 KB + 32 N bytes; 98, 118, 160 and 191 cycles measured for 64, 128, 192 and 256 columns where the products need 32, 64, 96 and 128); a
 // pair reads half of the columns' bytes a CTA, and fetches half of them from L2.
 //
-// The CTA of rank 0 issues for both.  Its peer's stages are announced to it by the peer's warp 1; commits go to both (multicast); accumulators are handed back by the
-// draining warps of both.
+// The CTA of rank 0 issues for both.  The copies of both complete on its barriers, which count the bytes of both (what has landed in the peer's shared memory is then
+// visible to the one who waits); commits go to both (multicast); accumulators are handed back by the draining warps of both, at the scope of the cluster: relaxed, as
+// what goes through tensor memory is ordered by the tcgen05 fences on either side, and nothing else is handed over.  (Released and acquired, a tile takes 0.35 us more;
+// stages announced one by one by a warp of the peer, released at that scope, 4096 x 4096 x 8192 188 us.)
 template <int N>
 struct Pair8 {
     static constexpr int kChunks = N <= 128 ? 1 : 2;
@@ -560,7 +562,7 @@ struct Pair8 {
     static constexpr uint32_t kBytes = kEntry8 + N / 2 * 128 + kChunks * kScales8;
     static constexpr int kEpi = 8;
     static constexpr uint32_t kStaging = 4096;
-    static constexpr uint32_t kFixed = kEpi * kStaging + 384;
+    static constexpr uint32_t kFixed = kEpi * kStaging + 256;
     static constexpr int kMost = (int)((kSmemBudget - kFixed) / kStage), kStages = kMost < 12 ? kMost : 12;
     static_assert(kAcc * N + 2 * kScaleCols <= 512, "tensor memory is 512 columns");
     static_assert(N % 64 == 0 && N / 2 * 128 % 1024 == 0, "halves are whole atoms, and scales begin at even columns");
@@ -580,7 +582,23 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t bar) {          // to t
                  ::"r"(bar), "h"((uint16_t)3) : "memory");
 }
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
-    asm volatile("mbarrier.arrive.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// After a wait for such arrivals: the phase that has been seen complete, seen at the scope of the cluster.
+__device__ __forceinline__ bool mbar_seen_cluster(uint32_t bar, uint32_t parity) {
+    uint32_t ok;
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "mbarrier.test_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
+    return ok != 0;
+}
+// A copy into this CTA's shared memory that completes on a barrier of either CTA of the pair.
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t cluster_bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(cluster_bar) : "memory");
 }
 
 template <int N>
@@ -594,11 +612,11 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t staging = ring + T::kStages * T::kStage, ctrl = staging + kEpi * T::kStaging;
     uint8_t *ctrl_gen = smem_raw + (ctrl - ring);
-    // barriers: full[s], empty[s] and (rank 0) the peer's full[s], s < 12; accumulators full, and (rank 0) empty
-    const uint32_t bar_full = ctrl, bar_empty = ctrl + 96, bar_peer = ctrl + 192, bar_tfull = ctrl + 288, bar_tempty = ctrl + 304;
-    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 320);
-    volatile int *abort_flag = reinterpret_cast<volatile int *>(ctrl_gen + 324);
-    const uint32_t rank = cluster_rank();
+    // barriers: (rank 0) full[s] of both, and empty[s], s < 12; accumulators full, and (rank 0) empty
+    const uint32_t bar_full = ctrl, bar_empty = ctrl + 96, bar_tfull = ctrl + 192, bar_tempty = ctrl + 208;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 224);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(ctrl_gen + 228);
+    const uint32_t rank = cluster_rank(), full0 = peer_address(bar_full, 0);
     const bool aligned = (ring & 1023u) == 0;
     if (warp == 1) {
         asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(const_cast<uint32_t *>(tmem_slot))), "r"(kTmemCols) : "memory");
@@ -606,7 +624,7 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     }
     if (threadIdx.x == 0) {
         prefetch_tensormap(&map_a); prefetch_tensormap(&map_x); prefetch_tensormap(&map_s);
-        for (int s = 0; s < T::kStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); mbar_init(bar_peer + 8 * s, 1); }
+        for (int s = 0; s < T::kStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
         for (int a = 0; a < T::kAcc; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, 2 * kEpi); }
         *abort_flag = aligned ? 0 : 1;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -622,9 +640,9 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const int pairs = (p.nrt + 1) >> 1, tile0 = (int)(blockIdx.x >> 1), tile_step = (int)(gridDim.x >> 1), len = p.kkeep;
 
     if (warp == 0) {
-        // -------------------------------------------------- this CTA's weights (an odd number of row tiles: the last one's once more), and its byte count
+        // -------------------------------------------------- this CTA's weights (an odd number of row tiles: the last one's once more), and (rank 0) both CTAs' byte count
         const bool leader = elect_one();
-        uint32_t dst = ring, full = bar_full, empty = bar_empty, ph = 0;
+        uint32_t dst = ring, full = full0, empty = bar_empty, ph = 0;
         int s = 0, fill = 0;
         bool ok = true;
         for (int t = tile0; t < p.num_tiles && ok; t += tile_step) {
@@ -632,13 +650,14 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             for (int e = 0; e < len; ++e) {
                 if (!wait_warp<true>(empty, ph ^ 1u, leader, abort_flag, p.wait_limit)) { ok = false; break; }
                 if (leader) {
-                    mbar_expect_tx(full, T::kBytes);
-                    if (fill != p.skip_fill) tma_load_2d(dst, &map_a, 0, row, full);
+                    // (the peer's bytes may come first: a phase ends with this arrival at the earliest, and the peer fills a stage anew when the one before has been multiplied)
+                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * T::kBytes);
+                    if (fill != p.skip_fill) tma_load_2d_pair(dst, &map_a, 0, row, full);
                 }
                 ++fill;
                 row += kEntry8 / 256;
                 dst += T::kStage; full += 8; empty += 8;
-                if (++s == T::kStages) { s = 0; dst = ring; full = bar_full; empty = bar_empty; ph ^= 1u; }
+                if (++s == T::kStages) { s = 0; dst = ring; full = full0; empty = bar_empty; ph ^= 1u; }
             }
         }
         wait_for_prerequisites();
@@ -646,7 +665,7 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         // -------------------------------------------------- this CTA's half of the columns, and the scales of all of them
         const bool leader = elect_one(), codes = warp == 2 + kEpi;
         const uint32_t at = codes ? T::kX : T::kS;
-        uint32_t dst = ring + at, full = bar_full, empty = bar_empty, ph = 0;
+        uint32_t dst = ring + at, full = full0, empty = bar_empty, ph = 0;
         int s = 0, fill = 0;
         bool ok = true;
         const int pitch = (int)(codes ? p.groups * 4 : p.chunks * 2);
@@ -656,29 +675,16 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             for (int e = 0; e < len; ++e) {
                 if (!wait_warp<false>(empty, ph ^ 1u, leader, abort_flag, p.wait_limit)) { ok = false; break; }
                 if (leader && fill != p.skip_fill) {
-                    if (codes) tma_load_2d(dst, &map_x, 0, row, full);
-                    else tma_load_2d(dst, &map_s, 0, row, full);
+                    if (codes) tma_load_2d_pair(dst, &map_x, 0, row, full);
+                    else tma_load_2d_pair(dst, &map_s, 0, row, full);
                 }
                 ++fill;
                 row += pitch;
                 dst += T::kStage; full += 8; empty += 8;
-                if (++s == T::kStages) { s = 0; dst = ring + at; full = bar_full; empty = bar_empty; ph ^= 1u; }
+                if (++s == T::kStages) { s = 0; dst = ring + at; full = full0; empty = bar_empty; ph ^= 1u; }
             }
         }
-    } else if (warp == 1 && rank == 1) {
-        // -------------------------------------------------- tells rank 0 which stages are here
-        const bool leader = elect_one();
-        const uint32_t there = peer_address(bar_peer, 0);
-        uint32_t ph = 0;
-        int s = 0;
-        bool ok = true;
-        for (int t = tile0; t < p.num_tiles && ok; t += tile_step)
-            for (int e = 0; e < len; ++e) {
-                if (!wait_warp<false>(bar_full + 8 * s, ph, leader, abort_flag, p.wait_limit)) { ok = false; break; }
-                if (leader) mbar_arrive_at(there + 8 * s);
-                if (++s == T::kStages) { s = 0; ph ^= 1u; }
-            }
-    } else if (warp == 1) {
+    } else if (warp == 1 && rank == 0) {
         // -------------------------------------------------- scales to tensor memory and MMAs, of both CTAs
         constexpr uint32_t idesc = (1u << 23) | ((uint32_t)(N >> 3) << 17) | (16u << 24);       // as make_idesc8, M = 256
         const bool leader = elect_one();
@@ -690,12 +696,12 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         for (int t = tile0; t < p.num_tiles; t += tile_step) {
             const uint32_t shift = (uint32_t)((int64_t)(t / pairs) * N & 127) >> 5;
             if (!wait_warp<false>(bar_tempty + 8 * acc, acc_ph ^ 1u, leader, abort_flag, p.wait_limit)) break;
+            (void)mbar_seen_cluster(bar_tempty + 8 * acc, acc_ph ^ 1u);
             tc_fence_after();
             const uint32_t d = tmem + acc * N;
             bool ok = true;
             for (int e = 0; e < len; ++e) {
-                if (!wait_warp<false>(bar_full + 8 * s, ph, leader, abort_flag, p.wait_limit) ||
-                    !wait_warp<false>(bar_peer + 8 * s, ph, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                if (!wait_warp<false>(bar_full + 8 * s, ph, leader, abort_flag, p.wait_limit)) { ok = false; break; }
                 tc_fence_after();
                 const uint32_t sa = scales + set * T::kScaleCols, sb = sa + 4;
                 if (leader) {
@@ -714,7 +720,7 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             if (leader) mma_commit_pair(bar_tfull + 8 * acc);
             if (++acc == T::kAcc) { acc = 0; acc_ph ^= 1u; }
         }
-    } else {
+    } else if (warp >= 2) {
         // -------------------------------------------------- drain: this CTA's row tile
         const int ew = warp - 2, q = warp & 3, part = ew >> 2;
         uint8_t *stage = smem_raw + (staging - ring) + ew * T::kStaging;
