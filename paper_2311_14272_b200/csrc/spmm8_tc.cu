@@ -547,10 +547,10 @@ spmm8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 // bytes a cycle (128 x N x 32: 4 KB + 32 N bytes; 98, 118, 160 and 191 cycles measured for 64, 128, 192 and 256 columns where the products need 32, 64, 96 and 128); a
 // pair reads half of the columns' bytes a CTA, and fetches half of them from L2.
 //
-// The CTA of rank 0 issues for both.  The copies of both complete on its barriers, which count the bytes of both (what has landed in the peer's shared memory is then
-// visible to the one who waits); commits go to both (multicast); accumulators are handed back by the draining warps of both, at the scope of the cluster: relaxed, as
-// what goes through tensor memory is ordered by the tcgen05 fences on either side, and nothing else is handed over.  (Released and acquired, a tile takes 0.35 us more;
-// stages announced one by one by a warp of the peer, released at that scope, 4096 x 4096 x 8192 188 us.)
+// The CTA of rank 0 issues for both.  The copies of both complete on its barriers, which count the bytes of both (what has landed in the peer's shared memory is acquired
+// at the scope of the cluster); commits go to both (multicast); accumulators are handed back by the draining warps of both.  These two are seen at the scope of the
+// cluster, relaxed: what tcgen05 instructions read and write is ordered by their commits and fences, and nothing else is handed over.  (Accumulators released and acquired, a
+// tile takes 0.35 us more; stages announced one by one by a warp of the peer, released at that scope, 4096 x 4096 x 8192 188 us.)
 template <int N>
 struct Pair8 {
     static constexpr int kChunks = N <= 128 ? 1 : 2;
@@ -584,15 +584,13 @@ __device__ __forceinline__ void mma_commit_pair(uint32_t bar) {          // to t
 __device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
     asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
 }
-// After a wait for such arrivals: the phase that has been seen complete, seen at the scope of the cluster.
-__device__ __forceinline__ bool mbar_seen_cluster(uint32_t bar, uint32_t parity) {
-    uint32_t ok;
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "mbarrier.test_wait.parity.relaxed.cluster.shared::cta.b64 p, [%1], %2;\n\t"
-        "selp.u32 %0, 1, 0, p;\n\t}"
-        : "=r"(ok) : "r"(bar), "r"(parity) : "memory");
-    return ok != 0;
+// After a wait at the CTA's scope: the phase that it has seen complete, seen at the scope of the cluster.
+template <bool kAcquire>
+__device__ __forceinline__ void mbar_seen_cluster(uint32_t bar, uint32_t parity) {
+    if constexpr (kAcquire)
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(bar), "r"(parity) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.relaxed.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(bar), "r"(parity) : "memory");
 }
 // A copy into this CTA's shared memory that completes on a barrier of either CTA of the pair.
 __device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t cluster_bar) {
@@ -649,6 +647,7 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             int row = min(2 * (t % pairs) + (int)rank, p.nrt - 1) * len * (int)(kEntry8 / 256);
             for (int e = 0; e < len; ++e) {
                 if (!wait_warp<true>(empty, ph ^ 1u, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                mbar_seen_cluster<false>(empty, ph ^ 1u);
                 if (leader) {
                     // (the peer's bytes may come first: a phase ends with this arrival at the earliest, and the peer fills a stage anew when the one before has been multiplied)
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * T::kBytes);
@@ -674,6 +673,7 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             int row = (int)(codes ? ((c0 >> 3) + rank * (N / 16)) * 4 : (c0 >> 7) * 2);
             for (int e = 0; e < len; ++e) {
                 if (!wait_warp<false>(empty, ph ^ 1u, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                mbar_seen_cluster<false>(empty, ph ^ 1u);
                 if (leader && fill != p.skip_fill) {
                     if (codes) tma_load_2d_pair(dst, &map_x, 0, row, full);
                     else tma_load_2d_pair(dst, &map_s, 0, row, full);
@@ -696,12 +696,13 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         for (int t = tile0; t < p.num_tiles; t += tile_step) {
             const uint32_t shift = (uint32_t)((int64_t)(t / pairs) * N & 127) >> 5;
             if (!wait_warp<false>(bar_tempty + 8 * acc, acc_ph ^ 1u, leader, abort_flag, p.wait_limit)) break;
-            (void)mbar_seen_cluster(bar_tempty + 8 * acc, acc_ph ^ 1u);
+            mbar_seen_cluster<false>(bar_tempty + 8 * acc, acc_ph ^ 1u);
             tc_fence_after();
             const uint32_t d = tmem + acc * N;
             bool ok = true;
             for (int e = 0; e < len; ++e) {
                 if (!wait_warp<false>(bar_full + 8 * s, ph, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                mbar_seen_cluster<true>(bar_full + 8 * s, ph);
                 tc_fence_after();
                 const uint32_t sa = scales + set * T::kScaleCols, sb = sa + 4;
                 if (leader) {
@@ -733,6 +734,7 @@ spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             if (lane == 0) go = !*abort_flag && mbar_wait(bar_tfull + 8 * acc, acc_ph, abort_flag, p.wait_limit);
             go = __shfl_sync(0xFFFFFFFFu, go, 0);
             if (!go) break;
+            mbar_seen_cluster<false>(bar_tfull + 8 * acc, acc_ph);
             tc_fence_after();
             const uint32_t from = tmem + acc * N + ((uint32_t)(32 * q) << 16);
             constexpr int kMine = N / 64;
