@@ -617,11 +617,13 @@ _AS_IT_IS = contextlib.nullcontext()
 
 
 def _allocating_for(stream):
-    """A context in which torch allocates memory for the stream of a call (None: the current one; a torch stream or an address)."""
+    """A context in which torch allocates memory for the stream of a call (None: the current one; a torch stream or an address, 0 for the default stream)."""
     if stream is None:
         return _AS_IT_IS
     import torch
-    return torch.cuda.stream(torch.cuda.ExternalStream(stream) if isinstance(stream, int) else stream)
+    if isinstance(stream, int):                          # (ExternalStream(0) would be a stream out of torch's pool)
+        stream = torch.cuda.ExternalStream(stream) if stream else torch.cuda.default_stream()
+    return torch.cuda.stream(stream)
 
 
 def _pitch(t) -> int:
