@@ -820,24 +820,27 @@ class HybridLayer:
             "weights are a bf16 CUDA matrix of the layer's shape with consecutive columns"
         assert w.device == self.device, "weights on another device than the layer"
         size = crisp_encode8_sizes(self.mask)
-        if self.buf8 is None or self.buf8.numel() < size:
-            self.buf8 = self.torch.empty(size, dtype=self.torch.uint8, device=self.device)
-        old, self.handle8 = self.handle8, 0
-        crisp_destroy8(old)
-        self._bias8 = None
         with self._on_device():
+            if self.buf8 is None or self.buf8.numel() < size:
+                with _allocating_for(stream):
+                    self.buf8 = self.torch.empty(size, dtype=self.torch.uint8, device=self.device)
+            old, self.handle8 = self.handle8, 0
+            crisp_destroy8(old)
+            self._bias8 = None
             self.handle8 = crisp_encode8(w, _pitch(w), self.mask, self.buf8, stream)
         return self
 
     def decode8(self, stream=None):
         """The dense bf16 weights that the 8-bit encoding stands for."""
         if self._gpu is not None and self._gpu == _current_device():
-            code, w = _network.decode8(self.handle8, self.desc.rows, self.desc.k, self._gpu, _stream(stream))
+            with _allocating_for(stream):
+                code, w = _network.decode8(self.handle8, self.desc.rows, self.desc.k, self._gpu, _stream(stream))
             if code:
                 raise CrispError(code, "crisp_decode8")
             return w
-        w = self.torch.empty_strided((self.desc.rows, self.desc.k), (self.desc.k, 1), dtype=self.torch.bfloat16, device=self.device)
         with self._on_device():
+            with _allocating_for(stream):
+                w = self.torch.empty_strided((self.desc.rows, self.desc.k), (self.desc.k, 1), dtype=self.torch.bfloat16, device=self.device)
             crisp_decode8(self.handle8, w, self.desc.k, stream)
         return w
 
@@ -872,12 +875,12 @@ class HybridLayer:
         assert not held or x.k == k, "activations of another k"
         shape = (ncols, rows) if tokens else (rows, ncols)
         dtype = torch.float32 if y_dtype else torch.bfloat16
-        if y is None:
-            y = torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=self.device)
-        else:
-            assert y.device == self.device and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1), \
-                "Y has the product's shape and type, and consecutive elements in a row"
+        assert y is None or (y.device == self.device and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1)), \
+            "Y has the product's shape and type, and consecutive elements in a row"
         with self._on_device():
+            if y is None:
+                with _allocating_for(stream):
+                    y = torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=self.device)
             if held:
                 crisp_spmm8_quantized(self.handle8, x.buffer, ncols, y, _pitch(y), int(tokens), y_dtype, stream)
                 return y
@@ -1253,19 +1256,17 @@ class AdamW:
         """(m, sqrt(v)) of 8-bit states as flat bf16 tensors, in which they are exact."""
         assert self.state_bits == 8, "32-bit states are their values"
         if _network and self.device.index == _current_device():
-            code, *out = _network.moments(self.m, self.m_exp, self.v, self.v_exp, _stream(stream))
+            with _allocating_for(stream):
+                code, *out = _network.moments(self.m, self.m_exp, self.v, self.v_exp, _stream(stream))
             if code:
                 raise CrispError(code, "crisp_adamw_moments")
             return out
         n = self.elements
-        both = self.torch.empty_strided((2, n), (n, 1), dtype=self.torch.bfloat16, device=self.device)
-        at = both.data_ptr()
-        args = (self.m.data_ptr(), self.m_exp.data_ptr(), self.v.data_ptr(), self.v_exp.data_ptr(), n, at, at + 2 * n)
-        if self.device.index == _current_device():
-            code = _lib.crisp_adamw_moments(*args, _stream(stream))
-        else:
-            with self.torch.cuda.device(self.device):
-                code = _lib.crisp_adamw_moments(*args, _stream(stream))
+        with self.torch.cuda.device(self.device):
+            with _allocating_for(stream):
+                both = self.torch.empty_strided((2, n), (n, 1), dtype=self.torch.bfloat16, device=self.device)
+            at = both.data_ptr()
+            code = _lib.crisp_adamw_moments(self.m.data_ptr(), self.m_exp.data_ptr(), self.v.data_ptr(), self.v_exp.data_ptr(), n, at, at + 2 * n, _stream(stream))
         if code:
             raise CrispError(code, "crisp_adamw_moments")
         return list(both.unbind(0))
