@@ -724,7 +724,7 @@ class HybridLayer:
         code, canonical_bytes, exec_bytes = _native.encode_sizes(self.mask)
         if code:
             raise CrispError(code, "crisp_encode_sizes")
-        self._reserve(canonical_bytes, exec_bytes)
+        self._reserve(canonical_bytes, exec_bytes, stream)
         old, self.handle = self.handle, 0
         code, self.handle = _native.encode(w.data_ptr(), strides[0], self.mask, self.canonical_buf.data_ptr(), self.exec_buf.data_ptr(),
                                            _stream(stream), old)
@@ -732,11 +732,13 @@ class HybridLayer:
             raise CrispError(code, "crisp_encode")
         return self
 
-    def _reserve(self, canonical_bytes, exec_bytes):
+    def _reserve(self, canonical_bytes, exec_bytes, stream=None):
         if self.canonical_buf is None or self.canonical_buf.numel() < canonical_bytes:
-            self.canonical_buf = self.torch.empty(canonical_bytes, dtype=self.torch.uint8, device=self.device)
+            with _allocating_for(stream):
+                self.canonical_buf = self.torch.empty(canonical_bytes, dtype=self.torch.uint8, device=self.device)
         if self.exec_buf is None or self.exec_buf.numel() < exec_bytes:
-            self.exec_buf = self.torch.empty(exec_bytes, dtype=self.torch.uint8, device=self.device)
+            with _allocating_for(stream):
+                self.exec_buf = self.torch.empty(exec_bytes, dtype=self.torch.uint8, device=self.device)
 
     def export(self, stream=None):
         import numpy as np
@@ -751,13 +753,16 @@ class HybridLayer:
     def decode(self, stream=None):
         desc, torch = self.desc, self.torch
         k = desc.k
+        if stream is not None:
+            with self._on_device(), _allocating_for(stream):
+                return self.decode()
         if self._gpu is not None:
-            code, w = _network.decode(self.handle, desc.rows, k, self._gpu, _stream(stream))
+            code, w = _network.decode(self.handle, desc.rows, k, self._gpu, _current_stream())
             if code:
                 raise CrispError(code, "crisp_decode")
             return w
         w = torch.empty_strided((desc.rows, k), (k, 1), dtype=torch.bfloat16, device=self.device)
-        code = _native.decode(self.handle, w.data_ptr(), k, _stream(stream))
+        code = _native.decode(self.handle, w.data_ptr(), k, _current_stream())
         if code:
             raise CrispError(code, "crisp_decode")
         return w
@@ -767,6 +772,9 @@ class HybridLayer:
         assert x.is_cuda and x.element_size() == 2 and strides[1] == 1 and shape[0] == self.desc.k
         ncols = shape[1]
         if y is None:
+            if stream is not None:
+                with self._on_device(), _allocating_for(stream):
+                    return self.spmm(x, None, y_dtype)
             y = self.torch.empty_strided((self.desc.rows, ncols), (ncols, 1), device=self.device,
                                          dtype=self.torch.float32 if y_dtype else self.torch.bfloat16)
         code = _native.spmm(self.handle, x.data_ptr(), strides[0], ncols, y.data_ptr(), y.stride()[0], y_dtype, _stream(stream))
@@ -782,7 +790,8 @@ class HybridLayer:
         if y is None:
             ho, wo = h + 2 * pad - kernel_h + 1, w + 2 * pad - kernel_w + 1
             dt = self.torch.float32 if y_dtype else self.torch.bfloat16
-            y = self.torch.empty((b, ho, wo, self.desc.rows) if nhwc_out else (self.desc.rows, b * ho * wo), dtype=dt, device=self.device)
+            with _allocating_for(stream):
+                y = self.torch.empty((b, ho, wo, self.desc.rows) if nhwc_out else (self.desc.rows, b * ho * wo), dtype=dt, device=self.device)
         ldy = y.stride()[2 if nhwc_out else 0]
         code = _native.spmm_conv(self.handle, act_nhwc.data_ptr(), b, h, w, c, kernel_h, kernel_w, pad, 1 if nhwc_out else 0,
                                  y.data_ptr(), ldy, y_dtype, _stream(stream))
@@ -832,16 +841,17 @@ class HybridLayer:
 
     def decode8(self, stream=None):
         """The dense bf16 weights that the 8-bit encoding stands for."""
+        if stream is not None:
+            with self._on_device(), _allocating_for(stream):
+                return self.decode8()
         if self._gpu is not None and self._gpu == _current_device():
-            with _allocating_for(stream):
-                code, w = _network.decode8(self.handle8, self.desc.rows, self.desc.k, self._gpu, _stream(stream))
+            code, w = _network.decode8(self.handle8, self.desc.rows, self.desc.k, self._gpu, _current_stream())
             if code:
                 raise CrispError(code, "crisp_decode8")
             return w
         with self._on_device():
-            with _allocating_for(stream):
-                w = self.torch.empty_strided((self.desc.rows, self.desc.k), (self.desc.k, 1), dtype=self.torch.bfloat16, device=self.device)
-            crisp_decode8(self.handle8, w, self.desc.k, stream)
+            w = self.torch.empty_strided((self.desc.rows, self.desc.k), (self.desc.k, 1), dtype=self.torch.bfloat16, device=self.device)
+            crisp_decode8(self.handle8, w, self.desc.k)
         return w
 
     def quantize8(self, x, tokens=False, stream=None):
@@ -1078,7 +1088,7 @@ class PruningNetwork:
                     have_c[i], have_e[i] = L.canonical_buf.numel(), L.exec_buf.numel()
                 old_masks[i], old_handles[i] = L.mask, L.handle
         # (a copy into pinned memory and a wait for the stream: 10 us less than a copy into pageable memory)
-        with torch.cuda.stream(stream):                      # (None: the current one)
+        with _allocating_for(stream):
             self._h_kkeep.copy_(self.d_kkeep, non_blocking=True)
             torch.cuda.current_stream(self.d_kkeep.device).synchronize()
         kk = self._h_kkeep.tolist()
@@ -1088,7 +1098,7 @@ class PruningNetwork:
         for i, (cb, eb) in enumerate(zip(canonical_bytes, exec_bytes)):
             if cb > have_c[i] or eb > have_e[i]:
                 P, L = arr[i], layers[i]
-                L._reserve(cb, eb)
+                L._reserve(cb, eb, stream)
                 P.d_canonical_buf, P.d_exec_buf = L.canonical_buf.data_ptr(), L.exec_buf.data_ptr()
         _check(_lib.crisp_prune_encode(count, arr, _stream(stream), masks, handles), "crisp_prune_encode")
         if _network:
@@ -1255,18 +1265,19 @@ class AdamW:
     def moments(self, stream=None):
         """(m, sqrt(v)) of 8-bit states as flat bf16 tensors, in which they are exact."""
         assert self.state_bits == 8, "32-bit states are their values"
+        if stream is not None:
+            with self.torch.cuda.device(self.device), _allocating_for(stream):
+                return self.moments()
         if _network and self.device.index == _current_device():
-            with _allocating_for(stream):
-                code, *out = _network.moments(self.m, self.m_exp, self.v, self.v_exp, _stream(stream))
+            code, *out = _network.moments(self.m, self.m_exp, self.v, self.v_exp, _current_stream())
             if code:
                 raise CrispError(code, "crisp_adamw_moments")
             return out
         n = self.elements
         with self.torch.cuda.device(self.device):
-            with _allocating_for(stream):
-                both = self.torch.empty_strided((2, n), (n, 1), dtype=self.torch.bfloat16, device=self.device)
+            both = self.torch.empty_strided((2, n), (n, 1), dtype=self.torch.bfloat16, device=self.device)
             at = both.data_ptr()
-            code = _lib.crisp_adamw_moments(self.m.data_ptr(), self.m_exp.data_ptr(), self.v.data_ptr(), self.v_exp.data_ptr(), n, at, at + 2 * n, _stream(stream))
+            code = _lib.crisp_adamw_moments(self.m.data_ptr(), self.m_exp.data_ptr(), self.v.data_ptr(), self.v_exp.data_ptr(), n, at, at + 2 * n, _current_stream())
         if code:
             raise CrispError(code, "crisp_adamw_moments")
         return list(both.unbind(0))

@@ -68,3 +68,53 @@ def test_8_bit_calls_do_not_write_what_the_current_stream_still_does(form, compi
         torch.cuda.synchronize()
     torch.cuda.synchronize()
     assert len(got) == len(want) and all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+@pytest.mark.parametrize("compiled", [True, False])
+@pytest.mark.parametrize("form", ["stream", "address"])
+def test_products_and_pruning_do_not_write_what_the_current_stream_still_does(form, compiled, monkeypatch):
+    """Encode, decode, products, convolutions and an iteration of pruning (which takes an address as the others do)."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    rows, k, ncols = 256, 576, 96
+    gen = torch.Generator("cuda").manual_seed(2)
+    w = torch.randn(rows, k, device="cuda", generator=gen).bfloat16()
+    x = torch.randn(k, ncols, device="cuda", generator=gen).bfloat16()
+    act = torch.randn(2, 8, 8, 64, device="cuda", generator=gen).bfloat16()
+    grads = [[torch.randn(rows, k, device="cuda", generator=gen)]]
+
+    def made():
+        return B.HybridLayer(rows, k, 2, 4, 64, 64, 0.5).build_mask(w.float().abs()), B.PruningNetwork([(rows, k)], 2, 4, 64, 64)
+    L, net = made()
+    L.encode(w)
+    want = [L.decode(), L.spmm(x), L.spmm(x, y_dtype=1), L.spmm_conv(act, 3, 3, 1), L.spmm_conv(act, 3, 3, 1, nhwc_out=True)]
+    kept = net.step([w], grads, 0.7)
+    want.append(net.layers[0].decode())
+    sizes = [L.canonical_buf.numel(), L.exec_buf.numel()]
+    L, net = made()
+    if not compiled:
+        monkeypatch.setattr(B, "_network", False)
+        L._gpu = net.layers[0]._gpu = None
+    side = torch.cuda.Stream()
+    stream = side if form == "stream" else side.cuda_stream
+    torch.cuda.synchronize()
+    for size in sizes:
+        spoil_later(torch, (size,), torch.uint8)
+    L.encode(w, stream=stream)
+    side.synchronize()
+    got = []
+    for call, shape, dtype in ((lambda: L.decode(stream=stream), (rows, k), torch.bfloat16),
+                               (lambda: L.spmm(x, stream=stream), (rows, ncols), torch.bfloat16),
+                               (lambda: L.spmm(x, y_dtype=1, stream=stream), (rows, ncols), torch.float32),
+                               (lambda: L.spmm_conv(act, 3, 3, 1, stream=stream), (rows, 128), torch.bfloat16),
+                               (lambda: L.spmm_conv(act, 3, 3, 1, stream=stream, nhwc_out=True), (2, 8, 8, rows), torch.bfloat16)):
+        spoil_later(torch, shape, dtype)
+        got.append(call())
+        side.synchronize()
+        assert not torch.cuda.current_stream().query()
+        torch.cuda.synchronize()
+    assert net.step([w], grads, 0.7, stream=stream) == kept
+    got.append(net.layers[0].decode(stream=stream))
+    torch.cuda.synchronize()
+    assert len(got) == len(want) and all(torch.equal(a, b) for a, b in zip(got, want))
+    net.close()
