@@ -617,7 +617,8 @@ _AS_IT_IS = contextlib.nullcontext()
 
 
 def _allocating_for(stream):
-    """A context in which torch allocates memory for the stream of a call (None: the current one; a torch stream or an address, 0 for the default stream)."""
+    """A context in which the stream of a call is the current one, so that torch allocates memory for it (None: the current one as it is; a torch stream or an
+    address, 0 for the default stream)."""
     if stream is None:
         return _AS_IT_IS
     import torch
@@ -1228,7 +1229,7 @@ class AdamW:
 
     def _launch(self, grads, stream):
         if self.capturable:                                  # (the step's own number, made before it and taken back if it is refused)
-            with self.torch.cuda.stream(stream):
+            with _allocating_for(stream):
                 self.d_step += 1
         try:
             code = None
@@ -1243,7 +1244,7 @@ class AdamW:
                 raise CrispError(code, "crisp_adamw")
         except Exception:
             if self.capturable:
-                with self.torch.cuda.stream(stream):
+                with _allocating_for(stream):
                     self.d_step -= 1
             raise
 

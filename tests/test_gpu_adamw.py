@@ -500,3 +500,25 @@ def test_scalars_that_are_not_finite_leave_pruned_weights_zero(which, value, bit
     for i, b in enumerate(bits_of):
         m, v = states(opt, i, b.size)
         assert not numbers(weights[i])[~b].any() and not m[~b].any() and not v[~b].any()
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_steps_that_count_on_the_device_on_any_stream(bits):
+    """A stream, its address, the default stream's address 0: the counter goes up before the step on the stream that the step is on."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    side = torch.cuda.Stream()
+    got = []
+    for streams in ((None, None, None), (side, side.cuda_stream, 0)):
+        w = torch.linspace(-1, 1, 640, device="cuda")
+        g = torch.linspace(1, 2, 640, device="cuda")
+        opt = B.AdamW([w], state_bits=bits, seed=2, capturable=True)
+        for stream in streams:
+            opt.step([g], stream=stream)
+            torch.cuda.synchronize()
+        with pytest.raises((AssertionError, B.CrispError)):
+            opt.step([g[:5]], stream=streams[1])
+        torch.cuda.synchronize()
+        assert int(opt.d_step) == 3
+        got.append((w, opt.m, opt.v))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
