@@ -1144,8 +1144,9 @@ class AdamW:
     state_bits 32, or 8 with a scale for each 128 elements.  The states of all tensors lie in the flat buffers m and v, each beginning at a multiple
               of 128 elements (`starts`): fp32 m and v, or uint8 codes of m and sqrt(v) with biased exponents in m_exp and v_exp (crisp.h).  They,
               `step_count` and `seed` are all there is to save.
-    capturable  the step number is kept in device memory (`d_step`, counted up by every step), and so may lr be (`d_lr`): a captured step
-              goes on counting when it is replayed.
+    capturable  the step number is kept in device memory (`d_step`, counted up by every step), and so is lr (`d_lr`): a captured step
+              goes on counting when it is replayed, and takes the lr that was assigned last.  Assigning `lr` writes d_lr on the current stream, and reading it
+              waits for the device.
     """
 
     def __init__(self, weights, copies=None, masks=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, seed=0, step=0,
@@ -1158,7 +1159,7 @@ class AdamW:
         self.masks = [None] * n if masks is None else list(masks)
         assert len(self.copies) == n and len(self.masks) == n, "a copy and a mask, or None, for each tensor"
         assert state_bits in (8, 32), "states are held in 8 bits or in 32"
-        self.lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
+        self._lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
         self.state_bits, self.seed, self.step_count = state_bits, seed, step
         self.device = self.weights[0].device if n else torch.device("cuda", torch.cuda.current_device())
         self._table = (AdamwTensor * n)()
@@ -1196,6 +1197,17 @@ class AdamW:
         if capturable:
             self._params.d_step, self._params.d_lr = self.d_step.data_ptr(), self.d_lr.data_ptr()
 
+    @property
+    def lr(self):
+        return float(self.d_lr) if self.capturable else self._lr
+
+    @lr.setter
+    def lr(self, value):
+        if self.capturable:
+            self.d_lr.fill_(value)
+        else:
+            self._lr = value
+
     def _place(self, T, w, c):
         """Where a tensor's weights and their copy lie."""
         torch, rows = self.torch, _rows_of(w)
@@ -1213,7 +1225,7 @@ class AdamW:
         grad_scale: an fp32 CUDA tensor of one element that the gradients are multiplied by (a clipping factor, say)."""
         assert len(grads) == len(self._table), "a gradient, or None, for each tensor"
         p = self._params
-        p.lr, (p.beta1, p.beta2), p.eps, p.weight_decay = self.lr, self.betas, self.eps, self.weight_decay
+        p.lr, (p.beta1, p.beta2), p.eps, p.weight_decay = self._lr, self.betas, self.eps, self.weight_decay
         p.step, p.seed = self.step_count + 1, self.seed
         if grad_scale is not None:
             assert grad_scale.is_cuda and grad_scale.device == self.device and grad_scale.dtype is self.torch.float32 and grad_scale.numel() == 1, \

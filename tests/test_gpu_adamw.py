@@ -522,3 +522,33 @@ def test_steps_that_count_on_the_device_on_any_stream(bits):
         assert int(opt.d_step) == 3
         got.append((w, opt.m, opt.v))
     assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_an_lr_that_is_assigned_is_the_next_steps(bits):
+    """As by a schedule, between steps and between replays of a captured one, where lr is kept on the device as where it is the host's."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    rates = [1e-2, 0.0, 3e-3, 1e-4]
+    got = []
+    for how in ("host", "device", "replayed"):
+        w = torch.linspace(-1, 1, 640, device="cuda")
+        g = torch.linspace(1, 2, 640, device="cuda")
+        opt = B.AdamW([w], state_bits=bits, seed=2, lr=rates[0], capturable=how != "host")
+        opt.step([g])
+        torch.cuda.synchronize()
+        if how == "replayed":
+            graph = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(graph):
+                opt.step([g])
+        for lr in rates[1:]:
+            before = w.clone()
+            opt.lr = lr
+            assert opt.lr == pytest.approx(lr, rel=2.0**-23, abs=0)
+            graph.replay() if how == "replayed" else opt.step([g])
+            assert torch.equal(w, before) == (lr == 0.0)
+        got.append((numbers(w), numbers(opt.m.float())))
+    # (lr and the corrections are numbers of fp32 on the device: at most eight roundings in each of four updates of at most 1.01 lr in all, and one of w each)
+    for w, m in got[1:]:
+        assert np.all(np.abs(w - got[0][0]) <= 8 * U * 1.01 * sum(rates) + 4 * U) and np.array_equal(m, got[0][1])
+    assert np.array_equal(got[1][0], got[2][0])
