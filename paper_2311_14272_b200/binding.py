@@ -1143,10 +1143,10 @@ class AdamW:
     masks     for each tensor None, or a HybridLayer of its shape (or a crisp_mask_t): weights without a bit in its mask become and stay 0
     state_bits 32, or 8 with a scale for each 128 elements.  The states of all tensors lie in the flat buffers m and v, each beginning at a multiple
               of 128 elements (`starts`): fp32 m and v, or uint8 codes of m and sqrt(v) with biased exponents in m_exp and v_exp (crisp.h).  They,
-              `step_count` and `seed` are all there is to save.
+              `step_count` and `seed` are all there is to save (and lr, where it is not the constructor's).
     capturable  the step number is kept in device memory (`d_step`, counted up by every step), and so is lr (`d_lr`): a captured step
-              goes on counting when it is replayed, and takes the lr that was assigned last.  Assigning `lr` writes d_lr on the current stream, and reading it
-              waits for the device.
+              goes on counting when it is replayed, and takes the lr that was assigned last.  Assigning `lr` and `step_count` writes d_lr and d_step on the
+              current stream, and reading them waits for the device.
     """
 
     def __init__(self, weights, copies=None, masks=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, seed=0, step=0,
@@ -1160,7 +1160,7 @@ class AdamW:
         assert len(self.copies) == n and len(self.masks) == n, "a copy and a mask, or None, for each tensor"
         assert state_bits in (8, 32), "states are held in 8 bits or in 32"
         self._lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
-        self.state_bits, self.seed, self.step_count = state_bits, seed, step
+        self.state_bits, self.seed, self._step_count = state_bits, seed, step
         self.device = self.weights[0].device if n else torch.device("cuda", torch.cuda.current_device())
         self._table = (AdamwTensor * n)()
         self._address = C.addressof(self._table)
@@ -1208,6 +1208,18 @@ class AdamW:
         else:
             self._lr = value
 
+    @property
+    def step_count(self):
+        """Steps made so far."""
+        return int(self.d_step) if self.capturable else self._step_count
+
+    @step_count.setter
+    def step_count(self, value):
+        if self.capturable:
+            self.d_step.fill_(value)
+        else:
+            self._step_count = value
+
     def _place(self, T, w, c):
         """Where a tensor's weights and their copy lie."""
         torch, rows = self.torch, _rows_of(w)
@@ -1226,7 +1238,7 @@ class AdamW:
         assert len(grads) == len(self._table), "a gradient, or None, for each tensor"
         p = self._params
         p.lr, (p.beta1, p.beta2), p.eps, p.weight_decay = self._lr, self.betas, self.eps, self.weight_decay
-        p.step, p.seed = self.step_count + 1, self.seed
+        p.step, p.seed = self._step_count + 1, self.seed     # (where it is kept on the device the first is not heeded)
         if grad_scale is not None:
             assert grad_scale.is_cuda and grad_scale.device == self.device and grad_scale.dtype is self.torch.float32 and grad_scale.numel() == 1, \
                 "grad_scale is an fp32 CUDA tensor of one element"
@@ -1236,7 +1248,8 @@ class AdamW:
         else:
             with self.torch.cuda.device(self.device):
                 self._launch(grads, stream)
-        self.step_count += 1
+        if not self.capturable:
+            self._step_count += 1
         return self
 
     def _launch(self, grads, stream):

@@ -552,3 +552,35 @@ def test_an_lr_that_is_assigned_is_the_next_steps(bits):
     for w, m in got[1:]:
         assert np.all(np.abs(w - got[0][0]) <= 8 * U * 1.01 * sum(rates) + 4 * U) and np.array_equal(m, got[0][1])
     assert np.array_equal(got[1][0], got[2][0])
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+@pytest.mark.parametrize("again", [False, True])
+def test_what_is_saved_after_replays_goes_on_as_they_would(bits, again):
+    """m, v, their exponents, the step count and the seed are all of an optimizer's state, also where replays of a captured step have counted."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    w = torch.linspace(-1, 1, 640, device="cuda").bfloat16()
+    g = torch.linspace(1, 2, 640, device="cuda")
+    opt = B.AdamW([w], state_bits=bits, seed=2, step=3, capturable=True)
+    assert opt.step_count == 3
+    opt.step([g])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        opt.step([g])
+    for _ in range(5):
+        graph.replay()
+    assert opt.step_count == 9 == int(opt.d_step)
+    held = w.clone()
+    other = B.AdamW([held], state_bits=bits, seed=opt.seed, capturable=True, step=opt.step_count if not again else 0)
+    if again:
+        other.step_count = opt.step_count
+    for name in ("m", "v", "m_exp", "v_exp"):
+        if getattr(opt, name) is not None:
+            getattr(other, name).copy_(getattr(opt, name))
+    graph.replay()
+    other.step([g])
+    torch.cuda.synchronize()
+    assert other.step_count == opt.step_count == 10
+    assert torch.equal(w, held) and torch.equal(opt.m, other.m) and torch.equal(opt.v, other.v)
