@@ -1225,7 +1225,7 @@ class AdamW:
         torch, rows = self.torch, _rows_of(w)
         assert w.is_cuda and w.device == self.device and rows and rows[:2] == (T.rows, T.k) and w.dtype == (torch.float32 if T.w_dtype else torch.bfloat16), \
             "weights are CUDA tensors of one device and keep their shape and type"
-        T.d_w, T.ld_w = w.data_ptr(), rows[2]
+        T.d_w, T.ld_w, T.d_copy_bf16, T.ld_copy = w.data_ptr(), rows[2], None, 0
         if c is not None:
             rows = _rows_of(c)
             assert c.is_cuda and c.device == self.device and c.dtype == torch.bfloat16 and T.w_dtype and c.shape == w.shape and rows, \

@@ -239,6 +239,7 @@ PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n) {
             rows[1] != T.k)
             Py_RETURN_NONE;
         T.d_w = w.data_ptr(); T.ld_w = rows[2];
+        T.d_copy_bf16 = nullptr; T.ld_copy = 0;              // (the table is kept from step to step, and a copy may have been given up)
         if (co != Py_None) {
             const at::Tensor &c = THPVariable_Unpack(co);
             if (!c.is_cuda() || c.layout() != at::kStrided || c.device() != w.device() || c.scalar_type() != at::kBFloat16 || !c.sizes().equals(w.sizes()) ||

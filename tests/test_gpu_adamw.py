@@ -584,3 +584,21 @@ def test_what_is_saved_after_replays_goes_on_as_they_would(bits, again):
     torch.cuda.synchronize()
     assert other.step_count == opt.step_count == 10
     assert torch.equal(w, held) and torch.equal(opt.m, other.m) and torch.equal(opt.v, other.v)
+
+
+@pytest.mark.parametrize("kind", [list, tuple])
+def test_a_copy_that_was_given_up_is_not_written(kind):
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    w = [torch.ones(8, 16, device="cuda") for _ in range(2)]
+    copies = [torch.zeros(8, 16, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    g = kind(torch.ones(8, 16, device="cuda") for _ in range(2))
+    opt = B.AdamW(w, copies=copies)
+    opt.step(g)
+    opt.copies[0] = None
+    held = copies[0].clone()
+    opt.step(g)
+    assert torch.equal(copies[0], held) and not torch.equal(copies[0], w[0].bfloat16()) and torch.equal(copies[1], w[1].bfloat16())
+    opt.copies[0] = copies[0]
+    opt.step(g)
+    assert all(torch.equal(c, x.bfloat16()) for c, x in zip(copies, w))
