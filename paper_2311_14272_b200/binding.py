@@ -883,7 +883,7 @@ class HybridLayer:
                 return done[1]
         held = isinstance(x, Activations8)
         ncols = x.ncols if held else self._columns8(x, tokens)
-        assert not held or x.k == k, "activations of another k"
+        assert not held or (x.k == k and x.buffer.device == self.device), "activations of another k or on another device"
         shape = (ncols, rows) if tokens else (rows, ncols)
         dtype = torch.float32 if y_dtype else torch.bfloat16
         assert y is None or (y.device == self.device and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1)), \
