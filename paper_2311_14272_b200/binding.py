@@ -803,7 +803,8 @@ class HybridLayer:
     def set_epilogue(self, bias=None, relu=False):
         """Y = act(W X + bias) for later products; `bias` is an fp32 CUDA tensor [rows] that this object keeps."""
         if bias is not None:
-            assert bias.is_cuda and bias.dtype == self.torch.float32 and bias.numel() == self.desc.rows
+            assert bias.device == self.device and bias.dtype == self.torch.float32 and bias.numel() == self.desc.rows and bias.is_contiguous(), \
+                "a bias is an fp32 tensor of as many consecutive elements as the layer has rows, on its device"
         self._bias = bias
         crisp_set_epilogue(self.handle, bias, 1 if relu else 0)
         return self
@@ -903,7 +904,8 @@ class HybridLayer:
     def set_epilogue8(self, bias=None, relu=False):
         """Y = act(W X + bias) for later 8-bit products; `bias` is an fp32 CUDA tensor [rows] that this object keeps."""
         if bias is not None:
-            assert bias.is_cuda and bias.dtype == self.torch.float32 and bias.numel() == self.desc.rows and bias.is_contiguous()
+            assert bias.device == self.device and bias.dtype == self.torch.float32 and bias.numel() == self.desc.rows and bias.is_contiguous(), \
+                "a bias is an fp32 tensor of as many consecutive elements as the layer has rows, on its device"
         self._bias8 = bias
         crisp_set_epilogue8(self.handle8, bias, 1 if relu else 0)
         return self

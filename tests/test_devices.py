@@ -31,3 +31,17 @@ def test_activations_that_were_quantised_on_another_device(layer):
         layer.spmm8(B.Activations8(64, 8, SimpleNamespace(device=HERE)), y)
     assert not layer.called
     assert layer.spmm8(B.Activations8(128, 8, SimpleNamespace(device=HERE)), y) is y and layer.called == ["crisp_spmm8_quantized"]
+
+
+@pytest.mark.parametrize("call,kept", [("set_epilogue8", "_bias8"), ("set_epilogue", "_bias")])
+def test_a_bias_on_another_device(layer, call, kept):
+    def bias(device, **other):
+        return SimpleNamespace(**{**dict(device=device, is_cuda=True, dtype=torch.float32, numel=lambda: 256, is_contiguous=lambda: True), **other})
+    for bad in (bias(ELSEWHERE), bias(HERE, dtype=torch.bfloat16), bias(HERE, numel=lambda: 255), bias(HERE, is_contiguous=lambda: False)):
+        with pytest.raises(AssertionError):
+            getattr(layer, call)(bad)
+    assert not layer.called and getattr(layer, kept) is None
+    good = bias(HERE)
+    assert getattr(layer, call)(good) is layer and getattr(layer, kept) is good and len(layer.called) == 1
+    getattr(layer, call)(None, relu=True)
+    assert getattr(layer, kept) is None and len(layer.called) == 2
