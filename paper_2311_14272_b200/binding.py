@@ -1261,7 +1261,8 @@ class AdamW:
         try:
             code = None
             if _network and type(grads) is list:
-                code = _network.adamw(self._address, self.weights, self.copies, grads, self.masks, C.addressof(self._params), _stream(stream))
+                code = _network.adamw(self._address, self.weights, self.copies, grads, self.masks, C.addressof(self._params), _stream(stream),
+                                      self.device.index)
             if code is None:
                 self._gradients(grads)
                 self.torch.autograd.graph.increment_version([t for ts, g in zip(zip(self.weights, self.copies), grads) for t in ts

@@ -214,15 +214,16 @@ bool rows_of(const at::Tensor &t, int64_t (&v)[3]) {
     return true;
 }
 
-// adamw(array of crisp_adamw_tensor_t, weights, copies, gradients, masks, crisp_adamw_t, stream) -> status: where the tensors of a step lie, and its masks, and the step;
+// adamw(array of crisp_adamw_tensor_t, weights, copies, gradients, masks, crisp_adamw_t, stream, GPU) -> status: where the tensors of a step lie, and its masks, and the step;
 // or None: not a step that this takes, and nothing done.  The four are lists of one length; an entry of `copies` and `gradients` may be None, one of `masks` a layer or None.  (The shapes and types of weights and copies
 // are those that the array was made for, or it is not filled in.)
 PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n) {
     HANDLE_TH_ERRORS
-    if (!arguments("adamw", n, 7)) return nullptr;
+    if (!arguments("adamw", n, 8)) return nullptr;
     crisp_adamw_tensor_t *arr = address<crisp_adamw_tensor_t>(args[0]);
     const crisp_adamw_t *params = address<const crisp_adamw_t>(args[5]);
     void *stream = PyLong_AsVoidPtr(args[6]);
+    const long gpu = PyLong_AsLong(args[7]);                 // of the states: all else has to lie there
     if (PyErr_Occurred()) return nullptr;
     if (!arr || !params) Py_RETURN_NONE;
     for (int i = 1; i < 5; ++i)
@@ -235,7 +236,7 @@ PyObject *adamw(PyObject *, PyObject *const *args, Py_ssize_t n) {
         if (!THPVariable_CheckExact(go) || !THPVariable_Check(wo) || (co != Py_None && !THPVariable_Check(co))) Py_RETURN_NONE;
         const at::Tensor &g = THPVariable_Unpack(go), &w = THPVariable_Unpack(wo);
         int64_t rows[3];
-        if (!w.is_cuda() || w.layout() != at::kStrided || w.scalar_type() != (T.w_dtype ? at::kFloat : at::kBFloat16) || !rows_of(w, rows) || rows[0] != T.rows ||
+        if (!w.is_cuda() || w.get_device() != gpu || w.layout() != at::kStrided || w.scalar_type() != (T.w_dtype ? at::kFloat : at::kBFloat16) || !rows_of(w, rows) || rows[0] != T.rows ||
             rows[1] != T.k)
             Py_RETURN_NONE;
         T.d_w = w.data_ptr(); T.ld_w = rows[2];

@@ -602,3 +602,21 @@ def test_a_copy_that_was_given_up_is_not_written(kind):
     opt.copies[0] = copies[0]
     opt.step(g)
     assert all(torch.equal(c, x.bfloat16()) for c, x in zip(copies, w))
+
+
+def test_weights_that_have_moved_to_another_device_are_refused(monkeypatch):
+    """The states stay where they were made.  (One device is enough to see it: the states' device is said to be another.)"""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    for kind in (list, tuple):
+        w = torch.ones(8, 16, device="cuda")
+        opt = B.AdamW([w])
+        opt.step([torch.ones(8, 16, device="cuda")])
+        held = w.clone(), opt.m.clone()
+        opt.device = torch.device("cuda", 1)
+        monkeypatch.setattr(B, "_current_device", lambda: 1)
+        with pytest.raises(AssertionError):
+            opt.step(kind([torch.ones(8, 16, device="cuda")]))
+        monkeypatch.undo()
+        torch.cuda.synchronize()
+        assert torch.equal(w, held[0]) and torch.equal(opt.m, held[1]) and opt.step_count == 1
