@@ -1164,6 +1164,7 @@ class AdamW:
         self._lr, self.betas, self.eps, self.weight_decay = lr, betas, eps, weight_decay
         self.state_bits, self.seed, self._step_count = state_bits, seed, step
         self.device = self.weights[0].device if n else torch.device("cuda", torch.cuda.current_device())
+        assert all(getattr(mask, "device", self.device) == self.device for mask in self.masks), "a layer and the weights under its mask lie on one device"
         self._table = (AdamwTensor * n)()
         self._address = C.addressof(self._table)
         self.starts, at = [], 0
@@ -1288,6 +1289,7 @@ class AdamW:
                 "a gradient is a bf16 or fp32 CUDA tensor of its weights' shape"
             rows = _rows_of(g)
             assert rows, "a gradient lies in rows of consecutive elements"
+            assert getattr(mask, "device", self.device) == self.device, "a layer and the weights under its mask lie on one device"
             T.d_grad, T.grad_dtype, T.ld_grad = g.data_ptr(), int(g.dtype == torch.float32), rows[2]
             T.mask = getattr(mask, "mask", mask) or None
 

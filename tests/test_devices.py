@@ -45,3 +45,10 @@ def test_a_bias_on_another_device(layer, call, kept):
     assert getattr(layer, call)(good) is layer and getattr(layer, kept) is good and len(layer.called) == 1
     getattr(layer, call)(None, relu=True)
     assert getattr(layer, kept) is None and len(layer.called) == 2
+
+
+def test_masks_on_another_device_than_their_weights():
+    w = SimpleNamespace(device=HERE, dtype=torch.float32)
+    mask = SimpleNamespace(device=ELSEWHERE, mask=4096)
+    with pytest.raises(AssertionError, match="one device"):
+        B.AdamW([w, w], masks=[None, mask])
