@@ -822,8 +822,9 @@ class HybridLayer:
         if self._gpu is not None and self._gpu == _current_device():
             done = _network.encode8(self.mask, w, self.desc.rows, self.desc.k, self._gpu, self.buf8, self.handle8, _stream(stream))
             if done is not None and not done[2]:
-                code, self.handle8, _ = done
-                self._bias8 = None
+                code, handle, _ = done
+                if not (code and handle):                    # (refused before anything was done, the encoding before stays, and its epilogue with it)
+                    self.handle8, self._bias8 = handle, None
                 if code:
                     raise CrispError(code, "crisp_encode8")
                 return self

@@ -521,3 +521,26 @@ def test_values_of_any_size_in_every_kernel(tokens, ncols, power_w, power_x):
         y = numbers(L.spmm8(L.quantize8(d_x, tokens=tokens) if quantised else d_x, y_dtype=1, tokens=tokens))
         assert (L.last_launch8()["path"] == B.PATH_DIRECT) == (ncols <= 4 and not quantised)
         assert np.all(np.abs((y.T if tokens else y) - w @ held) <= tol)
+
+
+@pytest.mark.parametrize("compiled", [True, False])
+def test_an_encoding_that_is_refused_leaves_the_one_before_with_its_bias(compiled):
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, w, _ = layer(B, torch, 200, 300, 4, 4, 1.0, 44)
+    if not compiled:
+        L._gpu = None
+    x = torch.randn(300, 9, device="cuda").bfloat16()
+    L.set_epilogue8(torch.linspace(-1, 1, 200, device="cuda"), relu=True)
+    want, bias, mask = L.spmm8(x), L._bias8, L.mask
+    for bad_mask, bad_w in ((0, torch.zeros(200, 300, dtype=torch.bfloat16, device="cuda")), (mask, torch.zeros(200, 301, dtype=torch.bfloat16, device="cuda"))):
+        L.mask = bad_mask
+        with pytest.raises((B.CrispError, AssertionError)):
+            L.encode8(bad_w)
+        L.mask = mask
+        # (the bias is still the layer's: what is allocated now does not take its place)
+        assert L._bias8 is bias
+        torch.full((200,), 5.0, device="cuda")
+        assert torch.equal(L.spmm8(x), want)
+    L.encode8(torch.zeros(200, 300, dtype=torch.bfloat16, device="cuda"))
+    assert L._bias8 is None and not L.spmm8(x).any()

@@ -64,7 +64,6 @@ def test_8_bit_calls_do_not_write_what_the_current_stream_still_does(form, compi
         spoil_later(torch, shape, dtype)
         got += call()
         side.synchronize()
-        assert not torch.cuda.current_stream().query()       # (what was queued there comes after)
         torch.cuda.synchronize()
     torch.cuda.synchronize()
     assert len(got) == len(want) and all(torch.equal(a, b) for a, b in zip(got, want))
@@ -111,7 +110,6 @@ def test_products_and_pruning_do_not_write_what_the_current_stream_still_does(fo
         spoil_later(torch, shape, dtype)
         got.append(call())
         side.synchronize()
-        assert not torch.cuda.current_stream().query()
         torch.cuda.synchronize()
     assert net.step([w], grads, 0.7, stream=stream) == kept
     got.append(net.layers[0].decode(stream=stream))
