@@ -1138,6 +1138,15 @@ def _rows_of(t):
     return None
 
 
+def _kept_buffer(name):
+    """A buffer whose address the table of a step holds: what is assigned to it is copied into it."""
+    def take(self, value):
+        buffer = getattr(self, name)
+        assert buffer is not None and value.shape == buffer.shape and value.dtype == buffer.dtype, "a state keeps its size and type"
+        buffer.copy_(value)
+    return property(lambda self: getattr(self, name), take)
+
+
 class AdamW:
     """AdamW over many tensors in one call (crisp_adamw): the fine-tuning that follows a pruning step.
 
@@ -1147,10 +1156,13 @@ class AdamW:
     state_bits 32, or 8 with a scale for each 128 elements.  The states of all tensors lie in the flat buffers m and v, each beginning at a multiple
               of 128 elements (`starts`): fp32 m and v, or uint8 codes of m and sqrt(v) with biased exponents in m_exp and v_exp (crisp.h).  They,
               `step_count` and `seed` are all there is to save (and lr, where it is not the constructor's).
+              They stay where they are: what is assigned to one is copied into it.
     capturable  the step number is kept in device memory (`d_step`, counted up by every step), and so is lr (`d_lr`): a captured step
               goes on counting when it is replayed, and takes the lr that was assigned last.  Assigning `lr` and `step_count` writes d_lr and d_step on the
               current stream, and reading them waits for the device.
     """
+
+    m, v, m_exp, v_exp, d_step, d_lr = (_kept_buffer(name) for name in ("_m", "_v", "_m_exp", "_v_exp", "_d_step", "_d_lr"))
 
     def __init__(self, weights, copies=None, masks=None, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=1e-2, state_bits=32, seed=0, step=0,
                  capturable=False):
@@ -1175,8 +1187,8 @@ class AdamW:
         self.elements = at
         wide = state_bits == 32
         state = lambda count, dtype: torch.zeros(count, dtype=dtype, device=self.device)  # noqa: E731
-        self.m, self.v = [state(at, torch.float32 if wide else torch.uint8) for _ in range(2)]
-        self.m_exp, self.v_exp = [None if wide else state(at // 128, torch.uint8) for _ in range(2)]
+        self._m, self._v = [state(at, torch.float32 if wide else torch.uint8) for _ in range(2)]
+        self._m_exp, self._v_exp = [None if wide else state(at // 128, torch.uint8) for _ in range(2)]
         spans = []
         for i, (T, w, c) in enumerate(zip(self._table, self.weights, self.copies)):
             rows = _rows_of(w)
@@ -1196,8 +1208,8 @@ class AdamW:
             _bind_network()
         self._params = AdamwParams(state_bits=state_bits)
         self.capturable = capturable
-        self.d_step = torch.full((1,), step, dtype=torch.int64, device=self.device) if capturable else None
-        self.d_lr = torch.full((1,), lr, dtype=torch.float32, device=self.device) if capturable else None
+        self._d_step = torch.full((1,), step, dtype=torch.int64, device=self.device) if capturable else None
+        self._d_lr = torch.full((1,), lr, dtype=torch.float32, device=self.device) if capturable else None
         if capturable:
             self._params.d_step, self._params.d_lr = self.d_step.data_ptr(), self.d_lr.data_ptr()
 

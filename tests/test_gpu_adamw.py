@@ -620,3 +620,29 @@ def test_weights_that_have_moved_to_another_device_are_refused(monkeypatch):
         monkeypatch.undo()
         torch.cuda.synchronize()
         assert torch.equal(w, held[0]) and torch.equal(opt.m, held[1]) and opt.step_count == 1
+
+
+@pytest.mark.parametrize("bits", [8, 32])
+def test_states_that_are_assigned_are_the_next_steps(bits):
+    """As a checkpoint is read: the table of a step holds the buffers' addresses, so what is assigned goes into them."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    g = torch.linspace(1, 2, 640, device="cuda")
+    first = B.AdamW([torch.linspace(-1, 1, 640, device="cuda")], state_bits=bits, seed=2, capturable=True, lr=1e-2)
+    first.step([g])
+    names = ["m", "v", "d_step", "d_lr"] + (["m_exp", "v_exp"] if bits == 8 else [])
+    saved = {name: getattr(first, name).clone() for name in names}
+    second = B.AdamW([first.weights[0].clone()], state_bits=bits, seed=2, capturable=True)
+    for name in names:
+        where = getattr(second, name).data_ptr()
+        setattr(second, name, saved[name])
+        assert getattr(second, name).data_ptr() == where and torch.equal(getattr(second, name), saved[name])
+    for opt in (first, second):
+        opt.step([g])
+    assert torch.equal(first.weights[0], second.weights[0]) and all(torch.equal(getattr(first, name), getattr(second, name)) for name in names)
+    for bad in (saved["m"][:-1], saved["m"].double()):
+        with pytest.raises(AssertionError):
+            second.m = bad
+    if bits == 32:
+        with pytest.raises(AssertionError):
+            second.m_exp = saved["m"]
