@@ -375,7 +375,7 @@ typedef struct {
 CRISP_API crisp_status_t crisp_adamw(int32_t n, const crisp_adamw_tensor_t *tensors, const crisp_adamw_t *params, void *stream);
 
 /* What 8-bit states stand for: d_m_bf16[e] = m and d_root_bf16[e] = sqrt(v) of `count` elements of one tensor, or of several whose states lie one
- * behind the other in whole blocks of 128 (both are exact in bf16).  d_m, d_v 16-byte aligned. */
+ * behind the other in whole blocks of 128 (both are exact in bf16, but for an m below 2^-126, which is rounded).  d_m, d_v 16-byte aligned. */
 CRISP_API crisp_status_t crisp_adamw_moments(const uint8_t *d_m, const uint8_t *d_m_exp, const uint8_t *d_v, const uint8_t *d_v_exp,
                                              int64_t count, uint16_t *d_m_bf16, uint16_t *d_root_bf16, void *stream);
 

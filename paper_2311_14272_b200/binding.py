@@ -1307,7 +1307,7 @@ class AdamW:
             T.mask = getattr(mask, "mask", mask) or None
 
     def moments(self, stream=None):
-        """(m, sqrt(v)) of 8-bit states as flat bf16 tensors, in which they are exact."""
+        """(m, sqrt(v)) of 8-bit states as flat bf16 tensors, in which they are exact (but for an m below 2^-126)."""
         assert self.state_bits == 8, "32-bit states are their values"
         if stream is not None:
             with self.torch.cuda.device(self.device), _allocating_for(stream):

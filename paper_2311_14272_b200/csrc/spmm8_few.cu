@@ -7,7 +7,7 @@
 // once.  Meanwhile the CTA quantises X into shared memory, block by block (its codes as fp32, and the scales).  Codes are multiplied in fp32: products of two codes are
 // exact, a block's sum is scaled once, and the sums of lanes and warps are added in a fixed order.
 // Not kept: mma.sync on fp16 codes, 16 rows a CTA.  The quantisation of X in every CTA is what is left then: 4096 x 4096 with half of its blocks, 4 tokens 5.3 instead of 6.5 us, but
-// 2048 x 8192 1 token 9.5 instead of 8.0, 512 x 4608 3.0 instead of 2.5.
+// 2048 x 8192 1 token 9.5 instead of 8.0, 512 x 4608 with a quarter 3.0 instead of 2.5 (2.3 since a block's scales are made once a column).
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -179,8 +179,9 @@ cudaError_t launch(const FewParams &p, unsigned ctas, int device, cudaStream_t s
 }  // namespace
 
 // Up to four columns whose codes fit in shared memory, and products of no more than 12 million weights times columns: beyond, the multiply-adds take longer than the
-// chain through tensor memory.  In a row, us here and there: 300 x 500 1 column 2.3 and 4.7, 4 columns 2.3 and 5.2; 1024 x 4096 3.5 and 5.9, 2 columns 4.4 and 6.0,
-// 4 columns 7.6 and 6.3; 4096 x 4096 7.5 and 7.7, 4 columns 20 and 7.8.
+// chain through tensor memory.  In a row, us here and there: 300 x 500 1 column 2.2 and 4.7, 4 columns 2.4 and 5.0; 1024 x 4096 3.2 and 6.0, 2 columns 4.5 and 6.0,
+// 4 columns 7.5 and 6.4; 4096 x 4096 with half of its blocks 3.9 and 6.2, 4 columns 11.9 and 6.5.  (One column alone crosses later: 4096 x 4096 5.9 and 7.0, 2048 x 8192 6.9 and
+// 7.4.  The line was drawn when these took 7.5 and 8.0 here.)
 bool few8(const Geometry &g, int64_t ncols) {
     return ncols <= 4 && g.kkeep > 0 && (int64_t)g.kkeep * ncols * 513 <= kFewBytes && (int64_t)g.rows * g.kkeep * 128 * ncols <= 12000000;
 }
