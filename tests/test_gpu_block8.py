@@ -544,3 +544,68 @@ def test_an_encoding_that_is_refused_leaves_the_one_before_with_its_bias(compile
         assert torch.equal(L.spmm8(x), want)
     L.encode8(torch.zeros(200, 300, dtype=torch.bfloat16, device="cuda"))
     assert L._bias8 is None and not L.spmm8(x).any()
+
+
+@pytest.mark.parametrize("keep", [1.0, 0.5])
+def test_offsets_beyond_32_bits(keep):
+    """Activations, then weights, of more than 2^32 elements: their last ones give the bits that they give alone."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    if torch.cuda.mem_get_info()[0] < 80e9:
+        pytest.skip("needs 60 GB")
+    k, n = 4096, 2**20 + 50_003
+    L = B.HybridLayer(130, k, 4, 4, 128, 128, keep).build_mask(torch.rand(130, k, device="cuda"))
+    L.encode8(torch.randn(130, k, device="cuda").bfloat16())
+    L.set_tuning8(tile_cols=256, split=1)
+    x = torch.zeros(n, k, dtype=torch.bfloat16, device="cuda")
+    x[-1000:].normal_()
+    want = L.spmm8(x[-1000:].clone(), tokens=True)
+    for split in (1, -1) if keep == 1.0 else (1,):
+        L.set_tuning8(tile_cols=256, split=split)
+        y = L.spmm8(x, tokens=True)
+        assert L.device_status8() == 0 and torch.equal(y[-1000:], want) and not y[:-1000].any()
+    x = x.t().contiguous()
+    y = L.spmm8(x)
+    assert torch.equal(y[:, -1000:].t(), want) and not y[:, :-1000].any()
+    del x, y
+    score = torch.rand(n, k, device="cuda")
+    w = torch.empty(n, k, dtype=torch.bfloat16, device="cuda").normal_()
+    L = B.HybridLayer(n, k, 2, 4, 128, 128, keep).build_mask(score).encode8(w)
+    at = (n - 1000) // 128 * 128
+    last = B.HybridLayer(n - at, k, 2, 4, 128, 128, keep).build_mask(score[at:].clone()).encode8(w[at:].clone())
+    assert torch.equal(L.decode8()[at:], last.decode8())
+    for ncols in (3, 40):
+        x = torch.randn(ncols, k, device="cuda").bfloat16()
+        for one in (L, last):
+            one.set_tuning8(tile_cols=64, split=1)
+        assert torch.equal(L.spmm8(x, tokens=True)[:, at:], last.spmm8(x, tokens=True)) and L.device_status8() == 0
+    del L, last, score, w
+    torch.cuda.empty_cache()
+
+
+def test_pairs_of_sms_on_two_streams_and_in_graphs_at_once():
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, _, _ = layer(B, torch, 700, 1024, 4, 4, 1.0, 45)
+    rng = np.random.default_rng(46)
+    xs = [bf16_dev(activations(rng, 1024, n), torch) for n in (3000, 2001)]
+    L.set_tuning8(tile_cols=256, split=-1)
+    want = [L.spmm8(x) for x in xs]
+    assert L.last_launch8()["stack"] == -1
+    torch.cuda.synchronize()
+    streams, graphs, made = [torch.cuda.Stream() for _ in xs], [], []
+    for x in xs:
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            made.append([L.spmm8(x) for _ in range(3)])
+        graphs.append(graph)
+    got = []
+    for _ in range(20):
+        for x, stream, graph in zip(xs, streams, graphs):
+            with torch.cuda.stream(stream):
+                graph.replay()
+                got.append(L.spmm8(x))
+    torch.cuda.synchronize()
+    assert L.device_status8() == 0
+    assert all(torch.equal(y, want[i % 2]) for i, y in enumerate(got))
+    assert all(torch.equal(y, w) for ys, w in zip(made, want) for y in ys)
