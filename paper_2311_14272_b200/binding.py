@@ -8,6 +8,7 @@ from __future__ import annotations
 
 import contextlib
 import ctypes as C
+import operator
 import os
 import re
 import sys
@@ -883,17 +884,20 @@ class HybridLayer:
                 if done[0]:
                     raise CrispError(done[0], "crisp_spmm8")
                 return done[1]
+        if y is None and stream is not None:
+            with self._on_device(), _allocating_for(stream):
+                return self.spmm8(x, None, y_dtype, tokens)
         held = isinstance(x, Activations8)
         ncols = x.ncols if held else self._columns8(x, tokens)
         assert not held or (x.k == k and x.buffer.device == self.device), "activations of another k or on another device"
         shape = (ncols, rows) if tokens else (rows, ncols)
         dtype = torch.float32 if y_dtype else torch.bfloat16
-        assert y is None or (y.device == self.device and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1)), \
-            "Y has the product's shape and type, and consecutive elements in a row"
+        if y is None:
+            y = torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=self.device)
+        else:
+            assert y.device == self.device and y.dtype == dtype and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1), \
+                "Y has the product's shape and type, and consecutive elements in a row"
         with self._on_device():
-            if y is None:
-                with _allocating_for(stream):
-                    y = torch.empty_strided(shape, (shape[1], 1), dtype=dtype, device=self.device)
             if held:
                 crisp_spmm8_quantized(self.handle8, x.buffer, ncols, y, _pitch(y), int(tokens), y_dtype, stream)
                 return y
@@ -1144,7 +1148,7 @@ def _kept_buffer(name):
         buffer = getattr(self, name)
         assert buffer is not None and value.shape == buffer.shape and value.dtype == buffer.dtype, "a state keeps its size and type"
         buffer.copy_(value)
-    return property(lambda self: getattr(self, name), take)
+    return property(operator.attrgetter(name), take)
 
 
 class AdamW:
@@ -1259,24 +1263,24 @@ class AdamW:
             assert grad_scale.is_cuda and grad_scale.device == self.device and grad_scale.dtype is self.torch.float32 and grad_scale.numel() == 1, \
                 "grad_scale is an fp32 CUDA tensor of one element"
         p.d_grad_scale = grad_scale.data_ptr() if grad_scale is not None else None
-        if self.device.index == _current_device():
-            self._launch(grads, stream)
+        gpu = self.device.index
+        if gpu == _current_device():
+            self._launch(grads, stream, gpu)
         else:
             with self.torch.cuda.device(self.device):
-                self._launch(grads, stream)
+                self._launch(grads, stream, gpu)
         if not self.capturable:
             self._step_count += 1
         return self
 
-    def _launch(self, grads, stream):
+    def _launch(self, grads, stream, gpu):
         if self.capturable:                                  # (the step's own number, made before it and taken back if it is refused)
             with _allocating_for(stream):
                 self.d_step += 1
         try:
             code = None
             if _network and type(grads) is list:
-                code = _network.adamw(self._address, self.weights, self.copies, grads, self.masks, C.addressof(self._params), _stream(stream),
-                                      self.device.index)
+                code = _network.adamw(self._address, self.weights, self.copies, grads, self.masks, C.addressof(self._params), _stream(stream), gpu)
             if code is None:
                 self._gradients(grads)
                 self.torch.autograd.graph.increment_version([t for ts, g in zip(zip(self.weights, self.copies), grads) for t in ts
@@ -1313,7 +1317,7 @@ class AdamW:
             with self.torch.cuda.device(self.device), _allocating_for(stream):
                 return self.moments()
         if _network and self.device.index == _current_device():
-            code, *out = _network.moments(self.m, self.m_exp, self.v, self.v_exp, _current_stream())
+            code, *out = _network.moments(self._m, self._m_exp, self._v, self._v_exp, _current_stream())
             if code:
                 raise CrispError(code, "crisp_adamw_moments")
             return out
