@@ -1276,7 +1276,7 @@ class AdamW:
     def _launch(self, grads, stream, gpu):
         if self.capturable:                                  # (the step's own number, made before it and taken back if it is refused)
             with _allocating_for(stream):
-                self.d_step += 1
+                self._d_step += 1
         try:
             code = None
             if _network and type(grads) is list:
@@ -1291,7 +1291,7 @@ class AdamW:
         except Exception:
             if self.capturable:
                 with _allocating_for(stream):
-                    self.d_step -= 1
+                    self._d_step -= 1
             raise
 
     def _gradients(self, grads):
