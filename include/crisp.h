@@ -513,6 +513,8 @@ CRISP_API crisp_status_t crisp_decode8(crisp_handle8_t h, uint16_t *d_w_dense_bf
  */
 CRISP_API crisp_status_t crisp_quantize8_sizes(int64_t k, int64_t ncols, size_t *bytes);
 CRISP_API crisp_status_t crisp_quantize8(const uint16_t *d_x_bf16, int64_t ldx, int32_t x_layout, int64_t k, int64_t ncols, void *d_act, void *stream);
+/* The bf16 values that they stand for, in either layout (of quantize8's own X or of the other one): an activation that was kept in 8 bits for the backward pass. */
+CRISP_API crisp_status_t crisp_dequantize8(const void *d_act, int32_t y_layout, int64_t k, int64_t ncols, uint16_t *d_y_bf16, int64_t ldy, void *stream);
 
 /*
  * The product.  crisp_spmm8 quantises X as crisp_quantize8 does and multiplies; d_act is a workspace of crisp_spmm8_sizes bytes, 256-byte aligned (0 for few columns, which
@@ -528,6 +530,40 @@ CRISP_API crisp_status_t crisp_spmm8(crisp_handle8_t h, const uint16_t *d_x_bf16
                                      int64_t ldy, int32_t y_layout, int32_t y_dtype, void *stream);
 CRISP_API crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_act, int64_t ncols, void *d_y, int64_t ldy, int32_t y_layout,
                                                int32_t y_dtype, void *stream);
+
+/*
+ * Group norm with an activation over channels-last activations, which stands between the pruned layers of a network (the paper's networks normalise after each
+ * convolution; it gives no formula of its own).  Of each sample's groups (pixels x channels / groups values):
+ *
+ *   h = (x - mean) * rstd,  rstd = 1 / sqrt(var + eps)        y = act(p),  p = gamma * h + beta      (per channel)
+ *   e = dy * act'(p)     dbeta = sum e     dgamma = sum e * h     dx = rstd * (gamma * e - m1 - h * m2),   m1, m2: the group's means of gamma * e and gamma * e * h
+ *
+ *   batch, pixels, channels   x, y, dy, dx are [batch * pixels, channels], channels consecutive, a pixel every ld.. >= channels elements
+ *   activation                0 none, 1 max(p, 0), 2 min(max(p, 0), 6), 3 p / (1 + exp(-p)); the slope on a border is 0
+ *   dtype                     of x, y, dy, dx: 0 bf16, 1 fp32, 2 fp16.  Sums and statistics are fp32, y and dx are rounded once
+ *   d_gamma, d_beta           [channels] fp32, or NULL: 1 and 0
+ *   d_stats                   [batch, groups, 2] fp32, 8-byte aligned: mean and rstd, written forward and read backward
+ *   d_x8, d_y8                8-bit forms of x and of y (before it is rounded to its type) to be written in the same pass, as crisp_quantize8 has them of [batch * pixels, channels]
+ *                             (crisp_quantize8_sizes(channels, batch * pixels) bytes, 256-byte aligned), or NULL.  With d_y8, d_y may be NULL
+ *   backward                  from x (d_x) or from its 8-bit form (d_x8): one of them, the other NULL; the gradient is that of the formula at the values that it stands for and the
+ *                             given statistics.  d_dgamma, d_dbeta: [channels] fp32, or NULL
+ *   d_workspace               crisp_group_norm_sizes bytes, 256-byte aligned (NULL where that is 0); a call's own until it has run
+ * y may lie on x, and dx on dy or x, with the same pitch.  A group with a value that is not finite becomes NaN.  Results do not depend on what else runs.  batch = 0: nothing is
+ * written but zeros in d_dgamma and d_dbeta.
+ */
+typedef struct {
+    int64_t batch, pixels;
+    int32_t channels, groups;
+    int32_t activation;
+    int32_t dtype;
+    double eps;
+} crisp_group_norm_t;
+CRISP_API crisp_status_t crisp_group_norm_sizes(const crisp_group_norm_t *desc, int32_t backward, size_t *workspace_bytes);
+CRISP_API crisp_status_t crisp_group_norm(const crisp_group_norm_t *desc, const void *d_x, int64_t ldx, const float *d_gamma, const float *d_beta, void *d_y, int64_t ldy,
+                                          float *d_stats, void *d_x8, void *d_y8, void *d_workspace, void *stream);
+CRISP_API crisp_status_t crisp_group_norm_backward(const crisp_group_norm_t *desc, const void *d_dy, int64_t ld_dy, const void *d_x, int64_t ldx, const void *d_x8,
+                                                   const float *d_stats, const float *d_gamma, const float *d_beta, void *d_dx, int64_t ld_dx, float *d_dgamma,
+                                                   float *d_dbeta, void *d_workspace, void *stream);
 
 /* crisp_set_epilogue, crisp_last_launch (path: CRISP_PATH_DIRECT where one to four columns ran on the CUDA cores; stack: CTAs that
  * share one tile's blocks, -1 for pairs), crisp_device_status, crisp_reset_status and crisp_set_tuning of an 8-bit handle.

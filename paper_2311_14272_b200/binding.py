@@ -58,6 +58,11 @@ class ConvDesc(C.Structure):
                 ("kernel_h", C.c_int32), ("kernel_w", C.c_int32), ("pad", C.c_int32), ("y_layout", C.c_int32)]
 
 
+class GroupNormDesc(C.Structure):
+    _fields_ = [("batch", C.c_int64), ("pixels", C.c_int64), ("channels", C.c_int32), ("groups", C.c_int32), ("activation", C.c_int32),
+                ("dtype", C.c_int32), ("eps", C.c_double)]
+
+
 class LaunchInfo(C.Structure):
     _fields_ = [("path", C.c_int32), ("tile_cols", C.c_int32), ("accumulators", C.c_int32), ("stack", C.c_int32),
                 ("epilogue_warps", C.c_int32), ("stages", C.c_int32), ("ctas", C.c_int32), ("conv", C.c_int32),
@@ -197,6 +202,10 @@ def load(path: Optional[str] = None):
         "crisp_decode8": [vp, vp, i64, vp],
         "crisp_quantize8_sizes": [i64, i64, P(sz)],
         "crisp_quantize8": [vp, i64, i32, i64, i64, vp, vp],
+        "crisp_dequantize8": [vp, i32, i64, i64, vp, i64, vp],
+        "crisp_group_norm_sizes": [P(GroupNormDesc), i32, P(sz)],
+        "crisp_group_norm": [P(GroupNormDesc), vp, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp],
+        "crisp_group_norm_backward": [P(GroupNormDesc), vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp],
         "crisp_spmm8_sizes": [vp, i64, P(sz)],
         "crisp_spmm8": [vp, vp, i64, i32, i64, vp, vp, i64, i32, i32, vp],
         "crisp_spmm8_quantized": [vp, vp, i64, vp, i64, i32, i32, vp],
@@ -569,6 +578,28 @@ def crisp_quantize8(d_x, ldx: int, x_layout: int, k: int, ncols: int, d_act, str
     _check(load().crisp_quantize8(_ptr(d_x), ldx, x_layout, k, ncols, _ptr(d_act), _stream(stream)), "crisp_quantize8")
 
 
+def crisp_dequantize8(d_act, y_layout: int, k: int, ncols: int, d_y, ldy: int, stream=None):
+    _check(load().crisp_dequantize8(_ptr(d_act), y_layout, k, ncols, _ptr(d_y), ldy, _stream(stream)), "crisp_dequantize8")
+
+
+def crisp_group_norm_sizes(desc: GroupNormDesc, backward: bool) -> int:
+    out = C.c_size_t()
+    _check(load().crisp_group_norm_sizes(C.byref(desc), int(backward), C.byref(out)), "crisp_group_norm_sizes")
+    return out.value
+
+
+def crisp_group_norm(desc: GroupNormDesc, d_x, ldx: int, d_gamma, d_beta, d_y, ldy: int, d_stats, d_x8, d_y8, d_workspace, stream=None):
+    _check(load().crisp_group_norm(C.byref(desc), _ptr(d_x), ldx, _ptr(d_gamma), _ptr(d_beta), _ptr(d_y), ldy, _ptr(d_stats), _ptr(d_x8), _ptr(d_y8),
+                                   _ptr(d_workspace), _stream(stream)), "crisp_group_norm")
+
+
+def crisp_group_norm_backward(desc: GroupNormDesc, d_dy, ld_dy: int, d_x, ldx: int, d_x8, d_stats, d_gamma, d_beta, d_dx, ld_dx: int, d_dgamma, d_dbeta,
+                              d_workspace, stream=None):
+    _check(load().crisp_group_norm_backward(C.byref(desc), _ptr(d_dy), ld_dy, _ptr(d_x), ldx, _ptr(d_x8), _ptr(d_stats), _ptr(d_gamma), _ptr(d_beta),
+                                            _ptr(d_dx), ld_dx, _ptr(d_dgamma), _ptr(d_dbeta), _ptr(d_workspace), _stream(stream)),
+           "crisp_group_norm_backward")
+
+
 def crisp_spmm8_sizes(handle8: int, ncols: int) -> int:
     out = C.c_size_t()
     _check(load().crisp_spmm8_sizes(handle8, ncols, C.byref(out)), "crisp_spmm8_sizes")
@@ -633,11 +664,52 @@ def _pitch(t) -> int:
     return t.stride()[0] if t.shape[0] > 1 else t.shape[1]
 
 
+def _on(device):
+    """A context in which `device` is the current one."""
+    if device.index == _current_device():
+        return _AS_IT_IS
+    import torch
+    return torch.cuda.device(device)
+
+
 class Activations8:
-    """Activations in 8 bits (HybridLayer.quantize8): a buffer of the library's form that layers of the same k multiply."""
+    """Activations in 8 bits (quantize8, GroupNorm.forward): a buffer of the library's form.  Layers of the same k multiply it (HybridLayer.spmm8), and it is the
+    checkpoint that a layer's weight gradient and a norm's backward pass take."""
 
     def __init__(self, k, ncols, buffer):
         self.k, self.ncols, self.buffer = k, ncols, buffer
+
+    def dequantize(self, tokens=False, y=None, stream=None):
+        """The bf16 values that it stands for: [k, ncols], or with tokens=True [ncols, k]."""
+        import torch
+        shape, device = (self.ncols, self.k) if tokens else (self.k, self.ncols), self.buffer.device
+        with _on(device):
+            if y is None:
+                with _allocating_for(stream):
+                    y = torch.empty_strided(shape, (shape[1], 1), dtype=torch.bfloat16, device=device)
+            else:
+                assert y.device == device and y.dtype == torch.bfloat16 and y.shape == shape and (y.stride()[1] == 1 or shape[1] == 1), \
+                    "Y is a bf16 matrix of the activations' shape on their device, with consecutive elements in a row"
+            crisp_dequantize8(self.buffer, int(tokens), self.k, self.ncols, y, _pitch(y), stream)
+        return y
+
+
+def quantize8(x, tokens=False, stream=None):
+    """X in 8 bits, for any layer of its k: x is a bf16 CUDA matrix [k, ncols], or with tokens=True [ncols, k] (NHWC activations: x.view(-1, channels))."""
+    import torch
+    assert x.is_cuda and x.dtype == torch.bfloat16 and len(x.shape) == 2 and (x.stride()[1] == 1 or x.shape[1] == 1), \
+        "X is a bf16 CUDA matrix, [k, ncols] or with tokens=True [ncols, k], with consecutive elements in a row"
+    ncols, k = x.shape if tokens else reversed(x.shape)
+    with _on(x.device):
+        act = _buffer8(k, ncols, x.device, stream)
+        crisp_quantize8(x, _pitch(x), int(tokens), k, ncols, act.buffer, stream)
+    return act
+
+
+def _buffer8(k, ncols, device, stream):
+    import torch
+    with _allocating_for(stream):
+        return Activations8(k, ncols, torch.empty_strided((crisp_quantize8_sizes(k, ncols),), (1,), dtype=torch.uint8, device=device))
 
 
 # -------------------------------------------------- buffer-owning convenience wrapper
@@ -1127,6 +1199,115 @@ class PruningNetwork:
     def close(self):
         for L in self.layers:
             L.close()
+
+
+class Normed:
+    """What GroupNorm.forward leaves: y, the statistics [batch, groups, 2] (mean, 1 / standard deviation) that the backward pass takes, and the 8-bit forms of
+    x and y that were asked for (Activations8 of k = channels and a column a pixel)."""
+    __slots__ = ("y", "statistics", "x8", "y8")
+
+    def __init__(self, y, statistics, x8, y8):
+        self.y, self.statistics, self.x8, self.y8 = y, statistics, x8, y8
+
+
+class GroupNorm:
+    """Group norm with an activation over channels-last activations (crisp_group_norm): y = act(weight * (x - mean) / sqrt(var + eps) + bias), mean and variance of
+    each sample's groups of channels.
+
+    x is a bf16, fp16 or fp32 CUDA tensor [batch, ..., channels] whose pixels lie a constant pitch apart (an NHWC tensor, or a slice of its channels); weight and
+    bias are fp32 CUDA tensors [channels] that this object keeps, or None.  activation: "none", "relu", "relu6" or "silu".
+    """
+    ACTIVATIONS = {"none": 0, "relu": 1, "relu6": 2, "silu": 3}
+
+    def __init__(self, channels, groups, weight=None, bias=None, eps=1e-5, activation="none"):
+        import torch
+        self.torch = torch
+        self.channels, self.groups, self.eps = channels, groups, float(eps)
+        self.activation = self.ACTIVATIONS["none" if activation is None else activation]
+        self.weight, self.bias = weight, bias
+        self._types = {torch.bfloat16: 0, torch.float32: 1, torch.float16: 2}
+        crisp_group_norm_sizes(self._desc(1, 1, 0), False)                   # (channels, groups and eps that the library refuses are refused here)
+
+    def _desc(self, batch, pixels, dtype):
+        return GroupNormDesc(batch, pixels, self.channels, self.groups, self.activation, dtype, self.eps)
+
+    def _rows(self, t, what, like=None):
+        """Elements from one pixel to the next."""
+        shape, strides = t.shape, t.stride()
+        assert t.is_cuda and t.dtype in self._types and len(shape) >= 2 and shape[-1] == self.channels, \
+            f"{what} is a bf16, fp16 or fp32 CUDA tensor [batch, ..., channels]"
+        assert like is None or (t.dtype == like.dtype and t.device == like.device and shape == like.shape), f"{what} has another shape, type or device"
+        assert strides[-1] == 1 or shape[-1] == 1, f"the channels of {what} are not consecutive"
+        pitch, count = None, 1                                               # of the innermost dimension that has one; pixels inside the present one
+        for size, stride in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+            if size == 1:
+                continue
+            if pitch is None:
+                pitch = stride
+            assert stride == pitch * count, f"the pixels of {what} do not lie one pitch apart"
+            count *= size
+        return self.channels if pitch is None else pitch
+
+    def _parameters(self, device):
+        for p in (self.weight, self.bias):
+            assert p is None or (p.device == device and p.dtype == self.torch.float32 and p.numel() == self.channels and p.is_contiguous()), \
+                "weight and bias are fp32 tensors of as many consecutive elements as there are channels, on the activations' device"
+
+    def _shape(self, t):
+        """batch, pixels of one sample"""
+        pixels = 1
+        for size in t.shape[1:-1]:
+            pixels *= size
+        return t.shape[0], pixels
+
+    def _workspace(self, desc, backward, device, stream):
+        size = crisp_group_norm_sizes(desc, backward)
+        with _allocating_for(stream):                                        # given back when the call returns: to the stream that uses it
+            return self.torch.empty_strided((size,), (1,), dtype=self.torch.uint8, device=device) if size else None
+
+    def forward(self, x, y=None, keep_x=False, keep_y=False, plain_y=True, stream=None):
+        """-> Normed.  keep_x, keep_y: x and y also in 8 bits, written in the same pass; plain_y=False: y in 8 bits alone.  y: where to write it (x itself, too)."""
+        torch = self.torch
+        ldx = self._rows(x, "x")
+        device, (batch, pixels) = x.device, self._shape(x)
+        self._parameters(device)
+        assert plain_y or (keep_y and y is None), "neither y nor its 8-bit form is asked for"
+        desc = self._desc(batch, pixels, self._types[x.dtype])
+        with _on(device):
+            with _allocating_for(stream):
+                statistics = torch.empty_strided((batch, self.groups, 2), (self.groups * 2, 2, 1), dtype=torch.float32, device=device)
+                if y is None and plain_y:
+                    y = torch.empty(x.shape, dtype=x.dtype, device=device)
+            ldy = self._rows(y, "y", x) if y is not None else 0
+            x8, y8 = (_buffer8(self.channels, batch * pixels, device, stream) if wanted and batch else None for wanted in (keep_x, keep_y))
+            crisp_group_norm(desc, x, ldx, self.weight, self.bias, y, ldy, statistics, x8 and x8.buffer, y8 and y8.buffer,
+                             self._workspace(desc, False, device, stream), stream)
+        return Normed(y, statistics, x8, y8)
+
+    __call__ = forward
+
+    def backward(self, dy, x, statistics, dx=None, stream=None):
+        """-> dx, dweight, dbias (fp32).  x: the forward pass's, as it was or in 8 bits (Normed.x8); statistics: Normed's.  dx: where to write it (dy or x, too)."""
+        torch = self.torch
+        ld_dy = self._rows(dy, "dy")
+        device, (batch, pixels) = dy.device, self._shape(dy)
+        self._parameters(device)
+        held = isinstance(x, Activations8)
+        if held:
+            assert x.k == self.channels and x.ncols == batch * pixels and x.buffer.device == device, "x in 8 bits of other sizes, or on another device"
+        ldx = 0 if held or x is None else self._rows(x, "x", dy)
+        assert statistics.device == device and statistics.dtype == torch.float32 and statistics.shape == (batch, self.groups, 2) and statistics.is_contiguous(), \
+            "statistics are the forward pass's, [batch, groups, 2]"
+        desc = self._desc(batch, pixels, self._types[dy.dtype])
+        with _on(device):
+            with _allocating_for(stream):
+                dweight, dbias = (torch.empty_strided((self.channels,), (1,), dtype=torch.float32, device=device) for _ in range(2))
+                if dx is None:
+                    dx = torch.empty(dy.shape, dtype=dy.dtype, device=device)
+            ld_dx = self._rows(dx, "dx", dy)
+            crisp_group_norm_backward(desc, dy, ld_dy, None if held else x, ldx, x.buffer if held else None, statistics, self.weight, self.bias, dx, ld_dx,
+                                      dweight, dbias, self._workspace(desc, True, device, stream), stream)
+        return dx, dweight, dbias
 
 
 def _rows_of(t):

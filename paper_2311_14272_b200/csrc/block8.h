@@ -60,4 +60,6 @@ cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, i
 // used: a byte a k-block, 0 for those that are left out, or nullptr for all
 cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t k, int64_t ncols, uint8_t *act, const uint8_t *used, cudaStream_t st);
 
+cudaError_t launch_dequantize8(const uint8_t *act, int layout, int64_t k, int64_t ncols, uint16_t *y, int64_t ldy, cudaStream_t st);
+
 }  // namespace crisp

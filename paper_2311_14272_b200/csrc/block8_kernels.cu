@@ -375,6 +375,90 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
     for (int i = threadIdx.x; i < atoms * 64; i += 256) out[i] = reinterpret_cast<const uint4 *>(tile)[i ^ (i >> 6 & 7)];
 }
 
+// Back to bf16.  Tokens: as quantize_tokens_kernel takes them, eight values a thread and block, U blocks a thread; all codes ahead of the first store.
+template <int U>
+__global__ void __launch_bounds__(256)
+dequantize_tokens_kernel(const uint8_t *codes, const uint8_t *scales, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint16_t *y, int64_t ldy,
+                         int vec_ok) {
+    wait_for_prerequisites();
+    const uint32_t spans = (uint32_t)((nblk + 2 * U - 1) / (2 * U)), g = blockIdx.x / spans;
+    const int lane = threadIdx.x & 15, r = threadIdx.x >> 4 & 7, side = threadIdx.x >> 7;
+    const int64_t col = (int64_t)g * 8 + r, kb0 = (int64_t)(blockIdx.x - g * spans) * (2 * U) + side * U;
+    if (col >= ncols) return;
+    uint2 c[U] = {};
+    uint32_t e[U] = {};
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        if (kb0 + i >= nblk) break;
+        c[i] = *reinterpret_cast<const uint2 *>(codes + ((kb0 + i) * groups + g) * 1024 + r * 128 + (((lane >> 1) ^ r) << 4) + (lane & 1) * 8);
+        e[i] = scales[((kb0 + i) * chunks + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4];
+    }
+#pragma unroll
+    for (int i = 0; i < U; ++i) {
+        const int64_t at = (kb0 + i) * 128 + lane * 8;
+        if (at >= k) break;
+        const float up = power_of(e[i]);
+        uint32_t out[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) out[j] = values2((j < 2 ? c[i].x : c[i].y) >> (16 * (j & 1)), up);
+        uint16_t *p = y + col * ldy + at;
+        if (vec_ok && at + 8 <= k) {
+            *reinterpret_cast<uint4 *>(p) = make_uint4(out[0], out[1], out[2], out[3]);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (at + j < k) p[j] = (uint16_t)(out[j / 2] >> (16 * (j & 1)));
+        }
+    }
+}
+
+// [k, ncols]: a CTA takes 128 columns of one k-block; its codes go through shared memory (rows of 132 bytes: neither side's words meet in a bank), a warp then writes
+// 16 rows, four columns a lane.
+__global__ void __launch_bounds__(256)
+dequantize_columns_kernel(const uint8_t *codes, const uint8_t *scales, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint16_t *y, int64_t ldy,
+                          int vec_ok) {
+    __shared__ uint32_t tile[128 * 33];
+    wait_for_prerequisites();
+    const int64_t kb = blockIdx.x / chunks, chunk = blockIdx.x - kb * chunks, c0 = chunk * 128;
+    const int atoms = (int)min((int64_t)16, groups - (c0 >> 3));
+    const uint32_t *from = reinterpret_cast<const uint32_t *>(codes + (kb * groups + (c0 >> 3)) * 1024);
+    for (int i = threadIdx.x; i < atoms * 256; i += 256) {
+        const int col = i >> 5, word = i & 31;
+        tile[col * 33 + ((((word >> 2) ^ col) & 7) << 2 | (word & 3))] = from[i];
+    }
+    __syncthreads();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int64_t col = c0 + 4 * lane;
+    if (col >= ncols) return;
+    const int here = (int)min((int64_t)4, ncols - col);
+    float up[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+        if (j < here) up[j] = power_of(scales[(kb * chunks + chunk) * kScales8 + ((col + j) & 31) * 16 + ((col + j) >> 5 & 3) * 4]);
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        uint32_t four[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) four[j] = j < here ? tile[(4 * lane + j) * 33 + warp * 4 + w] : 0u;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int64_t row = kb * 128 + warp * 16 + w * 4 + i;
+            if (row >= k) return;
+            uint32_t v[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = values2(four[j] >> (8 * i) & 0xFFu, up[j]) & 0xFFFFu;
+            uint16_t *p = y + row * ldy + col;
+            if (vec_ok && here == 4) {
+                *reinterpret_cast<uint2 *>(p) = make_uint2(v[0] | v[1] << 16, v[2] | v[3] << 16);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    if (j < here) p[j] = (uint16_t)v[j];
+            }
+        }
+    }
+}
+
 // Columns that a load or store may take.
 int columns_of(const void *p, int64_t ld) {
     const uintptr_t a = reinterpret_cast<uintptr_t>(p);
@@ -400,6 +484,18 @@ cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, i
     const Image8 I = image8(g);
     return launch_chained(decode8_kernel, (unsigned)(g.nrt * g.nblk), kDecode, 0, st, g, reinterpret_cast<const int32_t *>(buf + I.col_off), buf + I.exp_off,
                           buf + I.image_off, w, ld, columns_of(w, ld));
+}
+
+cudaError_t launch_dequantize8(const uint8_t *act, int layout, int64_t k, int64_t ncols, uint16_t *y, int64_t ldy, cudaStream_t st) {
+    const Act8 a = act8(k, ncols);
+    const int u = a.groups * a.nblk >= 8 * 1184 ? 4 : 1;
+    const int64_t ctas = layout ? a.groups * ((a.nblk + 2 * u - 1) / (2 * u)) : a.nblk * a.chunks;
+    if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
+    if (layout)
+        return launch_chained(u == 4 ? dequantize_tokens_kernel<4> : dequantize_tokens_kernel<1>, (unsigned)ctas, 256, 0, st, act, act + a.scale_off, k, ncols, a.nblk,
+                              a.groups, a.chunks, y, ldy, (int)aligned16(y, ldy));
+    const int quads = reinterpret_cast<uintptr_t>(y) % 8 == 0 && ldy % 4 == 0;
+    return launch_chained(dequantize_columns_kernel, (unsigned)ctas, 256, 0, st, act, act + a.scale_off, k, ncols, a.nblk, a.groups, a.chunks, y, ldy, quads);
 }
 
 cudaError_t launch_quantize8(const uint16_t *x, int64_t ldx, int layout, int64_t k, int64_t ncols, uint8_t *act, const uint8_t *used, cudaStream_t st) {

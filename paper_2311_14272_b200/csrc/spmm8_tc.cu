@@ -1068,6 +1068,13 @@ crisp_status_t crisp_quantize8(const uint16_t *d_x_bf16, int64_t ldx, int32_t x_
     return bad != CRISP_OK ? bad : quantize(d_x_bf16, ldx, x_layout, k, ncols, d_act, nullptr, stream);
 }
 
+crisp_status_t crisp_dequantize8(const void *d_act, int32_t y_layout, int64_t k, int64_t ncols, uint16_t *d_y_bf16, int64_t ldy, void *stream) {
+    const crisp_status_t bad = check_quantize(d_y_bf16, ldy, y_layout, k, ncols, d_act);
+    if (bad != CRISP_OK) return bad;
+    const cudaError_t e = launch_dequantize8(reinterpret_cast<const uint8_t *>(d_act), y_layout, k, ncols, d_y_bf16, ldy, (cudaStream_t)stream);
+    return e == cudaSuccess ? CRISP_OK : e == cudaErrorInvalidValue ? CRISP_UNSUPPORTED : CRISP_CUDA_ERROR;
+}
+
 crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_act, int64_t ncols, void *d_y, int64_t ldy, int32_t y_layout, int32_t y_dtype,
                                      void *stream) {
     const uint64_t moment = encodes.now();
