@@ -577,6 +577,45 @@ CRISP_API crisp_status_t crisp_reset_status8(crisp_handle8_t h, void *stream);
 CRISP_API crisp_status_t crisp_set_tuning8(crisp_handle8_t h, int32_t tile_cols, int32_t split, uint64_t wait_limit_cycles, int32_t skip_fill);
 CRISP_API void crisp_destroy8(crisp_handle8_t h);
 
+/*
+ * The weight gradient of a layer from its activations in 8 bits: what crisp_quantize8 (or crisp_group_norm) kept of the forward pass,
+ *
+ *   dW[r, k] (+)= sum over the columns c of  dY[r, c] * x[k, c],     x = what the 8-bit form stands for
+ *
+ * or with `conv` that of a convolution (Y as crisp_spmm_conv has it, stride 1), x being the 8-bit form of the NHWC activation (k = channels, a column a pixel):
+ *
+ *   dW[s, (i*kernel_w + j)*channels + r] (+)= sum over b, y, x of  dY[s, b, y, x] * A[b, y + i - pad, x + j - pad, r]
+ *
+ * Products are exact, sums are fp32 in an order of their own (the same for the same arguments), dW is rounded once.
+ *   rows, k       of dW; with conv k = kernel_h * kernel_w * channels
+ *   ncols         columns of dY: tokens, or batch * ho * wo
+ *   conv          or NULL (its y_layout is not read)
+ *   d_dy          bf16; dy_layout 0: [rows, ncols], ld_dy >= ncols; 1: [ncols, rows] (tokens, NHWC), ld_dy >= rows.  16-byte addresses and pitches are faster
+ *   d_act         the 8-bit form, of k (with conv: channels) and ncols (batch * height * width)
+ *   mask          NULL: every weight's gradient, as a saliency or a straight-through step takes it.  A mask of rows x k: 0 outside it, and (blocks of 128 x 128; a convolution's
+ *                 channels a multiple of 128) blocks that are not kept are not computed.
+ *                 What is not finite in a column of X reaches all of its channel's and tap's weights; outside a mask it does not
+ *   d_dw          [rows, k], ld_dw >= k, bf16 (dw_dtype 0) or fp32 (1); accumulate 1: added to what is there (outside a mask nothing is)
+ *   d_status      a device word, or NULL: becomes CRISP_TIMEOUT if a wait within the kernel ran out (dW is not to be used then)
+ *   d_workspace   crisp_weight_grad8_sizes bytes of the same arguments, 256-byte aligned; a call's own until it has run
+ */
+typedef struct {
+    int32_t rows, k;
+    int64_t ncols;
+    const crisp_conv_desc_t *conv;
+    const uint16_t *d_dy;
+    int64_t ld_dy;
+    int32_t dy_layout, dw_dtype;
+    const void *d_act;
+    crisp_mask_t mask;
+    void *d_dw;
+    int64_t ld_dw;
+    int32_t accumulate, reserved;        /* reserved: 0 */
+    int32_t *d_status;
+} crisp_weight_grad8_t;
+CRISP_API crisp_status_t crisp_weight_grad8_sizes(const crisp_weight_grad8_t *grad, size_t *workspace_bytes);
+CRISP_API crisp_status_t crisp_weight_grad8(const crisp_weight_grad8_t *grad, void *d_workspace, void *stream);
+
 /* Restrict crisp_spmm of this handle to one kernel family (CRISP_PATH_*), or -1 for the
  * default choice.  UNSUPPORTED if the handle's execution image cannot serve that path. */
 CRISP_API crisp_status_t crisp_set_path(crisp_handle_t h, int32_t path);

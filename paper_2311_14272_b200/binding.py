@@ -63,6 +63,12 @@ class GroupNormDesc(C.Structure):
                 ("dtype", C.c_int32), ("eps", C.c_double)]
 
 
+class WeightGrad8(C.Structure):
+    _fields_ = [("rows", C.c_int32), ("k", C.c_int32), ("ncols", C.c_int64), ("conv", C.POINTER(ConvDesc)), ("d_dy", C.c_void_p), ("ld_dy", C.c_int64),
+                ("dy_layout", C.c_int32), ("dw_dtype", C.c_int32), ("d_act", C.c_void_p), ("mask", C.c_void_p), ("d_dw", C.c_void_p), ("ld_dw", C.c_int64),
+                ("accumulate", C.c_int32), ("reserved", C.c_int32), ("d_status", C.c_void_p)]
+
+
 class LaunchInfo(C.Structure):
     _fields_ = [("path", C.c_int32), ("tile_cols", C.c_int32), ("accumulators", C.c_int32), ("stack", C.c_int32),
                 ("epilogue_warps", C.c_int32), ("stages", C.c_int32), ("ctas", C.c_int32), ("conv", C.c_int32),
@@ -203,6 +209,8 @@ def load(path: Optional[str] = None):
         "crisp_quantize8_sizes": [i64, i64, P(sz)],
         "crisp_quantize8": [vp, i64, i32, i64, i64, vp, vp],
         "crisp_dequantize8": [vp, i32, i64, i64, vp, i64, vp],
+        "crisp_weight_grad8_sizes": [P(WeightGrad8), P(sz)],
+        "crisp_weight_grad8": [P(WeightGrad8), vp, vp],
         "crisp_group_norm_sizes": [P(GroupNormDesc), i32, P(sz)],
         "crisp_group_norm": [P(GroupNormDesc), vp, i64, vp, vp, vp, i64, vp, vp, vp, vp, vp],
         "crisp_group_norm_backward": [P(GroupNormDesc), vp, i64, vp, i64, vp, vp, vp, vp, vp, i64, vp, vp, vp, vp],
@@ -582,6 +590,16 @@ def crisp_dequantize8(d_act, y_layout: int, k: int, ncols: int, d_y, ldy: int, s
     _check(load().crisp_dequantize8(_ptr(d_act), y_layout, k, ncols, _ptr(d_y), ldy, _stream(stream)), "crisp_dequantize8")
 
 
+def crisp_weight_grad8_sizes(grad: WeightGrad8) -> int:
+    out = C.c_size_t()
+    _check(load().crisp_weight_grad8_sizes(C.byref(grad), C.byref(out)), "crisp_weight_grad8_sizes")
+    return out.value
+
+
+def crisp_weight_grad8(grad: WeightGrad8, d_workspace, stream=None):
+    _check(load().crisp_weight_grad8(C.byref(grad), _ptr(d_workspace), _stream(stream)), "crisp_weight_grad8")
+
+
 def crisp_group_norm_sizes(desc: GroupNormDesc, backward: bool) -> int:
     out = C.c_size_t()
     _check(load().crisp_group_norm_sizes(C.byref(desc), int(backward), C.byref(out)), "crisp_group_norm_sizes")
@@ -672,6 +690,21 @@ def _on(device):
     return torch.cuda.device(device)
 
 
+def _pixel_pitch(t, what) -> int:
+    """Elements from one pixel of a channels-last tensor to the next."""
+    shape, strides = t.shape, t.stride()
+    assert strides[-1] == 1 or shape[-1] == 1, f"the channels of {what} are not consecutive"
+    pitch, count = None, 1                                                   # of the innermost dimension that has one; pixels inside the present one
+    for size, stride in zip(reversed(shape[:-1]), reversed(strides[:-1])):
+        if size == 1:
+            continue
+        if pitch is None:
+            pitch = stride
+        assert stride == pitch * count, f"the pixels of {what} do not lie one pitch apart"
+        count *= size
+    return shape[-1] if pitch is None else pitch
+
+
 class Activations8:
     """Activations in 8 bits (quantize8, GroupNorm.forward): a buffer of the library's form.  Layers of the same k multiply it (HybridLayer.spmm8), and it is the
     checkpoint that a layer's weight gradient and a norm's backward pass take."""
@@ -737,6 +770,7 @@ class HybridLayer:
         self.handle8 = 0
         self.buf8 = None
         self._bias8 = None
+        self._grad_status = torch.zeros(1, dtype=torch.int32, device=self.device)
         self.canonical_buf = None
         self.exec_buf = None
         self._gpu = self.device.index if (_network or _bind_network()) else None       # (decode makes its tensors through it)
@@ -977,6 +1011,52 @@ class HybridLayer:
                 act = torch.empty_strided((crisp_spmm8_sizes(self.handle8, ncols),), (1,), dtype=torch.uint8, device=self.device)
             crisp_spmm8(self.handle8, x, _pitch(x), int(tokens), ncols, act, y, _pitch(y), int(tokens), y_dtype, stream)
         return y
+
+    def weight_gradient8(self, dy, act, dw=None, dw_dtype=1, tokens=False, masked=False, accumulate=False, stream=None):
+        """dW = dY X^T [rows, k] from the activations that quantize8 (or a GroupNorm) kept in 8 bits.  dy: bf16 [rows, ncols], or with tokens=True [ncols, rows].
+        masked: 0 outside the layer's mask, and blocks that are not kept are not computed (what AdamW takes under the mask); else every weight's gradient, as a
+        saliency takes it.  dw: where to write it, bf16 (dw_dtype 0) or fp32 (1); accumulate: to add it there.  gradient_status says whether a wait ran out."""
+        shape = (act.ncols, self.desc.rows) if tokens else (self.desc.rows, act.ncols)
+        assert act.k == self.desc.k, "activations of another k"
+        assert dy.shape == shape, "dY is [rows, ncols], or with tokens=True [ncols, rows], with the activations' columns"
+        return self._gradient8(dy, _pitch(dy), act, act.ncols, None, tokens, dw, dw_dtype, masked, accumulate, stream)
+
+    def weight_gradient8_conv(self, dy_nhwc, act, kernel_h, kernel_w, pad, dw=None, dw_dtype=1, masked=False, accumulate=False, stream=None):
+        """The same of a convolution (stride 1).  dy_nhwc: bf16 [batch, ho, wo, rows], dense but for the pitch of a pixel; act: the 8-bit form of the NHWC activation
+        [batch, ho + kernel_h - 1 - 2 pad, wo + kernel_w - 1 - 2 pad, channels] (quantize8(x.view(-1, channels), tokens=True))."""
+        batch, ho, wo, rows = dy_nhwc.shape
+        height, width = ho + kernel_h - 1 - 2 * pad, wo + kernel_w - 1 - 2 * pad
+        assert rows == self.desc.rows and act.k * kernel_h * kernel_w == self.desc.k and act.ncols == batch * height * width and min(height, width) > 0, \
+            "dY, activations and kernel are not those of one convolution of the layer"
+        pitch = _pixel_pitch(dy_nhwc, "dY")
+        return self._gradient8(dy_nhwc, pitch, act, batch * ho * wo, ConvDesc(batch, height, width, act.k, kernel_h, kernel_w, pad, 1), True, dw, dw_dtype, masked,
+                               accumulate, stream)
+
+    def _gradient8(self, dy, ld, act, ncols, conv, tokens, dw, dw_dtype, masked, accumulate, stream):
+        torch, rows, k = self.torch, self.desc.rows, self.desc.k
+        dtype = torch.float32 if dw_dtype else torch.bfloat16
+        assert dy.device == self.device and dy.dtype == torch.bfloat16 and (dy.stride()[-1] == 1 or dy.shape[-1] == 1), \
+            "dY is a bf16 tensor on the layer's device with consecutive elements in a row"
+        assert act.buffer.device == self.device, "activations on another device than the layer"
+        assert not masked or self.mask, "the layer has no mask yet"
+        assert not accumulate or dw is not None, "there is nothing to add to"
+        assert dw is None or (dw.device == self.device and dw.dtype == dtype and dw.shape == (rows, k) and (dw.stride()[1] == 1 or k == 1)), \
+            "dW has the weights' shape and the type asked for, on the layer's device, and consecutive elements in a row"
+        with self._on_device():
+            with _allocating_for(stream):
+                if dw is None:
+                    dw = torch.empty_strided((rows, k), (k, 1), dtype=dtype, device=self.device)
+                g = WeightGrad8(rows, k, ncols, C.pointer(conv) if conv is not None else None, _ptr(dy), ld, int(tokens), int(bool(dw_dtype)), _ptr(act.buffer),
+                                self.mask if masked else None, _ptr(dw), _pitch(dw), int(accumulate), 0, _ptr(self._grad_status))
+                size = crisp_weight_grad8_sizes(g)                           # (given back when the call returns: to the stream that uses it)
+                workspace = torch.empty_strided((size,), (1,), dtype=torch.uint8, device=self.device) if size else None
+            crisp_weight_grad8(g, workspace, stream)
+        return dw
+
+    def gradient_status(self) -> int:
+        """0, or TIMEOUT where a wait within a weight gradient ran out (its dW is not to be used).  Waits for all that runs on the device."""
+        self.torch.cuda.synchronize(self.device)
+        return int(self._grad_status.item())
 
     def set_epilogue8(self, bias=None, relu=False):
         """Y = act(W X + bias) for later 8-bit products; `bias` is an fp32 CUDA tensor [rows] that this object keeps."""
@@ -1233,20 +1313,11 @@ class GroupNorm:
 
     def _rows(self, t, what, like=None):
         """Elements from one pixel to the next."""
-        shape, strides = t.shape, t.stride()
+        shape = t.shape
         assert t.is_cuda and t.dtype in self._types and len(shape) >= 2 and shape[-1] == self.channels, \
             f"{what} is a bf16, fp16 or fp32 CUDA tensor [batch, ..., channels]"
         assert like is None or (t.dtype == like.dtype and t.device == like.device and shape == like.shape), f"{what} has another shape, type or device"
-        assert strides[-1] == 1 or shape[-1] == 1, f"the channels of {what} are not consecutive"
-        pitch, count = None, 1                                               # of the innermost dimension that has one; pixels inside the present one
-        for size, stride in zip(reversed(shape[:-1]), reversed(strides[:-1])):
-            if size == 1:
-                continue
-            if pitch is None:
-                pitch = stride
-            assert stride == pitch * count, f"the pixels of {what} do not lie one pitch apart"
-            count *= size
-        return self.channels if pitch is None else pitch
+        return _pixel_pitch(t, what)
 
     def _parameters(self, device):
         for p in (self.weight, self.bias):

@@ -1,0 +1,558 @@
+// The weight gradient of a layer from its activations in 8 bits, dW[r, k] = sum over tokens t of dY[t, r] x[t, k], x = code * 2^E.
+//
+// The sum runs over tokens, and a block's scale belongs to one token: it cannot be taken out of the sum, so the tensor cores' block scaling does not apply.  But a code times a
+// power of two is exact in bf16: x goes back to bf16 (a pass over it, in the caller's workspace), and the product is one of bf16 with fp32 accumulators.  Tokens are the
+// slow dimension of both operands (dY [tokens, rows], NHWC; x as it was dequantised), and tcgen05 takes them that way round: no transposition.
+//
+// A CTA takes 128 rows by up to four boxes of 64 columns of dW (a box lies within one filter tap) and a part of the tokens, 64 at a time: a box of output pixels for a
+// convolution, whose x is the same box shifted by the tap (TMA fills in the padding).  Under a mask of 128 x 128 blocks the boxes are those of the row tile's kept blocks.
+//
+// The accumulators in tensor memory lose what is shifted out (measured: 1.1e-9 of the result for each token), so that chains are kept short: after 512 tokens eight warps
+// add the accumulator to sums in registers, rounding to nearest, while the next chain runs in the other accumulator.  Parts of the tokens are added by a second kernel, in their order.
+#include <cuda_bf16.h>
+
+#include <algorithm>
+#include <atomic>
+
+#include "block8.h"
+#include "tc_common.cuh"
+
+namespace crisp {
+
+using namespace tc;
+
+namespace {
+
+constexpr int kStep = 64;                                     // tokens a stage
+constexpr int kChain = 8;                                     // stages a chain
+constexpr int kBoxes = 4;                                     // boxes of 64 columns a tile, at most
+constexpr int kDrain = 8;                                     // warps
+constexpr int kGradThreads = 128 + 32 * kDrain;
+constexpr uint32_t kABytes = 16384, kBoxBytes = 8192, kStage = kABytes + kBoxes * kBoxBytes;
+constexpr int kStages = 4;
+constexpr size_t kGradSmem = kStages * kStage + 256 + 1024;
+
+struct Grad {
+    int rows, channels, kernel_w, pad, linear;
+    int cboxes;                                               // boxes of a tap's channels
+    int per, tiles_row, boxes, splits, items;                 // boxes a tile, tiles a row tile, boxes a row tile
+    int tw, th, tb, nx, ny;                                   // pixels of a stage; boxes of them along a line, lines along an image
+    int chunks, chunks_split;
+    const int32_t *blk_col;                                   // masks of 128 x 128: kept blocks of a row tile (else nullptr)
+    int kkeep;
+    const uint32_t *nm_bits;                                  // a mask, or nullptr
+    int wpr;
+    void *dw;
+    int64_t ld;
+    int f32, accumulate, vec;
+    float *partial;                                           // splits > 1: [item][256 columns][128 rows]
+    int32_t *status;
+    unsigned long long wait_limit;
+    int skip_fill;
+};
+
+// Box i of a row tile's list: its first column within a tap, and the tap.
+struct BoxAt { int tap, c; };
+__device__ __forceinline__ BoxAt box_at(const Grad &p, int rt, int i) {
+    const int b = p.blk_col ? 2 * p.blk_col[(int64_t)rt * p.kkeep + (i >> 1)] + (i & 1) : i;
+    if (p.linear) return {0, b * 64};
+    const int tap = b / p.cboxes;
+    return {tap, (b - tap * p.cboxes) * 64};
+}
+
+__device__ __forceinline__ uint32_t mask_bits(const Grad &p, int row, int col) {      // 32 columns from `col` on
+    const uint32_t *w = p.nm_bits + (int64_t)row * p.wpr;
+    const int i = col >> 5;
+    return __funnelshift_r(i < p.wpr ? w[i] : 0u, i + 1 < p.wpr ? w[i + 1] : 0u, col & 31);
+}
+
+// 32 sums of a row to dW.
+__device__ __forceinline__ void store32(const Grad &p, int row, int col, int n, float (&v)[32]) {
+    if (p.nm_bits) {
+        const uint32_t bits = mask_bits(p, row, col);
+#pragma unroll
+        for (int j = 0; j < 32; ++j)
+            if (!(bits >> j & 1u)) v[j] = 0.f;                // (a choice: what is not finite is gone, too)
+    }
+    const int64_t at = (int64_t)row * p.ld + col;
+    if (p.f32) {
+        float *to = reinterpret_cast<float *>(p.dw) + at;
+        if (p.vec && n == 32 && (col & 3) == 0) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) {
+                float4 q = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+                if (p.accumulate) {
+                    const float4 o = *reinterpret_cast<const float4 *>(to + j);
+                    q.x += o.x; q.y += o.y; q.z += o.z; q.w += o.w;
+                }
+                *reinterpret_cast<float4 *>(to + j) = q;
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (j < n) to[j] = p.accumulate ? to[j] + v[j] : v[j];
+        }
+    } else {
+        __nv_bfloat16 *to = reinterpret_cast<__nv_bfloat16 *>(p.dw) + at;
+        if (p.vec && n == 32 && (col & 7) == 0) {
+#pragma unroll
+            for (int j = 0; j < 32; j += 8) {
+                uint4 q = make_uint4(0, 0, 0, 0);
+                if (p.accumulate) q = *reinterpret_cast<const uint4 *>(to + j);
+                const uint32_t o[4] = {q.x, q.y, q.z, q.w};
+                uint32_t r[4];
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    float a = v[j + 2 * i], b = v[j + 2 * i + 1];
+                    if (p.accumulate) { a += __uint_as_float(o[i] << 16); b += __uint_as_float(o[i] & 0xFFFF0000u); }
+                    r[i] = pack_bf16(a, b);
+                }
+                *reinterpret_cast<uint4 *>(to + j) = make_uint4(r[0], r[1], r[2], r[3]);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 32; ++j)
+                if (j < n) to[j] = __float2bfloat16_rn(p.accumulate ? __bfloat162float(to[j]) + v[j] : v[j]);
+        }
+    }
+}
+
+template <bool kAMn>
+__global__ void __launch_bounds__(kGradThreads, 1)
+grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Grad p) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = smem_u32(smem_raw), ring = (base + 1023u) & ~1023u, ctrl = ring + kStages * kStage;
+    uint8_t *ctrl_gen = smem_raw + (ctrl - base);
+    const uint32_t bar_full = ctrl, bar_empty = ctrl + 64, bar_tfull = ctrl + 128, bar_tempty = ctrl + 144, bar_done = ctrl + 160;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 176);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(ctrl_gen + 180);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (warp == 2) {
+        tmem_alloc(smem_u32(const_cast<uint32_t *>(tmem_slot)), 512);
+        tmem_relinquish();
+    }
+    if (threadIdx.x == 0) {
+        prefetch_tensormap(&map_a);
+        prefetch_tensormap(&map_b);
+        for (int s = 0; s < kStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, kDrain); }
+        mbar_init(bar_done, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    wait_for_prerequisites();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0 && lane == 0) {
+        // ------------------------------------------------------------------ loads
+        uint32_t ph = 0;
+        int s = 0, fill = 0;
+        bool ok = true;
+        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            const int tile = item / p.splits, split = item - tile * p.splits, rt = tile / p.tiles_row, first = (tile - rt * p.tiles_row) * p.per;
+            const int n = min(p.per, p.boxes - first), c0 = split * p.chunks_split, c1 = min(c0 + p.chunks_split, p.chunks);
+            BoxAt box[kBoxes];
+#pragma unroll
+            for (int i = 0; i < kBoxes; ++i)
+                if (i < n) box[i] = box_at(p, rt, first + i);
+            int dx[kBoxes], dy[kBoxes];
+#pragma unroll
+            for (int i = 0; i < kBoxes; ++i) {
+                dx[i] = dy[i] = 0;
+                if (i < n && !p.linear) { dy[i] = box[i].tap / p.kernel_w; dx[i] = box[i].tap - dy[i] * p.kernel_w - p.pad; dy[i] -= p.pad; }
+            }
+            for (int c = c0; c < c1; ++c) {
+                if (!mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
+                const uint32_t dst = ring + s * kStage, full = bar_full + 8 * s;
+                const int by = c / p.nx, x0 = (c - by * p.nx) * p.tw, bb = by / p.ny, y0 = (by - bb * p.ny) * p.th, b0 = bb * p.tb;
+                mbar_expect_tx(full, kABytes + n * kBoxBytes);
+                if (fill++ != p.skip_fill) {
+                    if constexpr (kAMn) {
+                        tma_load_4d(dst, &map_a, rt * 128, x0, y0, b0, full);
+                        tma_load_4d(dst + 8192, &map_a, rt * 128 + 64, x0, y0, b0, full);
+                    } else {
+                        tma_load_2d(dst, &map_a, x0, rt * 128, full);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kBoxes; ++i)
+                        if (i < n) tma_load_4d(dst + kABytes + i * kBoxBytes, &map_b, box[i].c, x0 + dx[i], y0 + dy[i], b0, full);
+                }
+                if (++s == kStages) { s = 0; ph ^= 1u; }
+            }
+        }
+    } else if (warp == 1 && lane == 0) {
+        // ------------------------------------------------------------------ products
+        uint32_t ph = 0, acc = 0, acc_ph = 0;
+        int s = 0;
+        bool ok = true;
+        const uint64_t a0 = kAMn ? make_smem_desc(ring, 8192, 1024, kLayoutSw128) : make_smem_desc(ring, 16, 1024, kLayoutSw128);
+        const uint64_t b0 = make_smem_desc(ring + kABytes, kBoxBytes, 1024, kLayoutSw128);
+        constexpr uint32_t a_step = kAMn ? 128u : 2u;         // sixteen tokens on, in units of 16 bytes
+        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
+            const int tile = item / p.splits, split = item - tile * p.splits, first = tile % p.tiles_row * p.per;
+            const int n = min(p.per, p.boxes - first), c0 = split * p.chunks_split, c1 = min(c0 + p.chunks_split, p.chunks);
+            const uint32_t idesc = make_idesc(64 * n, false) | (kAMn ? 1u << 15 : 0u);
+            for (int c = c0; c < c1 && ok; c += kChain) {
+                ok = mbar_wait(bar_tempty + 8 * acc, acc_ph ^ 1u, abort_flag, p.wait_limit);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t d = tmem + acc * 256;
+                const int end = min(c + kChain, c1);
+                for (int i = c; i < end; ++i) {
+                    ok = mbar_wait(bar_full + 8 * s, ph, abort_flag, p.wait_limit);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t off = (uint32_t)s * (kStage >> 4);
+#pragma unroll
+                    for (int j = 0; j < kStep / 16; ++j) mma_dense(d, a0 + off + j * a_step, b0 + off + j * 128u, idesc, (uint32_t)((i - c) | j));
+                    mma_commit(bar_empty + 8 * s);
+                    if (++s == kStages) { s = 0; ph ^= 1u; }
+                }
+                if (!ok) break;
+                mma_commit(bar_tfull + 8 * acc);
+                if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+            }
+        }
+        mma_commit(bar_done);                                 // (also where a wait has run out: no accumulator is given back under a product)
+        mbar_wait(bar_done, 0, abort_flag, kWaitLimitCycles);
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ sums
+        const int q = warp & 3, half = (warp - 4) >> 2;       // a warp may read the lanes of its quarter only
+        uint32_t acc = 0, acc_ph = 0;
+        for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
+            const int tile = item / p.splits, split = item - tile * p.splits, rt = tile / p.tiles_row, first = (tile - rt * p.tiles_row) * p.per;
+            const int n = min(p.per, p.boxes - first), c0 = split * p.chunks_split, c1 = min(c0 + p.chunks_split, p.chunks);
+            float sum[4][32];
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+#pragma unroll
+                for (int j = 0; j < 32; ++j) sum[i][j] = 0.f;
+            int go = 1;
+            for (int c = c0; c < c1; c += kChain) {
+                if (lane == 0) go = !*abort_flag && mbar_wait(bar_tfull + 8 * acc, acc_ph, abort_flag, p.wait_limit);
+                go = __shfl_sync(0xFFFFFFFFu, go, 0);
+                if (!go) break;
+                tc_fence_after();
+                const uint32_t from = tmem + acc * 256 + half * 128 + ((uint32_t)(32 * q) << 16);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (half * 2 + i / 2 < n) {
+                        uint32_t r[32];
+                        tmem_ld32(from + 32 * i, r);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) sum[i][j] += __uint_as_float(r[j]);
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar_tempty + 8 * acc);
+                if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+            }
+            if (!go) break;
+            const int row = rt * 128 + 32 * q + lane;
+            if (p.splits > 1) {
+                float *to = p.partial + ((int64_t)item * 256 + half * 128) * 128 + 32 * q + lane;
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (half * 2 + i / 2 < n)
+#pragma unroll
+                        for (int j = 0; j < 32; ++j) to[(32 * i + j) * 128] = sum[i][j];
+            } else if (row < p.rows) {
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    if (half * 2 + i / 2 >= n) continue;
+                    const BoxAt at = box_at(p, rt, first + half * 2 + i / 2);
+                    const int c = at.c + 32 * (i & 1), here = min(32, p.channels - c);
+                    if (here > 0) store32(p, row, at.tap * p.channels + c, here, sum[i]);
+                }
+            }
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0 && p.status) atomicCAS(p.status, 0, (int)CRISP_TIMEOUT);
+        // copies that may still be in flight land before shared memory is released
+        const unsigned long long t0 = clock64();
+        while ((unsigned long long)(clock64() - t0) < 2000000ull) __nanosleep(1000);
+        __syncthreads();
+    }
+    if (warp == 2) {
+        tc_fence_after();
+        tmem_dealloc(tmem, 512);
+    }
+}
+
+// dW of a tile's 32 columns out of the parts of its tokens, added in their order: a warp reads four columns of 128 rows, then writes rows.
+__global__ void __launch_bounds__(256)
+add_parts_kernel(const __grid_constant__ Grad p) {
+    __shared__ float tile[32][129];
+    wait_for_prerequisites();
+    const int chunks = 2 * p.per, t = blockIdx.x / chunks, chunk = blockIdx.x - t * chunks;
+    const int rt = t / p.tiles_row, first = (t - rt * p.tiles_row) * p.per;
+    if (first + chunk / 2 >= p.boxes) return;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const float *from = p.partial + ((int64_t)t * p.splits * 256 + chunk * 32 + warp * 4) * 128 + lane * 4;
+    float4 sum[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum[i] = *reinterpret_cast<const float4 *>(from + i * 128);
+    for (int s = 1; s < p.splits; ++s) {
+        from += 256 * 128;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float4 v = *reinterpret_cast<const float4 *>(from + i * 128);
+            sum[i].x += v.x; sum[i].y += v.y; sum[i].z += v.z; sum[i].w += v.w;
+        }
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        float *to = &tile[warp * 4 + i][lane * 4];
+        to[0] = sum[i].x; to[1] = sum[i].y; to[2] = sum[i].z; to[3] = sum[i].w;
+    }
+    __syncthreads();
+    const BoxAt at = box_at(p, rt, first + chunk / 2);
+    const int c = at.c + 32 * (chunk & 1) + lane, col = at.tap * p.channels + c;
+    for (int r = warp; r < 128; r += 8) {
+        const int row = rt * 128 + r;
+        if (row >= p.rows) break;
+        if (c >= p.channels) continue;
+        float v = tile[lane][r];
+        if (p.nm_bits && !(p.nm_bits[(int64_t)row * p.wpr + (col >> 5)] >> (col & 31) & 1u)) v = 0.f;
+        const int64_t to = (int64_t)row * p.ld + col;
+        if (p.f32) {
+            float *w = reinterpret_cast<float *>(p.dw) + to;
+            *w = p.accumulate ? *w + v : v;
+        } else {
+            __nv_bfloat16 *w = reinterpret_cast<__nv_bfloat16 *>(p.dw) + to;
+            *w = __float2bfloat16_rn(p.accumulate ? __bfloat162float(*w) + v : v);
+        }
+    }
+}
+
+// Zeros in the blocks of dW that a row tile does not keep (128 x 128).
+__global__ void __launch_bounds__(256)
+zero_blocks_kernel(Geometry g, const int32_t *blk_col, void *dw, int64_t ld, int f32) {
+    wait_for_prerequisites();
+    const int rt = blockIdx.x / g.nblk, kb = blockIdx.x - rt * g.nblk;
+    int hit = 0;
+    for (int i = threadIdx.x; i < g.kkeep; i += 256) hit |= blk_col[(int64_t)rt * g.kkeep + i] == kb;
+    if (__syncthreads_or(hit)) return;
+    const int c = kb * 128 + (threadIdx.x & 127);
+    if (c >= g.k) return;
+    for (int r = rt * 128 + (threadIdx.x >> 7); r < min(g.rows, rt * 128 + 128); r += 2) {
+        if (f32) reinterpret_cast<float *>(dw)[(int64_t)r * ld + c] = 0.f;
+        else reinterpret_cast<uint16_t *>(dw)[(int64_t)r * ld + c] = 0;
+    }
+}
+
+// dY to [columns, rows] with a pitch that TMA takes, out of [rows, columns] or [columns, rows] of any pitch: tiles of 64 x 64.
+__global__ void __launch_bounds__(256)
+pack_dy_kernel(const uint16_t *dy, int64_t ld, int layout, int rows, int64_t ncols, uint16_t *to, int64_t pitch, int row_tiles) {
+    __shared__ uint16_t tile[64][66];
+    wait_for_prerequisites();
+    const int64_t u = blockIdx.x / row_tiles, t0 = u * 64;
+    const int r0 = (int)(blockIdx.x - u * row_tiles) * 64, x = threadIdx.x & 63, y = threadIdx.x >> 6;
+    for (int i = y; i < 64; i += 4) {
+        if (layout == 0) { if (r0 + i < rows && t0 + x < ncols) tile[x][i] = dy[(int64_t)(r0 + i) * ld + t0 + x]; }
+        else if (t0 + i < ncols && r0 + x < rows) tile[i][x] = dy[(t0 + i) * ld + r0 + x];
+    }
+    __syncthreads();
+    for (int i = y; i < 64; i += 4)
+        if (t0 + i < ncols && r0 + x < rows) to[(t0 + i) * pitch + r0 + x] = tile[i][x];
+}
+
+// ------------------------------------------------------------------------------------------------------------------- host
+
+bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
+int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
+
+struct GradPlan {
+    Grad p;
+    bool pack, k_major, blocks;                               // blocks: tiles follow the mask's list
+    int64_t pixels, cpitch, rpitch;                           // columns of x, pitches of x and of a packed dY
+    int ho, wo, batch;
+    size_t x_off, dy_off, partial_off, total;
+    int nrt;
+};
+
+crisp_status_t plan_grad(const crisp_weight_grad8_t *g, GradPlan *G) {
+    if (!g || (g->dy_layout != 0 && g->dy_layout != 1) || (g->dw_dtype != 0 && g->dw_dtype != 1) || (g->accumulate != 0 && g->accumulate != 1) || g->reserved != 0)
+        return CRISP_INVALID_ARG;
+    if (g->rows <= 0 || g->k <= 0 || g->ncols <= 0) return CRISP_BAD_SHAPE;
+    if (g->ncols > 0x7FFFFFFFll - 65536 || g->rows > 65535 * 32 || g->k > kMaxBlocksPerRowTile * 128) return CRISP_UNSUPPORTED;
+    *G = GradPlan{};
+    Grad &p = G->p;
+    p.rows = g->rows;
+    p.linear = g->conv == nullptr;
+    if (p.linear) {
+        p.channels = g->k; p.kernel_w = 1;
+        G->pixels = g->ncols; G->batch = 1; G->ho = 1; G->wo = (int)g->ncols;
+        p.tw = kStep; p.th = p.tb = 1;
+    } else {
+        const crisp_conv_desc_t &c = *g->conv;
+        if (c.batch <= 0 || c.height <= 0 || c.width <= 0 || c.channels <= 0 || c.kernel_h <= 0 || c.kernel_w <= 0 || c.pad < 0) return CRISP_BAD_SHAPE;
+        const int64_t ho = (int64_t)c.height + 2 * (int64_t)c.pad - c.kernel_h + 1, wo = (int64_t)c.width + 2 * (int64_t)c.pad - c.kernel_w + 1;
+        if (ho <= 0 || wo <= 0 || (int64_t)c.kernel_h * c.kernel_w > g->k || (int64_t)c.kernel_h * c.kernel_w * c.channels != g->k) return CRISP_BAD_SHAPE;
+        if (ho > 0x7FFFFFFF || wo > 0x7FFFFFFF || ho > g->ncols || wo > g->ncols || c.batch > g->ncols || (double)c.batch * (double)ho * (double)wo != (double)g->ncols)
+            return CRISP_BAD_SHAPE;
+        if ((double)c.batch * c.height * c.width > 2147418112.0) return CRISP_UNSUPPORTED;
+        p.channels = c.channels; p.kernel_w = c.kernel_w; p.pad = c.pad;
+        G->pixels = (int64_t)c.batch * c.height * c.width; G->batch = c.batch; G->ho = (int)ho; G->wo = (int)wo;
+        // the box of 64 output pixels that covers the fewest outside the images, the widest of them
+        int64_t best = -1;
+        for (int tw = kStep; tw >= 1; tw >>= 1)
+            for (int th = kStep / tw; th >= 1; th >>= 1) {
+                const int tb = kStep / tw / th;
+                const int64_t n = up(wo, tw) * up(ho, th) * up(c.batch, tb);
+                if (best < 0 || n < best) { best = n; p.tw = tw; p.th = th; p.tb = tb; }
+            }
+    }
+    p.nx = (int)up(G->wo, p.tw); p.ny = (int)up(G->ho, p.th);
+    const int64_t chunks = (int64_t)p.nx * p.ny * up(G->batch, p.tb);
+    if (chunks > 0x7FFFFFFFll - 4096) return CRISP_UNSUPPORTED;
+    p.chunks = (int)chunks;
+    p.cboxes = (int)up(p.channels, 64);
+    G->nrt = (int)up(p.rows, 128);
+    const int taps = g->k / p.channels;
+    p.boxes = taps * p.cboxes;
+    if (g->mask) {
+        const Geometry &m = g->mask->g;
+        if (m.rows != g->rows || m.k != g->k) return CRISP_BAD_SHAPE;
+        p.nm_bits = g->mask->d_nm_bits; p.wpr = m.wpr;
+        G->blocks = m.bm == 128 && m.bk == 128 && (taps == 1 || p.channels % 128 == 0);
+        if (G->blocks && m.kkeep < m.nblk) { p.blk_col = g->mask->d_blk_col; p.kkeep = m.kkeep; p.boxes = 2 * m.kkeep; }
+        else G->blocks = false;
+    }
+    size_t at = 0;
+    if (p.boxes > 0) {
+        p.tiles_row = (int)up(p.boxes, kBoxes);
+        p.per = (int)up(p.boxes, p.tiles_row);
+        if (p.blk_col) p.per = kBoxes;                        // (two blocks a tile)
+        p.tiles_row = (int)up(p.boxes, p.per);
+        const int64_t tiles = (int64_t)G->nrt * p.tiles_row;
+        if (tiles > (1 << 24)) return CRISP_UNSUPPORTED;
+        // parts of the tokens where there are fewer tiles than SMs, of 256 tokens at least
+        int64_t splits = std::max<int64_t>(1, std::min<int64_t>(148 / tiles, p.chunks / 4));
+        p.chunks_split = (int)up(p.chunks, splits);
+        p.splits = (int)up(p.chunks, p.chunks_split);
+        p.items = (int)(tiles * p.splits);
+        G->cpitch = up(p.channels, 64) * 64;
+        G->x_off = 0;
+        at = align_up((size_t)G->pixels * G->cpitch * 2);
+        const bool fits = aligned_to(g->d_dy, 16) && g->ld_dy % 8 == 0;
+        G->k_major = g->dy_layout == 0 && p.linear && fits;
+        G->pack = !G->k_major && !(g->dy_layout == 1 && fits);
+        if (G->pack) {
+            G->rpitch = up(p.rows, 8) * 8;
+            G->dy_off = at;
+            at += align_up((size_t)g->ncols * G->rpitch * 2);
+        }
+        if (p.splits > 1) {
+            G->partial_off = at;
+            at += (size_t)p.items * 256 * 128 * sizeof(float);
+        }
+    }
+    G->total = at;
+    return CRISP_OK;
+}
+
+template <bool kAMn>
+cudaError_t launch_grad(const CUtensorMap &a, const CUtensorMap &b, const Grad &p, int sms, int device, cudaStream_t st) {
+    static std::atomic<uint64_t> ready{0};
+    if (device >= 64 || !(ready.load(std::memory_order_relaxed) >> device & 1)) {
+        const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(grad8_kernel<kAMn>), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGradSmem);
+        if (e != cudaSuccess) return e;
+        if (device < 64) ready.fetch_or(1ull << device, std::memory_order_relaxed);
+    }
+    return launch_chained(grad8_kernel<kAMn>, (unsigned)std::min(p.items, sms), kGradThreads, kGradSmem, st, a, b, p);
+}
+
+cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cudaStream_t st) {
+    Grad &p = G.p;
+    cudaError_t e;
+    p.dw = g.d_dw; p.ld = g.ld_dw; p.f32 = g.dw_dtype; p.accumulate = g.accumulate;
+    p.vec = aligned_to(g.d_dw, 16) && g.ld_dw * (g.dw_dtype ? 4 : 2) % 16 == 0;
+    p.status = g.d_status;
+    p.wait_limit = kWaitLimitCycles;
+    p.skip_fill = -1;
+    if (G.blocks && !g.accumulate) {
+        const Geometry &m = g.mask->g;
+        e = launch_chained(zero_blocks_kernel, (unsigned)(m.nrt * m.nblk), 256, 0, st, m, g.mask->d_blk_col, g.d_dw, g.ld_dw, g.dw_dtype);
+        if (e != cudaSuccess) return e;
+    }
+    if (p.boxes == 0) return cudaSuccess;
+    int device = 0;
+    e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    e = ensure_context(device);
+    if (e != cudaSuccess) return e;
+    uint16_t *x = reinterpret_cast<uint16_t *>(ws + G.x_off);
+    p.partial = reinterpret_cast<float *>(ws + G.partial_off);
+    e = launch_dequantize8(reinterpret_cast<const uint8_t *>(g.d_act), 1, p.channels, G.pixels, x, G.cpitch, st);
+    if (e != cudaSuccess) return e;
+    const uint16_t *dy = g.d_dy;
+    int64_t ld = g.ld_dy;
+    if (G.pack) {
+        uint16_t *to = reinterpret_cast<uint16_t *>(ws + G.dy_off);
+        const int64_t row_tiles = up(p.rows, 64), ctas = row_tiles * up(g.ncols, 64);
+        if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
+        e = launch_chained(pack_dy_kernel, (unsigned)ctas, 256, 0, st, g.d_dy, g.ld_dy, g.dy_layout, p.rows, g.ncols, to, G.rpitch, (int)row_tiles);
+        if (e != cudaSuccess) return e;
+        dy = to; ld = G.rpitch;
+    }
+    CUtensorMap a, b;
+    const uint64_t W = g.conv ? g.conv->width : g.ncols, H = g.conv ? g.conv->height : 1, N = G.batch;
+    const uint32_t box[4] = {64u, (uint32_t)p.tw, (uint32_t)p.th, (uint32_t)p.tb};
+    const uint64_t xd[4] = {(uint64_t)p.channels, W, H, N}, xs[3] = {(uint64_t)G.cpitch * 2, W * G.cpitch * 2, W * H * G.cpitch * 2};
+    if (!make_map_4d(&b, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, x, xd, xs, box)) return cudaErrorInvalidValue;
+    if (G.k_major) {
+        if (!make_map_2d(&a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dy, (uint64_t)g.ncols, (uint64_t)p.rows, (uint64_t)ld, 64, 128)) return cudaErrorInvalidValue;
+    } else {
+        const uint64_t wo = G.wo, ho = G.ho, yd[4] = {(uint64_t)p.rows, wo, ho, N}, ys[3] = {(uint64_t)ld * 2, wo * ld * 2, wo * ho * ld * 2};
+        if (!make_map_4d(&a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dy, yd, ys, box)) return cudaErrorInvalidValue;
+    }
+    const int sms = sm_count_of(device);
+    e = G.k_major ? launch_grad<false>(a, b, p, sms, device, st) : launch_grad<true>(a, b, p, sms, device, st);
+    if (e == cudaSuccess && p.splits > 1)
+        e = launch_chained(add_parts_kernel, (unsigned)(G.nrt * p.tiles_row * 2 * p.per), 256, 0, st, p);
+    return e;
+}
+
+}  // namespace
+
+}  // namespace crisp
+
+extern "C" {
+
+using namespace crisp;
+
+crisp_status_t crisp_weight_grad8_sizes(const crisp_weight_grad8_t *grad, size_t *workspace_bytes) {
+    GradPlan G;
+    const crisp_status_t bad = plan_grad(grad, &G);
+    if (bad != CRISP_OK) return bad;
+    if (!workspace_bytes) return CRISP_INVALID_ARG;
+    *workspace_bytes = G.total;
+    return CRISP_OK;
+}
+
+crisp_status_t crisp_weight_grad8(const crisp_weight_grad8_t *grad, void *d_workspace, void *stream) {
+    GradPlan G;
+    const crisp_status_t bad = plan_grad(grad, &G);
+    if (bad != CRISP_OK) return bad;
+    const crisp_weight_grad8_t &g = *grad;
+    if (!g.d_dy || !g.d_act || !g.d_dw || (!d_workspace && G.total) || !aligned_to(g.d_dy, 2) || !aligned_to(g.d_act, kAlign) || !aligned_to(g.d_dw, g.dw_dtype ? 4 : 2) ||
+        !aligned_to(g.d_status, 4) || !aligned_to(d_workspace, kAlign))
+        return CRISP_INVALID_ARG;
+    if (g.ld_dy < (g.dy_layout ? (int64_t)g.rows : g.ncols) || g.ld_dw < g.k) return CRISP_BAD_SHAPE;
+    size_t bytes = 0;
+    if (crisp_quantize8_sizes(G.p.channels, G.pixels, &bytes) != CRISP_OK) return CRISP_UNSUPPORTED;
+    const cudaError_t e = run_grad(g, G, reinterpret_cast<uint8_t *>(d_workspace), (cudaStream_t)stream);
+    return e == cudaSuccess ? CRISP_OK : e == cudaErrorInvalidValue ? CRISP_UNSUPPORTED : CRISP_CUDA_ERROR;
+}
+
+}  // extern "C"
