@@ -4,13 +4,16 @@
 //   h = (x - mean) rstd      y = act(p), p = gamma h + beta
 //   backward:  e = dy act'(p)   dbeta = sum e   dgamma = sum e h   dx = rstd (gamma e - m1 - h m2),  m1, m2 = the group's means of gamma e, gamma e h
 //
-// Bound by memory: each value is needed twice, and what counts is that it comes from DRAM once.  A cluster of CTAs takes one sample's slice of whole groups; every
-// thread keeps the values that it has read in shared memory of its own (no barrier: it reads what it wrote) until the cluster's sums are there, and reads again what
-// does not fit.  Where one cluster's share of the SMs would be too few (one large image), and for groups of more channels than a slice holds, the same code runs as two
-// kernels with the partial sums in between.
+// Bound by memory: each value is needed twice, and what counts is that it comes from DRAM once.  A CTA takes some pixels of a sample's slice of channels, every thread
+// keeps what it has read in shared memory of its own (no barrier: it reads what it wrote), and when the sums of all CTAs of the slice are there, it finishes its pixels.
 //
-// A thread holds V = 16 bytes' worth of consecutive channels and goes over pixels.  Sums: each thread's values about its first one, so that a mean far from zero costs no
-// digits; then mean = sum n_i mean_i / n and M2 = sum M2_i + n_i (mean_i - mean)^2 over threads and over CTAs, always in the same order.
+//   small calls   a slice's CTAs are a cluster, and read one another's sums
+//   large ones    a cooperative launch of as many CTAs as fit, which go over the tiles of all samples in order and pass their sums through memory.  A slice of more
+//                 tiles than CTAs (27 MB) is read twice
+//
+// A thread holds V = 16 bytes' worth of consecutive channels and goes over pixels, two channels an instruction: per pair p = a x + b (a = gamma rstd, b = beta - mean a),
+// dx = a e + B x + C.  Forward sums are about the thread's first value, so that a mean far from zero costs no digits; then mean = sum n_i mean_i / n and
+// M2 = sum M2_i + n_i (mean_i - mean)^2 over threads and over CTAs, always in the same order.
 #include <cuda_bf16.h>
 #include <cuda_fp16.h>
 
@@ -20,6 +23,7 @@
 
 #include "block8.h"
 #include "block8.cuh"
+#include "mask_common.cuh"
 
 namespace crisp {
 
@@ -32,7 +36,6 @@ constexpr int kMaxCluster = 16;
 constexpr size_t kMaxSmem = 232448 - 1024;
 
 enum Act { kNone = 0, kRelu = 1, kRelu6 = 2, kSilu = 3 };
-enum Mode { kWhole = 0, kSums = 1, kApply = 2 };          // one kernel with clusters, or the first and the second of two
 
 struct Norm {
     const void *x, *dy;                  // dy: backward
@@ -41,67 +44,87 @@ struct Norm {
     uint8_t *x8, *y8;                    // forward: 8-bit forms to write, or nullptr
     const float *gamma, *beta;           // or nullptr: 1, 0
     float *stats;                        // [batch, groups, 2]
-    float2 *partial;                     // two kernels: [batch, groups, p_ranks, parts]
     float *sums;                         // backward: [batch * ranks][2][channels]
+    float2 *partial;                     // large calls: [batch, groups, ranks, parts]
+    uint32_t *arrived;                   // and CTAs whose pairs are there, of each unit (0 when the call begins)
+    uint32_t tiles, unit;                // all tiles; those whose sums meet: of a slice, or of a sample where groups lie in several slices
     int64_t ldx, ld_dy, ld_out;
-    int64_t cols8, groups8, chunks8;     // 8-bit form: columns (pixels of all samples), their groups of 8 and of 128
+    int64_t groups8, chunks8;            // 8-bit form: groups of 8 and of 128 columns (pixels of all samples)
     size_t scale_off;
     int pixels, channels, groups, cpg;   // cpg: channels a group
-    int width, slices;                   // channels a slice (kWhole: whole groups), slices a sample
+    int width, slices;                   // channels a slice, slices a sample
     int ranks, per;                      // CTAs of a sample's slice, pixels of one
-    int p_width, p_ranks, p_per, parts;  // the same of the kernel that fills `partial`, and the most slices that a group lies in there
+    int parts;                           // the most slices that a group lies in
     int cv, lanes;                       // threads a pixel, pixels at a time
     int resident;                        // items (V channels of a pixel) that a thread keeps
+    uint32_t across_magic;               // 2^32 / (entries of a whole group and lane), rounded up
     int act, vec, vec_dy, vec_out;       // vec: addresses and pitches allow 16 bytes at once
     float eps;
 };
 
+// V values as pairs.
 template <typename T>
 struct Of;
 template <>
 struct Of<float> {
     static constexpr int V = 4;
-    static __device__ __forceinline__ void open(const uint4 &u, float (&f)[4]) {
-        f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+    static __device__ __forceinline__ void open(const uint4 &u, uint64_t (&f)[2]) {
+        f[0] = f32x2(__uint_as_float(u.x), __uint_as_float(u.y)); f[1] = f32x2(__uint_as_float(u.z), __uint_as_float(u.w));
     }
-    static __device__ __forceinline__ uint4 close(const float (&f)[4]) {
-        return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+    static __device__ __forceinline__ uint4 close(const uint64_t (&f)[2]) {
+        const float2 a = f32x2_halves(f[0]), b = f32x2_halves(f[1]);
+        return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
     }
     static __device__ __forceinline__ float sigmoid(float p) { return 1.f / (1.f + expf(-p)); }
 };
-template <>
-struct Of<__nv_bfloat16> {
+struct Of16 {
     static constexpr int V = 8;
-    static __device__ __forceinline__ void open(const uint4 &u, float (&f)[8]) {
-        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { const float2 v = floats(w[i]); f[2 * i] = v.x; f[2 * i + 1] = v.y; }
-    }
-    static __device__ __forceinline__ uint4 close(const float (&f)[8]) {
-        uint32_t w[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) { const __nv_bfloat162 b = __floats2bfloat162_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t *>(&b); }
-        return make_uint4(w[0], w[1], w[2], w[3]);
-    }
     // (some 2^-21 of the value, far below the result's last place)
     static __device__ __forceinline__ float sigmoid(float p) { return __fdividef(1.f, 1.f + __expf(-p)); }
 };
 template <>
-struct Of<__half> {
-    static constexpr int V = 8;
-    static __device__ __forceinline__ void open(const uint4 &u, float (&f)[8]) {
+struct Of<__nv_bfloat16> : Of16 {
+    static __device__ __forceinline__ void open(const uint4 &u, uint64_t (&f)[4]) {
         const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&w[i])); f[2 * i] = v.x; f[2 * i + 1] = v.y; }
+        for (int i = 0; i < 4; ++i) f[i] = f32x2(__uint_as_float(w[i] << 16), __uint_as_float(w[i] & 0xFFFF0000u));
     }
-    static __device__ __forceinline__ uint4 close(const float (&f)[8]) {
+    static __device__ __forceinline__ uint4 close(const uint64_t (&f)[4]) {
         uint32_t w[4];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) { const __half2 b = __floats2half2_rn(f[2 * i], f[2 * i + 1]); w[i] = *reinterpret_cast<const uint32_t *>(&b); }
+        for (int i = 0; i < 4; ++i) {
+            const float2 v = f32x2_halves(f[i]);
+            const __nv_bfloat162 b = __floats2bfloat162_rn(v.x, v.y);
+            w[i] = *reinterpret_cast<const uint32_t *>(&b);
+        }
         return make_uint4(w[0], w[1], w[2], w[3]);
     }
-    static __device__ __forceinline__ float sigmoid(float p) { return __fdividef(1.f, 1.f + __expf(-p)); }
 };
+template <>
+struct Of<__half> : Of16 {
+    static __device__ __forceinline__ void open(const uint4 &u, uint64_t (&f)[4]) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int i = 0; i < 4; ++i) { const float2 v = __half22float2(*reinterpret_cast<const __half2 *>(&w[i])); f[i] = f32x2(v.x, v.y); }
+    }
+    static __device__ __forceinline__ uint4 close(const uint64_t (&f)[4]) {
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float2 v = f32x2_halves(f[i]);
+            const __half2 b = __floats2half2_rn(v.x, v.y);
+            w[i] = *reinterpret_cast<const uint32_t *>(&b);
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    }
+};
+
+__device__ __forceinline__ uint64_t fma2(uint64_t a, uint64_t b, uint64_t c) {
+    uint64_t r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ uint64_t both(float v) { return f32x2(v, v); }
 
 __device__ __forceinline__ uint32_t smem_at(const void *p) { return static_cast<uint32_t>(__cvta_generic_to_shared(p)); }
 template <int kBytes>
@@ -111,11 +134,11 @@ __device__ __forceinline__ void copy_async(void *to, const void *from) {
 }
 __device__ __forceinline__ void copies_done() { asm volatile("cp.async.wait_all;" ::: "memory"); }
 
-// V channels of one pixel, `n` of them there (the others 0).
-template <typename T>
+// V channels of one pixel, `n` of them there (the others 0).  kVec: all of them, at a multiple of 16 bytes.
+template <bool kVec, typename T>
 __device__ __forceinline__ uint4 fetch(const T *p, int vec, int n) {
     constexpr int V = Of<T>::V;
-    if (vec && n == V) return *reinterpret_cast<const uint4 *>(p);
+    if (kVec || (vec && n == V)) return *reinterpret_cast<const uint4 *>(p);
     uint32_t w[4] = {0, 0, 0, 0};
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -125,10 +148,10 @@ __device__ __forceinline__ uint4 fetch(const T *p, int vec, int n) {
         }
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
-template <typename T>
+template <bool kVec, typename T>
 __device__ __forceinline__ void put(T *p, const uint4 &u, int vec, int n) {
     constexpr int V = Of<T>::V;
-    if (vec && n == V) { *reinterpret_cast<uint4 *>(p) = u; return; }
+    if (kVec || (vec && n == V)) { *reinterpret_cast<uint4 *>(p) = u; return; }
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -146,48 +169,47 @@ __device__ __forceinline__ int64_t codes_at(const Norm &q, int64_t col, int ch) 
 __device__ __forceinline__ int64_t scale_at(const Norm &q, int64_t col, int ch) {
     return (int64_t)q.scale_off + ((int64_t)(ch >> 7) * q.chunks8 + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4;
 }
-// The values f of V channels (0 behind the last channel) to 8 bits; the 128 / V threads of a block are neighbours in a warp and all call this.
+// The values of V channels (0 behind the last channel) to 8 bits; the 128 / V threads of a block are neighbours in a warp and all call this.
 template <int V>
-__device__ __forceinline__ void hold(const Norm &q, uint8_t *to, const float (&f)[V], int64_t col, int ch) {
-    float top = 0.f;
+__device__ __forceinline__ void hold(const Norm &q, uint8_t *to, const uint64_t (&pairs)[V / 2], int64_t col, int ch) {
+    float f[V], top = 0.f;
 #pragma unroll
-    for (int j = 0; j < V; ++j) top = fmaxf(top, fabsf(f[j]) < INFINITY ? fabsf(f[j]) : 0.f);         // what is not finite leaves the scale alone
+    for (int j = 0; j < V; j += 2) {
+        const float2 v = f32x2_halves(pairs[j / 2]);
+        f[j] = v.x; f[j + 1] = v.y;
+        top = max_nan(top, max_nan(fabsf(v.x), fabsf(v.y)));
+    }
+    if (!(top < INFINITY)) {                                             // what is not finite becomes NaN and leaves the scale alone
+        top = 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            if (fabsf(f[j]) < INFINITY) top = fmaxf(top, fabsf(f[j]));
+            else f[j] = NAN;
+        }
+    }
     uint32_t bits = __float_as_uint(top);
-    const uint32_t lane = threadIdx.x & 31;
-    const uint32_t peers = V == 4 ? 0xFFFFFFFFu : 0xFFFFu << (lane & 16);
+    const uint32_t peers = V == 4 ? 0xFFFFFFFFu : 0xFFFFu << (threadIdx.x & 16);
 #pragma unroll
     for (int d = 64 / V; d; d >>= 1) bits = max(bits, __shfl_xor_sync(peers, bits, d));
     const uint32_t e = (uint32_t)max((int)((bits + (0x7FFFFFu - 0x600000u)) >> 23) - 8, 1);
     const float down = power_of(254u - e);
     uint32_t codes[V / 4];
 #pragma unroll
-    for (int j = 0; j < V; j += 4) {
-        float s[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) s[i] = fabsf(f[j + i]) < INFINITY ? f[j + i] * down : NAN;
-        codes[j / 4] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(s[0], s[1]), __NV_SATFINITE, __NV_E4M3) |
-                       (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(s[2], s[3]), __NV_SATFINITE, __NV_E4M3) << 16;
-    }
+    for (int j = 0; j < V; j += 4)
+        codes[j / 4] = (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f[j] * down, f[j + 1] * down), __NV_SATFINITE, __NV_E4M3) |
+                       (uint32_t)__nv_cvt_float2_to_fp8x2(make_float2(f[j + 2] * down, f[j + 3] * down), __NV_SATFINITE, __NV_E4M3) << 16;
     uint8_t *at = to + codes_at(q, col, ch);
     if constexpr (V == 8) *reinterpret_cast<uint2 *>(at) = make_uint2(codes[0], codes[1]);
     else *reinterpret_cast<uint32_t *>(at) = codes[0];
     if ((ch & 127) == 0) *reinterpret_cast<uint32_t *>(to + scale_at(q, col, ch)) = e * 0x01010101u;
 }
 
-template <int kAct, typename T>
-__device__ __forceinline__ float activate(float p) {
-    if constexpr (kAct == kRelu) return p < 0.f ? 0.f : p;                     // (NaN stays)
-    if constexpr (kAct == kRelu6) return p < 0.f ? 0.f : p > 6.f ? 6.f : p;
-    if constexpr (kAct == kSilu) return p * Of<T>::sigmoid(p);
-    return p;
-}
-
-// A CTA's place: sample, first channel, channels, groups, pixels.
+// A CTA's place: sample, first channel, channels, groups that it meets, pixels.
 struct Place {
     int n, slice, rank, c0, width, g0, ng, px0, px1;
-    __device__ __forceinline__ Place(const Norm &q) {
-        const uint32_t u = blockIdx.x / (uint32_t)q.ranks;
-        rank = (int)(blockIdx.x - u * (uint32_t)q.ranks);
+    __device__ __forceinline__ Place(const Norm &q, uint32_t cta) {
+        const uint32_t u = cta / (uint32_t)q.ranks;
+        rank = (int)(cta - u * (uint32_t)q.ranks);
         n = (int)(u / (uint32_t)q.slices);
         slice = (int)(u - (uint32_t)n * (uint32_t)q.slices);
         c0 = slice * q.width; width = min(q.width, q.channels - c0);
@@ -195,11 +217,38 @@ struct Place {
         px0 = min(rank * q.per, q.pixels); px1 = min(px0 + q.per, q.pixels);
     }
 };
+// A thread's place in it: its pixel lane, channels, items and first row.
+template <typename T>
+struct Mine {
+    int lane, v, ch, n, items;
+    int64_t row0;
+    __device__ __forceinline__ Mine(const Norm &q, const Place &at);
+};
 __device__ __forceinline__ int items_of(int pixels, int lane, int lanes) { return pixels > lane ? (pixels - lane + lanes - 1) / lanes : 0; }
+template <typename T>
+__device__ __forceinline__ Mine<T>::Mine(const Norm &q, const Place &at) {
+    constexpr int V = Of<T>::V;
+    lane = (int)((uint32_t)threadIdx.x / (uint32_t)q.cv); v = (int)threadIdx.x - lane * q.cv;
+    ch = at.c0 + v * V;
+    n = lane < q.lanes ? max(0, min(V, at.c0 + at.width - ch)) : 0;
+    items = lane < q.lanes ? items_of(at.px1 - at.px0, lane, q.lanes) : 0;
+    row0 = (int64_t)at.n * q.pixels + at.px0 + lane;
+}
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
     for (int d = 16; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
+    return v;
+}
+
+// How many neighbouring lanes share a group when `groups` of them are gone through (a power of two), and a sum over them.
+__device__ __forceinline__ int sharers(int groups) {
+    int k = 32;
+    while (k > 1 && groups * k > kThreads) k >>= 1;
+    return k;
+}
+__device__ __forceinline__ float shared_sum(float v, int k) {
+    for (int d = k >> 1; d; d >>= 1) v += __shfl_xor_sync(0xFFFFFFFFu, v, d);
     return v;
 }
 
@@ -208,454 +257,638 @@ struct Span { int lo, hi; };
 __device__ __forceinline__ Span span_of(const Norm &q, const Place &at, int g) {
     return {max(at.c0, (at.g0 + g) * q.cpg) - at.c0, min(at.c0 + at.width, (at.g0 + g + 1) * q.cpg) - at.c0};
 }
-// kSums: where the CTA's pair of group g goes.
+// Large calls: where the CTA's pair of group g goes.
 __device__ __forceinline__ float2 *partial_at(const Norm &q, const Place &at, int g) {
     const int64_t group = at.g0 + g;
-    return q.partial + (((int64_t)at.n * q.groups + group) * q.p_ranks + at.rank) * q.parts + (at.slice - (int)(group * q.cpg / q.p_width));
+    return q.partial + (((int64_t)at.n * q.groups + group) * q.ranks + at.rank) * q.parts + (at.slice - (int)(group * q.cpg / q.width));
 }
-// A pair of each group of the slice, of all CTAs: kWhole: `own` [ng] in their shared memory; kApply: `partial`.  combine(g, count, lane, read, weight) is called by one
-// warp a group; read(i) is the i-th pair and weight(i) the number of values that it stands for.
-template <int kMode, typename F>
-__device__ __forceinline__ void of_all(const Norm &q, const Place &at, const float2 *own, F combine) {
-    const int lane = threadIdx.x & 31;
-    if constexpr (kMode == kWhole) {
-        cluster_arrive();
-        cluster_wait();
-    }
-    for (int g = threadIdx.x >> 5; g < at.ng; g += kThreads / 32) {
-        if constexpr (kMode == kWhole) {
-            const uint32_t mine = smem_at(own + g);
-            combine(g, q.ranks, lane,
-                    [&](int i) {
-                        const uint32_t a = peer_address(mine, (uint32_t)i);
-                        return make_float2(__uint_as_float(lds32_peer(a)), __uint_as_float(lds32_peer(a + 4)));
-                    },
-                    [&](int i) { const int first = min(i * q.per, q.pixels); return (float)(min(first + q.per, q.pixels) - first) * (float)q.cpg; });
-        } else {
-            const int64_t group = at.g0 + g;
-            const int from = (int)(group * q.cpg), to = from + q.cpg, s0 = from / q.p_width, parts = (to - 1) / q.p_width + 1 - s0;
-            const float2 *row = q.partial + ((int64_t)at.n * q.groups + group) * q.p_ranks * q.parts;
-            combine(g, q.p_ranks * parts, lane,
-                    [&](int i) { const int r = i / parts; return row[r * q.parts + i - r * parts]; },
-                    [&](int i) {
-                        const int r = i / parts, s = s0 + i - r * parts, first = min(r * q.p_per, q.pixels);
-                        return (float)(min(first + q.p_per, q.pixels) - first) * (float)(min(to, (s + 1) * q.p_width) - max(from, s * q.p_width));
-                    });
-        }
+// combine(g, k, lane, count, read, weight) for the groups of the slice, by k neighbouring lanes each (all lanes of a warp call it together, g < ng or not); read(i) is
+// the i-th CTA's pair of the group, weight(i) the number of values that it stands for.
+template <typename R, typename F>
+__device__ __forceinline__ void of_groups(const Place &at, R reader, F combine) {
+    const int k = sharers(at.ng), lane = threadIdx.x & (k - 1);
+    for (int g0 = 0; g0 < at.ng; g0 += kThreads / k) {
+        const int g = g0 + threadIdx.x / k;
+        reader(min(g, at.ng - 1), [&](int count, auto read, auto weight) { combine(g, k, lane, count, read, weight); });
     }
     __syncwarp();
-    if constexpr (kMode == kWhole) cluster_arrive();         // (its wait is at the kernel's end: no CTA leaves while others read from it)
+}
+// In a cluster: `own` [ng] in the CTAs' shared memory.
+template <typename F>
+__device__ __forceinline__ void of_cluster(const Norm &q, const Place &at, const float2 *own, F combine) {
+    cluster_arrive();
+    cluster_wait();
+    of_groups(at, [&](int g, auto call) {
+        const uint32_t mine = smem_at(own + g);
+        call(q.ranks,
+             [&](int i) {
+                 const uint32_t a = peer_address(mine, (uint32_t)i);
+                 return make_float2(__uint_as_float(lds32_peer(a)), __uint_as_float(lds32_peer(a + 4)));
+             },
+             [&](int i) { const int first = min(i * q.per, q.pixels); return (float)(min(first + q.per, q.pixels) - first) * (float)q.cpg; });
+    }, combine);
+    cluster_arrive();                                        // (its wait is at the kernel's end: no CTA leaves while others read from it)
     __syncthreads();
+}
+// Large calls: out of `partial`, when all of the unit have written theirs.
+template <typename F>
+__device__ __forceinline__ void of_memory(const Norm &q, const Place &at, F combine) {
+    of_groups(at, [&](int g, auto call) {
+        const int64_t group = at.g0 + g, from = group * q.cpg, to = from + q.cpg;
+        const int s0 = (int)(from / q.width), parts = q.parts == 1 ? 1 : (int)((to - 1) / q.width) + 1 - s0;
+        const float2 *row = q.partial + ((int64_t)at.n * q.groups + group) * q.ranks * q.parts;
+        call(q.ranks * parts,
+             [&](int i) { const int r = parts == 1 ? i : i / parts; return __ldcg(row + r * q.parts + i - r * parts); },
+             [&](int i) {
+                 const int r = parts == 1 ? i : i / parts, first = min(r * q.per, q.pixels);
+                 const int64_t s = s0 + i - r * parts;
+                 return (float)(min(first + q.per, q.pixels) - first) * (float)(min(to, (s + 1) * q.width) - max(from, s * q.width));
+             });
+    }, combine);
+    __syncthreads();
+}
+// The CTA's pairs are written: says so.  (All threads call it.)
+__device__ __forceinline__ void arrive(const Norm &q, uint32_t unit) {
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        __threadfence();
+        atomicAdd(q.arrived + unit, 1u);
+    }
+}
+// Waits for those of the whole unit; false where they do not come within some two seconds (the others run, the launch is cooperative): the results are NaN then.
+__device__ __forceinline__ bool all_here(const Norm &q, uint32_t unit) {
+    __shared__ int here;
+    if (threadIdx.x == 0) {
+        uint32_t n = 0;
+        const long long t0 = clock64();
+        for (;;) {
+            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(n) : "l"(q.arrived + unit) : "memory");
+            if (n >= q.unit || clock64() - t0 > 4000000000ll) break;
+            __nanosleep(64);
+        }
+        here = n >= q.unit;
+        __threadfence();
+    }
+    __syncthreads();
+    return here != 0;
 }
 
 // ---------------------------------------------------------------------------------------------------------------- forward
 
-// kOne: a thread's channels are of one group.
-template <typename T, bool kOne, int kMode>
+// Pairs (mean, M2) of the CTA's groups to give(g, pair), out of what its threads have kept.
+template <typename T, bool kOne, bool kVec, typename F>
+__device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine<T> &me, float2 *threads, const uint4 *kept, F give) {
+    constexpr int V = Of<T>::V, P = V / 2;
+    uint64_t away[kOne ? 1 : P], s1[P], s2[P];               // away: less the thread's first values (kOne: its very first)
+#pragma unroll
+    for (int j = 0; j < P; ++j) s1[j] = s2[j] = 0;
+#pragma unroll
+    for (int j = 0; j < (kOne ? 1 : P); ++j) away[j] = 0;
+    if (me.n > 0 && me.items > 0) {
+        uint64_t f[P];
+        Of<T>::open(kept[0], f);
+#pragma unroll
+        for (int j = 0; j < (kOne ? 1 : P); ++j) { const float2 v = f32x2_halves(f[j]); away[j] = f32x2(-v.x, kOne ? -v.x : -v.y); }
+#pragma unroll 2
+        for (int i = 0; i < me.items; ++i) {
+            Of<T>::open(kept[i * kThreads], f);
+#pragma unroll
+            for (int j = 0; j < P; ++j) { const uint64_t d = add2(f[j], away[kOne ? 0 : j]); s1[j] = add2(s1[j], d); s2[j] = fma2(d, d, s2[j]); }
+        }
+    }
+    const float count = (float)me.items;
+    if constexpr (kOne) {                                    // (mean, M2) of the thread
+        const float one = f32x2_sum(P == 4 ? add2(add2(s1[0], s1[1]), add2(s1[P - 2], s1[P - 1])) : add2(s1[0], s1[1]));
+        const float two = f32x2_sum(P == 4 ? add2(add2(s2[0], s2[1]), add2(s2[P - 2], s2[P - 1])) : add2(s2[0], s2[1]));
+        const float d = me.items ? one / (count * V) : 0.f;
+        threads[threadIdx.x] = make_float2(d - f32x2_halves(away[0]).x, max_nan(0.f, fmaf(-one, d, two)));
+    } else {                                                 // of each channel
+        const float over = me.items ? 1.f / count : 0.f;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            const float2 a = f32x2_halves(away[j / 2]), b = f32x2_halves(s1[j / 2]), c = f32x2_halves(s2[j / 2]);
+            const float first = j & 1 ? -a.y : -a.x, one = j & 1 ? b.y : b.x, two = j & 1 ? c.y : c.x, d = one * over;
+            threads[threadIdx.x * V + j] = make_float2(first + d, max_nan(0.f, fmaf(-one, d, two)));
+        }
+    }
+    __syncthreads();
+    const int pixels = at.px1 - at.px0, k = sharers(at.ng), lane = threadIdx.x & (k - 1);
+    for (int g0 = 0; g0 < at.ng; g0 += kThreads / k) {
+        const int g = g0 + threadIdx.x / k;
+        const Span in = span_of(q, at, min(g, at.ng - 1));
+        const int wide = in.hi - in.lo, across = kOne ? (wide + V - 1) / V : wide, entries = across * q.lanes;       // entries of a group: `across` a lane
+        const float total = (float)pixels * (float)wide;
+        const bool as_all = wide == q.cpg;
+        const auto entry = [&](int i, float *weight) {
+            // (a product instead of a division: exact for i below 2^16, which entries are)
+            const int l = across == 1 ? i : as_all ? (int)__umulhi((uint32_t)i, q.across_magic) : i / across, a = i - l * across;
+            const float here = (float)items_of(pixels, l, q.lanes);
+            *weight = kOne ? here * V : here;
+            return threads[kOne ? l * q.cv + in.lo / V + a : l * q.cv * V + in.lo + a];
+        };
+        // (about the first entry's mean, for the same reason as above)
+        const float base = threads[kOne ? in.lo / V : in.lo].x;
+        float w, sum = 0.f, rest = 0.f;
+        for (int i = lane; i < entries; i += k) { const float2 e = entry(i, &w); sum += w > 0.f ? w * (e.x - base) : 0.f; }
+        const float m = base + (total > 0.f ? shared_sum(sum, k) / total : 0.f);
+        for (int i = lane; i < entries; i += k) { const float2 e = entry(i, &w); rest += w > 0.f ? e.y + w * (e.x - m) * (e.x - m) : 0.f; }
+        rest = shared_sum(rest, k);
+        if (lane == 0 && g < at.ng) give(g, make_float2(m, rest));
+    }
+}
+// Mean and rstd out of the CTAs' pairs, to the k lanes.
+template <typename R, typename W>
+__device__ __forceinline__ float2 combine_x(const Norm &q, int k, int lane, int count, R read, W weight) {
+    const float all = (float)q.pixels * (float)q.cpg, base = read(0).x;
+    float sum = 0.f, rest = 0.f, m;
+    if (count <= 4 * k) {                                    // (all reads in flight together)
+        float2 e[4];
+        float w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) { w[j] = 0.f; e[j] = make_float2(base, 0.f); if (lane + k * j < count) { e[j] = read(lane + k * j); w[j] = weight(lane + k * j); } }
+#pragma unroll
+        for (int j = 0; j < 4; ++j) sum += w[j] > 0.f ? w[j] * (e[j].x - base) : 0.f;
+        m = base + shared_sum(sum, k) / all;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) rest += w[j] > 0.f ? e[j].y + w[j] * (e[j].x - m) * (e[j].x - m) : 0.f;
+    } else {
+#pragma unroll 4
+        for (int i = lane; i < count; i += k) { const float w = weight(i); sum += w > 0.f ? w * (read(i).x - base) : 0.f; }
+        m = base + shared_sum(sum, k) / all;
+#pragma unroll 4
+        for (int i = lane; i < count; i += k) { const float2 e = read(i); const float w = weight(i); rest += w > 0.f ? e.y + w * (e.x - m) * (e.x - m) : 0.f; }
+    }
+    return make_float2(m, 1.f / sqrtf(shared_sum(rest, k) / all + q.eps));
+}
+
+template <int kAct, typename T>
+__device__ __forceinline__ uint64_t activate(uint64_t p) {   // (NaN stays)
+    const float2 v = f32x2_halves(p);
+    if constexpr (kAct == kRelu) return f32x2(max_nan(v.x, 0.f), max_nan(v.y, 0.f));
+    if constexpr (kAct == kRelu6) {
+        float a = max_nan(v.x, 0.f), b = max_nan(v.y, 0.f);
+        return f32x2(a > 6.f ? 6.f : a, b > 6.f ? 6.f : b);
+    }
+    if constexpr (kAct == kSilu) return mul2(p, f32x2(Of<T>::sigmoid(v.x), Of<T>::sigmoid(v.y)));
+    return p;
+}
+
+// y, and the 8-bit forms, of the CTA's pixels; known(g): the statistics of the sample's group g.
+template <typename T, bool kVec, bool kHold, typename F>
+__device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, const uint4 *kept, F known) {
+    constexpr int V = Of<T>::V, P = V / 2;
+    // (threads behind the last channel write the zeros that its block ends with; not of a block in which there is none)
+    if (me.lane >= q.lanes || !(me.n > 0 || (kHold && (me.ch & ~127) < q.channels))) return;
+    uint64_t a[P], b[P];
+#pragma unroll
+    for (int j = 0; j < P; ++j) {
+        float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int c = me.ch + 2 * j + i;
+            if ((kVec && !kHold) || 2 * j + i < me.n) {
+                const float2 k = known(c / q.cpg);
+                s[i] = k.y * (q.gamma ? q.gamma[c] : 1.f);
+                t[i] = fmaf(-k.x, s[i], q.beta ? q.beta[c] : 0.f);
+            }
+        }
+        a[j] = f32x2(s[0], s[1]); b[j] = f32x2(t[0], t[1]);
+    }
+    T *y = reinterpret_cast<T *>(q.out) + me.row0 * q.ld_out + me.ch;
+    const int64_t step_y = (int64_t)q.lanes * q.ld_out;
+    const auto finish = [&](auto act) {
+        int64_t col = me.row0;
+        const auto one = [&](const uint4 &u) {
+            uint64_t f[P];
+            Of<T>::open(u, f);
+            if constexpr (kHold) if (q.x8) hold<V>(q, q.x8, f, col, me.ch);
+#pragma unroll
+            for (int j = 0; j < P; ++j) f[j] = activate<decltype(act)::value, T>(fma2(f[j], a[j], b[j]));      // (0 behind the last channel: a = b = 0)
+            if constexpr (kHold) if (q.y8) hold<V>(q, q.y8, f, col, me.ch);
+            if (!kHold || (q.out && me.n > 0)) put<kVec && !kHold>(y, Of<T>::close(f), q.vec_out, me.n);
+            y += step_y;
+            col += q.lanes;
+        };
+#pragma unroll 2
+        for (int i = 0; i < me.items; ++i) one(!kHold || me.n ? kept[i * kThreads] : make_uint4(0, 0, 0, 0));
+    };
+    switch (q.act) {
+        case kRelu: finish(std::integral_constant<int, kRelu>()); break;
+        case kRelu6: finish(std::integral_constant<int, kRelu6>()); break;
+        case kSilu: finish(std::integral_constant<int, kSilu>()); break;
+        default: finish(std::integral_constant<int, kNone>());
+    }
+}
+
+template <typename T, bool kVec>
+__device__ __forceinline__ void keep_x(const Norm &q, const Mine<T> &me, uint4 *kept) {
+    if (me.n <= 0) return;
+    const T *x = reinterpret_cast<const T *>(q.x) + me.row0 * q.ldx + me.ch;
+    const int64_t step = (int64_t)q.lanes * q.ldx;
+    if (kVec || (q.vec && me.n == Of<T>::V)) {
+        for (int i = 0; i < me.items; ++i) copy_async<16>(kept + i * kThreads, x + i * step);
+        copies_done();
+    } else {
+        for (int i = 0; i < me.items; ++i) kept[i * kThreads] = fetch<false>(x + i * step, q.vec, me.n);
+    }
+}
+
+// kOne: a thread's channels are of one group.  kVec: every thread's V channels are there, at multiples of 16 bytes.  kHold: an 8-bit form is written.  kCluster: a small call.
+template <typename T, bool kOne, bool kVec, bool kHold, bool kCluster>
 __global__ void __launch_bounds__(kThreads, 3)
 norm_kernel(const __grid_constant__ Norm q) {
     constexpr int V = Of<T>::V;
     extern __shared__ __align__(16) uint8_t smem[];
     wait_for_prerequisites();
-    const Place at(q);
-    const int lane = threadIdx.x / q.cv, v = threadIdx.x - lane * q.cv;
-    const int ch = at.c0 + v * V, n = lane < q.lanes ? max(0, min(V, at.c0 + at.width - ch)) : 0;
-    const int items = lane < q.lanes ? items_of(at.px1 - at.px0, lane, q.lanes) : 0;
-    const int64_t row0 = (int64_t)at.n * q.pixels + at.px0 + lane;
-    const T *x = reinterpret_cast<const T *>(q.x) + row0 * q.ldx + ch;
-    const int64_t step = (int64_t)q.lanes * q.ldx;
-    float2 *groups = reinterpret_cast<float2 *>(smem);                       // [ng] of this CTA, then [ng] of all
-    float2 *threads = groups + 2 * at.ng;                                    // [kThreads] or [kThreads][V]
-    uint4 *kept = reinterpret_cast<uint4 *>(smem + ((2 * at.ng * 8 + kThreads * (kOne ? 1 : V) * 8 + 15) & ~15)) + threadIdx.x;
-    const int resident = kMode == kWhole ? min(items, q.resident) : 0;
-
-    if constexpr (kMode != kApply) {
-        if (n > 0) {
-            if (q.vec && n == V) {
-                for (int i = 0; i < resident; ++i) copy_async<16>(kept + i * kThreads, x + i * step);
-                copies_done();
-            } else {
-                for (int i = 0; i < resident; ++i) kept[i * kThreads] = fetch(x + i * step, q.vec, n);
-            }
-        }
-        float pivot[V], s1[V], s2[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) pivot[j] = s1[j] = s2[j] = 0.f;
-        if (n > 0 && items > 0) Of<T>::open(resident ? kept[0] : fetch(x, q.vec, n), pivot);
-        const auto add = [&](const uint4 &u) {
-            float f[V];
-            Of<T>::open(u, f);
-#pragma unroll
-            for (int j = 0; j < V; ++j) { const float d = f[j] - pivot[j]; s1[j] += d; s2[j] = fmaf(d, d, s2[j]); }
-        };
-        if (n > 0) {
-            for (int i = 0; i < resident; ++i) add(kept[i * kThreads]);
-            int i = resident;
-            for (; i + 4 <= items; i += 4) {
-                uint4 u[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) u[k] = fetch(x + (i + k) * step, q.vec, n);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) add(u[k]);
-            }
-            for (; i < items; ++i) add(fetch(x + i * step, q.vec, n));
-        }
-        // (mean, M2) of each channel, and of the thread
-        const float count = (float)items, over = items ? 1.f / count : 0.f;
-        float mean[V], m2[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const float d = s1[j] * over;
-            mean[j] = pivot[j] + d;
-            m2[j] = fmaxf(0.f, fmaf(-s1[j], d, s2[j]));
-            if (!(s2[j] < INFINITY)) m2[j] = NAN;                            // (fmaxf would lose it)
-        }
-        if constexpr (kOne) {
-            float all = 0.f, rest = 0.f;
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (j < n) all += mean[j] - mean[0];
-            const float m = mean[0] + (n ? all / (float)n : 0.f);
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (j < n) rest += m2[j] + count * (mean[j] - m) * (mean[j] - m);
-            threads[threadIdx.x] = make_float2(m, rest);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j) threads[threadIdx.x * V + j] = make_float2(mean[j], m2[j]);
-        }
+    const int most = q.width / q.cpg + 2;                                                // groups that a slice meets, at most
+    float2 *groups = reinterpret_cast<float2 *>(smem), *known = groups + most;           // of this CTA, of all
+    float2 *threads = known + most;                                                      // [kThreads] or [kThreads][V]
+    uint4 *kept = reinterpret_cast<uint4 *>(smem + ((2 * most * 8 + kThreads * (kOne ? 1 : V) * 8 + 15) & ~15)) + threadIdx.x;
+    if constexpr (kCluster) {
+        const Place at(q, blockIdx.x);
+        const Mine<T> me(q, at);
+        keep_x<T, kVec>(q, me, kept);
+        sum_x<T, kOne, kVec>(q, at, me, threads, kept, [&](int g, float2 pair) { groups[g] = pair; });
         __syncthreads();
-        for (int g = threadIdx.x >> 5; g < at.ng; g += kThreads / 32) {
-            const Span in = span_of(q, at, g);
-            const int wide = in.hi - in.lo, across = kOne ? (wide + V - 1) / V : wide;       // entries of a group and lane
-            const float total = (float)(at.px1 - at.px0) * (float)wide;
-            const int entries = across * q.lanes;
-            const auto entry = [&](int i, float *weight) {
-                const int l = i / across, a = i - l * across;
-                const float here = (float)items_of(at.px1 - at.px0, l, q.lanes);
-                if constexpr (kOne) {
-                    *weight = here * (float)min(V, wide - a * V);
-                    return threads[l * q.cv + in.lo / V + a];
-                } else {
-                    const int c = in.lo + a;
-                    *weight = here;
-                    return threads[l * q.cv * V + c];
-                }
-            };
-            // (about the first entry's mean, for the same reason as above)
-            const float base = threads[kOne ? in.lo / V : in.lo].x;
-            float w, sum = 0.f;
-            for (int i = threadIdx.x & 31; i < entries; i += 32) { const float2 e = entry(i, &w); sum += w > 0.f ? w * (e.x - base) : 0.f; }
-            const float m = base + (total > 0.f ? warp_sum(sum) / total : 0.f);
-            float rest = 0.f;
-            for (int i = threadIdx.x & 31; i < entries; i += 32) { const float2 e = entry(i, &w); rest += w > 0.f ? e.y + w * (e.x - m) * (e.x - m) : 0.f; }
-            rest = warp_sum(rest);
-            if ((threadIdx.x & 31) == 0) {
-                if constexpr (kMode == kSums) *partial_at(q, at, g) = make_float2(m, rest);
-                else groups[g] = make_float2(m, rest);
+        of_cluster(q, at, groups, [&](int g, int k, int lane, int count, auto read, auto weight) {
+            const float2 s = combine_x(q, k, lane, count, read, weight);
+            if (lane == 0 && g < at.ng) {
+                known[g] = s;
+                if (at.rank == 0) *reinterpret_cast<float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + at.g0 + g)) = s;
+            }
+        });
+        finish_y<T, kVec, kHold>(q, me, kept, [&](int g) { return known[g - at.g0]; });
+        __syncwarp();
+        cluster_wait();
+    } else {
+        for (uint32_t t = blockIdx.x; t < q.tiles;) {
+            const uint32_t unit = t / q.unit, end = min((unit + 1) * q.unit, q.tiles);
+            const bool again = t + gridDim.x < end;                                      // (more tiles of the unit than CTAs)
+            for (uint32_t u = t; u < end; u += gridDim.x) {
+                const Place at(q, u);
+                const Mine<T> me(q, at);
+                keep_x<T, kVec>(q, me, kept);
+                sum_x<T, kOne, kVec>(q, at, me, threads, kept, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
+                arrive(q, unit);
+            }
+            const bool ok = all_here(q, unit);
+            for (; t < end; t += gridDim.x) {
+                const Place at(q, t);
+                const Mine<T> me(q, at);
+                of_memory(q, at, [&](int g, int k, int lane, int count, auto read, auto weight) {
+                    const float2 s = ok ? combine_x(q, k, lane, count, read, weight) : make_float2(NAN, NAN);
+                    if (lane == 0 && g < at.ng) {
+                        known[g] = s;
+                        if (at.rank == 0 && (at.g0 + g) * q.cpg >= at.c0) *reinterpret_cast<float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + at.g0 + g)) = s;
+                    }
+                });
+                if (again) keep_x<T, kVec>(q, me, kept);
+                finish_y<T, kVec, kHold>(q, me, kept, [&](int g) { return known[g - at.g0]; });
+                __syncthreads();
             }
         }
-        if constexpr (kMode == kSums) return;
-        __syncthreads();
     }
-    float2 *known = groups + at.ng;
-    of_all<kMode>(q, at, groups, [&](int g, int count, int l, auto read, auto weight) {
-        const float all = (float)q.pixels * (float)q.cpg, base = read(0).x;
-        float sum = 0.f, rest = 0.f;
-        for (int i = l; i < count; i += 32) { const float w = weight(i); sum += w > 0.f ? w * (read(i).x - base) : 0.f; }
-        const float m = base + warp_sum(sum) / all;
-        for (int i = l; i < count; i += 32) { const float2 e = read(i); const float w = weight(i); rest += w > 0.f ? e.y + w * (e.x - m) * (e.x - m) : 0.f; }
-        rest = warp_sum(rest);
-        if (l == 0) {
-            const float2 s = make_float2(m, 1.f / sqrtf(rest / all + q.eps));
-            known[g] = s;
-            if (at.rank == 0 && (at.g0 + g) * q.cpg >= at.c0) *reinterpret_cast<float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + at.g0 + g)) = s;
-        }
-    });
-    const bool holds = q.x8 || q.y8;
-    // (threads behind the last channel write the zeros that its block ends with; not of a block in which there is none)
-    if (lane < q.lanes && (n > 0 || (holds && (ch & ~127) < q.channels))) {
-        constexpr int M = kOne ? 1 : V;
-        float mean[M], a[V], b[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            a[j] = b[j] = 0.f;
-            if (j == 0 || !kOne) mean[kOne ? 0 : j] = 0.f;
-            if (j >= n) continue;
-            const float2 s = known[(ch + j) / q.cpg - at.g0];
-            if (j == 0 || !kOne) mean[kOne ? 0 : j] = s.x;
-            a[j] = s.y * (q.gamma ? q.gamma[ch + j] : 1.f);
-            b[j] = q.beta ? q.beta[ch + j] : 0.f;
-        }
-        T *y = reinterpret_cast<T *>(q.out) + row0 * q.ld_out + ch;
-        const int64_t step_y = (int64_t)q.lanes * q.ld_out;
-        const auto finish = [&](int i, const uint4 &u) {
-            float f[V], r[V];
-            Of<T>::open(u, f);
-            if (q.x8) hold<V>(q, q.x8, f, row0 + (int64_t)i * q.lanes, ch);
-            const auto all = [&](auto act) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) r[j] = activate<decltype(act)::value, T>(fmaf(f[j] - mean[kOne ? 0 : j], a[j], b[j]));
-            };
-            switch (q.act) {
-                case kRelu: all(std::integral_constant<int, kRelu>()); break;
-                case kRelu6: all(std::integral_constant<int, kRelu6>()); break;
-                case kSilu: all(std::integral_constant<int, kSilu>()); break;
-                default: all(std::integral_constant<int, kNone>());
-            }
-            if (holds && n < V) {
-#pragma unroll
-                for (int j = 0; j < V; ++j) r[j] = j < n ? r[j] : 0.f;
-            }
-            if (q.y8) hold<V>(q, q.y8, r, row0 + (int64_t)i * q.lanes, ch);
-            if (q.out) put(y + i * step_y, Of<T>::close(r), q.vec_out, n);
-        };
-        const uint4 none = make_uint4(0, 0, 0, 0);
-        for (int i = 0; i < resident; ++i) finish(i, n ? kept[i * kThreads] : none);
-        int i = resident;
-        for (; i + 4 <= items; i += 4) {
-            uint4 u[4];
-#pragma unroll
-            for (int k = 0; k < 4; ++k) u[k] = n ? fetch(x + (i + k) * step, q.vec, n) : none;
-#pragma unroll
-            for (int k = 0; k < 4; ++k) finish(i + k, u[k]);
-        }
-        for (; i < items; ++i) finish(i, n ? fetch(x + i * step, q.vec, n) : none);
-    }
-    __syncwarp();
-    if constexpr (kMode == kWhole) cluster_wait();
 }
 
 // --------------------------------------------------------------------------------------------------------------- backward
 
 template <int V>
-__device__ __forceinline__ void decode(const uint32_t (&codes)[V / 4], uint32_t e, float (&f)[V]) {
-    const float up = power_of(e);
+__device__ __forceinline__ void decode(uint32_t lo, uint32_t hi, uint32_t e, uint64_t (&f)[V / 2]) {
+    const uint64_t up = both(power_of(e));
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) {
+        const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)((j < 2 ? lo : hi) >> (16 * (j & 1))), __NV_E4M3)));
+        f[j] = mul2(f32x2(v.x, v.y), up);
+    }
+}
+
+// A thread's coefficients of p = a x + b, and how near to a border of relu or relu6 p may be off.
+template <int P>
+struct Affine {
+    uint64_t a[P], b[P];
+    float near;
+};
+// Which side of the borders p lies on, from the formula in 64 bits: -1, 1 or 7.
+__device__ __noinline__ float side_of(const Norm &q, int64_t stat, int c, float x) {
+    const double exact = ((double)x - (double)q.stats[2 * stat]) * (double)q.stats[2 * stat + 1] * (q.gamma ? (double)q.gamma[c] : 1.0) + (q.beta ? (double)q.beta[c] : 0.0);
+    return exact > 0.0 ? (exact >= 6.0 ? 7.f : 1.f) : -1.f;
+}
+// e = dy act'(p).  Where p is within its roundings of a border, its side is taken from 64 bits, so that it is the formula's: one element on the wrong side would be
+// wrong by all of its dy.
+template <int kAct, typename T, int P>
+__device__ __forceinline__ void slope(const Norm &q, int n, int ch, const Affine<P> &k, const uint64_t (&x)[P], uint64_t (&dy)[P]) {
+    if constexpr (kAct == kNone) return;
+    if constexpr (kAct == kSilu) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const uint64_t p = fma2(x[j], k.a[j], k.b[j]);
+            const float2 v = f32x2_halves(p);
+            const uint64_t s = f32x2(Of<T>::sigmoid(v.x), Of<T>::sigmoid(v.y)), rest = fma2(s, both(-1.f), both(1.f));
+            dy[j] = mul2(dy[j], mul2(s, fma2(p, rest, both(1.f))));
+        }
+    } else {
+        float p[2 * P];
+        bool close = false;
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const float2 v = f32x2_halves(fma2(x[j], k.a[j], k.b[j]));
+            p[2 * j] = v.x; p[2 * j + 1] = v.y;
+            close |= fabsf(v.x) < k.near || fabsf(v.y) < k.near;
+            if constexpr (kAct == kRelu6) close |= fabsf(v.x - 6.f) < k.near || fabsf(v.y - 6.f) < k.near;
+        }
+        if (close) {
+#pragma unroll
+            for (int j = 0; j < 2 * P; ++j) {
+                if (ch + j >= q.channels) break;
+                if (fabsf(p[j]) < k.near || (kAct == kRelu6 && fabsf(p[j] - 6.f) < k.near)) {
+                    const float2 v = f32x2_halves(x[j / 2]);
+                    p[j] = side_of(q, (int64_t)n * q.groups + (ch + j) / q.cpg, ch + j, j & 1 ? v.y : v.x);
+                    if (kAct == kRelu && p[j] > 1.f) p[j] = 1.f;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const float2 d = f32x2_halves(dy[j]);
+            const bool lo = p[2 * j] > 0.f && (kAct == kRelu || p[2 * j] < 6.f), hi = p[2 * j + 1] > 0.f && (kAct == kRelu || p[2 * j + 1] < 6.f);
+            dy[j] = f32x2(lo ? d.x : 0.f, hi ? d.y : 0.f);
+        }
+    }
+}
+
+template <typename T, bool kOne>
+__device__ __forceinline__ void affine_of(const Norm &q, const Place &at, const Mine<T> &me, Affine<Of<T>::V / 2> *k, float (&mean)[kOne ? 1 : Of<T>::V],
+                                          float (&rstd)[kOne ? 1 : Of<T>::V]) {
+    constexpr int V = Of<T>::V;
+    k->near = 0.f;
 #pragma unroll
     for (int j = 0; j < V; j += 2) {
-        const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)(codes[j / 4] >> (8 * (j & 2))), __NV_E4M3)));
-        f[j] = v.x * up; f[j + 1] = v.y * up;
-    }
-}
-
-// e = dy act'(p).  Where p is within its rounding of a border of relu or relu6, it is taken again in 64 bits, so that which side it lies on is the formula's: one
-// element on the wrong side would be wrong by all of its dy.
-template <int kAct, typename T>
-__device__ __forceinline__ float slope(float dy, float x, float mean, float rstd, float gamma, float beta, float h) {
-    if constexpr (kAct == kNone) return dy;
-    float p = fmaf(h, gamma, beta);
-    if constexpr (kAct == kSilu) {
-        const float s = Of<T>::sigmoid(p);
-        return dy * (s * fmaf(p, 1.f - s, 1.f));
-    } else {
-        const float near = (fabsf(beta) + 8.f) * 0x1p-20f;                   // h, p: four roundings of values up to |beta| + 6 around the borders
-        if (fabsf(p) < near || (kAct == kRelu6 && fabsf(p - 6.f) < near)) {
-            const double exact = ((double)x - (double)mean) * (double)rstd * (double)gamma + (double)beta;
-            p = exact > 0.0 ? (kAct == kRelu6 && exact >= 6.0 ? 7.f : 1.f) : -1.f;
-        }
-        if constexpr (kAct == kRelu) return p <= 0.f ? 0.f : dy;
-        return p <= 0.f || p >= 6.f ? 0.f : dy;
-    }
-}
-
-template <typename T, bool kOne, bool k8, int kMode>
-__global__ void __launch_bounds__(kThreads, 2)
-norm_back_kernel(const __grid_constant__ Norm q) {
-    constexpr int V = Of<T>::V, M = kOne ? 1 : V;
-    extern __shared__ __align__(16) uint8_t smem[];
-    wait_for_prerequisites();
-    const Place at(q);
-    const int lane = threadIdx.x / q.cv, v = threadIdx.x - lane * q.cv;
-    const int ch = at.c0 + v * V, n = lane < q.lanes ? max(0, min(V, at.c0 + at.width - ch)) : 0;
-    const int items = n > 0 ? items_of(at.px1 - at.px0, lane, q.lanes) : 0;
-    const int64_t row0 = (int64_t)at.n * q.pixels + at.px0 + lane;
-    const T *x = reinterpret_cast<const T *>(q.x) + row0 * q.ldx + ch, *dy = reinterpret_cast<const T *>(q.dy) + row0 * q.ld_dy + ch;
-    const int64_t step_x = (int64_t)q.lanes * q.ldx, step_dy = (int64_t)q.lanes * q.ld_dy;
-    float2 *groups = reinterpret_cast<float2 *>(smem);
-    float2 *channels = groups + 2 * at.ng;                                   // [lanes][cv * V]: sums of e and of e h
-    uint8_t *kept = smem + ((2 * at.ng * 8 + kThreads * V * 8 + 15) & ~15);
-    // a thread's items: dy, then x; or its codes and the block's exponent
-    uint4 *kept_dy = reinterpret_cast<uint4 *>(kept) + threadIdx.x, *kept_x = kept_dy + q.resident * kThreads;
-    uint32_t *kept_codes = reinterpret_cast<uint32_t *>(kept + (size_t)q.resident * kThreads * 16) + threadIdx.x * (V / 4);
-    uint32_t *kept_e = reinterpret_cast<uint32_t *>(kept + (size_t)q.resident * kThreads * (16 + V)) + threadIdx.x;
-    const int resident = kMode == kWhole ? min(items, q.resident) : 0;
-
-    float mean[M], rstd[M], gamma[V], beta[V];
+        float a[2] = {0.f, 0.f}, b[2] = {0.f, 0.f};
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        gamma[j] = beta[j] = 0.f;
-        if (!kOne || j == 0) mean[kOne ? 0 : j] = rstd[kOne ? 0 : j] = 0.f;
-        if (j >= n) continue;
-        if (!kOne || j == 0) {
-            const float2 s = *reinterpret_cast<const float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + (ch + j) / q.cpg));
-            mean[kOne ? 0 : j] = s.x; rstd[kOne ? 0 : j] = s.y;
+        for (int i = 0; i < 2; ++i) {
+            const int c = me.ch + j + i, m = kOne ? 0 : j + i;
+            if (!kOne || j + i == 0) mean[m] = rstd[m] = 0.f;
+            if (j + i >= me.n) continue;
+            if (!kOne || j + i == 0) {
+                const float2 s = *reinterpret_cast<const float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + c / q.cpg));
+                mean[m] = s.x; rstd[m] = s.y;
+            }
+            const float beta = q.beta ? q.beta[c] : 0.f;
+            a[i] = rstd[m] * (q.gamma ? q.gamma[c] : 1.f);
+            b[i] = fmaf(-mean[m], a[i], beta);
+            // a and b are off by u of a x, of mean a and of b, p by one more of its own (u = 2^-24); at a border |a x| <= |b| + 6
+            k->near = fmaxf(k->near, (fabsf(beta) + 2.f * fabsf(mean[m] * a[i]) + 2.f * fabsf(b[i]) + 16.f) * 0x1p-22f);
         }
-        gamma[j] = q.gamma ? q.gamma[ch + j] : 1.f;
-        beta[j] = q.beta ? q.beta[ch + j] : 0.f;
+        k->a[j / 2] = f32x2(a[0], a[1]); k->b[j / 2] = f32x2(b[0], b[1]);
     }
-    struct Item { uint4 dy, x; };                                            // x: 16 bytes, or codes and exponent
-    const auto from_memory = [&](int i) {
+}
+
+struct Item { uint4 dy, x; };                                // x: 16 bytes, or codes and exponent
+
+template <typename T, bool k8, bool kVec>
+struct Reader {
+    static constexpr int V = Of<T>::V;
+    const Norm &q;
+    const Mine<T> &me;
+    const T *x, *dy;
+    int64_t step_x, step_dy;
+    __device__ __forceinline__ Reader(const Norm &q_, const Mine<T> &me_)
+        : q(q_), me(me_), x(reinterpret_cast<const T *>(q_.x) + me_.row0 * q_.ldx + me_.ch), dy(reinterpret_cast<const T *>(q_.dy) + me_.row0 * q_.ld_dy + me_.ch),
+          step_x((int64_t)q_.lanes * q_.ldx), step_dy((int64_t)q_.lanes * q_.ld_dy) {}
+    __device__ __forceinline__ Item operator()(int i) const {
         Item r;
-        r.dy = fetch(dy + i * step_dy, q.vec_dy, n);
+        r.dy = fetch<kVec>(dy + i * step_dy, q.vec_dy, me.n);
         if constexpr (k8) {
-            const int64_t col = row0 + (int64_t)i * q.lanes;
-            const uint8_t *p = q.from8 + codes_at(q, col, ch);
+            const int64_t col = me.row0 + (int64_t)i * q.lanes;
+            const uint8_t *p = q.from8 + codes_at(q, col, me.ch);
             if constexpr (V == 8) { const uint2 c = *reinterpret_cast<const uint2 *>(p); r.x.x = c.x; r.x.y = c.y; }
             else { r.x.x = *reinterpret_cast<const uint32_t *>(p); r.x.y = 0; }
-            r.x.z = *reinterpret_cast<const uint32_t *>(q.from8 + scale_at(q, col, ch));
+            r.x.z = *(q.from8 + scale_at(q, col, me.ch));
             r.x.w = 0;
         } else {
-            r.x = fetch(x + i * step_x, q.vec, n);
+            r.x = fetch<kVec>(x + i * step_x, q.vec, me.n);
         }
         return r;
-    };
-    const auto from_kept = [&](int i) {
-        Item r;
-        r.dy = kept_dy[i * kThreads];
-        if constexpr (k8) {
-            const uint32_t *c = kept_codes + i * kThreads * (V / 4);
-            r.x = make_uint4(c[0], V == 8 ? c[V / 4 - 1] : 0u, kept_e[i * kThreads], 0u);
-        } else {
-            r.x = kept_x[i * kThreads];
-        }
-        return r;
-    };
-    const auto keep = [&](int i, const Item &r) {
-        kept_dy[i * kThreads] = r.dy;
-        if constexpr (k8) {
-            uint32_t *c = kept_codes + i * kThreads * (V / 4);
-            c[0] = r.x.x;
-            if constexpr (V == 8) c[1] = r.x.y;
-            kept_e[i * kThreads] = r.x.z;
-        } else {
-            kept_x[i * kThreads] = r.x;
-        }
-    };
-    // calls f(e, h) with V values of each
-    const auto terms = [&](const Item &r, auto f) {
-        float d[V], xs[V], h[V];
+    }
+    static __device__ __forceinline__ void open(const Item &r, uint64_t (&d)[V / 2], uint64_t (&f)[V / 2]) {
         Of<T>::open(r.dy, d);
-        if constexpr (k8) {
-            uint32_t c[V / 4];
-            c[0] = r.x.x;
-            if constexpr (V == 8) c[1] = r.x.y;
-            decode<V>(c, r.x.z & 0xFFu, xs);
-        } else {
-            Of<T>::open(r.x, xs);
-        }
-        const auto all = [&](auto act) {
+        if constexpr (k8) decode<V>(r.x.x, r.x.y, r.x.z & 0xFFu, f);
+        else Of<T>::open(r.x, f);
+    }
+};
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F f) {
+    switch (act) {
+        case kRelu: f(std::integral_constant<int, kRelu>()); break;
+        case kRelu6: f(std::integral_constant<int, kRelu6>()); break;
+        case kSilu: f(std::integral_constant<int, kSilu>()); break;
+        default: f(std::integral_constant<int, kNone>());
+    }
+}
+
+// Sums of e and e h of the CTA's channels to q.sums, and of its groups (times gamma) to give(g, pair).  kept(i): what the thread has kept.
+template <typename T, bool kOne, bool k8, bool kVec, typename K, typename F>
+__device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine<T> &me, float2 *channels, K kept, F give) {
+    constexpr int V = Of<T>::V, P = V / 2, M = kOne ? 1 : V;
+    Affine<P> k;
+    float mean[M], rstd[M];
+    affine_of<T, kOne>(q, at, me, &k, mean, rstd);
+    uint64_t r[kOne ? 1 : P], s[kOne ? 1 : P], db[P], dg[P]; // h = r x + s
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                const float m = mean[kOne ? 0 : j], s = rstd[kOne ? 0 : j];
-                h[j] = (xs[j] - m) * s;
-                d[j] = slope<decltype(act)::value, T>(d[j], xs[j], m, s, gamma[j], beta[j], h[j]);
+    for (int j = 0; j < (kOne ? 1 : P); ++j) {
+        const float r0 = rstd[kOne ? 0 : 2 * j], r1 = rstd[kOne ? 0 : 2 * j + 1];
+        r[j] = f32x2(r0, r1); s[j] = f32x2(-mean[kOne ? 0 : 2 * j] * r0, -mean[kOne ? 0 : 2 * j + 1] * r1);
+    }
+#pragma unroll
+    for (int j = 0; j < P; ++j) db[j] = dg[j] = 0;
+    if (me.n > 0)
+        with_act(q.act, [&](auto act) {
+#pragma unroll 1
+            for (int i = 0; i < me.items; ++i) {
+                uint64_t d[P], x[P];
+                Reader<T, k8, kVec>::open(kept(i), d, x);
+                slope<decltype(act)::value, T, P>(q, at.n, me.ch, k, x, d);
+#pragma unroll
+                for (int j = 0; j < P; ++j) { db[j] = add2(db[j], d[j]); dg[j] = fma2(d[j], fma2(x[j], r[kOne ? 0 : j], s[kOne ? 0 : j]), dg[j]); }
             }
-        };
-        switch (q.act) {
-            case kRelu: all(std::integral_constant<int, kRelu>()); break;
-            case kRelu6: all(std::integral_constant<int, kRelu6>()); break;
-            case kSilu: all(std::integral_constant<int, kSilu>()); break;
-            default: all(std::integral_constant<int, kNone>());
+        });
+    const int row = q.cv * V;
+    if (me.lane < q.lanes) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            const float2 b = f32x2_halves(db[j]), g = f32x2_halves(dg[j]);
+            channels[me.lane * row + me.v * V + 2 * j] = make_float2(b.x, g.x);
+            channels[me.lane * row + me.v * V + 2 * j + 1] = make_float2(b.y, g.y);
         }
-        f(d, h);
-    };
-    if constexpr (kMode != kApply) {
-        if (q.vec_dy && (k8 || q.vec) && n == V) {
-            for (int i = 0; i < resident; ++i) {
-                copy_async<16>(kept_dy + i * kThreads, dy + i * step_dy);
+    }
+    __syncthreads();
+    // of each channel over the lanes: for gamma and beta, and to the first lane's place, times gamma, for the group
+    float *sums = q.sums + ((int64_t)at.n * q.ranks + at.rank) * 2 * q.channels;
+    for (int c = threadIdx.x; c < at.width; c += kThreads) {
+        float2 t = make_float2(0.f, 0.f);
+        for (int l = 0; l < q.lanes; ++l) { const float2 u = channels[l * row + c]; t.x += u.x; t.y += u.y; }
+        sums[at.c0 + c] = t.x;
+        sums[q.channels + at.c0 + c] = t.y;
+        const float w = q.gamma ? q.gamma[at.c0 + c] : 1.f;
+        channels[c] = make_float2(w * t.x, w * t.y);
+    }
+    __syncthreads();
+    const int k2 = sharers(at.ng), lane = threadIdx.x & (k2 - 1);
+    for (int g0 = 0; g0 < at.ng; g0 += kThreads / k2) {
+        const int g = g0 + threadIdx.x / k2;
+        const Span in = span_of(q, at, min(g, at.ng - 1));
+        float2 t = make_float2(0.f, 0.f);
+        for (int c = in.lo + lane; c < in.hi; c += k2) { const float2 u = channels[c]; t.x += u.x; t.y += u.y; }
+        t.x = shared_sum(t.x, k2); t.y = shared_sum(t.y, k2);
+        if (lane == 0 && g < at.ng) give(g, t);
+    }
+}
+template <typename R>
+__device__ __forceinline__ float2 combine_e(const Norm &q, int k, int lane, int count, R read) {
+    float2 t = make_float2(0.f, 0.f);
+#pragma unroll 4
+    for (int i = lane; i < count; i += k) { const float2 u = read(i); t.x += u.x; t.y += u.y; }
+    const float all = (float)q.pixels * (float)q.cpg;
+    return make_float2(shared_sum(t.x, k) / all, shared_sum(t.y, k) / all);
+}
+
+// dx of the CTA's pixels; known(g): m1 and m2 of the sample's group g.  dx = rstd (gamma e - m1 - h m2) = a e + B x + C.
+template <typename T, bool kOne, bool k8, bool kVec, typename K, typename F>
+__device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const Mine<T> &me, K kept, F known) {
+    constexpr int V = Of<T>::V, P = V / 2, M = kOne ? 1 : V;
+    if (me.n <= 0) return;
+    Affine<P> k;
+    float mean[M], rstd[M];
+    affine_of<T, kOne>(q, at, me, &k, mean, rstd);
+    uint64_t B[kOne ? 1 : P], C[kOne ? 1 : P];
+#pragma unroll
+    for (int j = 0; j < (kOne ? 1 : P); ++j) {
+        float b[2], c[2];
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+            const int m = kOne ? 0 : 2 * j + i;
+            const float2 g = m < me.n ? known((me.ch + m) / q.cpg) : make_float2(0.f, 0.f);
+            b[i] = -rstd[m] * rstd[m] * g.y;
+            c[i] = -fmaf(b[i], mean[m], rstd[m] * g.x);
+        }
+        B[j] = f32x2(b[0], b[1]); C[j] = f32x2(c[0], c[1]);
+    }
+    T *dx = reinterpret_cast<T *>(q.out) + me.row0 * q.ld_out + me.ch;
+    const int64_t step_out = (int64_t)q.lanes * q.ld_out;
+    with_act(q.act, [&](auto act) {
+#pragma unroll 1
+        for (int i = 0; i < me.items; ++i) {
+            uint64_t d[P], x[P];
+            Reader<T, k8, kVec>::open(kept(i), d, x);
+            slope<decltype(act)::value, T, P>(q, at.n, me.ch, k, x, d);
+#pragma unroll
+            for (int j = 0; j < P; ++j) d[j] = fma2(d[j], k.a[j], fma2(x[j], B[kOne ? 0 : j], C[kOne ? 0 : j]));
+            put<kVec>(dx + i * step_out, Of<T>::close(d), q.vec_out, me.n);
+        }
+    });
+}
+
+// Where a thread's items are kept: dy, then x; or its codes and the block's exponent.
+template <typename T, bool k8, bool kVec>
+struct Kept {
+    static constexpr int V = Of<T>::V;
+    uint4 *dy, *x;
+    uint32_t *codes, *e;
+    __device__ __forceinline__ Kept(const Norm &q, uint8_t *base)
+        : dy(reinterpret_cast<uint4 *>(base) + threadIdx.x), x(dy + q.resident * kThreads),
+          codes(reinterpret_cast<uint32_t *>(base + (size_t)q.resident * kThreads * 16) + threadIdx.x * (V / 4)),
+          e(reinterpret_cast<uint32_t *>(base + (size_t)q.resident * kThreads * (16 + V)) + threadIdx.x) {}
+    __device__ __forceinline__ Item operator()(int i) const {
+        Item r;
+        r.dy = dy[i * kThreads];
+        if constexpr (k8) {
+            const uint32_t *c = codes + i * kThreads * (V / 4);
+            r.x = make_uint4(c[0], V == 8 ? c[V / 4 - 1] : 0u, e[i * kThreads], 0u);
+        } else {
+            r.x = x[i * kThreads];
+        }
+        return r;
+    }
+    __device__ __forceinline__ void fill(const Norm &q, const Mine<T> &me) const {
+        if (me.n <= 0) return;
+        const Reader<T, k8, kVec> read(q, me);
+        if (kVec || (q.vec_dy && (k8 || q.vec) && me.n == V)) {
+            for (int i = 0; i < me.items; ++i) {
+                copy_async<16>(dy + i * kThreads, read.dy + i * read.step_dy);
                 if constexpr (k8) {
-                    const int64_t col = row0 + (int64_t)i * q.lanes;
-                    copy_async<V>(kept_codes + i * kThreads * (V / 4), q.from8 + codes_at(q, col, ch));
-                    copy_async<4>(kept_e + i * kThreads, q.from8 + scale_at(q, col, ch));
+                    const int64_t col = me.row0 + (int64_t)i * q.lanes;
+                    copy_async<V>(codes + i * kThreads * (V / 4), q.from8 + codes_at(q, col, me.ch));
+                    copy_async<4>(e + i * kThreads, q.from8 + scale_at(q, col, me.ch));
                 } else {
-                    copy_async<16>(kept_x + i * kThreads, x + i * step_x);
+                    copy_async<16>(x + i * kThreads, read.x + i * read.step_x);
                 }
             }
             copies_done();
         } else {
-            for (int i = 0; i < resident; ++i) keep(i, from_memory(i));
-        }
-        float db[V], dg[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) db[j] = dg[j] = 0.f;
-        const auto add = [&](const float (&e)[V], const float (&h)[V]) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) { db[j] += e[j]; dg[j] = fmaf(e[j], h[j], dg[j]); }
-        };
-        for (int i = 0; i < resident; ++i) terms(from_kept(i), add);
-        int i = resident;
-        for (; i + 2 <= items; i += 2) {
-            const Item a = from_memory(i), b = from_memory(i + 1);
-            terms(a, add);
-            terms(b, add);
-        }
-        if (i < items) terms(from_memory(i), add);
-        const int row = q.cv * V;
-        if (lane < q.lanes) {
-#pragma unroll
-            for (int j = 0; j < V; ++j) channels[lane * row + v * V + j] = make_float2(db[j], dg[j]);
-        }
-        __syncthreads();
-        // of each channel over the lanes: for gamma and beta, and back to the first lane's place times gamma for the group
-        float *sums = q.sums + ((int64_t)at.n * q.ranks + at.rank) * 2 * q.channels;
-        for (int c = threadIdx.x; c < at.width; c += kThreads) {
-            float2 s = make_float2(0.f, 0.f);
-            for (int l = 0; l < q.lanes; ++l) { const float2 t = channels[l * row + c]; s.x += t.x; s.y += t.y; }
-            sums[at.c0 + c] = s.x;
-            sums[q.channels + at.c0 + c] = s.y;
-            const float w = q.gamma ? q.gamma[at.c0 + c] : 1.f;
-            channels[c] = make_float2(w * s.x, w * s.y);
-        }
-        __syncthreads();
-        for (int g = threadIdx.x >> 5; g < at.ng; g += kThreads / 32) {
-            float2 s = make_float2(0.f, 0.f);
-            const Span in = span_of(q, at, g);
-            for (int c = in.lo + (threadIdx.x & 31); c < in.hi; c += 32) { const float2 t = channels[c]; s.x += t.x; s.y += t.y; }
-            s.x = warp_sum(s.x); s.y = warp_sum(s.y);
-            if ((threadIdx.x & 31) == 0) {
-                if constexpr (kMode == kSums) *partial_at(q, at, g) = s;
-                else groups[g] = s;
+            for (int i = 0; i < me.items; ++i) {
+                const Item r = read(i);
+                dy[i * kThreads] = r.dy;
+                if constexpr (k8) {
+                    uint32_t *c = codes + i * kThreads * (V / 4);
+                    c[0] = r.x.x;
+                    if constexpr (V == 8) c[1] = r.x.y;
+                    e[i * kThreads] = r.x.z;
+                } else {
+                    x[i * kThreads] = r.x;
+                }
             }
         }
-        if constexpr (kMode == kSums) return;
+    }
+};
+
+template <typename T, bool kOne, bool k8, bool kVec, bool kCluster>
+__global__ void __launch_bounds__(kThreads, 2)
+norm_back_kernel(const __grid_constant__ Norm q) {
+    constexpr int V = Of<T>::V;
+    extern __shared__ __align__(16) uint8_t smem[];
+    wait_for_prerequisites();
+    const int most = q.width / q.cpg + 2;
+    float2 *groups = reinterpret_cast<float2 *>(smem), *known = groups + most;
+    float2 *channels = known + most;                                         // [lanes][cv * V]: sums of e and of e h
+    const Kept<T, k8, kVec> kept(q, smem + ((2 * most * 8 + kThreads * V * 8 + 15) & ~15));
+    if constexpr (kCluster) {
+        const Place at(q, blockIdx.x);
+        const Mine<T> me(q, at);
+        kept.fill(q, me);
+        sum_e<T, kOne, k8, kVec>(q, at, me, channels, kept, [&](int g, float2 pair) { groups[g] = pair; });
         __syncthreads();
-    }
-    float2 *known = groups + at.ng;
-    of_all<kMode>(q, at, groups, [&](int g, int count, int l, auto read, auto) {
-        float2 s = make_float2(0.f, 0.f);
-        for (int i = l; i < count; i += 32) { const float2 t = read(i); s.x += t.x; s.y += t.y; }
-        s.x = warp_sum(s.x); s.y = warp_sum(s.y);
-        const float all = (float)q.pixels * (float)q.cpg;
-        if (l == 0) known[g] = make_float2(s.x / all, s.y / all);
-    });
-    if (items > 0) {
-        float2 m[M];
-#pragma unroll
-        for (int j = 0; j < M; ++j) m[j] = j < n ? known[(ch + j) / q.cpg - at.g0] : make_float2(0.f, 0.f);
-        T *dx = reinterpret_cast<T *>(q.out) + row0 * q.ld_out + ch;
-        const int64_t step_out = (int64_t)q.lanes * q.ld_out;
-        const auto finish = [&](int i, const Item &r) {
-            terms(r, [&](const float (&e)[V], const float (&h)[V]) {
-                float o[V];
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float2 g = m[kOne ? 0 : j];
-                    o[j] = rstd[kOne ? 0 : j] * (fmaf(gamma[j], e[j], -g.x) - h[j] * g.y);
-                }
-                put(dx + i * step_out, Of<T>::close(o), q.vec_out, n);
-            });
-        };
-        for (int i = 0; i < resident; ++i) finish(i, from_kept(i));
-        int i = resident;
-        for (; i + 2 <= items; i += 2) {
-            const Item a = from_memory(i), b = from_memory(i + 1);
-            finish(i, a);
-            finish(i + 1, b);
+        of_cluster(q, at, groups, [&](int g, int k, int lane, int count, auto read, auto) {
+            const float2 m = combine_e(q, k, lane, count, read);
+            if (lane == 0 && g < at.ng) known[g] = m;
+        });
+        finish_dx<T, kOne, k8, kVec>(q, at, me, kept, [&](int g) { return known[g - at.g0]; });
+        __syncwarp();
+        cluster_wait();
+    } else {
+        for (uint32_t t = blockIdx.x; t < q.tiles;) {
+            const uint32_t unit = t / q.unit, end = min((unit + 1) * q.unit, q.tiles);
+            const bool again = t + gridDim.x < end;
+            for (uint32_t u = t; u < end; u += gridDim.x) {
+                const Place at(q, u);
+                const Mine<T> me(q, at);
+                kept.fill(q, me);
+                sum_e<T, kOne, k8, kVec>(q, at, me, channels, kept, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
+                arrive(q, unit);
+            }
+            const bool ok = all_here(q, unit);
+            for (; t < end; t += gridDim.x) {
+                const Place at(q, t);
+                const Mine<T> me(q, at);
+                of_memory(q, at, [&](int g, int k, int lane, int count, auto read, auto) {
+                    const float2 m = ok ? combine_e(q, k, lane, count, read) : make_float2(NAN, NAN);
+                    if (lane == 0 && g < at.ng) known[g] = m;
+                });
+                if (again) kept.fill(q, me);
+                finish_dx<T, kOne, k8, kVec>(q, at, me, kept, [&](int g) { return known[g - at.g0]; });
+                __syncthreads();
+            }
         }
-        if (i < items) finish(i, from_memory(i));
     }
-    __syncwarp();
-    if constexpr (kMode == kWhole) cluster_wait();
 }
 
 // dbeta and dgamma: the sums of all CTAs' [rows][2][channels], a warp's lanes on 32 neighbouring ones, in one order.
@@ -666,8 +899,10 @@ sum_rows_kernel(const float *sums, int64_t rows, int channels, float *dgamma, fl
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int64_t c = (int64_t)blockIdx.x * 32 + lane;
     float s = 0.f;
-    if (c < 2 * (int64_t)channels)
+    if (c < 2 * (int64_t)channels) {
+#pragma unroll 8
         for (int64_t r = warp; r < rows; r += 32) s += sums[r * 2 * channels + c];
+    }
     part[warp][lane] = s;
     __syncthreads();
     s = warp_sum(part[lane][warp]);                                          // (column `warp` of the 32)
@@ -682,76 +917,80 @@ sum_rows_kernel(const float *sums, int64_t rows, int channels, float *dgamma, fl
 
 bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
-// How a call is cut: a kernel with clusters, or two without.
-struct Cut { int width, slices, ranks, per, cv; };
+// How a call is cut.
 struct Plan {
-    bool whole;
-    Cut sums, apply;                     // (whole: `sums` is the one kernel's)
-    int resident, parts;
-    int threads_smem, groups_smem;       // bytes in front of what the threads keep
+    bool cluster;                        // a small call
+    int width, slices, ranks, per, cv, parts;
+    int resident, fixed_smem;            // items a thread keeps, bytes in front of them
+    int64_t tiles, unit, units;
 };
 constexpr int kSms = 148;
-int ceil_div(int64_t a, int64_t b) { return (int)((a + b - 1) / b); }
-
-Cut cut_of(const crisp_group_norm_t &d, int V, int width, bool eight, int64_t most_ranks, int64_t ctas) {
-    Cut c{};
-    c.width = width;
-    c.slices = ceil_div(d.channels, width);
-    c.cv = eight ? ceil_div(width, 128) * (128 / V) : ceil_div(width, V);
-    const int lanes = kThreads / c.cv;
-    // enough CTAs, but two items a thread before a slice is cut further
-    int64_t ranks = std::min(most_ranks, std::max<int64_t>(1, ctas / std::max<int64_t>(1, d.batch * c.slices)));
-    ranks = std::max<int64_t>(1, std::min<int64_t>(ranks, ceil_div(d.pixels, 2 * lanes)));
-    c.per = ceil_div(d.pixels, ranks);
-    c.ranks = (int)ranks;
-    return c;
-}
+constexpr int64_t kSmallBytes = 12 << 20;
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 Plan plan_of(const crisp_group_norm_t &d, bool back, bool from8, bool eight) {
     Plan p{};
     const int size = d.dtype == 1 ? 4 : 2, V = 16 / size, C = d.channels, cpg = C / d.groups;
     const int most = kThreads * V, align = eight ? 128 : V;                  // channels that a CTA's threads hold side by side; multiples that slices are of
+    const int item = back ? (from8 ? 16 + V + 4 : 32) : 16;
+    const int64_t batch = std::max<int64_t>(1, d.batch), bytes = batch * d.pixels * C * item / V;
     int g = cpg, h = align;
     while (h) { const int t = g % h; g = h; h = t; }
-    const int64_t lcm = (int64_t)(cpg / g) * align;
-    const int unit = (int)std::min<int64_t>(lcm, C);                         // the narrowest slice of whole groups
-    const int item = back ? (from8 ? 16 + V + 4 : 32) : 16;
-    p.threads_smem = kThreads * (cpg % V == 0 && !back ? 1 : V) * 8;
-    if ((unit + align - 1) / align * align <= most) {
+    const int unit = (int)std::min<int64_t>((int64_t)(cpg / g) * align, C);  // the narrowest slice of whole groups
+    const bool whole = (unit + align - 1) / align * align <= most;
+    const auto slice = [&](int width) {
+        p.width = std::min(width, C);
+        p.slices = (int)ceil_div(C, p.width);
+        p.cv = (int)(eight ? ceil_div(p.width, 128) * (128 / V) : ceil_div(p.width, V));
+        p.fixed_smem = (2 * (p.width / cpg + 2) * 8 + kThreads * (cpg % V == 0 && C % V == 0 && !back ? 1 : V) * 8 + 15) & ~15;
+    };
+    const auto rank = [&](int64_t ranks) {
+        p.per = (int)ceil_div(d.pixels, std::max<int64_t>(1, std::min<int64_t>(ranks, d.pixels)));
+        p.ranks = (int)ceil_div(d.pixels, p.per);
+        p.resident = (int)ceil_div(p.per, kThreads / p.cv);
+    };
+    const auto wanted = [&] { return p.fixed_smem + (size_t)p.resident * kThreads * item; };
+    if (whole && bytes <= kSmallBytes) {
         int width = unit;
         while (width < C && width * size < 128 && width + unit <= most) width += unit;
-        width = std::min(width, C);
-        p.sums = cut_of(d, V, width, eight, kMaxCluster, 3 * kSms);
-        const int lanes = kThreads / p.sums.cv;
-        const auto fixed = [&] { return (size_t)((2 * (ceil_div(p.sums.width, cpg) + 1) * 8 + p.threads_smem + 15) & ~15); };
-        const auto wanted = [&] { return fixed() + (size_t)ceil_div(p.sums.per, lanes) * kThreads * item; };
-        while (wanted() > kMaxSmem / 3 && p.sums.ranks < kMaxCluster) {
-            p.sums.ranks = std::min(kMaxCluster, p.sums.ranks * 2);
-            p.sums.per = ceil_div(d.pixels, p.sums.ranks);
-        }
-        p.whole = d.batch * p.sums.slices * p.sums.ranks >= kSms / 2 || d.pixels * C * d.batch <= (1 << 20);
-        const size_t room = wanted() <= kMaxSmem / 3 ? kMaxSmem / 3 : wanted() <= kMaxSmem / 2 ? kMaxSmem / 2 : kMaxSmem;
-        p.resident = std::min(ceil_div(p.sums.per, lanes), (int)((room - fixed()) / (kThreads * item)));
+        slice(width);
+        // enough CTAs, but two items a thread before a slice is cut further
+        rank(std::min<int64_t>(std::min<int64_t>(kMaxCluster, ceil_div(2 * kSms, batch * p.slices)), ceil_div(d.pixels, 2 * (kThreads / p.cv))));
+        while (wanted() > kMaxSmem / 2 && p.ranks < kMaxCluster) rank(std::min(kMaxCluster, p.ranks * 2));
+        p.cluster = wanted() <= kMaxSmem && p.ranks <= kMaxCluster;
+        p.parts = 1;
     }
-    if (!p.whole) {
-        int width = align;
-        while (width < C && width * size < 512 && width + align <= most) width += align;
-        width = std::min(width, C);
-        p.sums = p.apply = cut_of(d, V, width, eight, 1 << 16, 6 * kSms);
-        p.resident = 0;
+    if (!p.cluster) {
+        // slices of whole groups and up to 512 channels; tiles that leave room for three CTAs an SM (backward two)
+        int width = whole ? unit : align;
+        while (width < C && width + (whole ? unit : align) <= std::min(most, 64 * V)) width += whole ? unit : align;
+        slice(width);
+        p.parts = whole ? 1 : (cpg + p.width - 2) / p.width + 1;
+        const int per_sm = back ? 2 : 3;
+        const int64_t items = std::max<int64_t>(1, ((int64_t)kMaxSmem / per_sm - 1024 - p.fixed_smem) / (kThreads * item)), slices = batch * p.slices, grid = kSms * per_sm;
+        int64_t ranks = ceil_div(d.pixels, items * (kThreads / p.cv));
+        // as many as fill the last round, too
+        const int64_t rounds = ceil_div(slices * ranks, grid), filled = rounds * grid / slices;
+        if (filled > ranks) ranks = std::min<int64_t>(filled, ceil_div(d.pixels, 2 * (kThreads / p.cv)) > ranks ? ceil_div(d.pixels, 2 * (kThreads / p.cv)) : ranks);
+        rank(ranks);
     }
-    p.parts = p.whole ? 1 : (cpg + p.sums.width - 2) / p.sums.width + 1;
-    p.groups_smem = 2 * (ceil_div(p.sums.width, cpg) + 1) * 8;
+    p.tiles = batch * p.slices * p.ranks;
+    p.unit = p.parts == 1 ? p.ranks : (int64_t)p.slices * p.ranks;
+    p.units = p.tiles / p.unit;
     return p;
 }
-size_t smem_of(const Plan &p, int item) { return (size_t)((p.groups_smem + p.threads_smem + 15) & ~15) + (size_t)p.resident * kThreads * item; }
 
-// Workspace: the sums of gamma's and beta's gradients, then the two kernels' partial sums.
-struct Space { size_t sums, partial; };
+// Workspace: the sums of gamma's and beta's gradients; for large calls the CTAs' pairs and the counters.
+struct Space { size_t sums, partial, arrived, total; };
 Space space_of(const crisp_group_norm_t &d, const Plan &p, bool back) {
     Space s{};
-    if (back) s.sums = align_up((size_t)d.batch * p.sums.ranks * 2 * d.channels * sizeof(float));
-    if (!p.whole) s.partial = align_up((size_t)d.batch * d.groups * p.sums.ranks * p.parts * sizeof(float2));
+    size_t at = 0;
+    if (back) at += align_up((size_t)d.batch * p.ranks * 2 * d.channels * sizeof(float));
+    s.partial = at;
+    if (!p.cluster) at += align_up((size_t)d.batch * d.groups * p.ranks * p.parts * sizeof(float2));
+    s.arrived = at;
+    if (!p.cluster) at += align_up((size_t)p.units * sizeof(uint32_t));
+    s.total = at;
     return s;
 }
 
@@ -765,60 +1004,84 @@ crisp_status_t check(const crisp_group_norm_t *d) {
 }
 
 template <auto kernel>
-cudaError_t launch(const Norm &q, int64_t batch, size_t smem, unsigned cluster, cudaStream_t st) {
-    const int64_t grid = batch * q.slices * q.ranks;
-    if (grid > 0x7FFFFFFFll) return cudaErrorInvalidValue;
-    static std::atomic<uint64_t> ready{0};                                    // (one a kernel: by device)
+cudaError_t allow(bool cluster) {                                            // (once a kernel and device)
+    static std::atomic<uint64_t> ready{0};
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
-    if (device >= 64 || !(ready.load(std::memory_order_relaxed) >> device & 1)) {
-        e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxSmem);
-        if (e == cudaSuccess) e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
-        if (e != cudaSuccess) return e;
-        if (device < 64) ready.fetch_or(1ull << device, std::memory_order_relaxed);
+    if (device < 64 && ready.load(std::memory_order_relaxed) >> device & 1) return cudaSuccess;
+    e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxSmem);
+    if (e == cudaSuccess && cluster) e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess && device < 64) ready.fetch_or(1ull << device, std::memory_order_relaxed);
+    return e;
+}
+template <auto small, auto large>
+cudaError_t run(const Plan &p, const Norm &q, int per_sm, int item, cudaStream_t st) {
+    if (p.tiles > 0x7FFFFFFFll / 2) return cudaErrorInvalidValue;
+    const size_t smem = p.fixed_smem + (size_t)p.resident * kThreads * item;
+    cudaError_t e = p.cluster ? allow<small>(true) : allow<large>(false);
+    if (e != cudaSuccess) return e;
+    if (p.cluster) return launch_clusters(small, (unsigned)p.tiles, kThreads, smem, st, (unsigned)q.ranks, q);
+    e = cudaMemsetAsync(q.arrived, 0, (size_t)p.units * sizeof(uint32_t), st);
+    if (e != cudaSuccess) return e;
+    int device = 0;
+    e = cudaGetDevice(&device);
+    if (e != cudaSuccess) return e;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeCooperative;                             // (its CTAs wait for one another)
+    attr[0].val.cooperative = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)std::min<int64_t>(p.tiles, (int64_t)sm_count_of(device) * per_sm));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = st;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    e = cudaLaunchKernelEx(&cfg, large, q);
+    if (e != cudaSuccess) (void)cudaGetLastError();
+    return e;
+}
+template <typename T, bool kOne, bool kVec, bool kHold>
+cudaError_t forward(const Plan &p, const Norm &q, cudaStream_t st) {
+    return run<norm_kernel<T, kOne, kVec, kHold, true>, norm_kernel<T, kOne, kVec, kHold, false>>(p, q, 3, 16, st);
+}
+template <typename T>
+cudaError_t forward(const Plan &p, const Norm &q, bool one, bool vec, bool hold, cudaStream_t st) {
+    if (one) {
+        if (vec) return hold ? forward<T, true, true, true>(p, q, st) : forward<T, true, true, false>(p, q, st);
+        return hold ? forward<T, true, false, true>(p, q, st) : forward<T, true, false, false>(p, q, st);
     }
-    return launch_clusters(kernel, (unsigned)grid, kThreads, smem, st, cluster, q);
+    if (vec) return hold ? forward<T, false, true, true>(p, q, st) : forward<T, false, true, false>(p, q, st);
+    return hold ? forward<T, false, false, true>(p, q, st) : forward<T, false, false, false>(p, q, st);
 }
-
-void set_cut(Norm *q, const Cut &c) {
-    q->width = c.width; q->slices = c.slices; q->ranks = c.ranks; q->per = c.per; q->cv = c.cv;
-    q->lanes = kThreads / c.cv;
+template <typename T, bool kOne, bool k8, bool kVec>
+cudaError_t backward(const Plan &p, const Norm &q, cudaStream_t st) {
+    return run<norm_back_kernel<T, kOne, k8, kVec, true>, norm_back_kernel<T, kOne, k8, kVec, false>>(p, q, 2, k8 ? 16 + Of<T>::V + 4 : 32, st);
 }
-
-template <typename T, bool kOne>
-cudaError_t forward(const crisp_group_norm_t &d, const Plan &p, Norm q, cudaStream_t st) {
-    set_cut(&q, p.sums);
-    if (p.whole) return launch<norm_kernel<T, kOne, kWhole>>(q, d.batch, smem_of(p, 16), (unsigned)q.ranks, st);
-    const cudaError_t e = launch<norm_kernel<T, kOne, kSums>>(q, d.batch, smem_of(p, 16), 1, st);
-    if (e != cudaSuccess) return e;
-    set_cut(&q, p.apply);
-    return launch<norm_kernel<T, kOne, kApply>>(q, d.batch, smem_of(p, 16), 1, st);
-}
-template <typename T, bool kOne, bool k8>
-cudaError_t backward(const crisp_group_norm_t &d, const Plan &p, Norm q, cudaStream_t st) {
-    const int item = k8 ? 16 + Of<T>::V + 4 : 32;
-    set_cut(&q, p.sums);
-    if (p.whole) return launch<norm_back_kernel<T, kOne, k8, kWhole>>(q, d.batch, smem_of(p, item), (unsigned)q.ranks, st);
-    const cudaError_t e = launch<norm_back_kernel<T, kOne, k8, kSums>>(q, d.batch, smem_of(p, item), 1, st);
-    if (e != cudaSuccess) return e;
-    set_cut(&q, p.apply);
-    return launch<norm_back_kernel<T, kOne, k8, kApply>>(q, d.batch, smem_of(p, item), 1, st);
+template <typename T>
+cudaError_t backward(const Plan &p, const Norm &q, bool one, bool vec, bool from8, cudaStream_t st) {
+    if (!vec) return from8 ? backward<T, false, true, false>(p, q, st) : backward<T, false, false, false>(p, q, st);
+    if (one) return from8 ? backward<T, true, true, true>(p, q, st) : backward<T, true, false, true>(p, q, st);
+    return from8 ? backward<T, false, true, true>(p, q, st) : backward<T, false, false, true>(p, q, st);
 }
 
 int vec_of(const void *p, int64_t ld, int size) { return aligned_to(p, 16) && ld * size % 16 == 0; }
 
 Norm norm_of(const crisp_group_norm_t &d, const Plan &p, const Space &s, void *workspace) {
     Norm q{};
-    q.sums = reinterpret_cast<float *>(workspace);
-    q.partial = reinterpret_cast<float2 *>(reinterpret_cast<uint8_t *>(workspace) + s.sums);
+    uint8_t *w = reinterpret_cast<uint8_t *>(workspace);
+    q.sums = reinterpret_cast<float *>(w);
+    q.partial = reinterpret_cast<float2 *>(w + s.partial);
+    q.arrived = reinterpret_cast<uint32_t *>(w + s.arrived);
     q.pixels = (int)d.pixels; q.channels = d.channels; q.groups = d.groups; q.cpg = d.channels / d.groups;
-    q.p_width = p.sums.width; q.p_ranks = p.sums.ranks; q.p_per = p.sums.per; q.parts = p.parts;
+    q.width = p.width; q.slices = p.slices; q.ranks = p.ranks; q.per = p.per; q.parts = p.parts; q.cv = p.cv;
+    q.lanes = kThreads / p.cv;
     q.resident = p.resident;
+    q.tiles = (uint32_t)p.tiles; q.unit = (uint32_t)p.unit;
     q.act = d.activation;
     q.eps = (float)d.eps;
     const Act8 a = act8(d.channels, d.batch * d.pixels);
-    q.cols8 = d.batch * d.pixels; q.groups8 = a.groups; q.chunks8 = a.chunks; q.scale_off = a.scale_off;
+    q.groups8 = a.groups; q.chunks8 = a.chunks; q.scale_off = a.scale_off;
     return q;
 }
 
@@ -838,7 +1101,7 @@ crisp_status_t crisp_group_norm_sizes(const crisp_group_norm_t *desc, int32_t ba
     for (int eight = 0; eight < 2; ++eight) {
         const Plan p = plan_of(*desc, backward != 0, backward && eight, !backward && eight);
         const Space s = space_of(*desc, p, backward != 0);
-        *workspace_bytes = std::max(*workspace_bytes, s.sums + s.partial);
+        *workspace_bytes = std::max(*workspace_bytes, s.total);
     }
     return CRISP_OK;
 }
@@ -859,16 +1122,18 @@ crisp_status_t crisp_group_norm(const crisp_group_norm_t *desc, const void *d_x,
     if (eight && crisp_quantize8_sizes(d.channels, d.batch * d.pixels, &bytes) != CRISP_OK) return CRISP_UNSUPPORTED;
     const Plan p = plan_of(d, false, false, eight);
     const Space s = space_of(d, p, false);
-    if (s.partial && !d_workspace) return CRISP_INVALID_ARG;
+    if (s.total && !d_workspace) return CRISP_INVALID_ARG;
     Norm q = norm_of(d, p, s, d_workspace);
     q.x = d_x; q.ldx = ldx; q.out = d_y; q.ld_out = ldy; q.gamma = d_gamma; q.beta = d_beta; q.stats = d_stats;
     q.x8 = reinterpret_cast<uint8_t *>(d_x8); q.y8 = reinterpret_cast<uint8_t *>(d_y8);
     q.vec = vec_of(d_x, ldx, size); q.vec_out = vec_of(d_y, ldy, size);
-    const bool one = q.cpg % (16 / size) == 0;
+    const int V = 16 / size;
+    const bool one = q.cpg % V == 0, vec = d.channels % V == 0 && q.vec && q.vec_out;
+    const uint32_t across = (uint32_t)(one ? q.cpg / V : q.cpg);
+    q.across_magic = (uint32_t)((((uint64_t)1 << 32) + across - 1) / across);
     cudaStream_t st = (cudaStream_t)stream;
-    const cudaError_t e = d.dtype == 1 ? (one ? forward<float, true>(d, p, q, st) : forward<float, false>(d, p, q, st))
-                        : d.dtype == 0 ? (one ? forward<__nv_bfloat16, true>(d, p, q, st) : forward<__nv_bfloat16, false>(d, p, q, st))
-                                       : (one ? forward<__half, true>(d, p, q, st) : forward<__half, false>(d, p, q, st));
+    const cudaError_t e = d.dtype == 1 ? forward<float>(p, q, one, vec, eight, st)
+                        : d.dtype == 0 ? forward<__nv_bfloat16>(p, q, one, vec, eight, st) : forward<__half>(p, q, one, vec, eight, st);
     return e == cudaSuccess ? CRISP_OK : e == cudaErrorInvalidValue ? CRISP_UNSUPPORTED : CRISP_CUDA_ERROR;
 }
 
@@ -900,16 +1165,12 @@ crisp_status_t crisp_group_norm_backward(const crisp_group_norm_t *desc, const v
     q.x = d_x; q.ldx = ldx; q.from8 = reinterpret_cast<const uint8_t *>(d_x8); q.dy = d_dy; q.ld_dy = ld_dy; q.out = d_dx; q.ld_out = ld_dx;
     q.gamma = d_gamma; q.beta = d_beta; q.stats = const_cast<float *>(d_stats);
     q.vec = vec_of(d_x, ldx, size); q.vec_dy = vec_of(d_dy, ld_dy, size); q.vec_out = vec_of(d_dx, ld_dx, size);
-    const bool one = q.cpg % (16 / size) == 0;
-    cudaError_t e;
-#define CRISP_BACK(T) (one ? (d_x8 ? backward<T, true, true>(d, p, q, st) : backward<T, true, false>(d, p, q, st)) \
-                           : (d_x8 ? backward<T, false, true>(d, p, q, st) : backward<T, false, false>(d, p, q, st)))
-    if (d.dtype == 1) e = CRISP_BACK(float);
-    else if (d.dtype == 0) e = CRISP_BACK(__nv_bfloat16);
-    else e = CRISP_BACK(__half);
-#undef CRISP_BACK
+    const int V = 16 / size;
+    const bool one = q.cpg % V == 0, vec = d.channels % V == 0 && (d_x8 || q.vec) && q.vec_dy && q.vec_out, from8 = d_x8 != nullptr;
+    cudaError_t e = d.dtype == 1 ? backward<float>(p, q, one, vec, from8, st)
+                  : d.dtype == 0 ? backward<__nv_bfloat16>(p, q, one, vec, from8, st) : backward<__half>(p, q, one, vec, from8, st);
     if (e == cudaSuccess && (d_dgamma || d_dbeta))
-        e = launch_chained(sum_rows_kernel, (unsigned)((2 * (int64_t)d.channels + 31) / 32), 1024, 0, st, q.sums, (int64_t)(d.batch * p.sums.ranks), d.channels, d_dgamma,
+        e = launch_chained(sum_rows_kernel, (unsigned)((2 * (int64_t)d.channels + 31) / 32), 1024, 0, st, q.sums, (int64_t)(d.batch * p.ranks), d.channels, d_dgamma,
                            d_dbeta);
     return e == cudaSuccess ? CRISP_OK : e == cudaErrorInvalidValue ? CRISP_UNSUPPORTED : CRISP_CUDA_ERROR;
 }
