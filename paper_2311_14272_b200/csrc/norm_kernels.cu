@@ -4,12 +4,11 @@
 //   h = (x - mean) rstd      y = act(p), p = gamma h + beta
 //   backward:  e = dy act'(p)   dbeta = sum e   dgamma = sum e h   dx = rstd (gamma e - m1 - h m2),  m1, m2 = the group's means of gamma e, gamma e h
 //
-// Bound by memory: each value is needed twice, and what counts is that it comes from DRAM once.  A CTA takes some pixels of a sample's slice of channels, every thread
-// keeps what it has read in shared memory of its own (no barrier: it reads what it wrote), and when the sums of all CTAs of the slice are there, it finishes its pixels.
+// Bound by memory: each value is needed twice, and what counts is that it comes from DRAM once.
 //
-//   small calls   a slice's CTAs are a cluster, and read one another's sums
-//   large ones    a cooperative launch of as many CTAs as fit, which go over the tiles of all samples in order and pass their sums through memory.  A slice of more
-//                 tiles than CTAs (27 MB) is read twice
+//   small calls   one kernel: a cluster of CTAs takes a sample's slice of whole groups, every thread keeps what it has read in shared memory of its own (no barrier: it
+//                 reads what it wrote) until the cluster's sums are there
+//   large ones    two kernels of as many CTAs as fit, each with its part of the pixels.  The second goes over them backwards: what the first read last is still in L2
 //
 // A thread holds V = 16 bytes' worth of consecutive channels and goes over pixels, two channels an instruction: per pair p = a x + b (a = gamma rstd, b = beta - mean a),
 // dx = a e + B x + C.  Forward sums are about the thread's first value, so that a mean far from zero costs no digits; then mean = sum n_i mean_i / n and
@@ -32,6 +31,7 @@ using namespace block8;
 namespace {
 
 constexpr int kThreads = 256;
+constexpr int kForwardCtas = 3, kBackwardCtas = 2;            // an SM, in large calls
 constexpr int kMaxCluster = 16;
 constexpr size_t kMaxSmem = 232448 - 1024;
 
@@ -46,8 +46,6 @@ struct Norm {
     float *stats;                        // [batch, groups, 2]
     float *sums;                         // backward: [batch * ranks][2][channels]
     float2 *partial;                     // large calls: [batch, groups, ranks, parts]
-    uint32_t *arrived;                   // and CTAs whose pairs are there, of each unit (0 when the call begins)
-    uint32_t tiles, unit;                // all tiles; those whose sums meet: of a slice, or of a sample where groups lie in several slices
     int64_t ldx, ld_dy, ld_out;
     int64_t groups8, chunks8;            // 8-bit form: groups of 8 and of 128 columns (pixels of all samples)
     size_t scale_off;
@@ -56,9 +54,11 @@ struct Norm {
     int ranks, per;                      // CTAs of a sample's slice, pixels of one
     int parts;                           // the most slices that a group lies in
     int cv, lanes;                       // threads a pixel, pixels at a time
+    int some, more, some_last, more_last;    // items of a pixel lane: `some`, the first `more` lanes one more (the last rank's: ..._last)
     int resident;                        // items (V channels of a pixel) that a thread keeps
-    uint32_t across_magic;               // 2^32 / (entries of a whole group and lane), rounded up
+    uint32_t across_magic, cpg_magic;    // 2^32 / (entries of a whole group and lane), / cpg, rounded up (0: not exact for all channels)
     int act, vec, vec_dy, vec_out;       // vec: addresses and pitches allow 16 bytes at once
+    int stream;                          // the results are not kept in L2 at the cost of what is still to be read
     float eps;
 };
 
@@ -79,8 +79,13 @@ struct Of<float> {
 };
 struct Of16 {
     static constexpr int V = 8;
-    // (some 2^-21 of the value, far below the result's last place)
-    static __device__ __forceinline__ float sigmoid(float p) { return __fdividef(1.f, 1.f + __expf(-p)); }
+    // (some 2^-21 of the value, far below the result's last place; 0 where it is below 2^-126)
+    static __device__ __forceinline__ float sigmoid(float p) {
+        float e, r;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(p * -1.44269504f));
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+        return r;
+    }
 };
 template <>
 struct Of<__nv_bfloat16> : Of16 {
@@ -149,9 +154,13 @@ __device__ __forceinline__ uint4 fetch(const T *p, int vec, int n) {
     return make_uint4(w[0], w[1], w[2], w[3]);
 }
 template <bool kVec, typename T>
-__device__ __forceinline__ void put(T *p, const uint4 &u, int vec, int n) {
+__device__ __forceinline__ void put(T *p, const uint4 &u, int vec, int n, int stream) {
     constexpr int V = Of<T>::V;
-    if (kVec || (vec && n == V)) { *reinterpret_cast<uint4 *>(p) = u; return; }
+    if (kVec || (vec && n == V)) {
+        if (stream) __stcs(reinterpret_cast<uint4 *>(p), u);
+        else *reinterpret_cast<uint4 *>(p) = u;
+        return;
+    }
     const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
     for (int j = 0; j < V; ++j)
@@ -204,6 +213,11 @@ __device__ __forceinline__ void hold(const Norm &q, uint8_t *to, const uint64_t 
     if ((ch & 127) == 0) *reinterpret_cast<uint32_t *>(to + scale_at(q, col, ch)) = e * 0x01010101u;
 }
 
+// (a product instead of a division of some twenty instructions)
+__device__ __forceinline__ int group_of(const Norm &q, int channel) {
+    return q.cpg_magic ? (int)__umulhi((uint32_t)channel, q.cpg_magic) : channel / q.cpg;
+}
+
 // A CTA's place: sample, first channel, channels, groups that it meets, pixels.
 struct Place {
     int n, slice, rank, c0, width, g0, ng, px0, px1;
@@ -213,7 +227,7 @@ struct Place {
         n = (int)(u / (uint32_t)q.slices);
         slice = (int)(u - (uint32_t)n * (uint32_t)q.slices);
         c0 = slice * q.width; width = min(q.width, q.channels - c0);
-        g0 = c0 / q.cpg; ng = (c0 + width - 1) / q.cpg + 1 - g0;
+        g0 = group_of(q, c0); ng = group_of(q, c0 + width - 1) + 1 - g0;
         px0 = min(rank * q.per, q.pixels); px1 = min(px0 + q.per, q.pixels);
     }
 };
@@ -222,18 +236,16 @@ template <typename T>
 struct Mine {
     int lane, v, ch, n, items;
     int64_t row0;
-    __device__ __forceinline__ Mine(const Norm &q, const Place &at);
+    __device__ __forceinline__ Mine(const Norm &q, const Place &at) {
+        constexpr int V = Of<T>::V;
+        lane = (int)((uint32_t)threadIdx.x / (uint32_t)q.cv); v = (int)threadIdx.x - lane * q.cv;
+        ch = at.c0 + v * V;
+        n = lane < q.lanes ? max(0, min(V, at.c0 + at.width - ch)) : 0;
+        const bool last = at.rank + 1 == q.ranks;
+        items = lane < q.lanes ? (last ? q.some_last : q.some) + (lane < (last ? q.more_last : q.more)) : 0;
+        row0 = (int64_t)at.n * q.pixels + at.px0 + lane;
+    }
 };
-__device__ __forceinline__ int items_of(int pixels, int lane, int lanes) { return pixels > lane ? (pixels - lane + lanes - 1) / lanes : 0; }
-template <typename T>
-__device__ __forceinline__ Mine<T>::Mine(const Norm &q, const Place &at) {
-    constexpr int V = Of<T>::V;
-    lane = (int)((uint32_t)threadIdx.x / (uint32_t)q.cv); v = (int)threadIdx.x - lane * q.cv;
-    ch = at.c0 + v * V;
-    n = lane < q.lanes ? max(0, min(V, at.c0 + at.width - ch)) : 0;
-    items = lane < q.lanes ? items_of(at.px1 - at.px0, lane, q.lanes) : 0;
-    row0 = (int64_t)at.n * q.pixels + at.px0 + lane;
-}
 
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll
@@ -262,82 +274,62 @@ __device__ __forceinline__ float2 *partial_at(const Norm &q, const Place &at, in
     const int64_t group = at.g0 + g;
     return q.partial + (((int64_t)at.n * q.groups + group) * q.ranks + at.rank) * q.parts + (at.slice - (int)(group * q.cpg / q.width));
 }
-// combine(g, k, lane, count, read, weight) for the groups of the slice, by k neighbouring lanes each (all lanes of a warp call it together, g < ng or not); read(i) is
-// the i-th CTA's pair of the group, weight(i) the number of values that it stands for.
+// combine(group, k, lane, count, read, weight) for `ng` groups of sample n from g0 on, by k neighbouring lanes each (all lanes of a warp call it together, the last groups
+// more than once); read(i) is the i-th CTA's pair of the group, weight(i) the number of values that it stands for.
 template <typename R, typename F>
-__device__ __forceinline__ void of_groups(const Place &at, R reader, F combine) {
-    const int k = sharers(at.ng), lane = threadIdx.x & (k - 1);
-    for (int g0 = 0; g0 < at.ng; g0 += kThreads / k) {
-        const int g = g0 + threadIdx.x / k;
-        reader(min(g, at.ng - 1), [&](int count, auto read, auto weight) { combine(g, k, lane, count, read, weight); });
+__device__ __forceinline__ void of_groups(int ng, R reader, F combine) {
+    const int k = sharers(ng), lane = threadIdx.x & (k - 1);
+    for (int g0 = 0; g0 < ng; g0 += kThreads / k) {
+        const int g = min(g0 + (int)threadIdx.x / k, ng - 1);
+        reader(g, [&](int count, auto read, auto weight) { combine(g, k, lane, count, read, weight); });
     }
     __syncwarp();
 }
-// In a cluster: `own` [ng] in the CTAs' shared memory.
+// Small calls, in a cluster: `own` [ng] in the CTAs' shared memory.
 template <typename F>
 __device__ __forceinline__ void of_cluster(const Norm &q, const Place &at, const float2 *own, F combine) {
     cluster_arrive();
     cluster_wait();
-    of_groups(at, [&](int g, auto call) {
+    of_groups(at.ng, [&](int g, auto call) {
         const uint32_t mine = smem_at(own + g);
         call(q.ranks,
              [&](int i) {
                  const uint32_t a = peer_address(mine, (uint32_t)i);
                  return make_float2(__uint_as_float(lds32_peer(a)), __uint_as_float(lds32_peer(a + 4)));
              },
-             [&](int i) { const int first = min(i * q.per, q.pixels); return (float)(min(first + q.per, q.pixels) - first) * (float)q.cpg; });
+             [&](int i) { return (float)(min((i + 1) * q.per, q.pixels) - i * q.per) * (float)q.cpg; });
     }, combine);
     cluster_arrive();                                        // (its wait is at the kernel's end: no CTA leaves while others read from it)
     __syncthreads();
 }
-// Large calls: out of `partial`, when all of the unit have written theirs.
+// Large calls: out of `partial`.
 template <typename F>
 __device__ __forceinline__ void of_memory(const Norm &q, const Place &at, F combine) {
-    of_groups(at, [&](int g, auto call) {
+    const float full = (float)q.per * (float)q.cpg, rest = (float)(q.pixels - (q.ranks - 1) * q.per) * (float)q.cpg;
+    of_groups(at.ng, [&](int g, auto call) {
         const int64_t group = at.g0 + g, from = group * q.cpg, to = from + q.cpg;
-        const int s0 = (int)(from / q.width), parts = q.parts == 1 ? 1 : (int)((to - 1) / q.width) + 1 - s0;
         const float2 *row = q.partial + ((int64_t)at.n * q.groups + group) * q.ranks * q.parts;
+        if (q.parts == 1) {
+            call(q.ranks, [&](int i) { return row[i]; }, [&](int i) { return i + 1 < q.ranks ? full : rest; });
+            return;
+        }
+        const int s0 = (int)(from / q.width), parts = (int)((to - 1) / q.width) + 1 - s0;
         call(q.ranks * parts,
-             [&](int i) { const int r = parts == 1 ? i : i / parts; return __ldcg(row + r * q.parts + i - r * parts); },
+             [&](int i) { const int r = i / parts; return row[r * q.parts + i - r * parts]; },
              [&](int i) {
-                 const int r = parts == 1 ? i : i / parts, first = min(r * q.per, q.pixels);
+                 const int r = i / parts;
                  const int64_t s = s0 + i - r * parts;
-                 return (float)(min(first + q.per, q.pixels) - first) * (float)(min(to, (s + 1) * q.width) - max(from, s * q.width));
+                 return (r + 1 < q.ranks ? full : rest) / (float)q.cpg * (float)(min(to, (s + 1) * q.width) - max(from, s * q.width));
              });
     }, combine);
     __syncthreads();
 }
-// The CTA's pairs are written: says so.  (All threads call it.)
-__device__ __forceinline__ void arrive(const Norm &q, uint32_t unit) {
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        __threadfence();
-        atomicAdd(q.arrived + unit, 1u);
-    }
-}
-// Waits for those of the whole unit; false where they do not come within some two seconds (the others run, the launch is cooperative): the results are NaN then.
-__device__ __forceinline__ bool all_here(const Norm &q, uint32_t unit) {
-    __shared__ int here;
-    if (threadIdx.x == 0) {
-        uint32_t n = 0;
-        const long long t0 = clock64();
-        for (;;) {
-            asm volatile("ld.acquire.gpu.global.u32 %0, [%1];" : "=r"(n) : "l"(q.arrived + unit) : "memory");
-            if (n >= q.unit || clock64() - t0 > 4000000000ll) break;
-            __nanosleep(64);
-        }
-        here = n >= q.unit;
-        __threadfence();
-    }
-    __syncthreads();
-    return here != 0;
-}
 
 // ---------------------------------------------------------------------------------------------------------------- forward
 
-// Pairs (mean, M2) of the CTA's groups to give(g, pair), out of what its threads have kept.
-template <typename T, bool kOne, bool kVec, typename F>
-__device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine<T> &me, float2 *threads, const uint4 *kept, F give) {
+// Pairs (mean, M2) of the CTA's groups to give(g, pair); item(i): what the thread has read, or reads, kAhead items at a time.
+template <typename T, bool kOne, int kAhead, typename I, typename F>
+__device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine<T> &me, float2 *threads, I item, F give) {
     constexpr int V = Of<T>::V, P = V / 2;
     uint64_t away[kOne ? 1 : P], s1[P], s2[P];               // away: less the thread's first values (kOne: its very first)
 #pragma unroll
@@ -346,15 +338,23 @@ __device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine
     for (int j = 0; j < (kOne ? 1 : P); ++j) away[j] = 0;
     if (me.n > 0 && me.items > 0) {
         uint64_t f[P];
-        Of<T>::open(kept[0], f);
+        Of<T>::open(item(0), f);
 #pragma unroll
         for (int j = 0; j < (kOne ? 1 : P); ++j) { const float2 v = f32x2_halves(f[j]); away[j] = f32x2(-v.x, kOne ? -v.x : -v.y); }
-#pragma unroll 2
-        for (int i = 0; i < me.items; ++i) {
-            Of<T>::open(kept[i * kThreads], f);
+        const auto add = [&](const uint4 &u) {
+            Of<T>::open(u, f);
 #pragma unroll
             for (int j = 0; j < P; ++j) { const uint64_t d = add2(f[j], away[kOne ? 0 : j]); s1[j] = add2(s1[j], d); s2[j] = fma2(d, d, s2[j]); }
+        };
+        int i = 0;
+        for (; i + kAhead <= me.items; i += kAhead) {
+            uint4 u[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) u[k] = item(i + k);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) add(u[k]);
         }
+        for (; i < me.items; ++i) add(item(i));
     }
     const float count = (float)me.items;
     if constexpr (kOne) {                                    // (mean, M2) of the thread
@@ -373,6 +373,8 @@ __device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine
     }
     __syncthreads();
     const int pixels = at.px1 - at.px0, k = sharers(at.ng), lane = threadIdx.x & (k - 1);
+    const bool is_last = at.rank + 1 == q.ranks;
+    const int some = is_last ? q.some_last : q.some, one_more = is_last ? q.more_last : q.more;
     for (int g0 = 0; g0 < at.ng; g0 += kThreads / k) {
         const int g = g0 + threadIdx.x / k;
         const Span in = span_of(q, at, min(g, at.ng - 1));
@@ -382,7 +384,7 @@ __device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine
         const auto entry = [&](int i, float *weight) {
             // (a product instead of a division: exact for i below 2^16, which entries are)
             const int l = across == 1 ? i : as_all ? (int)__umulhi((uint32_t)i, q.across_magic) : i / across, a = i - l * across;
-            const float here = (float)items_of(pixels, l, q.lanes);
+            const float here = (float)(l < one_more ? some + 1 : some);
             *weight = kOne ? here * V : here;
             return threads[kOne ? l * q.cv + in.lo / V + a : l * q.cv * V + in.lo + a];
         };
@@ -396,29 +398,21 @@ __device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine
         if (lane == 0 && g < at.ng) give(g, make_float2(m, rest));
     }
 }
-// Mean and rstd out of the CTAs' pairs, to the k lanes.
+// Mean and rstd out of the CTAs' pairs, to the k lanes; in 64 bits about the first one's mean, so that one pass does.
 template <typename R, typename W>
 __device__ __forceinline__ float2 combine_x(const Norm &q, int k, int lane, int count, R read, W weight) {
-    const float all = (float)q.pixels * (float)q.cpg, base = read(0).x;
-    float sum = 0.f, rest = 0.f, m;
-    if (count <= 4 * k) {                                    // (all reads in flight together)
-        float2 e[4];
-        float w[4];
-#pragma unroll
-        for (int j = 0; j < 4; ++j) { w[j] = 0.f; e[j] = make_float2(base, 0.f); if (lane + k * j < count) { e[j] = read(lane + k * j); w[j] = weight(lane + k * j); } }
-#pragma unroll
-        for (int j = 0; j < 4; ++j) sum += w[j] > 0.f ? w[j] * (e[j].x - base) : 0.f;
-        m = base + shared_sum(sum, k) / all;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) rest += w[j] > 0.f ? e[j].y + w[j] * (e[j].x - m) * (e[j].x - m) : 0.f;
-    } else {
-#pragma unroll 4
-        for (int i = lane; i < count; i += k) { const float w = weight(i); sum += w > 0.f ? w * (read(i).x - base) : 0.f; }
-        m = base + shared_sum(sum, k) / all;
-#pragma unroll 4
-        for (int i = lane; i < count; i += k) { const float2 e = read(i); const float w = weight(i); rest += w > 0.f ? e.y + w * (e.x - m) * (e.x - m) : 0.f; }
+    const float base = read(0).x;
+    double sum = 0.0, rest = 0.0;
+#pragma unroll 8
+    for (int i = lane; i < count; i += k) {
+        const float2 e = read(i);
+        const double w = weight(i), d = (double)e.x - (double)base;
+        sum += w * d;
+        rest += e.y + w * d * d;
     }
-    return make_float2(m, 1.f / sqrtf(shared_sum(rest, k) / all + q.eps));
+    for (int d = k >> 1; d; d >>= 1) { sum += __shfl_xor_sync(0xFFFFFFFFu, sum, d); rest += __shfl_xor_sync(0xFFFFFFFFu, rest, d); }
+    const double all = (double)q.pixels * (double)q.cpg, off = sum / all;
+    return make_float2((float)((double)base + off), 1.f / sqrtf((float)((rest - sum * off) / all) + q.eps));
 }
 
 template <int kAct, typename T>
@@ -433,9 +427,9 @@ __device__ __forceinline__ uint64_t activate(uint64_t p) {   // (NaN stays)
     return p;
 }
 
-// y, and the 8-bit forms, of the CTA's pixels; known(g): the statistics of the sample's group g.
-template <typename T, bool kVec, bool kHold, typename F>
-__device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, const uint4 *kept, F known) {
+// y, and the 8-bit forms, of the CTA's pixels, the last one first; known(g): the statistics of the sample's group g.
+template <typename T, bool kVec, bool kHold, int kAhead, typename I, typename F>
+__device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, I item, F known) {
     constexpr int V = Of<T>::V, P = V / 2;
     // (threads behind the last channel write the zeros that its block ends with; not of a block in which there is none)
     if (me.lane >= q.lanes || !(me.n > 0 || (kHold && (me.ch & ~127) < q.channels))) return;
@@ -447,7 +441,7 @@ __device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, const
         for (int i = 0; i < 2; ++i) {
             const int c = me.ch + 2 * j + i;
             if ((kVec && !kHold) || 2 * j + i < me.n) {
-                const float2 k = known(c / q.cpg);
+                const float2 k = known(group_of(q, c));
                 s[i] = k.y * (q.gamma ? q.gamma[c] : 1.f);
                 t[i] = fmaf(-k.x, s[i], q.beta ? q.beta[c] : 0.f);
             }
@@ -457,20 +451,29 @@ __device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, const
     T *y = reinterpret_cast<T *>(q.out) + me.row0 * q.ld_out + me.ch;
     const int64_t step_y = (int64_t)q.lanes * q.ld_out;
     const auto finish = [&](auto act) {
-        int64_t col = me.row0;
+        int i = me.items;
+        int64_t col = me.row0 + (int64_t)i * q.lanes;
+        y += i * step_y;
         const auto one = [&](const uint4 &u) {
             uint64_t f[P];
             Of<T>::open(u, f);
+            y -= step_y;
+            col -= q.lanes;
             if constexpr (kHold) if (q.x8) hold<V>(q, q.x8, f, col, me.ch);
 #pragma unroll
             for (int j = 0; j < P; ++j) f[j] = activate<decltype(act)::value, T>(fma2(f[j], a[j], b[j]));      // (0 behind the last channel: a = b = 0)
             if constexpr (kHold) if (q.y8) hold<V>(q, q.y8, f, col, me.ch);
-            if (!kHold || (q.out && me.n > 0)) put<kVec && !kHold>(y, Of<T>::close(f), q.vec_out, me.n);
-            y += step_y;
-            col += q.lanes;
+            if (!kHold || (q.out && me.n > 0)) put<kVec && !kHold>(y, Of<T>::close(f), q.vec_out, me.n, q.stream);
         };
-#pragma unroll 2
-        for (int i = 0; i < me.items; ++i) one(!kHold || me.n ? kept[i * kThreads] : make_uint4(0, 0, 0, 0));
+        const auto get = [&](int at) { return !kHold || me.n ? item(at) : make_uint4(0, 0, 0, 0); };
+        for (; i >= kAhead; i -= kAhead) {
+            uint4 u[kAhead];
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) u[k] = get(i - 1 - k);
+#pragma unroll
+            for (int k = 0; k < kAhead; ++k) one(u[k]);
+        }
+        for (; i > 0; --i) one(get(i - 1));
     };
     switch (q.act) {
         case kRelu: finish(std::integral_constant<int, kRelu>()); break;
@@ -480,22 +483,9 @@ __device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, const
     }
 }
 
-template <typename T, bool kVec>
-__device__ __forceinline__ void keep_x(const Norm &q, const Mine<T> &me, uint4 *kept) {
-    if (me.n <= 0) return;
-    const T *x = reinterpret_cast<const T *>(q.x) + me.row0 * q.ldx + me.ch;
-    const int64_t step = (int64_t)q.lanes * q.ldx;
-    if (kVec || (q.vec && me.n == Of<T>::V)) {
-        for (int i = 0; i < me.items; ++i) copy_async<16>(kept + i * kThreads, x + i * step);
-        copies_done();
-    } else {
-        for (int i = 0; i < me.items; ++i) kept[i * kThreads] = fetch<false>(x + i * step, q.vec, me.n);
-    }
-}
-
-// kOne: a thread's channels are of one group.  kVec: every thread's V channels are there, at multiples of 16 bytes.  kHold: an 8-bit form is written.  kCluster: a small call.
-template <typename T, bool kOne, bool kVec, bool kHold, bool kCluster>
-__global__ void __launch_bounds__(kThreads, 3)
+// kOne: a thread's channels are of one group.  kVec: every thread's V channels are there, at multiples of 16 bytes.  kHold: an 8-bit form is written.
+template <typename T, bool kOne, bool kVec, bool kHold>
+__global__ void __launch_bounds__(kThreads, kForwardCtas)
 norm_kernel(const __grid_constant__ Norm q) {
     constexpr int V = Of<T>::V;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -504,50 +494,63 @@ norm_kernel(const __grid_constant__ Norm q) {
     float2 *groups = reinterpret_cast<float2 *>(smem), *known = groups + most;           // of this CTA, of all
     float2 *threads = known + most;                                                      // [kThreads] or [kThreads][V]
     uint4 *kept = reinterpret_cast<uint4 *>(smem + ((2 * most * 8 + kThreads * (kOne ? 1 : V) * 8 + 15) & ~15)) + threadIdx.x;
-    if constexpr (kCluster) {
-        const Place at(q, blockIdx.x);
-        const Mine<T> me(q, at);
-        keep_x<T, kVec>(q, me, kept);
-        sum_x<T, kOne, kVec>(q, at, me, threads, kept, [&](int g, float2 pair) { groups[g] = pair; });
-        __syncthreads();
-        of_cluster(q, at, groups, [&](int g, int k, int lane, int count, auto read, auto weight) {
-            const float2 s = combine_x(q, k, lane, count, read, weight);
-            if (lane == 0 && g < at.ng) {
-                known[g] = s;
-                if (at.rank == 0) *reinterpret_cast<float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + at.g0 + g)) = s;
-            }
-        });
-        finish_y<T, kVec, kHold>(q, me, kept, [&](int g) { return known[g - at.g0]; });
-        __syncwarp();
-        cluster_wait();
-    } else {
-        for (uint32_t t = blockIdx.x; t < q.tiles;) {
-            const uint32_t unit = t / q.unit, end = min((unit + 1) * q.unit, q.tiles);
-            const bool again = t + gridDim.x < end;                                      // (more tiles of the unit than CTAs)
-            for (uint32_t u = t; u < end; u += gridDim.x) {
-                const Place at(q, u);
-                const Mine<T> me(q, at);
-                keep_x<T, kVec>(q, me, kept);
-                sum_x<T, kOne, kVec>(q, at, me, threads, kept, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
-                arrive(q, unit);
-            }
-            const bool ok = all_here(q, unit);
-            for (; t < end; t += gridDim.x) {
-                const Place at(q, t);
-                const Mine<T> me(q, at);
-                of_memory(q, at, [&](int g, int k, int lane, int count, auto read, auto weight) {
-                    const float2 s = ok ? combine_x(q, k, lane, count, read, weight) : make_float2(NAN, NAN);
-                    if (lane == 0 && g < at.ng) {
-                        known[g] = s;
-                        if (at.rank == 0 && (at.g0 + g) * q.cpg >= at.c0) *reinterpret_cast<float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + at.g0 + g)) = s;
-                    }
-                });
-                if (again) keep_x<T, kVec>(q, me, kept);
-                finish_y<T, kVec, kHold>(q, me, kept, [&](int g) { return known[g - at.g0]; });
-                __syncthreads();
-            }
+    const Place at(q, blockIdx.x);
+    const Mine<T> me(q, at);
+    if (me.n > 0) {
+        const T *x = reinterpret_cast<const T *>(q.x) + me.row0 * q.ldx + me.ch;
+        const int64_t step = (int64_t)q.lanes * q.ldx;
+        if (kVec || (q.vec && me.n == V)) {
+            for (int i = 0; i < me.items; ++i) copy_async<16>(kept + i * kThreads, x + i * step);
+            copies_done();
+        } else {
+            for (int i = 0; i < me.items; ++i) kept[i * kThreads] = fetch<false>(x + i * step, q.vec, me.n);
         }
     }
+    const auto item = [&](int i) { return kept[i * kThreads]; };
+    sum_x<T, kOne, 2>(q, at, me, threads, item, [&](int g, float2 pair) { groups[g] = pair; });
+    __syncthreads();
+    of_cluster(q, at, groups, [&](int g, int k, int lane, int count, auto read, auto weight) {
+        const float2 s = combine_x(q, k, lane, count, read, weight);
+        if (lane == 0) {
+            known[g] = s;
+            if (at.rank == 0) *reinterpret_cast<float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + at.g0 + g)) = s;
+        }
+    });
+    finish_y<T, kVec, kHold, 2>(q, me, item, [&](int g) { return known[g - at.g0]; });
+    __syncwarp();
+    cluster_wait();
+}
+
+// The two of a large call.
+template <typename T, bool kOne, bool kVec>
+__global__ void __launch_bounds__(kThreads, kForwardCtas)
+norm_sum_kernel(const __grid_constant__ Norm q) {
+    __shared__ float2 threads[kThreads * (kOne ? 1 : Of<T>::V)];
+    wait_for_prerequisites();
+    const Place at(q, blockIdx.x);
+    const Mine<T> me(q, at);
+    const T *x = reinterpret_cast<const T *>(q.x) + me.row0 * q.ldx + me.ch;
+    const int64_t step = (int64_t)q.lanes * q.ldx;
+    sum_x<T, kOne, 8>(q, at, me, threads, [&](int i) { return fetch<kVec>(x + i * step, q.vec, me.n); }, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
+}
+template <typename T, bool kVec, bool kHold>
+__global__ void __launch_bounds__(kThreads, kForwardCtas)
+norm_finish_kernel(const __grid_constant__ Norm q) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    float2 *known = reinterpret_cast<float2 *>(smem);
+    wait_for_prerequisites();
+    const Place at(q, gridDim.x - 1 - blockIdx.x);
+    const Mine<T> me(q, at);
+    of_memory(q, at, [&](int g, int k, int lane, int count, auto read, auto weight) {
+        const float2 s = combine_x(q, k, lane, count, read, weight);
+        if (lane == 0) {
+            known[g] = s;
+            if (at.rank == 0 && (at.g0 + g) * q.cpg >= at.c0) *reinterpret_cast<float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + at.g0 + g)) = s;
+        }
+    });
+    const T *x = reinterpret_cast<const T *>(q.x) + me.row0 * q.ldx + me.ch;
+    const int64_t step = (int64_t)q.lanes * q.ldx;
+    finish_y<T, kVec, kHold, 4>(q, me, [&](int i) { return fetch<kVec && !kHold>(x + i * step, q.vec, me.n); }, [&](int g) { return known[g - at.g0]; });
 }
 
 // --------------------------------------------------------------------------------------------------------------- backward
@@ -630,7 +633,7 @@ __device__ __forceinline__ void affine_of(const Norm &q, const Place &at, const 
             if (!kOne || j + i == 0) mean[m] = rstd[m] = 0.f;
             if (j + i >= me.n) continue;
             if (!kOne || j + i == 0) {
-                const float2 s = *reinterpret_cast<const float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + c / q.cpg));
+                const float2 s = *reinterpret_cast<const float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + group_of(q, c)));
                 mean[m] = s.x; rstd[m] = s.y;
             }
             const float beta = q.beta ? q.beta[c] : 0.f;
@@ -686,9 +689,9 @@ __device__ __forceinline__ void with_act(int act, F f) {
     }
 }
 
-// Sums of e and e h of the CTA's channels to q.sums, and of its groups (times gamma) to give(g, pair).  kept(i): what the thread has kept.
-template <typename T, bool kOne, bool k8, bool kVec, typename K, typename F>
-__device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine<T> &me, float2 *channels, K kept, F give) {
+// Sums of e and e h of the CTA's channels to q.sums, and of its groups (times gamma) to give(g, pair).  item(i): what the thread has read, or reads, kAhead at a time.
+template <typename T, bool kOne, bool k8, bool kVec, int kAhead, typename K, typename F>
+__device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine<T> &me, float2 *channels, K item, F give) {
     constexpr int V = Of<T>::V, P = V / 2, M = kOne ? 1 : V;
     Affine<P> k;
     float mean[M], rstd[M];
@@ -703,13 +706,25 @@ __device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine
     for (int j = 0; j < P; ++j) db[j] = dg[j] = 0;
     if (me.n > 0)
         with_act(q.act, [&](auto act) {
-#pragma unroll 1
-            for (int i = 0; i < me.items; ++i) {
+            const auto add = [&](const Item &u) {
                 uint64_t d[P], x[P];
-                Reader<T, k8, kVec>::open(kept(i), d, x);
+                Reader<T, k8, kVec>::open(u, d, x);
                 slope<decltype(act)::value, T, P>(q, at.n, me.ch, k, x, d);
 #pragma unroll
                 for (int j = 0; j < P; ++j) { db[j] = add2(db[j], d[j]); dg[j] = fma2(d[j], fma2(x[j], r[kOne ? 0 : j], s[kOne ? 0 : j]), dg[j]); }
+            };
+            int i = 0;
+#pragma unroll 1
+            for (; i + kAhead <= me.items; i += kAhead) {
+                Item u[kAhead];
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) u[j] = item(i + j);
+#pragma unroll
+                for (int j = 0; j < kAhead; ++j) add(u[j]);
+            }
+            if constexpr (kAhead > 1) {
+#pragma unroll 1
+                for (; i < me.items; ++i) add(item(i));
             }
         });
     const int row = q.cv * V;
@@ -752,9 +767,9 @@ __device__ __forceinline__ float2 combine_e(const Norm &q, int k, int lane, int 
     return make_float2(shared_sum(t.x, k) / all, shared_sum(t.y, k) / all);
 }
 
-// dx of the CTA's pixels; known(g): m1 and m2 of the sample's group g.  dx = rstd (gamma e - m1 - h m2) = a e + B x + C.
-template <typename T, bool kOne, bool k8, bool kVec, typename K, typename F>
-__device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const Mine<T> &me, K kept, F known) {
+// dx of the CTA's pixels, the last one first; known(g): m1 and m2 of the sample's group g.  dx = rstd (gamma e - m1 - h m2) = a e + B x + C.
+template <typename T, bool kOne, bool k8, bool kVec, int kAhead, typename K, typename F>
+__device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const Mine<T> &me, K item, F known) {
     constexpr int V = Of<T>::V, P = V / 2, M = kOne ? 1 : V;
     if (me.n <= 0) return;
     Affine<P> k;
@@ -767,7 +782,7 @@ __device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const 
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int m = kOne ? 0 : 2 * j + i;
-            const float2 g = m < me.n ? known((me.ch + m) / q.cpg) : make_float2(0.f, 0.f);
+            const float2 g = m < me.n ? known(group_of(q, me.ch + m)) : make_float2(0.f, 0.f);
             b[i] = -rstd[m] * rstd[m] * g.y;
             c[i] = -fmaf(b[i], mean[m], rstd[m] * g.x);
         }
@@ -776,14 +791,26 @@ __device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const 
     T *dx = reinterpret_cast<T *>(q.out) + me.row0 * q.ld_out + me.ch;
     const int64_t step_out = (int64_t)q.lanes * q.ld_out;
     with_act(q.act, [&](auto act) {
-#pragma unroll 1
-        for (int i = 0; i < me.items; ++i) {
+        const auto finish = [&](int i, const Item &u) {
             uint64_t d[P], x[P];
-            Reader<T, k8, kVec>::open(kept(i), d, x);
+            Reader<T, k8, kVec>::open(u, d, x);
             slope<decltype(act)::value, T, P>(q, at.n, me.ch, k, x, d);
 #pragma unroll
             for (int j = 0; j < P; ++j) d[j] = fma2(d[j], k.a[j], fma2(x[j], B[kOne ? 0 : j], C[kOne ? 0 : j]));
-            put<kVec>(dx + i * step_out, Of<T>::close(d), q.vec_out, me.n);
+            put<kVec>(dx + i * step_out, Of<T>::close(d), q.vec_out, me.n, q.stream);
+        };
+        int i = me.items;
+#pragma unroll 1
+        for (; i >= kAhead; i -= kAhead) {
+            Item u[kAhead];
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) u[j] = item(i - 1 - j);
+#pragma unroll
+            for (int j = 0; j < kAhead; ++j) finish(i - 1 - j, u[j]);
+        }
+        if constexpr (kAhead > 1) {
+#pragma unroll 1
+            for (; i > 0; --i) finish(i - 1, item(i - 1));
         }
     });
 }
@@ -841,8 +868,8 @@ struct Kept {
     }
 };
 
-template <typename T, bool kOne, bool k8, bool kVec, bool kCluster>
-__global__ void __launch_bounds__(kThreads, 2)
+template <typename T, bool kOne, bool k8, bool kVec>
+__global__ void __launch_bounds__(kThreads, kBackwardCtas)
 norm_back_kernel(const __grid_constant__ Norm q) {
     constexpr int V = Of<T>::V;
     extern __shared__ __align__(16) uint8_t smem[];
@@ -851,44 +878,44 @@ norm_back_kernel(const __grid_constant__ Norm q) {
     float2 *groups = reinterpret_cast<float2 *>(smem), *known = groups + most;
     float2 *channels = known + most;                                         // [lanes][cv * V]: sums of e and of e h
     const Kept<T, k8, kVec> kept(q, smem + ((2 * most * 8 + kThreads * V * 8 + 15) & ~15));
-    if constexpr (kCluster) {
-        const Place at(q, blockIdx.x);
-        const Mine<T> me(q, at);
-        kept.fill(q, me);
-        sum_e<T, kOne, k8, kVec>(q, at, me, channels, kept, [&](int g, float2 pair) { groups[g] = pair; });
-        __syncthreads();
-        of_cluster(q, at, groups, [&](int g, int k, int lane, int count, auto read, auto) {
-            const float2 m = combine_e(q, k, lane, count, read);
-            if (lane == 0 && g < at.ng) known[g] = m;
-        });
-        finish_dx<T, kOne, k8, kVec>(q, at, me, kept, [&](int g) { return known[g - at.g0]; });
-        __syncwarp();
-        cluster_wait();
-    } else {
-        for (uint32_t t = blockIdx.x; t < q.tiles;) {
-            const uint32_t unit = t / q.unit, end = min((unit + 1) * q.unit, q.tiles);
-            const bool again = t + gridDim.x < end;
-            for (uint32_t u = t; u < end; u += gridDim.x) {
-                const Place at(q, u);
-                const Mine<T> me(q, at);
-                kept.fill(q, me);
-                sum_e<T, kOne, k8, kVec>(q, at, me, channels, kept, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
-                arrive(q, unit);
-            }
-            const bool ok = all_here(q, unit);
-            for (; t < end; t += gridDim.x) {
-                const Place at(q, t);
-                const Mine<T> me(q, at);
-                of_memory(q, at, [&](int g, int k, int lane, int count, auto read, auto) {
-                    const float2 m = ok ? combine_e(q, k, lane, count, read) : make_float2(NAN, NAN);
-                    if (lane == 0 && g < at.ng) known[g] = m;
-                });
-                if (again) kept.fill(q, me);
-                finish_dx<T, kOne, k8, kVec>(q, at, me, kept, [&](int g) { return known[g - at.g0]; });
-                __syncthreads();
-            }
-        }
-    }
+    const Place at(q, blockIdx.x);
+    const Mine<T> me(q, at);
+    kept.fill(q, me);
+    sum_e<T, kOne, k8, kVec, 1>(q, at, me, channels, kept, [&](int g, float2 pair) { groups[g] = pair; });
+    __syncthreads();
+    of_cluster(q, at, groups, [&](int g, int k, int lane, int count, auto read, auto) {
+        const float2 m = combine_e(q, k, lane, count, read);
+        if (lane == 0) known[g] = m;
+    });
+    finish_dx<T, kOne, k8, kVec, 1>(q, at, me, kept, [&](int g) { return known[g - at.g0]; });
+    __syncwarp();
+    cluster_wait();
+}
+
+template <typename T, bool kOne, bool k8, bool kVec>
+__global__ void __launch_bounds__(kThreads, kBackwardCtas)
+norm_back_sum_kernel(const __grid_constant__ Norm q) {
+    __shared__ float2 channels[kThreads * Of<T>::V];
+    wait_for_prerequisites();
+    const Place at(q, blockIdx.x);
+    const Mine<T> me(q, at);
+    const Reader<T, k8, kVec> read(q, me);
+    sum_e<T, kOne, k8, kVec, 4>(q, at, me, channels, read, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
+}
+template <typename T, bool kOne, bool k8, bool kVec>
+__global__ void __launch_bounds__(kThreads, kBackwardCtas)
+norm_back_finish_kernel(const __grid_constant__ Norm q) {
+    extern __shared__ __align__(16) uint8_t smem[];
+    float2 *known = reinterpret_cast<float2 *>(smem);
+    wait_for_prerequisites();
+    const Place at(q, gridDim.x - 1 - blockIdx.x);
+    const Mine<T> me(q, at);
+    of_memory(q, at, [&](int g, int k, int lane, int count, auto read, auto) {
+        const float2 m = combine_e(q, k, lane, count, read);
+        if (lane == 0) known[g] = m;
+    });
+    const Reader<T, k8, kVec> read(q, me);
+    finish_dx<T, kOne, k8, kVec, 4>(q, at, me, read, [&](int g) { return known[g - at.g0]; });
 }
 
 // dbeta and dgamma: the sums of all CTAs' [rows][2][channels], a warp's lanes on 32 neighbouring ones, in one order.
@@ -922,7 +949,7 @@ struct Plan {
     bool cluster;                        // a small call
     int width, slices, ranks, per, cv, parts;
     int resident, fixed_smem;            // items a thread keeps, bytes in front of them
-    int64_t tiles, unit, units;
+    int64_t tiles;
 };
 constexpr int kSms = 148;
 constexpr int64_t kSmallBytes = 12 << 20;
@@ -961,35 +988,28 @@ Plan plan_of(const crisp_group_norm_t &d, bool back, bool from8, bool eight) {
         p.parts = 1;
     }
     if (!p.cluster) {
-        // slices of whole groups and up to 512 channels; tiles that leave room for three CTAs an SM (backward two)
-        int width = whole ? unit : align;
-        while (width < C && width + (whole ? unit : align) <= std::min(most, 64 * V)) width += whole ? unit : align;
-        slice(width);
-        p.parts = whole ? 1 : (cpg + p.width - 2) / p.width + 1;
-        const int per_sm = back ? 2 : 3;
-        const int64_t items = std::max<int64_t>(1, ((int64_t)kMaxSmem / per_sm - 1024 - p.fixed_smem) / (kThreads * item)), slices = batch * p.slices, grid = kSms * per_sm;
-        int64_t ranks = ceil_div(d.pixels, items * (kThreads / p.cv));
-        // as many as fill the last round, too
-        const int64_t rounds = ceil_div(slices * ranks, grid), filled = rounds * grid / slices;
-        if (filled > ranks) ranks = std::min<int64_t>(filled, ceil_div(d.pixels, 2 * (kThreads / p.cv)) > ranks ? ceil_div(d.pixels, 2 * (kThreads / p.cv)) : ranks);
-        rank(ranks);
+        slice((int)std::min<int64_t>(ceil_div(C, align) * align, most));
+        p.parts = p.slices == 1 ? 1 : (cpg + p.width - 2) / p.width + 1;
+        // as many CTAs as run at once; or, where the slices do not go into that, as many as that is filled some times over.  (Every CTA of the second kernel adds the pairs of
+        // its sample's: 128 of them at most.)
+        const int64_t slices = batch * p.slices, grid = kSms * (back ? kBackwardCtas : kForwardCtas), once = grid / slices;
+        const int64_t ranks = once * slices * 20 >= grid * 17 ? once : ceil_div(4 * grid, slices);
+        rank(std::min<int64_t>(std::min<int64_t>(ranks, 128), ceil_div(d.pixels, 4 * (kThreads / p.cv))));
+        p.resident = 0;
+        p.fixed_smem = (p.width / cpg + 2) * 8;
     }
     p.tiles = batch * p.slices * p.ranks;
-    p.unit = p.parts == 1 ? p.ranks : (int64_t)p.slices * p.ranks;
-    p.units = p.tiles / p.unit;
     return p;
 }
 
-// Workspace: the sums of gamma's and beta's gradients; for large calls the CTAs' pairs and the counters.
-struct Space { size_t sums, partial, arrived, total; };
+// Workspace: the sums of gamma's and beta's gradients; for large calls the CTAs' pairs.
+struct Space { size_t partial, total; };
 Space space_of(const crisp_group_norm_t &d, const Plan &p, bool back) {
     Space s{};
     size_t at = 0;
     if (back) at += align_up((size_t)d.batch * p.ranks * 2 * d.channels * sizeof(float));
     s.partial = at;
     if (!p.cluster) at += align_up((size_t)d.batch * d.groups * p.ranks * p.parts * sizeof(float2));
-    s.arrived = at;
-    if (!p.cluster) at += align_up((size_t)p.units * sizeof(uint32_t));
     s.total = at;
     return s;
 }
@@ -1004,46 +1024,31 @@ crisp_status_t check(const crisp_group_norm_t *d) {
 }
 
 template <auto kernel>
-cudaError_t allow(bool cluster) {                                            // (once a kernel and device)
+cudaError_t allow() {                                                        // (once a kernel and device)
     static std::atomic<uint64_t> ready{0};
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     if (device < 64 && ready.load(std::memory_order_relaxed) >> device & 1) return cudaSuccess;
     e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxSmem);
-    if (e == cudaSuccess && cluster) e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+    if (e == cudaSuccess) e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess && device < 64) ready.fetch_or(1ull << device, std::memory_order_relaxed);
     return e;
 }
-template <auto small, auto large>
-cudaError_t run(const Plan &p, const Norm &q, int per_sm, int item, cudaStream_t st) {
-    if (p.tiles > 0x7FFFFFFFll / 2) return cudaErrorInvalidValue;
+template <auto small, auto sum, auto finish>
+cudaError_t run(const Plan &p, const Norm &q, int item, cudaStream_t st) {
+    if (p.tiles > 0x7FFFFFFFll) return cudaErrorInvalidValue;
     const size_t smem = p.fixed_smem + (size_t)p.resident * kThreads * item;
-    cudaError_t e = p.cluster ? allow<small>(true) : allow<large>(false);
-    if (e != cudaSuccess) return e;
-    if (p.cluster) return launch_clusters(small, (unsigned)p.tiles, kThreads, smem, st, (unsigned)q.ranks, q);
-    e = cudaMemsetAsync(q.arrived, 0, (size_t)p.units * sizeof(uint32_t), st);
-    if (e != cudaSuccess) return e;
-    int device = 0;
-    e = cudaGetDevice(&device);
-    if (e != cudaSuccess) return e;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeCooperative;                             // (its CTAs wait for one another)
-    attr[0].val.cooperative = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3((unsigned)std::min<int64_t>(p.tiles, (int64_t)sm_count_of(device) * per_sm));
-    cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem;
-    cfg.stream = st;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    e = cudaLaunchKernelEx(&cfg, large, q);
-    if (e != cudaSuccess) (void)cudaGetLastError();
-    return e;
+    if (p.cluster) {
+        const cudaError_t e = allow<small>();
+        return e != cudaSuccess ? e : launch_clusters(small, (unsigned)p.tiles, kThreads, smem, st, (unsigned)q.ranks, q);
+    }
+    const cudaError_t e = launch_chained(sum, (unsigned)p.tiles, kThreads, 0, st, q);
+    return e != cudaSuccess ? e : launch_chained(finish, (unsigned)p.tiles, kThreads, smem, st, q);
 }
 template <typename T, bool kOne, bool kVec, bool kHold>
 cudaError_t forward(const Plan &p, const Norm &q, cudaStream_t st) {
-    return run<norm_kernel<T, kOne, kVec, kHold, true>, norm_kernel<T, kOne, kVec, kHold, false>>(p, q, 3, 16, st);
+    return run<norm_kernel<T, kOne, kVec, kHold>, norm_sum_kernel<T, kOne, kVec>, norm_finish_kernel<T, kVec, kHold>>(p, q, 16, st);
 }
 template <typename T>
 cudaError_t forward(const Plan &p, const Norm &q, bool one, bool vec, bool hold, cudaStream_t st) {
@@ -1056,7 +1061,8 @@ cudaError_t forward(const Plan &p, const Norm &q, bool one, bool vec, bool hold,
 }
 template <typename T, bool kOne, bool k8, bool kVec>
 cudaError_t backward(const Plan &p, const Norm &q, cudaStream_t st) {
-    return run<norm_back_kernel<T, kOne, k8, kVec, true>, norm_back_kernel<T, kOne, k8, kVec, false>>(p, q, 2, k8 ? 16 + Of<T>::V + 4 : 32, st);
+    return run<norm_back_kernel<T, kOne, k8, kVec>, norm_back_sum_kernel<T, kOne, k8, kVec>, norm_back_finish_kernel<T, kOne, k8, kVec>>(
+        p, q, k8 ? 16 + Of<T>::V + 4 : 32, st);
 }
 template <typename T>
 cudaError_t backward(const Plan &p, const Norm &q, bool one, bool vec, bool from8, cudaStream_t st) {
@@ -1072,12 +1078,14 @@ Norm norm_of(const crisp_group_norm_t &d, const Plan &p, const Space &s, void *w
     uint8_t *w = reinterpret_cast<uint8_t *>(workspace);
     q.sums = reinterpret_cast<float *>(w);
     q.partial = reinterpret_cast<float2 *>(w + s.partial);
-    q.arrived = reinterpret_cast<uint32_t *>(w + s.arrived);
     q.pixels = (int)d.pixels; q.channels = d.channels; q.groups = d.groups; q.cpg = d.channels / d.groups;
     q.width = p.width; q.slices = p.slices; q.ranks = p.ranks; q.per = p.per; q.parts = p.parts; q.cv = p.cv;
     q.lanes = kThreads / p.cv;
+    const int last = q.pixels - (p.ranks - 1) * p.per;
+    q.some = p.per / q.lanes; q.more = p.per % q.lanes; q.some_last = last / q.lanes; q.more_last = last % q.lanes;
     q.resident = p.resident;
-    q.tiles = (uint32_t)p.tiles; q.unit = (uint32_t)p.unit;
+    if (q.cpg > 1 && (double)d.channels * q.cpg < 4294967296.0) q.cpg_magic = (uint32_t)((((uint64_t)1 << 32) + q.cpg - 1) / q.cpg);
+    q.stream = !p.cluster && (double)d.batch * d.pixels * d.channels * (d.dtype == 1 ? 4 : 2) > 64e6;
     q.act = d.activation;
     q.eps = (float)d.eps;
     const Act8 a = act8(d.channels, d.batch * d.pixels);
