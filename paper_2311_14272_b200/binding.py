@@ -112,7 +112,9 @@ def _bind_network():
             if getattr(module, "built_for", None) == "%s %d.%d" % (release, *sys.version_info[:2]):
                 module.bind(*[C.cast(f, C.c_void_p).value for f in (lib.crisp_decode, lib.crisp_spmm8_sizes, lib.crisp_spmm8, lib.crisp_decode8,
                                                                         lib.crisp_encode8_sizes, lib.crisp_encode8, lib.crisp_destroy8, lib.crisp_adamw,
-                                                                        lib.crisp_adamw_moments)])
+                                                                        lib.crisp_adamw_moments, lib.crisp_quantize8_sizes, lib.crisp_group_norm_sizes,
+                                                                        lib.crisp_group_norm, lib.crisp_group_norm_backward, lib.crisp_weight_grad8_sizes,
+                                                                        lib.crisp_weight_grad8)])
                 _network = module
             else:
                 _network = False
@@ -1016,6 +1018,13 @@ class HybridLayer:
         """dW = dY X^T [rows, k] from the activations that quantize8 (or a GroupNorm) kept in 8 bits.  dy: bf16 [rows, ncols], or with tokens=True [ncols, rows].
         masked: 0 outside the layer's mask, and blocks that are not kept are not computed (what AdamW takes under the mask); else every weight's gradient, as a
         saliency takes it.  dw: where to write it, bf16 (dw_dtype 0) or fp32 (1); accumulate: to add it there.  gradient_status says whether a wait ran out."""
+        if dw is None and stream is None and not accumulate and self._gpu is not None and self._gpu == _current_device() and (self.mask or not masked):
+            done = _network.gradient8(dy, act.buffer, self._grad_status, self.mask if masked else 0, self.desc.rows, self.desc.k, act.k, act.ncols, 0, 0, 0, tokens, dw_dtype,
+                                      self._gpu, _current_stream())
+            if done is not None:
+                if done[0]:
+                    raise CrispError(done[0], "crisp_weight_grad8")
+                return done[1]
         shape = (act.ncols, self.desc.rows) if tokens else (self.desc.rows, act.ncols)
         assert act.k == self.desc.k, "activations of another k"
         assert dy.shape == shape, "dY is [rows, ncols], or with tokens=True [ncols, rows], with the activations' columns"
@@ -1024,6 +1033,13 @@ class HybridLayer:
     def weight_gradient8_conv(self, dy_nhwc, act, kernel_h, kernel_w, pad, dw=None, dw_dtype=1, masked=False, accumulate=False, stream=None):
         """The same of a convolution (stride 1).  dy_nhwc: bf16 [batch, ho, wo, rows], dense but for the pitch of a pixel; act: the 8-bit form of the NHWC activation
         [batch, ho + kernel_h - 1 - 2 pad, wo + kernel_w - 1 - 2 pad, channels] (quantize8(x.view(-1, channels), tokens=True))."""
+        if dw is None and stream is None and not accumulate and kernel_h > 0 and self._gpu is not None and self._gpu == _current_device() and (self.mask or not masked):
+            done = _network.gradient8(dy_nhwc, act.buffer, self._grad_status, self.mask if masked else 0, self.desc.rows, self.desc.k, act.k, act.ncols, kernel_h, kernel_w,
+                                      pad, True, dw_dtype, self._gpu, _current_stream())
+            if done is not None:
+                if done[0]:
+                    raise CrispError(done[0], "crisp_weight_grad8")
+                return done[1]
         batch, ho, wo, rows = dy_nhwc.shape
         height, width = ho + kernel_h - 1 - 2 * pad, wo + kernel_w - 1 - 2 * pad
         assert rows == self.desc.rows and act.k * kernel_h * kernel_w == self.desc.k and act.ncols == batch * height * width and min(height, width) > 0, \
@@ -1306,6 +1322,7 @@ class GroupNorm:
         self.activation = self.ACTIVATIONS["none" if activation is None else activation]
         self.weight, self.bias = weight, bias
         self._types = {torch.bfloat16: 0, torch.float32: 1, torch.float16: 2}
+        self._native = bool(_network or _bind_network())
         crisp_group_norm_sizes(self._desc(1, 1, 0), False)                   # (channels, groups and eps that the library refuses are refused here)
 
     def _desc(self, batch, pixels, dtype):
@@ -1339,6 +1356,15 @@ class GroupNorm:
     def forward(self, x, y=None, keep_x=False, keep_y=False, plain_y=True, stream=None):
         """-> Normed.  keep_x, keep_y: x and y also in 8 bits, written in the same pass; plain_y=False: y in 8 bits alone.  y: where to write it (x itself, too)."""
         torch = self.torch
+        if y is None and stream is None and self._native and (plain_y or keep_y):
+            done = _network.norm(x, self.weight, self.bias, self.eps, self.channels, self.groups, self.activation, keep_x, keep_y, plain_y, _current_device(),
+                                 _current_stream())
+            if done is not None:
+                code, y, statistics, x8, y8, columns = done
+                if code:
+                    raise CrispError(code, "crisp_group_norm")
+                return Normed(y, statistics, x8 if x8 is None else Activations8(self.channels, columns, x8),
+                              y8 if y8 is None else Activations8(self.channels, columns, y8))
         ldx = self._rows(x, "x")
         device, (batch, pixels) = x.device, self._shape(x)
         self._parameters(device)
@@ -1360,6 +1386,15 @@ class GroupNorm:
     def backward(self, dy, x, statistics, dx=None, stream=None):
         """-> dx, dweight, dbias (fp32).  x: the forward pass's, as it was or in 8 bits (Normed.x8); statistics: Normed's.  dx: where to write it (dy or x, too)."""
         torch = self.torch
+        if dx is None and stream is None and self._native:
+            held = type(x) is Activations8
+            if not held or x.k == self.channels:
+                done = _network.norm_backward(dy, x.buffer if held else x, statistics, self.weight, self.bias, self.eps, self.channels, self.groups, self.activation,
+                                              x.ncols if held else -1, _current_device(), _current_stream())
+                if done is not None:
+                    if done[0]:
+                        raise CrispError(done[0], "crisp_group_norm_backward")
+                    return done[1:]
         ld_dy = self._rows(dy, "dy")
         device, (batch, pixels) = dy.device, self._shape(dy)
         self._parameters(device)

@@ -5,6 +5,7 @@
 #define PY_SSIZE_T_CLEAN
 #include <Python.h>
 
+#include <ATen/ops/empty.h>
 #include <ATen/ops/empty_strided.h>
 #include <torch/csrc/Exceptions.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -26,6 +27,12 @@ decltype(&crisp_encode8) lib_encode8;
 decltype(&crisp_destroy8) lib_destroy8;
 decltype(&crisp_adamw) lib_adamw;
 decltype(&crisp_adamw_moments) lib_moments;
+decltype(&crisp_quantize8_sizes) lib_quantize8_sizes;
+decltype(&crisp_group_norm_sizes) lib_norm_sizes;
+decltype(&crisp_group_norm) lib_norm;
+decltype(&crisp_group_norm_backward) lib_norm_backward;
+decltype(&crisp_weight_grad8_sizes) lib_grad8_sizes;
+decltype(&crisp_weight_grad8) lib_grad8;
 
 // The names of attributes, made once.
 struct {
@@ -369,10 +376,187 @@ PyObject *product8(PyObject *, PyObject *const *args, Py_ssize_t n) {
     END_HANDLE_TH_ERRORS
 }
 
-// bind(addresses of crisp_decode, crisp_spmm8_sizes, crisp_spmm8, crisp_decode8, crisp_encode8_sizes, crisp_encode8, crisp_destroy8, crisp_adamw and
-// crisp_adamw_moments)
+// A plain tensor on the GPU, or nullptr.
+const at::Tensor *on_gpu(PyObject *o, int64_t gpu) {
+    if (!THPVariable_CheckExact(o)) return nullptr;
+    const at::Tensor &t = THPVariable_Unpack(o);
+    return t.is_cuda() && t.layout() == at::kStrided && t.get_device() == gpu ? &t : nullptr;
+}
+// Elements from one pixel of a channels-last tensor to the next (as the binding's _pixel_pitch has them); -1: they do not lie one pitch apart.
+int64_t pixel_pitch(const at::Tensor &t) {
+    const int64_t last = t.dim() - 1;
+    if (t.stride(last) != 1 && t.size(last) != 1) return -1;
+    int64_t pitch = -1, count = 1;
+    for (int64_t i = last - 1; i >= 0; --i) {
+        if (t.size(i) == 1) continue;
+        if (pitch < 0) pitch = t.stride(i);
+        if (t.stride(i) != pitch * count) return -1;
+        count *= t.size(i);
+    }
+    return pitch < 0 ? t.size(last) : pitch;
+}
+// [channels] fp32 (None: null, which is fine); false: not what the call takes.
+bool per_channel(PyObject *o, int64_t channels, int64_t gpu, const float **p) {
+    *p = nullptr;
+    if (o == Py_None) return true;
+    const at::Tensor *t = on_gpu(o, gpu);
+    if (!t || t->scalar_type() != at::kFloat || t->numel() != channels || !t->is_contiguous()) return false;
+    *p = static_cast<const float *>(t->data_ptr());
+    return true;
+}
+bool integers(PyObject *const *args, int first, int n, long long *v) {
+    for (int i = 0; i < n; ++i) {
+        v[i] = PyLong_AsLongLong(args[first + i]);
+        if (v[i] == -1 && PyErr_Occurred()) return false;
+    }
+    return true;
+}
+// The descriptor of a norm over t, [batch, ..., channels]; false: not a tensor that the call takes.
+bool norm_of(const at::Tensor &t, const long long *v, double eps, crisp_group_norm_t *d, int64_t *pitch) {
+    const int64_t last = t.dim() - 1;
+    if (last < 1 || t.size(last) != v[0] || t.size(0) < 1) return false;
+    d->dtype = t.scalar_type() == at::kBFloat16 ? 0 : t.scalar_type() == at::kFloat ? 1 : t.scalar_type() == at::kHalf ? 2 : -1;
+    if (d->dtype < 0) return false;
+    *pitch = pixel_pitch(t);
+    if (*pitch < 0) return false;
+    d->batch = t.size(0);
+    d->pixels = 1;
+    for (int64_t i = 1; i < last; ++i) d->pixels *= t.size(i);
+    d->channels = (int32_t)v[0]; d->groups = (int32_t)v[1]; d->activation = (int32_t)v[2];
+    d->eps = eps;
+    return d->pixels > 0;
+}
+at::Tensor bytes_of(size_t n, const at::TensorOptions &on) { return at::empty_strided({(int64_t)n}, {1}, on.dtype(at::kByte)); }
+PyObject *or_none(at::Tensor &t) { return t.defined() ? THPVariable_Wrap(std::move(t)) : Py_NewRef(Py_None); }
+
+// norm(x, weight, bias, eps, channels, groups, activation, keep x, keep y, plain y, GPU, stream) -> (status, y, statistics, 8-bit x, 8-bit y, columns), or None: left to the
+// Python code.  All are allocated for the current stream, which `stream` has to be.
+PyObject *norm(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arguments("norm", n, 12)) return nullptr;
+    const double eps = PyFloat_AsDouble(args[3]);
+    if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+    long long v[8];
+    if (!integers(args, 4, 8, v)) return nullptr;
+    const at::Tensor *x = on_gpu(args[0], v[6]);
+    const float *gamma, *beta;
+    crisp_group_norm_t d{};
+    int64_t ldx = 0;
+    if (!x || !per_channel(args[1], v[0], v[6], &gamma) || !per_channel(args[2], v[0], v[6], &beta) || !norm_of(*x, v, eps, &d, &ldx)) Py_RETURN_NONE;
+    const at::TensorOptions on = at::TensorOptions().device(at::Device(at::kCUDA, (at::DeviceIndex)v[6]));
+    at::Tensor y, x8, y8, workspace, statistics;
+    size_t bytes = 0, held = 0;
+    crisp_status_t s = lib_norm_sizes(&d, 0, &bytes);
+    if (s == CRISP_OK && (v[3] || v[4])) s = lib_quantize8_sizes(d.channels, d.batch * d.pixels, &held);
+    if (s == CRISP_OK) {
+        if (v[5]) y = at::empty(x->sizes(), x->options().requires_grad(false));
+        statistics = at::empty_strided({d.batch, d.groups, 2}, {(int64_t)d.groups * 2, 2, 1}, on.dtype(at::kFloat));
+        if (v[3]) x8 = bytes_of(held, on);
+        if (v[4]) y8 = bytes_of(held, on);
+        if (bytes) workspace = bytes_of(bytes, on);
+        Py_BEGIN_ALLOW_THREADS
+        s = lib_norm(&d, x->data_ptr(), ldx, gamma, beta, y.defined() ? y.data_ptr() : nullptr, d.channels, static_cast<float *>(statistics.data_ptr()),
+                     x8.defined() ? x8.data_ptr() : nullptr, y8.defined() ? y8.data_ptr() : nullptr, workspace.defined() ? workspace.data_ptr() : nullptr,
+                     reinterpret_cast<void *>((uintptr_t)v[7]));
+        Py_END_ALLOW_THREADS
+    }
+    Ref a(or_none(y)), b(or_none(statistics)), c(or_none(x8)), e(or_none(y8));
+    return a.p && b.p && c.p && e.p ? Py_BuildValue("lOOOOL", (long)s, a.p, b.p, c.p, e.p, (long long)(d.batch * d.pixels)) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
+// norm_backward(dy, x, statistics, weight, bias, eps, channels, groups, activation, columns, GPU, stream) -> (status, dx, dweight, dbias), or None: left to the Python code.
+// x: a tensor like dy; or the buffer of an 8-bit form of so many columns (-1: it is a tensor).
+PyObject *norm_backward(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arguments("norm_backward", n, 12)) return nullptr;
+    const double eps = PyFloat_AsDouble(args[5]);
+    if (eps == -1.0 && PyErr_Occurred()) return nullptr;
+    long long v[6];
+    if (!integers(args, 6, 6, v)) return nullptr;
+    const at::Tensor *dy = on_gpu(args[0], v[4]), *x = on_gpu(args[1], v[4]), *st = on_gpu(args[2], v[4]);
+    const float *gamma, *beta;
+    crisp_group_norm_t d{};
+    int64_t ld_dy = 0, ldx = 0;
+    if (!dy || !x || !st || !per_channel(args[3], v[0], v[4], &gamma) || !per_channel(args[4], v[0], v[4], &beta) || !norm_of(*dy, v, eps, &d, &ld_dy)) Py_RETURN_NONE;
+    const bool held = v[3] >= 0;
+    if (held ? v[3] != d.batch * d.pixels : !x->sizes().equals(dy->sizes()) || x->scalar_type() != dy->scalar_type()) Py_RETURN_NONE;
+    if (!held && (ldx = pixel_pitch(*x)) < 0) Py_RETURN_NONE;
+    if (st->scalar_type() != at::kFloat || st->dim() != 3 || st->size(0) != d.batch || st->size(1) != d.groups || st->size(2) != 2 || !st->is_contiguous()) Py_RETURN_NONE;
+    const at::TensorOptions on = at::TensorOptions().device(at::Device(at::kCUDA, (at::DeviceIndex)v[4]));
+    at::Tensor dx, dw, db, workspace;
+    size_t bytes = 0;
+    crisp_status_t s = lib_norm_sizes(&d, 1, &bytes);
+    if (s == CRISP_OK) {
+        dx = at::empty(dy->sizes(), dy->options().requires_grad(false));
+        dw = at::empty_strided({d.channels}, {1}, on.dtype(at::kFloat));
+        db = at::empty_strided({d.channels}, {1}, on.dtype(at::kFloat));
+        workspace = bytes_of(bytes, on);
+        Py_BEGIN_ALLOW_THREADS
+        s = lib_norm_backward(&d, dy->data_ptr(), ld_dy, held ? nullptr : x->data_ptr(), ldx, held ? x->data_ptr() : nullptr, static_cast<const float *>(st->data_ptr()), gamma, beta,
+                              dx.data_ptr(), d.channels, static_cast<float *>(dw.data_ptr()), static_cast<float *>(db.data_ptr()), workspace.data_ptr(),
+                              reinterpret_cast<void *>((uintptr_t)v[5]));
+        Py_END_ALLOW_THREADS
+    }
+    Ref a(or_none(dx)), b(or_none(dw)), c(or_none(db));
+    return a.p && b.p && c.p ? Py_BuildValue("lOOO", (long)s, a.p, b.p, c.p) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
+// gradient8(dY, buffer of the activations, status word, mask, rows, k, channels, columns, kernel_h, kernel_w, pad, tokens, fp32, GPU, stream) -> (status, dW), or None: left to
+// the Python code.  kernel_h 0: dY is a matrix of a linear layer; else NHWC.
+PyObject *gradient8(PyObject *, PyObject *const *args, Py_ssize_t n) {
+    HANDLE_TH_ERRORS
+    if (!arguments("gradient8", n, 15)) return nullptr;
+    long long v[12];
+    if (!integers(args, 3, 12, v)) return nullptr;
+    const int64_t rows = v[1], k = v[2], channels = v[3], columns = v[4], gpu = v[10];
+    const at::Tensor *dy = on_gpu(args[0], gpu), *act = on_gpu(args[1], gpu), *status = on_gpu(args[2], gpu);
+    if (!dy || !act || !status || dy->scalar_type() != at::kBFloat16) Py_RETURN_NONE;
+    crisp_weight_grad8_t g{};
+    crisp_conv_desc_t conv{};
+    g.rows = (int32_t)rows; g.k = (int32_t)k;
+    if (v[5] == 0) {
+        const bool tokens = v[8] != 0;
+        if (dy->dim() != 2 || channels != k || dy->size(tokens ? 1 : 0) != rows || dy->size(tokens ? 0 : 1) != columns || (dy->stride(1) != 1 && dy->size(1) != 1)) Py_RETURN_NONE;
+        g.ncols = columns; g.ld_dy = dy->size(0) > 1 ? dy->stride(0) : dy->size(1); g.dy_layout = tokens;
+    } else {
+        if (dy->dim() != 4 || dy->size(3) != rows || dy->numel() == 0 || (g.ld_dy = pixel_pitch(*dy)) < 0) Py_RETURN_NONE;
+        const int64_t height = dy->size(1) + v[5] - 1 - 2 * v[7], width = dy->size(2) + v[6] - 1 - 2 * v[7];
+        if (height < 1 || width < 1 || dy->size(0) > INT32_MAX || height > INT32_MAX || width > INT32_MAX || channels * v[5] * v[6] != k ||
+            dy->size(0) * height * width != columns)
+            Py_RETURN_NONE;
+        conv = {(int32_t)dy->size(0), (int32_t)height, (int32_t)width, (int32_t)channels, (int32_t)v[5], (int32_t)v[6], (int32_t)v[7], 1};
+        g.conv = &conv;
+        g.ncols = dy->size(0) * dy->size(1) * dy->size(2); g.dy_layout = 1;
+    }
+    g.d_dy = static_cast<const uint16_t *>(dy->data_ptr());
+    g.dw_dtype = v[9] != 0;
+    g.d_act = act->data_ptr();
+    g.mask = reinterpret_cast<crisp_mask_t>((uintptr_t)v[0]);
+    g.ld_dw = k;
+    g.d_status = static_cast<int32_t *>(status->data_ptr());
+    const at::TensorOptions on = at::TensorOptions().device(at::Device(at::kCUDA, (at::DeviceIndex)gpu));
+    size_t bytes = 0;
+    crisp_status_t s = lib_grad8_sizes(&g, &bytes);
+    at::Tensor dw, workspace;
+    if (s == CRISP_OK) {
+        dw = at::empty_strided({rows, k}, {k, 1}, on.dtype(v[9] ? at::kFloat : at::kBFloat16));
+        if (bytes) workspace = bytes_of(bytes, on);
+        g.d_dw = dw.data_ptr();
+        Py_BEGIN_ALLOW_THREADS
+        s = lib_grad8(&g, bytes ? workspace.data_ptr() : nullptr, reinterpret_cast<void *>((uintptr_t)v[11]));
+        Py_END_ALLOW_THREADS
+    }
+    Ref out(or_none(dw));
+    return out.p ? Py_BuildValue("lO", (long)s, out.p) : nullptr;
+    END_HANDLE_TH_ERRORS
+}
+
+// bind(addresses of crisp_decode, crisp_spmm8_sizes, crisp_spmm8, crisp_decode8, crisp_encode8_sizes, crisp_encode8, crisp_destroy8, crisp_adamw,
+// crisp_adamw_moments, crisp_quantize8_sizes, crisp_group_norm_sizes, crisp_group_norm, crisp_group_norm_backward, crisp_weight_grad8_sizes and crisp_weight_grad8)
 PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
-    if (!arguments("bind", n, 9)) return nullptr;
+    if (!arguments("bind", n, 15)) return nullptr;
     lib_adamw = reinterpret_cast<decltype(&crisp_adamw)>(PyLong_AsVoidPtr(args[7]));
     lib_moments = reinterpret_cast<decltype(&crisp_adamw_moments)>(PyLong_AsVoidPtr(args[8]));
     lib_decode8 = reinterpret_cast<decltype(&crisp_decode8)>(PyLong_AsVoidPtr(args[3]));
@@ -382,12 +566,18 @@ PyObject *bind(PyObject *, PyObject *const *args, Py_ssize_t n) {
     lib_decode = reinterpret_cast<decltype(&crisp_decode)>(PyLong_AsVoidPtr(args[0]));
     lib_spmm8_sizes = reinterpret_cast<decltype(&crisp_spmm8_sizes)>(PyLong_AsVoidPtr(args[1]));
     lib_spmm8 = reinterpret_cast<decltype(&crisp_spmm8)>(PyLong_AsVoidPtr(args[2]));
+    lib_quantize8_sizes = reinterpret_cast<decltype(&crisp_quantize8_sizes)>(PyLong_AsVoidPtr(args[9]));
+    lib_norm_sizes = reinterpret_cast<decltype(&crisp_group_norm_sizes)>(PyLong_AsVoidPtr(args[10]));
+    lib_norm = reinterpret_cast<decltype(&crisp_group_norm)>(PyLong_AsVoidPtr(args[11]));
+    lib_norm_backward = reinterpret_cast<decltype(&crisp_group_norm_backward)>(PyLong_AsVoidPtr(args[12]));
+    lib_grad8_sizes = reinterpret_cast<decltype(&crisp_weight_grad8_sizes)>(PyLong_AsVoidPtr(args[13]));
+    lib_grad8 = reinterpret_cast<decltype(&crisp_weight_grad8)>(PyLong_AsVoidPtr(args[14]));
     if (PyErr_Occurred()) return nullptr;
     Py_RETURN_NONE;
 }
 
 #define CRISP_METHOD(f) {#f, reinterpret_cast<PyCFunction>(reinterpret_cast<void (*)()>(f)), METH_FASTCALL, nullptr}
-PyMethodDef methods[] = {CRISP_METHOD(bind), CRISP_METHOD(table), CRISP_METHOD(encodings), CRISP_METHOD(encoded), CRISP_METHOD(decode), CRISP_METHOD(adamw), CRISP_METHOD(moments), CRISP_METHOD(product8), CRISP_METHOD(encode8), CRISP_METHOD(decode8), {nullptr, nullptr, 0, nullptr}};
+PyMethodDef methods[] = {CRISP_METHOD(bind), CRISP_METHOD(table), CRISP_METHOD(encodings), CRISP_METHOD(encoded), CRISP_METHOD(decode), CRISP_METHOD(adamw), CRISP_METHOD(moments), CRISP_METHOD(norm), CRISP_METHOD(norm_backward), CRISP_METHOD(gradient8), CRISP_METHOD(product8), CRISP_METHOD(encode8), CRISP_METHOD(decode8), {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_network", nullptr, 0, methods, nullptr, nullptr, nullptr, nullptr};
 
 }  // namespace

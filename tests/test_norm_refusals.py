@@ -94,6 +94,7 @@ def test_tensors_that_do_not_fit(lib, monkeypatch):
     monkeypatch.setattr(B, "crisp_group_norm", lambda *a: called.append(a))
     monkeypatch.setattr(B, "crisp_group_norm_backward", lambda *a: called.append(a))
     monkeypatch.setattr(B, "_current_device", lambda: 0)
+    monkeypatch.setattr(B, "_network", False)                                # (what the compiled code does not take, the Python code refuses)
     norm = B.GroupNorm(32, 4)
     elsewhere = torch.device("cuda", 1)
     for bad in (tensor((2, 3, 3, 31)), tensor((32,)), tensor((2, 3, 3, 32), dtype=torch.float64), tensor((2, 3, 3, 32), (288, 1, 96, 3)),
