@@ -42,6 +42,7 @@ struct Grad {
     int kkeep;
     const uint32_t *nm_bits;                                  // a mask, or nullptr
     int wpr;
+    int zero_row, zeros, zero_k;                              // blocks a row tile and in all that are to be looked at for zeros (0: none), columns of dW
     void *dw;
     int64_t ld;
     int f32, accumulate, vec;
@@ -66,20 +67,20 @@ __device__ __forceinline__ uint32_t mask_bits(const Grad &p, int row, int col) {
     return __funnelshift_r(i < p.wpr ? w[i] : 0u, i + 1 < p.wpr ? w[i + 1] : 0u, col & 31);
 }
 
-// 32 sums of a row to dW.
-__device__ __forceinline__ void store32(const Grad &p, int row, int col, int n, float (&v)[32]) {
+// 16 sums of a row to dW.
+__device__ __forceinline__ void store16(const Grad &p, int row, int col, int n, float (&v)[16]) {
     if (p.nm_bits) {
         const uint32_t bits = mask_bits(p, row, col);
 #pragma unroll
-        for (int j = 0; j < 32; ++j)
+        for (int j = 0; j < 16; ++j)
             if (!(bits >> j & 1u)) v[j] = 0.f;                // (a choice: what is not finite is gone, too)
     }
     const int64_t at = (int64_t)row * p.ld + col;
     if (p.f32) {
         float *to = reinterpret_cast<float *>(p.dw) + at;
-        if (p.vec && n == 32 && (col & 3) == 0) {
+        if (p.vec && n == 16 && (col & 3) == 0) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 4) {
+            for (int j = 0; j < 16; j += 4) {
                 float4 q = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
                 if (p.accumulate) {
                     const float4 o = *reinterpret_cast<const float4 *>(to + j);
@@ -89,14 +90,14 @@ __device__ __forceinline__ void store32(const Grad &p, int row, int col, int n, 
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
+            for (int j = 0; j < 16; ++j)
                 if (j < n) to[j] = p.accumulate ? to[j] + v[j] : v[j];
         }
     } else {
         __nv_bfloat16 *to = reinterpret_cast<__nv_bfloat16 *>(p.dw) + at;
-        if (p.vec && n == 32 && (col & 7) == 0) {
+        if (p.vec && n == 16 && (col & 7) == 0) {
 #pragma unroll
-            for (int j = 0; j < 32; j += 8) {
+            for (int j = 0; j < 16; j += 8) {
                 uint4 q = make_uint4(0, 0, 0, 0);
                 if (p.accumulate) q = *reinterpret_cast<const uint4 *>(to + j);
                 const uint32_t o[4] = {q.x, q.y, q.z, q.w};
@@ -111,11 +112,37 @@ __device__ __forceinline__ void store32(const Grad &p, int row, int col, int n, 
             }
         } else {
 #pragma unroll
-            for (int j = 0; j < 32; ++j)
+            for (int j = 0; j < 16; ++j)
                 if (j < n) to[j] = __float2bfloat16_rn(p.accumulate ? __bfloat162float(to[j]) + v[j] : v[j]);
         }
     }
 }
+
+__device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+        "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+
+// Where the CTA is: an item (a tile and a part of the tokens), and a chunk of it.
+struct Walk {
+    int item, rt, first, n, c, c1;
+    __device__ __forceinline__ void enter(const Grad &p, int i) {
+        item = i;
+        c = c1 = 0;
+        if (i >= p.items) return;
+        const int tile = i / p.splits, split = i - tile * p.splits;
+        rt = tile / p.tiles_row;
+        first = (tile - rt * p.tiles_row) * p.per;
+        n = min(p.per, p.boxes - first);
+        c = split * p.chunks_split;
+        c1 = min(c + p.chunks_split, p.chunks);
+    }
+    __device__ __forceinline__ bool over(const Grad &p) const { return item >= p.items; }
+};
 
 template <bool kAMn>
 __global__ void __launch_bounds__(kGradThreads, 1)
@@ -222,29 +249,28 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         // ------------------------------------------------------------------ sums
         const int q = warp & 3, half = (warp - 4) >> 2;       // a warp may read the lanes of its quarter only
         uint32_t acc = 0, acc_ph = 0;
-        for (int item = blockIdx.x; item < p.items; item += gridDim.x) {
-            const int tile = item / p.splits, split = item - tile * p.splits, rt = tile / p.tiles_row, first = (tile - rt * p.tiles_row) * p.per;
-            const int n = min(p.per, p.boxes - first), c0 = split * p.chunks_split, c1 = min(c0 + p.chunks_split, p.chunks);
-            float sum[4][32];
+        Walk w;
+        for (w.enter(p, blockIdx.x); !w.over(p); w.enter(p, w.item + gridDim.x)) {
+            float sum[8][16];
 #pragma unroll
-            for (int i = 0; i < 4; ++i)
+            for (int i = 0; i < 8; ++i)
 #pragma unroll
-                for (int j = 0; j < 32; ++j) sum[i][j] = 0.f;
+                for (int j = 0; j < 16; ++j) sum[i][j] = 0.f;
             int go = 1;
-            for (int c = c0; c < c1; c += kChain) {
+            for (int c = w.c; c < w.c1; c += kChain) {
                 if (lane == 0) go = !*abort_flag && mbar_wait(bar_tfull + 8 * acc, acc_ph, abort_flag, p.wait_limit);
                 go = __shfl_sync(0xFFFFFFFFu, go, 0);
                 if (!go) break;
                 tc_fence_after();
                 const uint32_t from = tmem + acc * 256 + half * 128 + ((uint32_t)(32 * q) << 16);
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (half * 2 + i / 2 < n) {
-                        uint32_t r[32];
-                        tmem_ld32(from + 32 * i, r);
+                for (int i = 0; i < 8; ++i) {
+                    if (half * 2 + i / 4 < w.n) {
+                        uint32_t r[16];
+                        tmem_ld_x16(from + 16 * i, r);
                         tmem_ld_wait();
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) sum[i][j] += __uint_as_float(r[j]);
+                        for (int j = 0; j < 16; ++j) sum[i][j] += __uint_as_float(r[j]);
                     }
                 }
                 tc_fence_before();
@@ -253,22 +279,45 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
             }
             if (!go) break;
-            const int row = rt * 128 + 32 * q + lane;
+            const int row = w.rt * 128 + 32 * q + lane;
             if (p.splits > 1) {
-                float *to = p.partial + ((int64_t)item * 256 + half * 128) * 128 + 32 * q + lane;
+                float *to = p.partial + ((int64_t)w.item * 256 + half * 128) * 128 + 32 * q + lane;
 #pragma unroll
-                for (int i = 0; i < 4; ++i)
-                    if (half * 2 + i / 2 < n)
+                for (int i = 0; i < 8; ++i)
+                    if (half * 2 + i / 4 < w.n)
 #pragma unroll
-                        for (int j = 0; j < 32; ++j) to[(32 * i + j) * 128] = sum[i][j];
+                        for (int j = 0; j < 16; ++j) to[(16 * i + j) * 128] = sum[i][j];
             } else if (row < p.rows) {
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    if (half * 2 + i / 2 >= n) continue;
-                    const BoxAt at = box_at(p, rt, first + half * 2 + i / 2);
-                    const int c = at.c + 32 * (i & 1), here = min(32, p.channels - c);
-                    if (here > 0) store32(p, row, at.tap * p.channels + c, here, sum[i]);
+                for (int i = 0; i < 8; ++i) {
+                    if (half * 2 + i / 4 >= w.n) continue;
+                    const BoxAt at = box_at(p, w.rt, w.first + half * 2 + i / 4);
+                    const int c = at.c + 16 * (i & 3), here = min(16, p.channels - c);
+                    if (here > 0) store16(p, row, at.tap * p.channels + c, here, sum[i]);
                 }
+            }
+        }
+    } else if (warp >= 2) {
+        // -------------------------------------------------------------- zeros of blocks that are not kept
+        const int size = p.f32 ? 4 : 2;
+        for (int u = 2 * blockIdx.x + (warp & 1); u < p.zeros; u += 2 * gridDim.x) {
+            const int rt = u / p.zero_row, kb = u - rt * p.zero_row;
+            bool kept = false;
+            for (int i = lane; i < p.kkeep; i += 32) kept |= p.blk_col[(int64_t)rt * p.kkeep + i] == kb;
+            if (__any_sync(0xFFFFFFFFu, kept)) continue;
+            const int bytes = min(128, p.zero_k - kb * 128) * size, rows = min(128, p.rows - rt * 128);
+            uint8_t *to = reinterpret_cast<uint8_t *>(p.dw) + ((int64_t)rt * 128 * p.ld + kb * 128) * size;
+            if (p.vec && bytes % 16 == 0) {
+                const int across = bytes >> 4;            // (16-byte pieces a row: 32, 16 or those of a last block)
+                for (int i = lane; i < rows * across; i += 32)
+                    *reinterpret_cast<uint4 *>(to + (int64_t)(i / across) * p.ld * size + i % across * 16) = make_uint4(0, 0, 0, 0);
+            } else {
+                const int across = bytes / size;
+                for (int r = 0; r < rows; ++r)
+                    for (int c = lane; c < across; c += 32) {
+                        if (p.f32) reinterpret_cast<float *>(to)[(int64_t)r * p.ld + c] = 0.f;
+                        else reinterpret_cast<uint16_t *>(to)[(int64_t)r * p.ld + c] = 0;
+                    }
             }
         }
     }
@@ -288,78 +337,101 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     }
 }
 
-// dW of a tile's 32 columns out of the parts of its tokens, added in their order: a warp reads four columns of 128 rows, then writes rows.
+// dW of eight columns of a tile out of the parts of its tokens, added in their order: a warp reads a column of 128 rows (eight parts in flight), a thread writes four columns of a row.
 __global__ void __launch_bounds__(256)
 add_parts_kernel(const __grid_constant__ Grad p) {
-    __shared__ float tile[32][129];
+    __shared__ float tile[8][132];
     wait_for_prerequisites();
-    const int chunks = 2 * p.per, t = blockIdx.x / chunks, chunk = blockIdx.x - t * chunks;
+    const int chunks = 8 * p.per, t = blockIdx.x / chunks, chunk = blockIdx.x - t * chunks;
     const int rt = t / p.tiles_row, first = (t - rt * p.tiles_row) * p.per;
-    if (first + chunk / 2 >= p.boxes) return;
+    if (first + chunk / 8 >= p.boxes) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const float *from = p.partial + ((int64_t)t * p.splits * 256 + chunk * 32 + warp * 4) * 128 + lane * 4;
-    float4 sum[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) sum[i] = *reinterpret_cast<const float4 *>(from + i * 128);
-    for (int s = 1; s < p.splits; ++s) {
-        from += 256 * 128;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const float4 v = *reinterpret_cast<const float4 *>(from + i * 128);
-            sum[i].x += v.x; sum[i].y += v.y; sum[i].z += v.z; sum[i].w += v.w;
-        }
+    const float4 *from = reinterpret_cast<const float4 *>(p.partial + ((int64_t)t * p.splits * 256 + chunk * 8 + warp) * 128) + lane;
+    float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
+    for (int s = 0; s < p.splits; ++s) {
+        const float4 v = from[s * (256 * 32)];
+        sum.x += v.x; sum.y += v.y; sum.z += v.z; sum.w += v.w;
     }
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        float *to = &tile[warp * 4 + i][lane * 4];
-        to[0] = sum[i].x; to[1] = sum[i].y; to[2] = sum[i].z; to[3] = sum[i].w;
-    }
+    *reinterpret_cast<float4 *>(&tile[warp][lane * 4]) = sum;
     __syncthreads();
-    const BoxAt at = box_at(p, rt, first + chunk / 2);
-    const int c = at.c + 32 * (chunk & 1) + lane, col = at.tap * p.channels + c;
-    for (int r = warp; r < 128; r += 8) {
-        const int row = rt * 128 + r;
-        if (row >= p.rows) break;
-        if (c >= p.channels) continue;
-        float v = tile[lane][r];
-        if (p.nm_bits && !(p.nm_bits[(int64_t)row * p.wpr + (col >> 5)] >> (col & 31) & 1u)) v = 0.f;
-        const int64_t to = (int64_t)row * p.ld + col;
-        if (p.f32) {
-            float *w = reinterpret_cast<float *>(p.dw) + to;
-            *w = p.accumulate ? *w + v : v;
-        } else {
-            __nv_bfloat16 *w = reinterpret_cast<__nv_bfloat16 *>(p.dw) + to;
-            *w = __float2bfloat16_rn(p.accumulate ? __bfloat162float(*w) + v : v);
+    const BoxAt at = box_at(p, rt, first + chunk / 8);
+    const int r = threadIdx.x >> 1, row = rt * 128 + r, c = at.c + 8 * (chunk & 7) + 4 * (threadIdx.x & 1), col = at.tap * p.channels + c, n = p.channels - c;
+    if (row >= p.rows || n <= 0) return;
+    float v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = tile[4 * (threadIdx.x & 1) + j][r];
+    if (p.nm_bits) {
+        const uint32_t bits = mask_bits(p, row, col);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (!(bits >> j & 1u)) v[j] = 0.f;
+    }
+    const int64_t to = (int64_t)row * p.ld + col;
+    if (p.f32) {
+        float *w = reinterpret_cast<float *>(p.dw) + to;
+        if (p.vec && n >= 4 && (col & 3) == 0) {
+            float4 o = make_float4(v[0], v[1], v[2], v[3]);
+            if (p.accumulate) { const float4 old = *reinterpret_cast<const float4 *>(w); o.x += old.x; o.y += old.y; o.z += old.z; o.w += old.w; }
+            *reinterpret_cast<float4 *>(w) = o;
+            return;
         }
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) w[j] = p.accumulate ? w[j] + v[j] : v[j];
+    } else {
+        __nv_bfloat16 *w = reinterpret_cast<__nv_bfloat16 *>(p.dw) + to;
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            if (j < n) w[j] = __float2bfloat16_rn(p.accumulate ? __bfloat162float(w[j]) + v[j] : v[j]);
     }
 }
 
-// Zeros in the blocks of dW that a row tile does not keep (128 x 128).
+// Zeros in all of dW: of a layer without kept blocks.
 __global__ void __launch_bounds__(256)
-zero_blocks_kernel(Geometry g, const int32_t *blk_col, void *dw, int64_t ld, int f32) {
+zero_kernel(int64_t rows, int k, void *dw, int64_t ld, int f32) {
     wait_for_prerequisites();
-    const int rt = blockIdx.x / g.nblk, kb = blockIdx.x - rt * g.nblk;
-    int hit = 0;
-    for (int i = threadIdx.x; i < g.kkeep; i += 256) hit |= blk_col[(int64_t)rt * g.kkeep + i] == kb;
-    if (__syncthreads_or(hit)) return;
-    const int c = kb * 128 + (threadIdx.x & 127);
-    if (c >= g.k) return;
-    for (int r = rt * 128 + (threadIdx.x >> 7); r < min(g.rows, rt * 128 + 128); r += 2) {
-        if (f32) reinterpret_cast<float *>(dw)[(int64_t)r * ld + c] = 0.f;
-        else reinterpret_cast<uint16_t *>(dw)[(int64_t)r * ld + c] = 0;
-    }
+    for (int64_t r = blockIdx.x; r < rows; r += gridDim.x)
+        for (int c = threadIdx.x; c < k; c += 256) {
+            if (f32) reinterpret_cast<float *>(dw)[r * ld + c] = 0.f;
+            else reinterpret_cast<uint16_t *>(dw)[r * ld + c] = 0;
+        }
 }
 
-// dY to [columns, rows] with a pitch that TMA takes, out of [rows, columns] or [columns, rows] of any pitch: tiles of 64 x 64.
+// dY's rows with a pitch that TMA takes: a warp copies 16-byte pieces of a row, whose elements it reads as wide as they lie (kWide: 4, 2 or 1 of them).
+template <int kWide>
 __global__ void __launch_bounds__(256)
-pack_dy_kernel(const uint16_t *dy, int64_t ld, int layout, int rows, int64_t ncols, uint16_t *to, int64_t pitch, int row_tiles) {
+repitch_dy_kernel(const uint16_t *dy, int64_t ld, int64_t rows, int64_t cols, uint16_t *to, int64_t pitch, int64_t pieces) {
+    wait_for_prerequisites();
+    const int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x, row = u / pieces, c = (u - row * pieces) * 8;
+    if (row >= rows) return;
+    const uint16_t *from = dy + row * ld + c;
+    uint32_t w[4] = {0, 0, 0, 0};
+    if (c + 8 <= cols) {
+        if constexpr (kWide == 4) {
+            const uint2 a = reinterpret_cast<const uint2 *>(from)[0], b = reinterpret_cast<const uint2 *>(from)[1];
+            w[0] = a.x; w[1] = a.y; w[2] = b.x; w[3] = b.y;
+        } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = kWide == 2 ? reinterpret_cast<const uint32_t *>(from)[j] : from[2 * j] | (uint32_t)from[2 * j + 1] << 16;
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (c + j < cols) w[j / 2] |= (uint32_t)from[j] << (16 * (j & 1));
+    }
+    *reinterpret_cast<uint4 *>(to + row * pitch + c) = make_uint4(w[0], w[1], w[2], w[3]);
+}
+
+// A convolution's dY [rows, columns] to [columns, rows] with a pitch that TMA takes: tiles of 64 x 64.
+__global__ void __launch_bounds__(256)
+transpose_dy_kernel(const uint16_t *dy, int64_t ld, int rows, int64_t ncols, uint16_t *to, int64_t pitch, int row_tiles) {
     __shared__ uint16_t tile[64][66];
     wait_for_prerequisites();
     const int64_t u = blockIdx.x / row_tiles, t0 = u * 64;
     const int r0 = (int)(blockIdx.x - u * row_tiles) * 64, x = threadIdx.x & 63, y = threadIdx.x >> 6;
     for (int i = y; i < 64; i += 4) {
-        if (layout == 0) { if (r0 + i < rows && t0 + x < ncols) tile[x][i] = dy[(int64_t)(r0 + i) * ld + t0 + x]; }
-        else if (t0 + i < ncols && r0 + x < rows) tile[i][x] = dy[(t0 + i) * ld + r0 + x];
+        if (r0 + i < rows && t0 + x < ncols) tile[x][i] = dy[(int64_t)(r0 + i) * ld + t0 + x];
     }
     __syncthreads();
     for (int i = y; i < 64; i += 4)
@@ -373,8 +445,8 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct GradPlan {
     Grad p;
-    bool pack, k_major, blocks;                               // blocks: tiles follow the mask's list
-    int64_t pixels, cpitch, rpitch;                           // columns of x, pitches of x and of a packed dY
+    bool k_major, copy, blocks;                               // dY as [rows, columns]; through a copy; tiles follow the mask's list
+    int64_t pixels, cpitch, pitch;                            // columns of x, pitches of x in bf16 and of a copied dY
     int ho, wo, batch;
     size_t x_off, dy_off, partial_off, total;
     int nrt;
@@ -444,13 +516,13 @@ crisp_status_t plan_grad(const crisp_weight_grad8_t *g, GradPlan *G) {
         G->cpitch = up(p.channels, 64) * 64;
         G->x_off = 0;
         at = align_up((size_t)G->pixels * G->cpitch * 2);
-        const bool fits = aligned_to(g->d_dy, 16) && g->ld_dy % 8 == 0;
-        G->k_major = g->dy_layout == 0 && p.linear && fits;
-        G->pack = !G->k_major && !(g->dy_layout == 1 && fits);
-        if (G->pack) {
-            G->rpitch = up(p.rows, 8) * 8;
+        // a matrix is taken as it lies, [rows, columns] too; a convolution's pixels have to be boxes
+        G->k_major = g->dy_layout == 0 && p.linear;
+        G->copy = !(aligned_to(g->d_dy, 16) && g->ld_dy % 8 == 0) || (g->dy_layout == 0 && !p.linear);
+        if (G->copy) {
+            G->pitch = up(G->k_major ? g->ncols : p.rows, 8) * 8;
             G->dy_off = at;
-            at += align_up((size_t)g->ncols * G->rpitch * 2);
+            at += align_up((size_t)(G->k_major ? p.rows : g->ncols) * G->pitch * 2);
         }
         if (p.splits > 1) {
             G->partial_off = at;
@@ -480,12 +552,9 @@ cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cu
     p.status = g.d_status;
     p.wait_limit = kWaitLimitCycles;
     p.skip_fill = -1;
-    if (G.blocks && !g.accumulate) {
-        const Geometry &m = g.mask->g;
-        e = launch_chained(zero_blocks_kernel, (unsigned)(m.nrt * m.nblk), 256, 0, st, m, g.mask->d_blk_col, g.d_dw, g.ld_dw, g.dw_dtype);
-        if (e != cudaSuccess) return e;
-    }
-    if (p.boxes == 0) return cudaSuccess;
+    if (p.boxes == 0)
+        return g.accumulate ? cudaSuccess : launch_chained(zero_kernel, (unsigned)std::min(g.rows, 4096), 256, 0, st, (int64_t)g.rows, (int)g.k, g.d_dw, g.ld_dw, (int)g.dw_dtype);
+    if (G.blocks && !g.accumulate) { p.zero_row = g.mask->g.nblk; p.zeros = g.mask->g.nrt * g.mask->g.nblk; p.zero_k = g.k; }
     int device = 0;
     e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
@@ -497,13 +566,20 @@ cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cu
     if (e != cudaSuccess) return e;
     const uint16_t *dy = g.d_dy;
     int64_t ld = g.ld_dy;
-    if (G.pack) {
+    if (G.copy) {
         uint16_t *to = reinterpret_cast<uint16_t *>(ws + G.dy_off);
-        const int64_t row_tiles = up(p.rows, 64), ctas = row_tiles * up(g.ncols, 64);
-        if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
-        e = launch_chained(pack_dy_kernel, (unsigned)ctas, 256, 0, st, g.d_dy, g.ld_dy, g.dy_layout, p.rows, g.ncols, to, G.rpitch, (int)row_tiles);
+        if (g.dy_layout == 0 && !p.linear) {
+            const int64_t row_tiles = up(p.rows, 64), ctas = row_tiles * up(g.ncols, 64);
+            if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
+            e = launch_chained(transpose_dy_kernel, (unsigned)ctas, 256, 0, st, g.d_dy, g.ld_dy, p.rows, g.ncols, to, G.pitch, (int)row_tiles);
+        } else {
+            const int64_t rows = G.k_major ? p.rows : g.ncols, cols = G.k_major ? g.ncols : p.rows, pieces = G.pitch / 8, ctas = up(rows * pieces, 256);
+            if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
+            const auto kernel = aligned_to(g.d_dy, 8) && g.ld_dy % 4 == 0 ? repitch_dy_kernel<4> : aligned_to(g.d_dy, 4) && g.ld_dy % 2 == 0 ? repitch_dy_kernel<2> : repitch_dy_kernel<1>;
+            e = launch_chained(kernel, (unsigned)ctas, 256, 0, st, g.d_dy, g.ld_dy, rows, cols, to, G.pitch, pieces);
+        }
         if (e != cudaSuccess) return e;
-        dy = to; ld = G.rpitch;
+        dy = to; ld = G.pitch;
     }
     CUtensorMap a, b;
     const uint64_t W = g.conv ? g.conv->width : g.ncols, H = g.conv ? g.conv->height : 1, N = G.batch;
@@ -519,7 +595,7 @@ cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cu
     const int sms = sm_count_of(device);
     e = G.k_major ? launch_grad<false>(a, b, p, sms, device, st) : launch_grad<true>(a, b, p, sms, device, st);
     if (e == cudaSuccess && p.splits > 1)
-        e = launch_chained(add_parts_kernel, (unsigned)(G.nrt * p.tiles_row * 2 * p.per), 256, 0, st, p);
+        e = launch_chained(add_parts_kernel, (unsigned)(G.nrt * p.tiles_row * 8 * p.per), 256, 0, st, p);
     return e;
 }
 

@@ -53,7 +53,7 @@ def test_workspaces(lib):
     n = C.c_size_t()
     assert lib.crisp_weight_grad8_sizes(None, C.byref(n)) == B.INVALID_ARG and lib.crisp_weight_grad8_sizes(C.byref(grad()), None) == B.INVALID_ARG
     assert lib.crisp_weight_grad8(None, 4096, None) == B.INVALID_ARG
-    assert lib.crisp_weight_grad8(C.byref(grad()), None, None) == B.INVALID_ARG and lib.crisp_weight_grad8(C.byref(grad()), 4096 + 64, None) == B.INVALID_ARG
+    assert lib.crisp_weight_grad8(C.byref(grad(ld_dy=33)), None, None) == B.INVALID_ARG and lib.crisp_weight_grad8(C.byref(grad()), 4096 + 64, None) == B.INVALID_ARG
     # one that TMA cannot address is brought into a form that it can
     assert B.crisp_weight_grad8_sizes(grad(ld_dy=33)) > B.crisp_weight_grad8_sizes(grad())
 
