@@ -144,6 +144,30 @@ struct Walk {
     __device__ __forceinline__ bool over(const Grad &p) const { return item >= p.items; }
 };
 
+// A chain's accumulator to the sums of a warp's 32 rows and 128 columns (two boxes).
+__device__ __forceinline__ void add_chain(uint32_t from, int n, int half, float (&sum)[8][16]) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (half * 2 + i / 4 < n) {
+            uint32_t r[16];
+            tmem_ld_x16(from + 16 * i, r);
+            tmem_ld_wait();
+#pragma unroll
+            for (int j = 0; j < 16; ++j) sum[i][j] += __uint_as_float(r[j]);
+        }
+    }
+}
+__device__ __forceinline__ void store_sums(const Grad &p, const Walk &w, int rt, int half, int row, float (&sum)[8][16]) {
+    if (row >= p.rows) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        if (half * 2 + i / 4 >= w.n) continue;
+        const BoxAt at = box_at(p, rt, w.first + half * 2 + i / 4);
+        const int c = at.c + 16 * (i & 3), here = min(16, p.channels - c);
+        if (here > 0) store16(p, row, at.tap * p.channels + c, here, sum[i]);
+    }
+}
+
 template <bool kAMn>
 __global__ void __launch_bounds__(kGradThreads, 1)
 grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Grad p) {
@@ -262,24 +286,13 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 go = __shfl_sync(0xFFFFFFFFu, go, 0);
                 if (!go) break;
                 tc_fence_after();
-                const uint32_t from = tmem + acc * 256 + half * 128 + ((uint32_t)(32 * q) << 16);
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (half * 2 + i / 4 < w.n) {
-                        uint32_t r[16];
-                        tmem_ld_x16(from + 16 * i, r);
-                        tmem_ld_wait();
-#pragma unroll
-                        for (int j = 0; j < 16; ++j) sum[i][j] += __uint_as_float(r[j]);
-                    }
-                }
+                add_chain(tmem + acc * 256 + half * 128 + ((uint32_t)(32 * q) << 16), w.n, half, sum);
                 tc_fence_before();
                 __syncwarp();
                 if (lane == 0) mbar_arrive(bar_tempty + 8 * acc);
                 if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
             }
             if (!go) break;
-            const int row = w.rt * 128 + 32 * q + lane;
             if (p.splits > 1) {
                 float *to = p.partial + ((int64_t)w.item * 256 + half * 128) * 128 + 32 * q + lane;
 #pragma unroll
@@ -287,14 +300,8 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                     if (half * 2 + i / 4 < w.n)
 #pragma unroll
                         for (int j = 0; j < 16; ++j) to[(16 * i + j) * 128] = sum[i][j];
-            } else if (row < p.rows) {
-#pragma unroll
-                for (int i = 0; i < 8; ++i) {
-                    if (half * 2 + i / 4 >= w.n) continue;
-                    const BoxAt at = box_at(p, w.rt, w.first + half * 2 + i / 4);
-                    const int c = at.c + 16 * (i & 3), here = min(16, p.channels - c);
-                    if (here > 0) store16(p, row, at.tap * p.channels + c, here, sum[i]);
-                }
+            } else {
+                store_sums(p, w, w.rt, half, w.rt * 128 + 32 * q + lane, sum);
             }
         }
     } else if (warp >= 2) {
@@ -334,6 +341,211 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     if (warp == 2) {
         tc_fence_after();
         tmem_dealloc(tmem, 512);
+    }
+}
+
+// ------------------------------------------------------------------------------------------------ pairs of SMs
+//
+// Two CTAs (a cluster) multiply 256 rows by 256 columns with cta_group::2: each fetches its 128 rows of dY and two of the four boxes of x, and the tensor cores of both read both
+// halves.  A CTA by itself is bound by what comes in from L2 (48 KB a chunk, some 11 TB/s in all); of a pair each fetches 32.  Not under a mask of blocks, where every row tile has
+// boxes of its own.
+//
+// The CTA of rank 0 issues for both.  The copies of both complete on its barriers, which count the bytes of both (what has landed in the peer's shared memory is acquired at the scope of the
+// cluster); commits go to both (multicast); accumulators are handed back by the adding warps of both.  These two are seen at the scope of the cluster, relaxed: what tcgen05
+// instructions read and write is ordered by their commits and fences, and nothing else is handed over.
+constexpr uint32_t kPairStage = kABytes + kBoxes / 2 * kBoxBytes;
+constexpr int kPairStages = 6;
+constexpr size_t kPairSmem = kPairStages * kPairStage + 256 + 1024;
+
+__device__ __forceinline__ void mma_dense_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\tsetp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
+        ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
+}
+__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {          // to the barrier at this place in both CTAs
+    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
+                 ::"r"(bar), "h"((uint16_t)3) : "memory");
+}
+__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+// After a wait at the CTA's scope: the phase that it has seen complete, seen at the scope of the cluster.
+template <bool kAcquire>
+__device__ __forceinline__ void mbar_seen_cluster(uint32_t bar, uint32_t parity) {
+    if constexpr (kAcquire)
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(bar), "r"(parity) : "memory");
+    else
+        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.relaxed.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(bar), "r"(parity) : "memory");
+}
+// Copies into this CTA's shared memory that complete on a barrier of either CTA of the pair.
+__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t cluster_bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
+        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, uint32_t cluster_bar) {
+    asm volatile(
+        "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
+        ::"r"(dst), "l"(map), "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(cluster_bar) : "memory");
+}
+
+// (p.tiles_row and p.per as for one CTA; Walk's row tiles are pairs of them)
+template <bool kAMn>
+__global__ void __launch_bounds__(kGradThreads, 1)
+grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Grad p) {
+    extern __shared__ uint8_t smem_raw[];
+    const uint32_t base = smem_u32(smem_raw), ring = (base + 1023u) & ~1023u, ctrl = ring + kPairStages * kPairStage;
+    uint8_t *ctrl_gen = smem_raw + (ctrl - base);
+    // barriers: (rank 0) full[s] of both, empty[s]; accumulators full, and (rank 0) empty
+    const uint32_t bar_full = ctrl, bar_empty = ctrl + 64, bar_tfull = ctrl + 128, bar_tempty = ctrl + 144, bar_done = ctrl + 160;
+    volatile uint32_t *tmem_slot = reinterpret_cast<volatile uint32_t *>(ctrl_gen + 176);
+    volatile int *abort_flag = reinterpret_cast<volatile int *>(ctrl_gen + 180);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t rank = cluster_rank();
+    if (warp == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(const_cast<uint32_t *>(tmem_slot))), "r"(512) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    }
+    if (threadIdx.x == 0) {
+        prefetch_tensormap(&map_a);
+        prefetch_tensormap(&map_b);
+        for (int s = 0; s < kPairStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, 2 * kDrain); }
+        mbar_init(bar_done, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    wait_for_prerequisites();
+    tc_fence_before();
+    __syncthreads();
+    cluster_arrive();                                        // (the peer's barriers are there, and its tensor memory)
+    cluster_wait();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+    const int item0 = (int)(blockIdx.x >> 1), step = (int)(gridDim.x >> 1);
+
+    if (warp == 0 && lane == 0) {
+        // ------------------------------------------------------------------ this CTA's rows and half of the boxes, and (rank 0) both CTAs' byte count
+        const uint32_t full0 = peer_address(bar_full, 0);
+        uint32_t ph = 0;
+        int s = 0, fill = 0;
+        bool ok = true;
+        Walk w;
+        for (w.enter(p, item0); !w.over(p) && ok; w.enter(p, w.item + step)) {
+            const int mine = (w.n + 1) / 2, row = (2 * w.rt + (int)rank) * 128;
+            BoxAt box[kBoxes / 2];
+            int dx[kBoxes / 2], dy[kBoxes / 2];
+#pragma unroll
+            for (int i = 0; i < kBoxes / 2; ++i) {
+                const int b = (int)rank * mine + i;
+                box[i] = {0, p.cboxes * 64};                  // (an odd number of boxes: the last one lies behind the last column and is zeros)
+                if (i < mine && b < w.n) box[i] = box_at(p, w.rt, w.first + b);
+                dx[i] = dy[i] = 0;
+                if (!p.linear) { dy[i] = box[i].tap / p.kernel_w; dx[i] = box[i].tap - dy[i] * p.kernel_w - p.pad; dy[i] -= p.pad; }
+            }
+            for (int c = w.c; c < w.c1; ++c) {
+                if (!mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
+                mbar_seen_cluster<false>(bar_empty + 8 * s, ph ^ 1u);
+                const uint32_t dst = ring + s * kPairStage, full = full0 + 8 * s;
+                const int by = c / p.nx, x0 = (c - by * p.nx) * p.tw, bb = by / p.ny, y0 = (by - bb * p.ny) * p.th, b0 = bb * p.tb;
+                // (the peer's bytes may come first: a phase ends with this arrival at the earliest, and the peer fills a stage anew when the one before has been multiplied)
+                if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * (kABytes + mine * kBoxBytes));
+                if (fill++ != p.skip_fill) {
+                    if constexpr (kAMn) {
+                        tma_load_4d_pair(dst, &map_a, row, x0, y0, b0, full);
+                        tma_load_4d_pair(dst + 8192, &map_a, row + 64, x0, y0, b0, full);
+                    } else {
+                        tma_load_2d_pair(dst, &map_a, x0, row, full);
+                    }
+#pragma unroll
+                    for (int i = 0; i < kBoxes / 2; ++i)
+                        if (i < mine) tma_load_4d_pair(dst + kABytes + i * kBoxBytes, &map_b, box[i].c, x0 + dx[i], y0 + dy[i], b0, full);
+                }
+                if (++s == kPairStages) { s = 0; ph ^= 1u; }
+            }
+        }
+    } else if (warp == 1 && lane == 0 && rank == 0) {
+        // ------------------------------------------------------------------ products, of both
+        uint32_t ph = 0, acc = 0, acc_ph = 0;
+        int s = 0;
+        bool ok = true;
+        const uint64_t a0 = kAMn ? make_smem_desc(ring, 8192, 1024, kLayoutSw128) : make_smem_desc(ring, 16, 1024, kLayoutSw128);
+        const uint64_t b0 = make_smem_desc(ring + kABytes, kBoxBytes, 1024, kLayoutSw128);
+        constexpr uint32_t a_step = kAMn ? 128u : 2u;
+        Walk w;
+        for (w.enter(p, item0); !w.over(p) && ok; w.enter(p, w.item + step)) {
+            // (as make_idesc, M = 256)
+            const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(128 * ((w.n + 1) / 2) >> 3) << 17) | (16u << 24) | (kAMn ? 1u << 15 : 0u);
+            for (int c = w.c; c < w.c1 && ok; c += kChain) {
+                ok = mbar_wait(bar_tempty + 8 * acc, acc_ph ^ 1u, abort_flag, p.wait_limit);
+                if (!ok) break;
+                mbar_seen_cluster<false>(bar_tempty + 8 * acc, acc_ph ^ 1u);
+                tc_fence_after();
+                const uint32_t d = tmem + acc * 256;
+                const int end = min(c + kChain, w.c1);
+                for (int i = c; i < end; ++i) {
+                    ok = mbar_wait(bar_full + 8 * s, ph, abort_flag, p.wait_limit);
+                    if (!ok) break;
+                    mbar_seen_cluster<true>(bar_full + 8 * s, ph);
+                    tc_fence_after();
+                    const uint32_t off = (uint32_t)s * (kPairStage >> 4);
+#pragma unroll
+                    for (int j = 0; j < kStep / 16; ++j) mma_dense_pair(d, a0 + off + j * a_step, b0 + off + j * 128u, idesc, (uint32_t)((i - c) | j));
+                    mma_commit_pair(bar_empty + 8 * s);
+                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                }
+                if (!ok) break;
+                mma_commit_pair(bar_tfull + 8 * acc);
+                if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+            }
+        }
+        mma_commit_pair(bar_done);
+        mbar_wait(bar_done, 0, abort_flag, kWaitLimitCycles);
+    } else if (warp >= 4) {
+        // ------------------------------------------------------------------ sums
+        const int q = warp & 3, half = (warp - 4) >> 2;
+        const uint32_t back = peer_address(bar_tempty, 0);
+        uint32_t acc = 0, acc_ph = 0;
+        Walk w;
+        for (w.enter(p, item0); !w.over(p); w.enter(p, w.item + step)) {
+            float sum[8][16];
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 16; ++j) sum[i][j] = 0.f;
+            int go = 1;
+            for (int c = w.c; c < w.c1; c += kChain) {
+                if (lane == 0) go = !*abort_flag && mbar_wait(bar_tfull + 8 * acc, acc_ph, abort_flag, p.wait_limit);
+                go = __shfl_sync(0xFFFFFFFFu, go, 0);
+                if (!go) break;
+                mbar_seen_cluster<false>(bar_tfull + 8 * acc, acc_ph);
+                tc_fence_after();
+                add_chain(tmem + acc * 256 + half * 128 + ((uint32_t)(32 * q) << 16), w.n, half, sum);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive_at(back + 8 * acc);
+                if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
+            }
+            if (!go) break;
+            store_sums(p, w, w.rt, half, (2 * w.rt + (int)rank) * 128 + 32 * q + lane, sum);
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if (*abort_flag) {
+        if (threadIdx.x == 0 && p.status) atomicCAS(p.status, 0, (int)CRISP_TIMEOUT);
+        // copies that may still be in flight land before shared memory is released
+        const unsigned long long t0 = clock64();
+        while ((unsigned long long)(clock64() - t0) < 2000000ull) __nanosleep(1000);
+        __syncthreads();
+    }
+    cluster_arrive();                                        // neither CTA's memory is read, nor its barriers arrived at, by the other any more
+    cluster_wait();
+    if (warp == 2) {
+        tc_fence_after();
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(512) : "memory");
     }
 }
 
@@ -445,7 +657,7 @@ int64_t up(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 struct GradPlan {
     Grad p;
-    bool k_major, copy, blocks;                               // dY as [rows, columns]; through a copy; tiles follow the mask's list
+    bool pair, k_major, copy, blocks;                               // dY as [rows, columns]; through a copy; tiles follow the mask's list
     int64_t pixels, cpitch, pitch;                            // columns of x, pitches of x in bf16 and of a copied dY
     int ho, wo, batch;
     size_t x_off, dy_off, partial_off, total;
@@ -513,6 +725,9 @@ crisp_status_t plan_grad(const crisp_weight_grad8_t *g, GradPlan *G) {
         p.chunks_split = (int)up(p.chunks, splits);
         p.splits = (int)up(p.chunks, p.chunks_split);
         p.items = (int)(tiles * p.splits);
+        // pairs where every SM has work all the same
+        G->pair = !p.blk_col && p.splits == 1 && G->nrt >= 2 && up(G->nrt, 2) * p.tiles_row >= 74;
+        if (G->pair) p.items = (int)(up(G->nrt, 2) * p.tiles_row);
         G->cpitch = up(p.channels, 64) * 64;
         G->x_off = 0;
         at = align_up((size_t)G->pixels * G->cpitch * 2);
@@ -533,15 +748,15 @@ crisp_status_t plan_grad(const crisp_weight_grad8_t *g, GradPlan *G) {
     return CRISP_OK;
 }
 
-template <bool kAMn>
-cudaError_t launch_grad(const CUtensorMap &a, const CUtensorMap &b, const Grad &p, int sms, int device, cudaStream_t st) {
-    static std::atomic<uint64_t> ready{0};
+template <auto kernel>
+cudaError_t launch_grad(const CUtensorMap &a, const CUtensorMap &b, const Grad &p, size_t smem, unsigned cluster, int sms, int device, cudaStream_t st) {
+    static std::atomic<uint64_t> ready{0};                                    // (one a kernel: by device)
     if (device >= 64 || !(ready.load(std::memory_order_relaxed) >> device & 1)) {
-        const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(grad8_kernel<kAMn>), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kGradSmem);
+        const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
         if (e != cudaSuccess) return e;
         if (device < 64) ready.fetch_or(1ull << device, std::memory_order_relaxed);
     }
-    return launch_chained(grad8_kernel<kAMn>, (unsigned)std::min(p.items, sms), kGradThreads, kGradSmem, st, a, b, p);
+    return launch_clusters(kernel, cluster * (unsigned)std::min(p.items, sms / (int)cluster), kGradThreads, smem, st, cluster, a, b, p);
 }
 
 cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cudaStream_t st) {
@@ -593,7 +808,10 @@ cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cu
         if (!make_map_4d(&a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dy, yd, ys, box)) return cudaErrorInvalidValue;
     }
     const int sms = sm_count_of(device);
-    e = G.k_major ? launch_grad<false>(a, b, p, sms, device, st) : launch_grad<true>(a, b, p, sms, device, st);
+    if (G.pair)
+        e = G.k_major ? launch_grad<grad8_pair_kernel<false>>(a, b, p, kPairSmem, 2, sms, device, st) : launch_grad<grad8_pair_kernel<true>>(a, b, p, kPairSmem, 2, sms, device, st);
+    else
+        e = G.k_major ? launch_grad<grad8_kernel<false>>(a, b, p, kGradSmem, 1, sms, device, st) : launch_grad<grad8_kernel<true>>(a, b, p, kGradSmem, 1, sms, device, st);
     if (e == cudaSuccess && p.splits > 1)
         e = launch_chained(add_parts_kernel, (unsigned)(G.nrt * p.tiles_row * 8 * p.per), 256, 0, st, p);
     return e;

@@ -162,6 +162,45 @@ def test_convolutions(batch, height, width, channels, rows, kh, kw, pad, f32):
         assert L.gradient_status() == 0
 
 
+@pytest.mark.parametrize("rows,k,tokens", [(2650, 2000, 200), (2560, 2048, 1100), (300, 9500, 70), (2433, 2113, 64)])
+@pytest.mark.parametrize("by_token", [False, True])
+def test_tiles_for_every_sm(rows, k, tokens, by_token):
+    """So many tiles that two SMs share one: odd numbers of row tiles and of boxes, rows and columns that end within one."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    xb, dyb = inputs(np.random.default_rng(rows), tokens, rows, k)
+    x, dy = held.activations(values_of(xb).T).T, values_of(dyb)
+    act = B.quantize8(bf16_dev(xb, torch), tokens=True)
+    want, size = dy.T @ x, np.abs(dy).T @ np.abs(x)
+    for block, n, keep, masked in ((128, 4, 1.0, False), (64, 2, 0.5, True), (128, 2, 1.0, True)):
+        L, mask = layer(B, torch, rows, k, n, 4, block, keep, 3, mask=masked)
+        for pitch, odd, f32 in ((0, 0, 1), (3, 1, 0)):
+            d_dy, _ = padded(torch, dyb if by_token else np.ascontiguousarray(dyb.T), pitch, odd)
+            dw, whole = padded(torch, np.zeros((rows, k), np.uint16), pitch, odd, torch.float32 if f32 else torch.bfloat16)
+            L.weight_gradient8(d_dy, act, dw=dw, dw_dtype=f32, tokens=by_token, masked=masked)
+            check(numbers(dw), want * mask, size * mask, tokens, f32)
+            assert bool((whole[odd:].view(rows, k + pitch)[:, k:] == 7.0).all() and (whole[:odd] == 7.0).all())
+            old = numbers(dw)
+            L.weight_gradient8(d_dy, act, dw=dw, dw_dtype=f32, tokens=by_token, masked=masked, accumulate=True)
+            check(numbers(dw), want * mask, size * mask, tokens, f32, old)
+    assert L.gradient_status() == 0
+
+
+def test_convolution_tiles_for_every_sm():
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    batch, height, width, channels, rows = 2, 9, 7, 200, 2400
+    rng = np.random.default_rng(0)
+    xb, _ = inputs(rng, batch * height * width, 1, channels)
+    x = held.activations(values_of(xb).T).T.reshape(batch, height, width, channels)
+    low, ho, wo = lowered(x, 3, 3, 1)
+    _, dyb = inputs(rng, batch * ho * wo, rows, 1)
+    dy = values_of(dyb)
+    L, _ = layer(B, torch, rows, 9 * channels, mask=False)
+    dw = L.weight_gradient8_conv(bf16_dev(dyb, torch).view(batch, ho, wo, rows), B.quantize8(bf16_dev(xb, torch), tokens=True), 3, 3, 1)
+    check(numbers(dw), dy.T @ low, np.abs(dy).T @ np.abs(low), batch * ho * wo, 1)
+
+
 def test_what_is_not_finite():
     import torch
     from paper_2311_14272_b200 import binding as B
