@@ -37,6 +37,7 @@ struct Grad {
     int cboxes;                                               // boxes of a tap's channels
     int per, tiles_row, boxes, splits, items;                 // boxes a tile, tiles a row tile, boxes a row tile
     int tw, th, tb, nx, ny;                                   // pixels of a stage; boxes of them along a line, lines along an image
+    int wo, ho;                                               // of dY (a linear layer: one line of tokens)
     int chunks, chunks_split;
     const int32_t *blk_col;                                   // masks of 128 x 128: kept blocks of a row tile (else nullptr)
     int kkeep;
@@ -127,6 +128,25 @@ __device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t (&r)[16]) {
         : "r"(taddr) : "memory");
 }
 
+// The first pixel of a chunk.  (The threads that issue copies are bound by their own instructions: they go from chunk to chunk without a division.  4096 x 4096, 8192 tokens,
+// in pairs: 280 us with two of them a chunk.)
+struct Pixels {
+    int x, y, z;
+    __device__ __forceinline__ Pixels(const Grad &p, int c) {
+        const int by = c / p.nx;
+        z = by / p.ny;
+        x = (c - by * p.nx) * p.tw; y = (by - z * p.ny) * p.th;
+        z *= p.tb;
+    }
+    __device__ __forceinline__ void next(const Grad &p) {
+        x += p.tw;
+        if (x < p.wo) return;
+        x = 0; y += p.th;
+        if (y < p.ho) return;
+        y = 0; z += p.tb;
+    }
+};
+
 // Where the CTA is: an item (a tile and a part of the tokens), and a chunk of it.
 struct Walk {
     int item, rt, first, n, c, c1;
@@ -185,7 +205,7 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     if (threadIdx.x == 0) {
         prefetch_tensormap(&map_a);
         prefetch_tensormap(&map_b);
-        for (int s = 0; s < kStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        for (int s = 0; s < kStages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, kDrain); }
         mbar_init(bar_done, 1);
         *abort_flag = 0;
@@ -197,78 +217,87 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
-    if (warp == 0 && lane == 0) {
-        // ------------------------------------------------------------------ loads
-        uint32_t ph = 0;
+    // The threads that issue copies and products are bound by their own instructions.  Their warps run the loops as a whole, so that addresses stay in uniform registers, where
+    // the instructions take them from, and an elected thread issues; dY and x have a warp each.
+    if (warp == 0 || warp == 3) {
+        // ------------------------------------------------------------------ dY, x
+        const bool leader = elect_one(), rows = warp == 0;
+        uint32_t dst = ring + (rows ? 0 : kABytes), full = bar_full, empty = bar_empty, ph = 0;
         int s = 0, fill = 0;
         bool ok = true;
-        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-            const int tile = item / p.splits, split = item - tile * p.splits, rt = tile / p.tiles_row, first = (tile - rt * p.tiles_row) * p.per;
-            const int n = min(p.per, p.boxes - first), c0 = split * p.chunks_split, c1 = min(c0 + p.chunks_split, p.chunks);
+        Walk w;
+        for (w.enter(p, blockIdx.x); !w.over(p) && ok; w.enter(p, w.item + gridDim.x)) {
             BoxAt box[kBoxes];
-#pragma unroll
-            for (int i = 0; i < kBoxes; ++i)
-                if (i < n) box[i] = box_at(p, rt, first + i);
             int dx[kBoxes], dy[kBoxes];
 #pragma unroll
             for (int i = 0; i < kBoxes; ++i) {
+                box[i] = {0, 0};
+                if (!rows && i < w.n) box[i] = box_at(p, w.rt, w.first + i);
                 dx[i] = dy[i] = 0;
-                if (i < n && !p.linear) { dy[i] = box[i].tap / p.kernel_w; dx[i] = box[i].tap - dy[i] * p.kernel_w - p.pad; dy[i] -= p.pad; }
+                if (!rows && !p.linear) { dy[i] = box[i].tap / p.kernel_w; dx[i] = box[i].tap - dy[i] * p.kernel_w - p.pad; dy[i] -= p.pad; }
             }
-            for (int c = c0; c < c1; ++c) {
-                if (!mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
-                const uint32_t dst = ring + s * kStage, full = bar_full + 8 * s;
-                const int by = c / p.nx, x0 = (c - by * p.nx) * p.tw, bb = by / p.ny, y0 = (by - bb * p.ny) * p.th, b0 = bb * p.tb;
-                mbar_expect_tx(full, kABytes + n * kBoxBytes);
-                if (fill++ != p.skip_fill) {
-                    if constexpr (kAMn) {
-                        tma_load_4d(dst, &map_a, rt * 128, x0, y0, b0, full);
-                        tma_load_4d(dst + 8192, &map_a, rt * 128 + 64, x0, y0, b0, full);
-                    } else {
-                        tma_load_2d(dst, &map_a, x0, rt * 128, full);
-                    }
+            const uint32_t bytes = rows ? kABytes : w.n * kBoxBytes;
+            const int row = w.rt * 128;
+            Pixels at(p, w.c);
+            for (int c = w.c; c < w.c1; ++c, at.next(p)) {
+                if (!wait_warp<false>(empty, ph ^ 1u, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                if (leader) {
+                    mbar_expect_tx(full, bytes);
+                    if (fill != p.skip_fill) {
+                        if (!rows) {
 #pragma unroll
-                    for (int i = 0; i < kBoxes; ++i)
-                        if (i < n) tma_load_4d(dst + kABytes + i * kBoxBytes, &map_b, box[i].c, x0 + dx[i], y0 + dy[i], b0, full);
+                            for (int i = 0; i < kBoxes; ++i)
+                                if (i < w.n) tma_load_4d(dst + i * kBoxBytes, &map_b, box[i].c, at.x + dx[i], at.y + dy[i], at.z, full);
+                        } else if constexpr (kAMn) {
+                            tma_load_4d(dst, &map_a, row, at.x, at.y, at.z, full);
+                            tma_load_4d(dst + 8192, &map_a, row + 64, at.x, at.y, at.z, full);
+                        } else {
+                            tma_load_2d(dst, &map_a, at.x, row, full);
+                        }
+                    }
                 }
-                if (++s == kStages) { s = 0; ph ^= 1u; }
+                ++fill;
+                dst += kStage; full += 8; empty += 8;
+                if (++s == kStages) { s = 0; dst -= kStages * kStage; full = bar_full; empty = bar_empty; ph ^= 1u; }
             }
         }
-    } else if (warp == 1 && lane == 0) {
+    } else if (warp == 1) {
         // ------------------------------------------------------------------ products
-        uint32_t ph = 0, acc = 0, acc_ph = 0;
+        const bool leader = elect_one();
+        uint32_t ph = 0, acc = 0, acc_ph = 0, off = 0;
         int s = 0;
         bool ok = true;
         const uint64_t a0 = kAMn ? make_smem_desc(ring, 8192, 1024, kLayoutSw128) : make_smem_desc(ring, 16, 1024, kLayoutSw128);
         const uint64_t b0 = make_smem_desc(ring + kABytes, kBoxBytes, 1024, kLayoutSw128);
         constexpr uint32_t a_step = kAMn ? 128u : 2u;         // sixteen tokens on, in units of 16 bytes
-        for (int item = blockIdx.x; item < p.items && ok; item += gridDim.x) {
-            const int tile = item / p.splits, split = item - tile * p.splits, first = tile % p.tiles_row * p.per;
-            const int n = min(p.per, p.boxes - first), c0 = split * p.chunks_split, c1 = min(c0 + p.chunks_split, p.chunks);
-            const uint32_t idesc = make_idesc(64 * n, false) | (kAMn ? 1u << 15 : 0u);
-            for (int c = c0; c < c1 && ok; c += kChain) {
-                ok = mbar_wait(bar_tempty + 8 * acc, acc_ph ^ 1u, abort_flag, p.wait_limit);
+        Walk w;
+        for (w.enter(p, blockIdx.x); !w.over(p) && ok; w.enter(p, w.item + gridDim.x)) {
+            const uint32_t idesc = make_idesc(64 * w.n, false) | (kAMn ? 1u << 15 : 0u);
+            for (int c = w.c; c < w.c1 && ok; c += kChain) {
+                ok = wait_warp<false>(bar_tempty + 8 * acc, acc_ph ^ 1u, leader, abort_flag, p.wait_limit);
                 if (!ok) break;
                 tc_fence_after();
                 const uint32_t d = tmem + acc * 256;
-                const int end = min(c + kChain, c1);
+                const int end = min(c + kChain, w.c1);
                 for (int i = c; i < end; ++i) {
-                    ok = mbar_wait(bar_full + 8 * s, ph, abort_flag, p.wait_limit);
+                    ok = wait_warp<false>(bar_full + 8 * s, ph, leader, abort_flag, p.wait_limit);
                     if (!ok) break;
                     tc_fence_after();
-                    const uint32_t off = (uint32_t)s * (kStage >> 4);
+                    if (leader) {
 #pragma unroll
-                    for (int j = 0; j < kStep / 16; ++j) mma_dense(d, a0 + off + j * a_step, b0 + off + j * 128u, idesc, (uint32_t)((i - c) | j));
-                    mma_commit(bar_empty + 8 * s);
-                    if (++s == kStages) { s = 0; ph ^= 1u; }
+                        for (int j = 0; j < kStep / 16; ++j) mma_dense(d, a0 + off + j * a_step, b0 + off + j * 128u, idesc, (uint32_t)((i - c) | j));
+                        mma_commit(bar_empty + 8 * s);
+                    }
+                    off += kStage >> 4;
+                    if (++s == kStages) { s = 0; off = 0; ph ^= 1u; }
                 }
                 if (!ok) break;
-                mma_commit(bar_tfull + 8 * acc);
+                if (leader) mma_commit(bar_tfull + 8 * acc);
                 if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
             }
         }
-        mma_commit(bar_done);                                 // (also where a wait has run out: no accumulator is given back under a product)
-        mbar_wait(bar_done, 0, abort_flag, kWaitLimitCycles);
+        if (leader) mma_commit(bar_done);                     // (also where a wait has run out: no accumulator is given back under a product)
+        wait_warp<false>(bar_done, 0, leader, abort_flag, kWaitLimitCycles);
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ sums
         const int q = warp & 3, half = (warp - 4) >> 2;       // a warp may read the lanes of its quarter only
@@ -304,26 +333,29 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                 store_sums(p, w, w.rt, half, w.rt * 128 + 32 * q + lane, sum);
             }
         }
-    } else if (warp >= 2) {
+    } else {
         // -------------------------------------------------------------- zeros of blocks that are not kept
         const int size = p.f32 ? 4 : 2;
-        for (int u = 2 * blockIdx.x + (warp & 1); u < p.zeros; u += 2 * gridDim.x) {
-            const int rt = u / p.zero_row, kb = u - rt * p.zero_row;
+        for (int u = blockIdx.x; u < 4 * p.zeros; u += gridDim.x) {
+            // (32 rows of a block)
+            const int block = u >> 2, rt = block / p.zero_row, kb = block - rt * p.zero_row, row0 = rt * 128 + 32 * (u & 3), rows = min(32, p.rows - row0);
             bool kept = false;
             for (int i = lane; i < p.kkeep; i += 32) kept |= p.blk_col[(int64_t)rt * p.kkeep + i] == kb;
             if (__any_sync(0xFFFFFFFFu, kept)) continue;
-            const int bytes = min(128, p.zero_k - kb * 128) * size, rows = min(128, p.rows - rt * 128);
-            uint8_t *to = reinterpret_cast<uint8_t *>(p.dw) + ((int64_t)rt * 128 * p.ld + kb * 128) * size;
-            if (p.vec && bytes % 16 == 0) {
-                const int across = bytes >> 4;            // (16-byte pieces a row: 32, 16 or those of a last block)
-                for (int i = lane; i < rows * across; i += 32)
-                    *reinterpret_cast<uint4 *>(to + (int64_t)(i / across) * p.ld * size + i % across * 16) = make_uint4(0, 0, 0, 0);
+            const int bytes = min(128, p.zero_k - kb * 128) * size, each = p.vec && bytes % 16 == 0 ? 16 : size, across = bytes / each;
+            uint8_t *to = reinterpret_cast<uint8_t *>(p.dw) + ((int64_t)row0 * p.ld + kb * 128) * size;
+            const int64_t pitch = p.ld * size;
+            if (each == 16 && (across & (across - 1)) == 0) {
+                const int at_once = 32 / across, first = lane / across;
+                to += first * pitch + (lane & (across - 1)) * 16;
+#pragma unroll 8
+                for (int r = first; r < rows; r += at_once, to += at_once * pitch) *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
             } else {
-                const int across = bytes / size;
-                for (int r = 0; r < rows; ++r)
+                for (int r = 0; r < rows; ++r, to += pitch)
                     for (int c = lane; c < across; c += 32) {
-                        if (p.f32) reinterpret_cast<float *>(to)[(int64_t)r * p.ld + c] = 0.f;
-                        else reinterpret_cast<uint16_t *>(to)[(int64_t)r * p.ld + c] = 0;
+                        if (each == 16) *reinterpret_cast<uint4 *>(to + c * 16) = make_uint4(0, 0, 0, 0);
+                        else if (each == 4) *reinterpret_cast<float *>(to + c * 4) = 0.f;
+                        else *reinterpret_cast<uint16_t *>(to + c * 2) = 0;
                     }
             }
         }
@@ -363,27 +395,6 @@ __device__ __forceinline__ void mma_dense_pair(uint32_t d, uint64_t a, uint64_t 
         "tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n\t}"
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(acc) : "memory");
 }
-__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {          // to the barrier at this place in both CTAs
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((uint16_t)3) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-// After a wait at the CTA's scope: the phase that it has seen complete, seen at the scope of the cluster.
-template <bool kAcquire>
-__device__ __forceinline__ void mbar_seen_cluster(uint32_t bar, uint32_t parity) {
-    if constexpr (kAcquire)
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(bar), "r"(parity) : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.relaxed.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(bar), "r"(parity) : "memory");
-}
-// Copies into this CTA's shared memory that complete on a barrier of either CTA of the pair.
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t cluster_bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(cluster_bar) : "memory");
-}
 __device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap *map, int c0, int c1, int c2, int c3, uint32_t cluster_bar) {
     asm volatile(
         "cp.async.bulk.tensor.4d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];"
@@ -410,7 +421,7 @@ grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     if (threadIdx.x == 0) {
         prefetch_tensormap(&map_a);
         prefetch_tensormap(&map_b);
-        for (int s = 0; s < kPairStages; ++s) { mbar_init(bar_full + 8 * s, 1); mbar_init(bar_empty + 8 * s, 1); }
+        for (int s = 0; s < kPairStages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, 2 * kDrain); }
         mbar_init(bar_done, 1);
         *abort_flag = 0;
@@ -425,10 +436,11 @@ grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     const uint32_t tmem = *tmem_slot;
     const int item0 = (int)(blockIdx.x >> 1), step = (int)(gridDim.x >> 1);
 
-    if (warp == 0 && lane == 0) {
-        // ------------------------------------------------------------------ this CTA's rows and half of the boxes, and (rank 0) both CTAs' byte count
+    if (warp == 0 || warp == 3) {
+        // ------------------------------------------------------------------ this CTA's rows, and its half of the boxes; (rank 0) both CTAs' byte counts
+        const bool leader = elect_one(), rows = warp == 0;
         const uint32_t full0 = peer_address(bar_full, 0);
-        uint32_t ph = 0;
+        uint32_t dst = ring + (rows ? 0 : kABytes), full = full0, empty = bar_empty, ph = 0;
         int s = 0, fill = 0;
         bool ok = true;
         Walk w;
@@ -440,34 +452,39 @@ grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             for (int i = 0; i < kBoxes / 2; ++i) {
                 const int b = (int)rank * mine + i;
                 box[i] = {0, p.cboxes * 64};                  // (an odd number of boxes: the last one lies behind the last column and is zeros)
-                if (i < mine && b < w.n) box[i] = box_at(p, w.rt, w.first + b);
+                if (!rows && i < mine && b < w.n) box[i] = box_at(p, w.rt, w.first + b);
                 dx[i] = dy[i] = 0;
-                if (!p.linear) { dy[i] = box[i].tap / p.kernel_w; dx[i] = box[i].tap - dy[i] * p.kernel_w - p.pad; dy[i] -= p.pad; }
+                if (!rows && !p.linear) { dy[i] = box[i].tap / p.kernel_w; dx[i] = box[i].tap - dy[i] * p.kernel_w - p.pad; dy[i] -= p.pad; }
             }
-            for (int c = w.c; c < w.c1; ++c) {
-                if (!mbar_wait(bar_empty + 8 * s, ph ^ 1u, abort_flag, p.wait_limit)) { ok = false; break; }
-                mbar_seen_cluster<false>(bar_empty + 8 * s, ph ^ 1u);
-                const uint32_t dst = ring + s * kPairStage, full = full0 + 8 * s;
-                const int by = c / p.nx, x0 = (c - by * p.nx) * p.tw, bb = by / p.ny, y0 = (by - bb * p.ny) * p.th, b0 = bb * p.tb;
-                // (the peer's bytes may come first: a phase ends with this arrival at the earliest, and the peer fills a stage anew when the one before has been multiplied)
-                if (rank == 0) mbar_expect_tx(bar_full + 8 * s, 2 * (kABytes + mine * kBoxBytes));
-                if (fill++ != p.skip_fill) {
-                    if constexpr (kAMn) {
-                        tma_load_4d_pair(dst, &map_a, row, x0, y0, b0, full);
-                        tma_load_4d_pair(dst + 8192, &map_a, row + 64, x0, y0, b0, full);
-                    } else {
-                        tma_load_2d_pair(dst, &map_a, x0, row, full);
+            const uint32_t bytes = 2 * (rows ? kABytes : mine * kBoxBytes);
+            Pixels at(p, w.c);
+            for (int c = w.c; c < w.c1; ++c, at.next(p)) {
+                if (!wait_warp<false>(empty, ph ^ 1u, leader, abort_flag, p.wait_limit)) { ok = false; break; }
+                mbar_seen_cluster<false>(empty, ph ^ 1u);
+                if (leader) {
+                    // (the peer's bytes may come first: a phase ends with these arrivals at the earliest, and the peer fills a stage anew when the one before has been multiplied)
+                    if (rank == 0) mbar_expect_tx(bar_full + 8 * s, bytes);
+                    if (fill != p.skip_fill) {
+                        if (!rows) {
+                            tma_load_4d_pair(dst, &map_b, box[0].c, at.x + dx[0], at.y + dy[0], at.z, full);
+                            if (mine > 1) tma_load_4d_pair(dst + kBoxBytes, &map_b, box[1].c, at.x + dx[1], at.y + dy[1], at.z, full);
+                        } else if constexpr (kAMn) {
+                            tma_load_4d_pair(dst, &map_a, row, at.x, at.y, at.z, full);
+                            tma_load_4d_pair(dst + 8192, &map_a, row + 64, at.x, at.y, at.z, full);
+                        } else {
+                            tma_load_2d_pair(dst, &map_a, at.x, row, full);
+                        }
                     }
-#pragma unroll
-                    for (int i = 0; i < kBoxes / 2; ++i)
-                        if (i < mine) tma_load_4d_pair(dst + kABytes + i * kBoxBytes, &map_b, box[i].c, x0 + dx[i], y0 + dy[i], b0, full);
                 }
-                if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                ++fill;
+                dst += kPairStage; full += 8; empty += 8;
+                if (++s == kPairStages) { s = 0; dst -= kPairStages * kPairStage; full = full0; empty = bar_empty; ph ^= 1u; }
             }
         }
-    } else if (warp == 1 && lane == 0 && rank == 0) {
+    } else if (warp == 1 && rank == 0) {
         // ------------------------------------------------------------------ products, of both
-        uint32_t ph = 0, acc = 0, acc_ph = 0;
+        const bool leader = elect_one();
+        uint32_t ph = 0, acc = 0, acc_ph = 0, off = 0;
         int s = 0;
         bool ok = true;
         const uint64_t a0 = kAMn ? make_smem_desc(ring, 8192, 1024, kLayoutSw128) : make_smem_desc(ring, 16, 1024, kLayoutSw128);
@@ -478,30 +495,32 @@ grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
             // (as make_idesc, M = 256)
             const uint32_t idesc = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 16) | ((uint32_t)(128 * ((w.n + 1) / 2) >> 3) << 17) | (16u << 24) | (kAMn ? 1u << 15 : 0u);
             for (int c = w.c; c < w.c1 && ok; c += kChain) {
-                ok = mbar_wait(bar_tempty + 8 * acc, acc_ph ^ 1u, abort_flag, p.wait_limit);
+                ok = wait_warp<false>(bar_tempty + 8 * acc, acc_ph ^ 1u, leader, abort_flag, p.wait_limit);
                 if (!ok) break;
                 mbar_seen_cluster<false>(bar_tempty + 8 * acc, acc_ph ^ 1u);
                 tc_fence_after();
                 const uint32_t d = tmem + acc * 256;
                 const int end = min(c + kChain, w.c1);
                 for (int i = c; i < end; ++i) {
-                    ok = mbar_wait(bar_full + 8 * s, ph, abort_flag, p.wait_limit);
+                    ok = wait_warp<false>(bar_full + 8 * s, ph, leader, abort_flag, p.wait_limit);
                     if (!ok) break;
                     mbar_seen_cluster<true>(bar_full + 8 * s, ph);
                     tc_fence_after();
-                    const uint32_t off = (uint32_t)s * (kPairStage >> 4);
+                    if (leader) {
 #pragma unroll
-                    for (int j = 0; j < kStep / 16; ++j) mma_dense_pair(d, a0 + off + j * a_step, b0 + off + j * 128u, idesc, (uint32_t)((i - c) | j));
-                    mma_commit_pair(bar_empty + 8 * s);
-                    if (++s == kPairStages) { s = 0; ph ^= 1u; }
+                        for (int j = 0; j < kStep / 16; ++j) mma_dense_pair(d, a0 + off + j * a_step, b0 + off + j * 128u, idesc, (uint32_t)((i - c) | j));
+                        mma_commit_pair(bar_empty + 8 * s);
+                    }
+                    off += kPairStage >> 4;
+                    if (++s == kPairStages) { s = 0; off = 0; ph ^= 1u; }
                 }
                 if (!ok) break;
-                mma_commit_pair(bar_tfull + 8 * acc);
+                if (leader) mma_commit_pair(bar_tfull + 8 * acc);
                 if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
             }
         }
-        mma_commit_pair(bar_done);
-        mbar_wait(bar_done, 0, abort_flag, kWaitLimitCycles);
+        if (leader) mma_commit_pair(bar_done);
+        wait_warp<false>(bar_done, 0, leader, abort_flag, kWaitLimitCycles);
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ sums
         const int q = warp & 3, half = (warp - 4) >> 2;
@@ -696,6 +715,7 @@ crisp_status_t plan_grad(const crisp_weight_grad8_t *g, GradPlan *G) {
                 if (best < 0 || n < best) { best = n; p.tw = tw; p.th = th; p.tb = tb; }
             }
     }
+    p.wo = G->wo; p.ho = G->ho;
     p.nx = (int)up(G->wo, p.tw); p.ny = (int)up(G->ho, p.th);
     const int64_t chunks = (int64_t)p.nx * p.ny * up(G->batch, p.tb);
     if (chunks > 0x7FFFFFFFll - 4096) return CRISP_UNSUPPORTED;

@@ -106,19 +106,6 @@ __host__ __device__ constexpr uint32_t make_idesc8(int n) { return (1u << 23) | 
 
 __device__ __forceinline__ float activation(float v, int relu) { return relu && v < 0.f ? 0.f : v; }         // (a NaN stays)
 
-__device__ __forceinline__ bool elect_one() {
-    uint32_t yes;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xFFFFFFFF;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(yes));
-    return yes != 0;
-}
-// A bounded wait of a whole warp.  kEarly: it may come before the kernel in front has finished, and the limit counts from then on.
-template <bool kEarly>
-__device__ __forceinline__ bool wait_warp(uint32_t bar, uint32_t parity, bool leader, volatile int *abort_flag, unsigned long long limit) {
-    if (__all_sync(0xFFFFFFFFu, mbar_try_wait(bar, parity))) return true;
-    if constexpr (kEarly) wait_for_prerequisites();
-    return __any_sync(0xFFFFFFFFu, leader && mbar_wait(bar, parity, abort_flag, limit)) != 0;
-}
-
 // One draining warp's 32 rows x 32 columns (lane = row, x[i] = column i), through its staging tile, so that the lanes write whole sectors.
 template <bool kF32>
 __device__ __forceinline__ void store_chunk8(const Params8 &p, uint8_t *stage, int lane, const float (&x)[32], int row0, int64_t col0) {
@@ -577,28 +564,6 @@ __device__ __forceinline__ void mma_scaled_pair(uint32_t d, uint64_t a, uint64_t
         "tcgen05.mma.cta_group::2.kind::mxf8f6f4.block_scale.scale_vec::1X [%0], %1, %2, %3, [%4], [%5], p;\n\t}"
         ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(acc) : "memory");
 }
-__device__ __forceinline__ void mma_commit_pair(uint32_t bar) {          // to the barrier at this place in both CTAs
-    asm volatile("tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;"
-                 ::"r"(bar), "h"((uint16_t)3) : "memory");
-}
-__device__ __forceinline__ void mbar_arrive_at(uint32_t cluster_bar) {
-    asm volatile("mbarrier.arrive.relaxed.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
-}
-// After a wait at the CTA's scope: the phase that it has seen complete, seen at the scope of the cluster.
-template <bool kAcquire>
-__device__ __forceinline__ void mbar_seen_cluster(uint32_t bar, uint32_t parity) {
-    if constexpr (kAcquire)
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.acquire.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(bar), "r"(parity) : "memory");
-    else
-        asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.relaxed.cluster.shared::cta.b64 p, [%0], %1;\n\t}" ::"r"(bar), "r"(parity) : "memory");
-}
-// A copy into this CTA's shared memory that completes on a barrier of either CTA of the pair.
-__device__ __forceinline__ void tma_load_2d_pair(uint32_t dst, const CUtensorMap *map, int x, int y, uint32_t cluster_bar) {
-    asm volatile(
-        "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3}], [%4];"
-        ::"r"(dst), "l"(map), "r"(x), "r"(y), "r"(cluster_bar) : "memory");
-}
-
 template <int N>
 __global__ void __launch_bounds__(32 * (4 + Pair8<N>::kEpi), 1)
 spmm8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_x, const __grid_constant__ CUtensorMap map_s,
