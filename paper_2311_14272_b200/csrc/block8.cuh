@@ -6,6 +6,8 @@
 #include <cuda_fp8.h>
 #include <stdint.h>
 
+#include "mask_common.cuh"
+
 namespace crisp {
 namespace block8 {
 
@@ -34,10 +36,11 @@ __device__ __forceinline__ uint32_t codes2(uint32_t pair, float down) {
     const float2 v = floats(pair);
     return __nv_cvt_float2_to_fp8x2(make_float2(v.x * down, v.y * down), __NV_SATFINITE, __NV_E4M3);
 }
-// Two codes times a scale, as bf16 (nearest even; exact but where a value is below 2^-133, or above the largest bf16).
-__device__ __forceinline__ uint32_t values2(uint32_t codes, float up) {
+// Two codes times a scale (in both halves of `up`), as bf16 (nearest even; exact but where a value is below 2^-133, or above the largest bf16).
+__device__ __forceinline__ uint32_t values2(uint32_t codes, uint64_t up) {
     const float2 v = __half22float2(__half2(__nv_cvt_fp8x2_to_halfraw2((__nv_fp8x2_storage_t)codes, __NV_E4M3)));
-    const __nv_bfloat162 b = __floats2bfloat162_rn(v.x * up, v.y * up);
+    const float2 w = f32x2_halves(mul2(f32x2(v.x, v.y), up));
+    const __nv_bfloat162 b = __floats2bfloat162_rn(w.x, w.y);
     return *reinterpret_cast<const uint32_t *>(&b);
 }
 __device__ __forceinline__ float power_of(uint32_t biased) { return __uint_as_float(biased << 23); }

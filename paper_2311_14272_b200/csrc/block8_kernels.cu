@@ -9,6 +9,7 @@
 
 #include "block8.h"
 #include "block8.cuh"
+#include "mask_common.cuh"
 
 namespace crisp {
 
@@ -375,39 +376,49 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
     for (int i = threadIdx.x; i < atoms * 64; i += 256) out[i] = reinterpret_cast<const uint4 *>(tile)[i ^ (i >> 6 & 7)];
 }
 
-// Back to bf16.  Tokens: as quantize_tokens_kernel takes them, eight values a thread and block, U blocks a thread; all codes ahead of the first store.
+// Back to bf16.  Tokens: eight threads a block of a column, 16 values each; 64 threads an atom (eight columns of a block), U atoms a thread, all codes ahead of the
+// first store.  Bound by instructions and by what leaves for DRAM (100352 x 256: 20.9 us with eight values a thread and two scalar products a pair, cold).
 template <int U>
 __global__ void __launch_bounds__(256)
 dequantize_tokens_kernel(const uint8_t *codes, const uint8_t *scales, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint16_t *y, int64_t ldy,
                          int vec_ok) {
     wait_for_prerequisites();
-    const uint32_t spans = (uint32_t)((nblk + 2 * U - 1) / (2 * U)), g = blockIdx.x / spans;
-    const int lane = threadIdx.x & 15, r = threadIdx.x >> 4 & 7, side = threadIdx.x >> 7;
-    const int64_t col = (int64_t)g * 8 + r, kb0 = (int64_t)(blockIdx.x - g * spans) * (2 * U) + side * U;
-    if (col >= ncols) return;
-    uint2 c[U] = {};
+    launch_dependents();
+    const int lane = threadIdx.x & 7, r = threadIdx.x >> 3 & 7;
+    const uint32_t atom0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * U;        // (atoms go along a group of columns first)
+    uint32_t g = atom0 / (uint32_t)nblk, kb = atom0 - g * (uint32_t)nblk;
+    uint4 c[U] = {};
     uint32_t e[U] = {};
+    int64_t to[U];
+    int n[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        if (kb0 + i >= nblk) break;
-        c[i] = *reinterpret_cast<const uint2 *>(codes + ((kb0 + i) * groups + g) * 1024 + r * 128 + (((lane >> 1) ^ r) << 4) + (lane & 1) * 8);
-        e[i] = scales[((kb0 + i) * chunks + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4];
+        const int64_t col = (int64_t)g * 8 + r;
+        const int at = (int)kb * 128 + lane * 16;
+        n[i] = g < groups && col < ncols ? (int)min((int64_t)16, k - at) : 0;
+        to[i] = col * ldy + at;
+        if (n[i] > 0) {
+            c[i] = *reinterpret_cast<const uint4 *>(codes + ((int64_t)kb * groups + g) * 1024 + r * 128 + ((lane ^ r) << 4));
+            e[i] = scales[((int64_t)kb * chunks + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4];
+        }
+        if (++kb == nblk) { kb = 0; ++g; }
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const int64_t at = (kb0 + i) * 128 + lane * 8;
-        if (at >= k) break;
-        const float up = power_of(e[i]);
-        uint32_t out[4];
+        if (n[i] <= 0) continue;
+        const uint64_t up = f32x2(power_of(e[i]), power_of(e[i]));
+        const uint32_t w[4] = {c[i].x, c[i].y, c[i].z, c[i].w};
+        uint32_t out[8];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) out[j] = values2((j < 2 ? c[i].x : c[i].y) >> (16 * (j & 1)), up);
-        uint16_t *p = y + col * ldy + at;
-        if (vec_ok && at + 8 <= k) {
-            *reinterpret_cast<uint4 *>(p) = make_uint4(out[0], out[1], out[2], out[3]);
+        for (int j = 0; j < 8; ++j) out[j] = values2(w[j / 2] >> (16 * (j & 1)), up);
+        uint16_t *p = y + to[i];
+        if (vec_ok && n[i] == 16) {
+            reinterpret_cast<uint4 *>(p)[0] = make_uint4(out[0], out[1], out[2], out[3]);
+            reinterpret_cast<uint4 *>(p)[1] = make_uint4(out[4], out[5], out[6], out[7]);
         } else {
 #pragma unroll
-            for (int j = 0; j < 8; ++j)
-                if (at + j < k) p[j] = (uint16_t)(out[j / 2] >> (16 * (j & 1)));
+            for (int j = 0; j < 16; ++j)
+                if (j < n[i]) p[j] = (uint16_t)(out[j / 2] >> (16 * (j & 1)));
         }
     }
 }
@@ -446,7 +457,7 @@ dequantize_columns_kernel(const uint8_t *codes, const uint8_t *scales, int64_t k
             if (row >= k) return;
             uint32_t v[4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = values2(four[j] >> (8 * i) & 0xFFu, up[j]) & 0xFFFFu;
+            for (int j = 0; j < 4; ++j) v[j] = values2(four[j] >> (8 * i) & 0xFFu, f32x2(up[j], up[j])) & 0xFFFFu;
             uint16_t *p = y + row * ldy + col;
             if (vec_ok && here == 4) {
                 *reinterpret_cast<uint2 *>(p) = make_uint2(v[0] | v[1] << 16, v[2] | v[3] << 16);
@@ -488,9 +499,9 @@ cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, i
 
 cudaError_t launch_dequantize8(const uint8_t *act, int layout, int64_t k, int64_t ncols, uint16_t *y, int64_t ldy, cudaStream_t st) {
     const Act8 a = act8(k, ncols);
-    const int u = a.groups * a.nblk >= 8 * 1184 ? 4 : 1;
-    const int64_t ctas = layout ? a.groups * ((a.nblk + 2 * u - 1) / (2 * u)) : a.nblk * a.chunks;
-    if (ctas > 0x7FFFFFFFll) return cudaErrorInvalidValue;
+    const int u = a.groups * a.nblk >= 16 * 1184 ? 4 : 1;
+    const int64_t ctas = layout ? (a.groups * a.nblk + 4 * u - 1) / (4 * u) : a.nblk * a.chunks;
+    if (ctas > 0x3FFFFFFFll / u) return cudaErrorInvalidValue;
     if (layout)
         return launch_chained(u == 4 ? dequantize_tokens_kernel<4> : dequantize_tokens_kernel<1>, (unsigned)ctas, 256, 0, st, act, act + a.scale_off, k, ncols, a.nblk,
                               a.groups, a.chunks, y, ldy, (int)aligned16(y, ldy));

@@ -170,10 +170,24 @@ __device__ __forceinline__ void put(T *p, const uint4 &u, int vec, int n, int st
         }
 }
 
+// A thread's items one after the other, the last one first if kDown; those to come are on their way to shared memory of its own, kDeep of them.  next() gives an item, done() says
+// that it has been used.  (Bound by how much is on its way: with four items at a time in registers 224 x 224 x 64, 32 images, took 117 us, whatever was in L2.)
+template <int kDeep>
+struct Ahead {
+    int head = 0, tail = 0;
+    __device__ __forceinline__ int in() { return head++ & (kDeep - 1); }
+    __device__ __forceinline__ int out() { return tail++ & (kDeep - 1); }
+    static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+    static __device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 1) : "memory"); }
+};
+constexpr int kDeepX = 16, kDeepDy = 8;
+constexpr int kRing = kThreads * kDeepX * 16;                // bytes; backward, items of up to 32 bytes: as many
+static_assert(kDeepX * 16 == kDeepDy * 32, "");
+
 // Where V channels of a column are in the 8-bit form, and the four bytes of their block's exponent.
 __device__ __forceinline__ int64_t codes_at(const Norm &q, int64_t col, int ch) {
-    const int kb = ch >> 7, c = ch & 127, r = (int)(col & 7);
-    return ((int64_t)kb * q.groups8 + (col >> 3)) * 1024 + r * 128 + (((c >> 4) ^ r) << 4) + (c & 15);
+    const int c = ch & 127;
+    return (int64_t)(ch >> 7) * q.groups8 * 1024 + col * 128 + ((((c >> 4) ^ (int)col) & 7) << 4) + (c & 15);
 }
 __device__ __forceinline__ int64_t scale_at(const Norm &q, int64_t col, int ch) {
     return (int64_t)q.scale_off + ((int64_t)(ch >> 7) * q.chunks8 + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4;
@@ -327,9 +341,47 @@ __device__ __forceinline__ void of_memory(const Norm &q, const Place &at, F comb
 
 // ---------------------------------------------------------------------------------------------------------------- forward
 
-// Pairs (mean, M2) of the CTA's groups to give(g, pair); item(i): what the thread has read, or reads, kAhead items at a time.
-template <typename T, bool kOne, int kAhead, typename I, typename F>
-__device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine<T> &me, float2 *threads, I item, F give) {
+// The thread's items of x out of memory, or (Kept) out of what it has kept.
+template <typename T, bool kVec, bool kDown>
+struct StreamX : Ahead<kDeepX> {
+    uint4 *slots;
+    const T *p;
+    int64_t step;
+    int left, n, vec;
+    __device__ __forceinline__ StreamX(const Norm &q, const Mine<T> &me, uint4 *smem) : slots(smem + threadIdx.x), n(me.n), vec(q.vec) {
+        step = (int64_t)q.lanes * q.ldx;
+        left = n > 0 ? me.items : 0;
+        p = reinterpret_cast<const T *>(q.x) + me.row0 * q.ldx + me.ch;
+        if (kDown) { p += (me.items - 1) * step; step = -step; }
+        if constexpr (kVec)
+            for (int i = 0; i < kDeepX; ++i) done();
+    }
+    __device__ __forceinline__ uint4 next() {
+        if constexpr (kVec) {
+            arrived();
+            return slots[out() * kThreads];
+        } else {
+            const uint4 u = fetch<false>(p, vec, n);
+            p += step;
+            return u;
+        }
+    }
+    __device__ __forceinline__ void done() {
+        if constexpr (kVec) {
+            if (left > 0) { copy_async<16>(slots + in() * kThreads, p); p += step; --left; }
+            commit();
+        }
+    }
+};
+struct KeptX {
+    const uint4 *slot;
+    __device__ __forceinline__ uint4 next() { const uint4 u = *slot; slot += kThreads; return u; }
+    __device__ __forceinline__ void done() {}
+};
+
+// Pairs (mean, M2) of the CTA's groups to give(g, pair).
+template <typename T, bool kOne, typename I, typename F>
+__device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine<T> &me, float2 *threads, I &items, F give) {
     constexpr int V = Of<T>::V, P = V / 2;
     uint64_t away[kOne ? 1 : P], s1[P], s2[P];               // away: less the thread's first values (kOne: its very first)
 #pragma unroll
@@ -338,23 +390,19 @@ __device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine
     for (int j = 0; j < (kOne ? 1 : P); ++j) away[j] = 0;
     if (me.n > 0 && me.items > 0) {
         uint64_t f[P];
-        Of<T>::open(item(0), f);
+        uint4 u = items.next();
+        Of<T>::open(u, f);
 #pragma unroll
         for (int j = 0; j < (kOne ? 1 : P); ++j) { const float2 v = f32x2_halves(f[j]); away[j] = f32x2(-v.x, kOne ? -v.x : -v.y); }
-        const auto add = [&](const uint4 &u) {
+#pragma unroll 2
+        for (int i = 0;;) {
             Of<T>::open(u, f);
 #pragma unroll
             for (int j = 0; j < P; ++j) { const uint64_t d = add2(f[j], away[kOne ? 0 : j]); s1[j] = add2(s1[j], d); s2[j] = fma2(d, d, s2[j]); }
-        };
-        int i = 0;
-        for (; i + kAhead <= me.items; i += kAhead) {
-            uint4 u[kAhead];
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) u[k] = item(i + k);
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) add(u[k]);
+            items.done();
+            if (++i >= me.items) break;
+            u = items.next();
         }
-        for (; i < me.items; ++i) add(item(i));
     }
     const float count = (float)me.items;
     if constexpr (kOne) {                                    // (mean, M2) of the thread
@@ -427,9 +475,9 @@ __device__ __forceinline__ uint64_t activate(uint64_t p) {   // (NaN stays)
     return p;
 }
 
-// y, and the 8-bit forms, of the CTA's pixels, the last one first; known(g): the statistics of the sample's group g.
-template <typename T, bool kVec, bool kHold, int kAhead, typename I, typename F>
-__device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, I item, F known) {
+// y, and the 8-bit forms, of the CTA's pixels (kDown: the last one first); known(g): the statistics of the sample's group g.
+template <typename T, bool kVec, bool kHold, bool kDown, typename I, typename F>
+__device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, I &items, F known) {
     constexpr int V = Of<T>::V, P = V / 2;
     // (threads behind the last channel write the zeros that its block ends with; not of a block in which there is none)
     if (me.lane >= q.lanes || !(me.n > 0 || (kHold && (me.ch & ~127) < q.channels))) return;
@@ -451,29 +499,22 @@ __device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, I ite
     T *y = reinterpret_cast<T *>(q.out) + me.row0 * q.ld_out + me.ch;
     const int64_t step_y = (int64_t)q.lanes * q.ld_out;
     const auto finish = [&](auto act) {
-        int i = me.items;
-        int64_t col = me.row0 + (int64_t)i * q.lanes;
-        y += i * step_y;
-        const auto one = [&](const uint4 &u) {
+        const int64_t skip = kDown ? me.items - 1 : 0, move = kDown ? -step_y : step_y;
+        int64_t col = me.row0 + skip * q.lanes;
+        y += skip * step_y;
+#pragma unroll 2
+        for (int i = 0; i < me.items; ++i) {
             uint64_t f[P];
-            Of<T>::open(u, f);
-            y -= step_y;
-            col -= q.lanes;
+            Of<T>::open(!kHold || me.n > 0 ? items.next() : make_uint4(0, 0, 0, 0), f);
             if constexpr (kHold) if (q.x8) hold<V>(q, q.x8, f, col, me.ch);
 #pragma unroll
             for (int j = 0; j < P; ++j) f[j] = activate<decltype(act)::value, T>(fma2(f[j], a[j], b[j]));      // (0 behind the last channel: a = b = 0)
             if constexpr (kHold) if (q.y8) hold<V>(q, q.y8, f, col, me.ch);
+            items.done();
             if (!kHold || (q.out && me.n > 0)) put<kVec && !kHold>(y, Of<T>::close(f), q.vec_out, me.n, q.stream);
-        };
-        const auto get = [&](int at) { return !kHold || me.n ? item(at) : make_uint4(0, 0, 0, 0); };
-        for (; i >= kAhead; i -= kAhead) {
-            uint4 u[kAhead];
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) u[k] = get(i - 1 - k);
-#pragma unroll
-            for (int k = 0; k < kAhead; ++k) one(u[k]);
+            y += move;
+            col += kDown ? -q.lanes : q.lanes;
         }
-        for (; i > 0; --i) one(get(i - 1));
     };
     switch (q.act) {
         case kRelu: finish(std::integral_constant<int, kRelu>()); break;
@@ -506,8 +547,8 @@ norm_kernel(const __grid_constant__ Norm q) {
             for (int i = 0; i < me.items; ++i) kept[i * kThreads] = fetch<false>(x + i * step, q.vec, me.n);
         }
     }
-    const auto item = [&](int i) { return kept[i * kThreads]; };
-    sum_x<T, kOne, 2>(q, at, me, threads, item, [&](int g, float2 pair) { groups[g] = pair; });
+    KeptX again{kept}, items{kept};
+    sum_x<T, kOne>(q, at, me, threads, items, [&](int g, float2 pair) { groups[g] = pair; });
     __syncthreads();
     of_cluster(q, at, groups, [&](int g, int k, int lane, int count, auto read, auto weight) {
         const float2 s = combine_x(q, k, lane, count, read, weight);
@@ -516,7 +557,7 @@ norm_kernel(const __grid_constant__ Norm q) {
             if (at.rank == 0) *reinterpret_cast<float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + at.g0 + g)) = s;
         }
     });
-    finish_y<T, kVec, kHold, 2>(q, me, item, [&](int g) { return known[g - at.g0]; });
+    finish_y<T, kVec, kHold, false>(q, me, again, [&](int g) { return known[g - at.g0]; });
     __syncwarp();
     cluster_wait();
 }
@@ -526,21 +567,22 @@ template <typename T, bool kOne, bool kVec>
 __global__ void __launch_bounds__(kThreads, kForwardCtas)
 norm_sum_kernel(const __grid_constant__ Norm q) {
     __shared__ float2 threads[kThreads * (kOne ? 1 : Of<T>::V)];
+    extern __shared__ __align__(16) uint8_t smem[];
     wait_for_prerequisites();
     const Place at(q, blockIdx.x);
     const Mine<T> me(q, at);
-    const T *x = reinterpret_cast<const T *>(q.x) + me.row0 * q.ldx + me.ch;
-    const int64_t step = (int64_t)q.lanes * q.ldx;
-    sum_x<T, kOne, 8>(q, at, me, threads, [&](int i) { return fetch<kVec>(x + i * step, q.vec, me.n); }, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
+    StreamX<T, kVec, false> items(q, me, reinterpret_cast<uint4 *>(smem));
+    sum_x<T, kOne>(q, at, me, threads, items, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
 }
 template <typename T, bool kVec, bool kHold>
 __global__ void __launch_bounds__(kThreads, kForwardCtas)
 norm_finish_kernel(const __grid_constant__ Norm q) {
     extern __shared__ __align__(16) uint8_t smem[];
-    float2 *known = reinterpret_cast<float2 *>(smem);
+    float2 *known = reinterpret_cast<float2 *>(smem + kRing);
     wait_for_prerequisites();
     const Place at(q, gridDim.x - 1 - blockIdx.x);
     const Mine<T> me(q, at);
+    StreamX<T, kVec, true> items(q, me, reinterpret_cast<uint4 *>(smem));
     of_memory(q, at, [&](int g, int k, int lane, int count, auto read, auto weight) {
         const float2 s = combine_x(q, k, lane, count, read, weight);
         if (lane == 0) {
@@ -548,9 +590,7 @@ norm_finish_kernel(const __grid_constant__ Norm q) {
             if (at.rank == 0 && (at.g0 + g) * q.cpg >= at.c0) *reinterpret_cast<float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + at.g0 + g)) = s;
         }
     });
-    const T *x = reinterpret_cast<const T *>(q.x) + me.row0 * q.ldx + me.ch;
-    const int64_t step = (int64_t)q.lanes * q.ldx;
-    finish_y<T, kVec, kHold, 4>(q, me, [&](int i) { return fetch<kVec && !kHold>(x + i * step, q.vec, me.n); }, [&](int g) { return known[g - at.g0]; });
+    finish_y<T, kVec, kHold, true>(q, me, items, [&](int g) { return known[g - at.g0]; });
 }
 
 // --------------------------------------------------------------------------------------------------------------- backward
@@ -689,9 +729,9 @@ __device__ __forceinline__ void with_act(int act, F f) {
     }
 }
 
-// Sums of e and e h of the CTA's channels to q.sums, and of its groups (times gamma) to give(g, pair).  item(i): what the thread has read, or reads, kAhead at a time.
-template <typename T, bool kOne, bool k8, bool kVec, int kAhead, typename K, typename F>
-__device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine<T> &me, float2 *channels, K item, F give) {
+// Sums of e and e h of the CTA's channels to q.sums, and of its groups (times gamma) to give(g, pair).
+template <typename T, bool kOne, bool k8, bool kVec, typename K, typename F>
+__device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine<T> &me, float2 *channels, K &items, F give) {
     constexpr int V = Of<T>::V, P = V / 2, M = kOne ? 1 : V;
     Affine<P> k;
     float mean[M], rstd[M];
@@ -706,25 +746,14 @@ __device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine
     for (int j = 0; j < P; ++j) db[j] = dg[j] = 0;
     if (me.n > 0)
         with_act(q.act, [&](auto act) {
-            const auto add = [&](const Item &u) {
+#pragma unroll 1
+            for (int i = 0; i < me.items; ++i) {
                 uint64_t d[P], x[P];
-                Reader<T, k8, kVec>::open(u, d, x);
+                Reader<T, k8, kVec>::open(items.next(), d, x);
                 slope<decltype(act)::value, T, P>(q, at.n, me.ch, k, x, d);
 #pragma unroll
                 for (int j = 0; j < P; ++j) { db[j] = add2(db[j], d[j]); dg[j] = fma2(d[j], fma2(x[j], r[kOne ? 0 : j], s[kOne ? 0 : j]), dg[j]); }
-            };
-            int i = 0;
-#pragma unroll 1
-            for (; i + kAhead <= me.items; i += kAhead) {
-                Item u[kAhead];
-#pragma unroll
-                for (int j = 0; j < kAhead; ++j) u[j] = item(i + j);
-#pragma unroll
-                for (int j = 0; j < kAhead; ++j) add(u[j]);
-            }
-            if constexpr (kAhead > 1) {
-#pragma unroll 1
-                for (; i < me.items; ++i) add(item(i));
+                items.done();
             }
         });
     const int row = q.cv * V;
@@ -767,9 +796,9 @@ __device__ __forceinline__ float2 combine_e(const Norm &q, int k, int lane, int 
     return make_float2(shared_sum(t.x, k) / all, shared_sum(t.y, k) / all);
 }
 
-// dx of the CTA's pixels, the last one first; known(g): m1 and m2 of the sample's group g.  dx = rstd (gamma e - m1 - h m2) = a e + B x + C.
-template <typename T, bool kOne, bool k8, bool kVec, int kAhead, typename K, typename F>
-__device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const Mine<T> &me, K item, F known) {
+// dx of the CTA's pixels (kDown: the last one first); known(g): m1 and m2 of the sample's group g.  dx = rstd (gamma e - m1 - h m2) = a e + B x + C.
+template <typename T, bool kOne, bool k8, bool kVec, bool kDown, typename K, typename F>
+__device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const Mine<T> &me, K &items, F known) {
     constexpr int V = Of<T>::V, P = V / 2, M = kOne ? 1 : V;
     if (me.n <= 0) return;
     Affine<P> k;
@@ -791,26 +820,17 @@ __device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const 
     T *dx = reinterpret_cast<T *>(q.out) + me.row0 * q.ld_out + me.ch;
     const int64_t step_out = (int64_t)q.lanes * q.ld_out;
     with_act(q.act, [&](auto act) {
-        const auto finish = [&](int i, const Item &u) {
+        const int64_t move = kDown ? -step_out : step_out;
+        if (kDown) dx += (me.items - 1) * step_out;
+#pragma unroll 1
+        for (int i = 0; i < me.items; ++i, dx += move) {
             uint64_t d[P], x[P];
-            Reader<T, k8, kVec>::open(u, d, x);
+            Reader<T, k8, kVec>::open(items.next(), d, x);
             slope<decltype(act)::value, T, P>(q, at.n, me.ch, k, x, d);
 #pragma unroll
             for (int j = 0; j < P; ++j) d[j] = fma2(d[j], k.a[j], fma2(x[j], B[kOne ? 0 : j], C[kOne ? 0 : j]));
-            put<kVec>(dx + i * step_out, Of<T>::close(d), q.vec_out, me.n, q.stream);
-        };
-        int i = me.items;
-#pragma unroll 1
-        for (; i >= kAhead; i -= kAhead) {
-            Item u[kAhead];
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) u[j] = item(i - 1 - j);
-#pragma unroll
-            for (int j = 0; j < kAhead; ++j) finish(i - 1 - j, u[j]);
-        }
-        if constexpr (kAhead > 1) {
-#pragma unroll 1
-            for (; i > 0; --i) finish(i - 1, item(i - 1));
+            items.done();
+            put<kVec>(dx, Of<T>::close(d), q.vec_out, me.n, q.stream);
         }
     });
 }
@@ -821,6 +841,9 @@ struct Kept {
     static constexpr int V = Of<T>::V;
     uint4 *dy, *x;
     uint32_t *codes, *e;
+    int at = 0;
+    __device__ __forceinline__ Item next() { return (*this)(at++); }
+    __device__ __forceinline__ void done() {}
     __device__ __forceinline__ Kept(const Norm &q, uint8_t *base)
         : dy(reinterpret_cast<uint4 *>(base) + threadIdx.x), x(dy + q.resident * kThreads),
           codes(reinterpret_cast<uint32_t *>(base + (size_t)q.resident * kThreads * 16) + threadIdx.x * (V / 4)),
@@ -881,41 +904,95 @@ norm_back_kernel(const __grid_constant__ Norm q) {
     const Place at(q, blockIdx.x);
     const Mine<T> me(q, at);
     kept.fill(q, me);
-    sum_e<T, kOne, k8, kVec, 1>(q, at, me, channels, kept, [&](int g, float2 pair) { groups[g] = pair; });
+    auto items = kept, again = kept;
+    sum_e<T, kOne, k8, kVec>(q, at, me, channels, items, [&](int g, float2 pair) { groups[g] = pair; });
     __syncthreads();
     of_cluster(q, at, groups, [&](int g, int k, int lane, int count, auto read, auto) {
         const float2 m = combine_e(q, k, lane, count, read);
         if (lane == 0) known[g] = m;
     });
-    finish_dx<T, kOne, k8, kVec, 1>(q, at, me, kept, [&](int g) { return known[g - at.g0]; });
+    finish_dx<T, kOne, k8, kVec, false>(q, at, me, again, [&](int g) { return known[g - at.g0]; });
     __syncwarp();
     cluster_wait();
 }
+
+// The thread's items out of memory.
+template <typename T, bool k8, bool kVec, bool kDown>
+struct StreamDy : Ahead<kDeepDy> {
+    static constexpr int V = Of<T>::V;
+    Reader<T, k8, kVec> read;
+    uint4 *dy, *x;
+    uint32_t *codes, *e;
+    int to_come, at;                                         // items that are not on their way yet, and the next of them (or, not kVec, the next one)
+    __device__ __forceinline__ StreamDy(const Norm &q, const Mine<T> &me, uint8_t *smem)
+        : read(q, me), dy(reinterpret_cast<uint4 *>(smem) + threadIdx.x), x(dy + kDeepDy * kThreads),
+          codes(reinterpret_cast<uint32_t *>(smem + kDeepDy * kThreads * 16) + threadIdx.x * (V / 4)),
+          e(reinterpret_cast<uint32_t *>(smem + kDeepDy * kThreads * (16 + V)) + threadIdx.x) {
+        to_come = me.n > 0 ? me.items : 0;
+        at = kDown ? me.items - 1 : 0;
+        if constexpr (kVec)
+            for (int i = 0; i < kDeepDy; ++i) done();
+    }
+    __device__ __forceinline__ Item next() {
+        if constexpr (kVec) {
+            arrived();
+            const int s = out() * kThreads;
+            Item r;
+            r.dy = dy[s];
+            if constexpr (k8) r.x = make_uint4(codes[s * (V / 4)], V == 8 ? codes[s * (V / 4) + V / 4 - 1] : 0u, e[s], 0u);
+            else r.x = x[s];
+            return r;
+        } else {
+            const Item r = read(at);
+            at += kDown ? -1 : 1;
+            return r;
+        }
+    }
+    __device__ __forceinline__ void done() {
+        if constexpr (kVec) {
+            if (to_come > 0) {
+                const int s = in() * kThreads;
+                copy_async<16>(dy + s, read.dy + at * read.step_dy);
+                if constexpr (k8) {
+                    const int64_t col = read.me.row0 + (int64_t)at * read.q.lanes;
+                    copy_async<V>(codes + s * (V / 4), read.q.from8 + codes_at(read.q, col, read.me.ch));
+                    copy_async<4>(e + s, read.q.from8 + scale_at(read.q, col, read.me.ch));
+                } else {
+                    copy_async<16>(x + s, read.x + at * read.step_x);
+                }
+                at += kDown ? -1 : 1;
+                --to_come;
+            }
+            commit();
+        }
+    }
+};
 
 template <typename T, bool kOne, bool k8, bool kVec>
 __global__ void __launch_bounds__(kThreads, kBackwardCtas)
 norm_back_sum_kernel(const __grid_constant__ Norm q) {
     __shared__ float2 channels[kThreads * Of<T>::V];
+    extern __shared__ __align__(16) uint8_t smem[];
     wait_for_prerequisites();
     const Place at(q, blockIdx.x);
     const Mine<T> me(q, at);
-    const Reader<T, k8, kVec> read(q, me);
-    sum_e<T, kOne, k8, kVec, 4>(q, at, me, channels, read, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
+    StreamDy<T, k8, kVec, false> items(q, me, smem);
+    sum_e<T, kOne, k8, kVec>(q, at, me, channels, items, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
 }
 template <typename T, bool kOne, bool k8, bool kVec>
 __global__ void __launch_bounds__(kThreads, kBackwardCtas)
 norm_back_finish_kernel(const __grid_constant__ Norm q) {
     extern __shared__ __align__(16) uint8_t smem[];
-    float2 *known = reinterpret_cast<float2 *>(smem);
+    float2 *known = reinterpret_cast<float2 *>(smem + kRing);
     wait_for_prerequisites();
     const Place at(q, gridDim.x - 1 - blockIdx.x);
     const Mine<T> me(q, at);
+    StreamDy<T, k8, kVec, true> items(q, me, smem);
     of_memory(q, at, [&](int g, int k, int lane, int count, auto read, auto) {
         const float2 m = combine_e(q, k, lane, count, read);
         if (lane == 0) known[g] = m;
     });
-    const Reader<T, k8, kVec> read(q, me);
-    finish_dx<T, kOne, k8, kVec, 4>(q, at, me, read, [&](int g) { return known[g - at.g0]; });
+    finish_dx<T, kOne, k8, kVec, true>(q, at, me, items, [&](int g) { return known[g - at.g0]; });
 }
 
 // dbeta and dgamma: the sums of all CTAs' [rows][2][channels], a warp's lanes on 32 neighbouring ones, in one order.
@@ -996,7 +1073,7 @@ Plan plan_of(const crisp_group_norm_t &d, bool back, bool from8, bool eight) {
         const int64_t ranks = once * slices * 20 >= grid * 17 ? once : ceil_div(4 * grid, slices);
         rank(std::min<int64_t>(std::min<int64_t>(ranks, 128), ceil_div(d.pixels, 4 * (kThreads / p.cv))));
         p.resident = 0;
-        p.fixed_smem = (p.width / cpg + 2) * 8;
+        p.fixed_smem = kRing + (p.width / cpg + 2) * 8;
     }
     p.tiles = batch * p.slices * p.ranks;
     return p;
@@ -1023,14 +1100,14 @@ crisp_status_t check(const crisp_group_norm_t *d) {
     return CRISP_OK;
 }
 
-template <auto kernel>
+template <auto kernel, size_t kSmem>
 cudaError_t allow() {                                                        // (once a kernel and device)
     static std::atomic<uint64_t> ready{0};
     int device = 0;
     cudaError_t e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
     if (device < 64 && ready.load(std::memory_order_relaxed) >> device & 1) return cudaSuccess;
-    e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kMaxSmem);
+    e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmem);
     if (e == cudaSuccess) e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
     if (e == cudaSuccess && device < 64) ready.fetch_or(1ull << device, std::memory_order_relaxed);
     return e;
@@ -1040,10 +1117,12 @@ cudaError_t run(const Plan &p, const Norm &q, int item, cudaStream_t st) {
     if (p.tiles > 0x7FFFFFFFll) return cudaErrorInvalidValue;
     const size_t smem = p.fixed_smem + (size_t)p.resident * kThreads * item;
     if (p.cluster) {
-        const cudaError_t e = allow<small>();
+        const cudaError_t e = allow<small, kMaxSmem>();
         return e != cudaSuccess ? e : launch_clusters(small, (unsigned)p.tiles, kThreads, smem, st, (unsigned)q.ranks, q);
     }
-    const cudaError_t e = launch_chained(sum, (unsigned)p.tiles, kThreads, 0, st, q);
+    cudaError_t e = allow<sum, kRing>();
+    if (e == cudaSuccess) e = allow<finish, kRing + (kThreads * 8 + 2) * 8>();
+    if (e == cudaSuccess) e = launch_chained(sum, (unsigned)p.tiles, kThreads, kRing, st, q);
     return e != cudaSuccess ? e : launch_chained(finish, (unsigned)p.tiles, kThreads, smem, st, q);
 }
 template <typename T, bool kOne, bool kVec, bool kHold>

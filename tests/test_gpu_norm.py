@@ -300,8 +300,9 @@ def test_pixels_beyond_32_bits():
     norm = B.GroupNorm(channels, 23, activation="relu")
     done = norm.forward(x, keep_x=True)
     alone = norm.forward(x[-1:], keep_x=True)
-    # (a batch of one is cut otherwise: sums of another order, results of another rounding)
-    near = lambda a, b: (a.float() - b.float()).abs().max().item() <= 2.0**-8 * b.float().abs().max().item()  # noqa: E731
+    # (a batch of one is cut otherwise: sums of another order.  Two values next to a border of bf16's rounding, however near, may be a step apart: 2^(e - 7) for values from 2^e on,
+    # at most 2^-7 of the value)
+    near = lambda a, b: (a.float() - b.float()).abs().max().item() <= 2.0**-7 * b.float().abs().max().item()  # noqa: E731
     assert near(done.y[-1:], alone.y) and near(done.statistics[-1:], alone.statistics)
     part = B.quantize8(x[-1, -64:], tokens=True).dequantize(tokens=True)
     assert torch.equal(done.x8.dequantize(tokens=True)[-64:], part)
