@@ -57,6 +57,7 @@ struct Norm {
     int some, more, some_last, more_last;    // items of a pixel lane: `some`, the first `more` lanes one more (the last rank's: ..._last)
     int resident;                        // items (V channels of a pixel) that a thread keeps
     uint32_t across_magic, cpg_magic;    // 2^32 / (entries of a whole group and lane), / cpg, rounded up (0: not exact for all channels)
+    int whole8;                          // slices are whole blocks of 128 channels
     int act, vec, vec_dy, vec_out;       // vec: addresses and pitches allow 16 bytes at once
     int stream;                          // the results are not kept in L2 at the cost of what is still to be read
     float eps;
@@ -76,15 +77,28 @@ struct Of<float> {
         return make_uint4(__float_as_uint(a.x), __float_as_uint(a.y), __float_as_uint(b.x), __float_as_uint(b.y));
     }
     static __device__ __forceinline__ float sigmoid(float p) { return 1.f / (1.f + expf(-p)); }
+    static __device__ __forceinline__ uint64_t sigmoid2(uint64_t p) { const float2 v = f32x2_halves(p); return f32x2(sigmoid(v.x), sigmoid(v.y)); }
 };
 struct Of16 {
     static constexpr int V = 8;
-    // (some 2^-21 of the value, far below the result's last place; 0 where it is below 2^-126)
+    // (some 2^-20 of the value, far below the result's last place; 0 where it is below 2^-126)
     static __device__ __forceinline__ float sigmoid(float p) {
         float e, r;
         asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(p * -1.44269504f));
         asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
         return r;
+    }
+    // Of two values, with one reciprocal of the product of both denominators: the special function unit is what the forward pass with silu is bound by (75 % of its rate with
+    // four of its instructions a pair).  Where a denominator is above 2^62, or NaN, each for itself.
+    static __device__ __forceinline__ uint64_t sigmoid2(uint64_t p) {
+        const float2 v = f32x2_halves(mul2(p, f32x2(-1.44269504f, -1.44269504f)));
+        float a, b, r;
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(a) : "f"(v.x));
+        asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(b) : "f"(v.y));
+        if (!(max_nan(a, b) <= 0x1p62f)) { const float2 w = f32x2_halves(p); return f32x2(sigmoid(w.x), sigmoid(w.y)); }
+        a += 1.f; b += 1.f;
+        asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(a * b));
+        return mul2(f32x2(r, r), f32x2(b, a));
     }
 };
 template <>
@@ -180,7 +194,7 @@ struct Ahead {
     static __device__ __forceinline__ void commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
     static __device__ __forceinline__ void arrived() { asm volatile("cp.async.wait_group %0;" ::"n"(kDeep - 1) : "memory"); }
 };
-constexpr int kDeepX = 16, kDeepDy = 8;
+constexpr int kDeepX = 8, kDeepDy = 4;
 constexpr int kRing = kThreads * kDeepX * 16;                // bytes; backward, items of up to 32 bytes: as many
 static_assert(kDeepX * 16 == kDeepDy * 32, "");
 
@@ -380,7 +394,7 @@ struct KeptX {
 };
 
 // Pairs (mean, M2) of the CTA's groups to give(g, pair).
-template <typename T, bool kOne, typename I, typename F>
+template <typename T, bool kOne, bool kOver, typename I, typename F>
 __device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine<T> &me, float2 *threads, I &items, F give) {
     constexpr int V = Of<T>::V, P = V / 2;
     uint64_t away[kOne ? 1 : P], s1[P], s2[P];               // away: less the thread's first values (kOne: its very first)
@@ -404,6 +418,7 @@ __device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine
             u = items.next();
         }
     }
+    if constexpr (kOver) __syncthreads();                    // (what follows lies over what the threads had on its way)
     const float count = (float)me.items;
     if constexpr (kOne) {                                    // (mean, M2) of the thread
         const float one = f32x2_sum(P == 4 ? add2(add2(s1[0], s1[1]), add2(s1[P - 2], s1[P - 1])) : add2(s1[0], s1[1]));
@@ -471,7 +486,7 @@ __device__ __forceinline__ uint64_t activate(uint64_t p) {   // (NaN stays)
         float a = max_nan(v.x, 0.f), b = max_nan(v.y, 0.f);
         return f32x2(a > 6.f ? 6.f : a, b > 6.f ? 6.f : b);
     }
-    if constexpr (kAct == kSilu) return mul2(p, f32x2(Of<T>::sigmoid(v.x), Of<T>::sigmoid(v.y)));
+    if constexpr (kAct == kSilu) return mul2(p, Of<T>::sigmoid2(p));
     return p;
 }
 
@@ -548,7 +563,7 @@ norm_kernel(const __grid_constant__ Norm q) {
         }
     }
     KeptX again{kept}, items{kept};
-    sum_x<T, kOne>(q, at, me, threads, items, [&](int g, float2 pair) { groups[g] = pair; });
+    sum_x<T, kOne, false>(q, at, me, threads, items, [&](int g, float2 pair) { groups[g] = pair; });
     __syncthreads();
     of_cluster(q, at, groups, [&](int g, int k, int lane, int count, auto read, auto weight) {
         const float2 s = combine_x(q, k, lane, count, read, weight);
@@ -566,13 +581,12 @@ norm_kernel(const __grid_constant__ Norm q) {
 template <typename T, bool kOne, bool kVec>
 __global__ void __launch_bounds__(kThreads, kForwardCtas)
 norm_sum_kernel(const __grid_constant__ Norm q) {
-    __shared__ float2 threads[kThreads * (kOne ? 1 : Of<T>::V)];
     extern __shared__ __align__(16) uint8_t smem[];
     wait_for_prerequisites();
     const Place at(q, blockIdx.x);
     const Mine<T> me(q, at);
     StreamX<T, kVec, false> items(q, me, reinterpret_cast<uint4 *>(smem));
-    sum_x<T, kOne>(q, at, me, threads, items, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
+    sum_x<T, kOne, true>(q, at, me, reinterpret_cast<float2 *>(smem), items, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
 }
 template <typename T, bool kVec, bool kHold>
 __global__ void __launch_bounds__(kThreads, kForwardCtas)
@@ -625,21 +639,19 @@ __device__ __forceinline__ void slope(const Norm &q, int n, int ch, const Affine
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             const uint64_t p = fma2(x[j], k.a[j], k.b[j]);
-            const float2 v = f32x2_halves(p);
-            const uint64_t s = f32x2(Of<T>::sigmoid(v.x), Of<T>::sigmoid(v.y)), rest = fma2(s, both(-1.f), both(1.f));
+            const uint64_t s = Of<T>::sigmoid2(p), rest = fma2(s, both(-1.f), both(1.f));
             dy[j] = mul2(dy[j], mul2(s, fma2(p, rest, both(1.f))));
         }
     } else {
-        float p[2 * P];
-        bool close = false;
+        float p[2 * P], least = INFINITY;                     // (three values a minimum)
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             const float2 v = f32x2_halves(fma2(x[j], k.a[j], k.b[j]));
             p[2 * j] = v.x; p[2 * j + 1] = v.y;
-            close |= fabsf(v.x) < k.near || fabsf(v.y) < k.near;
-            if constexpr (kAct == kRelu6) close |= fabsf(v.x - 6.f) < k.near || fabsf(v.y - 6.f) < k.near;
+            least = fminf(fminf(fabsf(v.x), fabsf(v.y)), least);
+            if constexpr (kAct == kRelu6) least = fminf(fminf(fabsf(v.x - 6.f), fabsf(v.y - 6.f)), least);
         }
-        if (close) {
+        if (least < k.near) {
 #pragma unroll
             for (int j = 0; j < 2 * P; ++j) {
                 if (ch + j >= q.channels) break;
@@ -695,6 +707,12 @@ struct Reader {
     const Mine<T> &me;
     const T *x, *dy;
     int64_t step_x, step_dy;
+    // Where a thread keeps an item's codes: in the order that they have in memory (swizzled by the column) where its block's threads are all there, so that a copy of half a warp goes
+    // to one line as it comes from one (else 53 wavefronts an item, not 14: backward of 56 x 56 x 256 from 8 bits, 32 images, 58 us).
+    __device__ __forceinline__ int place(int64_t col) const {
+        const int c = me.ch & 127;
+        return q.whole8 ? (int)(threadIdx.x & ~(128 / V - 1)) * V + ((((c >> 4) ^ (int)col) & 7) << 4) + (c & 15) : (int)threadIdx.x * V;
+    }
     __device__ __forceinline__ Reader(const Norm &q_, const Mine<T> &me_)
         : q(q_), me(me_), x(reinterpret_cast<const T *>(q_.x) + me_.row0 * q_.ldx + me_.ch), dy(reinterpret_cast<const T *>(q_.dy) + me_.row0 * q_.ld_dy + me_.ch),
           step_x((int64_t)q_.lanes * q_.ldx), step_dy((int64_t)q_.lanes * q_.ld_dy) {}
@@ -730,7 +748,7 @@ __device__ __forceinline__ void with_act(int act, F f) {
 }
 
 // Sums of e and e h of the CTA's channels to q.sums, and of its groups (times gamma) to give(g, pair).
-template <typename T, bool kOne, bool k8, bool kVec, typename K, typename F>
+template <typename T, bool kOne, bool k8, bool kVec, bool kOver, typename K, typename F>
 __device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine<T> &me, float2 *channels, K &items, F give) {
     constexpr int V = Of<T>::V, P = V / 2, M = kOne ? 1 : V;
     Affine<P> k;
@@ -756,6 +774,7 @@ __device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine
                 items.done();
             }
         });
+    if constexpr (kOver) __syncthreads();
     const int row = q.cv * V;
     if (me.lane < q.lanes) {
 #pragma unroll
@@ -905,7 +924,7 @@ norm_back_kernel(const __grid_constant__ Norm q) {
     const Mine<T> me(q, at);
     kept.fill(q, me);
     auto items = kept, again = kept;
-    sum_e<T, kOne, k8, kVec>(q, at, me, channels, items, [&](int g, float2 pair) { groups[g] = pair; });
+    sum_e<T, kOne, k8, kVec, false>(q, at, me, channels, items, [&](int g, float2 pair) { groups[g] = pair; });
     __syncthreads();
     of_cluster(q, at, groups, [&](int g, int k, int lane, int count, auto read, auto) {
         const float2 m = combine_e(q, k, lane, count, read);
@@ -922,14 +941,16 @@ struct StreamDy : Ahead<kDeepDy> {
     static constexpr int V = Of<T>::V;
     Reader<T, k8, kVec> read;
     uint4 *dy, *x;
-    uint32_t *codes, *e;
+    uint8_t *codes;
+    uint32_t *e;
+    int64_t col;                                             // of the item that next() gives
     int to_come, at;                                         // items that are not on their way yet, and the next of them (or, not kVec, the next one)
     __device__ __forceinline__ StreamDy(const Norm &q, const Mine<T> &me, uint8_t *smem)
         : read(q, me), dy(reinterpret_cast<uint4 *>(smem) + threadIdx.x), x(dy + kDeepDy * kThreads),
-          codes(reinterpret_cast<uint32_t *>(smem + kDeepDy * kThreads * 16) + threadIdx.x * (V / 4)),
-          e(reinterpret_cast<uint32_t *>(smem + kDeepDy * kThreads * (16 + V)) + threadIdx.x) {
+          codes(smem + kDeepDy * kThreads * 16), e(reinterpret_cast<uint32_t *>(smem + kDeepDy * kThreads * (16 + V)) + threadIdx.x) {
         to_come = me.n > 0 ? me.items : 0;
         at = kDown ? me.items - 1 : 0;
+        col = me.row0 + (int64_t)at * q.lanes;
         if constexpr (kVec)
             for (int i = 0; i < kDeepDy; ++i) done();
     }
@@ -939,8 +960,14 @@ struct StreamDy : Ahead<kDeepDy> {
             const int s = out() * kThreads;
             Item r;
             r.dy = dy[s];
-            if constexpr (k8) r.x = make_uint4(codes[s * (V / 4)], V == 8 ? codes[s * (V / 4) + V / 4 - 1] : 0u, e[s], 0u);
-            else r.x = x[s];
+            if constexpr (k8) {
+                const uint32_t *c = reinterpret_cast<const uint32_t *>(codes + s * V + read.place(col));
+                if constexpr (V == 8) { const uint2 two = *reinterpret_cast<const uint2 *>(c); r.x = make_uint4(two.x, two.y, e[s], 0u); }
+                else r.x = make_uint4(c[0], 0u, e[s], 0u);
+                col += kDown ? -read.q.lanes : read.q.lanes;
+            } else {
+                r.x = x[s];
+            }
             return r;
         } else {
             const Item r = read(at);
@@ -954,9 +981,9 @@ struct StreamDy : Ahead<kDeepDy> {
                 const int s = in() * kThreads;
                 copy_async<16>(dy + s, read.dy + at * read.step_dy);
                 if constexpr (k8) {
-                    const int64_t col = read.me.row0 + (int64_t)at * read.q.lanes;
-                    copy_async<V>(codes + s * (V / 4), read.q.from8 + codes_at(read.q, col, read.me.ch));
-                    copy_async<4>(e + s, read.q.from8 + scale_at(read.q, col, read.me.ch));
+                    const int64_t there = read.me.row0 + (int64_t)at * read.q.lanes;
+                    copy_async<V>(codes + s * V + read.place(there), read.q.from8 + codes_at(read.q, there, read.me.ch));
+                    copy_async<4>(e + s, read.q.from8 + scale_at(read.q, there, read.me.ch));
                 } else {
                     copy_async<16>(x + s, read.x + at * read.step_x);
                 }
@@ -971,13 +998,12 @@ struct StreamDy : Ahead<kDeepDy> {
 template <typename T, bool kOne, bool k8, bool kVec>
 __global__ void __launch_bounds__(kThreads, kBackwardCtas)
 norm_back_sum_kernel(const __grid_constant__ Norm q) {
-    __shared__ float2 channels[kThreads * Of<T>::V];
     extern __shared__ __align__(16) uint8_t smem[];
     wait_for_prerequisites();
     const Place at(q, blockIdx.x);
     const Mine<T> me(q, at);
     StreamDy<T, k8, kVec, false> items(q, me, smem);
-    sum_e<T, kOne, k8, kVec>(q, at, me, channels, items, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
+    sum_e<T, kOne, k8, kVec, true>(q, at, me, reinterpret_cast<float2 *>(smem), items, [&](int g, float2 pair) { *partial_at(q, at, g) = pair; });
 }
 template <typename T, bool kOne, bool k8, bool kVec>
 __global__ void __launch_bounds__(kThreads, kBackwardCtas)
@@ -1163,6 +1189,7 @@ Norm norm_of(const crisp_group_norm_t &d, const Plan &p, const Space &s, void *w
     const int last = q.pixels - (p.ranks - 1) * p.per;
     q.some = p.per / q.lanes; q.more = p.per % q.lanes; q.some_last = last / q.lanes; q.more_last = last % q.lanes;
     q.resident = p.resident;
+    q.whole8 = d.channels % 128 == 0 && p.width % 128 == 0;
     if (q.cpg > 1 && (double)d.channels * q.cpg < 4294967296.0) q.cpg_magic = (uint32_t)((((uint64_t)1 << 32) + q.cpg - 1) / q.cpg);
     q.stream = !p.cluster && (double)d.batch * d.pixels * d.channels * (d.dtype == 1 ? 4 : 2) > 64e6;
     q.act = d.activation;
