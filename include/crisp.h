@@ -610,8 +610,10 @@ typedef struct {
     crisp_mask_t mask;
     void *d_dw;
     int64_t ld_dw;
-    int32_t accumulate, reserved;        /* reserved: 0 */
+    int32_t accumulate;
+    int32_t skip_fill;                   /* test hook, 0 = off: every CTA leaves out the copies of its skip_fill-th pipeline fill, so that the wait for them expires */
     int32_t *d_status;
+    uint64_t wait_limit_cycles;          /* every wait within the kernel gives up after so many SM cycles; 0 = about two seconds */
 } crisp_weight_grad8_t;
 CRISP_API crisp_status_t crisp_weight_grad8_sizes(const crisp_weight_grad8_t *grad, size_t *workspace_bytes);
 CRISP_API crisp_status_t crisp_weight_grad8(const crisp_weight_grad8_t *grad, void *d_workspace, void *stream);

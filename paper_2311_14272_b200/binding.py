@@ -66,7 +66,7 @@ class GroupNormDesc(C.Structure):
 class WeightGrad8(C.Structure):
     _fields_ = [("rows", C.c_int32), ("k", C.c_int32), ("ncols", C.c_int64), ("conv", C.POINTER(ConvDesc)), ("d_dy", C.c_void_p), ("ld_dy", C.c_int64),
                 ("dy_layout", C.c_int32), ("dw_dtype", C.c_int32), ("d_act", C.c_void_p), ("mask", C.c_void_p), ("d_dw", C.c_void_p), ("ld_dw", C.c_int64),
-                ("accumulate", C.c_int32), ("reserved", C.c_int32), ("d_status", C.c_void_p)]
+                ("accumulate", C.c_int32), ("skip_fill", C.c_int32), ("d_status", C.c_void_p), ("wait_limit_cycles", C.c_uint64)]
 
 
 class LaunchInfo(C.Structure):

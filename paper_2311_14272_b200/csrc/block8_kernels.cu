@@ -376,8 +376,8 @@ quantize_columns_kernel(const uint16_t *x, int64_t ldx, int64_t k, int64_t ncols
     for (int i = threadIdx.x; i < atoms * 64; i += 256) out[i] = reinterpret_cast<const uint4 *>(tile)[i ^ (i >> 6 & 7)];
 }
 
-// Back to bf16.  Tokens: eight threads a block of a column, 16 values each; 64 threads an atom (eight columns of a block), U atoms a thread, all codes ahead of the
-// first store.  Bound by instructions and by what leaves for DRAM (100352 x 256: 20.9 us with eight values a thread and two scalar products a pair, cold).
+// Back to bf16.  Tokens: eight threads a block of a column, 16 values each; 64 threads an atom (eight columns of a block), U blocks a thread, all codes ahead of the
+// first store; a CTA takes 32 columns.  vec_ok: 2 for stores of whole sectors (32 bytes at multiples of as many), 1 for 16 bytes.
 template <int U>
 __global__ void __launch_bounds__(256)
 dequantize_tokens_kernel(const uint8_t *codes, const uint8_t *scales, int64_t k, int64_t ncols, int64_t nblk, int64_t groups, int64_t chunks, uint16_t *y, int64_t ldy,
@@ -385,23 +385,23 @@ dequantize_tokens_kernel(const uint8_t *codes, const uint8_t *scales, int64_t k,
     wait_for_prerequisites();
     launch_dependents();
     const int lane = threadIdx.x & 7, r = threadIdx.x >> 3 & 7;
-    const uint32_t atom0 = (blockIdx.x * 4 + (threadIdx.x >> 6)) * U;        // (atoms go along a group of columns first)
-    uint32_t g = atom0 / (uint32_t)nblk, kb = atom0 - g * (uint32_t)nblk;
+    const uint32_t spans = (uint32_t)((nblk + U - 1) / U), quad = blockIdx.x / spans, g = quad * 4 + (threadIdx.x >> 6);
+    uint32_t kb = (blockIdx.x - quad * spans) * U;
+    const int64_t col = (int64_t)g * 8 + r;
     uint4 c[U] = {};
     uint32_t e[U] = {};
     int64_t to[U];
     int n[U];
 #pragma unroll
     for (int i = 0; i < U; ++i) {
-        const int64_t col = (int64_t)g * 8 + r;
         const int at = (int)kb * 128 + lane * 16;
-        n[i] = g < groups && col < ncols ? (int)min((int64_t)16, k - at) : 0;
+        n[i] = kb < nblk && col < ncols ? (int)min((int64_t)16, k - at) : 0;
         to[i] = col * ldy + at;
         if (n[i] > 0) {
             c[i] = *reinterpret_cast<const uint4 *>(codes + ((int64_t)kb * groups + g) * 1024 + r * 128 + ((lane ^ r) << 4));
             e[i] = scales[((int64_t)kb * chunks + (col >> 7)) * kScales8 + (col & 31) * 16 + (col >> 5 & 3) * 4];
         }
-        if (++kb == nblk) { kb = 0; ++g; }
+        ++kb;
     }
 #pragma unroll
     for (int i = 0; i < U; ++i) {
@@ -412,7 +412,10 @@ dequantize_tokens_kernel(const uint8_t *codes, const uint8_t *scales, int64_t k,
 #pragma unroll
         for (int j = 0; j < 8; ++j) out[j] = values2(w[j / 2] >> (16 * (j & 1)), up);
         uint16_t *p = y + to[i];
-        if (vec_ok && n[i] == 16) {
+        if (vec_ok == 2 && n[i] == 16) {
+            asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(out[0]), "r"(out[1]), "r"(out[2]), "r"(out[3]), "r"(out[4]), "r"(out[5]),
+                         "r"(out[6]), "r"(out[7]) : "memory");
+        } else if (vec_ok && n[i] == 16) {
             reinterpret_cast<uint4 *>(p)[0] = make_uint4(out[0], out[1], out[2], out[3]);
             reinterpret_cast<uint4 *>(p)[1] = make_uint4(out[4], out[5], out[6], out[7]);
         } else {
@@ -499,12 +502,13 @@ cudaError_t launch_decode8(const Geometry &g, const uint8_t *buf, uint16_t *w, i
 
 cudaError_t launch_dequantize8(const uint8_t *act, int layout, int64_t k, int64_t ncols, uint16_t *y, int64_t ldy, cudaStream_t st) {
     const Act8 a = act8(k, ncols);
-    const int u = a.groups * a.nblk >= 16 * 1184 ? 4 : 1;
-    const int64_t ctas = layout ? (a.groups * a.nblk + 4 * u - 1) / (4 * u) : a.nblk * a.chunks;
-    if (ctas > 0x3FFFFFFFll / u) return cudaErrorInvalidValue;
-    if (layout)
-        return launch_chained(u == 4 ? dequantize_tokens_kernel<4> : dequantize_tokens_kernel<1>, (unsigned)ctas, 256, 0, st, act, act + a.scale_off, k, ncols, a.nblk,
-                              a.groups, a.chunks, y, ldy, (int)aligned16(y, ldy));
+    const int u = a.groups * a.nblk < 16 * 1184 || a.nblk < 2 ? 1 : 2;       // (two blocks a thread where there are CTAs enough; four take 48 registers and more time)
+    const int64_t ctas = layout ? (a.groups + 3) / 4 * ((a.nblk + u - 1) / u) : a.nblk * a.chunks;
+    if (ctas > 0x1FFFFFFFll) return cudaErrorInvalidValue;
+    if (layout) {
+        return launch_chained(u == 2 ? dequantize_tokens_kernel<2> : dequantize_tokens_kernel<1>, (unsigned)ctas, 256, 0, st, act, act + a.scale_off, k, ncols, a.nblk, a.groups, a.chunks, y, ldy,
+                              reinterpret_cast<uintptr_t>(y) % 32 == 0 && ldy % 16 == 0 ? 2 : (int)aligned16(y, ldy));
+    }
     const int quads = reinterpret_cast<uintptr_t>(y) % 8 == 0 && ldy % 4 == 0;
     return launch_chained(dequantize_columns_kernel, (unsigned)ctas, 256, 0, st, act, act + a.scale_off, k, ncols, a.nblk, a.groups, a.chunks, y, ldy, quads);
 }

@@ -684,7 +684,7 @@ struct GradPlan {
 };
 
 crisp_status_t plan_grad(const crisp_weight_grad8_t *g, GradPlan *G) {
-    if (!g || (g->dy_layout != 0 && g->dy_layout != 1) || (g->dw_dtype != 0 && g->dw_dtype != 1) || (g->accumulate != 0 && g->accumulate != 1) || g->reserved != 0)
+    if (!g || (g->dy_layout != 0 && g->dy_layout != 1) || (g->dw_dtype != 0 && g->dw_dtype != 1) || (g->accumulate != 0 && g->accumulate != 1) || g->skip_fill < 0)
         return CRISP_INVALID_ARG;
     if (g->rows <= 0 || g->k <= 0 || g->ncols <= 0) return CRISP_BAD_SHAPE;
     if (g->ncols > 0x7FFFFFFFll - 65536 || g->rows > 65535 * 32 || g->k > kMaxBlocksPerRowTile * 128) return CRISP_UNSUPPORTED;
@@ -785,8 +785,8 @@ cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cu
     p.dw = g.d_dw; p.ld = g.ld_dw; p.f32 = g.dw_dtype; p.accumulate = g.accumulate;
     p.vec = aligned_to(g.d_dw, 16) && g.ld_dw * (g.dw_dtype ? 4 : 2) % 16 == 0;
     p.status = g.d_status;
-    p.wait_limit = kWaitLimitCycles;
-    p.skip_fill = -1;
+    p.wait_limit = g.wait_limit_cycles ? g.wait_limit_cycles : kWaitLimitCycles;
+    p.skip_fill = g.skip_fill - 1;
     if (p.boxes == 0)
         return g.accumulate ? cudaSuccess : launch_chained(zero_kernel, (unsigned)std::min(g.rows, 4096), 256, 0, st, (int64_t)g.rows, (int)g.k, g.d_dw, g.ld_dw, (int)g.dw_dtype);
     if (G.blocks && !g.accumulate) { p.zero_row = g.mask->g.nblk; p.zeros = g.mask->g.nrt * g.mask->g.nblk; p.zero_k = g.k; }

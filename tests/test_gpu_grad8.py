@@ -156,7 +156,7 @@ def test_convolutions(batch, height, width, channels, rows, kh, kw, pad, f32):
         conv = B.ConvDesc(batch, height, width, channels, kh, kw, pad, 0)
         d_dy, out = bf16_dev(np.ascontiguousarray(dyb.T), torch), torch.empty_like(dw)
         g = B.WeightGrad8(rows, kh * kw * channels, batch * ho * wo, B.C.pointer(conv), d_dy.data_ptr(), batch * ho * wo, 0, f32, act.buffer.data_ptr(),
-                          L.mask if masked else None, out.data_ptr(), kh * kw * channels, 0, 0, None)
+                          L.mask if masked else None, out.data_ptr(), kh * kw * channels, 0, 0, None, 0)
         B.crisp_weight_grad8(g, torch.empty(B.crisp_weight_grad8_sizes(g), dtype=torch.uint8, device="cuda"))
         check(numbers(out), np.where(mask, want, 0.0), size * mask, batch * ho * wo, f32)
         assert L.gradient_status() == 0
@@ -230,6 +230,24 @@ def test_a_gradient_against_differences():
     slope = (value(w.double() + way.double()) - value(w.double() - way.double())) / 2
     # 39000 products of sums over 200 tokens, each off by 60 2^-23 of sum |g||x| ~ 130: independent, sqrt(39000) * 60 * 1.2e-7 * 130
     assert abs(slope - (dw.double() * way.double()).sum().item()) < 0.2
+
+
+@pytest.mark.parametrize("rows,k,tokens", [(256, 512, 600), (2560, 2048, 600)])
+def test_a_wait_that_runs_out(rows, k, tokens):
+    """Copies that never come: the kernel gives up after the limit, says so and returns; the next call is as ever.  One SM a tile, and pairs."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    x, dy = torch.randn(tokens, k, device="cuda").bfloat16(), torch.randn(tokens, rows, device="cuda").bfloat16()
+    act, dw, status = B.quantize8(x, tokens=True), torch.empty(rows, k, device="cuda"), torch.zeros(1, dtype=torch.int32, device="cuda")
+    g = B.WeightGrad8(rows, k, tokens, None, dy.data_ptr(), rows, 1, 1, act.buffer.data_ptr(), None, dw.data_ptr(), k, 0, 2, status.data_ptr(), 2000000)
+    workspace = torch.empty(B.crisp_weight_grad8_sizes(g), dtype=torch.uint8, device="cuda")
+    B.crisp_weight_grad8(g, workspace)
+    assert status.item() == B.TIMEOUT
+    status.zero_()
+    g.skip_fill, g.wait_limit_cycles = 0, 0
+    B.crisp_weight_grad8(g, workspace)
+    want = dy.double().t() @ act.dequantize(tokens=True).double()
+    assert status.item() == 0 and (dw - want).abs().max().item() <= 1e-4 * want.abs().max().item()
 
 
 def test_streams_and_graphs():

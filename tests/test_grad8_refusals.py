@@ -16,7 +16,7 @@ def lib():
 
 
 def grad(conv=None, **other):
-    d = dict(rows=32, k=64, ncols=100, conv=None, d_dy=4096, ld_dy=32, dy_layout=1, dw_dtype=1, d_act=4096, mask=None, d_dw=4096, ld_dw=64, accumulate=0, reserved=0, d_status=None)
+    d = dict(rows=32, k=64, ncols=100, conv=None, d_dy=4096, ld_dy=32, dy_layout=1, dw_dtype=1, d_act=4096, mask=None, d_dw=4096, ld_dw=64, accumulate=0, skip_fill=0, d_status=None)
     d.update(other)
     g = B.WeightGrad8(**d)
     if conv is not None:
@@ -27,7 +27,7 @@ def grad(conv=None, **other):
 
 @pytest.mark.parametrize("other,code", [
     (dict(rows=0), B.BAD_SHAPE), (dict(k=0), B.BAD_SHAPE), (dict(ncols=0), B.BAD_SHAPE), (dict(ncols=-5), B.BAD_SHAPE), (dict(ncols=1 << 31), B.UNSUPPORTED),
-    (dict(k=1 << 20), B.UNSUPPORTED), (dict(dy_layout=2), B.INVALID_ARG), (dict(dw_dtype=2), B.INVALID_ARG), (dict(accumulate=2), B.INVALID_ARG), (dict(reserved=1), B.INVALID_ARG),
+    (dict(k=1 << 20), B.UNSUPPORTED), (dict(dy_layout=2), B.INVALID_ARG), (dict(dw_dtype=2), B.INVALID_ARG), (dict(accumulate=2), B.INVALID_ARG), (dict(skip_fill=-1), B.INVALID_ARG),
     # 10 x 10 pixels of 64 channels under one tap are what the descriptor says; these are not
     (dict(conv=(1, 10, 10, 32, 1, 1, 0, 0)), B.BAD_SHAPE), (dict(conv=(1, 10, 9, 64, 1, 1, 0, 0)), B.BAD_SHAPE), (dict(conv=(0, 10, 10, 64, 1, 1, 0, 0)), B.BAD_SHAPE),
     (dict(conv=(1, 10, 10, 64, 1, 1, -1, 0)), B.BAD_SHAPE), (dict(conv=(1, 10, 10, 64, 0, 1, 0, 0)), B.BAD_SHAPE), (dict(conv=(1, 2, 2, 16, 2, 2, 0, 0)), B.BAD_SHAPE),
