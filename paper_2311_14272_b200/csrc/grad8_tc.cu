@@ -740,13 +740,15 @@ crisp_status_t plan_grad(const crisp_weight_grad8_t *g, GradPlan *G) {
         p.tiles_row = (int)up(p.boxes, p.per);
         const int64_t tiles = (int64_t)G->nrt * p.tiles_row;
         if (tiles > (1 << 24)) return CRISP_UNSUPPORTED;
-        // parts of the tokens where there are fewer tiles than SMs, of 256 tokens at least
+        // Parts of the tokens where there are fewer tiles than SMs, of 256 tokens at least.  (Half as many parts: 1024 x 1024, 4096 tokens 22.6 us instead of 18.0, 128 x 1152, 25088
+        // tokens 32.4 and 30.7; parts of 512 tokens: 256 x 1024, 512 tokens 12.4 and 10.3; of 128 the same.)
         int64_t splits = std::max<int64_t>(1, std::min<int64_t>(148 / tiles, p.chunks / 4));
         p.chunks_split = (int)up(p.chunks, splits);
         p.splits = (int)up(p.chunks, p.chunks_split);
         p.items = (int)(tiles * p.splits);
-        // pairs where every SM has work all the same
-        G->pair = !p.blk_col && p.splits == 1 && G->nrt >= 2 && up(G->nrt, 2) * p.tiles_row >= 74;
+        // Pairs where a tile is not cut into parts and half of the SMs have one.  Measured, us, one SM a tile and pairs: 64 pairs, 2048 x 2048 and 8192 tokens 61.1 and 57.4; 2304 x 2304
+        // and 2048 tokens 44.3 and 41.2; 4096 x 4096 73.8 and 69.1, and 8192 tokens 245 and 235 (with the loops of that time).
+        G->pair = !p.blk_col && p.splits == 1 && G->nrt >= 2 && tiles >= 74;
         if (G->pair) p.items = (int)(up(G->nrt, 2) * p.tiles_row);
         G->cpitch = up(p.channels, 64) * 64;
         G->x_off = 0;

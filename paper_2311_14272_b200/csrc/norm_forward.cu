@@ -287,7 +287,10 @@ sum_rows_kernel(const float *sums, int64_t rows, int channels, float *dgamma, fl
 bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 constexpr int kSms = 148;
-constexpr int64_t kSmallBytes = 12 << 20;
+// Small calls: those that read at most so much (dy, too).  Device times of one kernel with clusters and of two, us: forward 1 x 28 x 28 x 512 (0.8 MB) 7.4 and 8.3, 8 images (6.4 MB)
+// 7.9 and 12.0, 32 images (25.7 MB) 11.4 and 15.9, 48 images 18.3 and 19.5, 16 x 112 x 112 x 96 (38.5 MB) 34.9 and 22.0; backward 8 x 14 x 14 x 512 (3.2 MB) 9.1 and 12.2, 8 x 28 x 28 x 256
+// (6.4 MB) 11.4 and 13.8, 4 x 56 x 56 x 256 (12.8 MB) 20.2 and 15.6, 24 x 28 x 28 x 512 (38.5 MB) 28.9 and 22.2.
+constexpr int64_t kSmallForward = 28 << 20, kSmallBackward = 8 << 20;
 int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 Plan plan_of(const crisp_group_norm_t &d, bool back, bool from8, bool eight) {
@@ -312,13 +315,19 @@ Plan plan_of(const crisp_group_norm_t &d, bool back, bool from8, bool eight) {
         p.resident = (int)ceil_div(p.per, kThreads / p.cv);
     };
     const auto wanted = [&] { return p.fixed_smem + (size_t)p.resident * kThreads * item; };
-    if (whole && bytes <= kSmallBytes) {
-        int width = unit;
-        while (width < C && width * size < 128 && width + unit <= most) width += unit;
-        slice(width);
-        // enough CTAs, but two items a thread before a slice is cut further
-        rank(std::min<int64_t>(std::min<int64_t>(kMaxCluster, ceil_div(2 * kSms, batch * p.slices)), ceil_div(d.pixels, 2 * (kThreads / p.cv))));
-        while (wanted() > kMaxSmem / 2 && p.ranks < kMaxCluster) rank(std::min(kMaxCluster, p.ranks * 2));
+    if (whole && bytes <= (back ? kSmallBackward : kSmallForward)) {
+        // slices of 128 bytes a pixel and more, where there are CTAs enough, and of about the same width
+        int64_t width = unit;
+        while (width < C && width + unit <= most && (width * size < 128 || (2 * width <= most && batch * ceil_div(C, 2 * width) >= 2 * kSms))) width += unit;
+        const int64_t slices = ceil_div(C, width);
+        width = ceil_div(ceil_div(C, slices), unit) * unit;
+        slice((int)std::min<int64_t>(width, C));
+        // a power of two of CTAs (other clusters leave SMs of a GPC empty), no more in all than run at once, two items a thread before a slice is cut further
+        const int64_t at_once = 2 * kSms / (batch * p.slices), worth = ceil_div(d.pixels, 2 * (kThreads / p.cv));
+        int64_t ranks = 1;
+        while (2 * ranks <= kMaxCluster && 2 * ranks <= at_once && ranks < worth) ranks *= 2;
+        rank(ranks);
+        while (wanted() > kMaxSmem / 2 && p.ranks < kMaxCluster) rank(std::min<int64_t>(kMaxCluster, 2 * (int64_t)p.ranks));
         p.cluster = wanted() <= kMaxSmem && p.ranks <= kMaxCluster;
         p.parts = 1;
     }
