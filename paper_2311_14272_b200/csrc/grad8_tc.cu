@@ -30,7 +30,8 @@ constexpr int kDrain = 8;                                     // warps
 constexpr int kGradThreads = 128 + 32 * kDrain;
 constexpr uint32_t kABytes = 16384, kBoxBytes = 8192, kStage = kABytes + kBoxes * kBoxBytes;
 constexpr int kStages = 4;
-constexpr size_t kGradSmem = kStages * kStage + 256 + 1024;
+constexpr size_t kStaging = kDrain * 32 * 17 * 4;             // (16 columns of a warp's rows, where dW is not written in 16-byte pieces)
+constexpr size_t kGradSmem = kStages * kStage + 256 + kStaging + 1024;
 
 struct Grad {
     int rows, channels, kernel_w, pad, linear;
@@ -68,8 +69,34 @@ __device__ __forceinline__ uint32_t mask_bits(const Grad &p, int row, int col) {
     return __funnelshift_r(i < p.wpr ? w[i] : 0u, i + 1 < p.wpr ? w[i + 1] : 0u, col & 31);
 }
 
-// 16 sums of a row to dW.
-__device__ __forceinline__ void store16(const Grad &p, int row, int col, int n, float (&v)[16]) {
+// 16 sums of each of a warp's 32 rows to dW: in 16-byte pieces by the lanes that have them; or, where they do not lie at multiples of that, through the warp's staging rows, so that
+// a store covers pieces of two rows (4096 x 4095 in fp32, 16 tokens: 45 us; with an element a lane, each in a row of its own, 103).
+constexpr int kStaged = 17;
+__device__ __forceinline__ void store16(const Grad &p, float *stage, int row0, int lane, int col, int n, float (&v)[16]) {
+    if (!(p.vec && n == 16 && (col & (p.f32 ? 3 : 7)) == 0)) {
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 16; ++j) stage[lane * kStaged + j] = v[j];
+        __syncwarp();
+        const int j = lane & 15;
+        for (int r = lane >> 4; r < 32; r += 2) {
+            const int row = row0 + r;
+            if (row >= p.rows || j >= n) continue;
+            float x = stage[r * kStaged + j];
+            if (p.nm_bits && !(p.nm_bits[(int64_t)row * p.wpr + ((col + j) >> 5)] >> ((col + j) & 31) & 1u)) x = 0.f;
+            const int64_t at = (int64_t)row * p.ld + col + j;
+            if (p.f32) {
+                float *to = reinterpret_cast<float *>(p.dw) + at;
+                *to = p.accumulate ? *to + x : x;
+            } else {
+                __nv_bfloat16 *to = reinterpret_cast<__nv_bfloat16 *>(p.dw) + at;
+                *to = __float2bfloat16_rn(p.accumulate ? __bfloat162float(*to) + x : x);
+            }
+        }
+        return;
+    }
+    const int row = row0 + lane;
+    if (row >= p.rows) return;
     if (p.nm_bits) {
         const uint32_t bits = mask_bits(p, row, col);
 #pragma unroll
@@ -79,42 +106,30 @@ __device__ __forceinline__ void store16(const Grad &p, int row, int col, int n, 
     const int64_t at = (int64_t)row * p.ld + col;
     if (p.f32) {
         float *to = reinterpret_cast<float *>(p.dw) + at;
-        if (p.vec && n == 16 && (col & 3) == 0) {
 #pragma unroll
-            for (int j = 0; j < 16; j += 4) {
-                float4 q = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
-                if (p.accumulate) {
-                    const float4 o = *reinterpret_cast<const float4 *>(to + j);
-                    q.x += o.x; q.y += o.y; q.z += o.z; q.w += o.w;
-                }
-                *reinterpret_cast<float4 *>(to + j) = q;
+        for (int j = 0; j < 16; j += 4) {
+            float4 q = make_float4(v[j], v[j + 1], v[j + 2], v[j + 3]);
+            if (p.accumulate) {
+                const float4 o = *reinterpret_cast<const float4 *>(to + j);
+                q.x += o.x; q.y += o.y; q.z += o.z; q.w += o.w;
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (j < n) to[j] = p.accumulate ? to[j] + v[j] : v[j];
+            *reinterpret_cast<float4 *>(to + j) = q;
         }
     } else {
         __nv_bfloat16 *to = reinterpret_cast<__nv_bfloat16 *>(p.dw) + at;
-        if (p.vec && n == 16 && (col & 7) == 0) {
 #pragma unroll
-            for (int j = 0; j < 16; j += 8) {
-                uint4 q = make_uint4(0, 0, 0, 0);
-                if (p.accumulate) q = *reinterpret_cast<const uint4 *>(to + j);
-                const uint32_t o[4] = {q.x, q.y, q.z, q.w};
-                uint32_t r[4];
+        for (int j = 0; j < 16; j += 8) {
+            uint4 q = make_uint4(0, 0, 0, 0);
+            if (p.accumulate) q = *reinterpret_cast<const uint4 *>(to + j);
+            const uint32_t o[4] = {q.x, q.y, q.z, q.w};
+            uint32_t r[4];
 #pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float a = v[j + 2 * i], b = v[j + 2 * i + 1];
-                    if (p.accumulate) { a += __uint_as_float(o[i] << 16); b += __uint_as_float(o[i] & 0xFFFF0000u); }
-                    r[i] = pack_bf16(a, b);
-                }
-                *reinterpret_cast<uint4 *>(to + j) = make_uint4(r[0], r[1], r[2], r[3]);
+            for (int i = 0; i < 4; ++i) {
+                float a = v[j + 2 * i], b = v[j + 2 * i + 1];
+                if (p.accumulate) { a += __uint_as_float(o[i] << 16); b += __uint_as_float(o[i] & 0xFFFF0000u); }
+                r[i] = pack_bf16(a, b);
             }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 16; ++j)
-                if (j < n) to[j] = __float2bfloat16_rn(p.accumulate ? __bfloat162float(to[j]) + v[j] : v[j]);
+            *reinterpret_cast<uint4 *>(to + j) = make_uint4(r[0], r[1], r[2], r[3]);
         }
     }
 }
@@ -129,7 +144,7 @@ __device__ __forceinline__ void tmem_ld_x16(uint32_t taddr, uint32_t (&r)[16]) {
 }
 
 // The first pixel of a chunk.  (The threads that issue copies are bound by their own instructions: they go from chunk to chunk without a division.  4096 x 4096, 8192 tokens,
-// in pairs: 280 us with two of them a chunk.)
+// in pairs: 280 us with two of them a chunk and single threads that issue, 202 with none and whole warps in step.)
 struct Pixels {
     int x, y, z;
     __device__ __forceinline__ Pixels(const Grad &p, int c) {
@@ -177,14 +192,15 @@ __device__ __forceinline__ void add_chain(uint32_t from, int n, int half, float 
         }
     }
 }
-__device__ __forceinline__ void store_sums(const Grad &p, const Walk &w, int rt, int half, int row, float (&sum)[8][16]) {
-    if (row >= p.rows) return;
+// (all lanes of a warp; row0: its first row)
+__device__ __forceinline__ void store_sums(const Grad &p, const Walk &w, float *stage, int rt, int half, int row0, int lane, float (&sum)[8][16]) {
+    if (row0 >= p.rows) return;
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         if (half * 2 + i / 4 >= w.n) continue;
         const BoxAt at = box_at(p, rt, w.first + half * 2 + i / 4);
         const int c = at.c + 16 * (i & 3), here = min(16, p.channels - c);
-        if (here > 0) store16(p, row, at.tap * p.channels + c, here, sum[i]);
+        if (here > 0) store16(p, stage, row0, lane, at.tap * p.channels + c, here, sum[i]);
     }
 }
 
@@ -330,7 +346,7 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 #pragma unroll
                         for (int j = 0; j < 16; ++j) to[(16 * i + j) * 128] = sum[i][j];
             } else {
-                store_sums(p, w, w.rt, half, w.rt * 128 + 32 * q + lane, sum);
+                store_sums(p, w, reinterpret_cast<float *>(ctrl_gen + 256) + (warp - 4) * 32 * kStaged, w.rt, half, w.rt * 128 + 32 * q, lane, sum);
             }
         }
     } else {
@@ -379,15 +395,15 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
 // ------------------------------------------------------------------------------------------------ pairs of SMs
 //
 // Two CTAs (a cluster) multiply 256 rows by 256 columns with cta_group::2: each fetches its 128 rows of dY and two of the four boxes of x, and the tensor cores of both read both
-// halves.  A CTA by itself is bound by what comes in from L2 (48 KB a chunk, some 11 TB/s in all); of a pair each fetches 32.  Not under a mask of blocks, where every row tile has
-// boxes of its own.
+// halves: 32 KB a chunk into each instead of 48, and half as many instructions issued (4 to 6 % of the time, see where pairs are chosen).  Not under a mask of blocks, where every row
+// tile has boxes of its own.
 //
 // The CTA of rank 0 issues for both.  The copies of both complete on its barriers, which count the bytes of both (what has landed in the peer's shared memory is acquired at the scope of the
 // cluster); commits go to both (multicast); accumulators are handed back by the adding warps of both.  These two are seen at the scope of the cluster, relaxed: what tcgen05
 // instructions read and write is ordered by their commits and fences, and nothing else is handed over.
 constexpr uint32_t kPairStage = kABytes + kBoxes / 2 * kBoxBytes;
 constexpr int kPairStages = 6;
-constexpr size_t kPairSmem = kPairStages * kPairStage + 256 + 1024;
+constexpr size_t kPairSmem = kPairStages * kPairStage + 256 + kStaging + 1024;
 
 __device__ __forceinline__ void mma_dense_pair(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t acc) {
     asm volatile(
@@ -547,7 +563,7 @@ grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                 if (++acc == 2) { acc = 0; acc_ph ^= 1u; }
             }
             if (!go) break;
-            store_sums(p, w, w.rt, half, (2 * w.rt + (int)rank) * 128 + 32 * q + lane, sum);
+            store_sums(p, w, reinterpret_cast<float *>(ctrl_gen + 256) + (warp - 4) * 32 * kStaged, w.rt, half, (2 * w.rt + (int)rank) * 128 + 32 * q, lane, sum);
         }
     }
     __syncwarp();

@@ -109,7 +109,7 @@ struct Reader {
     const T *x, *dy;
     int64_t step_x, step_dy;
     // Where a thread keeps an item's codes: in the order that they have in memory (swizzled by the column) where its block's threads are all there, so that a copy of half a warp goes
-    // to one line as it comes from one (else 53 wavefronts an item, not 14: backward of 56 x 56 x 256 from 8 bits, 32 images, 58 us).
+    // to one line as it comes from one (else 53 wavefronts an item, not 14; the time of 56 x 56 x 256 from 8 bits, 32 images, is 58 us either way, bound by instructions).
     __device__ __forceinline__ int place(int64_t col) const {
         const int c = me.ch & 127;
         return q.whole8 ? (int)(threadIdx.x & ~(128 / V - 1)) * V + ((((c >> 4) ^ (int)col) & 7) << 4) + (c & 15) : (int)threadIdx.x * V;
@@ -250,7 +250,7 @@ __device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const 
 #pragma unroll
             for (int j = 0; j < P; ++j) d[j] = fma2(d[j], k.a[j], fma2(x[j], B[kOne ? 0 : j], C[kOne ? 0 : j]));
             items.done();
-            put<kVec>(dx, Of<T>::close(d), q.vec_out, me.n, q.stream);
+            put<kVec>(dx, Of<T>::close(d), q.vec_out, me.n);
         }
     });
 }

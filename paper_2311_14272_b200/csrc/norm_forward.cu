@@ -179,7 +179,7 @@ __device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, I &it
             for (int j = 0; j < P; ++j) f[j] = activate<decltype(act)::value, T>(fma2(f[j], a[j], b[j]));      // (0 behind the last channel: a = b = 0)
             if constexpr (kHold) if (q.y8) hold<V>(q, q.y8, f, col, me.ch);
             items.done();
-            if (!kHold || (q.out && me.n > 0)) put<kVec && !kHold>(y, Of<T>::close(f), q.vec_out, me.n, q.stream);
+            if (!kHold || (q.out && me.n > 0)) put<kVec && !kHold>(y, Of<T>::close(f), q.vec_out, me.n);
             y += move;
             col += kDown ? -q.lanes : q.lanes;
         }
@@ -395,7 +395,6 @@ Norm norm_of(const crisp_group_norm_t &d, const Plan &p, const Space &s, void *w
     q.resident = p.resident;
     q.whole8 = d.channels % 128 == 0 && p.width % 128 == 0;
     if (q.cpg > 1 && (double)d.channels * q.cpg < 4294967296.0) q.cpg_magic = (uint32_t)((((uint64_t)1 << 32) + q.cpg - 1) / q.cpg);
-    q.stream = !p.cluster && (double)d.batch * d.pixels * d.channels * (d.dtype == 1 ? 4 : 2) > 64e6;
     q.act = d.activation;
     q.eps = (float)d.eps;
     const Act8 a = act8(d.channels, d.batch * d.pixels);
