@@ -204,6 +204,21 @@ __device__ __forceinline__ void store_sums(const Grad &p, const Walk &w, float *
     }
 }
 
+// Zeros in `bytes` of each row (512 at most), by a warp, wherever they begin: 16 bytes a lane, and elements up to the first multiple of 16 and from the last one on.
+// (An element a lane, in a loop: 330 cycles a row of 128 in bf16.)
+__device__ __forceinline__ void zero_rows(uint8_t *to, int64_t pitch, int rows, int bytes, int size, int lane) {
+#pragma unroll 4
+    for (int r = 0; r < rows; ++r, to += pitch) {
+        const int up = -(int)reinterpret_cast<uintptr_t>(to) & 15, down = bytes - ((int)reinterpret_cast<uintptr_t>(to + bytes) & 15);
+        const int piece = up + lane * 16, one = lane < 8 ? lane * size : down + (lane - 16) * size;
+        if (piece + 16 <= bytes) *reinterpret_cast<uint4 *>(to + piece) = make_uint4(0, 0, 0, 0);
+        if (one < bytes && (lane < 8 ? one < up : lane >= 16 && one >= up)) {
+            if (size == 4) *reinterpret_cast<uint32_t *>(to + one) = 0;
+            else *reinterpret_cast<uint16_t *>(to + one) = 0;
+        }
+    }
+}
+
 template <bool kAMn>
 __global__ void __launch_bounds__(kGradThreads, 1)
 grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Grad p) {
@@ -358,21 +373,16 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
             bool kept = false;
             for (int i = lane; i < p.kkeep; i += 32) kept |= p.blk_col[(int64_t)rt * p.kkeep + i] == kb;
             if (__any_sync(0xFFFFFFFFu, kept)) continue;
-            const int bytes = min(128, p.zero_k - kb * 128) * size, each = p.vec && bytes % 16 == 0 ? 16 : size, across = bytes / each;
+            const int bytes = min(128, p.zero_k - kb * 128) * size, across = p.vec && bytes % 16 == 0 ? bytes / 16 : 0;
             uint8_t *to = reinterpret_cast<uint8_t *>(p.dw) + ((int64_t)row0 * p.ld + kb * 128) * size;
             const int64_t pitch = p.ld * size;
-            if (each == 16 && (across & (across - 1)) == 0) {
+            if (across && (across & (across - 1)) == 0) {
                 const int at_once = 32 / across, first = lane / across;
                 to += first * pitch + (lane & (across - 1)) * 16;
 #pragma unroll 8
                 for (int r = first; r < rows; r += at_once, to += at_once * pitch) *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
             } else {
-                for (int r = 0; r < rows; ++r, to += pitch)
-                    for (int c = lane; c < across; c += 32) {
-                        if (each == 16) *reinterpret_cast<uint4 *>(to + c * 16) = make_uint4(0, 0, 0, 0);
-                        else if (each == 4) *reinterpret_cast<float *>(to + c * 4) = 0.f;
-                        else *reinterpret_cast<uint16_t *>(to + c * 2) = 0;
-                    }
+                zero_rows(to, pitch, rows, bytes, size, lane);
             }
         }
     }
@@ -794,7 +804,7 @@ cudaError_t launch_grad(const CUtensorMap &a, const CUtensorMap &b, const Grad &
         if (e != cudaSuccess) return e;
         if (device < 64) ready.fetch_or(1ull << device, std::memory_order_relaxed);
     }
-    return launch_clusters(kernel, cluster * (unsigned)std::min(p.items, sms / (int)cluster), kGradThreads, smem, st, cluster, a, b, p);
+    return launch_clusters(kernel, cluster * (unsigned)std::min(std::max(p.items, 4 * p.zeros), sms / (int)cluster), kGradThreads, smem, st, cluster, a, b, p);
 }
 
 cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cudaStream_t st) {
