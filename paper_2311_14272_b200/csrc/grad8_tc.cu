@@ -44,7 +44,7 @@ struct Grad {
     int kkeep;
     const uint32_t *nm_bits;                                  // a mask, or nullptr
     int wpr;
-    int zero_row, zeros, zero_k;                              // blocks a row tile and in all that are to be looked at for zeros (0: none), columns of dW
+    int zero_row, zeros, zero_k, zero_warps;                              // blocks a row tile and in all that are to be looked at for zeros (0: none), columns of dW
     void *dw;
     int64_t ld;
     int f32, accumulate, vec;
@@ -73,17 +73,24 @@ __device__ __forceinline__ uint32_t mask_bits(const Grad &p, int row, int col) {
 // a store covers pieces of two rows (4096 x 4095 in fp32, 16 tokens: 45 us; with an element a lane, each in a row of its own, 103).
 constexpr int kStaged = 17;
 __device__ __forceinline__ void store16(const Grad &p, float *stage, int row0, int lane, int col, int n, float (&v)[16]) {
+    const int row = row0 + lane;
+    if (p.nm_bits && row < p.rows) {
+        const uint32_t bits = mask_bits(p, row, col);
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+            if (!(bits >> j & 1u)) v[j] = 0.f;                // (a choice: what is not finite is gone, too)
+    }
     if (!(p.vec && n == 16 && (col & (p.f32 ? 3 : 7)) == 0)) {
         __syncwarp();
 #pragma unroll
         for (int j = 0; j < 16; ++j) stage[lane * kStaged + j] = v[j];
         __syncwarp();
         const int j = lane & 15;
+#pragma unroll 8
         for (int r = lane >> 4; r < 32; r += 2) {
             const int row = row0 + r;
             if (row >= p.rows || j >= n) continue;
-            float x = stage[r * kStaged + j];
-            if (p.nm_bits && !(p.nm_bits[(int64_t)row * p.wpr + ((col + j) >> 5)] >> ((col + j) & 31) & 1u)) x = 0.f;
+            const float x = stage[r * kStaged + j];
             const int64_t at = (int64_t)row * p.ld + col + j;
             if (p.f32) {
                 float *to = reinterpret_cast<float *>(p.dw) + at;
@@ -95,14 +102,7 @@ __device__ __forceinline__ void store16(const Grad &p, float *stage, int row0, i
         }
         return;
     }
-    const int row = row0 + lane;
     if (row >= p.rows) return;
-    if (p.nm_bits) {
-        const uint32_t bits = mask_bits(p, row, col);
-#pragma unroll
-        for (int j = 0; j < 16; ++j)
-            if (!(bits >> j & 1u)) v[j] = 0.f;                // (a choice: what is not finite is gone, too)
-    }
     const int64_t at = (int64_t)row * p.ld + col;
     if (p.f32) {
         float *to = reinterpret_cast<float *>(p.dw) + at;
@@ -219,6 +219,29 @@ __device__ __forceinline__ void zero_rows(uint8_t *to, int64_t pitch, int rows, 
     }
 }
 
+// Zeros in the blocks that are not kept, by `zero_warps` warps of every CTA.
+__device__ __forceinline__ void zero_dropped(const Grad &p, int warp, int lane) {
+            const int size = p.f32 ? 4 : 2;
+            for (int u = blockIdx.x + gridDim.x * warp; u < 4 * p.zeros; u += gridDim.x * p.zero_warps) {
+                // (32 rows of a block)
+                const int block = u >> 2, rt = block / p.zero_row, kb = block - rt * p.zero_row, row0 = rt * 128 + 32 * (u & 3), rows = min(32, p.rows - row0);
+                bool kept = false;
+                for (int i = lane; i < p.kkeep; i += 32) kept |= p.blk_col[(int64_t)rt * p.kkeep + i] == kb;
+                if (__any_sync(0xFFFFFFFFu, kept)) continue;
+                const int bytes = min(128, p.zero_k - kb * 128) * size, across = p.vec && bytes % 16 == 0 ? bytes / 16 : 0;
+                uint8_t *to = reinterpret_cast<uint8_t *>(p.dw) + ((int64_t)row0 * p.ld + kb * 128) * size;
+                const int64_t pitch = p.ld * size;
+                if (across && (across & (across - 1)) == 0) {
+                    const int at_once = 32 / across, first = lane / across;
+                    to += first * pitch + (lane & (across - 1)) * 16;
+    #pragma unroll 8
+                    for (int r = first; r < rows; r += at_once, to += at_once * pitch) *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
+                } else {
+                    zero_rows(to, pitch, rows, bytes, size, lane);
+                }
+            }
+}
+
 template <bool kAMn>
 __global__ void __launch_bounds__(kGradThreads, 1)
 grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Grad p) {
@@ -332,6 +355,7 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     } else if (warp >= 4) {
         // ------------------------------------------------------------------ sums
         const int q = warp & 3, half = (warp - 4) >> 2;       // a warp may read the lanes of its quarter only
+        if (p.zero_warps > 1) zero_dropped(p, warp - 3, lane);
         uint32_t acc = 0, acc_ph = 0;
         Walk w;
         for (w.enter(p, blockIdx.x); !w.over(p); w.enter(p, w.item + gridDim.x)) {
@@ -366,25 +390,7 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         }
     } else {
         // -------------------------------------------------------------- zeros of blocks that are not kept
-        const int size = p.f32 ? 4 : 2;
-        for (int u = blockIdx.x; u < 4 * p.zeros; u += gridDim.x) {
-            // (32 rows of a block)
-            const int block = u >> 2, rt = block / p.zero_row, kb = block - rt * p.zero_row, row0 = rt * 128 + 32 * (u & 3), rows = min(32, p.rows - row0);
-            bool kept = false;
-            for (int i = lane; i < p.kkeep; i += 32) kept |= p.blk_col[(int64_t)rt * p.kkeep + i] == kb;
-            if (__any_sync(0xFFFFFFFFu, kept)) continue;
-            const int bytes = min(128, p.zero_k - kb * 128) * size, across = p.vec && bytes % 16 == 0 ? bytes / 16 : 0;
-            uint8_t *to = reinterpret_cast<uint8_t *>(p.dw) + ((int64_t)row0 * p.ld + kb * 128) * size;
-            const int64_t pitch = p.ld * size;
-            if (across && (across & (across - 1)) == 0) {
-                const int at_once = 32 / across, first = lane / across;
-                to += first * pitch + (lane & (across - 1)) * 16;
-#pragma unroll 8
-                for (int r = first; r < rows; r += at_once, to += at_once * pitch) *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
-            } else {
-                zero_rows(to, pitch, rows, bytes, size, lane);
-            }
-        }
+        zero_dropped(p, 0, lane);
     }
     __syncwarp();
     tc_fence_before();
@@ -817,7 +823,9 @@ cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cu
     p.skip_fill = g.skip_fill - 1;
     if (p.boxes == 0)
         return g.accumulate ? cudaSuccess : launch_chained(zero_kernel, (unsigned)std::min(g.rows, 4096), 256, 0, st, (int64_t)g.rows, (int)g.k, g.d_dw, g.ld_dw, (int)g.dw_dtype);
-    if (G.blocks && !g.accumulate) { p.zero_row = g.mask->g.nblk; p.zeros = g.mask->g.nrt * g.mask->g.nblk; p.zero_k = g.k; }
+    // Few tokens: the adding warps write zeros, too, before there is anything to add.  (2303 x 3301 in fp32, a quarter of the blocks kept, 9 tokens: 88 us with one warp of a CTA and the
+    // mask looked up for each element that is stored, 33 with nine and a look-up for a row's 16.)  Where there is much to multiply one warp is enough, and the others stay out of its way.
+    if (G.blocks && !g.accumulate) { p.zero_warps = p.chunks_split <= 2 * kChain ? 1 + kDrain : 1; p.zero_row = g.mask->g.nblk; p.zeros = g.mask->g.nrt * g.mask->g.nblk; p.zero_k = g.k; }
     int device = 0;
     e = cudaGetDevice(&device);
     if (e != cudaSuccess) return e;
