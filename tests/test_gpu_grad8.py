@@ -186,6 +186,26 @@ def test_tiles_for_every_sm(rows, k, tokens, by_token):
     assert L.gradient_status() == 0
 
 
+@pytest.mark.parametrize("rows,k,tokens,keep", [(2600, 2048, 1100, 0.5), (2600, 2049, 1100, 0.5), (739, 1739, 2, 0.17)])
+@pytest.mark.parametrize("f32", [0, 1])
+def test_zeros_of_many_blocks(rows, k, tokens, keep, f32):
+    """Blocks that are not kept, beside long products and short ones, in rows that begin anywhere."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    L, mask = layer(B, torch, rows, k, 4, 4, 128, keep, 2)
+    xb, dyb = inputs(np.random.default_rng(rows + k), tokens, rows, k)
+    x, dy = held.activations(values_of(xb).T).T, values_of(dyb)
+    act = B.quantize8(bf16_dev(xb, torch), tokens=True)
+    want, size = np.where(mask, dy.T @ x, 0.0), np.abs(dy).T @ np.abs(x) * mask
+    for pitch, odd in ((0, 0), (5, 3)):
+        dw, whole = padded(torch, np.full((rows, k), 0x4040, np.uint16), pitch, odd, torch.float32 if f32 else torch.bfloat16)
+        L.weight_gradient8(bf16_dev(dyb, torch), act, dw=dw, dw_dtype=f32, tokens=True, masked=True)
+        check(numbers(dw), want, size, tokens, f32)
+        assert np.all(numbers(dw)[~mask] == 0.0)
+        assert bool((whole[odd:].view(rows, k + pitch)[:, k:] == 7.0).all() and (whole[:odd] == 7.0).all())
+    assert L.gradient_status() == 0
+
+
 def test_convolution_tiles_for_every_sm():
     import torch
     from paper_2311_14272_b200 import binding as B
