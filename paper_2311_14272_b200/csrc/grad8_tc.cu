@@ -35,7 +35,7 @@ constexpr size_t kGradSmem = kStages * kStage + 256 + kStaging + 1024;
 
 struct Grad {
     int rows, channels, kernel_w, pad, linear;
-    int cboxes;                                               // boxes of a tap's channels
+    int cboxes;                                               // boxes of a tap's channels (one tap under a list: of its blocks, whose last box may lie behind the last channel)
     int per, tiles_row, boxes, splits, items;                 // boxes a tile, tiles a row tile, boxes a row tile
     int tw, th, tb, nx, ny;                                   // pixels of a stage; boxes of them along a line, lines along an image
     int wo, ho;                                               // of dY (a linear layer: one line of tokens)
@@ -761,7 +761,10 @@ crisp_status_t plan_grad(const crisp_weight_grad8_t *g, GradPlan *G) {
         if (m.rows != g->rows || m.k != g->k) return CRISP_BAD_SHAPE;
         p.nm_bits = g->mask->d_nm_bits; p.wpr = m.wpr;
         G->blocks = m.bm == 128 && m.bk == 128 && (taps == 1 || p.channels % 128 == 0);
-        if (G->blocks && m.kkeep < m.nblk) { p.blk_col = g->mask->d_blk_col; p.kkeep = m.kkeep; p.boxes = 2 * m.kkeep; }
+        if (G->blocks && m.kkeep < m.nblk) {
+            p.blk_col = g->mask->d_blk_col; p.kkeep = m.kkeep; p.boxes = 2 * m.kkeep;
+            if (taps == 1) p.cboxes = 2 * m.nblk;             // (with 192 channels the fourth box is none of a second tap: it is copied as zeros and not stored)
+        }
         else G->blocks = false;
     }
     size_t at = 0;

@@ -347,3 +347,40 @@ def test_a_step_of_fine_tuning():
     for w, old, m, d in zip(weights, before, mask, (dw_conv, dw_head)):
         m = m.cuda()
         assert torch.all(w[~m] == 0) and torch.all((w != old)[m & (d != 0)])
+
+
+@pytest.mark.parametrize("channels", [160, 192, 320, 448, 960])
+@pytest.mark.parametrize("batch,height,width,rows,pad", [(1, 7, 7, 130, 0), (2, 5, 6, 64, 1), (8, 28, 28, 128, 0), (1, 4, 5, 9700, 0)])
+@pytest.mark.parametrize("f32", [0, 1])
+def test_one_tap_whose_last_block_is_not_whole(channels, batch, height, width, rows, pad, f32):
+    """1 x 1 convolutions under a list of blocks, the last of which ends within its first or second 64 columns: nothing behind the last column, of parts of the pixels and of all at once."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    rng = np.random.default_rng(channels)
+    L = B.HybridLayer(rows, channels, 2, 4, 128, 128, 0.5)
+    assert L.kkeep < L.nblk
+    liking = rng.random((rows, channels)).astype(np.float32)
+    liking[:, channels // 128 * 128:] *= 100                                  # (the last block is kept by every row tile)
+    L.build_mask(to_dev(liking, torch))
+    mask = np.unpackbits(L.export_mask()[1].view(np.uint8), axis=1, bitorder="little")[:rows, :channels].astype(bool)
+    assert mask[:, channels // 128 * 128:].any(1).all()
+    xb, _ = inputs(rng, batch * height * width, 1, channels)
+    x = held.activations(values_of(xb).T).T.reshape(batch, height, width, channels)
+    low, ho, wo = lowered(x, 1, 1, pad)
+    tokens = batch * ho * wo
+    _, dyb = inputs(rng, tokens, rows, 1)
+    dy = values_of(dyb)
+    act, d_dy = B.quantize8(bf16_dev(xb, torch), tokens=True), bf16_dev(dyb, torch).view(batch, ho, wo, rows)
+    want, size = np.where(mask, dy.T @ low, 0.0), np.abs(dy).T @ np.abs(low) * mask
+    for pitch, odd in ((0, 0), (8, 0), (3, 1)):
+        whole = torch.full((odd + (rows + 64) * (channels + pitch),), 7.0, dtype=torch.float32 if f32 else torch.bfloat16, device="cuda")
+        dw, behind = whole[odd:].view(rows + 64, channels + pitch)[:rows, :channels], whole[odd:].view(rows + 64, channels + pitch)
+        L.weight_gradient8_conv(d_dy, act, 1, 1, pad, dw=dw, dw_dtype=f32, masked=True)
+        check(numbers(dw), want, size, tokens, f32)
+        assert bool((behind[rows:] == 7.0).all() and (behind[:, channels:] == 7.0).all() and (whole[:odd] == 7.0).all())
+        dw.fill_(3.0)
+        L.weight_gradient8_conv(d_dy, act, 1, 1, pad, dw=dw, dw_dtype=f32, masked=True, accumulate=True)
+        check(numbers(dw), want, size, tokens, f32, np.full(dw.shape, 3.0))
+        assert np.all(numbers(dw)[~mask] == 3.0)
+        assert bool((behind[rows:] == 7.0).all() and (behind[:, channels:] == 7.0).all() and (whole[:odd] == 7.0).all())
+    assert L.gradient_status() == 0
