@@ -59,7 +59,7 @@ struct Norm {
     int some, more, some_last, more_last;    // items of a pixel lane: `some`, the first `more` lanes one more (the last rank's: ..._last)
     int resident;                        // items (V channels of a pixel) that a thread keeps
     uint32_t across_magic, cpg_magic;    // 2^32 / (entries of a whole group and lane), / cpg, rounded up (0: not exact for all channels)
-    int whole8;                          // slices are whole blocks of 128 channels
+    int as_stored;                       // backward from 8 bits: codes keep their order on the way (slices of whole blocks of 128 channels, an order for each place of the ring)
     int act, vec, vec_dy, vec_out;       // vec: addresses and pitches allow 16 bytes at once
     float eps;
 };

@@ -109,10 +109,11 @@ struct Reader {
     const T *x, *dy;
     int64_t step_x, step_dy;
     // Where a thread keeps an item's codes: in the order that they have in memory (swizzled by the column) where its block's threads are all there, so that a copy of half a warp goes
-    // to one line as it comes from one (else 53 wavefronts an item, not 14; the time of 56 x 56 x 256 from 8 bits, 32 images, is 58 us either way, bound by instructions).
+    // to one line as it comes from one (else 53 wavefronts an item, not 14; the time of 56 x 56 x 256 from 8 bits, 32 images, is 58 us either way).  The items that come to
+    // one place of the ring lie a multiple of eight columns apart then, so that the bytes are the thread's own there.
     __device__ __forceinline__ int place(int64_t col) const {
         const int c = me.ch & 127;
-        return q.whole8 ? (int)(threadIdx.x & ~(128 / V - 1)) * V + ((((c >> 4) ^ (int)col) & 7) << 4) + (c & 15) : (int)threadIdx.x * V;
+        return q.as_stored ? (int)(threadIdx.x & ~(128 / V - 1)) * V + ((((c >> 4) ^ (int)col) & 7) << 4) + (c & 15) : (int)threadIdx.x * V;
     }
     __device__ __forceinline__ Reader(const Norm &q_, const Mine<T> &me_)
         : q(q_), me(me_), x(reinterpret_cast<const T *>(q_.x) + me_.row0 * q_.ldx + me_.ch), dy(reinterpret_cast<const T *>(q_.dy) + me_.row0 * q_.ld_dy + me_.ch),

@@ -393,7 +393,8 @@ Norm norm_of(const crisp_group_norm_t &d, const Plan &p, const Space &s, void *w
     const int last = q.pixels - (p.ranks - 1) * p.per;
     q.some = p.per / q.lanes; q.more = p.per % q.lanes; q.some_last = last / q.lanes; q.more_last = last % q.lanes;
     q.resident = p.resident;
-    q.whole8 = d.channels % 128 == 0 && p.width % 128 == 0;
+    // (an odd number of pixel lanes would have a place of the ring change its order, and a thread write where a neighbour has yet to read)
+    q.as_stored = d.channels % 128 == 0 && p.width % 128 == 0 && kDeepDy * q.lanes % 8 == 0;
     if (q.cpg > 1 && (double)d.channels * q.cpg < 4294967296.0) q.cpg_magic = (uint32_t)((((uint64_t)1 << 32) + q.cpg - 1) / q.cpg);
     q.act = d.activation;
     q.eps = (float)d.eps;

@@ -309,3 +309,31 @@ def test_pixels_beyond_32_bits():
     del alone
     dx, dg, db = norm.backward(done.y, x, done.statistics)
     assert near(dx[-1:], norm.backward(done.y[-1:], x[-1:], done.statistics[-1:])[0])
+
+
+@pytest.mark.parametrize("size", [(2, 4000, 384, 6), (1, 5000, 640, 40), (1, 1600, 2048, 32), (3, 1100, 896, 7), (2, 9001, 128, 16)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_large_backward_passes_from_8_bits(size, dtype):
+    """Two kernels, whose threads share the places that codes are fetched to; odd and even numbers of pixels at a time.  With statistics and parameters that put values on the borders, so
+    that some threads of a block take another way than the others."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    batch, pixels, channels, groups = size
+    T = kind(torch, dtype)
+    rng = np.random.default_rng(channels)
+    values = held_rows(np.round(rng.standard_normal((batch * pixels, channels)) * 2) / 2)           # (multiples of 1/2: exact in 8 bits)
+    d_x = cuda(torch, np.ascontiguousarray(values).reshape(batch, pixels, channels)).to(T)
+    x = numbers(d_x)
+    dy = cuda(torch, rng.standard_normal(x.shape)).to(T)
+    gamma, beta = rng.choice([1.0, 2.0, 3.0, 0.5], channels).astype(np.float32), rng.choice([0.0, 1.0, -0.5, 3.0, 5.0], channels).astype(np.float32)
+    stats = np.stack([np.zeros((batch, groups)), np.ones((batch, groups))], 2).astype(np.float32)
+    given = B.quantize8(d_x.bfloat16().view(-1, channels), tokens=True)
+    assert np.array_equal(numbers(given.dequantize(tokens=True)).reshape(x.shape), x)
+    for act in ("relu", "relu6", "silu"):
+        norm = B.GroupNorm(channels, groups, cuda(torch, gamma), cuda(torch, beta), activation=act)
+        got = norm.backward(dy, given, cuda(torch, stats))
+        want = ref.backward(numbers(dy), x, stats[..., 0].astype(np.float64), stats[..., 1].astype(np.float64), groups, gamma.astype(np.float64), beta.astype(np.float64), act, dtype == "fp32")
+        check(numbers(got[0]), want[0], want[3], T, torch)
+        check(numbers(got[1]), want[1], want[4], torch.float32, torch)
+        check(numbers(got[2]), want[2], want[5], torch.float32, torch)
+        assert all(torch.equal(a, b) for a, b in zip(got, norm.backward(dy, given, cuda(torch, stats))))
