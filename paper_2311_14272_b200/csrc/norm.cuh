@@ -12,8 +12,8 @@
 //                 is still in L2 (forward, us, backwards and not: 32 x 112 x 112 x 96, 77 MB, 38 and 42; of 50 MB 25 and 24; of 200 MB 115 and 116)
 //
 // A thread holds V = 16 bytes' worth of consecutive channels and goes over pixels, two channels an instruction: per pair p = a x + b (a = gamma rstd, b = beta - mean a),
-// dx = a e + B x + C.  Forward sums are about the thread's first value, so that a mean far from zero costs no digits; then mean = sum n_i mean_i / n and
-// M2 = sum M2_i + n_i (mean_i - mean)^2 over threads and over CTAs, always in the same order.
+// dx = a e + B x + C.  Forward sums are about the thread's first value, and then about its mean so far, so that neither a mean far from zero nor single
+// values far from the mean cost digits; then mean = sum n_i mean_i / n and M2 = sum M2_i + n_i (mean_i - mean)^2 over threads and over CTAs, always in the same order.
 #pragma once
 
 #include <cuda_bf16.h>

@@ -337,3 +337,40 @@ def test_large_backward_passes_from_8_bits(size, dtype):
         check(numbers(got[1]), want[1], want[4], torch.float32, torch)
         check(numbers(got[2]), want[2], want[5], torch.float32, torch)
         assert all(torch.equal(a, b) for a, b in zip(got, norm.backward(dy, given, cuda(torch, stats))))
+
+
+# batch, pixels, channels, groups: a thread's channels of one group, and of several; one kernel and two
+@pytest.mark.parametrize("size", [(2, 300000, 64, 8), (2, 300000, 64, 32), (9, 50000, 48, 16), (1, 50176, 64, 8), (3, 9000, 20, 4)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_the_variance_behind_outliers(size, dtype):
+    """Values far from the others where threads begin, wherever else, one and several of them; a border of zeros, and values about 100.  The variance is the formula's all the same."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    batch, pixels, channels, groups = size
+    T, each = kind(torch, dtype), channels // groups
+    rng = np.random.default_rng(pixels)
+    x = rng.standard_normal((batch, pixels, channels)).astype(np.float32)
+    far = [100, 300, 1000, 3000, -1000, 30000]
+    for b in range(batch):
+        for g in range(groups):
+            at = x[b, :, g * each:(g + 1) * each]
+            what = (b * groups + g) % 8
+            if what < 6:
+                at[0, 0] = far[what]
+            elif what == 6:
+                at[:3] = 1000 / (1 + np.arange(3)[:, None])                   # several, one behind the other
+            else:
+                at += 100
+                at[:pixels // 50] = 0
+            if g % 3 == 1:
+                at[rng.integers(0, pixels, 5), rng.integers(0, each, 5)] = 700
+    d_x = torch.from_numpy(x).to("cuda", T)
+    norm = B.GroupNorm(channels, groups, eps=0.0)
+    got = numbers(norm.forward(d_x).statistics)
+    for b in range(batch):
+        v = numbers(d_x[b]).reshape(pixels, groups, each)
+        mean = v.mean((0, 2))
+        rstd = 1 / np.sqrt(((v - mean[None, :, None])**2).mean((0, 2)))
+        off = np.abs(v - mean[None, :, None]).max((0, 2))
+        assert np.all(np.abs(got[b, :, 0] - mean) <= ref.U * (16 * off + 4 * np.abs(mean)))
+        assert np.all(np.abs(got[b, :, 1] / rstd - 1) <= 48 * ref.U), (np.abs(got[b, :, 1] / rstd - 1) / ref.U).max()
