@@ -538,7 +538,8 @@ CRISP_API crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_
  *   h = (x - mean) * rstd,  rstd = 1 / sqrt(var + eps)        y = act(p),  p = gamma * h + beta      (per channel)
  *   e = dy * act'(p)     dbeta = sum e     dgamma = sum e * h     dx = rstd * (gamma * e - m1 - h * m2),   m1, m2: the group's means of gamma * e and gamma * e * h
  *
- *   batch, pixels, channels   x, y, dy, dx are [batch * pixels, channels], channels consecutive, a pixel every ld.. >= channels elements
+ *   batch, pixels, channels   x, y, dy, dx are [batch * pixels, channels], channels consecutive, a pixel every ld.. >= channels elements; batch below 2^31, pixels (of a sample) to
+ *                             2^31 - 65537, more are UNSUPPORTED
  *   activation                0 none, 1 max(p, 0), 2 min(max(p, 0), 6), 3 p / (1 + exp(-p)); the slope on a border is 0
  *   dtype                     of x, y, dy, dx: 0 bf16, 1 fp32, 2 fp16.  Sums and statistics are fp32, y and dx are rounded once
  *   d_gamma, d_beta           [channels] fp32, or NULL: 1 and 0

@@ -393,7 +393,7 @@ Space space_of(const crisp_group_norm_t &d, const Plan &p, bool back) {
 crisp_status_t check(const crisp_group_norm_t *d) {
     if (!d || d->activation < 0 || d->activation > 3 || d->dtype < 0 || d->dtype > 2 || !(d->eps >= 0.0) || !std::isfinite(d->eps)) return CRISP_INVALID_ARG;
     if (d->batch < 0 || d->pixels <= 0 || d->channels <= 0 || d->groups <= 0 || d->channels % d->groups) return CRISP_BAD_SHAPE;
-    if (d->pixels > 0x7FFFFFFFll - 65536 || d->batch > 0x7FFFFFFFll / 65536 || d->channels > kMaxBlocksPerRowTile * 128 ||
+    if (d->pixels > 0x7FFFFFFFll - 65536 || d->batch > 0x7FFFFFFFll || d->channels > kMaxBlocksPerRowTile * 128 ||
         (double)d->batch * (double)d->pixels * (double)d->channels > 0x1p44)
         return CRISP_UNSUPPORTED;
     return CRISP_OK;

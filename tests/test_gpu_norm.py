@@ -374,3 +374,27 @@ def test_the_variance_behind_outliers(size, dtype):
         off = np.abs(v - mean[None, :, None]).max((0, 2))
         assert np.all(np.abs(got[b, :, 0] - mean) <= ref.U * (16 * off + 4 * np.abs(mean)))
         assert np.all(np.abs(got[b, :, 1] / rstd - 1) <= 48 * ref.U), (np.abs(got[b, :, 1] / rstd - 1) / ref.U).max()
+
+
+@pytest.mark.parametrize("shape,groups", [((40000, 64), 8), ((32768, 2, 24), 3), ((70000, 128), 4), ((66000, 3, 8), 8)])
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_many_samples(shape, groups, dtype):
+    """More samples than 32767, of a row or a few pixels each, from x as it is and from its 8-bit form."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    channels = shape[-1]
+    size = (shape[0], int(np.prod(shape[1:-1], dtype=int)), channels, groups)
+    x, gamma, beta, dy = inputs(torch, *size, seed=3)
+    d_x, d_dy = (cuda(torch, a).to(kind(torch, dtype)).view(shape) for a in (x, dy))
+    x, dy = (numbers(t).reshape(size[:3]) for t in (d_x, d_dy))
+    norm = B.GroupNorm(channels, groups, cuda(torch, gamma), cuda(torch, beta), eps=1e-2, activation="relu")
+    done = norm.forward(d_x, keep_x=True)
+    y, _, _, tol = ref.forward(x, groups, gamma.astype(np.float64), beta.astype(np.float64), 1e-2, "relu", dtype == "fp32")
+    check(numbers(done.y).reshape(x.shape), y, tol, d_x.dtype, torch)
+    s = numbers(done.statistics)
+    for given, values in ((d_x, x), (done.x8, held_rows(x.reshape(-1, channels)).reshape(x.shape))):
+        dx, dg, db = norm.backward(d_dy, given, done.statistics)
+        want = ref.backward(dy, values, s[..., 0], s[..., 1], groups, gamma.astype(np.float64), beta.astype(np.float64), "relu", dtype == "fp32")
+        check(numbers(dx).reshape(x.shape), want[0], want[3], d_x.dtype, torch)
+        check(numbers(dg), want[1], want[4], torch.float32, torch)
+        check(numbers(db), want[2], want[5], torch.float32, torch)

@@ -119,3 +119,14 @@ def test_tensors_that_do_not_fit(lib, monkeypatch):
         B.GroupNorm(32, 4, activation="gelu")
     with pytest.raises(B.CrispError):
         B.GroupNorm(32, 5)
+
+
+def test_the_most_samples_and_pixels(lib):
+    n = C.c_size_t()
+    for backward in (0, 1):
+        for most, other in ((dict(batch=(1 << 31) - 1, pixels=1), "batch"), (dict(pixels=(1 << 31) - 65537, batch=1), "pixels")):
+            assert lib.crisp_group_norm_sizes(C.byref(desc(**most)), backward, C.byref(n)) == B.OK
+            most[other] += 1
+            assert lib.crisp_group_norm_sizes(C.byref(desc(**most)), backward, C.byref(n)) == B.UNSUPPORTED
+        for batch in (32767, 32768, 65536, 1 << 20):
+            assert lib.crisp_group_norm_sizes(C.byref(desc(batch=batch, pixels=1)), backward, C.byref(n)) == B.OK
