@@ -1070,9 +1070,15 @@ class HybridLayer:
         return dw
 
     def gradient_status(self) -> int:
-        """0, or TIMEOUT where a wait within a weight gradient ran out (its dW is not to be used).  Waits for all that runs on the device."""
+        """0, or TIMEOUT where a wait within a weight gradient has run out since reset_gradient_status was last called (that one's dW is not to be used).  Waits for
+        all that runs on the device."""
         self.torch.cuda.synchronize(self.device)
         return int(self._grad_status.item())
+
+    def reset_gradient_status(self, stream=None):
+        """gradient_status says 0 again, of the gradients that come behind this call on the stream."""
+        with self._on_device(), _allocating_for(stream):
+            self._grad_status.zero_()
 
     def set_epilogue8(self, bias=None, relu=False):
         """Y = act(W X + bias) for later 8-bit products; `bias` is an fp32 CUDA tensor [rows] that this object keeps."""

@@ -384,3 +384,25 @@ def test_one_tap_whose_last_block_is_not_whole(channels, batch, height, width, r
         assert np.all(numbers(dw)[~mask] == 3.0)
         assert bool((behind[rows:] == 7.0).all() and (behind[:, channels:] == 7.0).all() and (whole[:odd] == 7.0).all())
     assert L.gradient_status() == 0
+
+
+def test_the_layers_status_is_reset():
+    """A wait that ran out, written to the layer's own word: said until it is reset, and not of the gradients after that."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    x, dy = torch.randn(300, 256, device="cuda").bfloat16(), torch.randn(300, 128, device="cuda").bfloat16()
+    L, _ = layer(B, torch, 128, 256, mask=False)
+    act, dw = B.quantize8(x, tokens=True), torch.empty(128, 256, device="cuda")
+    g = B.WeightGrad8(128, 256, 300, None, dy.data_ptr(), 128, 1, 1, act.buffer.data_ptr(), None, dw.data_ptr(), 256, 0, 1, L._grad_status.data_ptr(), 2000000)
+    workspace = torch.empty(B.crisp_weight_grad8_sizes(g), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    for stream in (None, side, side.cuda_stream, 0):
+        B.crisp_weight_grad8(g, workspace)
+        assert L.gradient_status() == B.TIMEOUT
+        L.weight_gradient8(dy, act, tokens=True)
+        assert L.gradient_status() == B.TIMEOUT                              # (of the one before; whoever resets it knows of which)
+        L.reset_gradient_status(stream)
+        assert L.gradient_status() == 0
+        got = L.weight_gradient8(dy, act, tokens=True)
+        want = dy.double().t() @ act.dequantize(tokens=True).double()
+        assert L.gradient_status() == 0 and (got - want).abs().max().item() <= 1e-4 * want.abs().max().item()
