@@ -595,7 +595,7 @@ CRISP_API void crisp_destroy8(crisp_handle8_t h);
  *   d_act         the 8-bit form, of k (with conv: channels) and ncols (batch * height * width)
  *   mask          NULL: every weight's gradient, as a saliency or a straight-through step takes it.  A mask of rows x k: 0 outside it, and (blocks of 128 x 128; a convolution's
  *                 channels a multiple of 128) blocks that are not kept are not computed.
- *                 What is not finite in a column of X reaches all of its channel's and tap's weights; outside a mask it does not
+ *                 What is not finite in X reaches the weights of its channel (with conv: under the taps that cover its pixel) in every row; outside a mask it does not
  *   d_dw          [rows, k], ld_dw >= k, bf16 (dw_dtype 0) or fp32 (1); accumulate 1: added to what is there (outside a mask nothing is)
  *   d_status      a device word, or NULL: becomes CRISP_TIMEOUT if a wait within the kernel ran out (dW is not to be used then)
  *   d_workspace   crisp_weight_grad8_sizes bytes of the same arguments, 256-byte aligned; a call's own until it has run

@@ -32,6 +32,7 @@ constexpr uint32_t kABytes = 16384, kBoxBytes = 8192, kStage = kABytes + kBoxes 
 constexpr int kStages = 4;
 constexpr size_t kStaging = kDrain * 32 * 17 * 4;             // (16 columns of a warp's rows, where dW is not written in 16-byte pieces)
 constexpr size_t kGradSmem = kStages * kStage + 256 + kStaging + 1024;
+constexpr int kMaps = 16;                                     // tensor maps of x, at most
 
 struct Grad {
     int rows, channels, kernel_w, pad, linear;
@@ -39,6 +40,7 @@ struct Grad {
     int per, tiles_row, boxes, splits, items;                 // boxes a tile, tiles a row tile, boxes a row tile
     int tw, th, tb, nx, ny;                                   // pixels of a stage; boxes of them along a line, lines along an image
     int wo, ho;                                               // of dY (a linear layer: one line of tokens)
+    int narrow, low, width0, height0;                         // columns and lines of taps with a map of their own, and what the first ones' maps show of the images
     int chunks, chunks_split;
     const int32_t *blk_col;                                   // masks of 128 x 128: kept blocks of a row tile (else nullptr)
     int kkeep;
@@ -61,6 +63,23 @@ __device__ __forceinline__ BoxAt box_at(const Grad &p, int rt, int i) {
     if (p.linear) return {0, b * 64};
     const int tap = b / p.cboxes;
     return {tap, (b - tap * p.cboxes) * 64};
+}
+
+// Boxes of pixels run past the output's last column and line, where dY is zeros.  x there has to be zeros, too, and not what the images hold behind the last pixel that a tap covers: 0 times
+// NaN would reach a weight in whose sum that pixel is not.  So the taps left of (above) the last ones that end inside the padding have maps that show no more of the images than they cover,
+// the first tap width0 x height0 pixels, the next one a column (line) more.
+template <int kCount>
+struct MapsOfX { CUtensorMap of[kCount]; };
+
+// Box i as it is copied: its map, first column and shift.
+struct From { const CUtensorMap *map; int c, dx, dy; };
+template <int kCount>
+__device__ __forceinline__ From from_of(const Grad &p, const MapsOfX<kCount> &maps, const BoxAt &at) {
+    if (p.linear) return {&maps.of[0], at.c, 0, 0};
+    const int i = at.tap / p.kernel_w, j = at.tap - i * p.kernel_w;
+    if constexpr (kCount == 1) return {&maps.of[0], at.c, j - p.pad, i - p.pad};
+    const bool nothing = (j < p.narrow && p.width0 + j <= 0) || (i < p.low && p.height0 + i <= 0);
+    return {&maps.of[min(i, p.low) * (p.narrow + 1) + min(j, p.narrow)], nothing ? p.cboxes * 64 : at.c, j - p.pad, i - p.pad};
 }
 
 __device__ __forceinline__ uint32_t mask_bits(const Grad &p, int row, int col) {      // 32 columns from `col` on
@@ -242,9 +261,9 @@ __device__ __forceinline__ void zero_dropped(const Grad &p, int warp, int lane) 
             }
 }
 
-template <bool kAMn>
+template <bool kAMn, int kCount>
 __global__ void __launch_bounds__(kGradThreads, 1)
-grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Grad p) {
+grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ MapsOfX<kCount> maps, const __grid_constant__ Grad p) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = smem_u32(smem_raw), ring = (base + 1023u) & ~1023u, ctrl = ring + kStages * kStage;
     uint8_t *ctrl_gen = smem_raw + (ctrl - base);
@@ -258,7 +277,7 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
     }
     if (threadIdx.x == 0) {
         prefetch_tensormap(&map_a);
-        prefetch_tensormap(&map_b);
+        prefetch_tensormap(&maps.of[kCount == 1 ? 0 : (p.low + 1) * (p.narrow + 1) - 1]);
         for (int s = 0; s < kStages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, kDrain); }
         mbar_init(bar_done, 1);
@@ -281,14 +300,11 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
         bool ok = true;
         Walk w;
         for (w.enter(p, blockIdx.x); !w.over(p) && ok; w.enter(p, w.item + gridDim.x)) {
-            BoxAt box[kBoxes];
-            int dx[kBoxes], dy[kBoxes];
+            From box[kBoxes];
 #pragma unroll
             for (int i = 0; i < kBoxes; ++i) {
-                box[i] = {0, 0};
-                if (!rows && i < w.n) box[i] = box_at(p, w.rt, w.first + i);
-                dx[i] = dy[i] = 0;
-                if (!rows && !p.linear) { dy[i] = box[i].tap / p.kernel_w; dx[i] = box[i].tap - dy[i] * p.kernel_w - p.pad; dy[i] -= p.pad; }
+                box[i] = {nullptr, 0, 0, 0};
+                if (!rows && i < w.n) box[i] = from_of(p, maps, box_at(p, w.rt, w.first + i));
             }
             const uint32_t bytes = rows ? kABytes : w.n * kBoxBytes;
             const int row = w.rt * 128;
@@ -301,7 +317,7 @@ grad8_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ 
                         if (!rows) {
 #pragma unroll
                             for (int i = 0; i < kBoxes; ++i)
-                                if (i < w.n) tma_load_4d(dst + i * kBoxBytes, &map_b, box[i].c, at.x + dx[i], at.y + dy[i], at.z, full);
+                                if (i < w.n) tma_load_4d(dst + i * kBoxBytes, box[i].map, box[i].c, at.x + box[i].dx, at.y + box[i].dy, at.z, full);
                         } else if constexpr (kAMn) {
                             tma_load_4d(dst, &map_a, row, at.x, at.y, at.z, full);
                             tma_load_4d(dst + 8192, &map_a, row + 64, at.x, at.y, at.z, full);
@@ -434,9 +450,9 @@ __device__ __forceinline__ void tma_load_4d_pair(uint32_t dst, const CUtensorMap
 }
 
 // (p.tiles_row and p.per as for one CTA; Walk's row tiles are pairs of them)
-template <bool kAMn>
+template <bool kAMn, int kCount>
 __global__ void __launch_bounds__(kGradThreads, 1)
-grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ CUtensorMap map_b, const __grid_constant__ Grad p) {
+grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_constant__ MapsOfX<kCount> maps, const __grid_constant__ Grad p) {
     extern __shared__ uint8_t smem_raw[];
     const uint32_t base = smem_u32(smem_raw), ring = (base + 1023u) & ~1023u, ctrl = ring + kPairStages * kPairStage;
     uint8_t *ctrl_gen = smem_raw + (ctrl - base);
@@ -452,7 +468,7 @@ grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
     }
     if (threadIdx.x == 0) {
         prefetch_tensormap(&map_a);
-        prefetch_tensormap(&map_b);
+        prefetch_tensormap(&maps.of[kCount == 1 ? 0 : (p.low + 1) * (p.narrow + 1) - 1]);
         for (int s = 0; s < kPairStages; ++s) { mbar_init(bar_full + 8 * s, 2); mbar_init(bar_empty + 8 * s, 1); }
         for (int a = 0; a < 2; ++a) { mbar_init(bar_tfull + 8 * a, 1); mbar_init(bar_tempty + 8 * a, 2 * kDrain); }
         mbar_init(bar_done, 1);
@@ -478,15 +494,12 @@ grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
         Walk w;
         for (w.enter(p, item0); !w.over(p) && ok; w.enter(p, w.item + step)) {
             const int mine = (w.n + 1) / 2, row = (2 * w.rt + (int)rank) * 128;
-            BoxAt box[kBoxes / 2];
-            int dx[kBoxes / 2], dy[kBoxes / 2];
+            From box[kBoxes / 2];
 #pragma unroll
             for (int i = 0; i < kBoxes / 2; ++i) {
                 const int b = (int)rank * mine + i;
-                box[i] = {0, p.cboxes * 64};                  // (an odd number of boxes: the last one lies behind the last column and is zeros)
-                if (!rows && i < mine && b < w.n) box[i] = box_at(p, w.rt, w.first + b);
-                dx[i] = dy[i] = 0;
-                if (!rows && !p.linear) { dy[i] = box[i].tap / p.kernel_w; dx[i] = box[i].tap - dy[i] * p.kernel_w - p.pad; dy[i] -= p.pad; }
+                box[i] = {&maps.of[0], p.cboxes * 64, 0, 0};  // (an odd number of boxes: the last one lies behind the last column and is zeros)
+                if (!rows && i < mine && b < w.n) box[i] = from_of(p, maps, box_at(p, w.rt, w.first + b));
             }
             const uint32_t bytes = 2 * (rows ? kABytes : mine * kBoxBytes);
             Pixels at(p, w.c);
@@ -498,8 +511,8 @@ grad8_pair_kernel(const __grid_constant__ CUtensorMap map_a, const __grid_consta
                     if (rank == 0) mbar_expect_tx(bar_full + 8 * s, bytes);
                     if (fill != p.skip_fill) {
                         if (!rows) {
-                            tma_load_4d_pair(dst, &map_b, box[0].c, at.x + dx[0], at.y + dy[0], at.z, full);
-                            if (mine > 1) tma_load_4d_pair(dst + kBoxBytes, &map_b, box[1].c, at.x + dx[1], at.y + dy[1], at.z, full);
+                            tma_load_4d_pair(dst, box[0].map, box[0].c, at.x + box[0].dx, at.y + box[0].dy, at.z, full);
+                            if (mine > 1) tma_load_4d_pair(dst + kBoxBytes, box[1].map, box[1].c, at.x + box[1].dx, at.y + box[1].dy, at.z, full);
                         } else if constexpr (kAMn) {
                             tma_load_4d_pair(dst, &map_a, row, at.x, at.y, at.z, full);
                             tma_load_4d_pair(dst + 8192, &map_a, row + 64, at.x, at.y, at.z, full);
@@ -738,14 +751,17 @@ crisp_status_t plan_grad(const crisp_weight_grad8_t *g, GradPlan *G) {
         if ((double)c.batch * c.height * c.width > 2147418112.0) return CRISP_UNSUPPORTED;
         p.channels = c.channels; p.kernel_w = c.kernel_w; p.pad = c.pad;
         G->pixels = (int64_t)c.batch * c.height * c.width; G->batch = c.batch; G->ho = (int)ho; G->wo = (int)wo;
-        // the box of 64 output pixels that covers the fewest outside the images, the widest of them
+        // the box of 64 output pixels that covers the fewest outside the images, the widest of them.  (Kernels of many taps beside little padding have a box that ends with the lines or with
+        // the columns: it needs fewer maps, or none but one.)
+        const int left = std::max(0, c.kernel_w - 1 - c.pad), above = std::max(0, c.kernel_h - 1 - c.pad);
         int64_t best = -1;
         for (int tw = kStep; tw >= 1; tw >>= 1)
             for (int th = kStep / tw; th >= 1; th >>= 1) {
-                const int tb = kStep / tw / th;
+                const int tb = kStep / tw / th, narrow = wo % tw ? left : 0, low = ho % th ? above : 0;
                 const int64_t n = up(wo, tw) * up(ho, th) * up(c.batch, tb);
-                if (best < 0 || n < best) { best = n; p.tw = tw; p.th = th; p.tb = tb; }
+                if ((best < 0 || n < best) && (int64_t)(narrow + 1) * (low + 1) <= kMaps) { best = n; p.tw = tw; p.th = th; p.tb = tb; p.narrow = narrow; p.low = low; }
             }
+        p.width0 = (int)wo - c.pad; p.height0 = (int)ho - c.pad;
     }
     p.wo = G->wo; p.ho = G->ho;
     p.nx = (int)up(G->wo, p.tw); p.ny = (int)up(G->ho, p.th);
@@ -805,8 +821,8 @@ crisp_status_t plan_grad(const crisp_weight_grad8_t *g, GradPlan *G) {
     return CRISP_OK;
 }
 
-template <auto kernel>
-cudaError_t launch_grad(const CUtensorMap &a, const CUtensorMap &b, const Grad &p, size_t smem, unsigned cluster, int sms, int device, cudaStream_t st) {
+template <auto kernel, int kCount>
+cudaError_t launch_grad(const CUtensorMap &a, const MapsOfX<kCount> &b, const Grad &p, size_t smem, unsigned cluster, int sms, int device, cudaStream_t st) {
     static std::atomic<uint64_t> ready{0};                                    // (one a kernel: by device)
     if (device >= 64 || !(ready.load(std::memory_order_relaxed) >> device & 1)) {
         const cudaError_t e = cudaFuncSetAttribute(reinterpret_cast<const void *>(kernel), cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
@@ -814,6 +830,15 @@ cudaError_t launch_grad(const CUtensorMap &a, const CUtensorMap &b, const Grad &
         if (device < 64) ready.fetch_or(1ull << device, std::memory_order_relaxed);
     }
     return launch_clusters(kernel, cluster * (unsigned)std::min(std::max(p.items, 4 * p.zeros), sms / (int)cluster), kGradThreads, smem, st, cluster, a, b, p);
+}
+
+template <int kCount>
+cudaError_t launch_product(const GradPlan &G, const CUtensorMap &a, const MapsOfX<kCount> &b, int sms, int device, cudaStream_t st) {
+    if constexpr (kCount == 1)
+        if (G.k_major)
+            return G.pair ? launch_grad<grad8_pair_kernel<false, 1>>(a, b, G.p, kPairSmem, 2, sms, device, st) : launch_grad<grad8_kernel<false, 1>>(a, b, G.p, kGradSmem, 1, sms, device, st);
+    return G.pair ? launch_grad<grad8_pair_kernel<true, kCount>>(a, b, G.p, kPairSmem, 2, sms, device, st)
+                  : launch_grad<grad8_kernel<true, kCount>>(a, b, G.p, kGradSmem, 1, sms, device, st);
 }
 
 cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cudaStream_t st) {
@@ -855,11 +880,17 @@ cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cu
         if (e != cudaSuccess) return e;
         dy = to; ld = G.pitch;
     }
-    CUtensorMap a, b;
+    CUtensorMap a;
+    MapsOfX<kMaps> b;
     const uint64_t W = g.conv ? g.conv->width : g.ncols, H = g.conv ? g.conv->height : 1, N = G.batch;
     const uint32_t box[4] = {64u, (uint32_t)p.tw, (uint32_t)p.th, (uint32_t)p.tb};
-    const uint64_t xd[4] = {(uint64_t)p.channels, W, H, N}, xs[3] = {(uint64_t)G.cpitch * 2, W * G.cpitch * 2, W * H * G.cpitch * 2};
-    if (!make_map_4d(&b, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, x, xd, xs, box)) return cudaErrorInvalidValue;
+    const uint64_t xs[3] = {(uint64_t)G.cpitch * 2, W * G.cpitch * 2, W * H * G.cpitch * 2};
+    const int maps = (p.low + 1) * (p.narrow + 1);
+    for (int i = 0; i < maps; ++i) {
+        const int row = i / (p.narrow + 1), column = i - row * (p.narrow + 1);
+        const uint64_t xd[4] = {(uint64_t)p.channels, column < p.narrow ? (uint64_t)std::max(1, p.width0 + column) : W, row < p.low ? (uint64_t)std::max(1, p.height0 + row) : H, N};
+        if (!make_map_4d(&b.of[i], CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, x, xd, xs, box)) return cudaErrorInvalidValue;
+    }
     if (G.k_major) {
         if (!make_map_2d(&a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dy, (uint64_t)g.ncols, (uint64_t)p.rows, (uint64_t)ld, 64, 128)) return cudaErrorInvalidValue;
     } else {
@@ -867,10 +898,7 @@ cudaError_t run_grad(const crisp_weight_grad8_t &g, GradPlan &G, uint8_t *ws, cu
         if (!make_map_4d(&a, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 2, dy, yd, ys, box)) return cudaErrorInvalidValue;
     }
     const int sms = sm_count_of(device);
-    if (G.pair)
-        e = G.k_major ? launch_grad<grad8_pair_kernel<false>>(a, b, p, kPairSmem, 2, sms, device, st) : launch_grad<grad8_pair_kernel<true>>(a, b, p, kPairSmem, 2, sms, device, st);
-    else
-        e = G.k_major ? launch_grad<grad8_kernel<false>>(a, b, p, kGradSmem, 1, sms, device, st) : launch_grad<grad8_kernel<true>>(a, b, p, kGradSmem, 1, sms, device, st);
+    e = maps > 1 ? launch_product(G, a, b, sms, device, st) : launch_product(G, a, MapsOfX<1>{{b.of[0]}}, sms, device, st);
     if (e == cudaSuccess && p.splits > 1)
         e = launch_chained(add_parts_kernel, (unsigned)(G.nrt * p.tiles_row * 8 * p.per), 256, 0, st, p);
     return e;

@@ -406,3 +406,34 @@ def test_the_layers_status_is_reset():
         got = L.weight_gradient8(dy, act, tokens=True)
         want = dy.double().t() @ act.dequantize(tokens=True).double()
         assert L.gradient_status() == 0 and (got - want).abs().max().item() <= 1e-4 * want.abs().max().item()
+
+
+@pytest.mark.parametrize("batch,height,width,channels,rows,kh,kw,pad", [(1, 9, 11, 64, 64, 3, 3, 0), (2, 9, 11, 40, 130, 3, 3, 1), (3, 27, 31, 24, 40, 5, 5, 0), (1, 7, 5, 130, 2500, 3, 2, 1),
+                                                                        (1, 13, 13, 16, 32, 7, 7, 3), (2, 11, 9, 8, 16, 7, 7, 0), (1, 1, 2, 64, 64, 5, 5, 2), (1, 3, 70, 72, 9700, 1, 3, 0),
+                                                                        (1, 30, 1, 64, 64, 3, 1, 0), (4, 28, 28, 64, 64, 3, 3, 1), (2, 9, 11, 64, 64, 1, 1, 2)])
+def test_what_is_not_finite_at_pixels_that_a_tap_does_not_cover(batch, height, width, channels, rows, kh, kw, pad):
+    """NaN at the last column, the last line and the corners of the images: in the weights of the taps that come by there, and in no other, as the sum over output pixels has it."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    rng = np.random.default_rng(width)
+    xb, _ = inputs(rng, batch * height * width, 1, channels)
+    x = torch.from_numpy(values_of(xb)).view(batch, height, width, channels)
+    places = [(batch - 1, height - 1, width - 1, 0), (0, 0, width - 1, 1), (0, height - 1, 0, 2), (0, 0, 0, 3), (0, height // 2, max(width - 2, 0), 4), (batch - 1, max(height - 2, 0), width // 2, 5),
+              (0, height // 2, width // 2, 6)]
+    for p in places:
+        x[p] = float("nan")
+    act = B.quantize8(x.to("cuda", torch.bfloat16).view(-1, channels), tokens=True)
+    low, ho, wo = lowered(numbers(act.dequantize(tokens=True)).reshape(batch, height, width, channels), kh, kw, pad)
+    _, dyb = inputs(rng, batch * ho * wo, rows, 1)
+    dy = values_of(dyb)
+    bad = np.isnan(low).any(0)
+    low = np.where(bad, 0, low)
+    want, size = dy.T @ low, np.abs(dy).T @ np.abs(low)
+    L, mask = layer(B, torch, rows, kh * kw * channels, 2, 4, 128, 0.6, 2)
+    for masked in (False, True):
+        inside = mask if masked else np.ones_like(mask)
+        for f32 in (0, 1):
+            dw = numbers(L.weight_gradient8_conv(bf16_dev(dyb, torch).view(batch, ho, wo, rows), act, kh, kw, pad, dw_dtype=f32, masked=masked))
+            assert np.array_equal(np.isnan(dw), bad & inside)
+            check(np.where(bad, 0, dw), np.where(inside, want, 0), size * inside, batch * ho * wo, f32)
+    assert L.gradient_status() == 0
