@@ -240,25 +240,25 @@ __device__ __forceinline__ void zero_rows(uint8_t *to, int64_t pitch, int rows, 
 
 // Zeros in the blocks that are not kept, by `zero_warps` warps of every CTA.
 __device__ __forceinline__ void zero_dropped(const Grad &p, int warp, int lane) {
-            const int size = p.f32 ? 4 : 2;
-            for (int u = blockIdx.x + gridDim.x * warp; u < 4 * p.zeros; u += gridDim.x * p.zero_warps) {
-                // (32 rows of a block)
-                const int block = u >> 2, rt = block / p.zero_row, kb = block - rt * p.zero_row, row0 = rt * 128 + 32 * (u & 3), rows = min(32, p.rows - row0);
-                bool kept = false;
-                for (int i = lane; i < p.kkeep; i += 32) kept |= p.blk_col[(int64_t)rt * p.kkeep + i] == kb;
-                if (__any_sync(0xFFFFFFFFu, kept)) continue;
-                const int bytes = min(128, p.zero_k - kb * 128) * size, across = p.vec && bytes % 16 == 0 ? bytes / 16 : 0;
-                uint8_t *to = reinterpret_cast<uint8_t *>(p.dw) + ((int64_t)row0 * p.ld + kb * 128) * size;
-                const int64_t pitch = p.ld * size;
-                if (across && (across & (across - 1)) == 0) {
-                    const int at_once = 32 / across, first = lane / across;
-                    to += first * pitch + (lane & (across - 1)) * 16;
-    #pragma unroll 8
-                    for (int r = first; r < rows; r += at_once, to += at_once * pitch) *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
-                } else {
-                    zero_rows(to, pitch, rows, bytes, size, lane);
-                }
-            }
+    const int size = p.f32 ? 4 : 2;
+    for (int u = blockIdx.x + gridDim.x * warp; u < 4 * p.zeros; u += gridDim.x * p.zero_warps) {
+        // (32 rows of a block)
+        const int block = u >> 2, rt = block / p.zero_row, kb = block - rt * p.zero_row, row0 = rt * 128 + 32 * (u & 3), rows = min(32, p.rows - row0);
+        bool kept = false;
+        for (int i = lane; i < p.kkeep; i += 32) kept |= p.blk_col[(int64_t)rt * p.kkeep + i] == kb;
+        if (__any_sync(0xFFFFFFFFu, kept)) continue;
+        const int bytes = min(128, p.zero_k - kb * 128) * size, across = p.vec && bytes % 16 == 0 ? bytes / 16 : 0;
+        uint8_t *to = reinterpret_cast<uint8_t *>(p.dw) + ((int64_t)row0 * p.ld + kb * 128) * size;
+        const int64_t pitch = p.ld * size;
+        if (across && (across & (across - 1)) == 0) {
+            const int at_once = 32 / across, first = lane / across;
+            to += first * pitch + (lane & (across - 1)) * 16;
+#pragma unroll 8
+            for (int r = first; r < rows; r += at_once, to += at_once * pitch) *reinterpret_cast<uint4 *>(to) = make_uint4(0, 0, 0, 0);
+        } else {
+            zero_rows(to, pitch, rows, bytes, size, lane);
+        }
+    }
 }
 
 template <bool kAMn, int kCount>

@@ -410,7 +410,8 @@ def test_the_layers_status_is_reset():
 
 @pytest.mark.parametrize("batch,height,width,channels,rows,kh,kw,pad", [(1, 9, 11, 64, 64, 3, 3, 0), (2, 9, 11, 40, 130, 3, 3, 1), (3, 27, 31, 24, 40, 5, 5, 0), (1, 7, 5, 130, 2500, 3, 2, 1),
                                                                         (1, 13, 13, 16, 32, 7, 7, 3), (2, 11, 9, 8, 16, 7, 7, 0), (1, 1, 2, 64, 64, 5, 5, 2), (1, 3, 70, 72, 9700, 1, 3, 0),
-                                                                        (1, 30, 1, 64, 64, 3, 1, 0), (4, 28, 28, 64, 64, 3, 3, 1), (2, 9, 11, 64, 64, 1, 1, 2)])
+                                                                        (1, 30, 1, 64, 64, 3, 1, 0), (4, 28, 28, 64, 64, 3, 3, 1), (2, 9, 11, 64, 64, 1, 1, 2),
+                                                                                                                                                                (2, 9, 11, 128, 256, 3, 3, 1), (1, 10, 10, 64, 1300, 7, 7, 3)])
 def test_what_is_not_finite_at_pixels_that_a_tap_does_not_cover(batch, height, width, channels, rows, kh, kw, pad):
     """NaN at the last column, the last line and the corners of the images: in the weights of the taps that come by there, and in no other, as the sum over output pixels has it."""
     import torch
