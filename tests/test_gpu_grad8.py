@@ -438,3 +438,25 @@ def test_what_is_not_finite_at_pixels_that_a_tap_does_not_cover(batch, height, w
             assert np.array_equal(np.isnan(dw), bad & inside)
             check(np.where(bad, 0, dw), np.where(inside, want, 0), size * inside, batch * ho * wo, f32)
     assert L.gradient_status() == 0
+
+
+def test_a_layers_status_word_is_its_own():
+    """Layers are made without a launch each (their words come out of blocks), and a wait that ran out in one is not said of another."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    layers = [B.HybridLayer(128, 256, 4, 4, 128, 128, 1.0) for _ in range(200)]
+    assert len({L._grad_status.data_ptr() for L in layers}) == 200 and all(L.gradient_status() == 0 for L in layers)
+    x, dy = torch.randn(300, 256, device="cuda").bfloat16(), torch.randn(300, 128, device="cuda").bfloat16()
+    act, dw = B.quantize8(x, tokens=True), torch.empty(128, 256, device="cuda")
+    g = B.WeightGrad8(128, 256, 300, None, dy.data_ptr(), 128, 1, 1, act.buffer.data_ptr(), None, dw.data_ptr(), 256, 0, 1, layers[77]._grad_status.data_ptr(), 2000000)
+    B.crisp_weight_grad8(g, torch.empty(B.crisp_weight_grad8_sizes(g), dtype=torch.uint8, device="cuda"))
+    assert [i for i, L in enumerate(layers) if L.gradient_status()] == [77]
+    graph = torch.cuda.CUDAGraph()
+    B._status_words.clear()
+    with torch.cuda.graph(graph):                                            # (one that is made in a capture)
+        L = B.HybridLayer(128, 256, 4, 4, 128, 128, 1.0)
+        got = L.weight_gradient8(dy, act, tokens=True)
+    assert not B._status_words
+    other = B.HybridLayer(128, 256, 4, 4, 128, 128, 1.0)
+    graph.replay()
+    assert torch.equal(got, other.weight_gradient8(dy, act, tokens=True)) and L.gradient_status() == other.gradient_status() == 0
