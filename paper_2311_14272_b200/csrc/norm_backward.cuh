@@ -20,10 +20,10 @@ __device__ __forceinline__ void decode(uint32_t lo, uint32_t hi, uint32_t e, uin
     }
 }
 
-// A thread's coefficients of p = a x + b, and how near to a border of relu or relu6 p may be off.
-template <int P>
+// A thread's coefficients of p = a (x - mean) + b, and how near to a border of relu or relu6 p may be off.
+template <int P, bool kOne>
 struct Affine {
-    uint64_t a[P], b[P];
+    uint64_t away[kOne ? 1 : P], a[P], b[P];                 // away: less the means
     float near;
 };
 // Which side of the borders p lies on, from the formula in 64 bits: -1, 1 or 7.
@@ -31,15 +31,15 @@ __device__ __noinline__ float side_of(const Norm &q, int64_t stat, int c, float 
     const double exact = ((double)x - (double)q.stats[2 * stat]) * (double)q.stats[2 * stat + 1] * (q.gamma ? (double)q.gamma[c] : 1.0) + (q.beta ? (double)q.beta[c] : 0.0);
     return exact > 0.0 ? (exact >= 6.0 ? 7.f : 1.f) : -1.f;
 }
-// e = dy act'(p).  Where p is within its roundings of a border, its side is taken from 64 bits, so that it is the formula's: one element on the wrong side would be
-// wrong by all of its dy.
-template <int kAct, typename T, int P>
-__device__ __forceinline__ void slope(const Norm &q, int n, int ch, const Affine<P> &k, const uint64_t (&x)[P], uint64_t (&dy)[P]) {
+// e = dy act'(p), d = x - mean.  Where p is within its roundings of a border, its side is taken from 64 bits, so that it is the formula's: one element on the wrong side would be
+// wrong by all of its dy.  again(x): x once more.
+template <int kAct, typename T, int P, bool kOne, typename F>
+__device__ __forceinline__ void slope(const Norm &q, int n, int ch, const Affine<P, kOne> &k, const uint64_t (&d)[P], uint64_t (&dy)[P], F again) {
     if constexpr (kAct == kNone) return;
     if constexpr (kAct == kSilu) {
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint64_t p = fma2(x[j], k.a[j], k.b[j]);
+            const uint64_t p = fma2(d[j], k.a[j], k.b[j]);
             const uint64_t s = Of<T>::sigmoid2(p), rest = fma2(s, both(-1.f), both(1.f));
             dy[j] = mul2(dy[j], mul2(s, fma2(p, rest, both(1.f))));
         }
@@ -47,12 +47,14 @@ __device__ __forceinline__ void slope(const Norm &q, int n, int ch, const Affine
         float p[2 * P], least = INFINITY;                     // (three values a minimum)
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const float2 v = f32x2_halves(fma2(x[j], k.a[j], k.b[j]));
+            const float2 v = f32x2_halves(fma2(d[j], k.a[j], k.b[j]));
             p[2 * j] = v.x; p[2 * j + 1] = v.y;
             least = fminf(fminf(fabsf(v.x), fabsf(v.y)), least);
             if constexpr (kAct == kRelu6) least = fminf(fminf(fabsf(v.x - 6.f), fabsf(v.y - 6.f)), least);
         }
         if (least < k.near) {
+            uint64_t x[P];
+            again(x);
 #pragma unroll
             for (int j = 0; j < 2 * P; ++j) {
                 if (ch + j >= q.channels) break;
@@ -73,28 +75,28 @@ __device__ __forceinline__ void slope(const Norm &q, int n, int ch, const Affine
 }
 
 template <typename T, bool kOne>
-__device__ __forceinline__ void affine_of(const Norm &q, const Place &at, const Mine<T> &me, Affine<Of<T>::V / 2> *k, float (&mean)[kOne ? 1 : Of<T>::V],
-                                          float (&rstd)[kOne ? 1 : Of<T>::V]) {
+__device__ __forceinline__ void affine_of(const Norm &q, const Place &at, const Mine<T> &me, Affine<Of<T>::V / 2, kOne> *k, float (&rstd)[kOne ? 1 : Of<T>::V]) {
     constexpr int V = Of<T>::V;
     k->near = 0.f;
 #pragma unroll
     for (int j = 0; j < V; j += 2) {
-        float a[2] = {0.f, 0.f}, b[2] = {0.f, 0.f};
+        float mean[2] = {0.f, 0.f}, a[2] = {0.f, 0.f}, b[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int c = me.ch + j + i, m = kOne ? 0 : j + i;
-            if (!kOne || j + i == 0) mean[m] = rstd[m] = 0.f;
+            if (!kOne || j + i == 0) rstd[m] = 0.f;
             if (j + i >= me.n) continue;
             if (!kOne || j + i == 0) {
                 const float2 s = *reinterpret_cast<const float2 *>(q.stats + 2 * ((int64_t)at.n * q.groups + group_of(q, c)));
-                mean[m] = s.x; rstd[m] = s.y;
+                mean[i] = s.x; rstd[m] = s.y;
             }
-            const float beta = q.beta ? q.beta[c] : 0.f;
             a[i] = rstd[m] * (q.gamma ? q.gamma[c] : 1.f);
-            b[i] = fmaf(-mean[m], a[i], beta);
-            // a and b are off by u of a x, of mean a and of b, p by one more of its own (u = 2^-24); at a border |a x| <= |b| + 6
-            k->near = fmaxf(k->near, (fabsf(beta) + 2.f * fabsf(mean[m] * a[i]) + 2.f * fabsf(b[i]) + 16.f) * 0x1p-22f);
+            b[i] = q.beta ? q.beta[c] : 0.f;
+            // a and x - mean are each off by u (2^-24), p by one more of its own; at a border |a (x - mean)| <= |b| + 6
+            k->near = fmaxf(k->near, (fabsf(b[i]) + 8.f) * 0x1p-22f);
         }
+        if constexpr (kOne) { if (j == 0) k->away[0] = both(-mean[0]); }
+        else k->away[j / 2] = f32x2(-mean[0], -mean[1]);
         k->a[j / 2] = f32x2(a[0], a[1]); k->b[j / 2] = f32x2(b[0], b[1]);
     }
 }
@@ -135,6 +137,9 @@ struct Reader {
     }
     static __device__ __forceinline__ void open(const Item &r, uint64_t (&d)[V / 2], uint64_t (&f)[V / 2]) {
         Of<T>::open(r.dy, d);
+        open_x(r, f);
+    }
+    static __device__ __forceinline__ void open_x(const Item &r, uint64_t (&f)[V / 2]) {
         if constexpr (k8) decode<V>(r.x.x, r.x.y, r.x.z & 0xFFu, f);
         else Of<T>::open(r.x, f);
     }
@@ -153,26 +158,24 @@ __device__ __forceinline__ void with_act(int act, F f) {
 template <typename T, bool kOne, bool k8, bool kVec, bool kOver, typename K, typename F>
 __device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine<T> &me, float2 *channels, K &items, F give) {
     constexpr int V = Of<T>::V, P = V / 2, M = kOne ? 1 : V;
-    Affine<P> k;
-    float mean[M], rstd[M];
-    affine_of<T, kOne>(q, at, me, &k, mean, rstd);
-    uint64_t r[kOne ? 1 : P], s[kOne ? 1 : P], db[P], dg[P]; // h = r x + s
-#pragma unroll
-    for (int j = 0; j < (kOne ? 1 : P); ++j) {
-        const float r0 = rstd[kOne ? 0 : 2 * j], r1 = rstd[kOne ? 0 : 2 * j + 1];
-        r[j] = f32x2(r0, r1); s[j] = f32x2(-mean[kOne ? 0 : 2 * j] * r0, -mean[kOne ? 0 : 2 * j + 1] * r1);
-    }
+    Affine<P, kOne> k;
+    float rstd[M];
+    affine_of<T, kOne>(q, at, me, &k, rstd);
+    uint64_t db[P], dg[P];                                   // dg: of e (x - mean)
 #pragma unroll
     for (int j = 0; j < P; ++j) db[j] = dg[j] = 0;
     if (me.n > 0)
         with_act(q.act, [&](auto act) {
 #pragma unroll 1
             for (int i = 0; i < me.items; ++i) {
-                uint64_t d[P], x[P];
-                Reader<T, k8, kVec>::open(items.next(), d, x);
-                slope<decltype(act)::value, T, P>(q, at.n, me.ch, k, x, d);
+                uint64_t e[P], d[P];
+                const Item item = items.next();
+                Reader<T, k8, kVec>::open(item, e, d);
 #pragma unroll
-                for (int j = 0; j < P; ++j) { db[j] = add2(db[j], d[j]); dg[j] = fma2(d[j], fma2(x[j], r[kOne ? 0 : j], s[kOne ? 0 : j]), dg[j]); }
+                for (int j = 0; j < P; ++j) d[j] = add2(d[j], k.away[kOne ? 0 : j]);
+                slope<decltype(act)::value, T, P, kOne>(q, at.n, me.ch, k, d, e, [&](uint64_t (&x)[P]) { Reader<T, k8, kVec>::open_x(item, x); });
+#pragma unroll
+                for (int j = 0; j < P; ++j) { db[j] = add2(db[j], e[j]); dg[j] = fma2(e[j], d[j], dg[j]); }
                 items.done();
             }
         });
@@ -182,8 +185,8 @@ __device__ __forceinline__ void sum_e(const Norm &q, const Place &at, const Mine
 #pragma unroll
         for (int j = 0; j < P; ++j) {
             const float2 b = f32x2_halves(db[j]), g = f32x2_halves(dg[j]);
-            channels[me.lane * row + me.v * V + 2 * j] = make_float2(b.x, g.x);
-            channels[me.lane * row + me.v * V + 2 * j + 1] = make_float2(b.y, g.y);
+            channels[me.lane * row + me.v * V + 2 * j] = make_float2(b.x, g.x * rstd[kOne ? 0 : 2 * j]);
+            channels[me.lane * row + me.v * V + 2 * j + 1] = make_float2(b.y, g.y * rstd[kOne ? 0 : 2 * j + 1]);
         }
     }
     __syncthreads();
@@ -217,14 +220,14 @@ __device__ __forceinline__ float2 combine_e(const Norm &q, int k, int lane, int 
     return make_float2(shared_sum(t.x, k) / all, shared_sum(t.y, k) / all);
 }
 
-// dx of the CTA's pixels (kDown: the last one first); known(g): m1 and m2 of the sample's group g.  dx = rstd (gamma e - m1 - h m2) = a e + B x + C.
+// dx of the CTA's pixels (kDown: the last one first); known(g): m1 and m2 of the sample's group g.  dx = rstd (gamma e - m1 - h m2) = a e + B (x - mean) + C.
 template <typename T, bool kOne, bool k8, bool kVec, bool kDown, typename K, typename F>
 __device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const Mine<T> &me, K &items, F known) {
     constexpr int V = Of<T>::V, P = V / 2, M = kOne ? 1 : V;
     if (me.n <= 0) return;
-    Affine<P> k;
-    float mean[M], rstd[M];
-    affine_of<T, kOne>(q, at, me, &k, mean, rstd);
+    Affine<P, kOne> k;
+    float rstd[M];
+    affine_of<T, kOne>(q, at, me, &k, rstd);
     uint64_t B[kOne ? 1 : P], C[kOne ? 1 : P];
 #pragma unroll
     for (int j = 0; j < (kOne ? 1 : P); ++j) {
@@ -234,7 +237,7 @@ __device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const 
             const int m = kOne ? 0 : 2 * j + i;
             const float2 g = m < me.n ? known(group_of(q, me.ch + m)) : make_float2(0.f, 0.f);
             b[i] = -rstd[m] * rstd[m] * g.y;
-            c[i] = -fmaf(b[i], mean[m], rstd[m] * g.x);
+            c[i] = -rstd[m] * g.x;
         }
         B[j] = f32x2(b[0], b[1]); C[j] = f32x2(c[0], c[1]);
     }
@@ -245,13 +248,16 @@ __device__ __forceinline__ void finish_dx(const Norm &q, const Place &at, const 
         if (kDown) dx += (me.items - 1) * step_out;
 #pragma unroll 1
         for (int i = 0; i < me.items; ++i, dx += move) {
-            uint64_t d[P], x[P];
-            Reader<T, k8, kVec>::open(items.next(), d, x);
-            slope<decltype(act)::value, T, P>(q, at.n, me.ch, k, x, d);
+            uint64_t e[P], d[P];
+            const Item item = items.next();
+            Reader<T, k8, kVec>::open(item, e, d);
 #pragma unroll
-            for (int j = 0; j < P; ++j) d[j] = fma2(d[j], k.a[j], fma2(x[j], B[kOne ? 0 : j], C[kOne ? 0 : j]));
+            for (int j = 0; j < P; ++j) d[j] = add2(d[j], k.away[kOne ? 0 : j]);
+            slope<decltype(act)::value, T, P, kOne>(q, at.n, me.ch, k, d, e, [&](uint64_t (&x)[P]) { Reader<T, k8, kVec>::open_x(item, x); });
+#pragma unroll
+            for (int j = 0; j < P; ++j) e[j] = fma2(e[j], k.a[j], fma2(d[j], B[kOne ? 0 : j], C[kOne ? 0 : j]));
             items.done();
-            put<kVec>(dx, Of<T>::close(d), q.vec_out, me.n);
+            put<kVec>(dx, Of<T>::close(e), q.vec_out, me.n);
         }
     });
 }

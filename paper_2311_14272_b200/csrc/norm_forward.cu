@@ -181,20 +181,21 @@ __device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, I &it
     constexpr int V = Of<T>::V, P = V / 2;
     // (threads behind the last channel write the zeros that its block ends with; not of a block in which there is none)
     if (me.lane >= q.lanes || !(me.n > 0 || (kHold && (me.ch & ~127) < q.channels))) return;
-    uint64_t a[P], b[P];
+    uint64_t away[P], a[P], b[P];                            // p = a (x - mean) + beta
 #pragma unroll
     for (int j = 0; j < P; ++j) {
-        float s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
+        float m[2] = {0.f, 0.f}, s[2] = {0.f, 0.f}, t[2] = {0.f, 0.f};
 #pragma unroll
         for (int i = 0; i < 2; ++i) {
             const int c = me.ch + 2 * j + i;
             if ((kVec && !kHold) || 2 * j + i < me.n) {
                 const float2 k = known(group_of(q, c));
+                m[i] = -k.x;
                 s[i] = k.y * (q.gamma ? q.gamma[c] : 1.f);
-                t[i] = fmaf(-k.x, s[i], q.beta ? q.beta[c] : 0.f);
+                t[i] = q.beta ? q.beta[c] : 0.f;
             }
         }
-        a[j] = f32x2(s[0], s[1]); b[j] = f32x2(t[0], t[1]);
+        away[j] = f32x2(m[0], m[1]); a[j] = f32x2(s[0], s[1]); b[j] = f32x2(t[0], t[1]);
     }
     T *y = reinterpret_cast<T *>(q.out) + me.row0 * q.ld_out + me.ch;
     const int64_t step_y = (int64_t)q.lanes * q.ld_out;
@@ -208,7 +209,7 @@ __device__ __forceinline__ void finish_y(const Norm &q, const Mine<T> &me, I &it
             Of<T>::open(!kHold || me.n > 0 ? items.next() : make_uint4(0, 0, 0, 0), f);
             if constexpr (kHold) if (q.x8) hold<V>(q, q.x8, f, col, me.ch);
 #pragma unroll
-            for (int j = 0; j < P; ++j) f[j] = activate<decltype(act)::value, T>(fma2(f[j], a[j], b[j]));      // (0 behind the last channel: a = b = 0)
+            for (int j = 0; j < P; ++j) f[j] = activate<decltype(act)::value, T>(fma2(add2(f[j], away[j]), a[j], b[j]));      // (0 behind the last channel)
             if constexpr (kHold) if (q.y8) hold<V>(q, q.y8, f, col, me.ch);
             items.done();
             if (!kHold || (q.out && me.n > 0)) put<kVec && !kHold>(y, Of<T>::close(f), q.vec_out, me.n);

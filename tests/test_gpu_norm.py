@@ -398,3 +398,42 @@ def test_many_samples(shape, groups, dtype):
         check(numbers(dx).reshape(x.shape), want[0], want[3], d_x.dtype, torch)
         check(numbers(dg), want[1], want[4], torch.float32, torch)
         check(numbers(db), want[2], want[5], torch.float32, torch)
+
+
+@pytest.mark.parametrize("size", [(2, 1, 768, 64), (2, 300, 64, 8), (1, 40, 100, 25), (1, 70000, 96, 32), (3, 25000, 64, 4)])
+@pytest.mark.parametrize("dtype", TYPES)
+def test_a_mean_that_is_many_deviations_from_zero(size, dtype):
+    """Values about 3000, and groups of one value: results are the formula's at the statistics that the call itself leaves, with x - mean rounded once, not with roundings of mean times
+    gamma / deviation (a group of -700 was off by 0.02 where y is the bias)."""
+    import torch
+    from paper_2311_14272_b200 import binding as B
+    batch, pixels, channels, groups = size
+    T = kind(torch, dtype)
+    for i, act in enumerate(ACTS):
+        x, gamma, beta, dy = inputs(torch, *size, seed=i)
+        x += 3000
+        ref.grouped(x, groups)[0, :, ::2] = -700
+        ref.grouped(x, groups)[0, :, ::4] = 0.1
+        d_x, d_dy = cuda(torch, x).to(T), cuda(torch, dy).to(T)
+        x, dy = numbers(d_x), numbers(d_dy)
+        norm = B.GroupNorm(channels, groups, cuda(torch, gamma), cuda(torch, beta), activation=act)
+        done = norm.forward(d_x)
+        s = numbers(done.statistics)
+        about = x - ref.spread(s[..., 0], channels)                           # (exact in 64 bits)
+        h = about * ref.spread(s[..., 1], channels)
+        p = gamma * h + beta
+        y = ref.act(p, act)
+        # x - mean, gamma / deviation and the sum are rounded; the sigmoid as norm_reference.py has it
+        tol = ref.U * (3 * np.abs(gamma * h) + np.abs(p) + np.abs(beta))
+        if act == "silu":
+            tol = 1.2 * tol + (8 * ref.U if dtype == "fp32" else 2.0**-19) * np.abs(y)
+        check(numbers(done.y), y, tol, T, torch)
+        same = np.broadcast_to(ref.spread(np.ptp(ref.grouped(x, groups), axis=(1, 3)) == 0, channels), x.shape)
+        assert same.any()
+        if act == "none" and dtype == "fp32":
+            assert np.array_equal(numbers(done.y)[same], np.broadcast_to(beta, x.shape)[same])
+        got = norm.backward(d_dy, d_x, done.statistics)
+        want = ref.backward(dy, about, 0 * s[..., 0], s[..., 1], groups, gamma.astype(np.float64), beta.astype(np.float64), act, dtype == "fp32")
+        check(numbers(got[0]), want[0], want[3], T, torch)
+        check(numbers(got[1]), want[1], want[4], torch.float32, torch)
+        check(numbers(got[2]), want[2], want[5], torch.float32, torch)
