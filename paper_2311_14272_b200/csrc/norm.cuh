@@ -11,8 +11,8 @@
 //   large ones    two kernels of as many CTAs as fit, each with its part of the pixels.  The second goes over them backwards: what the first read last
 //                 is still in L2 (forward, us, backwards and not: 32 x 112 x 112 x 96, 77 MB, 38 and 42; of 50 MB 25 and 24; of 200 MB 115 and 116)
 //
-// A thread holds V = 16 bytes' worth of consecutive channels and goes over pixels, two channels an instruction: per pair p = a x + b (a = gamma rstd, b = beta - mean a),
-// dx = a e + B x + C.  Forward sums are about the thread's first value, and then about its mean so far, so that neither a mean far from zero nor single
+// A thread holds V = 16 bytes' worth of consecutive channels and goes over pixels, two channels an instruction: per pair p = a (x - mean) + beta (a = gamma rstd),
+// dx = a e + B (x - mean) + C.  (With a x + (beta - mean a), an addition less, mean a is rounded: equal values of -700 gave y off by 0.016; the times are the same.)  Forward sums are about the thread's first value, and then about its mean so far, so that neither a mean far from zero nor single
 // values far from the mean cost digits; then mean = sum n_i mean_i / n and M2 = sum M2_i + n_i (mean_i - mean)^2 over threads and over CTAs, always in the same order.
 #pragma once
 

@@ -47,26 +47,26 @@ struct KeptX {
 };
 
 __device__ __forceinline__ uint64_t minus(uint64_t a) { return mul2(a, f32x2(-1.f, -1.f)); }
-// A thread's sums of `count` items (values less a point, and their squares) about the mean so far.  Done after 1, 4, 16 ... items: those that follow, three times as many, add 3 count d^2 for
-// the distance d of their mean from that one, of which 3/4 count d^2 is theirs to add, so that no more than four times a sum is added and taken away again (eight times in a first item of eight
-// channels), wherever the values lie that are far from the others.  (About the first value all along: a first one of 1000, and 240 others of size one, left 1e-4 of the variance wrong.)
+// A thread's sums of `count` items (values less a point, and their squares) about the mean so far; over = 1 / count.  Done after 1, 4, 16 ... items: those that follow, three times as many, add
+// 3 count d^2 for the distance d of their mean from that one, of which 3/4 count d^2 is theirs to add, so that no more than four times a sum is added and taken away again (eight times in a first
+// item of eight channels), wherever the values lie that are far from the others.  (About the first value all along: a first one of 1000, and 240 others of size one, left 1e-4 of the variance wrong.)
 template <int V, bool kOne>
-__device__ __forceinline__ void about_mean(int count, uint64_t (&away)[kOne ? 1 : V / 2], uint64_t (&s1)[V / 2], uint64_t (&s2)[V / 2]) {
+__device__ __forceinline__ void about_mean(int count, float over, uint64_t (&away)[kOne ? 1 : V / 2], uint64_t (&s1)[V / 2], uint64_t (&s2)[V / 2]) {
     constexpr int P = V / 2;
     if constexpr (kOne) {
         const float one = f32x2_sum(P == 4 ? add2(add2(s1[0], s1[1]), add2(s1[P - 2], s1[P - 1])) : add2(s1[0], s1[1]));
         const float two = f32x2_sum(P == 4 ? add2(add2(s2[0], s2[1]), add2(s2[P - 2], s2[P - 1])) : add2(s2[0], s2[1]));
-        const float old = f32x2_halves(away[0]).x, n = (float)count * V, point = old - one / n, by = old - point, rest = fmaf(-n, by, one);
+        const float old = f32x2_halves(away[0]).x, n = (float)count * V, point = fmaf(one, -over / V, old), by = old - point, rest = fmaf(-n, by, one);
         away[0] = both(point);
 #pragma unroll
         for (int j = 0; j < P; ++j) s1[j] = s2[j] = 0;
         s1[0] = f32x2(rest, 0.f);
         s2[0] = f32x2(fmaf(-by, one + rest, two), 0.f);      // sum (v - by)^2 = sum v^2 - by (sum v + sum (v - by))
     } else {
-        const uint64_t n = both(-(float)count), over = both(-1.f / (float)count);
+        const uint64_t n = both(-(float)count), less = both(-over);
 #pragma unroll
         for (int j = 0; j < P; ++j) {
-            const uint64_t old = away[j], by = add2(old, minus(away[j] = fma2(s1[j], over, old))), one = s1[j];
+            const uint64_t old = away[j], by = add2(old, minus(away[j] = fma2(s1[j], less, old))), one = s1[j];
             s1[j] = fma2(n, by, one);
             s2[j] = fma2(minus(by), add2(one, s1[j]), s2[j]);
         }
@@ -87,7 +87,8 @@ __device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine
         Of<T>::open(u, f);
 #pragma unroll
         for (int j = 0; j < (kOne ? 1 : P); ++j) { const float2 v = f32x2_halves(f[j]); away[j] = f32x2(-v.x, kOne ? -v.x : -v.y); }
-        for (int i = 0, until = 1;; until *= 4) {
+        float over = 1.f;
+        for (int i = 0, until = 1;; until *= 4, over *= 0.25f) {
             const int end = min(until, me.items);
 #pragma unroll 2
             for (;;) {
@@ -99,7 +100,7 @@ __device__ __forceinline__ void sum_x(const Norm &q, const Place &at, const Mine
                 u = items.next();
             }
             if (i >= me.items) break;
-            about_mean<V, kOne>(i, away, s1, s2);
+            about_mean<V, kOne>(i, over, away, s1, s2);
             u = items.next();
         }
     }
