@@ -532,8 +532,8 @@ CRISP_API crisp_status_t crisp_spmm8_quantized(crisp_handle8_t h, const void *d_
                                                int32_t y_dtype, void *stream);
 
 /*
- * Group norm with an activation over channels-last activations, which stands between the pruned layers of a network (the paper's networks normalise after each
- * convolution; it gives no formula of its own).  Of each sample's groups (pixels x channels / groups values):
+ * Group norm with an activation over channels-last activations, between the pruned layers of a network that is fine-tuned in small batches (the paper gives no
+ * formula for it).  Of each sample's groups (pixels x channels / groups values):
  *
  *   h = (x - mean) * rstd,  rstd = 1 / sqrt(var + eps)        y = act(p),  p = gamma * h + beta      (per channel)
  *   e = dy * act'(p)     dbeta = sum e     dgamma = sum e * h     dx = rstd * (gamma * e - m1 - h * m2),   m1, m2: the group's means of gamma * e and gamma * e * h

@@ -321,7 +321,7 @@ sum_rows_kernel(const float *sums, int64_t rows, int channels, float *dgamma, fl
 bool aligned_to(const void *p, size_t a) { return (reinterpret_cast<uintptr_t>(p) % a) == 0; }
 
 constexpr int kSms = 148;
-// Small calls: those that read at most so much (dy, too).  Device times of one kernel with clusters and of two, us: forward 1 x 28 x 28 x 512 (0.8 MB) 7.4 and 8.3, 8 images (6.4 MB)
+// Small calls: those that read at most so much (dy, too); above that either form can be ahead, by the shape.  Device times of one kernel with clusters and of two, us: forward 1 x 28 x 28 x 512 (0.8 MB) 7.4 and 8.3, 8 images (6.4 MB)
 // 7.9 and 12.0, 32 images (25.7 MB) 11.4 and 15.9, 48 images 18.3 and 19.5, 16 x 112 x 112 x 96 (38.5 MB) 34.9 and 22.0; backward 8 x 14 x 14 x 512 (3.2 MB) 9.1 and 12.2, 8 x 28 x 28 x 256
 // (6.4 MB) 11.4 and 13.8, 4 x 56 x 56 x 256 (12.8 MB) 20.2 and 15.6, 24 x 28 x 28 x 512 (38.5 MB) 28.9 and 22.2.
 constexpr int64_t kSmallForward = 28 << 20, kSmallBackward = 8 << 20;
